@@ -2,8 +2,8 @@
 
 A round of speculative decoding over tokens appends the window's keys and values to a
 cache held in 8 bits (``api.cache_append``), attends over it (``api.cache_attend``), scores
-tokens under the logits (``api.token_scores``, with ``api.token_scores_grad`` where the model
-is trained on them) and verifies the drafted window (``api.token_verify``).  ``run`` makes
+tokens under the logits (``api.token_scores``; ``api.token_scores_train`` with the gradient, where
+the model is trained on them) and verifies the drafted window (``api.token_verify``).  ``run`` makes
 those calls where ``own`` is true and computes the same in elementary torch operations
 elsewhere; ``exact`` restates the definitions in 64 bits.
 
@@ -391,9 +391,8 @@ def _own(st):
         names = ["logprob", "entropy", "row_max", "log_sum"] + (["top_ids", "top_logprob"] if st["top_k"] else [])
         return {k: r[k] for k in names}
     if kind == "train":
-        r = api.token_scores(st["logits"], st["tokens"])
-        dx = api.token_scores_grad(st["logits"], st["tokens"], r, st["g_logprob"], st["g_entropy"])
-        return dict(logprob=r["logprob"], entropy=r["entropy"], d_logits=dx)
+        r = api.token_scores_train(st["logits"], st["tokens"], st["g_logprob"], st["g_entropy"])
+        return {k: r[k] for k in ("logprob", "entropy", "d_logits")}
     if kind == "verify":
         r = api.token_verify(st["target"], st["draft"], st["tokens"], mode=st["mode"], temperature=st["temperature"],
                              L_eff=st["L_eff"], coins=st["coins"], race=st["race"])
