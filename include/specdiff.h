@@ -390,6 +390,156 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
                   float comp_var, int K, float churn, float beta_min, float beta_max,
                   float t_floor, uint64_t seed, float *y_out, sdv_stream_t stream);
 
+/* ---- speculative decoding over tokens ---------------------------------------
+ *
+ * The same verification step for a token model: the window's keys and values go into a
+ * cache held in 8 bits (sdv_cache_append), the target attends over it for all positions at
+ * once (sdv_cache_attend), the drafted tokens are scored under its logits (sdv_token_scores;
+ * with gradients, sdv_token_scores_train) and verified (sdv_token_verify: Algorithms
+ * token-/block-verification with distributions over V tokens in place of Gaussian kernels).
+ * The conventions above hold, but that logits, keys, values and queries are strided: strides
+ * are in elements, the last axis is contiguous.  Arithmetic is fp32.
+ */
+#define SDV_F16 2              /* float16, in these entry points only */
+
+/* further status bits */
+#define SDV_STATUS_EMPTY_ROW  8u   /* a row of logits with nothing but -inf */
+#define SDV_STATUS_BAD_TOKEN 16u   /* a token outside [0, V) */
+#define SDV_STATUS_BAD_PAGE  32u   /* a page outside the cache, or a token past the page table */
+
+#define SDV_MAX_TOP   32       /* largest number of alternatives */
+#define SDV_MAX_BLOCK 128      /* largest number of tokens of a cache page (a multiple of 16) */
+
+/*
+ * sdv_token_scores - for each of N rows of logits x (row n at logits + n row_stride elements,
+ * V of them), with m = max x, d_v = (x_v - m)/temperature and s = sum e^{d_v}:
+ *   logprob[n]  = d_t - log s of the token t = tokens[n]; 0 for t = -1 (no token)
+ *   entropy[n]  = log s - sum p_v d_v, p_v = e^{d_v} / s
+ *   row_max[n]  = m,  log_sum[n] = log s
+ *   top_ids, top_logprob [N, top_k]: the top_k largest logits' indices, the larger first and
+ *     of equal ones the lower index, and their log probabilities; -1 and -inf past the
+ *     row's unmasked logits
+ * A logit of -inf is masked: probability 0.  A row without any other has row_max, log_sum and
+ * logprob -inf, entropy 0 (SDV_STATUS_EMPTY_ROW); one with a NaN or +inf has NaN everywhere and
+ * no alternatives (SDV_STATUS_NONFINITE).  A token outside [0, V) other than -1 has NaN
+ * (SDV_STATUS_BAD_TOKEN).
+ *   dtype SDV_F32, SDV_BF16 or SDV_F16; N >= 0 (0: nothing is done), V >= 1,
+ *   0 <= top_k <= min(V, SDV_MAX_TOP), temperature > 0, row_stride >= V
+ *   tokens and logprob may both be NULL, and each other output (not all); status [N] uint32
+ */
+int sdv_token_scores(const void *logits, int64_t row_stride, int N, int V, int dtype,
+                     const int32_t *tokens, float temperature, int top_k, float *logprob,
+                     float *entropy, float *row_max, float *log_sum, int32_t *top_ids,
+                     float *top_logprob, uint32_t *status, sdv_stream_t stream);
+
+/*
+ * sdv_token_scores_grad - the gradient of sum_n g_logprob[n] logprob[n] + g_entropy[n] entropy[n]
+ * with respect to the logits, from the row_max, log_sum (and entropy, where g_entropy is given)
+ * of sdv_token_scores:
+ *   d_v = (1/temperature) [g_lp (1[v = t] - p_v) - g_H p_v (log p_v + entropy)]
+ * g_logprob (then tokens too) or g_entropy may be NULL, not both.  Masked logits and empty rows
+ * get 0, rows with a NaN or +inf NaN; a row whose token is -1 or outside [0, V) has no part from
+ * g_logprob.  d_logits (`dtype`, rows d_stride elements apart) may be the logits themselves,
+ * with their stride.
+ */
+int sdv_token_scores_grad(const void *logits, int64_t row_stride, int N, int V, int dtype,
+                          const int32_t *tokens, float temperature, const float *row_max,
+                          const float *log_sum, const float *entropy, const float *g_logprob,
+                          const float *g_entropy, void *d_logits, int64_t d_stride,
+                          sdv_stream_t stream);
+
+/*
+ * sdv_token_scores_train - both: the scores and, from given upstream gradients, the gradient, with
+ * the logits read once (rows of up to 512 KB; longer ones are read twice).  entropy, row_max
+ * and log_sum are required; the rest as above.
+ */
+int sdv_token_scores_train(const void *logits, int64_t row_stride, int N, int V, int dtype,
+                           const int32_t *tokens, float temperature, const float *g_logprob,
+                           const float *g_entropy, float *logprob, float *entropy, float *row_max,
+                           float *log_sum, uint32_t *status, void *d_logits, int64_t d_stride,
+                           sdv_stream_t stream);
+
+/*
+ * sdv_token_verify - verification of L drafted tokens of B chains and each chain's next token.
+ * With q_j = softmax(target row j / temperature), p_j = softmax(draft row j /
+ * draft_temperature), t_j = tokens[b, j] and n the chain's window:
+ *   ell_j = log q_j(t_j) - log p_j(t_j)
+ *   sample: accepted = the tokens before the first eta_j >= e^ell_j
+ *   block:  log alpha_{j+1} = min{0, log alpha_j + ell_j}, alpha_0 = 1;
+ *           v_j = sum_v max{0, alpha_j q_j(v) - p_j(v)}, h_j = v_j / (v_j + 1 - alpha_j) for
+ *           0 < j < n, h_n = alpha_n; accepted = max{j : eta_{j-1} < h_j}, or 0
+ *   next token: from max{0, alpha q_a(v) - p_a(v)}, normalised, with a = accepted < n and
+ *           alpha = alpha_a (1 in sample mode); from q_n on full accept.  It is the index of the
+ *           largest r_v / E_v, the lower of equal ones, for that (unnormalised) r and
+ *           exponential variates E_v.
+ *   target : [B, L + 1, V] rows at b target_stride_b + j target_stride_row; draft [B, L, V]
+ *   tokens [B, L] int32; L_eff [B] int32 or NULL: windows n <= L; n = 0 draws from target row 0,
+ *     n < 0 marks an inactive chain (accepted_len 0, next_token -1)
+ *   coins  [B, L] fp32 in [0, 1) or NULL: eta; NULL draws them as sdv_verify does
+ *   race   [B, V] fp32 > 0 or NULL: E; NULL takes -log(uniform) of Philox counter
+ *     (b, v/4, 7, 0), word v % 4
+ *   accepted_len, next_token [B] int32 out; log_ratio_out [B, L] fp32 out or NULL (0 past the
+ *     window); status_out [B] uint32 out or NULL
+ * A token outside [0, V), a masked token (target -inf) and a step whose rows hold a NaN or
+ * +inf are rejected; a masked draft token with a possible target token has ell = +inf.  Where
+ * alpha q - p leaves nothing, the target's own row is drawn from (SDV_STATUS_ZERO_DELTA); a
+ * target row without probabilities gives next_token -1.  A draft row without any counts as 0.
+ */
+int sdv_token_verify(const void *target, int64_t target_stride_b, int64_t target_stride_row,
+                     const void *draft, int64_t draft_stride_b, int64_t draft_stride_row,
+                     const int32_t *tokens, int B, int L, int V, int dtype, float temperature,
+                     float draft_temperature, int mode, const int32_t *L_eff, uint64_t seed,
+                     const float *coins, const float *race, int32_t *accepted_len,
+                     int32_t *next_token, float *log_ratio_out, uint32_t *status_out,
+                     sdv_stream_t stream);
+
+/*
+ * The cache: k_codes [pages, H, block, D] and v_codes [pages, H, D, block] hold e4m3 codes (values
+ * transposed: contiguous along the tokens), k_scale and v_scale [pages, H] fp32 what a
+ * page's codes of a head are multiplied by.  Token i of sequence b is row i % block of page
+ * page_table[b, i / block] (page_table [B, max_pages] int32, only the entries of its tokens
+ * are read).  D is 64 or 128, block a multiple of 16 up to SDV_MAX_BLOCK; code arrays are
+ * 16-byte aligned.
+ *
+ * sdv_cache_append - appends counts[b] (W if NULL; at most W) new tokens behind the lengths[b]
+ * that sequence b holds.  k_new and v_new are [B, W, H, D] (F32, BF16 or F16) with the strides
+ * given, the same for both.  A page's scale becomes the least power of two (2^-126 or more)
+ * whose 448-fold holds the new tokens' magnitudes, or stays if tokens that it holds already have a larger
+ * one; if it grows, those tokens' codes are restated under it.  Codes are rounded to
+ * nearest even; infinities become +-448, NaN a NaN code, and neither counts for the scale.
+ * Rows behind the new tokens keep what they held.  A token whose page does not exist is left out
+ * (SDV_STATUS_BAD_PAGE).  status [B] uint32 or NULL: bits are added to it.  No page may be
+ * appended to by two sequences.
+ */
+int sdv_cache_append(const void *k_new, const void *v_new, int64_t stride_b, int64_t stride_t,
+                     int64_t stride_h, int dtype, int B, int W, int H, int D, int block,
+                     void *k_codes, void *v_codes, float *k_scale, float *v_scale, int64_t pages,
+                     const int32_t *page_table, int max_pages, const int32_t *lengths,
+                     const int32_t *counts, uint32_t *status, sdv_stream_t stream);
+
+/* Bytes of device workspace sdv_cache_attend needs; 0 for invalid sizes. */
+size_t sdv_attend_workspace_bytes(int W, int Hq, int H, int D);
+
+/*
+ * sdv_cache_attend - attention of the last counts[b] (W if NULL) of the lengths[b] tokens in the
+ * cache over all tokens up to themselves: query i of sequence b has position lengths[b] -
+ * counts[b] + i and sees the keys up to its position (with span > 0, the last `span` of them).
+ *   s_j = scale ks_j (q . k_j), out = sum_j softmax(s)_j vs_j v_j, lse = log sum_j e^{s_j}
+ * q is [B, W, Hq, D] (BF16 or F16) with the strides given; query heads h G .. h G + G - 1,
+ * G = Hq / H, read key head h.  out [B, W, Hq, D] (`dtype`), lse [B, W, Hq] fp32 or NULL, dense.
+ * Queries i >= counts[b], or with nothing to see, get 0 and -inf.  A NaN code in a key or value that
+ * a query sees makes its row NaN; what it does not see has no effect.  Tokens of a page
+ * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL).
+ * Probabilities are rounded to fp16 (11 bits) before they meet the values, sums are fp32.
+ */
+int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h,
+                     int dtype, int B, int W, int Hq, int H, int D, int block,
+                     const void *k_codes, const void *v_codes, const float *k_scale,
+                     const float *v_scale, int64_t pages, const int32_t *page_table,
+                     int max_pages, const int32_t *lengths, const int32_t *counts, float scale,
+                     int span, void *out, float *lse, uint32_t *status, void *workspace,
+                     size_t workspace_bytes, sdv_stream_t stream);
+
 /*
  * Profiling aid (not part of the method): when enabled, sdv_verify /
  * sdv_verify_ex calls made on this host thread record CUDA events on their

@@ -11,6 +11,7 @@ from . import binding as B
 _DTYPES = {torch.float32: B.SDV_F32, torch.bfloat16: B.SDV_BF16}
 _MODES = {"sample": B.SDV_MODE_SAMPLE, "block": B.SDV_MODE_BLOCK,
           B.SDV_MODE_SAMPLE: B.SDV_MODE_SAMPLE, B.SDV_MODE_BLOCK: B.SDV_MODE_BLOCK}
+_TOKEN_DTYPES = {torch.float32: B.SDV_F32, torch.bfloat16: B.SDV_BF16, torch.float16: B.SDV_F16}
 _RESIDUALS = {"decomposition": B.SDV_RESIDUAL_DECOMPOSITION,
               "reflection": B.SDV_RESIDUAL_REFLECTION}
 
@@ -348,3 +349,195 @@ def em_sample(Bn, target, seed):
     B.sdv_em_sample(Bn, target.d, *target.params(), int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(y),
                     _stream())
     return y
+
+
+# ---- speculative decoding over tokens: scores, verification, 8-bit cache
+
+
+def _dense(what, t, dtype, shape):
+    """A contiguous CUDA tensor of the type and shape, or None."""
+    if t is None:
+        return
+    if not (t.is_cuda and t.is_contiguous()) or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: a contiguous CUDA %s tensor of shape %s expected" % (what, dtype, tuple(shape)))
+
+
+def _out(out, name, shape, dtype, dev):
+    t = out.get(name) if out else None
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _dense(name, t, dtype, shape)
+    return t
+
+
+def _rows(what, t, dims):
+    """A CUDA tensor of logits (or keys, queries) whose last axis is contiguous; its type's code."""
+    if not t.is_cuda or t.dim() != dims or t.dtype not in _TOKEN_DTYPES or t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("%s: a %d-d CUDA float32/bfloat16/float16 tensor with a contiguous last axis expected" % (what, dims))
+    return _TOKEN_DTYPES[t.dtype]
+
+
+def _row_stride(t):
+    """Elements between rows of [..., N, V] (rows of a single one may be anywhere)."""
+    return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+
+
+def token_scores(logits, tokens=None, *, top_k=0, temperature=1.0, entropy=True, out=None):
+    """Log probabilities of given tokens, entropy and top alternatives of logits [N, V]
+    (sdv_token_scores); returns a dict: logprob [N] (with tokens [N] int32, -1 for none), entropy
+    [N], row_max, log_sum [N], status [N], and top_ids, top_logprob [N, top_k]."""
+    dt = _rows("logits", logits, 2)
+    N, V = logits.shape
+    dev, f32 = logits.device, torch.float32
+    _dense("tokens", tokens, torch.int32, (N,))
+    r = {}
+    if tokens is not None:
+        r["logprob"] = _out(out, "logprob", (N,), f32, dev)
+    if entropy:
+        r["entropy"] = _out(out, "entropy", (N,), f32, dev)
+    r["row_max"] = _out(out, "row_max", (N,), f32, dev)
+    r["log_sum"] = _out(out, "log_sum", (N,), f32, dev)
+    r["status"] = _out(out, "status", (N,), torch.int32, dev)
+    if top_k:
+        r["top_ids"] = _out(out, "top_ids", (N, top_k), torch.int32, dev)
+        r["top_logprob"] = _out(out, "top_logprob", (N, top_k), f32, dev)
+    B._call("sdv_token_scores", logits.data_ptr(), _row_stride(logits), N, V, dt, _ptr(tokens), float(temperature), int(top_k),
+            _ptr(r.get("logprob")), _ptr(r.get("entropy")), r["row_max"].data_ptr(), r["log_sum"].data_ptr(),
+            _ptr(r.get("top_ids")), _ptr(r.get("top_logprob")), r["status"].data_ptr(), _stream())
+    return r
+
+
+def _grad_like(logits, d_logits):
+    """The gradient's tensor: rows laid out as the logits' where they are (nearly) dense, so that
+    both meet 16-byte boundaries at the same places."""
+    N, V = logits.shape
+    if d_logits is None:
+        st = _row_stride(logits)
+        if V < st <= V + 128:
+            return torch.empty(N, st, dtype=logits.dtype, device=logits.device)[:, :V]
+        return torch.empty(N, V, dtype=logits.dtype, device=logits.device)
+    if not d_logits.is_cuda or d_logits.dtype != logits.dtype or d_logits.shape != logits.shape or d_logits.stride(1) != 1 and V > 1:
+        raise ValueError("d_logits: a CUDA tensor of the logits' type and shape with a contiguous last axis expected")
+    return d_logits
+
+
+def token_scores_grad(logits, tokens, scores, g_logprob=None, g_entropy=None, *, temperature=1.0, d_logits=None):
+    """The gradient of sum g_logprob logprob + g_entropy entropy with respect to the logits, from
+    the dict of token_scores (sdv_token_scores_grad); d_logits may be the logits themselves."""
+    dt = _rows("logits", logits, 2)
+    N, V = logits.shape
+    _dense("tokens", tokens, torch.int32, (N,))
+    for what, t in (("g_logprob", g_logprob), ("g_entropy", g_entropy), ("row_max", scores["row_max"]),
+                    ("log_sum", scores["log_sum"]), ("entropy", scores.get("entropy"))):
+        _dense(what, t, torch.float32, (N,))
+    dx = _grad_like(logits, d_logits)
+    B._call("sdv_token_scores_grad", logits.data_ptr(), _row_stride(logits), N, V, dt,
+            _ptr(tokens) if g_logprob is not None else 0, float(temperature), scores["row_max"].data_ptr(),
+            scores["log_sum"].data_ptr(), _ptr(scores.get("entropy")), _ptr(g_logprob), _ptr(g_entropy), dx.data_ptr(),
+            _row_stride(dx), _stream())
+    return dx
+
+
+def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temperature=1.0, d_logits=None, out=None):
+    """Scores and gradient in one call that reads the logits once (sdv_token_scores_train);
+    returns the dict of token_scores with d_logits."""
+    dt = _rows("logits", logits, 2)
+    N, V = logits.shape
+    dev, f32 = logits.device, torch.float32
+    _dense("tokens", tokens, torch.int32, (N,))
+    _dense("g_logprob", g_logprob, f32, (N,))
+    _dense("g_entropy", g_entropy, f32, (N,))
+    r = {k: _out(out, k, (N,), f32, dev) for k in ("logprob", "entropy", "row_max", "log_sum") if k != "logprob" or tokens is not None}
+    r["status"] = _out(out, "status", (N,), torch.int32, dev)
+    r["d_logits"] = dx = _grad_like(logits, d_logits)
+    B._call("sdv_token_scores_train", logits.data_ptr(), _row_stride(logits), N, V, dt, _ptr(tokens), float(temperature),
+            _ptr(g_logprob), _ptr(g_entropy), _ptr(r.get("logprob")), r["entropy"].data_ptr(), r["row_max"].data_ptr(),
+            r["log_sum"].data_ptr(), r["status"].data_ptr(), dx.data_ptr(), _row_stride(dx), _stream())
+    return r
+
+
+def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L_eff=None, temperature=1.0,
+                 draft_temperature=None, coins=None, race=None, out=None):
+    """Verification of drafted tokens [B, L] from target logits [B, L + 1, V] and draft logits
+    [B, L, V] (sdv_token_verify); returns accepted_len, next_token, status [B] and log_ratio
+    [B, L].  draft_temperature defaults to temperature; coins [B, L] and race [B, V] (exponential
+    variates) replace the draws from `seed`."""
+    dt = _rows("target_logits", target_logits, 3)
+    if _rows("draft_logits", draft_logits, 3) != dt:
+        raise ValueError("target_logits and draft_logits must share a type")
+    Bn, L, V = draft_logits.shape
+    if tuple(target_logits.shape) != (Bn, L + 1, V):
+        raise ValueError("target_logits [B, L + 1, V] expected")
+    i32, f32, dev = torch.int32, torch.float32, target_logits.device
+    _dense("tokens", tokens, i32, (Bn, L))
+    _dense("L_eff", L_eff, i32, (Bn,))
+    _dense("coins", coins, f32, (Bn, L))
+    _dense("race", race, f32, (Bn, V))
+    r = dict(accepted_len=_out(out, "accepted_len", (Bn,), i32, dev), next_token=_out(out, "next_token", (Bn,), i32, dev),
+             log_ratio=_out(out, "log_ratio", (Bn, L), f32, dev), status=_out(out, "status", (Bn,), i32, dev))
+    B._call("sdv_token_verify", target_logits.data_ptr(), target_logits.stride(0), _row_stride(target_logits),
+            draft_logits.data_ptr(), draft_logits.stride(0), _row_stride(draft_logits), tokens.data_ptr(), Bn, L, V, dt,
+            float(temperature), float(temperature if draft_temperature is None else draft_temperature), _MODES[mode],
+            _ptr(L_eff), int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(coins), _ptr(race), r["accepted_len"].data_ptr(),
+            r["next_token"].data_ptr(), r["log_ratio"].data_ptr(), r["status"].data_ptr(), _stream())
+    return r
+
+
+def make_token_cache(pages, heads, block, dim, device="cuda"):
+    """An empty 8-bit cache: codes k [pages, heads, block, dim] and v [pages, heads, dim, block]
+    (float8_e4m3fn), k_scale and v_scale [pages, heads]."""
+    f8 = torch.float8_e4m3fn
+    return dict(k=torch.zeros(pages, heads, block, dim, dtype=torch.uint8, device=device).view(f8),
+                v=torch.zeros(pages, heads, dim, block, dtype=torch.uint8, device=device).view(f8),
+                k_scale=torch.ones(pages, heads, dtype=torch.float32, device=device),
+                v_scale=torch.ones(pages, heads, dtype=torch.float32, device=device))
+
+
+def _cache_args(cache, page_table, lengths, counts):
+    k = cache["k"]
+    P, H, block, D = k.shape
+    f8 = torch.float8_e4m3fn
+    _dense("cache k", k, f8, (P, H, block, D))
+    _dense("cache v", cache["v"], f8, (P, H, D, block))
+    _dense("cache k_scale", cache["k_scale"], torch.float32, (P, H))
+    _dense("cache v_scale", cache["v_scale"], torch.float32, (P, H))
+    Bn, M = page_table.shape
+    _dense("page_table", page_table, torch.int32, (Bn, M))
+    _dense("lengths", lengths, torch.int32, (Bn,))
+    _dense("counts", counts, torch.int32, (Bn,))
+    return P, H, block, D, Bn, M
+
+
+def cache_append(cache, k_new, v_new, page_table, lengths, *, counts=None, status=None):
+    """Appends k_new, v_new [B, W, H, D] behind the lengths [B] tokens that the cache holds of each
+    sequence (sdv_cache_append); status [B] int32 gets bits added to it."""
+    P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
+    dt = _rows("k_new", k_new, 4)
+    W = k_new.shape[1]
+    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or v_new.stride() != k_new.stride():
+        raise ValueError("k_new and v_new: [B, W, heads, dim] of one type and layout expected")
+    _dense("status", status, torch.int32, (Bn,))
+    B._call("sdv_cache_append", k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), k_new.stride(2), dt, Bn, W, H,
+            D, block, cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
+            page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), _ptr(status), _stream())
+
+
+def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span=0, status=None, workspace=None, out=None):
+    """Attention of the window q [B, W, Hq, D], whose tokens are the last ones of the cache, over
+    the lengths [B] tokens that it holds (sdv_cache_attend); returns out [B, W, Hq, D] and lse
+    [B, W, Hq].  scale defaults to D^-1/2."""
+    P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
+    dt = _rows("q", q, 4)
+    W, Hq = q.shape[1], q.shape[2]
+    if tuple(q.shape) != (Bn, W, Hq, D):
+        raise ValueError("q: [B, W, query heads, dim] expected")
+    _dense("status", status, torch.int32, (Bn,))
+    dev = q.device
+    r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
+    if workspace is None:
+        workspace = torch.empty(max(B.sdv_attend_workspace_bytes(W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
+    B._call("sdv_cache_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
+            cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
+            page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),
+            r["out"].data_ptr(), r["lse"].data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel(), _stream())
+    return r

@@ -30,6 +30,12 @@ SDV_STATUS_ZERO_DELTA = 1
 SDV_STATUS_NONFINITE = 2
 SDV_STATUS_USAMPLE_RANGE = 4
 SDV_MAX_L = 64
+SDV_F16 = 2
+SDV_STATUS_EMPTY_ROW = 8
+SDV_STATUS_BAD_TOKEN = 16
+SDV_STATUS_BAD_PAGE = 32
+SDV_MAX_TOP = 32
+SDV_MAX_BLOCK = 128
 SDV_MAX_COMPONENTS = 16
 SDV_DRAFTER_FREE = 0
 SDV_DRAFTER_FROZEN = 1
@@ -76,6 +82,17 @@ SIGNATURES = {
                                _SZ, _P]),
     "sdv_sampler_end": (_I, [_I, _I, _I64, _P, _SZ, _P, _P, _P, _P, _P, _P]),
     "sdv_em_sample": (_I, [_I, _I64, _P, _P, _I, _F, _I, _F, _F, _F, _F, _U64, _P, _P]),
+    "sdv_token_scores": (_I, [_P, _I64, _I, _I, _I, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "sdv_token_scores_grad": (_I, [_P, _I64, _I, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "sdv_token_scores_train": (_I, [_P, _I64, _I, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _P, _P, _I64,
+                                    _P]),
+    "sdv_token_verify": (_I, [_P, _I64, _I64, _P, _I64, _I64, _P, _I, _I, _I, _I, _F, _F, _I, _P, _U64,
+                              _P, _P, _P, _P, _P, _P, _P]),
+    "sdv_cache_append": (_I, [_P, _P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
+                              _P, _I, _P, _P, _P, _P]),
+    "sdv_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
+    "sdv_cache_attend": (_I, [_P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
+                              _P, _I, _P, _P, _F, _I, _P, _P, _P, _P, _SZ, _P]),
     "sdv_timing_enable": (_I, [_I]),
     "sdv_timing_stride": (_I, [_I]),
     "sdv_timing_read": (_I, [_I, _P]),
@@ -297,3 +314,52 @@ def sdv_em_sample(B, d, means, log_weights, C, comp_var, K, churn, beta_min, bet
                   seed, y_out, stream):
     return _call("sdv_em_sample", B, d, means, log_weights, C, comp_var, K, churn, beta_min,
                  beta_max, t_floor, seed, y_out, stream)
+
+
+def sdv_token_scores(logits, row_stride, N, V, dtype, tokens, temperature, top_k, logprob, entropy,
+                     row_max, log_sum, top_ids, top_logprob, status, stream):
+    return _call("sdv_token_scores", logits, row_stride, N, V, dtype, tokens, temperature, top_k,
+                 logprob, entropy, row_max, log_sum, top_ids, top_logprob, status, stream)
+
+
+def sdv_token_scores_grad(logits, row_stride, N, V, dtype, tokens, temperature, row_max, log_sum,
+                          entropy, g_logprob, g_entropy, d_logits, d_stride, stream):
+    return _call("sdv_token_scores_grad", logits, row_stride, N, V, dtype, tokens, temperature,
+                 row_max, log_sum, entropy, g_logprob, g_entropy, d_logits, d_stride, stream)
+
+
+def sdv_token_scores_train(logits, row_stride, N, V, dtype, tokens, temperature, g_logprob,
+                           g_entropy, logprob, entropy, row_max, log_sum, status, d_logits, d_stride,
+                           stream):
+    return _call("sdv_token_scores_train", logits, row_stride, N, V, dtype, tokens, temperature,
+                 g_logprob, g_entropy, logprob, entropy, row_max, log_sum, status, d_logits, d_stride,
+                 stream)
+
+
+def sdv_token_verify(target, target_stride_b, target_stride_row, draft, draft_stride_b,
+                     draft_stride_row, tokens, B, L, V, dtype, temperature, draft_temperature, mode,
+                     L_eff, seed, coins, race, accepted_len, next_token, log_ratio_out, status_out,
+                     stream):
+    return _call("sdv_token_verify", target, target_stride_b, target_stride_row, draft, draft_stride_b,
+                 draft_stride_row, tokens, B, L, V, dtype, temperature, draft_temperature, mode, L_eff,
+                 seed, coins, race, accepted_len, next_token, log_ratio_out, status_out, stream)
+
+
+def sdv_cache_append(k_new, v_new, stride_b, stride_t, stride_h, dtype, B, W, H, D, block, k_codes,
+                     v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths, counts, status,
+                     stream):
+    return _call("sdv_cache_append", k_new, v_new, stride_b, stride_t, stride_h, dtype, B, W, H, D,
+                 block, k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths,
+                 counts, status, stream)
+
+
+def sdv_attend_workspace_bytes(W, Hq, H, D):
+    return int(load().sdv_attend_workspace_bytes(W, Hq, H, D))
+
+
+def sdv_cache_attend(q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D, block, k_codes,
+                     v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths, counts, scale,
+                     span, out, lse, status, workspace, workspace_bytes, stream):
+    return _call("sdv_cache_attend", q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D,
+                 block, k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths,
+                 counts, scale, span, out, lse, status, workspace, workspace_bytes, stream)

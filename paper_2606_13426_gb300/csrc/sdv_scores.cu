@@ -1,0 +1,582 @@
+// sdv_scores.cu - log probabilities of given tokens, entropy and the top alternatives of rows
+// of logits (k_scores), the gradient from given statistics (k_scores_grad), and statistics and
+// gradient in one pass over the logits (k_scores_train).
+//
+// With d_v = x_v - m, m = max x, and s = sum e^{d_v/T}:
+//   log p_t = d_t/T - log s,     H = log s - (1/T) sum p_v d_v,
+//   dx_v = (1/T) [g_lp (1[v = t] - p_v) - g_H p_v (log p_v + H)].
+// A row is split over the CTAs of a cluster, which join their statistics through distributed
+// shared memory.
+#include "sdv_tokens.cuh"
+
+namespace sdv {
+
+constexpr int kScoreThreads = 256;
+constexpr int kScoreUnroll = 4;        // 16-byte vectors in flight per thread
+constexpr int kGroups = 64;            // groups of threads whose maxima give the alternatives' threshold
+constexpr int kCandMax = 512;          // candidates a CTA ranks; more: k passes over its part
+constexpr int kScoreMaxCluster = 8;
+
+struct ScoreArgs {
+  const void* x;
+  int64_t stride;
+  int V;
+  const int32_t* tokens;
+  float c;                             // log2(e) / T
+  float inv_t;
+  int top_k;
+  float* logprob;
+  float* entropy;
+  float* row_max;
+  float* log_sum;
+  int32_t* top_ids;
+  float* top_lp;
+  uint32_t* status;
+};
+
+struct Cand {
+  float x;
+  int i;
+};
+
+// The token of a row and its logit, read before any gradient is written (which may be in place).
+struct Token {
+  int t;
+  float x;
+};
+template <int kDtype>
+__device__ __forceinline__ Token row_token(const ScoreArgs& A, const typename Num<kDtype>::T* row, int64_t n) {
+  Token k{A.tokens ? A.tokens[n] : -1, 0.f};
+  if (k.t >= 0 && k.t < A.V) k.x = Num<kDtype>::to(row[k.t]);
+  return k;
+}
+
+// The outputs of a row other than its alternatives.
+__device__ __forceinline__ void write_row(const ScoreArgs& A, int64_t n, const Stat& a, const Token& tok) {
+  uint32_t st = 0;
+  const bool bad = !(a.m < INFINITY);                    // NaN or +inf
+  const bool empty = a.m == -INFINITY;
+  if (bad) st |= SDV_STATUS_NONFINITE;
+  if (empty) st |= SDV_STATUS_EMPTY_ROW;
+  const float log_s = bad ? NAN : (empty ? -INFINITY : logf(a.s));
+  if (A.row_max) A.row_max[n] = bad ? NAN : a.m;
+  if (A.log_sum) A.log_sum[n] = log_s;
+  if (A.entropy) A.entropy[n] = bad ? NAN : (empty ? 0.f : log_s - a.w / a.s * A.inv_t);
+  if (A.tokens) {
+    const int t = tok.t;
+    float lp = 0.f;
+    if (t != -1) {
+      if (t < 0 || t >= A.V) {
+        st |= SDV_STATUS_BAD_TOKEN;
+        lp = NAN;
+      } else if (bad) {
+        lp = NAN;
+      } else {
+        lp = empty ? -INFINITY : (tok.x - a.m) * A.inv_t - log_s;
+      }
+    }
+    A.logprob[n] = lp;
+  }
+  if (A.status) A.status[n] = st;
+}
+
+// Ranks the n candidates in `c` by counting and hands those of rank < k to put(rank, candidate).
+template <typename Put>
+__device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put put) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const Cand me = c[i];
+    int r = 0;
+    for (int j = 0; j < n; ++j) {
+      const Cand o = c[j];
+      r += before(o.x, o.i, me.x, me.i);
+    }
+    if (r < k) put(r, me);
+  }
+}
+
+template <int kDtype, bool kTop>
+__global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
+  using E = Num<kDtype>;
+  using T = typename E::T;
+  constexpr int kPer = E::kPer16;
+  constexpr int kWarps = kScoreThreads / 32;
+  cg::cluster_group cl = cg::this_cluster();
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int64_t n = blockIdx.x / C;
+  const int tid = threadIdx.x;
+  __shared__ Stat wstat[kWarps];
+  __shared__ Stat cstat[kScoreMaxCluster];
+  __shared__ float tmax[kTop ? kScoreThreads : 1];
+  __shared__ float gmax[kTop ? kGroups : 1];
+  __shared__ float thr_s[2];
+  __shared__ int ncand;
+  __shared__ Cand cand[kTop ? kCandMax : 1];
+  __shared__ Cand lists[kTop ? kScoreMaxCluster * SDV_MAX_TOP : 1];
+  __shared__ Cand best_w[kWarps];
+  if (C > 1) cl.barrier_arrive();
+  const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
+  const Row<kDtype> R(row, A.V);
+  const int v0 = (int)((int64_t)R.nvec * rank / C), v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
+  const uint4* vec = R.vec();
+  Stat a = stat_empty();
+  int v = v0 + tid;
+  for (; v + (kScoreUnroll - 1) * kScoreThreads < v1; v += kScoreUnroll * kScoreThreads) {
+    uint4 raw[kScoreUnroll];
+#pragma unroll
+    for (int u = 0; u < kScoreUnroll; ++u) raw[u] = __ldg(vec + v + u * kScoreThreads);
+#pragma unroll
+    for (int u = 0; u < kScoreUnroll; ++u) {
+      float f[kPer];
+      E::unpack(raw[u], f);
+      stat_add<kPer>(a, f, A.c);
+    }
+  }
+  for (; v < v1; v += kScoreThreads) {
+    float f[kPer];
+    E::unpack(__ldg(vec + v), f);
+    stat_add<kPer>(a, f, A.c);
+  }
+  if (rank == 0 && tid < R.singles()) {
+    const float f = E::to(row[R.single(tid)]);
+    stat_add<1>(a, &f, A.c);
+  }
+  const float tm = a.m;                       // the largest of this thread's logits
+  a = stat_warp(a, A.c);
+  if ((tid & 31) == 0) wstat[tid >> 5] = a;
+  if (kTop) {
+    tmax[tid] = tm;
+    if (tid == 0) ncand = 0;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a = wstat[0];
+    for (int w = 1; w < kWarps; ++w) a = stat_join(a, wstat[w], A.c);
+    wstat[0] = a;
+  }
+  if constexpr (kTop) {
+    // At least k of the part's logits are at or above the k-th largest of the groups' maxima.
+    if (tid < kGroups) {
+      float g = tmax[tid];
+      for (int j = tid + kGroups; j < kScoreThreads; j += kGroups) g = fmaxf(g, tmax[j]);
+      gmax[tid] = g;
+    }
+    __syncthreads();
+    if (tid < kGroups) {
+      const float g = gmax[tid];
+      int above = 0;
+      for (int j = 0; j < kGroups; ++j) above += gmax[j] > g;
+      float t = above < A.top_k ? g : INFINITY;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) t = fminf(t, __shfl_xor_sync(0xffffffffu, t, o));
+      if ((tid & 31) == 0) thr_s[tid >> 5] = t;
+    }
+    __syncthreads();
+    const float thr = fminf(thr_s[0], thr_s[1]);
+    auto keep = [&](float x, int i) {
+      if (x >= thr && x > -INFINITY) {
+        const int at = atomicAdd(&ncand, 1);     // their order does not matter: they are ranked
+        if (at < kCandMax) cand[at] = Cand{x, i};
+      }
+    };
+    if (tm >= thr) {
+      for (v = v0 + tid; v < v1; v += kScoreThreads) {
+        float f[kPer];
+        E::unpack(__ldg(vec + v), f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) keep(f[e], R.head + v * kPer + e);
+      }
+      if (rank == 0 && tid < R.singles()) keep(E::to(row[R.single(tid)]), R.single(tid));
+    }
+    __syncthreads();
+    if (C > 1) cl.barrier_wait();               // the leader has started: its lists can be written
+    Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * SDV_MAX_TOP;
+    const int nc = ncand;
+    if (nc <= kCandMax) {
+      rank_candidates(cand, nc, A.top_k, [&](int r, Cand c) { mine[r] = c; });
+      if (tid >= nc && tid < A.top_k) mine[tid] = Cand{-INFINITY, -1};
+    } else {                                      // many equal logits: one alternative per pass
+      Cand last{INFINITY, -1};
+      for (int r = 0; r < A.top_k; ++r) {
+        Cand b{-INFINITY, 0x7fffffff};
+        auto see = [&](float x, int i) {
+          if (x > -INFINITY && before(last.x, last.i, x, i) && before(x, i, b.x, b.i)) b = Cand{x, i};
+        };
+        for (v = v0 + tid; v < v1; v += kScoreThreads) {
+          float f[kPer];
+          E::unpack(__ldg(vec + v), f);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) see(f[e], R.head + v * kPer + e);
+        }
+        if (rank == 0 && tid < R.singles()) see(E::to(row[R.single(tid)]), R.single(tid));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+          const float ox = __shfl_xor_sync(0xffffffffu, b.x, o);
+          const int oi = __shfl_xor_sync(0xffffffffu, b.i, o);
+          if (before(ox, oi, b.x, b.i)) b = Cand{ox, oi};
+        }
+        __syncthreads();
+        if ((tid & 31) == 0) best_w[tid >> 5] = b;
+        __syncthreads();
+        b = best_w[0];
+        for (int w = 1; w < kWarps; ++w)
+          if (before(best_w[w].x, best_w[w].i, b.x, b.i)) b = best_w[w];
+        if (tid == 0) mine[r] = b.x > -INFINITY ? b : Cand{-INFINITY, -1};
+        last = b;
+      }
+    }
+  } else {
+    if (C > 1) cl.barrier_wait();
+  }
+  if (tid == 0) {
+    Stat* to = C > 1 ? cl.map_shared_rank(cstat, 0) : cstat;
+    to[rank] = wstat[0];
+  }
+  if (C > 1) {
+    cl.sync();
+    if (rank) return;
+  } else {
+    __syncthreads();
+  }
+  a = cstat[0];
+  for (int r = 1; r < C; ++r) a = stat_join(a, cstat[r], A.c);
+  if (tid == 0) write_row(A, n, a, row_token<kDtype>(A, row, n));
+  if constexpr (kTop) {
+    const bool bad = !(a.m < INFINITY);
+    const float log_s = logf(a.s);
+    const int k = A.top_k;
+    auto put = [&](int r, Cand c) {
+      const bool none = bad || c.i < 0;
+      A.top_ids[n * k + r] = none ? -1 : c.i;
+      A.top_lp[n * k + r] = bad ? NAN : (none ? -INFINITY : (c.x - a.m) * A.inv_t - log_s);
+    };
+    // the CTAs' lists, placeholders left out, one behind the other
+    int total = 0;
+    for (int i = tid; i < C * k; i += kScoreThreads) {
+      const Cand me = lists[(i / k) * SDV_MAX_TOP + i % k];
+      if (me.i < 0) continue;
+      int r = 0;
+      for (int j = 0; j < C * k; ++j) {
+        const Cand o = lists[(j / k) * SDV_MAX_TOP + j % k];
+        r += o.i >= 0 && before(o.x, o.i, me.x, me.i);
+      }
+      if (r < k) put(r, me);
+    }
+    for (int j = 0; j < C * k; ++j) total += lists[(j / k) * SDV_MAX_TOP + j % k].i >= 0;
+    if (bad) total = 0;
+    for (int r = total + tid; r < k; r += kScoreThreads) put(r, Cand{-INFINITY, -1});
+  }
+}
+
+struct GradArgs {
+  const void* x;
+  int64_t stride;
+  int V;
+  const int32_t* tokens;
+  float c, inv_t;
+  const float* row_max;
+  const float* log_sum;
+  const float* entropy;
+  const float* g_lp;
+  const float* g_h;
+  void* dx;
+  int64_t dstride;
+};
+
+// The gradient of a row: p_v (a + b d_v), and at the token g more.
+struct RowGrad {
+  float m, ls2;          // maximum, log2 s
+  float a, b, g;
+  int t;                 // the token, or -1
+  float nan;             // what every element gets if the row has no gradient (0 or NaN), else unused
+  bool flat;
+};
+__device__ __forceinline__ RowGrad row_grad(float m, float log_s, float H, int t, int V, float g_lp, float g_h, float inv_t) {
+  RowGrad r;
+  const bool token = t >= 0 && t < V;
+  r.t = token ? t : -1;
+  r.m = m;
+  r.ls2 = log_s * kLog2E;
+  const float gl = token ? g_lp : 0.f;
+  r.a = -inv_t * (gl + g_h * (H - log_s));
+  r.b = -inv_t * inv_t * g_h;
+  r.g = inv_t * gl;
+  r.flat = !(m > -INFINITY && m < INFINITY);
+  r.nan = m == -INFINITY ? 0.f : NAN;
+  return r;
+}
+__device__ __forceinline__ float grad_of(const RowGrad& r, float x, float c) {
+  const float d = fmaxf(x - r.m, kFar);
+  const float p = ex2(fmaf(d, c, -r.ls2));
+  return r.flat ? r.nan : p * fmaf(r.b, d, r.a);
+}
+template <int kPer>
+__device__ __forceinline__ void grad_vec(const RowGrad& r, const float* f, float* o, int first, float c) {
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) o[e] = grad_of(r, f[e], c);
+  const unsigned at = (unsigned)(r.t - first);
+  if (r.t >= 0 && at < (unsigned)kPer && !r.flat) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if ((int)at == e && f[e] > -INFINITY) o[e] += r.g;
+  }
+}
+// Stores a vector of results whose place need not be on a 16-byte boundary.
+template <int kDtype>
+__device__ __forceinline__ void put_vec(typename Num<kDtype>::T* to, const float* o, bool vec) {
+  using E = Num<kDtype>;
+  if (vec) {
+    *reinterpret_cast<uint4*>(to) = E::pack(o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E::kPer16; ++e) to[e] = E::from(o[e]);
+  }
+}
+template <int kDtype>
+__device__ __forceinline__ bool same_phase(const void* a, const void* b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0;
+}
+
+// grid (parts of a row, rows)
+template <int kDtype>
+__global__ void __launch_bounds__(kScoreThreads) k_scores_grad(const GradArgs A, int parts) {
+  using E = Num<kDtype>;
+  using T = typename E::T;
+  constexpr int kPer = E::kPer16;
+  const int64_t n = blockIdx.x / parts;
+  const int part = blockIdx.x % parts;
+  const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
+  T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
+  const Row<kDtype> R(row, A.V);
+  const bool vec_out = same_phase<kDtype>(row, out);
+  const RowGrad g = row_grad(A.row_max[n], A.log_sum[n], A.entropy ? A.entropy[n] : 0.f, A.tokens ? A.tokens[n] : -1, A.V,
+                             A.g_lp ? A.g_lp[n] : 0.f, A.g_h ? A.g_h[n] : 0.f, A.inv_t);
+  const int v0 = (int)((int64_t)R.nvec * part / parts), v1 = (int)((int64_t)R.nvec * (part + 1) / parts);
+  const uint4* vec = R.vec();
+  for (int v = v0 + threadIdx.x; v < v1; v += kScoreThreads) {
+    float f[kPer], o[kPer];
+    E::unpack(vec[v], f);
+    grad_vec<kPer>(g, f, o, R.head + v * kPer, A.c);
+    put_vec<kDtype>(out + R.head + v * kPer, o, vec_out);
+  }
+  if (part == 0 && threadIdx.x < R.singles()) {
+    const int i = R.single(threadIdx.x);
+    const float f = E::to(row[i]);
+    float o;
+    grad_vec<1>(g, &f, &o, i, A.c);
+    out[i] = E::from(o);
+  }
+}
+
+struct TrainArgs {
+  ScoreArgs S;
+  const float* g_lp;
+  const float* g_h;
+  void* dx;
+  int64_t dstride;
+};
+
+// Statistics and gradient with the row read once: each thread of the cluster keeps its part of
+// it, as read, in registers (kVecs vectors) while the statistics are joined.
+template <int kDtype, int kThreads, int kVecs>
+__global__ void __launch_bounds__(kThreads) k_scores_train(const TrainArgs A) {
+  using E = Num<kDtype>;
+  using T = typename E::T;
+  constexpr int kPer = E::kPer16;
+  constexpr int kWarps = kThreads / 32;
+  cg::cluster_group cl = cg::this_cluster();
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int64_t n = blockIdx.x / C;
+  const int tid = threadIdx.x;
+  __shared__ Stat wstat[kWarps];
+  __shared__ Stat cstat[kScoreMaxCluster];
+  if (C > 1) cl.barrier_arrive();
+  const T* row = reinterpret_cast<const T*>(A.S.x) + n * A.S.stride;
+  T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
+  const Row<kDtype> R(row, A.S.V);
+  const bool vec_out = same_phase<kDtype>(row, out);
+  const int v0 = (int)((int64_t)R.nvec * rank / C), v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
+  const uint4* vec = R.vec();
+  uint4 raw[kVecs];
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const int v = v0 + tid + u * kThreads;
+    if (v < v1) raw[u] = vec[v];
+  }
+  const int si = rank == 0 && tid < R.singles() ? R.single(tid) : -1;
+  const float sx = si >= 0 ? E::to(row[si]) : 0.f;
+  Stat a = stat_empty();
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    if (v0 + tid + u * kThreads < v1) {
+      float f[kPer];
+      E::unpack(raw[u], f);
+      stat_add<kPer>(a, f, A.S.c);
+    }
+  }
+  if (si >= 0) stat_add<1>(a, &sx, A.S.c);
+  a = stat_warp(a, A.S.c);
+  if ((tid & 31) == 0) wstat[tid >> 5] = a;
+  Token tok{-1, 0.f};
+  if (rank == 0 && tid == 0) tok = row_token<kDtype>(A.S, row, n);
+  __syncthreads();
+  if (C > 1) cl.barrier_wait();
+  if (tid < C) {                              // every CTA of the cluster gets every CTA's statistics
+    a = wstat[0];
+    for (int w = 1; w < kWarps; ++w) a = stat_join(a, wstat[w], A.S.c);
+    Stat* to = C > 1 ? cl.map_shared_rank(cstat, tid) : cstat;
+    to[rank] = a;
+  }
+  if (C > 1) cl.sync();
+  else __syncthreads();
+  a = cstat[0];
+  for (int r = 1; r < C; ++r) a = stat_join(a, cstat[r], A.S.c);
+  if (rank == 0 && tid == 0) write_row(A.S, n, a, tok);
+  const float log_s = logf(a.s);
+  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, A.S.tokens ? A.S.tokens[n] : -1, A.S.V,
+                             A.g_lp ? A.g_lp[n] : 0.f, A.g_h ? A.g_h[n] : 0.f, A.S.inv_t);
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const int v = v0 + tid + u * kThreads;
+    if (v < v1) {
+      float f[kPer], o[kPer];
+      E::unpack(raw[u], f);
+      grad_vec<kPer>(g, f, o, R.head + v * kPer, A.S.c);
+      put_vec<kDtype>(out + R.head + v * kPer, o, vec_out);
+    }
+  }
+  if (si >= 0) {
+    float o;
+    grad_vec<1>(g, &sx, &o, si, A.S.c);
+    out[si] = E::from(o);
+  }
+}
+
+// CTAs per row: as many as give every SM two CTAs, as long as each has some vectors per thread.
+static int score_cluster(int64_t N, int V, int dtype) {
+  const int64_t nvec = (int64_t)V * (int64_t)elem_bytes(dtype) / 16;
+  int c = 1;
+  while (c < kScoreMaxCluster && N * c < 2 * sm_count() && nvec / (2 * c) >= kScoreThreads) c *= 2;
+  return c;
+}
+
+static int check_rows(const void* x, int64_t stride, int N, int V, int dtype, float temperature) {
+  if (!token_dtype(dtype) || N < 0 || V < 1 || V > (1 << 30) || stride < V) return SDV_EINVAL;
+  if (!(temperature > 0.f) || !(kLog2E / temperature < INFINITY) || !(temperature < INFINITY)) return SDV_EINVAL;
+  if (!x) return SDV_EINVAL;
+  if (!aligned_to(x, elem_bytes(dtype))) return SDV_EALIGN;
+  return SDV_OK;
+}
+
+template <int kDtype>
+static cudaError_t launch_scores(const ScoreArgs& A, int N, int dtype, cudaStream_t s) {
+  const int C = score_cluster(N, A.V, dtype);
+  const dim3 grid((unsigned)(N * (int64_t)C));
+  if (A.top_k) return launch_cluster(k_scores<kDtype, true>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+  return launch_cluster(k_scores<kDtype, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+}
+
+constexpr int kTrainThreads = 512;
+constexpr int kTrainVecs = 8;
+
+// CTAs per row of k_scores_train: as few as hold it, 0 if the largest cluster does not.
+static int train_cluster(int V, int dtype) {
+  const int64_t nvec = ((int64_t)V * (int64_t)elem_bytes(dtype) + 15) / 16;
+  for (int c = 1; c <= kScoreMaxCluster; c *= 2)
+    if (nvec <= (int64_t)c * kTrainThreads * kTrainVecs) return c;
+  return 0;
+}
+
+template <int kDtype>
+static cudaError_t launch_grad(const GradArgs& G, int N, int dtype, cudaStream_t s) {
+  const int64_t nvec = (int64_t)G.V * (int64_t)elem_bytes(dtype) / 16;
+  int parts = 1;
+  while (parts < 64 && (int64_t)N * parts < 8 * sm_count() && nvec / (2 * parts) >= kScoreThreads) parts *= 2;
+  k_scores_grad<kDtype><<<(unsigned)(N * (int64_t)parts), kScoreThreads, 0, s>>>(G, parts);
+  return cudaGetLastError();
+}
+
+template <int kDtype>
+static cudaError_t launch_train(const TrainArgs& A, int N, int C, cudaStream_t s) {
+  return launch_cluster(k_scores_train<kDtype, kTrainThreads, kTrainVecs>, dim3((unsigned)(N * (int64_t)C)), kTrainThreads, 0,
+                        (unsigned)C, s, A);
+}
+
+}  // namespace sdv
+
+using namespace sdv;
+
+extern "C" {
+
+int sdv_token_scores(const void* logits, int64_t row_stride, int N, int V, int dtype, const int32_t* tokens,
+                     float temperature, int top_k, float* logprob, float* entropy, float* row_max, float* log_sum,
+                     int32_t* top_ids, float* top_logprob, uint32_t* status, sdv_stream_t stream) {
+  if (N == 0) return token_dtype(dtype) && V >= 1 ? SDV_OK : SDV_EINVAL;
+  int rc = check_rows(logits, row_stride, N, V, dtype, temperature);
+  if (rc) return rc;
+  if (N > (1 << 27) || top_k < 0 || top_k > SDV_MAX_TOP || top_k > V) return SDV_EINVAL;
+  if ((tokens == nullptr) != (logprob == nullptr)) return SDV_EINVAL;
+  if (top_k && (!top_ids || !top_logprob)) return SDV_EINVAL;
+  if (!logprob && !entropy && !row_max && !log_sum && !top_k && !status) return SDV_EINVAL;
+  const void* four[] = {tokens, logprob, entropy, row_max, log_sum, top_ids, top_logprob, status};
+  for (const void* p : four)
+    if (!aligned_to(p, 4)) return SDV_EALIGN;
+  const ScoreArgs A{logits, row_stride, V, tokens, kLog2E / temperature, 1.f / temperature, top_k, logprob, entropy,
+                    row_max, log_sum, top_ids, top_logprob, status};
+  cudaStream_t s = (cudaStream_t)stream;
+  return launched(dtype == SDV_F32    ? launch_scores<SDV_F32>(A, N, dtype, s)
+                  : dtype == SDV_BF16 ? launch_scores<SDV_BF16>(A, N, dtype, s)
+                                      : launch_scores<SDV_F16>(A, N, dtype, s));
+}
+
+int sdv_token_scores_grad(const void* logits, int64_t row_stride, int N, int V, int dtype, const int32_t* tokens,
+                          float temperature, const float* row_max, const float* log_sum, const float* entropy,
+                          const float* g_logprob, const float* g_entropy, void* d_logits, int64_t d_stride,
+                          sdv_stream_t stream) {
+  if (N == 0) return token_dtype(dtype) && V >= 1 ? SDV_OK : SDV_EINVAL;
+  int rc = check_rows(logits, row_stride, N, V, dtype, temperature);
+  if (rc) return rc;
+  if (N > (1 << 25) || d_stride < V || !d_logits || !row_max || !log_sum) return SDV_EINVAL;
+  if ((!g_logprob && !g_entropy) || (tokens == nullptr) != (g_logprob == nullptr) || (g_entropy && !entropy)) return SDV_EINVAL;
+  if (!aligned_to(d_logits, elem_bytes(dtype))) return SDV_EALIGN;
+  const void* four[] = {tokens, row_max, log_sum, entropy, g_logprob, g_entropy};
+  for (const void* p : four)
+    if (!aligned_to(p, 4)) return SDV_EALIGN;
+  const GradArgs G{logits, row_stride, V, tokens, kLog2E / temperature, 1.f / temperature, row_max, log_sum, entropy,
+                   g_logprob, g_entropy, d_logits, d_stride};
+  cudaStream_t s = (cudaStream_t)stream;
+  return launched(dtype == SDV_F32    ? launch_grad<SDV_F32>(G, N, dtype, s)
+                  : dtype == SDV_BF16 ? launch_grad<SDV_BF16>(G, N, dtype, s)
+                                      : launch_grad<SDV_F16>(G, N, dtype, s));
+}
+
+int sdv_token_scores_train(const void* logits, int64_t row_stride, int N, int V, int dtype, const int32_t* tokens,
+                           float temperature, const float* g_logprob, const float* g_entropy, float* logprob,
+                           float* entropy, float* row_max, float* log_sum, uint32_t* status, void* d_logits,
+                           int64_t d_stride, sdv_stream_t stream) {
+  if (N == 0) return token_dtype(dtype) && V >= 1 ? SDV_OK : SDV_EINVAL;
+  int rc = check_rows(logits, row_stride, N, V, dtype, temperature);
+  if (rc) return rc;
+  if (N > (1 << 27) || d_stride < V || !d_logits || !entropy || !row_max || !log_sum) return SDV_EINVAL;
+  if ((!g_logprob && !g_entropy) || (tokens == nullptr) != (logprob == nullptr) || (g_logprob && !tokens)) return SDV_EINVAL;
+  if (!aligned_to(d_logits, elem_bytes(dtype))) return SDV_EALIGN;
+  const void* four[] = {tokens, g_logprob, g_entropy, logprob, entropy, row_max, log_sum, status};
+  for (const void* p : four)
+    if (!aligned_to(p, 4)) return SDV_EALIGN;
+  const int C = train_cluster(V, dtype);
+  if (!C) {                                   // rows that no cluster holds: read twice
+    rc = sdv_token_scores(logits, row_stride, N, V, dtype, tokens, temperature, 0, logprob, entropy, row_max, log_sum,
+                          nullptr, nullptr, status, stream);
+    if (rc) return rc;
+    return sdv_token_scores_grad(logits, row_stride, N, V, dtype, g_logprob ? tokens : nullptr, temperature, row_max,
+                                 log_sum, entropy, g_logprob, g_entropy, d_logits, d_stride, stream);
+  }
+  const TrainArgs A{ScoreArgs{logits, row_stride, V, tokens, kLog2E / temperature, 1.f / temperature, 0, logprob, entropy,
+                              row_max, log_sum, nullptr, nullptr, status},
+                    g_logprob, g_entropy, d_logits, d_stride};
+  cudaStream_t s = (cudaStream_t)stream;
+  return launched(dtype == SDV_F32    ? launch_train<SDV_F32>(A, N, C, s)
+                  : dtype == SDV_BF16 ? launch_train<SDV_BF16>(A, N, C, s)
+                                      : launch_train<SDV_F16>(A, N, C, s));
+}
+
+}  // extern "C"

@@ -1,0 +1,208 @@
+// sdv_tokens.cuh - what the token operators' kernels share: rows of logits read as 16-byte
+// vectors from wherever they start, running softmax statistics, clusters.
+#pragma once
+
+#include <cooperative_groups.h>
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "../../include/specdiff.h"
+#include "sdv_host.h"
+
+namespace sdv {
+
+namespace cg = cooperative_groups;
+
+constexpr float kLog2E = 1.44269504088896341f;   // log2 e
+constexpr float kLn2f = 0.69314718055994531f;    // log 2
+// Far below any difference of two logits that leaves a probability, and finite: 0 * kFar is 0
+// where 0 * -inf would be NaN.
+constexpr float kFar = -1e30f;
+
+template <int kDtype>
+struct Num;
+template <>
+struct Num<SDV_F32> {
+  using T = float;
+  static constexpr int kPer16 = 4;
+  static __device__ __forceinline__ float to(T x) { return x; }
+  static __device__ __forceinline__ T from(float x) { return x; }
+  static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <>
+struct Num<SDV_BF16> {
+  using T = __nv_bfloat16;
+  static constexpr int kPer16 = 8;
+  static __device__ __forceinline__ float to(T x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ T from(float x) { return __float2bfloat16_rn(x); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Num<SDV_F16> {
+  using T = __half;
+  static constexpr int kPer16 = 8;
+  static __device__ __forceinline__ float to(T x) { return __half2float(x); }
+  static __device__ __forceinline__ T from(float x) { return __float2half_rn(x); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = p.x;
+      f[2 * i + 1] = p.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// A row of V elements as `head` single elements up to the next 16-byte boundary, `nvec`
+// vectors and `tail` single elements.
+template <int kDtype>
+struct Row {
+  using T = typename Num<kDtype>::T;
+  static constexpr int kPer = Num<kDtype>::kPer16;
+  const T* p;
+  int V, head, nvec, tail;
+  __device__ __forceinline__ Row(const T* row, int V_) : p(row), V(V_) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    head = off ? min(V, kPer - off) : 0;
+    nvec = (V - head) / kPer;
+    tail = V - head - nvec * kPer;
+  }
+  __device__ __forceinline__ const uint4* vec() const { return reinterpret_cast<const uint4*>(p + head); }
+  // Element of single i (the head's, then the tail's).
+  __device__ __forceinline__ int single(int i) const { return i < head ? i : V - tail + (i - head); }
+  __device__ __forceinline__ int singles() const { return head + tail; }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Maximum that keeps a NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// Running softmax statistics of x_v / T: the maximum m of x, s = sum e^{(x - m)/T} and
+// w = sum e^{(x - m)/T} (x - m).  A NaN or +inf logit shows as such in m.
+struct Stat {
+  float m, s, w;
+};
+__device__ __forceinline__ Stat stat_empty() { return Stat{-INFINITY, 0.f, 0.f}; }
+
+// c = log2(e) / T
+__device__ __forceinline__ void stat_rebase(Stat& a, float m, float c) {
+  const float d = fmaxf(a.m - m, kFar);          // a.m = -inf holds nothing: s = w = 0
+  const float f = ex2(d * c);
+  a.w = f * fmaf(a.s, d, a.w);
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
+  const float m = max_nan(a.m, b.m);
+  stat_rebase(a, m, c);
+  stat_rebase(b, m, c);
+  return Stat{m, a.s + b.s, a.w + b.w};
+}
+// Adds n values, in 32 bits each.
+template <int n>
+__device__ __forceinline__ void stat_add(Stat& a, const float* x, float c) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < n; ++i) top = max_nan(top, x[i]);
+  if (!(top <= a.m)) stat_rebase(a, max_nan(top, a.m), c);
+  const float m = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const float d = fmaxf(x[i] - m, kFar);
+    const float e = ex2(d * c);
+    a.s += e;
+    a.w = fmaf(e, d, a.w);
+  }
+}
+__device__ __forceinline__ Stat stat_warp(Stat a, float c) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    Stat b;
+    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+    b.w = __shfl_xor_sync(0xffffffffu, a.w, o);
+    a = stat_join(a, b, c);
+  }
+  return a;
+}
+
+// The order of the alternatives: the larger logit first, of equal ones the lower index.
+__device__ __forceinline__ bool before(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
+
+// A launch in clusters of `cluster` CTAs along x.
+template <typename Kern, typename... Args>
+inline cudaError_t launch_cluster(Kern kern, dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t s,
+                                  Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline size_t elem_bytes(int dtype) { return dtype == SDV_F32 ? 4 : 2; }
+inline bool token_dtype(int dtype) { return dtype == SDV_F32 || dtype == SDV_BF16 || dtype == SDV_F16; }
+
+// The return code of a launch.
+inline int launched(cudaError_t e) {
+  if (e == cudaSuccess) return SDV_OK;
+  cudaGetLastError();
+  set_last_cuda_error((int)e);
+  return SDV_ECUDA;
+}
+
+}  // namespace sdv
