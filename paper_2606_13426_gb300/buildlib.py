@@ -20,7 +20,7 @@ LIBDIR = os.path.join(PKG, "lib")
 LIBNAME = "libspecdiff.so"
 SOURCES = ["sdv_verify.cu", "sdv_chain_f32.cu", "sdv_chain_bf16.cu", "sdv_sampler.cu", "sdv_rounds_c8.cu",
            "sdv_rounds_c16.cu", "sdv_noalloc.cu", "sdv_scores.cu", "sdv_token_verify.cu", "sdv_cache.cu",
-           "sdv_attend.cu"]
+           "sdv_attend.cu", "sdv_attend_d64.cu", "sdv_attend_d128.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I" + INCLUDE,
               "-I" + CSRC]
