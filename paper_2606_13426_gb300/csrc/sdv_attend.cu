@@ -33,6 +33,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   A.bf16 = dtype == SDV_BF16;
   A.q_sb = q_stride_b, A.q_st = q_stride_t, A.q_sh = q_stride_h;
   A.c = CacheView{(uint8_t*)k_codes, (uint8_t*)v_codes, (float*)k_scale, (float*)v_scale, page_table, pages, max_pages, H, D, block};
+  A.cpb = chunk_div(block / kChunk);
   A.B = B, A.W = W, A.G = Hq / H, A.R = (int)R, A.RT = tiles.rt;
   A.lengths = lengths, A.counts = counts;
   A.scale2 = scale * kLog2E;

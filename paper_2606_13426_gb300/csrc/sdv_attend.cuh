@@ -27,8 +27,7 @@
 
 namespace sdv {
 
-constexpr int kAttWarps = 8;
-constexpr int kAttThreads = 32 * kAttWarps;
+constexpr int kJoinThreads = 256;
 constexpr int kTile = 64;                 // keys of a unit of work: two steps of kSub
 constexpr int kSub = 32;
 constexpr int kMaxNt = 5;                 // eights of rows of an item
@@ -36,11 +35,20 @@ constexpr float kNone = -3e38f;           // the reference of a row that has see
 constexpr float kSlack = 8.f;
 constexpr float kPScale = 128.f;          // f16 holds 2^kSlack * kPScale; what is below 2^-28 of the reference is lost
 
+// Division by the chunks of a page (up to 8) of numbers below 2^28: a product's upper half.
+struct ChunkDiv {
+  uint32_t magic, n;
+  __device__ __forceinline__ int over(int x) const { return magic ? (int)__umulhi((uint32_t)x, magic) : x; }
+  __device__ __forceinline__ int rest(int x) const { return x - over(x) * (int)n; }
+};
+inline ChunkDiv chunk_div(int n) { return ChunkDiv{n == 1 ? 0u : (uint32_t)((0x100000000ull + n - 1) / n), (uint32_t)n}; }
+
 struct AttendArgs {
   const void* q;
   bool bf16;
   int64_t q_sb, q_st, q_sh;
   CacheView c;
+  ChunkDiv cpb;
   int B, W, G, R, RT;                      // rows W * G, row tiles
   const int32_t* lengths;
   const int32_t* counts;
@@ -130,19 +138,28 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from, bool real) 
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(n));
 }
 
+// A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others under
+// way.  Few rows leave registers for sixteen warps, whose latencies overlap; more rows take
+// eight.
 template <int kD, int kNt>
 struct AttendShape {
+  static constexpr int kWarps = kNt <= 2 ? 16 : 8;
+  static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRows = 8 * kNt;
   static constexpr int kSlot = kRows * (kD + 2);         // floats of a partial: rows' output, max, sum
-  static constexpr int kStage = 2 * kSub * kD;            // bytes: keys, then values
-  static constexpr int kStages = kD == 128 ? 3 : 6;
+  static constexpr int kHalf = kSub * kD;                 // bytes
+  static constexpr int kHalves = (kWarps == 16 ? 3 : 5) * (kD == 64 ? 2 : 1) - (kD == 64 ? 1 : 0);
+  static constexpr int kAhead = (kHalves - 1) / 2;        // steps
+  static constexpr int kScaleSlots = kAhead + 1;
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
-  static constexpr int kRing = kAttWarps * kStages * kStage;
-  static constexpr int kQBytes = kNt * kKv * 2 * 32 * 16;
-  static constexpr int kScaleBytes = kAttWarps * kStages * 32;   // of a stage: ks, vs of both chunks; absent chunks
-  static constexpr size_t kSmem = (size_t)kRing + kQBytes + kScaleBytes;
   static constexpr int kOutStride = kD + 4;
-  static_assert(kAttWarps * kRows * kOutStride * 4 <= kRing, "the warps' outputs join in the ring");
+  static constexpr int kRing = kWarps * kHalves * kHalf;
+  static constexpr int kJoin = kWarps * kRows * kOutStride * 4;   // the warps' outputs join in its place
+  static constexpr int kQAt = kRing > kJoin ? kRing : kJoin;
+  static constexpr int kQBytes = kNt * kKv * 2 * 32 * 16;
+  static constexpr int kScaleBytes = kWarps * kScaleSlots * 32;   // of a step: ks, vs of both chunks; absent chunks
+  static constexpr size_t kSmem = (size_t)kQAt + kQBytes + kScaleBytes;
+  static_assert(kHalves % 2 == 1 && kSmem <= 220 * 1024, "");
 };
 
 // Writes four elements of row `row` of an item's results, and its log sum with the first of them.
@@ -170,8 +187,9 @@ __device__ __forceinline__ float q_value(const AttendArgs& A, int64_t at) {
 }
 
 template <int kD, int kNt>
-__global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
+__global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
+  constexpr int kAttWarps = S::kWarps, kAttThreads = S::kThreads;
   constexpr int kKv = S::kKv;
   constexpr int kMt = kD / 16;                             // sixteens of the output
   constexpr int kR = 2 * kNt;                              // rows of a thread: 8 n + 2 t + e
@@ -183,9 +201,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
   __shared__ float wm[kAttWarps][S::kRows], wl[kAttWarps][S::kRows];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int H = A.c.H, per = H * A.RT;                     // items of a sequence
-  uint8_t* ring = smem + warp * S::kStages * S::kStage;
-  uint4* qf = reinterpret_cast<uint4*>(smem + S::kRing);
-  float* scales = reinterpret_cast<float*>(smem + S::kRing + S::kQBytes) + warp * S::kStages * 8;
+  uint8_t* ring = smem + warp * S::kHalves * S::kHalf;
+  uint4* qf = reinterpret_cast<uint4*>(smem + S::kQAt);
+  float* scales = reinterpret_cast<float*>(smem + S::kQAt + S::kQBytes) + warp * S::kScaleSlots * 8;
 
   const int64_t units = tile_sums(A, 0, red).total * per;
   const int runs = (int)min((int64_t)A.ctas, units);       // none of them empty
@@ -233,49 +251,63 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
     const int tile0 = (int)(u - item_u);
     const int tile1 = (int)min((int64_t)sq.tiles, u_end - item_u);
     const int32_t* table = A.c.table + (int64_t)b * A.c.max_pages;
-    const int cpb = A.c.block / kChunk;                    // chunks of a page
     // this warp's steps: two of every kAttWarps-th unit
     const int steps = tile1 - tile0 > warp ? 2 * ((tile1 - tile0 - warp - 1) / kAttWarps + 1) : 0;
     auto key_of = [&](int n) { return (sq.first + tile0 + warp + (n >> 1) * kAttWarps) * kTile + (n & 1) * kSub; };
     // the page of the chunk of 16 tokens from `key` on, or -1 where there is none
     auto page_of = [&](int key) {
       if (key >= sq.len) return -1;
-      const int chunk = key / kChunk;
-      const int p = table[chunk / cpb];
-      if (p >= 0 && p < A.c.pages) return p;
+      const int p = table[A.cpb.over(key / kChunk)];
+      if (p >= 0 && p < (int)A.c.pages) return p;
       if (A.status && lane == 0) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
       return -1;
     };
-    auto issue = [&](int n, int stage, int p0, int p1) {   // the copies of step n into a stage
-      const uint32_t to = smem_addr(ring + stage * S::kStage);
+    // The copies of a step's keys (and scales) or values into a half.  Lanes take the pieces of
+    // whole keys, in the order of memory, to where the threads read them as fragments.
+    constexpr int kPieces = kD / 16, kKeysOf = 32 / kPieces;   // pieces of a key; keys of one copy of the warp
+    const int lk = lane / kPieces, lp = lane % kPieces;
+    int key_to;                                                // this lane's place of copy 0, and what copy j adds
+    if (kD == 128) key_to = ((lk >> 1) * kKv + (lp >> 2)) * 512 + ((lk & 1) * 4 + (lp & 3)) * 16;
+    else key_to = ((lk >> 2 & 1) * 2 + (lk >> 1 & 1)) * 512 + ((lk & 1) * 4 + lp) * 16;
+    const int64_t head_keys = (int64_t)h * A.c.block;
+    auto issue_keys = [&](int n, int half, int slot, int p0, int p1) {
+      const uint32_t to = smem_addr(ring + half * S::kHalf) + key_to;
       const int c = key_of(n) / kChunk;
-      const int o0 = c % cpb * kChunk, o1 = (c + 1) % cpb * kChunk;
-      const int64_t h0 = (int64_t)max(p0, 0) * H + h, h1 = (int64_t)max(p1, 0) * H + h;
-      constexpr int kPieces = kD / 16;                      // of a key
-      const int piece = lane % kPieces;
+      const int o0 = A.cpb.rest(c) * kChunk, o1 = A.cpb.rest(c + 1) * kChunk;
+      const int64_t h0 = (int64_t)max(p0, 0) * H, h1 = (int64_t)max(p1, 0) * H;
+      const uint8_t* k0 = A.c.k + (h0 * A.c.block + head_keys + o0 + lk) * kD + lp * 16;
+      const uint8_t* k1 = A.c.k + (h1 * A.c.block + head_keys + o1 + lk) * kD + lp * 16;
+      constexpr int kCopies = kSub / kKeysOf;
 #pragma unroll
-      for (int j = 0; j < kSub * kPieces / 32; ++j) {
-        const int tok = j * (32 / kPieces) + lane / kPieces;
-        const bool second = j >= kSub * kPieces / 64;       // the second chunk's tokens
-        const uint8_t* from = A.c.k + ((second ? h1 : h0) * A.c.block + (second ? o1 : o0) + (tok & 15)) * kD + piece * 16;
-        const int gg = 2 * (tok >> 3) + (tok & 1), sh = (tok >> 2 & 1) * 2 + (tok >> 1 & 1);
-        copy16(to + ((sh * kKv + (piece >> 2)) * 32 + gg * 4 + (piece & 3)) * 16, from, second ? p1 >= 0 : p0 >= 0);
+      for (int j = 0; j < kCopies; ++j) {
+        // token kKeysOf j + lk is of column pair j / 2 (D = 128) or j (D = 64), step j % 2 or lk's
+        const int add = kD == 128 ? (j & 1) * 2 * kKv * 512 + (j >> 1) * 2 * 64 : j * 2 * 64;
+        const bool second = j >= kCopies / 2;
+        copy16(to + add, (second ? k1 : k0) + (j % (kCopies / 2)) * kKeysOf * kD, second ? p1 >= 0 : p0 >= 0);
       }
-      const bool odd = lane & 1;
-      const uint8_t* vp = A.c.v + ((odd ? h1 : h0) * kD + (lane >> 1)) * A.c.block + (odd ? o1 : o0);
-#pragma unroll
-      for (int j = 0; j < kD / 16; ++j)
-        copy16(to + kSub * kD + (32 * j + lane) * 16, vp + (int64_t)(16 * j) * A.c.block, odd ? p1 >= 0 : p0 >= 0);
-      float* sc = scales + stage * 8;
+      float* sc = scales + slot * 8;
       if (lane < 4) {
-        const int64_t hh = lane & 2 ? h1 : h0;
+        const int64_t hh = (lane & 2 ? h1 : h0) + h;
         copy4(smem_addr(sc + lane), (lane & 1 ? A.c.vs : A.c.ks) + hh, (lane & 2 ? p1 : p0) >= 0);
       }
       if (lane == 0) sc[4] = __int_as_float((p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0));
+      asm volatile("cp.async.commit_group;");
     };
+    auto issue_values = [&](int n, int half, int p0, int p1) {
+      const uint32_t to = smem_addr(ring + half * S::kHalf) + lane * 16;
+      const int c = key_of(n) / kChunk + (lane & 1), p = lane & 1 ? p1 : p0;
+      const uint8_t* from = A.c.v + (((int64_t)max(p, 0) * H + h) * kD + (lane >> 1)) * A.c.block + A.cpb.rest(c) * kChunk;
+      const int64_t stride = 16 * A.c.block;
+#pragma unroll
+      for (int j = 0; j < kD / 16; ++j) {
+        copy16(to + 512 * j, from, p >= 0);
+        from += stride;
+      }
+      asm volatile("cp.async.commit_group;");
+    };
+    auto nothing = [] { asm volatile("cp.async.commit_group;"); };
     __syncthreads();                                       // the rows before these are done with shared memory
     int np0 = -1, np1 = -1;                                 // pages of the next step to issue
-    int next = 0;
     auto look = [&](int n) {
       if (n < steps) {
         np0 = page_of(key_of(n));
@@ -284,10 +316,15 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
     };
     look(0);
 #pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s) {
-      if (next < steps) issue(next, s, np0, np1);
-      asm volatile("cp.async.commit_group;");
-      look(++next);
+    for (int n = 0; n < S::kAhead; ++n) {
+      if (n < steps) {
+        issue_keys(n, 2 * n, n, np0, np1);
+        issue_values(n, 2 * n + 1, np0, np1);
+      } else {
+        nothing();
+        nothing();
+      }
+      look(n + 1);
     }
     // the rows' queries as fragments, in f16: bf16 rows are scaled by a power of two into its range
     for (int r = warp; r < S::kRows; r += kAttWarps) {
@@ -348,15 +385,17 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
       mx[k] = kNone;
       sum[k] = 0.f;
     }
-    int stage = 0;
+    int half = 0, slot = 0;                                 // of this step's keys
+    auto after = [](int x, int by, int of) { return x + by >= of ? x + by - of : x + by; };
     for (int n = 0; n < steps; ++n) {
-      if (next < steps) issue(next, stage == 0 ? S::kStages - 1 : stage - 1, np0, np1);
-      asm volatile("cp.async.commit_group;");
-      look(++next);
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1));
+      const int free_half = after(half, S::kHalves - 1, S::kHalves), free_slot = after(slot, S::kAhead, S::kScaleSlots);
+      if (n + S::kAhead < steps) issue_keys(n + S::kAhead, free_half, free_slot, np0, np1);
+      else nothing();
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
-      const uint8_t* from = ring + stage * S::kStage;
-      const float* sc = scales + stage * 8;
+      const uint8_t* from = ring + half * S::kHalf;
+      const uint8_t* values = ring + after(half, 1, S::kHalves) * S::kHalf;
+      const float* sc = scales + slot * 8;
       const int key0 = key_of(n);
       // scores: sx[s][n][0, 1] of key row g and rows 2t, 2t + 1; [2, 3] of key row g + 8
       float sx[2][kNt][4];
@@ -387,6 +426,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
           }
         }
       }
+      __syncwarp();                                          // the keys are read: their half is the next values'
+      if (n + S::kAhead < steps) issue_values(n + S::kAhead, half, np0, np1);
+      else nothing();
+      look(n + S::kAhead + 1);
       const int chunk = g >> 2;
       const float ks = sc[2 * chunk];
       float vs = sc[2 * chunk + 1];
@@ -404,6 +447,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
           sx[s][k >> 1][2 + (k & 1)] *= f;
         }
       }
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
+      __syncwarp();
       uint32_t drop = 0;                                   // which of this thread's 8 value tokens count as 0
       if (masked) {
         const int have = sq.len - key0 - 8 * t;
@@ -411,7 +456,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
         uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
 #pragma unroll
         for (int m = 0; m < 2 * kMt; ++m) {
-          const uint2 v = *reinterpret_cast<const uint2*>(from + kSub * kD + (m * 32 + lane) * 8);
+          const uint2 v = *reinterpret_cast<const uint2*>(values + (m * 32 + lane) * 8);
 #pragma unroll
           for (int e = 0; e < 8; ++e) nan_keys |= (uint32_t)(((e < 4 ? v.x : v.y) >> (8 * (e & 3)) & 0x7f) == 0x7f) << e;
         }
@@ -485,8 +530,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
           }
 #pragma unroll
       for (int m = 0; m < kMt; ++m) {
-        uint2 v0 = *reinterpret_cast<const uint2*>(from + kSub * kD + ((2 * m) * 32 + lane) * 8);
-        uint2 v1 = *reinterpret_cast<const uint2*>(from + kSub * kD + ((2 * m + 1) * 32 + lane) * 8);
+        uint2 v0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
+        uint2 v1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
         if (drop) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -505,7 +550,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
           for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
         }
       }
-      stage = stage + 1 == S::kStages ? 0 : stage + 1;
+      half = after(half, 2, S::kHalves);
+      slot = after(slot, 1, S::kScaleSlots);
       __syncwarp();
     }
     asm volatile("cp.async.wait_group 0;");
@@ -534,7 +580,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
     __syncthreads();
     const bool whole = tile0 == 0 && tile1 == sq.tiles;
     const int live = min(kAttWarps, tile1 - tile0);         // warps that had any
-    float* slot = A.part + ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * S::kSlot;
+    float* part = A.part + ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * S::kSlot;
     for (int i = tid; i < S::kRows * kD / 4; i += kAttThreads) {
       const int r = i / (kD / 4), d = i % (kD / 4) * 4;
       if (row0 + r >= A.R) break;
@@ -554,10 +600,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
       if (whole) {
         put_row<kD>(A, sq.count, b, h, row0 + r, d, o, m, l);
       } else {
-        *reinterpret_cast<float4*>(slot + r * kD + d) = o;
+        *reinterpret_cast<float4*>(part + r * kD + d) = o;
         if (d == 0) {
-          slot[S::kRows * kD + r] = m;
-          slot[S::kRows * kD + S::kRows + r] = l;
+          part[S::kRows * kD + r] = m;
+          part[S::kRows * kD + S::kRows + r] = l;
         }
       }
     }
@@ -569,9 +615,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_attend(const AttendArgs A) {
 // Joins the partials of an item that several CTAs' runs hold; an item without tiles gets zeros.
 // A CTA has eight rows of an item, a warp each.
 template <int kD, int kNt>
-__global__ void __launch_bounds__(kAttThreads) k_attend_join(const AttendArgs A) {
+__global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
-  __shared__ int64_t red[2 * kAttWarps];
+  __shared__ int64_t red[2 * (kJoinThreads / 32)];
   const int per = A.c.H * A.RT;
   const int rows8 = blockIdx.x % kNt, ib = blockIdx.x / kNt;
   const int b = ib / per, item = ib % per, h = item / A.RT, row0 = item % A.RT * S::kRows;
@@ -632,10 +678,10 @@ static cudaError_t launch_attend(const AttendArgs& A, cudaStream_t s) {
   using S = AttendShape<kD, kNt>;
   cudaError_t e = cudaFuncSetAttribute(k_attend<kD, kNt>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
-  k_attend<kD, kNt><<<(unsigned)A.ctas, kAttThreads, S::kSmem, s>>>(A);
+  k_attend<kD, kNt><<<(unsigned)A.ctas, S::kThreads, S::kSmem, s>>>(A);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  k_attend_join<kD, kNt><<<(unsigned)((int64_t)A.B * A.c.H * A.RT * kNt), kAttThreads, 0, s>>>(A);
+  k_attend_join<kD, kNt><<<(unsigned)((int64_t)A.B * A.c.H * A.RT * kNt), kJoinThreads, 0, s>>>(A);
   return cudaGetLastError();
 }
 template <int kD>
