@@ -4,6 +4,8 @@ PyTorch provides device memory and the current stream only; every step of the
 verification path runs in libspecdiff's kernels.  Inputs must be CUDA tensors
 (this module never computes anything itself and has no CPU path).
 """
+import functools
+
 import torch
 
 from . import binding as B
@@ -356,9 +358,7 @@ def em_sample(Bn, target, seed):
 
 def _dense(what, t, dtype, shape):
     """A contiguous CUDA tensor of the type and shape, or None."""
-    if t is None:
-        return
-    if not (t.is_cuda and t.is_contiguous()) or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()):
         raise ValueError("%s: a contiguous CUDA %s tensor of shape %s expected" % (what, dtype, tuple(shape)))
 
 
@@ -370,11 +370,22 @@ def _out(out, name, shape, dtype, dev):
     return t
 
 
+def _outs(out, names, n, dtype, dev):
+    """Outputs [n] of one type by name: the caller's, or rows of one allocation."""
+    if not out:
+        return dict(zip(names, torch.empty(len(names), n, dtype=dtype, device=dev).unbind(0)))
+    return {k: _out(out, k, (n,), dtype, dev) for k in names}
+
+
+_attend_workspace = functools.lru_cache(maxsize=None)(B.sdv_attend_workspace_bytes)
+
+
 def _rows(what, t, dims):
     """A CUDA tensor of logits (or keys, queries) whose last axis is contiguous; its type's code."""
-    if not t.is_cuda or t.dim() != dims or t.dtype not in _TOKEN_DTYPES or t.stride(-1) != 1 and t.shape[-1] > 1:
+    dt = _TOKEN_DTYPES.get(t.dtype)
+    if dt is None or not t.is_cuda or t.dim() != dims or t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError("%s: a %d-d CUDA float32/bfloat16/float16 tensor with a contiguous last axis expected" % (what, dims))
-    return _TOKEN_DTYPES[t.dtype]
+    return dt
 
 
 def _row_stride(t):
@@ -390,13 +401,8 @@ def token_scores(logits, tokens=None, *, top_k=0, temperature=1.0, entropy=True,
     N, V = logits.shape
     dev, f32 = logits.device, torch.float32
     _dense("tokens", tokens, torch.int32, (N,))
-    r = {}
-    if tokens is not None:
-        r["logprob"] = _out(out, "logprob", (N,), f32, dev)
-    if entropy:
-        r["entropy"] = _out(out, "entropy", (N,), f32, dev)
-    r["row_max"] = _out(out, "row_max", (N,), f32, dev)
-    r["log_sum"] = _out(out, "log_sum", (N,), f32, dev)
+    names = ("row_max", "log_sum") + (("logprob",) if tokens is not None else ()) + (("entropy",) if entropy else ())
+    r = _outs(out, names, N, f32, dev)
     r["status"] = _out(out, "status", (N,), torch.int32, dev)
     if top_k:
         r["top_ids"] = _out(out, "top_ids", (N, top_k), torch.int32, dev)
@@ -447,7 +453,7 @@ def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temper
     _dense("tokens", tokens, torch.int32, (N,))
     _dense("g_logprob", g_logprob, f32, (N,))
     _dense("g_entropy", g_entropy, f32, (N,))
-    r = {k: _out(out, k, (N,), f32, dev) for k in ("logprob", "entropy", "row_max", "log_sum") if k != "logprob" or tokens is not None}
+    r = _outs(out, ("entropy", "row_max", "log_sum") + (("logprob",) if tokens is not None else ()), N, f32, dev)
     r["status"] = _out(out, "status", (N,), torch.int32, dev)
     r["d_logits"] = dx = _grad_like(logits, d_logits)
     B._call("sdv_token_scores_train", logits.data_ptr(), _row_stride(logits), N, V, dt, _ptr(tokens), float(temperature),
@@ -473,8 +479,8 @@ def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L
     _dense("L_eff", L_eff, i32, (Bn,))
     _dense("coins", coins, f32, (Bn, L))
     _dense("race", race, f32, (Bn, V))
-    r = dict(accepted_len=_out(out, "accepted_len", (Bn,), i32, dev), next_token=_out(out, "next_token", (Bn,), i32, dev),
-             log_ratio=_out(out, "log_ratio", (Bn, L), f32, dev), status=_out(out, "status", (Bn,), i32, dev))
+    r = _outs(out, ("accepted_len", "next_token", "status"), Bn, i32, dev)
+    r["log_ratio"] = _out(out, "log_ratio", (Bn, L), f32, dev)
     B._call("sdv_token_verify", target_logits.data_ptr(), target_logits.stride(0), _row_stride(target_logits),
             draft_logits.data_ptr(), draft_logits.stride(0), _row_stride(draft_logits), tokens.data_ptr(), Bn, L, V, dt,
             float(temperature), float(temperature if draft_temperature is None else draft_temperature), _MODES[mode],
@@ -535,7 +541,7 @@ def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span
     dev = q.device
     r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
     if workspace is None:
-        workspace = torch.empty(max(B.sdv_attend_workspace_bytes(W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(_attend_workspace(W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
     B._call("sdv_cache_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
             cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
             page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),

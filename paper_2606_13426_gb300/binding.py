@@ -148,7 +148,9 @@ def _bind_native(lib):
         warnings.warn("libspecdiff: calls go through ctypes (%s)" % e)
         return
     for name, fn in (("sdv_verify_ex", mod.verify), ("sdv_verify_pipelined", mod.verify),
-                     ("sdv_log_ratios", mod.ratios)):
+                     ("sdv_log_ratios", mod.ratios), ("sdv_token_scores", mod.scores),
+                     ("sdv_token_scores_train", mod.train), ("sdv_token_verify", mod.token_verify),
+                     ("sdv_cache_append", mod.append), ("sdv_cache_attend", mod.attend)):
         _fns[name] = functools.partial(fn, ctypes.cast(getattr(lib, name), ctypes.c_void_p).value)
 
 

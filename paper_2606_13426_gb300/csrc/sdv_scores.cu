@@ -12,7 +12,7 @@
 namespace sdv {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScoreUnroll = 4;        // 16-byte vectors in flight per thread
+constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread: all under way at once, and kept
 constexpr int kGroups = 64;            // groups of threads whose maxima give the alternatives' threshold
 constexpr int kCandMax = 512;          // candidates a CTA ranks; more: k passes over its part
 constexpr int kScoreMaxCluster = 8;
@@ -94,8 +94,49 @@ __device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put
   }
 }
 
-template <int kDtype, bool kTop>
-__global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
+// A thread's part of a row: vectors v0 + tid + u kThreads < v1 (kept as read, where kKeep), and one
+// of the row's single elements.
+template <int kDtype, int kThreads>
+struct Part {
+  using E = Num<kDtype>;
+  const uint4* vec;
+  int v0, v1, single;
+  float x;
+  uint4 raw[kScoreVecs];
+  __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int C) {
+    vec = R.vec();
+    v0 = (int)((int64_t)R.nvec * rank / C) + (int)threadIdx.x;
+    v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
+    single = rank == 0 && (int)threadIdx.x < R.singles() ? R.single(threadIdx.x) : -1;
+    x = single >= 0 ? E::to(R.p[single]) : 0.f;
+  }
+  __device__ __forceinline__ bool has(int u) const { return v0 + u * kThreads < v1; }
+  // Statistics; the vectors are (the last kScoreVecs of them stay) in raw.
+  __device__ __forceinline__ Run read(float c) {
+    Run r = run_empty();
+    for (;;) {
+#pragma unroll
+      for (int u = 0; u < kScoreVecs; ++u)
+        if (has(u)) raw[u] = vec[v0 + u * kThreads];
+#pragma unroll
+      for (int u = 0; u < kScoreVecs; ++u)
+        if (has(u)) {
+          float f[E::kPer16];
+          run_see(r, vec_max<kDtype>(raw[u]), c);
+          E::unpack(raw[u], f);
+          run_add<E::kPer16>(r, f, c);
+        }
+      if (v0 + kScoreVecs * kThreads >= v1) break;
+      v0 += kScoreVecs * kThreads;
+    }
+    if (single >= 0) run_one(r, x, c);
+    return r;
+  }
+};
+
+// kKept: a CTA's part of the row fits its registers, and is not read again for the alternatives.
+template <int kDtype, bool kTop, bool kKept>
+__global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
@@ -106,8 +147,9 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
   const int tid = threadIdx.x;
   __shared__ Stat wstat[kWarps];
   __shared__ Stat cstat[kScoreMaxCluster];
+  __shared__ int listed[kScoreMaxCluster];
   __shared__ float tmax[kTop ? kScoreThreads : 1];
-  __shared__ float gmax[kTop ? kGroups : 1];
+  __shared__ __align__(16) float gmax[kTop ? kGroups : 4];
   __shared__ float thr_s[2];
   __shared__ int ncand;
   __shared__ Cand cand[kTop ? kCandMax : 1];
@@ -116,39 +158,18 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
   if (C > 1) cl.barrier_arrive();
   const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
   const Row<kDtype> R(row, A.V);
-  const int v0 = (int)((int64_t)R.nvec * rank / C), v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
-  const uint4* vec = R.vec();
-  Stat a = stat_empty();
-  int v = v0 + tid;
-  for (; v + (kScoreUnroll - 1) * kScoreThreads < v1; v += kScoreUnroll * kScoreThreads) {
-    uint4 raw[kScoreUnroll];
-#pragma unroll
-    for (int u = 0; u < kScoreUnroll; ++u) raw[u] = __ldg(vec + v + u * kScoreThreads);
-#pragma unroll
-    for (int u = 0; u < kScoreUnroll; ++u) {
-      float f[kPer];
-      E::unpack(raw[u], f);
-      stat_add<kPer>(a, f, A.c);
-    }
-  }
-  for (; v < v1; v += kScoreThreads) {
-    float f[kPer];
-    E::unpack(__ldg(vec + v), f);
-    stat_add<kPer>(a, f, A.c);
-  }
-  if (rank == 0 && tid < R.singles()) {
-    const float f = E::to(row[R.single(tid)]);
-    stat_add<1>(a, &f, A.c);
-  }
-  const float tm = a.m;                       // the largest of this thread's logits
-  a = stat_warp(a, A.c);
+  Part<kDtype, kScoreThreads> P(R, rank, C);
+  const int first = P.v0;
+  const Run run = P.read(A.c);
+  const float tm = run.top;                   // the largest of this thread's logits
+  Stat a = stat_warp(run_stat(run, A.c), A.c);
   if ((tid & 31) == 0) wstat[tid >> 5] = a;
   if (kTop) {
     tmax[tid] = tm;
     if (tid == 0) ncand = 0;
   }
   __syncthreads();
-  if (tid == 0) {
+  if (tid == kScoreThreads - 32) {            // (a warp that has nothing to do with the threshold)
     a = wstat[0];
     for (int w = 1; w < kWarps; ++w) a = stat_join(a, wstat[w], A.c);
     wstat[0] = a;
@@ -157,14 +178,19 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
     // At least k of the part's logits are at or above the k-th largest of the groups' maxima.
     if (tid < kGroups) {
       float g = tmax[tid];
-      for (int j = tid + kGroups; j < kScoreThreads; j += kGroups) g = fmaxf(g, tmax[j]);
+#pragma unroll
+      for (int j = kGroups; j < kScoreThreads; j += kGroups) g = fmaxf(g, tmax[tid + j]);
       gmax[tid] = g;
     }
     __syncthreads();
     if (tid < kGroups) {
       const float g = gmax[tid];
       int above = 0;
-      for (int j = 0; j < kGroups; ++j) above += gmax[j] > g;
+#pragma unroll
+      for (int j = 0; j < kGroups; j += 4) {
+        const float4 o = *reinterpret_cast<const float4*>(gmax + j);
+        above += (o.x > g) + (o.y > g) + (o.z > g) + (o.w > g);
+      }
       float t = above < A.top_k ? g : INFINITY;
 #pragma unroll
       for (int o = 16; o; o >>= 1) t = fminf(t, __shfl_xor_sync(0xffffffffu, t, o));
@@ -178,36 +204,46 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
         if (at < kCandMax) cand[at] = Cand{x, i};
       }
     };
-    if (tm >= thr) {
-      for (v = v0 + tid; v < v1; v += kScoreThreads) {
+    auto keep_vec = [&](const uint4& raw, int v) {
+      if (vec_max<kDtype>(raw) >= thr) {
         float f[kPer];
-        E::unpack(__ldg(vec + v), f);
+        E::unpack(raw, f);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) keep(f[e], R.head + v * kPer + e);
       }
-      if (rank == 0 && tid < R.singles()) keep(E::to(row[R.single(tid)]), R.single(tid));
+    };
+    if (tm >= thr) {
+      if constexpr (kKept) {
+#pragma unroll
+        for (int u = 0; u < kScoreVecs; ++u)
+          if (P.has(u)) keep_vec(P.raw[u], P.v0 + u * kScoreThreads);
+      } else {
+#pragma unroll 4
+        for (int v = first; v < P.v1; v += kScoreThreads) keep_vec(__ldg(P.vec + v), v);
+      }
+      if (P.single >= 0) keep(P.x, P.single);
     }
     __syncthreads();
     if (C > 1) cl.barrier_wait();               // the leader has started: its lists can be written
-    Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * SDV_MAX_TOP;
-    const int nc = ncand;
+    Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * A.top_k;
+    int nc = ncand;
     if (nc <= kCandMax) {
       rank_candidates(cand, nc, A.top_k, [&](int r, Cand c) { mine[r] = c; });
-      if (tid >= nc && tid < A.top_k) mine[tid] = Cand{-INFINITY, -1};
+      nc = min(nc, A.top_k);
     } else {                                      // many equal logits: one alternative per pass
       Cand last{INFINITY, -1};
-      for (int r = 0; r < A.top_k; ++r) {
+      for (nc = 0; nc < A.top_k; ++nc) {
         Cand b{-INFINITY, 0x7fffffff};
         auto see = [&](float x, int i) {
           if (x > -INFINITY && before(last.x, last.i, x, i) && before(x, i, b.x, b.i)) b = Cand{x, i};
         };
-        for (v = v0 + tid; v < v1; v += kScoreThreads) {
+        for (int v = first; v < P.v1; v += kScoreThreads) {
           float f[kPer];
-          E::unpack(__ldg(vec + v), f);
+          E::unpack(__ldg(P.vec + v), f);
 #pragma unroll
           for (int e = 0; e < kPer; ++e) see(f[e], R.head + v * kPer + e);
         }
-        if (rank == 0 && tid < R.singles()) see(E::to(row[R.single(tid)]), R.single(tid));
+        if (P.single >= 0) see(P.x, P.single);
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
           const float ox = __shfl_xor_sync(0xffffffffu, b.x, o);
@@ -220,17 +256,17 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
         b = best_w[0];
         for (int w = 1; w < kWarps; ++w)
           if (before(best_w[w].x, best_w[w].i, b.x, b.i)) b = best_w[w];
-        if (tid == 0) mine[r] = b.x > -INFINITY ? b : Cand{-INFINITY, -1};
+        if (!(b.x > -INFINITY)) break;
+        if (tid == 0) mine[nc] = b;
         last = b;
       }
     }
+    if (tid == 0) (C > 1 ? cl.map_shared_rank(listed, 0) : listed)[rank] = nc;
   } else {
+    __syncthreads();
     if (C > 1) cl.barrier_wait();
   }
-  if (tid == 0) {
-    Stat* to = C > 1 ? cl.map_shared_rank(cstat, 0) : cstat;
-    to[rank] = wstat[0];
-  }
+  if (tid == 0) (C > 1 ? cl.map_shared_rank(cstat, 0) : cstat)[rank] = wstat[0];
   if (C > 1) {
     cl.sync();
     if (rank) return;
@@ -249,21 +285,22 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores(const ScoreArgs A) {
       A.top_ids[n * k + r] = none ? -1 : c.i;
       A.top_lp[n * k + r] = bad ? NAN : (none ? -INFINITY : (c.x - a.m) * A.inv_t - log_s);
     };
-    // the CTAs' lists, placeholders left out, one behind the other
     int total = 0;
-    for (int i = tid; i < C * k; i += kScoreThreads) {
-      const Cand me = lists[(i / k) * SDV_MAX_TOP + i % k];
-      if (me.i < 0) continue;
-      int r = 0;
-      for (int j = 0; j < C * k; ++j) {
-        const Cand o = lists[(j / k) * SDV_MAX_TOP + j % k];
-        r += o.i >= 0 && before(o.x, o.i, me.x, me.i);
+    for (int r = 0; r < C; ++r) total += listed[r];
+    if (!bad)
+      for (int i = tid; i < C * k; i += kScoreThreads) {
+        const int q = i / k;
+        if (i - q * k >= listed[q]) continue;
+        const Cand me = lists[i];
+        int r = 0;
+        for (int p = 0; p < C; ++p) {
+          const int np = listed[p];
+          const Cand* l = lists + p * k;
+          for (int j = 0; j < np; ++j) r += before(l[j].x, l[j].i, me.x, me.i);
+        }
+        if (r < k) put(r, me);
       }
-      if (r < k) put(r, me);
-    }
-    for (int j = 0; j < C * k; ++j) total += lists[(j / k) * SDV_MAX_TOP + j % k].i >= 0;
-    if (bad) total = 0;
-    for (int r = total + tid; r < k; r += kScoreThreads) put(r, Cand{-INFINITY, -1});
+    for (int r = (bad ? 0 : total) + tid; r < k; r += kScoreThreads) put(r, Cand{-INFINITY, -1});
   }
 }
 
@@ -309,15 +346,28 @@ __device__ __forceinline__ float grad_of(const RowGrad& r, float x, float c) {
   const float p = ex2(fmaf(d, c, -r.ls2));
   return r.flat ? r.nan : p * fmaf(r.b, d, r.a);
 }
+__device__ __forceinline__ float grad_one(const RowGrad& r, float x, int i, float c) {
+  const float o = grad_of(r, x, c);
+  return i == r.t && !r.flat && x > -INFINITY ? o + r.g : o;
+}
 template <int kPer>
 __device__ __forceinline__ void grad_vec(const RowGrad& r, const float* f, float* o, int first, float c) {
+  const f32x2 m = pair(-r.m, -r.m), c2 = pair(c, c), l = pair(-r.ls2, -r.ls2), a = pair(r.a, r.a), b = pair(r.b, r.b);
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) o[e] = grad_of(r, f[e], c);
-  const unsigned at = (unsigned)(r.t - first);
-  if (r.t >= 0 && at < (unsigned)kPer && !r.flat) {
+  for (int e = 0; e < kPer; e += 2) {
+    const f32x2 d = far2(add2(pair(f[e], f[e + 1]), m));
+    const float2 t = unpair(fma2(d, c2, l));
+    const float2 y = unpair(mul2(pair(ex2(t.x), ex2(t.y)), fma2(b, d, a)));
+    o[e] = y.x;
+    o[e + 1] = y.y;
+  }
+  if (r.flat) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = r.nan;
+  } else if ((unsigned)(r.t - first) < (unsigned)kPer) {    // (t = -1: no token)
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-      if ((int)at == e && f[e] > -INFINITY) o[e] += r.g;
+      if (r.t - first == e && f[e] > -INFINITY) o[e] += r.g;
   }
 }
 // Stores a vector of results whose place need not be on a 16-byte boundary.
@@ -360,10 +410,7 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores_grad(const GradArgs A,
   }
   if (part == 0 && threadIdx.x < R.singles()) {
     const int i = R.single(threadIdx.x);
-    const float f = E::to(row[i]);
-    float o;
-    grad_vec<1>(g, &f, &o, i, A.c);
-    out[i] = E::from(o);
+    out[i] = E::from(grad_one(g, E::to(row[i]), i, A.c));
   }
 }
 
@@ -376,9 +423,9 @@ struct TrainArgs {
 };
 
 // Statistics and gradient with the row read once: each thread of the cluster keeps its part of
-// it, as read, in registers (kVecs vectors) while the statistics are joined.
-template <int kDtype, int kThreads, int kVecs>
-__global__ void __launch_bounds__(kThreads) k_scores_train(const TrainArgs A) {
+// it, as read, in registers while the statistics are joined.
+template <int kDtype, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_scores_train(const TrainArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
@@ -393,31 +440,13 @@ __global__ void __launch_bounds__(kThreads) k_scores_train(const TrainArgs A) {
   const T* row = reinterpret_cast<const T*>(A.S.x) + n * A.S.stride;
   T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
   const Row<kDtype> R(row, A.S.V);
-  const bool vec_out = same_phase<kDtype>(row, out);
-  const int v0 = (int)((int64_t)R.nvec * rank / C), v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
-  const uint4* vec = R.vec();
-  uint4 raw[kVecs];
-#pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
-    const int v = v0 + tid + u * kThreads;
-    if (v < v1) raw[u] = vec[v];
-  }
-  const int si = rank == 0 && tid < R.singles() ? R.single(tid) : -1;
-  const float sx = si >= 0 ? E::to(row[si]) : 0.f;
-  Stat a = stat_empty();
-#pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
-    if (v0 + tid + u * kThreads < v1) {
-      float f[kPer];
-      E::unpack(raw[u], f);
-      stat_add<kPer>(a, f, A.S.c);
-    }
-  }
-  if (si >= 0) stat_add<1>(a, &sx, A.S.c);
-  a = stat_warp(a, A.S.c);
+  Part<kDtype, kThreads> P(R, rank, C);
+  Stat a = stat_warp(run_stat(P.read(A.S.c), A.S.c), A.S.c);
   if ((tid & 31) == 0) wstat[tid >> 5] = a;
   Token tok{-1, 0.f};
   if (rank == 0 && tid == 0) tok = row_token<kDtype>(A.S, row, n);
+  const int t = A.S.tokens ? A.S.tokens[n] : -1;
+  const float g_lp = A.g_lp ? A.g_lp[n] : 0.f, g_h = A.g_h ? A.g_h[n] : 0.f;
   __syncthreads();
   if (C > 1) cl.barrier_wait();
   if (tid < C) {                              // every CTA of the cluster gets every CTA's statistics
@@ -432,30 +461,38 @@ __global__ void __launch_bounds__(kThreads) k_scores_train(const TrainArgs A) {
   for (int r = 1; r < C; ++r) a = stat_join(a, cstat[r], A.S.c);
   if (rank == 0 && tid == 0) write_row(A.S, n, a, tok);
   const float log_s = logf(a.s);
-  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, A.S.tokens ? A.S.tokens[n] : -1, A.S.V,
-                             A.g_lp ? A.g_lp[n] : 0.f, A.g_h ? A.g_h[n] : 0.f, A.S.inv_t);
+  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, t, A.S.V, g_lp, g_h, A.S.inv_t);
+  T* to = out + R.head + P.v0 * kPer;
+  if (same_phase<kDtype>(row, out)) {
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
-    const int v = v0 + tid + u * kThreads;
-    if (v < v1) {
-      float f[kPer], o[kPer];
-      E::unpack(raw[u], f);
-      grad_vec<kPer>(g, f, o, R.head + v * kPer, A.S.c);
-      put_vec<kDtype>(out + R.head + v * kPer, o, vec_out);
-    }
+    for (int u = 0; u < kScoreVecs; ++u)
+      if (P.has(u)) {
+        float f[kPer], o[kPer];
+        E::unpack(P.raw[u], f);
+        grad_vec<kPer>(g, f, o, R.head + (P.v0 + u * kThreads) * kPer, A.S.c);
+        put_vec<kDtype>(to + u * kThreads * kPer, o, true);
+      }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kScoreVecs; ++u)
+      if (P.has(u)) {
+        float f[kPer], o[kPer];
+        E::unpack(P.raw[u], f);
+        grad_vec<kPer>(g, f, o, R.head + (P.v0 + u * kThreads) * kPer, A.S.c);
+        put_vec<kDtype>(to + u * kThreads * kPer, o, false);
+      }
   }
-  if (si >= 0) {
-    float o;
-    grad_vec<1>(g, &sx, &o, si, A.S.c);
-    out[si] = E::from(o);
-  }
+  if (P.single >= 0) out[P.single] = E::from(grad_one(g, P.x, P.single, A.S.c));
 }
 
-// CTAs per row: as many as give every SM two CTAs, as long as each has some vectors per thread.
+// CTAs per row: as many as keep the row in their registers, and while there are fewer than two CTAs
+// an SM, as many as leave every thread a vector.
 static int score_cluster(int64_t N, int V, int dtype) {
   const int64_t nvec = (int64_t)V * (int64_t)elem_bytes(dtype) / 16;
   int c = 1;
-  while (c < kScoreMaxCluster && N * c < 2 * sm_count() && nvec / (2 * c) >= kScoreThreads) c *= 2;
+  while (c < kScoreMaxCluster && (nvec > (int64_t)c * kScoreThreads * kScoreVecs ||
+                                  (N * c < 2 * sm_count() && nvec >= 2 * c * kScoreThreads)))
+    c *= 2;
   return c;
 }
 
@@ -471,19 +508,24 @@ template <int kDtype>
 static cudaError_t launch_scores(const ScoreArgs& A, int N, int dtype, cudaStream_t s) {
   const int C = score_cluster(N, A.V, dtype);
   const dim3 grid((unsigned)(N * (int64_t)C));
-  if (A.top_k) return launch_cluster(k_scores<kDtype, true>, grid, kScoreThreads, 0, (unsigned)C, s, A);
-  return launch_cluster(k_scores<kDtype, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+  const int64_t nvec = ((int64_t)A.V * (int64_t)elem_bytes(dtype) + 15) / 16;
+  const bool kept = nvec <= (int64_t)C * kScoreThreads * kScoreVecs;
+  if (A.top_k && kept) return launch_cluster(k_scores<kDtype, true, true>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+  if (A.top_k) return launch_cluster(k_scores<kDtype, true, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+  return launch_cluster(k_scores<kDtype, false, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
 }
 
-constexpr int kTrainThreads = 512;
-constexpr int kTrainVecs = 8;
-
-// CTAs per row of k_scores_train: as few as hold it, 0 if the largest cluster does not.
-static int train_cluster(int V, int dtype) {
+// CTAs per row of k_scores_train and their threads: as few as hold the row; c = 0 if the largest
+// cluster does not.
+struct TrainShape {
+  int c, threads;
+};
+static TrainShape train_shape(int V, int dtype) {
   const int64_t nvec = ((int64_t)V * (int64_t)elem_bytes(dtype) + 15) / 16;
-  for (int c = 1; c <= kScoreMaxCluster; c *= 2)
-    if (nvec <= (int64_t)c * kTrainThreads * kTrainVecs) return c;
-  return 0;
+  for (int threads = 256; threads <= 512; threads *= 2)
+    for (int c = 1; c <= kScoreMaxCluster; c *= 2)
+      if (nvec <= (int64_t)c * threads * kScoreVecs) return TrainShape{c, threads};
+  return TrainShape{0, 0};
 }
 
 template <int kDtype>
@@ -496,9 +538,10 @@ static cudaError_t launch_grad(const GradArgs& G, int N, int dtype, cudaStream_t
 }
 
 template <int kDtype>
-static cudaError_t launch_train(const TrainArgs& A, int N, int C, cudaStream_t s) {
-  return launch_cluster(k_scores_train<kDtype, kTrainThreads, kTrainVecs>, dim3((unsigned)(N * (int64_t)C)), kTrainThreads, 0,
-                        (unsigned)C, s, A);
+static cudaError_t launch_train(const TrainArgs& A, int N, TrainShape t, cudaStream_t s) {
+  const dim3 grid((unsigned)(N * (int64_t)t.c));
+  if (t.threads == 256) return launch_cluster(k_scores_train<kDtype, 256>, grid, 256, 0, (unsigned)t.c, s, A);
+  return launch_cluster(k_scores_train<kDtype, 512>, grid, 512, 0, (unsigned)t.c, s, A);
 }
 
 }  // namespace sdv
@@ -562,8 +605,8 @@ int sdv_token_scores_train(const void* logits, int64_t row_stride, int N, int V,
   const void* four[] = {tokens, g_logprob, g_entropy, logprob, entropy, row_max, log_sum, status};
   for (const void* p : four)
     if (!aligned_to(p, 4)) return SDV_EALIGN;
-  const int C = train_cluster(V, dtype);
-  if (!C) {                                   // rows that no cluster holds: read twice
+  const TrainShape t = train_shape(V, dtype);
+  if (!t.c) {                                   // rows that no cluster holds: read twice
     rc = sdv_token_scores(logits, row_stride, N, V, dtype, tokens, temperature, 0, logprob, entropy, row_max, log_sum,
                           nullptr, nullptr, status, stream);
     if (rc) return rc;
@@ -574,9 +617,9 @@ int sdv_token_scores_train(const void* logits, int64_t row_stride, int N, int V,
                               row_max, log_sum, nullptr, nullptr, status},
                     g_logprob, g_entropy, d_logits, d_stride};
   cudaStream_t s = (cudaStream_t)stream;
-  return launched(dtype == SDV_F32    ? launch_train<SDV_F32>(A, N, C, s)
-                  : dtype == SDV_BF16 ? launch_train<SDV_BF16>(A, N, C, s)
-                                      : launch_train<SDV_F16>(A, N, C, s));
+  return launched(dtype == SDV_F32    ? launch_train<SDV_F32>(A, N, t, s)
+                  : dtype == SDV_BF16 ? launch_train<SDV_BF16>(A, N, t, s)
+                                      : launch_train<SDV_F16>(A, N, t, s));
 }
 
 }  // extern "C"

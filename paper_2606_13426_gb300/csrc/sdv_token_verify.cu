@@ -22,6 +22,7 @@ constexpr int kVerThreads = 512;
 constexpr int kVerWarps = kVerThreads / 32;
 constexpr int kVerMaxCluster = 8;
 constexpr int kVerSegs = 8;            // segments of a CTA's part of a row, a warp each
+constexpr int kBatch = 8;
 constexpr int kVerRows = 2 * SDV_MAX_L + 1;
 constexpr uint32_t kStreamRace = 7;
 
@@ -44,6 +45,10 @@ struct TokenVerifyArgs {
 
 struct Best {
   float x;
+  int i;
+};
+struct Racer {
+  float r, e;
   int i;
 };
 
@@ -112,6 +117,71 @@ __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, cons
   }
 }
 
+// Calls f(index, q, p, race) for this thread's share of part `part` of `parts` of the rows.
+template <int kDtype, typename F>
+__device__ __forceinline__ void each_race(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, const float* race,
+                                          int V, int part, int parts, int tid, F f) {
+  using E = Num<kDtype>;
+  constexpr int kPer = E::kPer16, kUn = kPer == 8 ? 2 : 4;
+  const Row<kDtype> R(q, V);
+  const bool whole = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0 && aligned16(race + R.head);
+  if (whole) {
+    const uint4* vq = R.vec();
+    const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
+    const float4* vr = reinterpret_cast<const float4*>(race + R.head);
+    const int v0 = (int)((int64_t)R.nvec * part / parts), v1 = (int)((int64_t)R.nvec * (part + 1) / parts);
+    for (int v = v0 + tid; v < v1; v += kUn * kVerThreads) {
+      uint4 a[kUn], b[kUn];
+      float4 e[kUn * kPer / 4];
+#pragma unroll
+      for (int u = 0; u < kUn; ++u) {
+        const int w = v + u * kVerThreads;
+        if (w < v1) {
+          a[u] = __ldg(vq + w);
+          b[u] = __ldg(vp + w);
+#pragma unroll
+          for (int k = 0; k < kPer / 4; ++k) e[u * (kPer / 4) + k] = __ldg(vr + (int64_t)w * (kPer / 4) + k);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kUn; ++u) {
+        const int w = v + u * kVerThreads;
+        if (w < v1) {
+          float x[kPer], y[kPer];
+          E::unpack(a[u], x);
+          E::unpack(b[u], y);
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) {
+            const float4 ev = e[u * (kPer / 4) + k / 4];
+            f(R.head + w * kPer + k, x[k], y[k], k % 4 == 0 ? ev.x : k % 4 == 1 ? ev.y : k % 4 == 2 ? ev.z : ev.w);
+          }
+        }
+      }
+    }
+    if (part == 0 && tid < R.singles()) {
+      const int i = R.single(tid);
+      f(i, E::to(q[i]), E::to(p[i]), race[i]);
+    }
+  } else {
+    const int e0 = (int)((int64_t)V * part / parts), e1 = (int)((int64_t)V * (part + 1) / parts);
+    for (int e = e0 + tid; e < e1; e += 8 * kVerThreads) {
+      float x[8], y[8], z[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = e + u * kVerThreads;
+        if (i < e1) {
+          x[u] = E::to(q[i]);
+          y[u] = E::to(p[i]);
+          z[u] = race[i];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (e + u * kVerThreads < e1) f(e + u * kVerThreads, x[u], y[u], z[u]);
+    }
+  }
+}
+
 template <int kDtype>
 __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyArgs A) {
   using E = Num<kDtype>;
@@ -152,39 +222,64 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
   const T* p0 = reinterpret_cast<const T*>(A.p) + b * A.p_sb;
   auto row_of = [&](int r) { return r <= n ? q0 + r * A.q_sr : p0 + (r - n - 1) * A.p_sr; };
-  // statistics: target rows 0 .. n, then draft rows 0 .. n - 1
+  // statistics: target rows 0 .. n, then draft rows 0 .. n - 1, a warp per segment of a row; the
+  // next kBatch vectors of each lane are under way while it works on the last ones
   const int parts = C * kVerSegs;
-  for (int u = warp; u < rows * kVerSegs; u += kVerWarps) {
-    const int r = u / kVerSegs, sg = rank * kVerSegs + u % kVerSegs;
-    const float c = r <= n ? A.cq : A.cp;
-    const T* row = row_of(r);
-    const Row<kDtype> R(row, V);
-    const uint4* vec = R.vec();
-    const int v0 = (int)((int64_t)R.nvec * sg / parts), v1 = (int)((int64_t)R.nvec * (sg + 1) / parts);
-    Stat a = stat_empty();
-    int v = v0 + lane;
-    for (; v + 7 * 32 < v1; v += 8 * 32) {
-      uint4 raw[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) raw[k] = __ldg(vec + v + 32 * k);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float f[kPer];
-        E::unpack(raw[k], f);
-        stat_add<kPer>(a, f, c);
+  {
+    struct At {
+      int u, v, v1;                                            // unit, this lane's vector, the unit's end
+    };
+    auto unit = [&](int u) {
+      At a{u, 0, 0};
+      if (u < rows * kVerSegs) {
+        const Row<kDtype> R(row_of(u / kVerSegs), V);
+        const int sg = rank * kVerSegs + u % kVerSegs;
+        a.v = (int)((int64_t)R.nvec * sg / parts) + lane;
+        a.v1 = (int)((int64_t)R.nvec * (sg + 1) / parts);
       }
+      return a;
+    };
+    auto load = [&](const At& a, uint4* raw) {
+      if (a.u >= rows * kVerSegs) return;
+      const uint4* vec = Row<kDtype>(row_of(a.u / kVerSegs), V).vec() + a.v;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (a.v + 32 * k < a.v1) raw[k] = __ldg(vec + 32 * k);
+    };
+    uint4 raw[kBatch], ahead[kBatch];
+    At at = unit(warp);
+    load(at, raw);
+    Run run = run_empty();
+    while (at.u < rows * kVerSegs) {
+      const int r = at.u / kVerSegs;
+      const float c = r <= n ? A.cq : A.cp;
+      At next = at;
+      next.v += 32 * kBatch;
+      const bool last = next.v - lane >= at.v1;
+      if (last) next = unit(at.u + kVerWarps);
+      load(next, ahead);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (at.v + 32 * k < at.v1) {
+          float f[kPer];
+          run_see(run, vec_max<kDtype>(raw[k]), c);
+          E::unpack(raw[k], f);
+          run_add<kPer>(run, f, c);
+        }
+      if (last) {
+        if (rank == 0 && at.u % kVerSegs == 0) {
+          const T* row = row_of(r);
+          const Row<kDtype> R(row, V);
+          if (lane < R.singles()) run_one(run, E::to(row[R.single(lane)]), c);
+        }
+        const Stat a = stat_warp(run_stat(run, c), c);
+        if (lane == 0) seg[at.u] = RowStat{a.m, a.s};
+        run = run_empty();
+      }
+      at = next;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) raw[k] = ahead[k];
     }
-    for (; v < v1; v += 32) {
-      float f[kPer];
-      E::unpack(__ldg(vec + v), f);
-      stat_add<kPer>(a, f, c);
-    }
-    if (sg == 0 && lane < R.singles()) {
-      const float f = E::to(row[R.single(lane)]);
-      stat_add<1>(a, &f, c);
-    }
-    a = stat_warp(a, c);
-    if (lane == 0) seg[u] = RowStat{a.m, a.s};
   }
   __syncthreads();
   if (C > 1) cl.barrier_wait();
@@ -306,27 +401,33 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   for (int attempt = 0; attempt < 2; ++attempt) {
     const bool rest = attempt == 0 && acc < n && row_ok(rp);
     const T* p = rest ? p0 + acc * A.p_sr : q;
-    Best me{0.f, 0x7fffffff};
-    int blk = -1;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (row_ok(rq))
-      each_pair<kDtype>(q, p, V, rank, C, tid, kVerThreads, [&](int i, float x, float y) {
-        const float r = rest ? prob(rq, x, A.cq, sh) - prob(rp, y, A.cp, 0.f) : prob(rq, x, A.cq, 0.f);
-        if (!(r > 0.f)) return;
-        float e;
-        if (A.race) {
-          e = A.race[(int64_t)b * V + i];
-        } else {
+    Racer top{0.f, 1.f, 0x7fffffff};
+    if (row_ok(rq)) {
+      if (A.race) {
+        const float* race = A.race + (int64_t)b * V;
+        each_race<kDtype>(q, p, race, V, rank, C, tid, [&](int i, float x, float y, float e) {
+          const float r = prob(rq, x, A.cq, rest ? sh : 0.f) - (rest ? prob(rp, y, A.cp, 0.f) : 0.f);
+          const float mine = r * top.e, theirs = top.r * e;      // r / e against the best so far
+          if (mine > theirs || (mine == theirs && r > 0.f && i < top.i)) top = Racer{r, e, i};
+        });
+      } else {
+        int blk = -1;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        each_pair<kDtype>(q, p, V, rank, C, tid, kVerThreads, [&](int i, float x, float y) {
+          const float r = prob(rq, x, A.cq, rest ? sh : 0.f) - (rest ? prob(rp, y, A.cp, 0.f) : 0.f);
+          if (!(r > 0.f)) return;
           if ((i >> 2) != blk) {
             blk = i >> 2;
             w = philox_block(A.seed, (uint32_t)b, (uint32_t)blk, kStreamRace, 0);
           }
           const uint32_t k = i & 3;
-          e = -log_uniform(k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w);
-        }
-        const float sc = r / e;
-        if (before(sc, i, me.x, me.i)) me = Best{sc, i};
-      });
+          const float e = -log_uniform(k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w);
+          const float mine = r * top.e, theirs = top.r * e;
+          if (mine > theirs || (mine == theirs && i < top.i)) top = Racer{r, e, i};
+        });
+      }
+    }
+    Best me{top.r > 0.f ? top.r / top.e : 0.f, top.i};
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
       const float ox = __shfl_xor_sync(0xffffffffu, me.x, o);

@@ -142,21 +142,100 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
   stat_rebase(b, m, c);
   return Stat{m, a.s + b.s, a.w + b.w};
 }
-// Adds n values, in 32 bits each.
-template <int n>
-__device__ __forceinline__ void stat_add(Stat& a, const float* x, float c) {
-  float top = x[0];
-#pragma unroll
-  for (int i = 1; i < n; ++i) top = max_nan(top, x[i]);
-  if (!(top <= a.m)) stat_rebase(a, max_nan(top, a.m), c);
-  const float m = a.m == -INFINITY ? 0.f : a.m;
-#pragma unroll
-  for (int i = 0; i < n; ++i) {
-    const float d = fmaxf(x[i] - m, kFar);
-    const float e = ex2(d * c);
-    a.s += e;
-    a.w = fmaf(e, d, a.w);
+// Two fp32 operations an instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(f32x2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 far2(f32x2 d) {             // max(d, kFar)
+  const float2 x = unpair(d);
+  return pair(fmaxf(x.x, kFar), fmaxf(x.y, kFar));
+}
+
+// The largest value of a 16-byte vector (a NaN stays).
+template <int kDtype>
+__device__ __forceinline__ float vec_max(const uint4& v) {
+  if constexpr (kDtype == SDV_F32) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (kDtype == SDV_BF16) {
+      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(w);
+      const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+      return max_nan(__low2float(m), __high2float(m));
+    } else {
+      const __half2* p = reinterpret_cast<const __half2*>(w);
+      const __half2 m = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+      return max_nan(__low2float(m), __high2float(m));
+    }
   }
+}
+
+// A thread's running statistics: sums against a reference that moves only when a logit passes it by
+// 2^8 (in e^{d/T}), and the largest logit.
+struct Run {
+  float ref, lim, top;
+  f32x2 s, w;
+};
+__device__ __forceinline__ Run run_empty() { return Run{-INFINITY, -INFINITY, -INFINITY, 0ull, 0ull}; }
+// Makes room for logits up to `top`.
+__device__ __forceinline__ void run_see(Run& r, float top, float c) {
+  r.top = max_nan(r.top, top);
+  if (!(top <= r.lim)) {
+    const float d = fmaxf(r.ref - top, kFar), f = ex2(d * c);      // ref = -inf holds nothing
+    r.w = mul2(pair(f, f), fma2(r.s, pair(d, d), r.w));
+    r.s = mul2(pair(f, f), r.s);
+    r.ref = top;
+    r.lim = top + 8.f / c;
+  }
+}
+// Adds n (even) logits that it has made room for.
+template <int n>
+__device__ __forceinline__ void run_add(Run& r, const float* x, float c) {
+  const f32x2 m = pair(-r.ref, -r.ref), c2 = pair(c, c);
+#pragma unroll
+  for (int i = 0; i < n; i += 2) {
+    const f32x2 d = far2(add2(pair(x[i], x[i + 1]), m));
+    const float2 t = unpair(mul2(d, c2));
+    const f32x2 e = pair(ex2(t.x), ex2(t.y));
+    r.s = add2(r.s, e);
+    r.w = fma2(e, d, r.w);
+  }
+}
+// The statistics against the largest logit.
+__device__ __forceinline__ Stat run_stat(const Run& r, float c) {
+  const float2 s = unpair(r.s), w = unpair(r.w);
+  Stat a{r.ref, s.x + s.y, w.x + w.y};
+  stat_rebase(a, r.top, c);
+  return a;
+}
+// A single logit.
+__device__ __forceinline__ void run_one(Run& r, float x, float c) {
+  run_see(r, x, c);
+  const float two[2] = {x, -INFINITY};
+  run_add<2>(r, two, c);
 }
 __device__ __forceinline__ Stat stat_warp(Stat a, float c) {
 #pragma unroll
