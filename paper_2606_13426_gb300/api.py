@@ -371,9 +371,9 @@ def _out(out, name, shape, dtype, dev):
 
 
 def _outs(out, names, n, dtype, dev):
-    """Outputs [n] of one type by name: the caller's, or rows of one allocation."""
+    """Outputs [n] of one type by name: the caller's, or new ones."""
     if not out:
-        return dict(zip(names, torch.empty(len(names), n, dtype=dtype, device=dev).unbind(0)))
+        return {k: torch.empty(n, dtype=dtype, device=dev) for k in names}
     return {k: _out(out, k, (n,), dtype, dev) for k in names}
 
 

@@ -7,13 +7,15 @@
 //   dx_v = (1/T) [g_lp (1[v = t] - p_v) - g_H p_v (log p_v + H)].
 // A row is split over the CTAs of a cluster, which join their statistics through distributed
 // shared memory.
+#include <type_traits>
+
 #include "sdv_tokens.cuh"
 
 namespace sdv {
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread: all under way at once, and kept
-constexpr int kGroups = 64;            // groups of threads whose maxima give the alternatives' threshold
+constexpr int kGroups = 32;            // groups of threads whose maxima give the alternatives' threshold
 constexpr int kCandMax = 512;          // candidates a CTA ranks; more: k passes over its part
 constexpr int kScoreMaxCluster = 8;
 
@@ -112,21 +114,28 @@ struct Part {
   }
   __device__ __forceinline__ bool has(int u) const { return v0 + u * kThreads < v1; }
   // Statistics; the vectors are (the last kScoreVecs of them stay) in raw.
+  template <bool kAll>
+  __device__ __forceinline__ void batch(Run& r, float c) {
+#pragma unroll
+    for (int u = 0; u < kScoreVecs; ++u)
+      if (kAll || has(u)) raw[u] = vec[v0 + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < kScoreVecs; ++u)
+      if (kAll || has(u)) {
+        float f[E::kPer16];
+        run_see(r, vec_max<kDtype>(raw[u]), c);
+        E::unpack(raw[u], f);
+        run_add<E::kPer16>(r, f, c);
+      }
+  }
+  // Whether every thread of the CTA has all of a batch from v0 on.
+  __device__ __forceinline__ bool full() const { return v0 - (int)threadIdx.x + kScoreVecs * kThreads <= v1; }
   __device__ __forceinline__ Run read(float c) {
     Run r = run_empty();
     for (;;) {
-#pragma unroll
-      for (int u = 0; u < kScoreVecs; ++u)
-        if (has(u)) raw[u] = vec[v0 + u * kThreads];
-#pragma unroll
-      for (int u = 0; u < kScoreVecs; ++u)
-        if (has(u)) {
-          float f[E::kPer16];
-          run_see(r, vec_max<kDtype>(raw[u]), c);
-          E::unpack(raw[u], f);
-          run_add<E::kPer16>(r, f, c);
-        }
-      if (v0 + kScoreVecs * kThreads >= v1) break;
+      if (full()) batch<true>(r, c);
+      else batch<false>(r, c);
+      if (v0 - (int)threadIdx.x + kScoreVecs * kThreads >= v1) break;
       v0 += kScoreVecs * kThreads;
     }
     if (single >= 0) run_one(r, x, c);
@@ -145,12 +154,9 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int64_t n = blockIdx.x / C;
   const int tid = threadIdx.x;
-  __shared__ Stat wstat[kWarps];
-  __shared__ Stat cstat[kScoreMaxCluster];
+  __shared__ Stat stats[kScoreMaxCluster * kWarps];           // the leader's: every warp's
   __shared__ int listed[kScoreMaxCluster];
-  __shared__ float tmax[kTop ? kScoreThreads : 1];
-  __shared__ __align__(16) float gmax[kTop ? kGroups : 4];
-  __shared__ float thr_s[2];
+  __shared__ __align__(16) float gmax[kGroups];
   __shared__ int ncand;
   __shared__ Cand cand[kTop ? kCandMax : 1];
   __shared__ Cand lists[kTop ? kScoreMaxCluster * SDV_MAX_TOP : 1];
@@ -162,42 +168,29 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   const int first = P.v0;
   const Run run = P.read(A.c);
   const float tm = run.top;                   // the largest of this thread's logits
-  Stat a = stat_warp(run_stat(run, A.c), A.c);
-  if ((tid & 31) == 0) wstat[tid >> 5] = a;
-  if (kTop) {
-    tmax[tid] = tm;
+  Stat a = run_warp(run, A.c);
+  if constexpr (kTop) {
+    float g = tm;                             // a group's: of kScoreThreads / kGroups threads
+#pragma unroll
+    for (int o = 1; o < kScoreThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (tid % (kScoreThreads / kGroups) == 0) gmax[tid / (kScoreThreads / kGroups)] = g;
     if (tid == 0) ncand = 0;
+    __syncthreads();
   }
-  __syncthreads();
-  if (tid == kScoreThreads - 32) {            // (a warp that has nothing to do with the threshold)
-    a = wstat[0];
-    for (int w = 1; w < kWarps; ++w) a = stat_join(a, wstat[w], A.c);
-    wstat[0] = a;
-  }
+  if (C > 1) cl.barrier_wait();               // the leader has started: its memory can be written
+  if ((tid & 31) == 0) (C > 1 ? cl.map_shared_rank(stats, 0) : stats)[rank * kWarps + tid / 32] = a;
   if constexpr (kTop) {
     // At least k of the part's logits are at or above the k-th largest of the groups' maxima.
-    if (tid < kGroups) {
-      float g = tmax[tid];
+    const float mine_max = gmax[tid & 31];
+    int above = 0;
 #pragma unroll
-      for (int j = kGroups; j < kScoreThreads; j += kGroups) g = fmaxf(g, tmax[tid + j]);
-      gmax[tid] = g;
+    for (int j = 0; j < kGroups; j += 4) {
+      const float4 o = *reinterpret_cast<const float4*>(gmax + j);
+      above += (o.x > mine_max) + (o.y > mine_max) + (o.z > mine_max) + (o.w > mine_max);
     }
-    __syncthreads();
-    if (tid < kGroups) {
-      const float g = gmax[tid];
-      int above = 0;
+    float thr = above < A.top_k ? mine_max : INFINITY;
 #pragma unroll
-      for (int j = 0; j < kGroups; j += 4) {
-        const float4 o = *reinterpret_cast<const float4*>(gmax + j);
-        above += (o.x > g) + (o.y > g) + (o.z > g) + (o.w > g);
-      }
-      float t = above < A.top_k ? g : INFINITY;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) t = fminf(t, __shfl_xor_sync(0xffffffffu, t, o));
-      if ((tid & 31) == 0) thr_s[tid >> 5] = t;
-    }
-    __syncthreads();
-    const float thr = fminf(thr_s[0], thr_s[1]);
+    for (int o = 16; o; o >>= 1) thr = fminf(thr, __shfl_xor_sync(0xffffffffu, thr, o));
     auto keep = [&](float x, int i) {
       if (x >= thr && x > -INFINITY) {
         const int at = atomicAdd(&ncand, 1);     // their order does not matter: they are ranked
@@ -224,7 +217,6 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
       if (P.single >= 0) keep(P.x, P.single);
     }
     __syncthreads();
-    if (C > 1) cl.barrier_wait();               // the leader has started: its lists can be written
     Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * A.top_k;
     int nc = ncand;
     if (nc <= kCandMax) {
@@ -262,19 +254,15 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
       }
     }
     if (tid == 0) (C > 1 ? cl.map_shared_rank(listed, 0) : listed)[rank] = nc;
-  } else {
-    __syncthreads();
-    if (C > 1) cl.barrier_wait();
   }
-  if (tid == 0) (C > 1 ? cl.map_shared_rank(cstat, 0) : cstat)[rank] = wstat[0];
   if (C > 1) {
     cl.sync();
     if (rank) return;
   } else {
     __syncthreads();
   }
-  a = cstat[0];
-  for (int r = 1; r < C; ++r) a = stat_join(a, cstat[r], A.c);
+  if (!kTop && tid >= 32) return;
+  a = stat_gather(stats, C * kWarps, tid & 31, A.c);
   if (tid == 0) write_row(A, n, a, row_token<kDtype>(A, row, n));
   if constexpr (kTop) {
     const bool bad = !(a.m < INFINITY);
@@ -290,13 +278,19 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
     if (!bad)
       for (int i = tid; i < C * k; i += kScoreThreads) {
         const int q = i / k;
-        if (i - q * k >= listed[q]) continue;
+        int r = i - q * k;                                    // its place in its own list, and in the others
+        if (r >= listed[q]) continue;
         const Cand me = lists[i];
-        int r = 0;
-        for (int p = 0; p < C; ++p) {
-          const int np = listed[p];
-          const Cand* l = lists + p * k;
-          for (int j = 0; j < np; ++j) r += before(l[j].x, l[j].i, me.x, me.i);
+        for (int p = 0; p < C && r < k; ++p) {
+          if (p == q) continue;
+          int lo = 0, hi = listed[p];
+          while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            const Cand o = lists[p * k + mid];
+            if (before(o.x, o.i, me.x, me.i)) lo = mid + 1;
+            else hi = mid;
+          }
+          r += lo;
         }
         if (r < k) put(r, me);
       }
@@ -324,8 +318,6 @@ struct RowGrad {
   float m, ls2;          // maximum, log2 s
   float a, b, g;
   int t;                 // the token, or -1
-  float nan;             // what every element gets if the row has no gradient (0 or NaN), else unused
-  bool flat;
 };
 __device__ __forceinline__ RowGrad row_grad(float m, float log_s, float H, int t, int V, float g_lp, float g_h, float inv_t) {
   RowGrad r;
@@ -337,21 +329,18 @@ __device__ __forceinline__ RowGrad row_grad(float m, float log_s, float H, int t
   r.a = -inv_t * (gl + g_h * (H - log_s));
   r.b = -inv_t * inv_t * g_h;
   r.g = inv_t * gl;
-  r.flat = !(m > -INFINITY && m < INFINITY);
-  r.nan = m == -INFINITY ? 0.f : NAN;
+  if (m == -INFINITY) r.ls2 = r.a = r.b = 0.f, r.t = -1;      // an empty row: p = 0
+  if (!(m < INFINITY)) r.a = NAN, r.t = -1;
   return r;
 }
-__device__ __forceinline__ float grad_of(const RowGrad& r, float x, float c) {
-  const float d = fmaxf(x - r.m, kFar);
-  const float p = ex2(fmaf(d, c, -r.ls2));
-  return r.flat ? r.nan : p * fmaf(r.b, d, r.a);
-}
 __device__ __forceinline__ float grad_one(const RowGrad& r, float x, int i, float c) {
-  const float o = grad_of(r, x, c);
-  return i == r.t && !r.flat && x > -INFINITY ? o + r.g : o;
+  const float d = fmaxf(x - r.m, kFar);
+  const float o = ex2(fmaf(d, c, -r.ls2)) * fmaf(r.b, d, r.a);
+  return i == r.t && x > -INFINITY ? o + r.g : o;
 }
+// Without the token's part, which grad_one writes afterwards.
 template <int kPer>
-__device__ __forceinline__ void grad_vec(const RowGrad& r, const float* f, float* o, int first, float c) {
+__device__ __forceinline__ void grad_vec(const RowGrad& r, const float* f, float* o, float c) {
   const f32x2 m = pair(-r.m, -r.m), c2 = pair(c, c), l = pair(-r.ls2, -r.ls2), a = pair(r.a, r.a), b = pair(r.b, r.b);
 #pragma unroll
   for (int e = 0; e < kPer; e += 2) {
@@ -360,14 +349,6 @@ __device__ __forceinline__ void grad_vec(const RowGrad& r, const float* f, float
     const float2 y = unpair(mul2(pair(ex2(t.x), ex2(t.y)), fma2(b, d, a)));
     o[e] = y.x;
     o[e + 1] = y.y;
-  }
-  if (r.flat) {
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = r.nan;
-  } else if ((unsigned)(r.t - first) < (unsigned)kPer) {    // (t = -1: no token)
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      if (r.t - first == e && f[e] > -INFINITY) o[e] += r.g;
   }
 }
 // Stores a vector of results whose place need not be on a 16-byte boundary.
@@ -405,7 +386,12 @@ __global__ void __launch_bounds__(kScoreThreads) k_scores_grad(const GradArgs A,
   for (int v = v0 + threadIdx.x; v < v1; v += kScoreThreads) {
     float f[kPer], o[kPer];
     E::unpack(vec[v], f);
-    grad_vec<kPer>(g, f, o, R.head + v * kPer, A.c);
+    grad_vec<kPer>(g, f, o, A.c);
+    if ((unsigned)(g.t - R.head - v * kPer) < (unsigned)kPer) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (g.t - R.head - v * kPer == e) o[e] = grad_one(g, f[e], g.t, A.c);
+    }
     put_vec<kDtype>(out + R.head + v * kPer, o, vec_out);
   }
   if (part == 0 && threadIdx.x < R.singles()) {
@@ -434,54 +420,41 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_scores_train(cons
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int64_t n = blockIdx.x / C;
   const int tid = threadIdx.x;
-  __shared__ Stat wstat[kWarps];
-  __shared__ Stat cstat[kScoreMaxCluster];
+  __shared__ Stat stats[kScoreMaxCluster * kWarps];           // every warp's of the cluster
   if (C > 1) cl.barrier_arrive();
   const T* row = reinterpret_cast<const T*>(A.S.x) + n * A.S.stride;
   T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
   const Row<kDtype> R(row, A.S.V);
   Part<kDtype, kThreads> P(R, rank, C);
-  Stat a = stat_warp(run_stat(P.read(A.S.c), A.S.c), A.S.c);
-  if ((tid & 31) == 0) wstat[tid >> 5] = a;
-  Token tok{-1, 0.f};
-  if (rank == 0 && tid == 0) tok = row_token<kDtype>(A.S, row, n);
-  const int t = A.S.tokens ? A.S.tokens[n] : -1;
+  const Stat mine = run_warp(P.read(A.S.c), A.S.c);
+  // the token, and whether one of this thread's vectors holds it
+  const Token tok = row_token<kDtype>(A.S, row, n);
   const float g_lp = A.g_lp ? A.g_lp[n] : 0.f, g_h = A.g_h ? A.g_h[n] : 0.f;
-  __syncthreads();
+  const int at = tok.t >= R.head && tok.t < A.S.V - R.tail ? (tok.t - R.head) / kPer : -1;
+  const bool own = at >= P.v0 && at < P.v1 && (at - P.v0) % kThreads == 0;
   if (C > 1) cl.barrier_wait();
-  if (tid < C) {                              // every CTA of the cluster gets every CTA's statistics
-    a = wstat[0];
-    for (int w = 1; w < kWarps; ++w) a = stat_join(a, wstat[w], A.S.c);
-    Stat* to = C > 1 ? cl.map_shared_rank(cstat, tid) : cstat;
-    to[rank] = a;
-  }
+  if ((tid & 31) < C) (C > 1 ? cl.map_shared_rank(stats, tid & 31) : stats)[rank * kWarps + tid / 32] = mine;
   if (C > 1) cl.sync();
   else __syncthreads();
-  a = cstat[0];
-  for (int r = 1; r < C; ++r) a = stat_join(a, cstat[r], A.S.c);
+  const Stat a = stat_gather(stats, C * kWarps, tid & 31, A.S.c);
   if (rank == 0 && tid == 0) write_row(A.S, n, a, tok);
   const float log_s = logf(a.s);
-  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, t, A.S.V, g_lp, g_h, A.S.inv_t);
+  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, tok.t, A.S.V, g_lp, g_h, A.S.inv_t);
   T* to = out + R.head + P.v0 * kPer;
-  if (same_phase<kDtype>(row, out)) {
+  auto write = [&](auto all, bool vec) {
 #pragma unroll
     for (int u = 0; u < kScoreVecs; ++u)
-      if (P.has(u)) {
+      if (decltype(all)::value || P.has(u)) {
         float f[kPer], o[kPer];
         E::unpack(P.raw[u], f);
-        grad_vec<kPer>(g, f, o, R.head + (P.v0 + u * kThreads) * kPer, A.S.c);
-        put_vec<kDtype>(to + u * kThreads * kPer, o, true);
+        grad_vec<kPer>(g, f, o, A.S.c);
+        put_vec<kDtype>(to + u * kThreads * kPer, o, vec);
       }
-  } else {
-#pragma unroll
-    for (int u = 0; u < kScoreVecs; ++u)
-      if (P.has(u)) {
-        float f[kPer], o[kPer];
-        E::unpack(P.raw[u], f);
-        grad_vec<kPer>(g, f, o, R.head + (P.v0 + u * kThreads) * kPer, A.S.c);
-        put_vec<kDtype>(to + u * kThreads * kPer, o, false);
-      }
-  }
+  };
+  const bool vec = same_phase<kDtype>(row, out);
+  if (P.full() && vec) write(std::true_type{}, true);
+  else write(std::false_type{}, vec);
+  if (own) out[tok.t] = E::from(grad_one(g, tok.x, tok.t, A.S.c));
   if (P.single >= 0) out[P.single] = E::from(grad_one(g, P.x, P.single, A.S.c));
 }
 

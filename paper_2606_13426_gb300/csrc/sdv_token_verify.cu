@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
           const Row<kDtype> R(row, V);
           if (lane < R.singles()) run_one(run, E::to(row[R.single(lane)]), c);
         }
-        const Stat a = stat_warp(run_stat(run, c), c);
+        const Stat a = run_warp(run, c);
         if (lane == 0) seg[at.u] = RowStat{a.m, a.s};
         run = run_empty();
       }

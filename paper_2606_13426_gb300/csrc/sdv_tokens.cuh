@@ -19,7 +19,7 @@ constexpr float kLog2E = 1.44269504088896341f;   // log2 e
 constexpr float kLn2f = 0.69314718055994531f;    // log 2
 // Far below any difference of two logits that leaves a probability, and finite: 0 * kFar is 0
 // where 0 * -inf would be NaN.
-constexpr float kFar = -1e30f;
+constexpr float kFar = -1e15f;
 
 template <int kDtype>
 struct Num;
@@ -224,11 +224,19 @@ __device__ __forceinline__ void run_add(Run& r, const float* x, float c) {
     r.w = fma2(e, d, r.w);
   }
 }
-// The statistics against the largest logit.
-__device__ __forceinline__ Stat run_stat(const Run& r, float c) {
+// A warp's statistics, against its largest logit.
+__device__ __forceinline__ Stat run_warp(const Run& r, float c) {
   const float2 s = unpair(r.s), w = unpair(r.w);
   Stat a{r.ref, s.x + s.y, w.x + w.y};
-  stat_rebase(a, r.top, c);
+  float m = r.top;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  stat_rebase(a, m, c);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
+  }
   return a;
 }
 // A single logit.
@@ -237,16 +245,24 @@ __device__ __forceinline__ void run_one(Run& r, float x, float c) {
   const float two[2] = {x, -INFINITY};
   run_add<2>(r, two, c);
 }
+// The warp's statistics: one rebase a lane to the common maximum, then plain sums.
 __device__ __forceinline__ Stat stat_warp(Stat a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  stat_rebase(a, m, c);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    Stat b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.w = __shfl_xor_sync(0xffffffffu, a.w, o);
-    a = stat_join(a, b, c);
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
   }
   return a;
+}
+// The statistics of n parts, by a whole warp.
+__device__ __forceinline__ Stat stat_gather(const Stat* part, int n, int lane, float c) {
+  Stat a = stat_empty();
+  for (int i = lane; i < n; i += 32) a = i == lane ? part[i] : stat_join(a, part[i], c);
+  return stat_warp(a, c);
 }
 
 // The order of the alternatives: the larger logit first, of equal ones the lower index.
