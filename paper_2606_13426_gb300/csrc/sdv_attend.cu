@@ -7,7 +7,8 @@ extern "C" {
 
 size_t sdv_attend_workspace_bytes(int W, int Hq, int H, int D) {
   if (W < 1 || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
-  return (size_t)sm_count() * 2 * 8 * (size_t)row_tiles((int64_t)W * (Hq / H)).nt * (size_t)(D + 2) * 4;
+  const int nt = row_tiles((int64_t)W * (Hq / H)).nt;
+  return (size_t)sm_count() * (size_t)attend_warps(nt) * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4;
 }
 
 int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int dtype, int B, int W,
@@ -22,7 +23,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   if (q_stride_b < 0 || q_stride_t < 0 || q_stride_h < 0 || span < 0 || !(fabsf(scale) < INFINITY)) return SDV_EINVAL;
   const int64_t R = (int64_t)W * (Hq / H);
   if (R > (1 << 24) || (int64_t)B * H * ((R + 7) / 8 + kMaxNt) > 0x7fffffff) return SDV_EINVAL;
-  if (!aligned_to(q, 2) || !aligned_to(out, 16) || !aligned_to(lse, 4) || !aligned_to(status, 4) || !aligned_to(lengths, 4) ||
+  if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(status, 4) || !aligned_to(lengths, 4) ||
       !aligned_to(counts, 4))
     return SDV_EALIGN;
   if (!workspace || workspace_bytes < sdv_attend_workspace_bytes(W, Hq, H, D)) return SDV_ENOWORKSPACE;
@@ -31,6 +32,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   const RowTiles tiles = row_tiles(R);
   A.q = q;
   A.bf16 = dtype == SDV_BF16;
+  A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
   A.q_sb = q_stride_b, A.q_st = q_stride_t, A.q_sh = q_stride_h;
   A.c = CacheView{(uint8_t*)k_codes, (uint8_t*)v_codes, (float*)k_scale, (float*)v_scale, page_table, pages, max_pages, H, D, block};
   A.cpb = chunk_div(block / kChunk);

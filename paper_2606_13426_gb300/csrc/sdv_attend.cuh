@@ -3,13 +3,14 @@
 // For query i of sequence b (position len - count + i) and the keys up to its position:
 //   s_j = scale ks_j (q . k_j),  p_j = e^{s_j - max} / sum,  out = sum_j p_j vs_j v_j.
 // The G = Hq / H query heads of a key head and the window's queries are the rows of one item, so
-// that a key is read once for up to 8 kMaxNt of them.  The (sequence, head, row tile) items' tiles
-// of 64 keys, laid end to end, are dealt out to the CTAs in equal runs; a run that does not hold
-// an item's whole length leaves (max, sum, output) in the workspace, and k_attend_join joins them.
+// that a key is read once for up to 8 kMaxNt of them.  The (sequence, head, row tile) items' steps
+// of 32 keys, laid end to end, are dealt out to the warps in equal runs, so that no warp waits for
+// another; a run that does not hold an item's whole length leaves (max, sum, output) in the
+// workspace, and k_attend_join joins them.
 //
 // Both products are taken transposed, S' = K Q' and O' = V' P': the cache is the operand with 16
 // rows, the queries' rows come in eights, so that a single token's few heads waste little.  A warp
-// works on 32 keys at a time, from a ring of cp.async stages of its own.  Codes widen to f16
+// reads its steps from a cp.async ring of its own.  Codes widen to f16
 // exactly; with g = lane / 4 and t = lane % 4:
 //   * key row g (g + 8) of score tile s is token 8 (g / 2) + 4 s + g % 2 (+ 2), which makes the tokens
 //     that a thread multiplies in step s of the second product, 8 t + 4 s .. + 3, adjacent
@@ -27,9 +28,10 @@
 
 namespace sdv {
 
-constexpr int kJoinThreads = 256;
-constexpr int kTile = 64;                 // keys of a unit of work: two steps of kSub
-constexpr int kSub = 32;
+constexpr int kSub = 32;                  // keys of a step
+constexpr int kJoinWarps = 8;
+constexpr int kJoinThreads = 32 * kJoinWarps;
+constexpr int kMinSteps = 2;              // of a run, where there are fewer steps than warps could take
 constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
@@ -45,7 +47,7 @@ inline ChunkDiv chunk_div(int n) { return ChunkDiv{n == 1 ? 0u : (uint32_t)((0x1
 
 struct AttendArgs {
   const void* q;
-  bool bf16;
+  bool bf16, q_vec;                        // queries in whole aligned vectors of 16 bytes
   int64_t q_sb, q_st, q_sh;
   CacheView c;
   ChunkDiv cpb;
@@ -57,13 +59,13 @@ struct AttendArgs {
   void* out;
   float* lse;
   uint32_t* status;
-  float* part;                             // workspace: 2 slots a CTA
+  float* part;                             // workspace: 2 slots a warp
   int ctas;
 };
 
-// A sequence's tokens, new ones and tiles.
+// A sequence's tokens, new ones and steps.
 struct Seq {
-  int len, count, first, tiles;            // first: the first tile that a query sees
+  int len, count, first, steps;            // first: the first step that a query sees
 };
 __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   Seq s;
@@ -71,41 +73,33 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   s.len = min(max(A.lengths[b], 0), cap);
   s.count = min(max(A.counts ? A.counts[b] : A.W, 0), A.W);
   s.first = 0;
-  if (A.span > 0) s.first = max(0, s.len - s.count - A.span + 1) / kTile;
-  s.tiles = s.count && s.len ? (s.len + kTile - 1) / kTile - s.first : 0;
+  if (A.span > 0) s.first = max(0, s.len - s.count - A.span + 1) / kSub;
+  s.steps = s.count && s.len ? (s.len + kSub - 1) / kSub - s.first : 0;
   return s;
 }
 
-// Tiles of the sequences before b and of all (each for one head and row tile).
+// Steps of the sequences before b and of all (each for one head and row tile), by a warp.
 struct Sums {
   int64_t before, total;
 };
-__device__ __forceinline__ Sums tile_sums(const AttendArgs& A, int b, int64_t* red) {
-  int64_t mine = 0, all = 0;
-  for (int i = threadIdx.x; i < A.B; i += blockDim.x) {
-    const int t = seq_of(A, i).tiles;
-    all += t;
-    if (i < b) mine += t;
+__device__ __forceinline__ Sums step_sums(const AttendArgs& A, int b, int lane) {
+  Sums s{0, 0};
+  for (int i = lane; i < A.B; i += 32) {
+    const int t = seq_of(A, i).steps;
+    s.total += t;
+    if (i < b) s.before += t;
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    all += __shfl_xor_sync(0xffffffffu, all, o);
+    s.before += __shfl_xor_sync(0xffffffffu, s.before, o);
+    s.total += __shfl_xor_sync(0xffffffffu, s.total, o);
   }
-  if ((threadIdx.x & 31) == 0) {
-    red[2 * (threadIdx.x >> 5)] = mine;
-    red[2 * (threadIdx.x >> 5) + 1] = all;
-  }
-  __syncthreads();
-  Sums s{0, 0};
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) {
-    s.before += red[2 * w];
-    s.total += red[2 * w + 1];
-  }
-  __syncthreads();
   return s;
 }
-__device__ __forceinline__ int64_t run_start(int64_t units, int g, int ctas) { return units * g / ctas; }
+__device__ __forceinline__ int64_t run_start(int64_t units, int g, int runs) { return units * g / runs; }
+__device__ __forceinline__ int run_count(int64_t units, int warps) {
+  return (int)min((int64_t)warps, (units + kMinSteps - 1) / kMinSteps);
+}
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool real) {
@@ -138,122 +132,101 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from, bool real) 
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(n));
 }
 
+// Warps of a CTA of k_attend.
+constexpr int attend_warps(int nt) { return nt == 1 ? 16 : nt == 2 ? 12 : 8; }
+
+__device__ __forceinline__ void put_out(const AttendArgs& A, int64_t at, float x) {
+  if (A.bf16) reinterpret_cast<__nv_bfloat16*>(A.out)[at] = __float2bfloat16_rn(x);
+  else reinterpret_cast<__half*>(A.out)[at] = __float2half_rn(x);
+}
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + log2f(l)) * kLn2f : (l == 0.f ? -INFINITY : NAN); }
+
 // A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others under
-// way.  Few rows leave registers for sixteen warps, whose latencies overlap; more rows take
-// eight.
+// way; its queries' fragments are beside it.  Few rows leave registers and shared memory for more
+// warps, whose latencies overlap.
 template <int kD, int kNt>
 struct AttendShape {
-  static constexpr int kWarps = kNt <= 2 ? 16 : 8;
+  static constexpr int kWarps = attend_warps(kNt);
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRows = 8 * kNt;
   static constexpr int kSlot = kRows * (kD + 2);         // floats of a partial: rows' output, max, sum
   static constexpr int kHalf = kSub * kD;                 // bytes
-  static constexpr int kHalves = (kWarps == 16 ? 3 : 5) * (kD == 64 ? 2 : 1) - (kD == 64 ? 1 : 0);
+  static constexpr int kHalves = (kNt <= 2 || kNt == 5 ? 3 : 5) * (kD == 64 ? 2 : 1) - (kD == 64 ? 1 : 0);
   static constexpr int kAhead = (kHalves - 1) / 2;        // steps
   static constexpr int kScaleSlots = kAhead + 1;
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
-  static constexpr int kOutStride = kD + 4;
-  static constexpr int kRing = kWarps * kHalves * kHalf;
-  static constexpr int kJoin = kWarps * kRows * kOutStride * 4;   // the warps' outputs join in its place
-  static constexpr int kQAt = kRing > kJoin ? kRing : kJoin;
-  static constexpr int kQBytes = kNt * kKv * 2 * 32 * 16;
-  static constexpr int kScaleBytes = kWarps * kScaleSlots * 32;   // of a step: ks, vs of both chunks; absent chunks
-  static constexpr size_t kSmem = (size_t)kQAt + kQBytes + kScaleBytes;
-  static_assert(kHalves % 2 == 1 && kSmem <= 220 * 1024, "");
+  static constexpr int kQBytes = kRows * kD * 2;
+  static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
+  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes;
+  static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
+  static_assert(kHalves % 2 == 1 && kSmem <= 227 * 1024, "");
 };
 
-// Writes four elements of row `row` of an item's results, and its log sum with the first of them.
-template <int kD>
-__device__ __forceinline__ void put_row(const AttendArgs& A, int count, int b, int h, int row, int d, float4 o, float m, float l) {
-  if (row >= A.R) return;
-  const int i = row / A.G, head = h * A.G + row % A.G;
-  if (i >= count) l = 0.f;                                  // past the sequence's window
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int64_t at = ((int64_t)b * A.W + i) * (A.c.H * A.G) + head;
-  uint2 w;
-  if (A.bf16) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(o.x * inv, o.y * inv), y = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-    w = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-  } else {
-    w = make_uint2(pack_half(o.x * inv, o.y * inv), pack_half(o.z * inv, o.w * inv));
-  }
-  *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(A.out) + at * kD + d) = w;
-  if (A.lse && d == 0) A.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2f : (l == 0.f ? -INFINITY : NAN);
-}
-
-__device__ __forceinline__ float q_value(const AttendArgs& A, int64_t at) {
-  return A.bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(A.q)[at]) : __half2float(reinterpret_cast<const __half*>(A.q)[at]);
+// Eight elements of a query, as they are held.
+__device__ __forceinline__ uint4 q_load8(const AttendArgs& A, int64_t at) {
+  if (A.q_vec) return __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(A.q) + at));
+  uint32_t w[4];
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(A.q) + at;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int kD, int kNt>
 __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
-  constexpr int kAttWarps = S::kWarps, kAttThreads = S::kThreads;
   constexpr int kKv = S::kKv;
   constexpr int kMt = kD / 16;                             // sixteens of the output
   constexpr int kR = 2 * kNt;                              // rows of a thread: 8 n + 2 t + e
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ int64_t red[2 * kAttWarps];
-  __shared__ int start_b;
-  __shared__ int64_t start_before;
-  __shared__ float row_scale[S::kRows];
-  __shared__ float wm[kAttWarps][S::kRows], wl[kAttWarps][S::kRows];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int H = A.c.H, per = H * A.RT;                     // items of a sequence
-  uint8_t* ring = smem + warp * S::kHalves * S::kHalf;
-  uint4* qf = reinterpret_cast<uint4*>(smem + S::kQAt);
-  float* scales = reinterpret_cast<float*>(smem + S::kQAt + S::kQBytes) + warp * S::kScaleSlots * 8;
+  uint8_t* ring = smem + warp * S::kWarpBytes;
+  uint4* qf = reinterpret_cast<uint4*>(ring + S::kHalves * S::kHalf);
+  float* scales = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes);
 
-  const int64_t units = tile_sums(A, 0, red).total * per;
-  const int runs = (int)min((int64_t)A.ctas, units);       // none of them empty
-  if ((int)blockIdx.x >= runs) return;
-  int64_t u = run_start(units, blockIdx.x, runs);
-  const int64_t u_end = run_start(units, blockIdx.x + 1, runs);
-  // the sequence that holds unit u
-  if (tid == 0) start_b = A.B;
-  if (warp == 0) {
-    int64_t before = 0;
-    for (int b0 = 0; b0 < A.B; b0 += 32) {
-      const int64_t mine = b0 + lane < A.B ? (int64_t)seq_of(A, b0 + lane).tiles * per : 0;
-      int64_t inc = mine;
+  const int64_t units = step_sums(A, 0, lane).total * per;
+  const int runs = run_count(units, A.ctas * S::kWarps);   // none of them empty
+  // neighbours in the order of the runs sit on different SMs when there are few
+  const int run = runs < A.ctas * S::kWarps ? warp * A.ctas + (int)blockIdx.x : (int)blockIdx.x * S::kWarps + warp;
+  if (run >= runs) return;
+  int64_t u = run_start(units, run, runs);
+  const int64_t u_end = run_start(units, run + 1, runs);
+  // the sequence that holds unit u, and the unit of its first step
+  int b = A.B;
+  int64_t seq_u = 0;
+  for (int b0 = 0; b0 < A.B; b0 += 32) {
+    const int64_t mine = b0 + lane < A.B ? (int64_t)seq_of(A, b0 + lane).steps * per : 0;
+    int64_t inc = mine;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += x;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, before + inc > u);
-      if (hit) {
-        const int k = __ffs(hit) - 1;
-        if (lane == k) {
-          start_b = b0 + k;
-          start_before = before + inc - mine;
-        }
-        break;
-      }
-      before += __shfl_sync(0xffffffffu, inc, 31);
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
     }
+    const unsigned hit = __ballot_sync(0xffffffffu, seq_u + inc > u);
+    if (hit) {
+      const int k = __ffs(hit) - 1;
+      b = b0 + k;
+      seq_u += __shfl_sync(0xffffffffu, inc - mine, k);
+      break;
+    }
+    seq_u += __shfl_sync(0xffffffffu, inc, 31);
   }
-  __syncthreads();
-  int b = start_b;
-  int64_t seq_u = start_before;                            // unit of the sequence's first tile
   bool first_segment = true;
   while (u < u_end && b < A.B) {
     const Seq sq = seq_of(A, b);
-    if (u >= seq_u + (int64_t)sq.tiles * per) {
-      seq_u += (int64_t)sq.tiles * per;
+    if (u >= seq_u + (int64_t)sq.steps * per) {
+      seq_u += (int64_t)sq.steps * per;
       ++b;
       continue;
     }
-    const int item = (int)((u - seq_u) / sq.tiles);
+    const int item = (int)((u - seq_u) / sq.steps);
     const int h = item / A.RT, row0 = item % A.RT * S::kRows;
-    const int64_t item_u = seq_u + (int64_t)item * sq.tiles;
-    const int tile0 = (int)(u - item_u);
-    const int tile1 = (int)min((int64_t)sq.tiles, u_end - item_u);
+    const int64_t item_u = seq_u + (int64_t)item * sq.steps;
+    const int step0 = (int)(u - item_u);
+    const int steps = (int)min((int64_t)sq.steps, u_end - item_u) - step0;
     const int32_t* table = A.c.table + (int64_t)b * A.c.max_pages;
-    // this warp's steps: two of every kAttWarps-th unit
-    const int steps = tile1 - tile0 > warp ? 2 * ((tile1 - tile0 - warp - 1) / kAttWarps + 1) : 0;
-    auto key_of = [&](int n) { return (sq.first + tile0 + warp + (n >> 1) * kAttWarps) * kTile + (n & 1) * kSub; };
+    auto key_of = [&](int n) { return (sq.first + step0 + n) * kSub; };
     // the page of the chunk of 16 tokens from `key` on, or -1 where there is none
     auto page_of = [&](int key) {
       if (key >= sq.len) return -1;
@@ -266,7 +239,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     // whole keys, in the order of memory, to where the threads read them as fragments.
     constexpr int kPieces = kD / 16, kKeysOf = 32 / kPieces;   // pieces of a key; keys of one copy of the warp
     const int lk = lane / kPieces, lp = lane % kPieces;
-    int key_to;                                                // this lane's place of copy 0, and what copy j adds
+    int key_to;                                                // this lane's place of copy 0
     if (kD == 128) key_to = ((lk >> 1) * kKv + (lp >> 2)) * 512 + ((lk & 1) * 4 + (lp & 3)) * 16;
     else key_to = ((lk >> 2 & 1) * 2 + (lk >> 1 & 1)) * 512 + ((lk & 1) * 4 + lp) * 16;
     const int64_t head_keys = (int64_t)h * A.c.block;
@@ -306,7 +279,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       asm volatile("cp.async.commit_group;");
     };
     auto nothing = [] { asm volatile("cp.async.commit_group;"); };
-    __syncthreads();                                       // the rows before these are done with shared memory
+    __syncwarp();                                          // the item before is done with the ring and the queries
     int np0 = -1, np1 = -1;                                 // pages of the next step to issue
     auto look = [&](int n) {
       if (n < steps) {
@@ -326,51 +299,53 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
       look(n + 1);
     }
-    // the rows' queries as fragments, in f16: bf16 rows are scaled by a power of two into its range
-    for (int r = warp; r < S::kRows; r += kAttWarps) {
-      const int row = row0 + r, i = row / A.G;
-      float f[kD / 32];
+    // the rows' queries as fragments, in f16: bf16 ones are scaled by a power of two into its range
+    float rsc = A.scale2;
+    {
+      constexpr int kN = S::kRows * kD / 8 / 32;            // eights of elements of a lane
+      uint4 raw[kN];
       float amax = 0.f;
 #pragma unroll
-      for (int e = 0; e < kD / 32; ++e) {
-        f[e] = 0.f;
-        if (row < A.R) f[e] = q_value(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row % A.G) * A.q_sh + lane + 32 * e);
-        amax = fmaxf(amax, fabsf(f[e]));
+      for (int j = 0; j < kN; ++j) {
+        const int p = lane + 32 * j, row = row0 + p / (kD / 8), i = row / A.G;
+        raw[j] = make_uint4(0, 0, 0, 0);
+        if (row < A.R) raw[j] = q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
+      }
+      float up = 1.f;
+      if (A.bf16) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          float f[8];
+          Num<SDV_BF16>::unpack(raw[j], f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[e]) < INFINITY ? fabsf(f[e]) : 0.f);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        if (amax > 0.f) {
+          const int k = min(max(139 - (int)(__float_as_uint(amax) >> 23), -100), 100);
+          up = __uint_as_float((uint32_t)(127 + k) << 23);
+          rsc *= __uint_as_float((uint32_t)(127 - k) << 23);
+        }
       }
 #pragma unroll
-      for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      float up = 1.f, down = 1.f;
-      if (A.bf16 && amax > 0.f && amax < INFINITY) {
-        const int k = min(max(139 - (int)(__float_as_uint(amax) >> 23), -100), 100);
-        up = __uint_as_float((uint32_t)(127 + k) << 23);
-        down = __uint_as_float((uint32_t)(127 - k) << 23);
-      }
-      if (lane == 0) row_scale[r] = down;
+      for (int j = 0; j < kN; ++j) {
+        const int p = lane + 32 * j, r = p / (kD / 8), e8 = p % (kD / 8);
+        if (A.bf16) {
+          float f[8];
+          Num<SDV_BF16>::unpack(raw[j], f);
 #pragma unroll
-      for (int e = 0; e < kD / 32; ++e) {                  // element d: piece d / 16 is thread t's, i-th
-        const int d = lane + 32 * e, piece = d / 16;
-        __half* to = reinterpret_cast<__half*>(qf + (((r >> 3) * kKv + (piece >> 2)) * 2 + (d >> 3 & 1)) * 32 + (r & 7) * 4 + (piece & 3));
-        to[d & 7] = __float2half_rn(f[e] * up);
+          for (int e = 0; e < 8; ++e) f[e] *= up;
+          raw[j] = Num<SDV_F16>::pack(f);
+        }
+        qf[(((r >> 3) * kKv + (e8 >> 3)) * 2 + (e8 & 1)) * 32 + (r & 7) * 4 + (e8 >> 1 & 3)] = raw[j];
       }
+      __syncwarp();
     }
-    __syncthreads();
-    float rsc[kR];
-    int min_last = 0x7fffffff, max_begin = 0;
+    // the window's rows of this item: the last key that all of them see, the first that one does not
     const int at0 = sq.len - sq.count;                     // position of the window's first query
-#pragma unroll
-    for (int k = 0; k < kR; ++k) {
-      const int r = 8 * (k >> 1) + 2 * t + (k & 1), row = row0 + r, i = row / A.G;
-      rsc[k] = row_scale[r] * A.scale2;
-      if (row < A.R && i < sq.count) {                     // what the other rows get is not written
-        min_last = min(min_last, at0 + i);
-        if (A.span > 0) max_begin = max(max_begin, at0 + i - A.span + 1);
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      min_last = min(min_last, __shfl_xor_sync(0xffffffffu, min_last, o));
-      max_begin = max(max_begin, __shfl_xor_sync(0xffffffffu, max_begin, o));
-    }
+    const int i0 = row0 / A.G, i1 = min((min(row0 + S::kRows, A.R) - 1) / A.G, sq.count - 1);
+    const int min_last = at0 + i0, max_begin = A.span > 0 ? at0 + i1 - A.span + 1 : 0;
     float acc[kMt][kNt][4];
     float mx[kR], sum[kR];
     float vref = 0.f, winv = 0.f;
@@ -431,25 +406,26 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       else nothing();
       look(n + S::kAhead + 1);
       const int chunk = g >> 2;
-      const float ks = sc[2 * chunk];
+      float f = sc[2 * chunk] * rsc;                         // what a raw score is to be multiplied by
       float vs = sc[2 * chunk + 1];
       const int absent = __float_as_int(sc[4]);
       const float v0 = fabsf(sc[1]), v1 = fabsf(sc[3]);
       const bool odd_scale = !(v0 < INFINITY) || !(v1 < INFINITY);
       const float va = fmaxf(v0 < INFINITY ? v0 : 0.f, v1 < INFINITY ? v1 : 0.f);
       const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || odd_scale;
+      if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
+        const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
 #pragma unroll
-      for (int k = 0; k < kR; ++k) {
-        const float f = ks * rsc[k];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          sx[s][k >> 1][k & 1] *= f;
-          sx[s][k >> 1][2 + (k & 1)] *= f;
-        }
+          for (int k = 0; k < kNt; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sx[s][k][e] *= by;
+        f = f < 0.f ? -f : 1.f;
       }
+      uint32_t drop = 0;                                   // which of this thread's 8 value tokens count as 0
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
-      uint32_t drop = 0;                                   // which of this thread's 8 value tokens count as 0
       if (masked) {
         const int have = sq.len - key0 - 8 * t;
         drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
@@ -489,8 +465,8 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       bool move = va > vref;
 #pragma unroll
       for (int k = 0; k < kR; ++k) {
-        top[k] = max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
-                         max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
+        top[k] = f * max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
+                             max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
         move |= !(top[k] <= mx[k] + kSlack);
       }
       if (__any_sync(0xffffffffu, move)) {
@@ -523,29 +499,29 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float e0 = ex2(sx[s][k][2 * e] - mx[2 * k]), e1 = ex2(sx[s][k][2 * e + 1] - mx[2 * k + 1]);
+            const float e0 = ex2(fmaf(sx[s][k][2 * e], f, -mx[2 * k])), e1 = ex2(fmaf(sx[s][k][2 * e + 1], f, -mx[2 * k + 1]));
             sum[2 * k] += e0;
             sum[2 * k + 1] += e1;
             pb[s][k][e] = transpose8(pack_half(e0 * pw, e1 * pw));
           }
 #pragma unroll
       for (int m = 0; m < kMt; ++m) {
-        uint2 v0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
-        uint2 v1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
+        uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
+        uint2 w1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
         if (drop) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (drop >> e & 1) {
               const uint32_t keep = ~(0xffu << (8 * (e & 3)));
-              if (e < 4) v0.x &= keep, v1.x &= keep;
-              else v0.y &= keep, v1.y &= keep;
+              if (e < 4) w0.x &= keep, w1.x &= keep;
+              else w0.y &= keep, w1.y &= keep;
             }
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           uint32_t a[4];
-          widen4(s ? v0.y : v0.x, a[0], a[2]);
-          widen4(s ? v1.y : v1.x, a[1], a[3]);
+          widen4(s ? w0.y : w0.x, a[0], a[2]);
+          widen4(s ? w1.y : w1.x, a[1], a[3]);
 #pragma unroll
           for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
         }
@@ -555,88 +531,75 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       __syncwarp();
     }
     asm volatile("cp.async.wait_group 0;");
-    // the warps' states join in shared memory (the ring is free): output rows in value units
+    // the item's results, or a partial of them (its output in value units, unnormalised)
+    const bool whole = steps == sq.steps;
+    float* part = A.part + ((int64_t)run * 2 + (first_segment ? 0 : 1)) * S::kSlot;
+    const float unit = vref * (1.f / kPScale);
 #pragma unroll
     for (int k = 0; k < kR; ++k) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
-      if (g == 0) {
-        wm[warp][8 * (k >> 1) + 2 * t + (k & 1)] = mx[k];
-        wl[warp][8 * (k >> 1) + 2 * t + (k & 1)] = sum[k];
-      }
-    }
-    __syncthreads();
-    float* wo = reinterpret_cast<float*>(smem);            // [warp][row][kOutStride]
-    const float unit = vref * (1.f / kPScale);
-#pragma unroll
-    for (int k = 0; k < kR; ++k) {
-      float* to = wo + (warp * S::kRows + 8 * (k >> 1) + 2 * t + (k & 1)) * S::kOutStride + g;
-#pragma unroll
-      for (int m = 0; m < kMt; ++m) {
-        to[16 * m] = acc[m][k >> 1][k & 1] * unit;
-        to[16 * m + 8] = acc[m][k >> 1][2 + (k & 1)] * unit;
-      }
-    }
-    __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == sq.tiles;
-    const int live = min(kAttWarps, tile1 - tile0);         // warps that had any
-    float* part = A.part + ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * S::kSlot;
-    for (int i = tid; i < S::kRows * kD / 4; i += kAttThreads) {
-      const int r = i / (kD / 4), d = i % (kD / 4) * 4;
-      if (row0 + r >= A.R) break;
-      float m = wm[0][r];
-      for (int w = 1; w < live; ++w) m = max_nan(m, wm[w][r]);
-      float l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int w = 0; w < live; ++w) {
-        const float c = ex2(wm[w][r] - m);
-        const float4 x = *reinterpret_cast<const float4*>(wo + (w * S::kRows + r) * S::kOutStride + d);
-        l = fmaf(c, wl[w][r], l);
-        o.x = fmaf(c, x.x, o.x);
-        o.y = fmaf(c, x.y, o.y);
-        o.z = fmaf(c, x.z, o.z);
-        o.w = fmaf(c, x.w, o.w);
-      }
+      const int r = 8 * (k >> 1) + 2 * t + (k & 1), row = row0 + r;
+      if (row >= A.R) continue;
       if (whole) {
-        put_row<kD>(A, sq.count, b, h, row0 + r, d, o, m, l);
+        const int i = row / A.G;
+        const float l = i < sq.count ? sum[k] : 0.f;         // a row past the sequence's window gets zeros
+        const float by = l == 0.f ? 0.f : unit / l;
+        const int64_t at = ((int64_t)b * A.W + i) * (H * A.G) + h * A.G + row - i * A.G;
+#pragma unroll
+        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            put_out(A, at * kD + 16 * m + 8 * e + g, l == 0.f ? 0.f : acc[m][k >> 1][2 * e + (k & 1)] * by);
+        if (A.lse && g == 0) A.lse[at] = lse_of(mx[k], l);
       } else {
-        *reinterpret_cast<float4*>(part + r * kD + d) = o;
-        if (d == 0) {
-          part[S::kRows * kD + r] = m;
-          part[S::kRows * kD + S::kRows + r] = l;
+#pragma unroll
+        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) part[r * kD + 16 * m + 8 * e + g] = acc[m][k >> 1][2 * e + (k & 1)] * unit;
+        if (g == 0) {
+          part[S::kRows * kD + r] = mx[k];
+          part[S::kRows * kD + S::kRows + r] = sum[k];
         }
       }
     }
     first_segment = false;
-    u = item_u + tile1;
+    u += steps;
   }
 }
 
-// Joins the partials of an item that several CTAs' runs hold; an item without tiles gets zeros.
-// A CTA has eight rows of an item, a warp each.
-template <int kD, int kNt>
+// Joins the partials of an item that several warps' runs hold; an item without steps gets zeros.
+// kSplit: a CTA has one row, and its warps take the partials in turn (few items, many partials of
+// each); otherwise a warp has a row.
+template <int kD, int kNt, bool kSplit>
 __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
-  __shared__ int64_t red[2 * (kJoinThreads / 32)];
+  constexpr int kV = kD / 32;                                // elements of a lane
+  __shared__ float wo[kSplit ? kJoinWarps : 1][kD];
+  __shared__ float wl[kJoinWarps];
   const int per = A.c.H * A.RT;
-  const int rows8 = blockIdx.x % kNt, ib = blockIdx.x / kNt;
-  const int b = ib / per, item = ib % per, h = item / A.RT, row0 = item % A.RT * S::kRows;
-  const int r = 8 * rows8 + (int)threadIdx.x / 32, lane = threadIdx.x & 31;
-  if (row0 + 8 * rows8 >= A.R) return;
-  const Sums ts = tile_sums(A, b, red);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int ctas = kSplit ? S::kRows : kNt;                  // of an item
+  const int ib = blockIdx.x / ctas;
+  const int r = kSplit ? blockIdx.x % ctas : blockIdx.x % ctas * 8 + warp;
+  const int b = ib / per, item = ib % per, h = item / A.RT, row = item % A.RT * S::kRows + r;
+  const Sums ts = step_sums(A, b, lane);
+  // the partials are there; CTAs without work wait as well, so that this kernel ends after k_attend
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (row >= A.R) return;
   const Seq sq = seq_of(A, b);
-  const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.tiles, u1 = u0 + sq.tiles;
-  const int runs = (int)min((int64_t)A.ctas, units);
+  const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps, u1 = u0 + sq.steps;
+  const int runs = run_count(units, A.ctas * S::kWarps);
   int g0 = 0, g1 = -1;
-  if (sq.tiles) {
-    // the CTAs whose runs [units g / runs, units (g + 1) / runs) meet [u0, u1)
+  if (sq.steps) {
+    // the runs [units g / runs, units (g + 1) / runs) that meet [u0, u1)
     g0 = (int)((u0 * runs) / units);
     while (run_start(units, g0 + 1, runs) <= u0) ++g0;
     while (run_start(units, g0, runs) > u0) --g0;
     g1 = (int)(((u1 - 1) * runs) / units);
     while (run_start(units, g1 + 1, runs) <= u1 - 1) ++g1;
     while (run_start(units, g1, runs) > u1 - 1) --g1;
-    if (g0 == g1) return;                                  // written by that CTA
+    if (g0 == g1) return;                                    // written by that run's warp
   }
   // the item is the first segment of a run that starts inside it or with it, which only g0's may not
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
@@ -645,23 +608,37 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   for (int gi = g0 + lane; gi <= g1; gi += 32) m = max_nan(m, slot_of(gi)[S::kRows * kD + r]);
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int d = 4 * lane;
+  float l = 0.f, o[kV];
+#pragma unroll
+  for (int e = 0; e < kV; ++e) o[e] = 0.f;
 #pragma unroll 4
-  for (int gi = g0; gi <= g1; ++gi) {
+  for (int gi = kSplit ? g0 + warp : g0; gi <= g1; gi += kSplit ? kJoinWarps : 1) {
     const float* slot = slot_of(gi);
     const float c = ex2(slot[S::kRows * kD + r] - m);
     l = fmaf(c, slot[S::kRows * kD + S::kRows + r], l);
-    if (d < kD) {
-      const float4 x = *reinterpret_cast<const float4*>(slot + r * kD + d);
-      o.x = fmaf(c, x.x, o.x);
-      o.y = fmaf(c, x.y, o.y);
-      o.z = fmaf(c, x.z, o.z);
-      o.w = fmaf(c, x.w, o.w);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) o[e] = fmaf(c, slot[r * kD + e * 32 + lane], o[e]);
+  }
+  if constexpr (kSplit) {
+#pragma unroll
+    for (int e = 0; e < kV; ++e) wo[warp][e * 32 + lane] = o[e];
+    if (lane == 0) wl[warp] = l;
+    __syncthreads();
+    if (warp) return;
+    const int parts = min(kJoinWarps, g1 - g0 + 1);
+    for (int w = 1; w < parts; ++w) {
+      l += wl[w];
+#pragma unroll
+      for (int e = 0; e < kV; ++e) o[e] += wo[w][e * 32 + lane];
     }
   }
-  if (d < kD) put_row<kD>(A, sq.count, b, h, row0 + r, d, o, m, l);
+  const int i = row / A.G;
+  if (i >= sq.count) l = 0.f;                                // past the sequence's window
+  const int64_t at = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + row - i * A.G;
+  const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < kV; ++e) put_out(A, at * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
+  if (A.lse && lane == 0) A.lse[at] = lse_of(m, l);
 }
 
 // Row tiles of R rows (as few as kMaxNt eights allow, of about equal size), and the eights of each.
@@ -681,9 +658,21 @@ static cudaError_t launch_attend(const AttendArgs& A, cudaStream_t s) {
   k_attend<kD, kNt><<<(unsigned)A.ctas, S::kThreads, S::kSmem, s>>>(A);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  k_attend_join<kD, kNt><<<(unsigned)((int64_t)A.B * A.c.H * A.RT * kNt), kJoinThreads, 0, s>>>(A);
-  return cudaGetLastError();
+  // the join's CTAs start while the last runs end, and wait for them
+  cudaLaunchConfig_t cfg = {};
+  const int64_t items = (int64_t)A.B * A.c.H * A.RT;
+  const bool split = items * 12 < (int64_t)A.ctas * S::kWarps;       // a dozen partials of an item, or more
+  cfg.gridDim = dim3((unsigned)(items * (split ? S::kRows : kNt)));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return split ? cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, true>, A) : cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, false>, A);
 }
+
 template <int kD>
 cudaError_t launch_attend_d(const AttendArgs& A, int nt, cudaStream_t s) {
   switch (nt) {
