@@ -459,6 +459,9 @@ int sdv_token_scores_train(const void *logits, int64_t row_stride, int N, int V,
                            float *log_sum, uint32_t *status, void *d_logits, int64_t d_stride,
                            sdv_stream_t stream);
 
+/* Bytes of device workspace sdv_token_verify needs; 0 for invalid sizes. */
+size_t sdv_token_verify_workspace_bytes(int B, int L);
+
 /*
  * sdv_token_verify - verification of L drafted tokens of B chains and each chain's next token.
  * With q_j = softmax(target row j / temperature), p_j = softmax(draft row j /
@@ -491,7 +494,7 @@ int sdv_token_verify(const void *target, int64_t target_stride_b, int64_t target
                      float draft_temperature, int mode, const int32_t *L_eff, uint64_t seed,
                      const float *coins, const float *race, int32_t *accepted_len,
                      int32_t *next_token, float *log_ratio_out, uint32_t *status_out,
-                     sdv_stream_t stream);
+                     void *workspace, size_t workspace_bytes, sdv_stream_t stream);
 
 /*
  * The cache: k_codes [pages, H, block, D] and v_codes [pages, H, D, block] hold e4m3 codes (values

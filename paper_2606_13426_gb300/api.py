@@ -377,6 +377,7 @@ def _outs(out, names, n, dtype, dev):
     return {k: _out(out, k, (n,), dtype, dev) for k in names}
 
 
+_verify_workspace = functools.lru_cache(maxsize=None)(B.sdv_token_verify_workspace_bytes)
 _attend_workspace = functools.lru_cache(maxsize=None)(B.sdv_attend_workspace_bytes)
 
 
@@ -463,7 +464,7 @@ def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temper
 
 
 def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L_eff=None, temperature=1.0,
-                 draft_temperature=None, coins=None, race=None, out=None):
+                 draft_temperature=None, coins=None, race=None, workspace=None, out=None):
     """Verification of drafted tokens [B, L] from target logits [B, L + 1, V] and draft logits
     [B, L, V] (sdv_token_verify); returns accepted_len, next_token, status [B] and log_ratio
     [B, L].  draft_temperature defaults to temperature; coins [B, L] and race [B, V] (exponential
@@ -481,11 +482,14 @@ def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L
     _dense("race", race, f32, (Bn, V))
     r = _outs(out, ("accepted_len", "next_token", "status"), Bn, i32, dev)
     r["log_ratio"] = _out(out, "log_ratio", (Bn, L), f32, dev)
+    if workspace is None:
+        workspace = torch.empty(_verify_workspace(Bn, L), dtype=torch.uint8, device=dev)
     B._call("sdv_token_verify", target_logits.data_ptr(), target_logits.stride(0), _row_stride(target_logits),
             draft_logits.data_ptr(), draft_logits.stride(0), _row_stride(draft_logits), tokens.data_ptr(), Bn, L, V, dt,
             float(temperature), float(temperature if draft_temperature is None else draft_temperature), _MODES[mode],
             _ptr(L_eff), int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(coins), _ptr(race), r["accepted_len"].data_ptr(),
-            r["next_token"].data_ptr(), r["log_ratio"].data_ptr(), r["status"].data_ptr(), _stream())
+            r["next_token"].data_ptr(), r["log_ratio"].data_ptr(), r["status"].data_ptr(), workspace.data_ptr(),
+            workspace.numel(), _stream())
     return r
 
 

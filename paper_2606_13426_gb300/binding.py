@@ -87,7 +87,8 @@ SIGNATURES = {
     "sdv_token_scores_train": (_I, [_P, _I64, _I, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _P, _P, _I64,
                                     _P]),
     "sdv_token_verify": (_I, [_P, _I64, _I64, _P, _I64, _I64, _P, _I, _I, _I, _I, _F, _F, _I, _P, _U64,
-                              _P, _P, _P, _P, _P, _P, _P]),
+                              _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "sdv_token_verify_workspace_bytes": (_SZ, [_I, _I]),
     "sdv_cache_append": (_I, [_P, _P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
                               _P, _I, _P, _P, _P, _P]),
     "sdv_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
@@ -341,10 +342,15 @@ def sdv_token_scores_train(logits, row_stride, N, V, dtype, tokens, temperature,
 def sdv_token_verify(target, target_stride_b, target_stride_row, draft, draft_stride_b,
                      draft_stride_row, tokens, B, L, V, dtype, temperature, draft_temperature, mode,
                      L_eff, seed, coins, race, accepted_len, next_token, log_ratio_out, status_out,
-                     stream):
+                     workspace, workspace_bytes, stream):
     return _call("sdv_token_verify", target, target_stride_b, target_stride_row, draft, draft_stride_b,
                  draft_stride_row, tokens, B, L, V, dtype, temperature, draft_temperature, mode, L_eff,
-                 seed, coins, race, accepted_len, next_token, log_ratio_out, status_out, stream)
+                 seed, coins, race, accepted_len, next_token, log_ratio_out, status_out, workspace,
+                 workspace_bytes, stream)
+
+
+def sdv_token_verify_workspace_bytes(B, L):
+    return int(load().sdv_token_verify_workspace_bytes(B, L))
 
 
 def sdv_cache_append(k_new, v_new, stride_b, stride_t, stride_h, dtype, B, W, H, D, block, k_codes,

@@ -141,10 +141,10 @@ static PyObject *train(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 typedef int (*token_verify_fn)(const void *, int64_t, int64_t, const void *, int64_t, int64_t, const int32_t *, int, int, int,
                                int, float, float, int, const int32_t *, uint64_t, const float *, const float *, int32_t *,
-                               int32_t *, float *, uint32_t *, sdv_stream_t);
+                               int32_t *, float *, uint32_t *, void *, size_t, sdv_stream_t);
 static PyObject *token_verify(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
-  if (n != 24) return wrong_count("token_verify", 24, n);
+  if (n != 26) return wrong_count("token_verify", 26, n);
   const token_verify_fn fn = (token_verify_fn)ptr(a[0]);
   ++a;
   const void *q = ptr(a[0]), *p = ptr(a[3]);
@@ -157,11 +157,14 @@ static PyObject *token_verify(PyObject *self, PyObject *const *a, Py_ssize_t n) 
   int32_t *acc = ptr(a[18]), *next = ptr(a[19]);
   float *lr = ptr(a[20]);
   uint32_t *st = ptr(a[21]);
-  const sdv_stream_t stream = ptr(a[22]);
+  void *ws = ptr(a[22]);
+  const size_t bytes = (size_t)u64(a[23]);
+  const sdv_stream_t stream = ptr(a[24]);
   int rc;
   if (PyErr_Occurred()) return NULL;
   Py_BEGIN_ALLOW_THREADS
-  rc = fn(q, qb, qr, p, pb, pr, tokens, B, L, V, dtype, t, td, mode, L_eff, seed, coins, race, acc, next, lr, st, stream);
+  rc = fn(q, qb, qr, p, pb, pr, tokens, B, L, V, dtype, t, td, mode, L_eff, seed, coins, race, acc, next, lr, st, ws, bytes,
+          stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }

@@ -7,17 +7,12 @@
 //   dx_v = (1/T) [g_lp (1[v = t] - p_v) - g_H p_v (log p_v + H)].
 // A row is split over the CTAs of a cluster, which join their statistics through distributed
 // shared memory.
-#include <type_traits>
-
 #include "sdv_tokens.cuh"
 
 namespace sdv {
 
-constexpr int kScoreThreads = 256;
-constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread: all under way at once, and kept
 constexpr int kGroups = 32;            // groups of threads whose maxima give the alternatives' threshold
 constexpr int kCandMax = 512;          // candidates a CTA ranks; more: k passes over its part
-constexpr int kScoreMaxCluster = 8;
 
 struct ScoreArgs {
   const void* x;
@@ -96,55 +91,7 @@ __device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put
   }
 }
 
-// A thread's part of a row: vectors v0 + tid + u kThreads < v1 (kept as read, where kKeep), and one
-// of the row's single elements.
-template <int kDtype, int kThreads>
-struct Part {
-  using E = Num<kDtype>;
-  const uint4* vec;
-  int v0, v1, single;
-  float x;
-  uint4 raw[kScoreVecs];
-  __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int C) {
-    vec = R.vec();
-    v0 = (int)((int64_t)R.nvec * rank / C) + (int)threadIdx.x;
-    v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
-    single = rank == 0 && (int)threadIdx.x < R.singles() ? R.single(threadIdx.x) : -1;
-    x = single >= 0 ? E::to(R.p[single]) : 0.f;
-  }
-  __device__ __forceinline__ bool has(int u) const { return v0 + u * kThreads < v1; }
-  // Statistics; the vectors are (the last kScoreVecs of them stay) in raw.
-  template <bool kAll>
-  __device__ __forceinline__ void batch(Run& r, float c) {
-#pragma unroll
-    for (int u = 0; u < kScoreVecs; ++u)
-      if (kAll || has(u)) raw[u] = vec[v0 + u * kThreads];
-#pragma unroll
-    for (int u = 0; u < kScoreVecs; ++u)
-      if (kAll || has(u)) {
-        float f[E::kPer16];
-        run_see(r, vec_max<kDtype>(raw[u]), c);
-        E::unpack(raw[u], f);
-        run_add<E::kPer16>(r, f, c);
-      }
-  }
-  // Whether every thread of the CTA has all of a batch from v0 on.
-  __device__ __forceinline__ bool full() const { return v0 - (int)threadIdx.x + kScoreVecs * kThreads <= v1; }
-  __device__ __forceinline__ Run read(float c) {
-    Run r = run_empty();
-    for (;;) {
-      if (full()) batch<true>(r, c);
-      else batch<false>(r, c);
-      if (v0 - (int)threadIdx.x + kScoreVecs * kThreads >= v1) break;
-      v0 += kScoreVecs * kThreads;
-    }
-    if (single >= 0) run_one(r, x, c);
-    return r;
-  }
-};
-
-// kKept: a CTA's part of the row fits its registers, and is not read again for the alternatives.
-template <int kDtype, bool kTop, bool kKept>
+template <int kDtype, bool kTop>
 __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
@@ -166,7 +113,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   const Row<kDtype> R(row, A.V);
   Part<kDtype, kScoreThreads> P(R, rank, C);
   const int first = P.v0;
-  const Run run = P.read(A.c);
+  const Run run = P.template read<false>(A.c);
   const float tm = run.top;                   // the largest of this thread's logits
   Stat a = run_warp(run, A.c);
   if constexpr (kTop) {
@@ -197,22 +144,24 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
         if (at < kCandMax) cand[at] = Cand{x, i};
       }
     };
-    auto keep_vec = [&](const uint4& raw, int v) {
-      if (vec_max<kDtype>(raw) >= thr) {
-        float f[kPer];
-        E::unpack(raw, f);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) keep(f[e], R.head + v * kPer + e);
-      }
-    };
     if (tm >= thr) {
-      if constexpr (kKept) {
+      // a thread that has candidates (about as many as alternatives are wanted) reads its vectors again
+#pragma unroll 1
+      for (int v = first; v < P.v1; v += 4 * kScoreThreads) {
+        uint4 raw[4];
 #pragma unroll
-        for (int u = 0; u < kScoreVecs; ++u)
-          if (P.has(u)) keep_vec(P.raw[u], P.v0 + u * kScoreThreads);
-      } else {
-#pragma unroll 4
-        for (int v = first; v < P.v1; v += kScoreThreads) keep_vec(__ldg(P.vec + v), v);
+        for (int u = 0; u < 4; ++u) {
+          raw[u] = vec_masked<kDtype>();
+          if (v + u * kScoreThreads < P.v1) raw[u] = __ldg(P.vec + v + u * kScoreThreads);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (vec_max<kDtype>(raw[u]) >= thr) {
+            float f[kPer];
+            E::unpack(raw[u], f);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) keep(f[e], R.head + (v + u * kScoreThreads) * kPer + e);
+          }
       }
       if (P.single >= 0) keep(P.x, P.single);
     }
@@ -426,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_scores_train(cons
   T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
   const Row<kDtype> R(row, A.S.V);
   Part<kDtype, kThreads> P(R, rank, C);
-  const Stat mine = run_warp(P.read(A.S.c), A.S.c);
+  const Stat mine = run_warp(P.template read<true>(A.S.c), A.S.c);
   // the token, and whether one of this thread's vectors holds it
   const Token tok = row_token<kDtype>(A.S, row, n);
   const float g_lp = A.g_lp ? A.g_lp[n] : 0.f, g_h = A.g_h ? A.g_h[n] : 0.f;
@@ -441,32 +390,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_scores_train(cons
   const float log_s = logf(a.s);
   const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, tok.t, A.S.V, g_lp, g_h, A.S.inv_t);
   T* to = out + R.head + P.v0 * kPer;
-  auto write = [&](auto all, bool vec) {
-#pragma unroll
-    for (int u = 0; u < kScoreVecs; ++u)
-      if (decltype(all)::value || P.has(u)) {
-        float f[kPer], o[kPer];
-        E::unpack(P.raw[u], f);
-        grad_vec<kPer>(g, f, o, A.S.c);
-        put_vec<kDtype>(to + u * kThreads * kPer, o, vec);
-      }
-  };
   const bool vec = same_phase<kDtype>(row, out);
-  if (P.full() && vec) write(std::true_type{}, true);
-  else write(std::false_type{}, vec);
+#pragma unroll
+  for (int u = 0; u < kScoreVecs; ++u)
+    if (P.has(u)) {
+      float f[kPer], o[kPer];
+      E::unpack(P.raw[u], f);
+      grad_vec<kPer>(g, f, o, A.S.c);
+      put_vec<kDtype>(to + u * kThreads * kPer, o, vec);
+    }
   if (own) out[tok.t] = E::from(grad_one(g, tok.x, tok.t, A.S.c));
   if (P.single >= 0) out[P.single] = E::from(grad_one(g, P.x, P.single, A.S.c));
-}
-
-// CTAs per row: as many as keep the row in their registers, and while there are fewer than two CTAs
-// an SM, as many as leave every thread a vector.
-static int score_cluster(int64_t N, int V, int dtype) {
-  const int64_t nvec = (int64_t)V * (int64_t)elem_bytes(dtype) / 16;
-  int c = 1;
-  while (c < kScoreMaxCluster && (nvec > (int64_t)c * kScoreThreads * kScoreVecs ||
-                                  (N * c < 2 * sm_count() && nvec >= 2 * c * kScoreThreads)))
-    c *= 2;
-  return c;
 }
 
 static int check_rows(const void* x, int64_t stride, int N, int V, int dtype, float temperature) {
@@ -481,11 +415,8 @@ template <int kDtype>
 static cudaError_t launch_scores(const ScoreArgs& A, int N, int dtype, cudaStream_t s) {
   const int C = score_cluster(N, A.V, dtype);
   const dim3 grid((unsigned)(N * (int64_t)C));
-  const int64_t nvec = ((int64_t)A.V * (int64_t)elem_bytes(dtype) + 15) / 16;
-  const bool kept = nvec <= (int64_t)C * kScoreThreads * kScoreVecs;
-  if (A.top_k && kept) return launch_cluster(k_scores<kDtype, true, true>, grid, kScoreThreads, 0, (unsigned)C, s, A);
-  if (A.top_k) return launch_cluster(k_scores<kDtype, true, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
-  return launch_cluster(k_scores<kDtype, false, false>, grid, kScoreThreads, 0, (unsigned)C, s, A);
+  if (A.top_k) return launch_cluster(k_scores<kDtype, true>, grid, kScoreThreads, 0, (unsigned)C, false, s, A);
+  return launch_cluster(k_scores<kDtype, false>, grid, kScoreThreads, 0, (unsigned)C, false, s, A);
 }
 
 // CTAs per row of k_scores_train and their threads: as few as hold the row; c = 0 if the largest
@@ -513,8 +444,8 @@ static cudaError_t launch_grad(const GradArgs& G, int N, int dtype, cudaStream_t
 template <int kDtype>
 static cudaError_t launch_train(const TrainArgs& A, int N, TrainShape t, cudaStream_t s) {
   const dim3 grid((unsigned)(N * (int64_t)t.c));
-  if (t.threads == 256) return launch_cluster(k_scores_train<kDtype, 256>, grid, 256, 0, (unsigned)t.c, s, A);
-  return launch_cluster(k_scores_train<kDtype, 512>, grid, 512, 0, (unsigned)t.c, s, A);
+  if (t.threads == 256) return launch_cluster(k_scores_train<kDtype, 256>, grid, 256, 0, (unsigned)t.c, false, s, A);
+  return launch_cluster(k_scores_train<kDtype, 512>, grid, 512, 0, (unsigned)t.c, false, s, A);
 }
 
 }  // namespace sdv

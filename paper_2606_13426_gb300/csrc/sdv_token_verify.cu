@@ -8,21 +8,20 @@
 // row behind the accepted tokens, normalised, or q of the last row on full accept: the index of
 // the largest r_v / E_v, the E_v exponential variates (a race, which needs no cumulated sums).
 //
-// One cluster of CTAs per chain; each CTA has a part of every row's columns.  The statistics of
-// all rows come first (one read of the logits), are joined through distributed shared memory,
-// and the masses v_j that can matter and the race are taken from a second read of those rows,
-// which the L2 still holds.  h_j <= alpha_j, so that a step with eta_j >= alpha_j fails, and one
-// with alpha_j = 1 succeeds, without its mass.
+// k_token_stats takes every row's softmax statistics, one read of the logits with all rows alike, a
+// cluster of CTAs each.  k_token_verify has a cluster of CTAs per chain, each with a part of
+// every row's columns: the masses v_j that can matter and the race are taken from a second read
+// of those rows, which the L2 still holds.  h_j <= alpha_j, so that a step with eta_j >= alpha_j
+// fails, and one with alpha_j = 1 succeeds, without its mass.
 #include "sdv_device.cuh"
 #include "sdv_tokens.cuh"
 
 namespace sdv {
 
-constexpr int kVerThreads = 512;
+constexpr int kVerThreads = 256;
 constexpr int kVerWarps = kVerThreads / 32;
-constexpr int kVerMaxCluster = 8;
-constexpr int kVerSegs = 8;            // segments of a CTA's part of a row, a warp each
-constexpr int kBatch = 8;
+constexpr int kVerMaxCluster = 16;
+constexpr int kVerSegs = kVerWarps;    // segments of a CTA's part of a row, a warp each
 constexpr int kVerRows = 2 * SDV_MAX_L + 1;
 constexpr uint32_t kStreamRace = 7;
 
@@ -41,6 +40,7 @@ struct TokenVerifyArgs {
   int32_t* next;
   float* ell;
   uint32_t* status;
+  struct RowStat* stats;                // workspace [B, 2 L + 1]: target rows, then draft rows
 };
 
 struct Best {
@@ -62,128 +62,104 @@ __device__ __forceinline__ float prob(const RowStat& r, float x, float c, float 
   return ex2(fmaf(fmaxf(x - r.m, kFar), c, shift - r.l2));
 }
 
-// Calls f(index, q, p) for this thread's share (of `step` threads) of elements [.., ..) of two rows;
-// part `part` of `parts`.  Rows in the same phase of 16 bytes are read as vectors.
+// Four exponential variates: E_v of elements 4 block .. 4 block + 3 of chain b, from the seed.
+static __device__ __noinline__ float4 race4(uint64_t seed, uint32_t b, uint32_t block) {
+  const uint4 w = philox_block(seed, b, block, kStreamRace, 0);
+  return make_float4(-log_uniform(w.x), -log_uniform(w.y), -log_uniform(w.z), -log_uniform(w.w));
+}
+
+// Calls f(first index, n, q, p) with n <= 8 (kPer) consecutive elements of two rows at a time: this
+// thread's share (of `step` threads) of part `part` of `parts`.  Rows in the same phase of 16 bytes
+// are read as vectors, others element by element, a warp's next to each other (n = 1).  The body of
+// f is there once: the passes over the rows run from a cold instruction cache.
 template <int kDtype, typename F>
 __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, int V, int part,
                                           int parts, int lane, int step, F f) {
   using E = Num<kDtype>;
-  constexpr int kPer = E::kPer16;
-  if (((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0) {
-    const Row<kDtype> R(q, V);
-    const uint4* vq = R.vec();
-    const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
-    const int v0 = (int)((int64_t)R.nvec * part / parts), v1 = (int)((int64_t)R.nvec * (part + 1) / parts);
-    int v = v0 + lane;
-    for (; v + 3 * step < v1; v += 4 * step) {
-      uint4 a[4], b[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        a[u] = __ldg(vq + v + u * step);
-        b[u] = __ldg(vp + v + u * step);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float x[kPer], y[kPer];
-        E::unpack(a[u], x);
-        E::unpack(b[u], y);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) f(R.head + (v + u * step) * kPer + e, x[e], y[e]);
-      }
-    }
-    for (; v < v1; v += step) {
+  constexpr int kPer = E::kPer16, kUn = 2;
+  const bool vec = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0;
+  const Row<kDtype> R(q, V);
+  const int total = vec ? R.nvec : V / kPer * kPer / kPer;          // groups of kPer
+  const int g0 = (int)((int64_t)total * part / parts), g1 = (int)((int64_t)total * (part + 1) / parts);
+  const uint4* vq = R.vec();
+  const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
+  const int done = vec ? R.head + R.nvec * kPer : total * kPer, head = vec ? R.head : 0;
+  // elements outside of the groups first: at most 2 kPer - 2
+  if (part == 0) {
+    const int rest = head + V - done;
+    for (int s = lane; s < rest; s += step) {
+      const int i = s < head ? s : done + s - head;
       float x[kPer], y[kPer];
-      E::unpack(__ldg(vq + v), x);
-      E::unpack(__ldg(vp + v), y);
+      x[0] = E::to(q[i]);
+      y[0] = E::to(p[i]);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) f(R.head + v * kPer + e, x[e], y[e]);
+      for (int e = 1; e < kPer; ++e) x[e] = y[e] = -INFINITY;
+      f(i, 1, x, y);
     }
-    if (part == 0)
-      for (int s = lane; s < R.singles(); s += step) f(R.single(s), E::to(q[R.single(s)]), E::to(p[R.single(s)]));
-  } else {
-    const int e0 = (int)((int64_t)V * part / parts), e1 = (int)((int64_t)V * (part + 1) / parts);
-    int e = e0 + lane;
-    for (; e + 7 * step < e1; e += 8 * step) {
-      float x[8], y[8];
+  }
+#pragma unroll 1
+  for (int g = g0 + lane; g - lane < g1; g += kUn * step) {
+    float x[kUn][kPer], y[kUn][kPer];
+    if (vec) {
+      uint4 a[kUn], b[kUn];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        x[u] = E::to(q[e + u * step]);
-        y[u] = E::to(p[e + u * step]);
+      for (int u = 0; u < kUn; ++u) {
+        a[u] = b[u] = vec_masked<kDtype>();
+        if (g + u * step < g1) {
+          a[u] = __ldg(vq + g + u * step);
+          b[u] = __ldg(vp + g + u * step);
+        }
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) f(e + u * step, x[u], y[u]);
+      for (int u = 0; u < kUn; ++u) {
+        E::unpack(a[u], x[u]);
+        E::unpack(b[u], y[u]);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUn; ++u)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const bool in = g + u * step < g1;
+          const int i = (g + u * step) * kPer + e;
+          x[u][e] = in ? E::to(q[i]) : -INFINITY;
+          y[u][e] = in ? E::to(p[i]) : -INFINITY;
+        }
     }
-    for (; e < e1; e += step) f(e, E::to(q[e]), E::to(p[e]));
+#pragma unroll
+    for (int u = 0; u < kUn; ++u)
+      if (g + u * step < g1) f(head + (g + u * step) * kPer, kPer, x[u], y[u]);
   }
 }
 
-// Calls f(index, q, p, race) for this thread's share of part `part` of `parts` of the rows.
-template <int kDtype, typename F>
-__device__ __forceinline__ void each_race(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, const float* race,
-                                          int V, int part, int parts, int tid, F f) {
-  using E = Num<kDtype>;
-  constexpr int kPer = E::kPer16, kUn = kPer == 8 ? 2 : 4;
-  const Row<kDtype> R(q, V);
-  const bool whole = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0 && aligned16(race + R.head);
-  if (whole) {
-    const uint4* vq = R.vec();
-    const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
-    const float4* vr = reinterpret_cast<const float4*>(race + R.head);
-    const int v0 = (int)((int64_t)R.nvec * part / parts), v1 = (int)((int64_t)R.nvec * (part + 1) / parts);
-    for (int v = v0 + tid; v < v1; v += kUn * kVerThreads) {
-      uint4 a[kUn], b[kUn];
-      float4 e[kUn * kPer / 4];
-#pragma unroll
-      for (int u = 0; u < kUn; ++u) {
-        const int w = v + u * kVerThreads;
-        if (w < v1) {
-          a[u] = __ldg(vq + w);
-          b[u] = __ldg(vp + w);
-#pragma unroll
-          for (int k = 0; k < kPer / 4; ++k) e[u * (kPer / 4) + k] = __ldg(vr + (int64_t)w * (kPer / 4) + k);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kUn; ++u) {
-        const int w = v + u * kVerThreads;
-        if (w < v1) {
-          float x[kPer], y[kPer];
-          E::unpack(a[u], x);
-          E::unpack(b[u], y);
-#pragma unroll
-          for (int k = 0; k < kPer; ++k) {
-            const float4 ev = e[u * (kPer / 4) + k / 4];
-            f(R.head + w * kPer + k, x[k], y[k], k % 4 == 0 ? ev.x : k % 4 == 1 ? ev.y : k % 4 == 2 ? ev.z : ev.w);
-          }
-        }
-      }
-    }
-    if (part == 0 && tid < R.singles()) {
-      const int i = R.single(tid);
-      f(i, E::to(q[i]), E::to(p[i]), race[i]);
-    }
-  } else {
-    const int e0 = (int)((int64_t)V * part / parts), e1 = (int)((int64_t)V * (part + 1) / parts);
-    for (int e = e0 + tid; e < e1; e += 8 * kVerThreads) {
-      float x[8], y[8], z[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int i = e + u * kVerThreads;
-        if (i < e1) {
-          x[u] = E::to(q[i]);
-          y[u] = E::to(p[i]);
-          z[u] = race[i];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (e + u * kVerThreads < e1) f(e + u * kVerThreads, x[u], y[u], z[u]);
-    }
-  }
+// The statistics of one row a cluster; rows past a chain's window are left out.
+template <int kDtype>
+__global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVerifyArgs A) {
+  using T = typename Num<kDtype>::T;
+  constexpr int kWarps = kScoreThreads / 32;
+  cg::cluster_group cl = cg::this_cluster();
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int n = blockIdx.x / C, per = 2 * A.L + 1, b = n / per, r = n % per;
+  const int window = A.L_eff ? min(A.L_eff[b], A.L) : A.L;
+  if (r <= A.L ? r > window : r - A.L - 1 >= window) return;
+  __shared__ Stat stats[kScoreMaxCluster * kWarps];
+  if (C > 1) cl.barrier_arrive();
+  const T* row = r <= A.L ? reinterpret_cast<const T*>(A.q) + b * A.q_sb + r * A.q_sr
+                          : reinterpret_cast<const T*>(A.p) + b * A.p_sb + (r - A.L - 1) * A.p_sr;
+  const float c = r <= A.L ? A.cq : A.cp;
+  Part<kDtype, kScoreThreads, false> P(Row<kDtype>(row, A.V), rank, C);
+  const Stat a = run_warp(P.template read<false>(c), c);
+  if (C > 1) cl.barrier_wait();
+  if ((threadIdx.x & 31) == 0) (C > 1 ? cl.map_shared_rank(stats, 0) : stats)[rank * kWarps + threadIdx.x / 32] = Stat{a.m, a.s, 0.f};
+  if (C > 1) cl.sync();
+  else __syncthreads();
+  if (rank || threadIdx.x >= 32) return;
+  const Stat all = stat_gather(stats, C * kWarps, threadIdx.x, c);
+  if (threadIdx.x == 0) A.stats[n] = RowStat{all.m, log2f(all.s)};
 }
 
 template <int kDtype>
-__global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyArgs A) {
+__global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVerifyArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
@@ -193,6 +169,7 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   const int L = A.L, V = A.V;
   const int n_in = A.L_eff ? A.L_eff[b] : L;
   if (n_in < 0) {                                  // an inactive chain
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (rank == 0) {
       if (tid == 0) {
         A.accepted[b] = 0;
@@ -206,8 +183,6 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   }
   const int n = min(n_in, L);
   const int rows = 2 * n + 1;
-  __shared__ RowStat seg[kVerRows * kVerSegs];              // a CTA's segments of a row: m and s
-  __shared__ RowStat part_s[kVerMaxCluster * kVerRows];      // the CTAs' parts
   __shared__ RowStat rs[kVerRows];
   __shared__ float mass_seg[SDV_MAX_L * kVerSegs];
   __shared__ float mass_part[kVerMaxCluster * SDV_MAX_L];
@@ -221,98 +196,41 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   if (tid == 0) status_s = 0;
   const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
   const T* p0 = reinterpret_cast<const T*>(A.p) + b * A.p_sb;
-  auto row_of = [&](int r) { return r <= n ? q0 + r * A.q_sr : p0 + (r - n - 1) * A.p_sr; };
-  // statistics: target rows 0 .. n, then draft rows 0 .. n - 1, a warp per segment of a row; the
-  // next kBatch vectors of each lane are under way while it works on the last ones
+  // what is needed later and known now: this thread's step's token and its logits; the race's part
+  int my_token = -1;
+  float my_xq = 0.f, my_xp = 0.f;
+  if (tid < n) {
+    my_token = A.tokens[(int64_t)b * L + tid];
+    if (my_token >= 0 && my_token < V) {
+      my_xq = E::to(q0[tid * A.q_sr + my_token]);
+      my_xp = E::to(p0[tid * A.p_sr + my_token]);
+    }
+  }
+  if (A.race) {
+    const float* race = A.race + (int64_t)b * V;
+    for (int i = (int)((int64_t)V * rank / C) + tid * 32; i < (int)((int64_t)V * (rank + 1) / C); i += kVerThreads * 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
+  }
   const int parts = C * kVerSegs;
-  {
-    struct At {
-      int u, v, v1;                                            // unit, this lane's vector, the unit's end
-    };
-    auto unit = [&](int u) {
-      At a{u, 0, 0};
-      if (u < rows * kVerSegs) {
-        const Row<kDtype> R(row_of(u / kVerSegs), V);
-        const int sg = rank * kVerSegs + u % kVerSegs;
-        a.v = (int)((int64_t)R.nvec * sg / parts) + lane;
-        a.v1 = (int)((int64_t)R.nvec * (sg + 1) / parts);
-      }
-      return a;
-    };
-    auto load = [&](const At& a, uint4* raw) {
-      if (a.u >= rows * kVerSegs) return;
-      const uint4* vec = Row<kDtype>(row_of(a.u / kVerSegs), V).vec() + a.v;
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k)
-        if (a.v + 32 * k < a.v1) raw[k] = __ldg(vec + 32 * k);
-    };
-    uint4 raw[kBatch], ahead[kBatch];
-    At at = unit(warp);
-    load(at, raw);
-    Run run = run_empty();
-    while (at.u < rows * kVerSegs) {
-      const int r = at.u / kVerSegs;
-      const float c = r <= n ? A.cq : A.cp;
-      At next = at;
-      next.v += 32 * kBatch;
-      const bool last = next.v - lane >= at.v1;
-      if (last) next = unit(at.u + kVerWarps);
-      load(next, ahead);
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k)
-        if (at.v + 32 * k < at.v1) {
-          float f[kPer];
-          run_see(run, vec_max<kDtype>(raw[k]), c);
-          E::unpack(raw[k], f);
-          run_add<kPer>(run, f, c);
-        }
-      if (last) {
-        if (rank == 0 && at.u % kVerSegs == 0) {
-          const T* row = row_of(r);
-          const Row<kDtype> R(row, V);
-          if (lane < R.singles()) run_one(run, E::to(row[R.single(lane)]), c);
-        }
-        const Stat a = run_warp(run, c);
-        if (lane == 0) seg[at.u] = RowStat{a.m, a.s};
-        run = run_empty();
-      }
-      at = next;
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) raw[k] = ahead[k];
-    }
-  }
-  __syncthreads();
-  if (C > 1) cl.barrier_wait();
-  auto join = [&](const RowStat* from, int count, int stride, float c) {
-    Stat a{from[0].m, from[0].l2, 0.f};
-    for (int i = 1; i < count; ++i) a = stat_join(a, Stat{from[i * stride].m, from[i * stride].l2, 0.f}, c);
-    return a;
-  };
+  asm volatile("griddepcontrol.wait;" ::: "memory");         // the rows' statistics are there
   for (int r = tid; r < rows; r += kVerThreads) {
-    const Stat a = join(seg + r * kVerSegs, kVerSegs, 1, r <= n ? A.cq : A.cp);
-    for (int k = 0; k < C; ++k) {
-      RowStat* to = C > 1 ? cl.map_shared_rank(part_s, k) : part_s;
-      to[rank * kVerRows + r] = RowStat{a.m, a.s};
-    }
-  }
-  if (C > 1) cl.sync();
-  else __syncthreads();
-  for (int r = tid; r < rows; r += kVerThreads) {
-    const Stat a = join(part_s + r, C, kVerRows, r <= n ? A.cq : A.cp);
-    rs[r] = RowStat{a.m, log2f(a.s)};
+    const RowStat a = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
+    rs[r] = a;
     uint32_t st = 0;
     if (!(a.m < INFINITY)) st |= SDV_STATUS_NONFINITE;
     if (a.m == -INFINITY) st |= SDV_STATUS_EMPTY_ROW;
     if (st) atomicOr(&status_s, st);
   }
+  if (C > 1) cl.barrier_wait();                              // every CTA of the cluster has started
   __syncthreads();
   // log ratios and coins
-  for (int j = tid; j < n; j += kVerThreads) {
-    const int t = A.tokens[(int64_t)b * L + j];
+  static_assert(SDV_MAX_L <= kVerThreads, "a thread per step");
+  if (tid < n) {
+    const int j = tid, t = my_token;
     float ell = NAN;
     if (t >= 0 && t < V) {
       const RowStat rq = rs[j], rp = rs[n + 1 + j];
-      const float xq = E::to(q0[j * A.q_sr + t]), xp = E::to(p0[j * A.p_sr + t]);
+      const float xq = my_xq, xp = my_xp;
       if (rq.m < INFINITY && rp.m < INFINITY) {
         const float lq = row_ok(rq) && xq > -INFINITY ? (xq - rq.m) * A.iq - rq.l2 * kLn2f : -INFINITY;
         const float lp = row_ok(rp) && xp > -INFINITY ? (xp - rp.m) * A.ip - rp.l2 * kLn2f : -INFINITY;
@@ -361,10 +279,11 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
       const float sh = la[j] * kLog2E;
       float sum = 0.f;
       const bool has_p = row_ok(rp);
-      each_pair<kDtype>(q0 + j * A.q_sr, p0 + j * A.p_sr, V, rank * kVerSegs + u % kVerSegs, parts, lane, 32,
-                        [&](int, float x, float y) {
-                          const float d = prob(rq, x, A.cq, sh) - (has_p ? prob(rp, y, A.cp, 0.f) : 0.f);
-                          sum += fmaxf(d, 0.f);
+      each_pair<kDtype>(q0 + j * A.q_sr, has_p ? p0 + j * A.p_sr : q0 + j * A.q_sr, V, rank * kVerSegs + u % kVerSegs, parts, lane, 32,
+                        [&](int, int, const float* x, const float* y) {
+#pragma unroll
+                          for (int e = 0; e < kPer; ++e)
+                            sum += fmaxf(prob(rq, x[e], A.cq, sh) - (has_p ? prob(rp, y[e], A.cp, 0.f) : 0.f), 0.f);
                         });
 #pragma unroll
       for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -402,31 +321,38 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
     const bool rest = attempt == 0 && acc < n && row_ok(rp);
     const T* p = rest ? p0 + acc * A.p_sr : q;
     Racer top{0.f, 1.f, 0x7fffffff};
-    if (row_ok(rq)) {
-      if (A.race) {
-        const float* race = A.race + (int64_t)b * V;
-        each_race<kDtype>(q, p, race, V, rank, C, tid, [&](int i, float x, float y, float e) {
-          const float r = prob(rq, x, A.cq, rest ? sh : 0.f) - (rest ? prob(rp, y, A.cp, 0.f) : 0.f);
-          const float mine = r * top.e, theirs = top.r * e;      // r / e against the best so far
-          if (mine > theirs || (mine == theirs && r > 0.f && i < top.i)) top = Racer{r, e, i};
-        });
-      } else {
-        int blk = -1;
-        uint4 w = make_uint4(0, 0, 0, 0);
-        each_pair<kDtype>(q, p, V, rank, C, tid, kVerThreads, [&](int i, float x, float y) {
-          const float r = prob(rq, x, A.cq, rest ? sh : 0.f) - (rest ? prob(rp, y, A.cp, 0.f) : 0.f);
-          if (!(r > 0.f)) return;
-          if ((i >> 2) != blk) {
-            blk = i >> 2;
-            w = philox_block(A.seed, (uint32_t)b, (uint32_t)blk, kStreamRace, 0);
+    const float* race = A.race ? A.race + (int64_t)b * V : nullptr;
+    if (row_ok(rq))
+      each_pair<kDtype>(q, p, V, rank, C, tid, kVerThreads, [&](int i, int count, const float* x, const float* y) {
+        float r[kPer], e[kPer];
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+          r[k] = prob(rq, x[k], A.cq, rest ? sh : 0.f) - (rest ? prob(rp, y[k], A.cp, 0.f) : 0.f);
+          any |= r[k] > 0.f;
+        }
+        if (!any) return;
+        if (race && count == kPer && aligned16(race + i)) {
+#pragma unroll
+          for (int k = 0; k < kPer; k += 4) *reinterpret_cast<float4*>(e + k) = __ldg(reinterpret_cast<const float4*>(race + i + k));
+        } else if (race) {
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) e[k] = k < count ? __ldg(race + i + k) : 1.f;
+        } else {
+          float4 four = race4(A.seed, (uint32_t)b, (uint32_t)i >> 2);
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) {
+            if (k && ((i + k) & 3) == 0) four = race4(A.seed, (uint32_t)b, (uint32_t)(i + k) >> 2);
+            const int w = (i + k) & 3;
+            e[k] = w == 0 ? four.x : w == 1 ? four.y : w == 2 ? four.z : four.w;
           }
-          const uint32_t k = i & 3;
-          const float e = -log_uniform(k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w);
-          const float mine = r * top.e, theirs = top.r * e;
-          if (mine > theirs || (mine == theirs && i < top.i)) top = Racer{r, e, i};
-        });
-      }
-    }
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {                            // r / e against the best so far
+          const float mine = r[k] * top.e, theirs = top.r * e[k];
+          if (mine > theirs || (mine == theirs && r[k] > 0.f && i + k < top.i)) top = Racer{r[k], e[k], i + k};
+        }
+      });
     Best me{top.r > 0.f ? top.r / top.e : 0.f, top.i};
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -466,18 +392,27 @@ __global__ void __launch_bounds__(kVerThreads) k_token_verify(const TokenVerifyA
   }
 }
 
-// CTAs per chain.
+// CTAs per chain: as many as fit beside the other chains' (four an SM, some left for clusters that do
+// not fill their part of the chip), as long as each thread has a vector of a row.  Clusters of 16
+// leave fewer places than those of 8.
 static int verify_cluster(int B, int V, int dtype) {
   const int64_t nvec = (int64_t)V * (int64_t)elem_bytes(dtype) / 16;
   int c = 1;
-  while (c < kVerMaxCluster && (int64_t)B * c < 2 * sm_count() && nvec / (2 * c) >= 32 * kVerSegs) c *= 2;
+  while (c < kVerMaxCluster && (int64_t)B * 2 * c <= 3 * sm_count() && nvec >= 2 * c * kVerThreads) c *= 2;
   return c;
 }
 
 template <int kDtype>
 static cudaError_t launch_token_verify(const TokenVerifyArgs& A, int B, int dtype, cudaStream_t s) {
   const int C = verify_cluster(B, A.V, dtype);
-  return launch_cluster(k_token_verify<kDtype>, dim3((unsigned)B * (unsigned)C), kVerThreads, 0, (unsigned)C, s, A);
+  if (C > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(k_token_verify<kDtype>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  const int rows = B * (2 * A.L + 1), Cs = score_cluster(rows, A.V, dtype);
+  const cudaError_t e = launch_cluster(k_token_stats<kDtype>, dim3((unsigned)rows * (unsigned)Cs), kScoreThreads, 0, (unsigned)Cs, false, s, A);
+  if (e != cudaSuccess) return e;
+  return launch_cluster(k_token_verify<kDtype>, dim3((unsigned)B * (unsigned)C), kVerThreads, 0, (unsigned)C, true, s, A);
 }
 
 }  // namespace sdv
@@ -486,12 +421,18 @@ using namespace sdv;
 
 extern "C" {
 
+size_t sdv_token_verify_workspace_bytes(int B, int L) {
+  if (B < 1 || B > (1 << 20) || L < 1 || L > SDV_MAX_L) return 0;
+  return ((size_t)B * (2 * L + 1) * sizeof(RowStat) + 255) / 256 * 256;
+}
+
 int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target_stride_row, const void* draft,
                      int64_t draft_stride_b, int64_t draft_stride_row, const int32_t* tokens, int B, int L, int V, int dtype,
                      float temperature, float draft_temperature, int mode, const int32_t* L_eff, uint64_t seed,
                      const float* coins, const float* race, int32_t* accepted_len, int32_t* next_token,
-                     float* log_ratio_out, uint32_t* status_out, sdv_stream_t stream) {
-  if (B < 1 || B > (1 << 27) || L < 1 || L > SDV_MAX_L || V < 1 || V > (1 << 30) || !token_dtype(dtype)) return SDV_EINVAL;
+                     float* log_ratio_out, uint32_t* status_out, void* workspace, size_t workspace_bytes,
+                     sdv_stream_t stream) {
+  if (B < 1 || B > (1 << 20) || L < 1 || L > SDV_MAX_L || V < 1 || V > (1 << 30) || !token_dtype(dtype)) return SDV_EINVAL;
   if (mode != SDV_MODE_SAMPLE && mode != SDV_MODE_BLOCK) return SDV_EINVAL;
   const float t[2] = {temperature, draft_temperature};
   for (float x : t)
@@ -502,10 +443,12 @@ int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target
   const void* four[] = {tokens, L_eff, coins, race, accepted_len, next_token, log_ratio_out, status_out};
   for (const void* p : four)
     if (!aligned_to(p, 4)) return SDV_EALIGN;
+  if (!workspace || workspace_bytes < sdv_token_verify_workspace_bytes(B, L)) return SDV_ENOWORKSPACE;
+  if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   const TokenVerifyArgs A{target, draft, target_stride_b, target_stride_row, draft_stride_b, draft_stride_row, tokens, L, V,
                           mode, kLog2E / temperature, kLog2E / draft_temperature, 1.f / temperature,
                           1.f / draft_temperature, L_eff, seed, coins, race, accepted_len, next_token, log_ratio_out,
-                          status_out};
+                          status_out, (RowStat*)workspace};
   cudaStream_t s = (cudaStream_t)stream;
   return launched(dtype == SDV_F32    ? launch_token_verify<SDV_F32>(A, B, dtype, s)
                   : dtype == SDV_BF16 ? launch_token_verify<SDV_BF16>(A, B, dtype, s)

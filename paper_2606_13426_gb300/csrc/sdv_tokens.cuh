@@ -174,6 +174,13 @@ __device__ __forceinline__ f32x2 far2(f32x2 d) {             // max(d, kFar)
   return pair(fmaxf(x.x, kFar), fmaxf(x.y, kFar));
 }
 
+// A vector of masked logits.
+template <int kDtype>
+__device__ __forceinline__ uint4 vec_masked() {
+  const uint32_t w = kDtype == SDV_F32 ? 0xff800000u : kDtype == SDV_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+  return make_uint4(w, w, w, w);
+}
+
 // The largest value of a 16-byte vector (a NaN stays).
 template <int kDtype>
 __device__ __forceinline__ float vec_max(const uint4& v) {
@@ -212,7 +219,7 @@ __device__ __forceinline__ void run_see(Run& r, float top, float c) {
   }
 }
 // Adds n (even) logits that it has made room for.
-template <int n>
+template <int n, bool kEntropy = true>
 __device__ __forceinline__ void run_add(Run& r, const float* x, float c) {
   const f32x2 m = pair(-r.ref, -r.ref), c2 = pair(c, c);
 #pragma unroll
@@ -221,7 +228,7 @@ __device__ __forceinline__ void run_add(Run& r, const float* x, float c) {
     const float2 t = unpair(mul2(d, c2));
     const f32x2 e = pair(ex2(t.x), ex2(t.y));
     r.s = add2(r.s, e);
-    r.w = fma2(e, d, r.w);
+    if (kEntropy) r.w = fma2(e, d, r.w);
   }
 }
 // A warp's statistics, against its largest logit.
@@ -268,22 +275,98 @@ __device__ __forceinline__ Stat stat_gather(const Stat* part, int n, int lane, f
 // The order of the alternatives: the larger logit first, of equal ones the lower index.
 __device__ __forceinline__ bool before(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 
-// A launch in clusters of `cluster` CTAs along x.
+constexpr int kScoreThreads = 256;
+constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread under way at once
+constexpr int kScoreMaxCluster = 8;
+
+// A thread's part of a row: vectors v0 + tid + u kThreads < v1 (kept as read, where kKeep), and one
+// of the row's single elements.
+template <int kDtype, int kThreads, bool kEntropy = true>
+struct Part {
+  using E = Num<kDtype>;
+  const uint4* vec;
+  int v0, v1, single;
+  float x;
+  uint4 raw[kScoreVecs];
+  __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int C) {
+    vec = R.vec();
+    v0 = (int)((int64_t)R.nvec * rank / C) + (int)threadIdx.x;
+    v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
+    single = rank == 0 && (int)threadIdx.x < R.singles() ? R.single(threadIdx.x) : -1;
+    x = single >= 0 ? E::to(R.p[single]) : 0.f;
+  }
+  __device__ __forceinline__ bool has(int u) const { return v0 + u * kThreads < v1; }
+  // Statistics; the vectors are (the last kScoreVecs of them stay) in raw.  kKeep: the whole part is
+  // one batch that its caller goes on to use; otherwise what is past the part counts as masked.
+  template <bool kKeep>
+  __device__ __forceinline__ Run read(float c) {
+    Run r = run_empty();
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int u = 0; u < kScoreVecs; ++u)
+        if (has(u)) raw[u] = vec[v0 + u * kThreads];
+#pragma unroll
+      for (int u = 0; u < kScoreVecs; ++u)
+        if (has(u)) {
+          float f[E::kPer16];
+          run_see(r, vec_max<kDtype>(raw[u]), c);
+          E::unpack(raw[u], f);
+          run_add<E::kPer16, kEntropy>(r, f, c);
+        }
+    } else {
+#pragma unroll 1
+      for (; v0 - (int)threadIdx.x < v1; v0 += kScoreVecs * kThreads) {
+#pragma unroll
+        for (int u = 0; u < kScoreVecs; ++u) {
+          raw[u] = vec_masked<kDtype>();
+          if (has(u)) raw[u] = vec[v0 + u * kThreads];
+        }
+#pragma unroll
+        for (int u = 0; u < kScoreVecs; ++u) {
+          float f[E::kPer16];
+          if (u % 4 == 0) {
+            float top = vec_max<kDtype>(raw[u]);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) top = max_nan(top, vec_max<kDtype>(raw[u + k]));
+            run_see(r, top, c);
+          }
+          E::unpack(raw[u], f);
+          run_add<E::kPer16, kEntropy>(r, f, c);
+        }
+      }
+    }
+    if (single >= 0) run_one(r, x, c);
+    return r;
+  }
+};
+
+// CTAs per row: while there are fewer than four an SM, as many as leave every thread four vectors.
+inline int score_cluster(int64_t N, int V, int dtype) {
+  const int64_t nvec = (int64_t)V * (dtype == SDV_F32 ? 4 : 2) / 16;
+  int c = 1;
+  while (c < kScoreMaxCluster && N * 2 * c <= 4 * sm_count() && nvec >= 4 * c * kScoreThreads) c *= 2;
+  return c;
+}
+
+// A launch in clusters of `cluster` CTAs along x; early: it may start before the kernel before it
+// ends (and waits for it itself).
 template <typename Kern, typename... Args>
-inline cudaError_t launch_cluster(Kern kern, dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t s,
-                                  Args... args) {
+inline cudaError_t launch_cluster(Kern kern, dim3 grid, unsigned threads, size_t smem, unsigned cluster, bool early,
+                                  cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = cluster;
   at[0].val.clusterDim.y = 1;
   at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
