@@ -371,7 +371,8 @@ def _out(out, name, shape, dtype, dev):
 
 
 def _outs(out, names, n, dtype, dev):
-    """Outputs [n] of one type by name: the caller's, or new ones."""
+    """Outputs [n] of one type by name: the caller's, or new ones (an allocation takes 1.5 us here, a
+    view of one more)."""
     if not out:
         return {k: torch.empty(n, dtype=dtype, device=dev) for k in names}
     return {k: _out(out, k, (n,), dtype, dev) for k in names}
@@ -394,23 +395,24 @@ def _row_stride(t):
     return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
 
 
-def token_scores(logits, tokens=None, *, top_k=0, temperature=1.0, entropy=True, out=None):
+def token_scores(logits, tokens=None, *, top_k=0, temperature=1.0, entropy=True, with_status=False, out=None):
     """Log probabilities of given tokens, entropy and top alternatives of logits [N, V]
     (sdv_token_scores); returns a dict: logprob [N] (with tokens [N] int32, -1 for none), entropy
-    [N], row_max, log_sum [N], status [N], and top_ids, top_logprob [N, top_k]."""
+    [N], row_max, log_sum [N], status [N] if wanted, and top_ids, top_logprob [N, top_k]."""
     dt = _rows("logits", logits, 2)
     N, V = logits.shape
     dev, f32 = logits.device, torch.float32
     _dense("tokens", tokens, torch.int32, (N,))
     names = ("row_max", "log_sum") + (("logprob",) if tokens is not None else ()) + (("entropy",) if entropy else ())
     r = _outs(out, names, N, f32, dev)
-    r["status"] = _out(out, "status", (N,), torch.int32, dev)
+    if with_status:
+        r["status"] = _out(out, "status", (N,), torch.int32, dev)
     if top_k:
         r["top_ids"] = _out(out, "top_ids", (N, top_k), torch.int32, dev)
         r["top_logprob"] = _out(out, "top_logprob", (N, top_k), f32, dev)
     B._call("sdv_token_scores", logits.data_ptr(), _row_stride(logits), N, V, dt, _ptr(tokens), float(temperature), int(top_k),
             _ptr(r.get("logprob")), _ptr(r.get("entropy")), r["row_max"].data_ptr(), r["log_sum"].data_ptr(),
-            _ptr(r.get("top_ids")), _ptr(r.get("top_logprob")), r["status"].data_ptr(), _stream())
+            _ptr(r.get("top_ids")), _ptr(r.get("top_logprob")), _ptr(r.get("status")), _stream())
     return r
 
 
@@ -445,7 +447,8 @@ def token_scores_grad(logits, tokens, scores, g_logprob=None, g_entropy=None, *,
     return dx
 
 
-def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temperature=1.0, d_logits=None, out=None):
+def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temperature=1.0, d_logits=None,
+                       with_status=False, out=None):
     """Scores and gradient in one call that reads the logits once (sdv_token_scores_train);
     returns the dict of token_scores with d_logits."""
     dt = _rows("logits", logits, 2)
@@ -455,11 +458,12 @@ def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temper
     _dense("g_logprob", g_logprob, f32, (N,))
     _dense("g_entropy", g_entropy, f32, (N,))
     r = _outs(out, ("entropy", "row_max", "log_sum") + (("logprob",) if tokens is not None else ()), N, f32, dev)
-    r["status"] = _out(out, "status", (N,), torch.int32, dev)
+    if with_status:
+        r["status"] = _out(out, "status", (N,), torch.int32, dev)
     r["d_logits"] = dx = _grad_like(logits, d_logits)
     B._call("sdv_token_scores_train", logits.data_ptr(), _row_stride(logits), N, V, dt, _ptr(tokens), float(temperature),
             _ptr(g_logprob), _ptr(g_entropy), _ptr(r.get("logprob")), r["entropy"].data_ptr(), r["row_max"].data_ptr(),
-            r["log_sum"].data_ptr(), r["status"].data_ptr(), dx.data_ptr(), _row_stride(dx), _stream())
+            r["log_sum"].data_ptr(), _ptr(r.get("status")), dx.data_ptr(), _row_stride(dx), _stream())
     return r
 
 

@@ -200,6 +200,25 @@ __device__ __forceinline__ float vec_max(const uint4& v) {
   }
 }
 
+// The same without regard to NaN.
+template <int kDtype>
+__device__ __forceinline__ float vec_max_num(const uint4& v) {
+  if constexpr (kDtype == SDV_F32) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (kDtype == SDV_BF16) {
+      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(w);
+      const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    } else {
+      const __half2* p = reinterpret_cast<const __half2*>(w);
+      const __half2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    }
+  }
+}
+
 // A thread's running statistics: sums against a reference that moves only when a logit passes it by
 // 2^8 (in e^{d/T}), and the largest logit.
 struct Run {

@@ -109,7 +109,7 @@ def test_scores(api, N, V, pad, off, dtype):
     x = make_logits(g, N, V, dtype, pad, off)
     tok = make_tokens(g, N, V)
     for k, T in ((0, 1.0), (min(V, 5), 0.7), (min(V, 32), 1.0)):
-        r = api.token_scores(x, tok, top_k=k, temperature=T)
+        r = api.token_scores(x, tok, top_k=k, temperature=T, with_status=True)
         o = plain_scores(x, tok, T, k)
         assert near(r["logprob"], o["logprob"], 1e-5)
         assert near(r["entropy"], o["entropy"], 2e-5)
@@ -131,7 +131,7 @@ def test_scores_of_rows_with_nan_or_inf(api):
     x[2, 5] = INF
     x[3, 0] = NAN
     tok = torch.tensor([0, 7, 5, 9, -1, 0], device="cuda", dtype=torch.int32)
-    r = api.token_scores(x, tok, top_k=4)
+    r = api.token_scores(x, tok, top_k=4, with_status=True)
     bad = torch.tensor([0, 1, 1, 1, 0, 0], device="cuda").bool()
     for k in ("logprob", "entropy", "row_max", "log_sum"):
         assert torch.equal(r[k].isnan(), bad)
@@ -184,12 +184,12 @@ def test_gradient_matches_the_formula(api, N, V, pad, off, dtype):
     zero = torch.zeros(N, device="cuda")
     T = 0.8
     o = plain_scores(x, tok, T, 0)
-    r = api.token_scores(x, tok, temperature=T)
+    r = api.token_scores(x, tok, temperature=T, with_status=True)
     assert grad_ok(api.token_scores_grad(x, tok, r, gl, gh, temperature=T), x, tok, o, gl, gh, T)
     assert grad_ok(api.token_scores_grad(x, tok, r, gl, temperature=T), x, tok, o, gl, zero, T)
     assert grad_ok(api.token_scores_grad(x, tok, r, None, gh, temperature=T), x, tok, o, zero, gh, T)
     wide = torch.full((N, V + 3), 7.0, dtype=dtype, device="cuda")      # another layout of the rows
-    t = api.token_scores_train(x, tok, gl, gh, temperature=T, d_logits=wide[:, :V])
+    t = api.token_scores_train(x, tok, gl, gh, temperature=T, d_logits=wide[:, :V], with_status=True)
     assert grad_ok(wide[:, :V], x, tok, o, gl, gh, T) and (wide[:, V:] == 7).all()
     for k in ("logprob", "entropy", "log_sum"):
         assert near(t[k], o[k], 2e-5)
