@@ -450,7 +450,7 @@ int sdv_token_scores_grad(const void *logits, int64_t row_stride, int N, int V, 
 
 /*
  * sdv_token_scores_train - both: the scores and, from given upstream gradients, the gradient, with
- * the logits read once (rows of up to 512 KB; longer ones are read twice).  entropy, row_max
+ * the logits read once (rows of up to 768 KB; longer ones are read twice).  entropy, row_max
  * and log_sum are required; the rest as above.
  */
 int sdv_token_scores_train(const void *logits, int64_t row_stride, int N, int V, int dtype,

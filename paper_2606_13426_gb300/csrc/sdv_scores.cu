@@ -7,6 +7,8 @@
 //   dx_v = (1/T) [g_lp (1[v = t] - p_v) - g_H p_v (log p_v + H)].
 // A row is split over the CTAs of a cluster, which join their statistics through distributed
 // shared memory.
+#include <cstdint>
+
 #include "sdv_tokens.cuh"
 
 namespace sdv {
@@ -98,8 +100,8 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   constexpr int kPer = E::kPer16;
   constexpr int kWarps = kScoreThreads / 32;
   cg::cluster_group cl = cg::this_cluster();
-  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int64_t n = blockIdx.x / C;
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
+  const int64_t n = blockIdx.x >> log_c;
   const int tid = threadIdx.x;
   __shared__ Stat stats[kScoreMaxCluster * kWarps];           // the leader's: every warp's
   __shared__ int listed[kScoreMaxCluster];
@@ -111,9 +113,9 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   if (C > 1) cl.barrier_arrive();
   const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
   const Row<kDtype> R(row, A.V);
-  Part<kDtype, kScoreThreads> P(R, rank, C);
+  const Part<kDtype, true> P(R, rank, log_c);
   const int first = P.v0;
-  const Run run = P.template read<false>(A.c);
+  const Run run = P.read(A.c);
   const float tm = run.top;                   // the largest of this thread's logits
   Stat a = run_warp(run, A.c);
   if constexpr (kTop) {
@@ -318,19 +320,19 @@ __device__ __forceinline__ bool same_phase(const void* a, const void* b) {
 
 // grid (parts of a row, rows)
 template <int kDtype>
-__global__ void __launch_bounds__(kScoreThreads) k_scores_grad(const GradArgs A, int parts) {
+__global__ void __launch_bounds__(kScoreThreads) k_scores_grad(const GradArgs A, int log_parts) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
-  const int64_t n = blockIdx.x / parts;
-  const int part = blockIdx.x % parts;
+  const int64_t n = blockIdx.x >> log_parts;
+  const int part = blockIdx.x & ((1 << log_parts) - 1);
   const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
   T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
   const Row<kDtype> R(row, A.V);
   const bool vec_out = same_phase<kDtype>(row, out);
   const RowGrad g = row_grad(A.row_max[n], A.log_sum[n], A.entropy ? A.entropy[n] : 0.f, A.tokens ? A.tokens[n] : -1, A.V,
                              A.g_lp ? A.g_lp[n] : 0.f, A.g_h ? A.g_h[n] : 0.f, A.inv_t);
-  const int v0 = (int)((int64_t)R.nvec * part / parts), v1 = (int)((int64_t)R.nvec * (part + 1) / parts);
+  const int v0 = share(R.nvec, part, log_parts), v1 = share(R.nvec, part + 1, log_parts);
   const uint4* vec = R.vec();
   for (int v = v0 + threadIdx.x; v < v1; v += kScoreThreads) {
     float f[kPer], o[kPer];
@@ -357,50 +359,113 @@ struct TrainArgs {
   int64_t dstride;
 };
 
-// Statistics and gradient with the row read once: each thread of the cluster keeps its part of
-// it, as read, in registers while the statistics are joined.
-template <int kDtype, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_scores_train(const TrainArgs A) {
+constexpr int kTrainThreads = 256;
+constexpr int kTrainMaxVecs = 24;      // vectors of a thread: 96 KB of shared memory a CTA, two an SM
+
+// Statistics and gradient with the row read once: a cluster takes row after row, each thread's vectors
+// of a row in shared memory that it alone reads and writes.  A vector's place is filled with the
+// next row's (asynchronously) as soon as its gradient is out, so that the reads never stop.  The
+// statistics of all warps are exchanged in one cluster barrier a row, their places taken in turn.
+template <int kDtype>
+__global__ void __launch_bounds__(kTrainThreads, 4) k_scores_train(const TrainArgs A, int N) {
   using E = Num<kDtype>;
   using T = typename E::T;
-  constexpr int kPer = E::kPer16;
-  constexpr int kWarps = kThreads / 32;
+  constexpr int kPer = E::kPer16, kThreads = kTrainThreads, kWarps = kThreads / 32;
+  extern __shared__ __align__(16) uint4 buffer[];               // [vecs][kThreads]
+  __shared__ Stat stats[2][kScoreMaxCluster * kWarps];
   cg::cluster_group cl = cg::this_cluster();
-  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int64_t n = blockIdx.x / C;
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
   const int tid = threadIdx.x;
-  __shared__ Stat stats[kScoreMaxCluster * kWarps];           // every warp's of the cluster
+  const int step = gridDim.x >> log_c;
+  struct Mine {                                                  // this thread's part of a row
+    const T* row;
+    const uint4* vec;                                            // its first vector
+    int first, have, single, t;                                  // the vector's first element, vectors
+    float x, g_lp, g_h;
+  };
+  auto locate = [&](int64_t n) {
+    Mine p;
+    p.row = reinterpret_cast<const T*>(A.S.x) + n * A.S.stride;
+    const Row<kDtype> R(p.row, A.S.V);
+    const int v0 = share(R.nvec, rank, log_c) + tid, v1 = share(R.nvec, rank + 1, log_c);
+    p.vec = R.vec() + v0;
+    p.first = R.head + v0 * kPer;
+    p.have = v0 < v1 ? (v1 - v0 - 1) / kThreads + 1 : 0;
+    p.single = rank == 0 && tid < R.singles() ? R.single(tid) : -1;
+    p.x = p.single >= 0 ? E::to(p.row[p.single]) : 0.f;
+    p.t = A.S.tokens ? A.S.tokens[n] : -1;
+    p.g_lp = A.g_lp ? A.g_lp[n] : 0.f;
+    p.g_h = A.g_h ? A.g_h[n] : 0.f;
+    return p;
+  };
+  uint4* mine = buffer + tid;
+  const uint32_t place = smem_addr(mine);
   if (C > 1) cl.barrier_arrive();
-  const T* row = reinterpret_cast<const T*>(A.S.x) + n * A.S.stride;
-  T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
-  const Row<kDtype> R(row, A.S.V);
-  Part<kDtype, kThreads> P(R, rank, C);
-  const Stat mine = run_warp(P.template read<true>(A.S.c), A.S.c);
-  // the token, and whether one of this thread's vectors holds it
-  const Token tok = row_token<kDtype>(A.S, row, n);
-  const float g_lp = A.g_lp ? A.g_lp[n] : 0.f, g_h = A.g_h ? A.g_h[n] : 0.f;
-  const int at = tok.t >= R.head && tok.t < A.S.V - R.tail ? (tok.t - R.head) / kPer : -1;
-  const bool own = at >= P.v0 && at < P.v1 && (at - P.v0) % kThreads == 0;
+  int64_t n = blockIdx.x >> log_c;
+  Mine p = locate(n);
+  for (int u = 0; u < p.have; ++u) copy16(place + u * kThreads * 16, p.vec + u * kThreads, true);
+  asm volatile("cp.async.commit_group;");
+  Token tok{p.t, p.t >= 0 && p.t < A.S.V ? E::to(p.row[p.t]) : 0.f};
   if (C > 1) cl.barrier_wait();
-  if ((tid & 31) < C) (C > 1 ? cl.map_shared_rank(stats, tid & 31) : stats)[rank * kWarps + tid / 32] = mine;
-  if (C > 1) cl.sync();
-  else __syncthreads();
-  const Stat a = stat_gather(stats, C * kWarps, tid & 31, A.S.c);
-  if (rank == 0 && tid == 0) write_row(A.S, n, a, tok);
-  const float log_s = logf(a.s);
-  const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, tok.t, A.S.V, g_lp, g_h, A.S.inv_t);
-  T* to = out + R.head + P.v0 * kPer;
-  const bool vec = same_phase<kDtype>(row, out);
+#pragma unroll 1
+  for (int turn = 0;; turn ^= 1) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    Run run = run_empty();
+#pragma unroll 1
+    for (int u = 0; u < p.have; u += 4) {
+      uint4 raw[4];
 #pragma unroll
-  for (int u = 0; u < kScoreVecs; ++u)
-    if (P.has(u)) {
-      float f[kPer], o[kPer];
-      E::unpack(P.raw[u], f);
-      grad_vec<kPer>(g, f, o, A.S.c);
-      put_vec<kDtype>(to + u * kThreads * kPer, o, vec);
+      for (int k = 0; k < 4; ++k) {
+        raw[k] = vec_masked<kDtype>();
+        if (u + k < p.have) raw[k] = mine[(u + k) * kThreads];
+      }
+      run_see(run, max_nan(max_nan(vec_max<kDtype>(raw[0]), vec_max<kDtype>(raw[1])),
+                           max_nan(vec_max<kDtype>(raw[2]), vec_max<kDtype>(raw[3]))), A.S.c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float f[kPer];
+        E::unpack(raw[k], f);
+        run_add<kPer>(run, f, A.S.c);
+      }
     }
-  if (own) out[tok.t] = E::from(grad_one(g, tok.x, tok.t, A.S.c));
-  if (P.single >= 0) out[P.single] = E::from(grad_one(g, P.x, P.single, A.S.c));
+    if (p.single >= 0) run_one(run, p.x, A.S.c);
+    Stat a = run_warp(run, A.S.c);
+    if ((tid & 31) < C) (C > 1 ? cl.map_shared_rank(stats[turn], tid & 31) : stats[turn])[rank * kWarps + tid / 32] = a;
+    const int64_t next = n + step;
+    Mine q = p;
+    q.have = 0;
+    if (next < N) q = locate(next);
+    if (C > 1) cl.sync();
+    else __syncthreads();
+    a = stat_gather(stats[turn], C * kWarps, tid & 31, A.S.c);
+    if (rank == 0 && tid == 0) write_row(A.S, n, a, tok);
+    const float log_s = logf(a.s);
+    const RowGrad g = row_grad(a.m, log_s, log_s - a.w / a.s * A.S.inv_t, tok.t, A.S.V, p.g_lp, p.g_h, A.S.inv_t);
+    // the next row's token, before that row's gradient can be written
+    tok = Token{q.t, q.t >= 0 && q.t < A.S.V ? E::to(q.row[q.t]) : 0.f};
+    T* out = reinterpret_cast<T*>(A.dx) + n * A.dstride;
+    const bool vec = same_phase<kDtype>(p.row, out);
+    T* to = out + p.first;
+#pragma unroll 2
+    for (int u = 0; u < p.have; ++u) {
+      float f[kPer], o[kPer];
+      E::unpack(mine[u * kThreads], f);
+      grad_vec<kPer>(g, f, o, A.S.c);
+      if ((unsigned)(g.t - p.first - u * kThreads * kPer) < (unsigned)kPer) {     // the token's vector
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          if (g.t - p.first - u * kThreads * kPer == e) o[e] = grad_one(g, f[e], g.t, A.S.c);
+      }
+      put_vec<kDtype>(to + u * kThreads * kPer, o, vec);
+      if (u < q.have) copy16(place + u * kThreads * 16, q.vec + u * kThreads, true);
+    }
+    for (int u = p.have; u < q.have; ++u) copy16(place + u * kThreads * 16, q.vec + u * kThreads, true);
+    asm volatile("cp.async.commit_group;");
+    if (p.single >= 0) out[p.single] = E::from(grad_one(g, p.x, p.single, A.S.c));
+    if (next >= N) break;
+    n = next;
+    p = q;
+  }
 }
 
 static int check_rows(const void* x, int64_t stride, int N, int V, int dtype, float temperature) {
@@ -419,33 +484,49 @@ static cudaError_t launch_scores(const ScoreArgs& A, int N, int dtype, cudaStrea
   return launch_cluster(k_scores<kDtype, false>, grid, kScoreThreads, 0, (unsigned)C, false, s, A);
 }
 
-// CTAs per row of k_scores_train and their threads: as few as hold the row; c = 0 if the largest
-// cluster does not.
+// How k_scores_train runs: CTAs per row, vectors per thread, clusters.  As many clusters as are resident
+// together (a few SMs' worth less: clusters do not fill every part of the chip) take the rows in
+// rounds; a CTA's row costs its vectors and about five more for what is done once a row (of
+// 4096 rows of 65536 bf16, two CTAs a row: 500 of 1450 instructions a warp).  c = 0 if no cluster
+// holds a row.
 struct TrainShape {
-  int c, threads;
+  int c, vecs, clusters;
 };
-static TrainShape train_shape(int V, int dtype) {
+static TrainShape train_shape(int N, int V, int dtype) {
   const int64_t nvec = ((int64_t)V * (int64_t)elem_bytes(dtype) + 15) / 16;
-  for (int threads = 256; threads <= 512; threads *= 2)
-    for (int c = 1; c <= kScoreMaxCluster; c *= 2)
-      if (nvec <= (int64_t)c * threads * kScoreVecs) return TrainShape{c, threads};
-  return TrainShape{0, 0};
+  TrainShape best{0, 0, 0};
+  int64_t least = INT64_MAX;
+  for (int c = 1; c <= kScoreMaxCluster; c *= 2) {
+    const int64_t vecs = ((nvec + c - 1) / c + kTrainThreads - 1) / kTrainThreads;
+    if (vecs > kTrainMaxVecs) continue;
+    const int per_sm = min_int(4, (int)(225 * 1024 / (vecs * kTrainThreads * 16 + 3 * 1024)));
+    const int most = (sm_count() - 6) * per_sm / c;
+    const int rounds = (N + most - 1) / most;
+    const int64_t cost = (int64_t)rounds * per_sm * (vecs + 5);
+    if (cost < least) {
+      least = cost;
+      best = TrainShape{c, (int)vecs, (N + rounds - 1) / rounds};
+    }
+  }
+  return best;
 }
 
 template <int kDtype>
 static cudaError_t launch_grad(const GradArgs& G, int N, int dtype, cudaStream_t s) {
   const int64_t nvec = (int64_t)G.V * (int64_t)elem_bytes(dtype) / 16;
-  int parts = 1;
-  while (parts < 64 && (int64_t)N * parts < 8 * sm_count() && nvec / (2 * parts) >= kScoreThreads) parts *= 2;
-  k_scores_grad<kDtype><<<(unsigned)(N * (int64_t)parts), kScoreThreads, 0, s>>>(G, parts);
+  int parts = 0;                                                  // (a logarithm)
+  while (parts < 6 && ((int64_t)N << parts) < 8 * sm_count() && nvec >> (parts + 1) >= kScoreThreads) ++parts;
+  k_scores_grad<kDtype><<<(unsigned)((int64_t)N << parts), kScoreThreads, 0, s>>>(G, parts);
   return cudaGetLastError();
 }
 
 template <int kDtype>
 static cudaError_t launch_train(const TrainArgs& A, int N, TrainShape t, cudaStream_t s) {
-  const dim3 grid((unsigned)(N * (int64_t)t.c));
-  if (t.threads == 256) return launch_cluster(k_scores_train<kDtype, 256>, grid, 256, 0, (unsigned)t.c, false, s, A);
-  return launch_cluster(k_scores_train<kDtype, 512>, grid, 512, 0, (unsigned)t.c, false, s, A);
+  const cudaError_t e = cudaFuncSetAttribute(k_scores_train<kDtype>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             kTrainMaxVecs * kTrainThreads * 16);
+  if (e != cudaSuccess) return e;
+  return launch_cluster(k_scores_train<kDtype>, dim3((unsigned)(t.clusters * t.c)), kTrainThreads,
+                        (size_t)t.vecs * kTrainThreads * 16, (unsigned)t.c, false, s, A, N);
 }
 
 }  // namespace sdv
@@ -509,7 +590,7 @@ int sdv_token_scores_train(const void* logits, int64_t row_stride, int N, int V,
   const void* four[] = {tokens, g_logprob, g_entropy, logprob, entropy, row_max, log_sum, status};
   for (const void* p : four)
     if (!aligned_to(p, 4)) return SDV_EALIGN;
-  const TrainShape t = train_shape(V, dtype);
+  const TrainShape t = train_shape(N, V, dtype);
   if (!t.c) {                                   // rows that no cluster holds: read twice
     rc = sdv_token_scores(logits, row_stride, N, V, dtype, tokens, temperature, 0, logprob, entropy, row_max, log_sum,
                           nullptr, nullptr, status, stream);

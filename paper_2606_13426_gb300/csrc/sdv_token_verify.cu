@@ -21,9 +21,12 @@ namespace sdv {
 constexpr int kVerThreads = 256;
 constexpr int kVerWarps = kVerThreads / 32;
 constexpr int kVerMaxCluster = 16;
+constexpr int kLogVerSegs = 3;
 constexpr int kVerSegs = kVerWarps;    // segments of a CTA's part of a row, a warp each
 constexpr int kVerRows = 2 * SDV_MAX_L + 1;
 constexpr uint32_t kStreamRace = 7;
+
+static_assert(kVerSegs == 1 << kLogVerSegs, "");
 
 struct TokenVerifyArgs {
   const void* q;
@@ -69,18 +72,18 @@ static __device__ __noinline__ float4 race4(uint64_t seed, uint32_t b, uint32_t 
 }
 
 // Calls f(first index, n, q, p) with n <= 8 (kPer) consecutive elements of two rows at a time: this
-// thread's share (of `step` threads) of part `part` of `parts`.  Rows in the same phase of 16 bytes
+// thread's share (of `step` threads) of part `part` of 2^log_parts.  Rows in the same phase of 16 bytes
 // are read as vectors, others element by element, a warp's next to each other (n = 1).  The body of
 // f is there once: the passes over the rows run from a cold instruction cache.
 template <int kDtype, typename F>
 __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, int V, int part,
-                                          int parts, int lane, int step, F f) {
+                                          int log_parts, int lane, int step, F f) {
   using E = Num<kDtype>;
   constexpr int kPer = E::kPer16, kUn = 2;
   const bool vec = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0;
   const Row<kDtype> R(q, V);
   const int total = vec ? R.nvec : V / kPer * kPer / kPer;          // groups of kPer
-  const int g0 = (int)((int64_t)total * part / parts), g1 = (int)((int64_t)total * (part + 1) / parts);
+  const int g0 = share(total, part, log_parts), g1 = share(total, part + 1, log_parts);
   const uint4* vq = R.vec();
   const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
   const int done = vec ? R.head + R.nvec * kPer : total * kPer, head = vec ? R.head : 0;
@@ -138,8 +141,8 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   using T = typename Num<kDtype>::T;
   constexpr int kWarps = kScoreThreads / 32;
   cg::cluster_group cl = cg::this_cluster();
-  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int n = blockIdx.x / C, per = 2 * A.L + 1, b = n / per, r = n % per;
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
+  const int n = blockIdx.x >> log_c, per = 2 * A.L + 1, b = n / per, r = n % per;
   const int window = A.L_eff ? min(A.L_eff[b], A.L) : A.L;
   if (r <= A.L ? r > window : r - A.L - 1 >= window) return;
   __shared__ Stat stats[kScoreMaxCluster * kWarps];
@@ -147,8 +150,8 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   const T* row = r <= A.L ? reinterpret_cast<const T*>(A.q) + b * A.q_sb + r * A.q_sr
                           : reinterpret_cast<const T*>(A.p) + b * A.p_sb + (r - A.L - 1) * A.p_sr;
   const float c = r <= A.L ? A.cq : A.cp;
-  Part<kDtype, kScoreThreads, false> P(Row<kDtype>(row, A.V), rank, C);
-  const Stat a = run_warp(P.template read<false>(c), c);
+  const Part<kDtype, false> P(Row<kDtype>(row, A.V), rank, log_c);
+  const Stat a = run_warp(P.read(c), c);
   if (C > 1) cl.barrier_wait();
   if ((threadIdx.x & 31) == 0) (C > 1 ? cl.map_shared_rank(stats, 0) : stats)[rank * kWarps + threadIdx.x / 32] = Stat{a.m, a.s, 0.f};
   if (C > 1) cl.sync();
@@ -164,8 +167,8 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
   cg::cluster_group cl = cg::this_cluster();
-  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
+  const int b = blockIdx.x >> log_c, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int L = A.L, V = A.V;
   const int n_in = A.L_eff ? A.L_eff[b] : L;
   if (n_in < 0) {                                  // an inactive chain
@@ -208,10 +211,9 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
   }
   if (A.race) {
     const float* race = A.race + (int64_t)b * V;
-    for (int i = (int)((int64_t)V * rank / C) + tid * 32; i < (int)((int64_t)V * (rank + 1) / C); i += kVerThreads * 32)
+    for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
       asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
   }
-  const int parts = C * kVerSegs;
   asm volatile("griddepcontrol.wait;" ::: "memory");         // the rows' statistics are there
   for (int r = tid; r < rows; r += kVerThreads) {
     const RowStat a = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
@@ -279,7 +281,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
       const float sh = la[j] * kLog2E;
       float sum = 0.f;
       const bool has_p = row_ok(rp);
-      each_pair<kDtype>(q0 + j * A.q_sr, has_p ? p0 + j * A.p_sr : q0 + j * A.q_sr, V, rank * kVerSegs + u % kVerSegs, parts, lane, 32,
+      each_pair<kDtype>(q0 + j * A.q_sr, has_p ? p0 + j * A.p_sr : q0 + j * A.q_sr, V, rank * kVerSegs + u % kVerSegs, log_c + kLogVerSegs, lane, 32,
                         [&](int, int, const float* x, const float* y) {
 #pragma unroll
                           for (int e = 0; e < kPer; ++e)
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
     Racer top{0.f, 1.f, 0x7fffffff};
     const float* race = A.race ? A.race + (int64_t)b * V : nullptr;
     if (row_ok(rq))
-      each_pair<kDtype>(q, p, V, rank, C, tid, kVerThreads, [&](int i, int count, const float* x, const float* y) {
+      each_pair<kDtype>(q, p, V, rank, log_c, tid, kVerThreads, [&](int i, int count, const float* x, const float* y) {
         float r[kPer], e[kPer];
         bool any = false;
 #pragma unroll

@@ -109,6 +109,12 @@ struct Row {
   __device__ __forceinline__ int singles() const { return head + tail; }
 };
 
+// The first of part `part`'s share of n (below 2^28) things in 2^log_parts parts, part at most 2^log_parts.
+// (A shift: 64-bit divisions took a third of the instructions of the kernels with one row a CTA.)
+__device__ __forceinline__ int share(int n, int part, int log_parts) {
+  return (int)((uint64_t)(uint32_t)n * (uint32_t)part >> log_parts);
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -298,60 +304,44 @@ constexpr int kScoreThreads = 256;
 constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread under way at once
 constexpr int kScoreMaxCluster = 8;
 
-// A thread's part of a row: vectors v0 + tid + u kThreads < v1 (kept as read, where kKeep), and one
-// of the row's single elements.
-template <int kDtype, int kThreads, bool kEntropy = true>
+// A thread's part of a row: vectors v0 + tid + u kScoreThreads < v1, and one of the row's single
+// elements.
+template <int kDtype, bool kEntropy>
 struct Part {
   using E = Num<kDtype>;
   const uint4* vec;
   int v0, v1, single;
   float x;
-  uint4 raw[kScoreVecs];
-  __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int C) {
+  __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int log_c) {
     vec = R.vec();
-    v0 = (int)((int64_t)R.nvec * rank / C) + (int)threadIdx.x;
-    v1 = (int)((int64_t)R.nvec * (rank + 1) / C);
+    v0 = share(R.nvec, rank, log_c) + (int)threadIdx.x;
+    v1 = share(R.nvec, rank + 1, log_c);
     single = rank == 0 && (int)threadIdx.x < R.singles() ? R.single(threadIdx.x) : -1;
     x = single >= 0 ? E::to(R.p[single]) : 0.f;
   }
-  __device__ __forceinline__ bool has(int u) const { return v0 + u * kThreads < v1; }
-  // Statistics; the vectors are (the last kScoreVecs of them stay) in raw.  kKeep: the whole part is
-  // one batch that its caller goes on to use; otherwise what is past the part counts as masked.
-  template <bool kKeep>
-  __device__ __forceinline__ Run read(float c) {
+  // Its statistics; what is past the part counts as masked: one copy of the code for whole and partial
+  // batches, which are run once and so from a cold instruction cache.
+  __device__ __forceinline__ Run read(float c) const {
     Run r = run_empty();
-    if constexpr (kKeep) {
-#pragma unroll
-      for (int u = 0; u < kScoreVecs; ++u)
-        if (has(u)) raw[u] = vec[v0 + u * kThreads];
-#pragma unroll
-      for (int u = 0; u < kScoreVecs; ++u)
-        if (has(u)) {
-          float f[E::kPer16];
-          run_see(r, vec_max<kDtype>(raw[u]), c);
-          E::unpack(raw[u], f);
-          run_add<E::kPer16, kEntropy>(r, f, c);
-        }
-    } else {
 #pragma unroll 1
-      for (; v0 - (int)threadIdx.x < v1; v0 += kScoreVecs * kThreads) {
+    for (int v = v0; v - (int)threadIdx.x < v1; v += kScoreVecs * kScoreThreads) {
+      uint4 raw[kScoreVecs];
 #pragma unroll
-        for (int u = 0; u < kScoreVecs; ++u) {
-          raw[u] = vec_masked<kDtype>();
-          if (has(u)) raw[u] = vec[v0 + u * kThreads];
+      for (int u = 0; u < kScoreVecs; ++u) {
+        raw[u] = vec_masked<kDtype>();
+        if (v + u * kScoreThreads < v1) raw[u] = vec[v + u * kScoreThreads];
+      }
+#pragma unroll
+      for (int u = 0; u < kScoreVecs; ++u) {
+        float f[E::kPer16];
+        if (u % 4 == 0) {
+          float top = vec_max<kDtype>(raw[u]);
+#pragma unroll
+          for (int k = 1; k < 4; ++k) top = max_nan(top, vec_max<kDtype>(raw[u + k]));
+          run_see(r, top, c);
         }
-#pragma unroll
-        for (int u = 0; u < kScoreVecs; ++u) {
-          float f[E::kPer16];
-          if (u % 4 == 0) {
-            float top = vec_max<kDtype>(raw[u]);
-#pragma unroll
-            for (int k = 1; k < 4; ++k) top = max_nan(top, vec_max<kDtype>(raw[u + k]));
-            run_see(r, top, c);
-          }
-          E::unpack(raw[u], f);
-          run_add<E::kPer16, kEntropy>(r, f, c);
-        }
+        E::unpack(raw[u], f);
+        run_add<E::kPer16, kEntropy>(r, f, c);
       }
     }
     if (single >= 0) run_one(r, x, c);
@@ -365,6 +355,12 @@ inline int score_cluster(int64_t N, int V, int dtype) {
   int c = 1;
   while (c < kScoreMaxCluster && N * 2 * c <= 4 * sm_count() && nvec >= 4 * c * kScoreThreads) c *= 2;
   return c;
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool real) {
+  const int n = real ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n));
 }
 
 // A launch in clusters of `cluster` CTAs along x; early: it may start before the kernel before it
@@ -390,6 +386,7 @@ inline cudaError_t launch_cluster(Kern kern, dim3 grid, unsigned threads, size_t
 }
 
 __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline int min_int(int a, int b) { return a < b ? a : b; }
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t elem_bytes(int dtype) { return dtype == SDV_F32 ? 4 : 2; }
 inline bool token_dtype(int dtype) { return dtype == SDV_F32 || dtype == SDV_BF16 || dtype == SDV_F16; }

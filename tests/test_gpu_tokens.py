@@ -175,7 +175,7 @@ def grad_ok(dx, x, tok, o, gl, gh, T):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("N,V,pad,off", SIZES + [(3, 140001, 0, 0)])
+@pytest.mark.parametrize("N,V,pad,off", SIZES + [(3, 140001, 0, 0), (2, 210001, 0, 1)])
 def test_gradient_matches_the_formula(api, N, V, pad, off, dtype):
     g = gen(N + 3 * V)
     x = make_logits(g, N, V, dtype, pad, off)
