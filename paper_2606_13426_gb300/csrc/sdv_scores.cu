@@ -85,6 +85,7 @@ __device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const Cand me = c[i];
     int r = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) {
       const Cand o = c[j];
       r += before(o.x, o.i, me.x, me.i);
@@ -110,9 +111,12 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   __shared__ Cand cand[kTop ? kCandMax : 1];
   __shared__ Cand lists[kTop ? kScoreMaxCluster * SDV_MAX_TOP : 1];
   __shared__ Cand best_w[kWarps];
+  __shared__ uint8_t who[kWarps][32];
   if (C > 1) cl.barrier_arrive();
   const T* row = reinterpret_cast<const T*>(A.x) + n * A.stride;
   const Row<kDtype> R(row, A.V);
+  Token tok{-1, 0.f};
+  if (rank == 0 && tid == 0) tok = row_token<kDtype>(A, row, n);   // (under way with the row)
   const Part<kDtype, true> P(R, rank, log_c);
   const int first = P.v0;
   const Run run = P.read(A.c);
@@ -146,26 +150,28 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
         if (at < kCandMax) cand[at] = Cand{x, i};
       }
     };
-    if (tm >= thr) {
-      // a thread that has candidates (about as many as alternatives are wanted) reads its vectors again
-#pragma unroll 1
-      for (int v = first; v < P.v1; v += 4 * kScoreThreads) {
-        uint4 raw[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          raw[u] = vec_masked<kDtype>();
-          if (v + u * kScoreThreads < P.v1) raw[u] = __ldg(P.vec + v + u * kScoreThreads);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (vec_max<kDtype>(raw[u]) >= thr) {
+    // The vectors of the threads that have candidates (about as many as alternatives are wanted) are
+    // read again, a warp's threads' together.
+    const unsigned flagged = __ballot_sync(0xffffffffu, tm >= thr);
+    if (flagged) {
+      const int nf = __popc(flagged), w0 = first - (tid & 31);           // the warp's first vector
+      if (flagged >> (tid & 31) & 1) who[tid / 32][__popc(flagged & ((1u << (tid & 31)) - 1u))] = (uint8_t)(tid & 31);
+      __syncwarp();
+      const int log_v = 32 - __clz(max((P.v1 - w0 + kScoreThreads - 1) / kScoreThreads - 1, 0));   // vectors a thread, as a power of two
+#pragma unroll 2
+      for (int i = tid & 31; i < nf << log_v; i += 32) {
+        const int v = w0 + who[tid / 32][i >> log_v] + (i & ((1 << log_v) - 1)) * kScoreThreads;
+        if (v < P.v1) {
+          const uint4 raw = __ldg(P.vec + v);
+          if (vec_max<kDtype>(raw) >= thr) {
             float f[kPer];
-            E::unpack(raw[u], f);
+            E::unpack(raw, f);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) keep(f[e], R.head + (v + u * kScoreThreads) * kPer + e);
+            for (int e = 0; e < kPer; ++e) keep(f[e], R.head + v * kPer + e);
           }
+        }
       }
-      if (P.single >= 0) keep(P.x, P.single);
+      if (P.single >= 0 && tm >= thr) keep(P.x, P.single);
     }
     __syncthreads();
     Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * A.top_k;
@@ -214,7 +220,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   }
   if (!kTop && tid >= 32) return;
   a = stat_gather(stats, C * kWarps, tid & 31, A.c);
-  if (tid == 0) write_row(A, n, a, row_token<kDtype>(A, row, n));
+  if (tid == 0) write_row(A, n, a, tok);
   if constexpr (kTop) {
     const bool bad = !(a.m < INFINITY);
     const float log_s = logf(a.s);
