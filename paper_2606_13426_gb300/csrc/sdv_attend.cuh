@@ -401,12 +401,12 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       else nothing();
       look(n + S::kAhead + 1);
       const int chunk = g >> 2;
-      float f = sc[2 * chunk] * rsc;                         // what a raw score is to be multiplied by
-      float vs = sc[2 * chunk + 1];
+      const float4 s4 = *reinterpret_cast<const float4*>(sc);   // ks, vs of the first chunk, of the second
+      float f = (chunk ? s4.z : s4.x) * rsc;                 // what a raw score is to be multiplied by
+      float vs = chunk ? s4.w : s4.y;
       const int absent = __float_as_int(sc[4]);
-      const float v0 = fabsf(sc[1]), v1 = fabsf(sc[3]);
-      const bool odd_scale = !(v0 < INFINITY) || !(v1 < INFINITY);
-      const float va = fmaxf(v0 < INFINITY ? v0 : 0.f, v1 < INFINITY ? v1 : 0.f);
+      float va = max_nan(fabsf(s4.y), fabsf(s4.w));
+      const bool odd_scale = !(va < INFINITY);
       const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || odd_scale;
       if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
         const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
@@ -436,9 +436,12 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         nan_keys &= ~drop;
         drop |= nan_keys;
         nan_keys = __shfl_sync(0xffffffffu, nan_keys, g >> 1);   // of this thread's keys
-        if (!(fabsf(vs) < INFINITY)) {                     // a scale that is none: as NaN codes
-          nan_keys = 0xffu;
-          vs = 0.f;
+        if (odd_scale) {                                   // a scale that is none: as NaN codes
+          va = fmaxf(fabsf(s4.y) < INFINITY ? fabsf(s4.y) : 0.f, fabsf(s4.w) < INFINITY ? fabsf(s4.w) : 0.f);
+          if (!(fabsf(vs) < INFINITY)) {
+            nan_keys = 0xffu;
+            vs = 0.f;
+          }
         }
         const bool here = !(absent >> chunk & 1);
 #pragma unroll
@@ -486,19 +489,27 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
           }
         }
       }
-      const float pw = vs * winv;
+      // The values' scale goes into the exponent, and out of the sums: p' = p pw, sum += (sum p') / pw.  A
+      // weight below 2^-80 (a scale of 0) leaves p' = 0 in f16, and the sums right.
+      const float pw = fmaxf(fabsf(vs) * winv, 0x1p-80f), ipw = __frcp_rn(pw), lw = __log2f(pw);
+      const uint32_t sign = vs < 0.f ? 0x80008000u : 0u;
       uint32_t pb[2][kNt][2];                               // probabilities, transposed
 #pragma unroll
-      for (int k = 0; k < kNt; ++k)
+      for (int k = 0; k < kNt; ++k) {
+        const float m0 = lw - mx[2 * k], m1 = lw - mx[2 * k + 1];
+        float s0 = 0.f, s1 = 0.f;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float e0 = ex2(fmaf(sx[s][k][2 * e], f, -mx[2 * k])), e1 = ex2(fmaf(sx[s][k][2 * e + 1], f, -mx[2 * k + 1]));
-            sum[2 * k] += e0;
-            sum[2 * k + 1] += e1;
-            pb[s][k][e] = transpose8(pack_half(e0 * pw, e1 * pw));
+            const float e0 = ex2(fmaf(sx[s][k][2 * e], f, m0)), e1 = ex2(fmaf(sx[s][k][2 * e + 1], f, m1));
+            s0 += e0;
+            s1 += e1;
+            pb[s][k][e] = transpose8(pack_half(e0, e1) ^ sign);
           }
+        sum[2 * k] = fmaf(s0, ipw, sum[2 * k]);
+        sum[2 * k + 1] = fmaf(s1, ipw, sum[2 * k + 1]);
+      }
 #pragma unroll
       for (int m = 0; m < kMt; ++m) {
         uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
