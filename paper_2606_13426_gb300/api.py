@@ -468,10 +468,10 @@ def token_scores_train(logits, tokens, g_logprob=None, g_entropy=None, *, temper
 
 
 def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L_eff=None, temperature=1.0,
-                 draft_temperature=None, coins=None, race=None, workspace=None, out=None):
+                 draft_temperature=None, coins=None, race=None, with_status=False, workspace=None, out=None):
     """Verification of drafted tokens [B, L] from target logits [B, L + 1, V] and draft logits
-    [B, L, V] (sdv_token_verify); returns accepted_len, next_token, status [B] and log_ratio
-    [B, L].  draft_temperature defaults to temperature; coins [B, L] and race [B, V] (exponential
+    [B, L, V] (sdv_token_verify); returns accepted_len, next_token [B], log_ratio [B, L], and
+    status [B] if wanted.  draft_temperature defaults to temperature; coins [B, L] and race [B, V] (exponential
     variates) replace the draws from `seed`."""
     dt = _rows("target_logits", target_logits, 3)
     if _rows("draft_logits", draft_logits, 3) != dt:
@@ -484,7 +484,7 @@ def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L
     _dense("L_eff", L_eff, i32, (Bn,))
     _dense("coins", coins, f32, (Bn, L))
     _dense("race", race, f32, (Bn, V))
-    r = _outs(out, ("accepted_len", "next_token", "status"), Bn, i32, dev)
+    r = _outs(out, ("accepted_len", "next_token", "status") if with_status else ("accepted_len", "next_token"), Bn, i32, dev)
     r["log_ratio"] = _out(out, "log_ratio", (Bn, L), f32, dev)
     if workspace is None:
         workspace = torch.empty(_verify_workspace(Bn, L), dtype=torch.uint8, device=dev)
@@ -492,7 +492,7 @@ def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L
             draft_logits.data_ptr(), draft_logits.stride(0), _row_stride(draft_logits), tokens.data_ptr(), Bn, L, V, dt,
             float(temperature), float(temperature if draft_temperature is None else draft_temperature), _MODES[mode],
             _ptr(L_eff), int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(coins), _ptr(race), r["accepted_len"].data_ptr(),
-            r["next_token"].data_ptr(), r["log_ratio"].data_ptr(), r["status"].data_ptr(), workspace.data_ptr(),
+            r["next_token"].data_ptr(), r["log_ratio"].data_ptr(), _ptr(r.get("status")), workspace.data_ptr(),
             workspace.numel(), _stream())
     return r
 

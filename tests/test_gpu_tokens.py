@@ -373,7 +373,7 @@ def test_verify_masks_and_bad_rows(api):
     for mode in ("block", "sample"):
         ok = [0, 1, 8, 9, 10]
         check_verify(api, tl[ok], dl[ok], tok[ok], coins[ok], race[ok], mode)
-        r = api.token_verify(tl, dl, tok, mode=mode, coins=coins, race=race)
+        r = api.token_verify(tl, dl, tok, mode=mode, coins=coins, race=race, with_status=True)
         acc, nxt, st, lr = (r[k].tolist() for k in ("accepted_len", "next_token", "status", "log_ratio"))
         assert all(t < 300 for t in nxt[:1])
         assert lr[1] == [INF] * L
@@ -400,7 +400,7 @@ def test_verify_with_nothing_left(api):
     tl[0, 0, 7] = -INF                       # the rejected token: q = 0 there
     dl[0, 0, 7] = -INF
     tok[0, 0] = 7
-    r = api.token_verify(tl, dl, tok, mode="sample", coins=torch.zeros(1, 1, device="cuda"), race=race)
+    r = api.token_verify(tl, dl, tok, mode="sample", coins=torch.zeros(1, 1, device="cuda"), race=race, with_status=True)
     assert int(r["accepted_len"]) == 0 and int(r["status"]) & 1
     q = torch.softmax(tl[0, 0].double(), 0) / race[0].double()
     assert int(r["next_token"]) == int(q.argmax())
