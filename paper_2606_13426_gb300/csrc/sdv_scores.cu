@@ -79,21 +79,27 @@ __device__ __forceinline__ void write_row(const ScoreArgs& A, int64_t n, const S
   if (A.status) A.status[n] = st;
 }
 
-// Ranks the n candidates in `c` by counting and hands those of rank < k to put(rank, candidate).
+// Ranks the n candidates in `c` by counting, eight lanes a candidate, and hands those of rank < k to
+// put(rank, candidate).
 template <typename Put>
 __device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put put) {
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const Cand me = c[i];
+#pragma unroll 1
+  for (int i = threadIdx.x / 8; i - (int)(threadIdx.x & 31) / 8 < n; i += kScoreThreads / 8) {
+    const Cand me = i < n ? c[i] : Cand{0.f, 0};
     int r = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
+#pragma unroll 1
+    for (int j = threadIdx.x & 7; j < n; j += 8) {
       const Cand o = c[j];
       r += before(o.x, o.i, me.x, me.i);
     }
-    if (r < k) put(r, me);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+    if (i < n && r < k && (threadIdx.x & 7) == 0) put(r, me);
   }
 }
 
+// What follows the row's read runs once a CTA, mostly from a cold instruction cache (a line of eight
+// instructions took about 350 cycles where rows fill the L2): loops there are not unrolled.
 template <int kDtype, bool kTop>
 __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) {
   using E = Num<kDtype>;
@@ -107,7 +113,8 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   __shared__ Stat stats[kScoreMaxCluster * kWarps];           // the leader's: every warp's
   __shared__ int listed[kScoreMaxCluster];
   __shared__ __align__(16) float gmax[kGroups];
-  __shared__ int ncand;
+  __shared__ int ncand, nhot;
+  __shared__ int hot[kTop ? kCandMax : 1];
   __shared__ Cand cand[kTop ? kCandMax : 1];
   __shared__ Cand lists[kTop ? kScoreMaxCluster * SDV_MAX_TOP : 1];
   __shared__ Cand best_w[kWarps];
@@ -127,7 +134,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
 #pragma unroll
     for (int o = 1; o < kScoreThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
     if (tid % (kScoreThreads / kGroups) == 0) gmax[tid / (kScoreThreads / kGroups)] = g;
-    if (tid == 0) ncand = 0;
+    if (tid == 0) ncand = nhot = 0;
     __syncthreads();
   }
   if (C > 1) cl.barrier_wait();               // the leader has started: its memory can be written
@@ -151,32 +158,42 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
       }
     };
     // The vectors of the threads that have candidates (about as many as alternatives are wanted) are
-    // read again, a warp's threads' together.
-    const unsigned flagged = __ballot_sync(0xffffffffu, tm >= thr);
+    // read again, a warp's threads' together, and then those that hold some, an element a thread.
+    const unsigned flagged = __ballot_sync(0xffffffffu, tm >= thr && tm > -INFINITY);
     if (flagged) {
       const int nf = __popc(flagged), w0 = first - (tid & 31);           // the warp's first vector
       if (flagged >> (tid & 31) & 1) who[tid / 32][__popc(flagged & ((1u << (tid & 31)) - 1u))] = (uint8_t)(tid & 31);
       __syncwarp();
       const int log_v = 32 - __clz(max((P.v1 - w0 + kScoreThreads - 1) / kScoreThreads - 1, 0));   // vectors a thread, as a power of two
-#pragma unroll 2
-      for (int i = tid & 31; i < nf << log_v; i += 32) {
-        const int v = w0 + who[tid / 32][i >> log_v] + (i & ((1 << log_v) - 1)) * kScoreThreads;
-        if (v < P.v1) {
-          const uint4 raw = __ldg(P.vec + v);
-          if (vec_max<kDtype>(raw) >= thr) {
-            float f[kPer];
-            E::unpack(raw, f);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) keep(f[e], R.head + v * kPer + e);
-          }
+#pragma unroll 1
+      for (int i = tid & 31; i < nf << log_v; i += 64) {
+        const int i2 = i + 32;
+        const int va = w0 + who[tid / 32][i >> log_v] + (i & ((1 << log_v) - 1)) * kScoreThreads;
+        const int vb = i2 < nf << log_v ? w0 + who[tid / 32][i2 >> log_v] + (i2 & ((1 << log_v) - 1)) * kScoreThreads : P.v1;
+        const uint4 ra = va < P.v1 ? __ldg(P.vec + va) : vec_masked<kDtype>(), rb = vb < P.v1 ? __ldg(P.vec + vb) : vec_masked<kDtype>();
+        const float ta = vec_max<kDtype>(ra), tb = vec_max<kDtype>(rb);
+        if (ta >= thr && va < P.v1) {
+          const int at = atomicAdd(&nhot, 1);
+          if (at < kCandMax) hot[at] = va;
+        }
+        if (tb >= thr && vb < P.v1) {
+          const int at = atomicAdd(&nhot, 1);
+          if (at < kCandMax) hot[at] = vb;
         }
       }
-      if (P.single >= 0 && tm >= thr) keep(P.x, P.single);
+      if (P.single >= 0) keep(P.x, P.single);
+    }
+    __syncthreads();
+    const int hots = nhot;
+#pragma unroll 1
+    for (int i = tid; i < min(hots, kCandMax) * kPer; i += kScoreThreads) {
+      const int at = R.head + hot[i / kPer] * kPer + i % kPer;
+      keep(E::to(row[at]), at);
     }
     __syncthreads();
     Cand* mine = (C > 1 ? cl.map_shared_rank(lists, 0) : lists) + rank * A.top_k;
     int nc = ncand;
-    if (nc <= kCandMax) {
+    if (nc <= kCandMax && hots <= kCandMax) {
       rank_candidates(cand, nc, A.top_k, [&](int r, Cand c) { mine[r] = c; });
       nc = min(nc, A.top_k);
     } else {                                      // many equal logits: one alternative per pass
@@ -231,27 +248,35 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
       A.top_lp[n * k + r] = bad ? NAN : (none ? -INFINITY : (c.x - a.m) * A.inv_t - log_s);
     };
     int total = 0;
+#pragma unroll 1
     for (int r = 0; r < C; ++r) total += listed[r];
-    if (!bad)
-      for (int i = tid; i < C * k; i += kScoreThreads) {
-        const int q = i / k;
-        int r = i - q * k;                                    // its place in its own list, and in the others
-        if (r >= listed[q]) continue;
-        const Cand me = lists[i];
-        for (int p = 0; p < C && r < k; ++p) {
-          if (p == q) continue;
-          int lo = 0, hi = listed[p];
-          while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            const Cand o = lists[p * k + mid];
-            if (before(o.x, o.i, me.x, me.i)) lo = mid + 1;
-            else hi = mid;
-          }
-          r += lo;
+    if (bad) {
+      total = 0;
+    } else if (C == 1) {
+      if (tid < min(total, k)) put(tid, lists[tid]);
+    } else {
+      // a lane for each list that an alternative has its place in: its own, and the others by bisection
+#pragma unroll 1
+      for (int i = tid / 8; i - (tid & 31) / 8 < C * k; i += kScoreThreads / 8) {
+        const int q = i / k, j = i - q * k, p = tid & 7;
+        const bool is = i < C * k && j < listed[q];
+        const Cand me = is ? lists[i] : Cand{0.f, 0};
+        int lo = 0, hi = p < C ? listed[p] : 0;
+        if (p == q) lo = hi = j;
+#pragma unroll 1
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          const Cand o = lists[p * k + mid];
+          if (before(o.x, o.i, me.x, me.i)) lo = mid + 1;
+          else hi = mid;
         }
-        if (r < k) put(r, me);
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) lo += __shfl_xor_sync(0xffffffffu, lo, o);
+        if (is && lo < k && p == 0) put(lo, me);
       }
-    for (int r = (bad ? 0 : total) + tid; r < k; r += kScoreThreads) put(r, Cand{-INFINITY, -1});
+    }
+#pragma unroll 1
+    for (int r = total + tid; r < k; r += kScoreThreads) put(r, Cand{-INFINITY, -1});
   }
 }
 
