@@ -246,30 +246,47 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
                      : ((float)philox_block(A.seed, (uint32_t)b, (uint32_t)j, kStreamCoin, 0).x + 0.5f) * 0x1p-32f;
   }
   __syncthreads();
-  if (tid == 0) {
-    int acc = 0, m = 0;
+  if (tid == 0) {                                             // the recursion, which is sequential
+    float run = 0.f;
     la[0] = 0.f;
-    if (A.mode == SDV_MODE_SAMPLE) {
-      while (acc < n && (ell_s[acc] >= 0.f || eta[acc] < expf(ell_s[acc]))) ++acc;
-      for (int j = 0; j < n; ++j) la[j + 1] = 0.f;
-    } else {
-      float run = 0.f;
-      for (int j = 0; j < n; ++j) {
-        const float e = ell_s[j];
-        run = e == e ? fminf(0.f, run + e) : -INFINITY;
-        if (!(run == run)) run = -INFINITY;                 // -inf + inf
-        la[j + 1] = run;
-        const float alpha = expf(run);
-        if (run == 0.f || (j == n - 1 && eta[j] < alpha)) {
-          acc = j + 1;
-          m = 0;                                            // what is below cannot matter any more
-        } else if (j < n - 1 && eta[j] < alpha) {
-          need[m++] = j + 1;
+    for (int j = 0; j < n; ++j) {
+      const float e = ell_s[j];
+      run = e == e ? fminf(0.f, run + e) : -INFINITY;
+      if (!(run == run)) run = -INFINITY;                     // -inf + inf
+      la[j + 1] = A.mode == SDV_MODE_SAMPLE ? 0.f : run;
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {                                            // and what each step's coin says, a lane a step
+    uint64_t sure = 0, open = 0;                              // steps that succeed, steps whose mass decides
+    for (int j0 = 0; j0 < n; j0 += 32) {
+      const int j = j0 + lane;
+      bool hit = false, may = false;
+      if (j < n) {
+        if (A.mode == SDV_MODE_SAMPLE) {
+          hit = ell_s[j] >= 0.f || eta[j] < expf(ell_s[j]);
+        } else {
+          const bool below = eta[j] < expf(la[j + 1]);
+          hit = la[j + 1] == 0.f || (j == n - 1 && below);
+          may = !hit && j < n - 1 && below;
         }
       }
+      sure |= (uint64_t)__ballot_sync(0xffffffffu, hit) << j0;
+      open |= (uint64_t)__ballot_sync(0xffffffffu, may) << j0;
     }
-    acc_s = acc;
-    n_need = m;
+    int acc;
+    if (A.mode == SDV_MODE_SAMPLE) acc = sure == ~0ull ? n : min(n, __ffsll((long long)~sure) - 1);
+    else acc = 64 - __clzll((long long)sure);                 // the last success so far; steps before it cannot matter
+    const uint64_t rest = acc >= 64 ? 0 : open >> acc << acc;
+    if (A.mode == SDV_MODE_BLOCK)
+      for (int j0 = 0; j0 < n; j0 += 32) {
+        const int j = j0 + lane;
+        if (j < n && (rest >> j & 1)) need[__popcll((unsigned long long)(rest & ((1ull << j) - 1)))] = j + 1;
+      }
+    if (lane == 0) {
+      acc_s = acc;
+      n_need = A.mode == SDV_MODE_BLOCK ? __popcll((unsigned long long)rest) : 0;
+    }
   }
   __syncthreads();
   int acc = acc_s;
