@@ -425,11 +425,12 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         const int have = sq.len - key0 - 8 * t;
         drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
         uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
-#pragma unroll
+#pragma unroll 1
         for (int m = 0; m < 2 * kMt; ++m) {
           const uint2 v = *reinterpret_cast<const uint2*>(values + (m * 32 + lane) * 8);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) nan_keys |= (uint32_t)(((e < 4 ? v.x : v.y) >> (8 * (e & 3)) & 0x7f) == 0x7f) << e;
+          // a byte's low seven bits are all ones: its top bit after adding one to them
+          const uint32_t x = ((v.x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u, y = ((v.y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+          nan_keys |= (x >> 7 & 1) | (x >> 14 & 2) | (x >> 21 & 4) | (x >> 28 & 8) | (y >> 3 & 16) | (y >> 10 & 32) | (y >> 17 & 64) | (y >> 24 & 128);
         }
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) nan_keys |= __shfl_xor_sync(0xffffffffu, nan_keys, o);
