@@ -398,7 +398,8 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
  * with gradients, sdv_token_scores_train) and verified (sdv_token_verify: Algorithms
  * token-/block-verification with distributions over V tokens in place of Gaussian kernels).
  * The conventions above hold, but that logits, keys, values and queries are strided: strides
- * are in elements, the last axis is contiguous.  Arithmetic is fp32.
+ * are in elements, the last axis is contiguous.  Sums, softmax statistics and log probabilities
+ * are fp32.
  */
 #define SDV_F16 2              /* float16, in these entry points only */
 
@@ -499,7 +500,8 @@ int sdv_token_verify(const void *target, int64_t target_stride_b, int64_t target
 /*
  * The cache: k_codes [pages, H, block, D] and v_codes [pages, H, D, block] hold e4m3 codes (values
  * transposed: contiguous along the tokens), k_scale and v_scale [pages, H] fp32 what a
- * page's codes of a head are multiplied by.  Token i of sequence b is row i % block of page
+ * page's codes of a head are multiplied by (what sdv_cache_append writes are powers of two; a
+ * caller's own may be any number).  Token i of sequence b is row i % block of page
  * page_table[b, i / block] (page_table [B, max_pages] int32, only the entries of its tokens
  * are read).  D is 64 or 128, block a multiple of 16 up to SDV_MAX_BLOCK; code arrays are
  * 16-byte aligned.
@@ -532,8 +534,12 @@ size_t sdv_attend_workspace_bytes(int W, int Hq, int H, int D);
  * G = Hq / H, read key head h.  out [B, W, Hq, D] (`dtype`), lse [B, W, Hq] fp32 or NULL, dense.
  * Queries i >= counts[b], or with nothing to see, get 0 and -inf.  A NaN code in a key or value that
  * a query sees makes its row NaN; what it does not see has no effect.  Tokens of a page
- * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL).
- * Probabilities are rounded to fp16 (11 bits) before they meet the values, sums are fp32.
+ * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL), and a
+ * length beyond the page table counts as its end.  Probabilities are rounded to fp16 (11 bits,
+ * together with their values' scale) before they meet the values; bf16 queries go through fp16
+ * with a common power of two (exact above 2^-36 of a key head's largest); codes are exact and
+ * sums fp32.  The lengths of the batch decide where a sequence's keys are split, and so
+ * the order of its sums.
  */
 int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h,
                      int dtype, int B, int W, int Hq, int H, int D, int block,

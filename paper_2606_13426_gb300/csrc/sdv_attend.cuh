@@ -593,6 +593,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   const Sums ts = step_sums(A, b, lane);
   // the partials are there; CTAs without work wait as well, so that this kernel ends after k_attend
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (A.status && threadIdx.x == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
   if (row >= A.R) return;
   const Seq sq = seq_of(A, b);
   const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps, u1 = u0 + sq.steps;

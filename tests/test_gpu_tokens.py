@@ -791,3 +791,50 @@ def test_attend_refuses(api):
         api.cache_attend(q.to(BF16), c, pt.long(), n)
     with pytest.raises(ValueError):
         api.cache_attend(q.to(BF16), dict(c, v=c["k"]), pt, n)
+
+
+def test_attend_scales_of_any_sign_and_lengths_past_the_table(api):
+    g = gen(61)
+    cache = make_cache(api, g, 60, 2, 16, 64)
+    for k in ("k_scale", "v_scale"):
+        cache[k] *= torch.where(torch.rand(60, 2, generator=g, device="cuda") < 0.4, -1.0, 1.0)
+    pages = torch.randperm(60, generator=g, device="cuda")[:40].to(torch.int32).view(2, 20)
+    n = torch.tensor([300, 177], device="cuda", dtype=torch.int32)
+    q = torch.randn(2, 3, 6, 64, generator=g, device="cuda").to(BF16)
+    ref = check_attend(api, q, cache, pages, n)
+    st = torch.zeros(2, dtype=torch.int32, device="cuda")
+    full = torch.tensor([320, 177], device="cuda", dtype=torch.int32)
+    a = check_attend(api, q, cache, pages, full, status=st)
+    assert st.tolist() == [0, 0]
+    b = api.cache_attend(q, cache, pages, torch.tensor([5000, 177], device="cuda", dtype=torch.int32), status=st)
+    assert st.tolist() == [32, 0] and torch.equal(a["out"], b["out"])
+    # a scale that is no number shows in the rows that see its page, and in no others
+    spare = torch.tensor([p for p in range(60) if p not in pages.flatten().tolist()], device="cuda")
+    cache["v_scale"][spare] = NAN
+    cache["k_scale"][spare] = INF
+    assert torch.equal(api.cache_attend(q, cache, pages, n)["out"], ref["out"])
+    cache["v_scale"][int(pages[0, 3]), 1] = INF
+    cache["k_scale"][int(pages[1, 4]), 0] = NAN
+    r = api.cache_attend(q, cache, pages, n)["out"].float()
+    assert r[0, :, 3:].isnan().all() and torch.equal(r[0, :, :3], ref["out"][0, :, :3].float())
+    assert r[1, :, :3].isnan().all() and torch.equal(r[1, :, 3:], ref["out"][1, :, 3:].float())
+    # the last page of the window: its first query sees tokens before that page alone
+    n = torch.tensor([290, 177], device="cuda", dtype=torch.int32)          # queries at 287, 288, 289
+    ref = api.cache_attend(q, cache, pages[:, :], n)["out"]
+    cache["v_scale"][int(pages[0, 18]), 0] = NAN                              # tokens 288 .. 303
+    r = api.cache_attend(q, cache, pages, n)["out"]
+    assert torch.equal(r[0, 0, :3], ref[0, 0, :3]) and r[0, 1:, :3].float().isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_of_a_few_whole_sizes(api, dtype):
+    """Row sizes at which the rows' split over threads and clusters changes."""
+    g = gen(71)
+    for N, V in ((1, 8192 * 2), (5, 32768), (3, 32768 + 8), (2, 65536 * 2), (900, 4096), (400, 20000)):
+        x = make_logits(g, N, V, dtype, special=False)
+        tok = make_tokens(g, N, V)
+        gl, gh = torch.randn(N, generator=g, device="cuda"), torch.randn(N, generator=g, device="cuda")
+        t = api.token_scores_train(x, tok, gl, gh)
+        o = plain_scores(x, tok, 1.0, 0)
+        assert grad_ok(t["d_logits"], x, tok, o, gl, gh, 1.0)
+        assert near(t["logprob"], o["logprob"], 1e-5) and near(t["entropy"], o["entropy"], 2e-5)
