@@ -523,7 +523,7 @@ int sdv_cache_append(const void *k_new, const void *v_new, int64_t stride_b, int
                      const int32_t *counts, uint32_t *status, sdv_stream_t stream);
 
 /* Bytes of device workspace sdv_cache_attend needs; 0 for invalid sizes. */
-size_t sdv_attend_workspace_bytes(int W, int Hq, int H, int D);
+size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
 
 /*
  * sdv_cache_attend - attention of the last counts[b] (W if NULL) of the lengths[b] tokens in the

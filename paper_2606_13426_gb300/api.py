@@ -549,7 +549,7 @@ def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span
     dev = q.device
     r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
     if workspace is None:
-        workspace = torch.empty(max(_attend_workspace(W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(_attend_workspace(Bn, W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
     B._call("sdv_cache_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
             cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
             page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),

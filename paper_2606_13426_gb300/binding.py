@@ -91,7 +91,7 @@ SIGNATURES = {
     "sdv_token_verify_workspace_bytes": (_SZ, [_I, _I]),
     "sdv_cache_append": (_I, [_P, _P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
                               _P, _I, _P, _P, _P, _P]),
-    "sdv_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
+    "sdv_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
     "sdv_cache_attend": (_I, [_P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
                               _P, _I, _P, _P, _F, _I, _P, _P, _P, _P, _SZ, _P]),
     "sdv_timing_enable": (_I, [_I]),
@@ -361,8 +361,8 @@ def sdv_cache_append(k_new, v_new, stride_b, stride_t, stride_h, dtype, B, W, H,
                  counts, status, stream)
 
 
-def sdv_attend_workspace_bytes(W, Hq, H, D):
-    return int(load().sdv_attend_workspace_bytes(W, Hq, H, D))
+def sdv_attend_workspace_bytes(B, W, Hq, H, D):
+    return int(load().sdv_attend_workspace_bytes(B, W, Hq, H, D))
 
 
 def sdv_cache_attend(q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D, block, k_codes,

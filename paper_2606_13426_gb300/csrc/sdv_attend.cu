@@ -1,14 +1,53 @@
 // sdv_attend.cu - the entry points of the attention over the 8-bit cache.
 #include "sdv_attend.cuh"
 
+namespace sdv {
+
+// prefix[b]: the steps of the sequences before b, b = 0 .. B.
+__global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendArgs A, int64_t* prefix) {
+  __shared__ int64_t warps[kPrefixThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < A.B; b0 += kPrefixThreads) {
+    const int64_t mine = b0 + tid < A.B ? seq_of(A, b0 + tid).steps : 0;
+    int64_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    if (lane == 31) warps[tid / 32] = inc;
+    __syncthreads();
+    int64_t base = before;
+    for (int w = 0; w < kPrefixThreads / 32; ++w) {
+      if (w < tid / 32) base += warps[w];
+      before += warps[w];
+    }
+    if (b0 + tid < A.B) prefix[b0 + tid] = base + inc - mine;
+    __syncthreads();
+  }
+  if (tid == 0) prefix[A.B] = before;
+}
+
+// The workspace: the warps' partials, then the sums of the steps.
+struct AttendSpace {
+  size_t part, total;
+};
+static AttendSpace attend_space(int B, int W, int Hq, int H, int D) {
+  const int nt = row_tiles((int64_t)W * (Hq / H)).nt;
+  const size_t part = ((size_t)sm_count() * (size_t)attend_warps(nt) * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4 + 255) / 256 * 256;
+  return AttendSpace{part, part + (B > kPrefixFrom ? ((size_t)B + 1) * sizeof(int64_t) : 0)};
+}
+
+}  // namespace sdv
+
 using namespace sdv;
 
 extern "C" {
 
-size_t sdv_attend_workspace_bytes(int W, int Hq, int H, int D) {
-  if (W < 1 || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
-  const int nt = row_tiles((int64_t)W * (Hq / H)).nt;
-  return (size_t)sm_count() * (size_t)attend_warps(nt) * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4;
+size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D) {
+  if (B < 1 || W < 1 || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
+  return attend_space(B, W, Hq, H, D).total;
 }
 
 int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int dtype, int B, int W,
@@ -26,7 +65,8 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(status, 4) || !aligned_to(lengths, 4) ||
       !aligned_to(counts, 4))
     return SDV_EALIGN;
-  if (!workspace || workspace_bytes < sdv_attend_workspace_bytes(W, Hq, H, D)) return SDV_ENOWORKSPACE;
+  const AttendSpace space = attend_space(B, W, Hq, H, D);
+  if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   AttendArgs A{};
   const RowTiles tiles = row_tiles(R);
@@ -44,6 +84,13 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   A.part = (float*)workspace;
   A.ctas = sm_count();
   cudaStream_t s = (cudaStream_t)stream;
+  if (B > kPrefixFrom) {
+    int64_t* prefix = (int64_t*)((char*)workspace + space.part);
+    k_attend_prefix<<<1, kPrefixThreads, 0, s>>>(A, prefix);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return launched(e);
+    A.prefix = prefix;
+  }
   return launched(D == 64 ? launch_attend_64(A, tiles.nt, s) : launch_attend_128(A, tiles.nt, s));
 }
 

@@ -91,8 +91,8 @@ def test_cache_attend(lib):
     from paper_2606_13426_gb300 import binding as B
     bad, align = B.SDV_EINVAL, B.SDV_EALIGN
     names = "q sb st_ sh dtype B W Hq H D block kc vc ks vs pages tab M n cnt scale span out lse st ws wsb s".split()
-    wsb = B.sdv_attend_workspace_bytes(2, 4, 2, 64)
-    assert wsb > 0 and B.sdv_attend_workspace_bytes(2, 3, 2, 64) == 0 and B.sdv_attend_workspace_bytes(2, 4, 2, 80) == 0
+    wsb = B.sdv_attend_workspace_bytes(2, 2, 4, 2, 64)
+    assert wsb > 0 and B.sdv_attend_workspace_bytes(2, 2, 3, 2, 64) == 0 and B.sdv_attend_workspace_bytes(2, 2, 4, 2, 80) == 0
     base = dict(CACHE, q=0x1000, sb=512, st_=256, sh=64, dtype=B.SDV_BF16, B=2, W=2, Hq=4, H=2, D=64, block=16, scale=0.1, span=0,
                 out=0x2000, lse=0x3000, ws=0x100000, wsb=wsb, s=None)
     check(lib, "sdv_cache_attend", names, base, [

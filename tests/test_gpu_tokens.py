@@ -725,6 +725,26 @@ def test_attend_over_long_caches_and_many_sequences(api):
     check_attend(api, q, cache, pages, n)
 
 
+@pytest.mark.parametrize("B", [256, 257, 3000])
+def test_attend_over_batches_with_empty_sequences(api, B):
+    """Runs of sequences without tokens or without queries, at the ends too, around the batch size from
+    which the steps are added up by a kernel of their own."""
+    g = gen(48 + B)
+    cache = make_cache(api, g, 2000, 1, 16, 64)
+    n = torch.zeros(B, dtype=torch.int32)
+    live = torch.randperm(B - 20, generator=torch.Generator().manual_seed(B))[:40] + 10
+    n[live] = torch.randint(1, 400, (40,), generator=torch.Generator().manual_seed(B + 1), dtype=torch.int32)
+    n = n.cuda()
+    counts = (torch.rand(B, generator=g, device="cuda") < 0.8).to(torch.int32)
+    pages = torch.randint(0, 2000, (B, 25), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randn(B, 1, 2, 64, generator=g, device="cuda").to(BF16)
+    check_attend(api, q, cache, pages, n)
+    check_attend(api, q, cache, pages, n, counts)
+    check_attend(api, q, cache, pages, torch.zeros_like(n))
+    n[0] = n[B - 1] = 333
+    check_attend(api, q, cache, pages, n)
+
+
 def test_cache_offsets_past_32_bits(api):
     """Pages behind the first 2^32 bytes of codes."""
     H, block, D = 4, 64, 128
