@@ -35,6 +35,8 @@ constexpr int kMinSteps = 2;              // of a run, where there are fewer ste
 constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
+// The values' scale that the others are taken relative to, 4 times it and kPScale over that, stay finite.
+constexpr float kLeastVs = 0x1p-118f, kMostVs = 0x1.fp125f;
 constexpr float kPScale = 128.f;          // f16 holds 2^kSlack * kPScale; what is below 2^-28 of the reference is lost
 
 // Division by the chunks of a page (up to 8) of numbers below 2^28: a product's upper half.
@@ -497,6 +499,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
             }
         }
       }
+      va = fminf(fmaxf(va, kLeastVs), kMostVs);
       float top[kR];
       bool move = va > vref;
 #pragma unroll

@@ -697,6 +697,36 @@ def test_attend_missing_pages_and_zero_scales(api):
     assert st.tolist() == [32, 32, 0]
 
 
+def test_attend_extreme_value_scales(api):
+    """Keys and values of zeros as they are appended (the least scale), then some that are not zero; scales near both
+    ends of fp32."""
+    g = gen(49)
+    cache = api.make_token_cache(6, 2, 32, 64)
+    pages = torch.arange(6, device="cuda", dtype=torch.int32).view(2, 3)
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    zero = torch.zeros(2, 40, 2, 64, device="cuda")
+    api.cache_append(cache, zero, zero, pages, none)
+    n = none + 40
+    q = torch.randn(2, 3, 4, 64, generator=g, device="cuda").to(BF16)
+    r = api.cache_attend(q, cache, pages, n)
+    assert not r["out"].any() and near(r["lse"], torch.log(torch.tensor([38.0, 39.0, 40.0], device="cuda", dtype=torch.float64))
+                                       .view(1, 3, 1).expand(2, 3, 4), 2e-5)
+    x = torch.randn(2, 30, 2, 64, generator=g, device="cuda")
+    api.cache_append(cache, x, x, pages, n)
+    check_attend(api, q, cache, pages, n + 30)
+    for size in (2.0 ** -126, 2.0 ** -110, 2.0 ** 100, 1e38 / 448):
+        c = make_cache(api, g, 6, 2, 32, 64)
+        c["v_scale"].fill_(size)
+        out, _, mag = plain_attend(q, c, pages, n, [3, 3], 0.125, 0)
+        got = api.cache_attend(q, c, pages, n)["out"].double()
+        # bf16's least step, 2^-133, twice (the result's rounding, and a sum's of fp32 results below 2^-126)
+        assert ((got - out).abs() <= 2.0 ** -11 * mag + 1.01 * 2.0 ** -8 * out.abs() + 2.0 ** -132).all(), size
+    c["v_scale"].copy_(torch.tensor([2.0 ** -126, 1.0, 2.0 ** 100], device="cuda").repeat(2)[:, None].expand(6, 2))
+    out, _, mag = plain_attend(q, c, pages, n + 50, [3, 3], 0.125, 0)
+    got = api.cache_attend(q, c, pages, n + 50)["out"].double()
+    assert ((got - out).abs() <= 2.0 ** -11 * mag + 1.01 * 2.0 ** -8 * out.abs()).all()
+
+
 def test_attend_large_and_tiny_queries(api):
     """bf16 queries outside f16's range, scores far apart, values of very different scales."""
     g = gen(44)
