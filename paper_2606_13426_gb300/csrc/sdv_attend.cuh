@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       for (int j = 0; j < kN; ++j) {
         const int p = lane + 32 * j, row = row0 + p / (kD / 8), i = row / A.G;
         raw[j] = make_uint4(0, 0, 0, 0);
-        if (row < A.R) raw[j] = q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
+        if (row < A.R && i < sq.count) raw[j] = q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
       }
       float up = 1.f;
       if (A.bf16) {

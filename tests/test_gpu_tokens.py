@@ -727,6 +727,22 @@ def test_attend_extreme_value_scales(api):
     assert ((got - out).abs() <= 2.0 ** -11 * mag + 1.01 * 2.0 ** -8 * out.abs()).all()
 
 
+def test_attend_rows_past_the_window_do_not_matter(api):
+    """Queries i >= counts[b] may hold anything: large numbers there leave the others' results alone."""
+    g = gen(50)
+    cache = make_cache(api, g, 20, 2, 32, 128)
+    pages = torch.arange(20, device="cuda", dtype=torch.int32).view(2, 10)
+    n = torch.tensor([300, 77], device="cuda", dtype=torch.int32)
+    counts = torch.tensor([2, 3], device="cuda", dtype=torch.int32)
+    q = torch.randn(2, 4, 6, 128, generator=g, device="cuda").to(BF16)
+    ref = check_attend(api, q, cache, pages, n, counts)
+    for x in (1e30, 3e38, INF, NAN):
+        q[0, 2:] = x
+        q[1, 3:] = -x
+        r = api.cache_attend(q, cache, pages, n, counts=counts)
+        assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"])
+
+
 def test_attend_large_and_tiny_queries(api):
     """bf16 queries outside f16's range, scores far apart, values of very different scales."""
     g = gen(44)
