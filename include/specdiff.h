@@ -503,7 +503,7 @@ int sdv_token_verify(const void *target, int64_t target_stride_b, int64_t target
  * page's codes of a head are multiplied by (what sdv_cache_append writes are powers of two; a
  * caller's own may be any number).  Token i of sequence b is row i % block of page
  * page_table[b, i / block] (page_table [B, max_pages] int32, only the entries of its tokens
- * are read).  D is 64 or 128, block a multiple of 16 up to SDV_MAX_BLOCK; code arrays are
+ * are read; max_pages block is at most 2^30).  D is 64 or 128, block a multiple of 16 up to SDV_MAX_BLOCK; code arrays are
  * 16-byte aligned.
  *
  * sdv_cache_append - appends counts[b] (W if NULL; at most W) new tokens behind the lengths[b]

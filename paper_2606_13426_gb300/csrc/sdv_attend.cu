@@ -79,7 +79,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   A.B = B, A.W = W, A.G = Hq / H, A.R = (int)R, A.RT = tiles.rt;
   A.lengths = lengths, A.counts = counts;
   A.scale2 = scale * kLog2E;
-  A.span = span;
+  A.span = span < max_pages * block ? span : 0;             // as many as there can be, or more: all
   A.out = out, A.lse = lse, A.status = status;
   A.part = (float*)workspace;
   A.ctas = sm_count();

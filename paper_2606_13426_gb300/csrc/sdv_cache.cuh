@@ -23,6 +23,8 @@ struct CacheView {
   int H, D, block;
 };
 
+// Tokens of a sequence at most: a position less a span, or plus a step, is an int.
+constexpr int64_t kMaxTokens = 1 << 30;
 constexpr int kChunk = 16;          // tokens: a block is a whole number of chunks
 
 inline int check_cache(const void* k, const void* v, const void* ks, const void* vs, int64_t pages, const void* table,
@@ -30,7 +32,7 @@ inline int check_cache(const void* k, const void* v, const void* ks, const void*
   if (!k || !v || !ks || !vs || !table) return SDV_EINVAL;
   if (pages < 1 || pages > 0x7fffffff || max_pages < 1 || H < 1 || H > 65535 || (D != 64 && D != 128)) return SDV_EINVAL;
   if (block < kChunk || block > SDV_MAX_BLOCK || block % kChunk) return SDV_EINVAL;
-  if ((int64_t)max_pages * block > 0x7fffffff) return SDV_EINVAL;
+  if ((int64_t)max_pages * block > kMaxTokens) return SDV_EINVAL;
   if (!aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(ks, 4) || !aligned_to(vs, 4) || !aligned_to(table, 4))
     return SDV_EALIGN;
   return SDV_OK;

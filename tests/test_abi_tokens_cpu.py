@@ -99,6 +99,7 @@ def test_cache_attend(lib):
         (dict(q=0), bad), (dict(out=0), bad), (dict(n=0), bad), (dict(dtype=B.SDV_F32), bad), (dict(Hq=3), bad), (dict(Hq=1), bad),
         (dict(H=0), bad), (dict(W=0), bad), (dict(B=0), bad), (dict(D=32), bad), (dict(block=12), bad), (dict(span=-1), bad),
         (dict(scale=float("nan")), bad), (dict(scale=float("inf")), bad), (dict(st_=-1), bad), (dict(q=0x1001), align),
+        (dict(M=(1 << 26) + 1), bad), (dict(M=(1 << 23) + 1, block=128), bad),
         (dict(out=0x2001), align), (dict(lse=0x3002), align), (dict(kc=0x10004), align), (dict(ws=0), B.SDV_ENOWORKSPACE),
         (dict(wsb=wsb - 1), B.SDV_ENOWORKSPACE), (dict(ws=0x100080), align)])
 

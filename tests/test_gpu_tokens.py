@@ -743,6 +743,20 @@ def test_attend_rows_past_the_window_do_not_matter(api):
         assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"])
 
 
+def test_attend_spans_as_long_as_the_cache(api):
+    """Spans of the cache's length and more, up to the largest int, see everything; with fewer tokens than queries too."""
+    g = gen(51)
+    cache = make_cache(api, g, 20, 2, 16, 64)
+    pages = torch.arange(20, device="cuda", dtype=torch.int32).view(4, 5)
+    n = torch.tensor([80, 4, 1, 33], device="cuda", dtype=torch.int32)
+    q = torch.randn(4, 9, 2, 64, generator=g, device="cuda").to(BF16)
+    ref = check_attend(api, q, cache, pages, n)
+    for span in (80, 81, (1 << 31) - 1):
+        r = check_attend(api, q, cache, pages, n, span=span)
+        assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"])
+    check_attend(api, q, cache, pages, n, span=79)
+
+
 def test_attend_large_and_tiny_queries(api):
     """bf16 queries outside f16's range, scores far apart, values of very different scales."""
     g = gen(44)
