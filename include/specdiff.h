@@ -485,7 +485,8 @@ size_t sdv_token_verify_workspace_bytes(int B, int L);
  *   accepted_len, next_token [B] int32 out; log_ratio_out [B, L] fp32 out or NULL (0 past the
  *     window); status_out [B] uint32 out or NULL
  * A token outside [0, V), a masked token (target -inf) and a step whose rows hold a NaN or
- * +inf are rejected; a masked draft token with a possible target token has ell = +inf.  Where
+ * +inf are rejected; a masked draft token with a possible target token has ell = +inf
+ * (alpha = 0 stays 0 there).  Where
  * alpha q - p leaves nothing, the target's own row is drawn from (SDV_STATUS_ZERO_DELTA); a
  * target row without probabilities gives next_token -1.  A draft row without any counts as 0.
  */

@@ -250,9 +250,8 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
     float run = 0.f;
     la[0] = 0.f;
     for (int j = 0; j < n; ++j) {
-      const float e = ell_s[j];
-      run = e == e ? fminf(0.f, run + e) : -INFINITY;
-      if (!(run == run)) run = -INFINITY;                     // -inf + inf
+      const float next = run + ell_s[j];
+      run = next == next ? fminf(0.f, next) : -INFINITY;      // NaN: a step without a ratio, or -inf + inf
       la[j + 1] = A.mode == SDV_MODE_SAMPLE ? 0.f : run;
     }
   }

@@ -388,6 +388,23 @@ def test_verify_masks_and_bad_rows(api):
         assert acc[11] == L and nxt[11] == -1
 
 
+def test_verify_an_impossible_token_before_one_the_draft_calls_impossible(api):
+    """alpha = 0 behind a token that the target masks, whatever follows: ell = +inf does not bring it back."""
+    g = gen(13)
+    B, L, V = 4, 4, 300
+    tl, dl, tok, coins, race = make_verify(g, B, L, V, F32)
+    tl[:, 1, 7] = -INF
+    tok[:, 1] = 7                            # rejected, and with it all that follows
+    dl[:, 2, 9] = -INF
+    dl[:, 3, 9] = -INF
+    tok[:, 2:] = 9
+    coins[:] = 0.25
+    for mode in ("block", "sample"):
+        r = api.token_verify(tl, dl, tok, mode=mode, coins=coins, race=race)
+        assert (r["accepted_len"] <= 1).all()
+        assert r["log_ratio"][:, 1].tolist() == [-INF] * B and r["log_ratio"][:, 2:].flatten().tolist() == [INF] * 2 * B
+
+
 def test_verify_with_nothing_left(api):
     """alpha q - p <= 0 everywhere, by a coin that no draw gives: the target's own row is drawn from."""
     tl = torch.zeros(1, 2, 100, device="cuda")
