@@ -425,7 +425,7 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
  * no alternatives (SDV_STATUS_NONFINITE).  A token outside [0, V) other than -1 has NaN
  * (SDV_STATUS_BAD_TOKEN).
  *   dtype SDV_F32, SDV_BF16 or SDV_F16; N >= 0 (0: nothing is done), V >= 1,
- *   0 <= top_k <= min(V, SDV_MAX_TOP), temperature > 0, row_stride >= V
+ *   0 <= top_k <= min(V, SDV_MAX_TOP), 1e-9 <= temperature <= 1e9, row_stride >= V
  *   tokens and logprob may both be NULL, and each other output (not all); status [N] uint32
  */
 int sdv_token_scores(const void *logits, int64_t row_stride, int N, int V, int dtype,
@@ -477,6 +477,7 @@ size_t sdv_token_verify_workspace_bytes(int B, int L);
  *           largest r_v / E_v, the lower of equal ones, for that (unnormalised) r and
  *           exponential variates E_v.
  *   target : [B, L + 1, V] rows at b target_stride_b + j target_stride_row; draft [B, L, V]
+ *   temperatures from 1e-9 to 1e9
  *   tokens [B, L] int32; L_eff [B] int32 or NULL: windows n <= L; n = 0 draws from target row 0,
  *     n < 0 marks an inactive chain (accepted_len 0, next_token -1)
  *   coins  [B, L] fp32 in [0, 1) or NULL: eta; NULL draws them as sdv_verify does

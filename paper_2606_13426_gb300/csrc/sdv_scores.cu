@@ -501,8 +501,7 @@ __global__ void __launch_bounds__(kTrainThreads, 4) k_scores_train(const TrainAr
 
 static int check_rows(const void* x, int64_t stride, int N, int V, int dtype, float temperature) {
   if (!token_dtype(dtype) || N < 0 || V < 1 || V > (1 << 30) || stride < V) return SDV_EINVAL;
-  if (!(temperature > 0.f) || !(kLog2E / temperature < INFINITY) || !(temperature < INFINITY)) return SDV_EINVAL;
-  if (!x) return SDV_EINVAL;
+  if (!temperature_ok(temperature) || !x) return SDV_EINVAL;
   if (!aligned_to(x, elem_bytes(dtype))) return SDV_EALIGN;
   return SDV_OK;
 }

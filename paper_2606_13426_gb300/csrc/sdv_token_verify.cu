@@ -452,9 +452,7 @@ int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target
                      sdv_stream_t stream) {
   if (B < 1 || B > (1 << 20) || L < 1 || L > SDV_MAX_L || V < 1 || V > (1 << 30) || !token_dtype(dtype)) return SDV_EINVAL;
   if (mode != SDV_MODE_SAMPLE && mode != SDV_MODE_BLOCK) return SDV_EINVAL;
-  const float t[2] = {temperature, draft_temperature};
-  for (float x : t)
-    if (!(x > 0.f) || !(x < INFINITY) || !(kLog2E / x < INFINITY)) return SDV_EINVAL;
+  if (!temperature_ok(temperature) || !temperature_ok(draft_temperature)) return SDV_EINVAL;
   if (!target || !draft || !tokens || !accepted_len || !next_token) return SDV_EINVAL;
   if (target_stride_row < V || draft_stride_row < V || target_stride_b < 0 || draft_stride_b < 0) return SDV_EINVAL;
   if (!aligned_to(target, elem_bytes(dtype)) || !aligned_to(draft, elem_bytes(dtype))) return SDV_EALIGN;

@@ -18,8 +18,10 @@ namespace cg = cooperative_groups;
 constexpr float kLog2E = 1.44269504088896341f;   // log2 e
 constexpr float kLn2f = 0.69314718055994531f;    // log 2
 // Far below any difference of two logits that leaves a probability, and finite: 0 * kFar is 0
-// where 0 * -inf would be NaN.
-constexpr float kFar = -1e15f;
+// where 0 * -inf would be NaN.  The temperatures allowed keep it so: kFar / T is -1000 or less,
+// and kFar / T^2, a factor in the entropy's gradient, finite.
+constexpr float kFar = -1e12f;
+constexpr float kLeastTemperature = 1e-9f, kMostTemperature = 1e9f;
 
 template <int kDtype>
 struct Num;
@@ -389,6 +391,7 @@ __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_c
 inline int min_int(int a, int b) { return a < b ? a : b; }
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t elem_bytes(int dtype) { return dtype == SDV_F32 ? 4 : 2; }
+inline bool temperature_ok(float t) { return t >= kLeastTemperature && t <= kMostTemperature; }
 inline bool token_dtype(int dtype) { return dtype == SDV_F32 || dtype == SDV_BF16 || dtype == SDV_F16; }
 
 // The return code of a launch.

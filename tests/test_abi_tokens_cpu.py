@@ -31,6 +31,7 @@ def test_scores(lib):
     check(lib, "sdv_token_scores", names, base, [
         (dict(x=0), bad), (dict(stride=99), bad), (dict(N=-1), bad), (dict(V=0), bad), (dict(V=(1 << 30) + 1, stride=1 << 31), bad),
         (dict(dtype=3), bad), (dict(T=0.0), bad), (dict(T=float("inf")), bad), (dict(T=float("nan")), bad), (dict(T=1e-39), bad),
+        (dict(T=9e-10), bad), (dict(T=1.1e9), bad),
         (dict(k=-1), bad), (dict(k=33), bad), (dict(V=3, k=4), bad), (dict(ids=0), bad), (dict(tlp=0), bad), (dict(lp=0), bad),
         (dict(tok=0), bad), (dict(x=0x1001), align), (dict(x=0x1002, dtype=B.SDV_F32), align), (dict(H=0x4002), align),
         (dict(ids=0x7001), align), (dict(tok=0, lp=0, H=0, m=0, ls=0, k=0), bad),
@@ -45,7 +46,7 @@ def test_gradients(lib):
                 dx=0x8000, dstride=100, s=None)
     check(lib, "sdv_token_scores_grad", names, base, [
         (dict(dx=0), bad), (dict(dstride=99), bad), (dict(m=0), bad), (dict(ls=0), bad), (dict(H=0), bad), (dict(gl=0, gh=0), bad),
-        (dict(tok=0), bad), (dict(gl=0), bad), (dict(T=-1.0), bad), (dict(dx=0x8002), align), (dict(gh=0x7001), align),
+        (dict(tok=0), bad), (dict(gl=0), bad), (dict(T=-1.0), bad), (dict(T=1e-12), bad), (dict(dx=0x8002), align), (dict(gh=0x7001), align),
         (dict(N=0, x=0), B.SDV_OK)])
     names = "x stride N V dtype tok T gl gh lp H m ls st dx dstride s".split()
     base.update(lp=0x9000, st=0)
@@ -66,6 +67,7 @@ def test_token_verify(lib):
     check(lib, "sdv_token_verify", names, base, [
         (dict(q=0), bad), (dict(p=0), bad), (dict(tok=0), bad), (dict(acc=0), bad), (dict(nxt=0), bad), (dict(B=0), bad), (dict(L=0), bad),
         (dict(L=65), bad), (dict(V=0), bad), (dict(dtype=7), bad), (dict(T=0.0), bad), (dict(Td=float("nan")), bad), (dict(mode=2), bad),
+        (dict(T=1e-10), bad), (dict(Td=1e10), bad),
         (dict(qr=99), bad), (dict(pr=99), bad), (dict(qb=-1), bad), (dict(q=0x1001), align), (dict(p=0x2001), align),
         (dict(tok=0x3002), align), (dict(race=0x7001), align), (dict(ws=0), B.SDV_ENOWORKSPACE), (dict(wsb=wsb - 1), B.SDV_ENOWORKSPACE),
         (dict(ws=0x6010), align)])

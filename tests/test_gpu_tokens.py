@@ -209,6 +209,33 @@ def test_gradient_matches_the_formula(api, N, V, pad, off, dtype):
             assert grad_ok(api.token_scores_grad(y2, tok, r, gl, gh, temperature=T, d_logits=y2), x, tok, o, gl, gh, T)
 
 
+@pytest.mark.parametrize("T", [1e-9, 1e9])
+def test_extreme_temperatures_with_masks(api, T):
+    """Masked logits have no part in anything at either end of the temperatures: nearly one-hot, nearly flat."""
+    g = gen(52)
+    N, V = 6, 1500
+    x = 3.0 * torch.randn(N, V, generator=g, device="cuda")
+    masked = torch.rand(N, V, generator=g, device="cuda") < 0.5
+    masked[:, 0] = False
+    x[masked] = -INF
+    tok = torch.zeros(N, dtype=torch.int32, device="cuda")
+    one = torch.ones(N, device="cuda")
+    r = api.token_scores_train(x, tok, one, one, temperature=T)
+    live = (~masked).sum(1).double()
+    dx = r["d_logits"].double()
+    assert (dx[masked] == 0).all() and not dx.isnan().any()
+    if T > 1:
+        assert near(r["logprob"], -live.log(), 1e-5) and near(r["entropy"], live.log(), 1e-5)
+        p = torch.where(masked, 0.0, 1 / live[:, None])
+        want = ((torch.arange(V, device="cuda") == 0).double() - p) / T
+        # p (log p + H): the parts of H - log s + d/T cancel to about 1e-6 of themselves, against 1
+        assert ((dx - want).abs() <= 1e-5 / T * (p * live[:, None].log() + want.abs() * T)).all()
+    else:
+        assert (r["entropy"] == 0).all() and (x.gather(1, x.argmax(1)[:, None])[:, 0] == r["row_max"]).all()
+    v = api.token_verify(x[None, :4], x[None, :3], x[:3].argmax(1).to(torch.int32)[None], 5, "block", temperature=T)
+    assert int(v["accepted_len"]) == 3 and not masked[3, int(v["next_token"])]
+
+
 def test_gradient_matches_differences(api):
     """Central differences of the forward kernel: step 1e-2, so that its 1e-5 (1 + |value|) weighs 4e-3
     at most here, and the third derivative's share is below 1e-4."""
