@@ -512,7 +512,7 @@ int sdv_token_verify(const void *target, int64_t target_stride_b, int64_t target
  * that sequence b holds.  k_new and v_new are [B, W, H, D] (F32, BF16 or F16) with the strides
  * given, the same for both.  A page's scale becomes the least power of two (2^-126 or more)
  * whose 448-fold holds the new tokens' magnitudes, or stays if tokens that it holds already have a larger
- * one; if it grows, those tokens' codes are restated under it.  Codes are rounded to
+ * one; if it grows (or was negative, and becomes its magnitude), those tokens' codes are restated under it.  Codes are rounded to
  * nearest even; infinities become +-448, NaN a NaN code, and neither counts for the scale.
  * Rows behind the new tokens keep what they held.  A token whose page does not exist is left out
  * (SDV_STATUS_BAD_PAGE).  status [B] uint32 or NULL: bits are added to it.  No page may be

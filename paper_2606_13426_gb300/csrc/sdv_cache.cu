@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(kAppendThreads, append_ctas(kDtype, kUnits)) k
   for (int kind = 1; kind >= 0; --kind) {
     const float need = scale_for(amax[kind]);
     const float s_old = r0 ? was[kind] : need;
-    const float s = fmaxf(s_old, need);
+    const float s = fmaxf(fabsf(s_old), need);                    // (a caller's own may be negative: codes change sign)
     const bool restate = r0 && s != s_old;
     const float ratio = s_old / s;
     const bool pow2 = (__float_as_uint(s) & 0x807fffffu) == 0 && s >= 0x1p-126f && s <= 0x1p126f;

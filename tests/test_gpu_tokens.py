@@ -596,6 +596,31 @@ def test_append_extreme_values_and_missing_pages(api):
         assert same(cache[k], o[k]), k
 
 
+def test_append_to_pages_with_negative_scales(api):
+    """A page whose scale a caller made negative gets its magnitude, or a larger one, and keeps its values."""
+    g = gen(32)
+    cache = random_cache(api, g, 2, 2, 32, 64)
+    for k in ("k_scale", "v_scale"):
+        cache[k].copy_(torch.tensor([[-4.0, -0.25], [-8.0, 2.0]], device="cuda"))
+    pages = torch.tensor([[0], [1]], device="cuda", dtype=torch.int32)
+    n = torch.tensor([7, 20], device="cuda", dtype=torch.int32)
+    was = {k: cache[k].double() * cache[k + "_scale"].double()[:, :, None, None] for k in ("k", "v")}
+    x = torch.rand(2, 3, 2, 64, generator=g, device="cuda") + 400.0
+    api.cache_append(cache, x, x, pages, n)
+    for k in ("k", "v"):
+        s = cache[k + "_scale"]
+        assert s.tolist() == [[4.0, 1.0], [8.0, 2.0]]
+        now = cache[k].double() * s.double()[:, :, None, None]
+        for b, m in ((0, 7), (1, 20)):
+            old, new = (was[k][b], now[b]) if k == "k" else (was[k][b].transpose(1, 2), now[b].transpose(1, 2))
+            # under a scale 4 times as large: half a step of the least codes, 2^-10, or 2^-4 of a value
+            tol = torch.maximum(old[:, :m].abs() * 2.0 ** -4, s[b].double()[:, None, None] * 2.0 ** -10)
+            tol[s[b] != 1.0] = 0
+            assert torch.equal(new[:, :m].isnan(), old[:, :m].isnan())
+            assert ((new[:, :m] - old[:, :m]).nan_to_num().abs() <= tol.nan_to_num()).all()
+            assert ((new[:, m:m + 3] - x[b].double().transpose(0, 1)).abs() <= 2.0 ** -4 * 401).all()
+
+
 def test_append_refuses(api):
     from paper_2606_13426_gb300 import binding as B
     c = api.make_token_cache(4, 2, 16, 64)
