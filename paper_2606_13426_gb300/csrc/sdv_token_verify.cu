@@ -9,9 +9,9 @@
 // the largest r_v / E_v, the E_v exponential variates (a race, which needs no cumulated sums).
 //
 // k_token_stats takes every row's softmax statistics, one read of the logits with all rows alike, a
-// cluster of CTAs each.  k_token_verify has a cluster of CTAs per chain, each with a part of
-// every row's columns: the masses v_j that can matter and the race are taken from a second read
-// of those rows, which the L2 still holds.  h_j <= alpha_j, so that a step with eta_j >= alpha_j
+// cluster of CTAs each (in small calls k_token_verify does it).  k_token_verify has a cluster of
+// CTAs per chain, each with a part of every row's columns: the masses v_j that can matter and the
+// race are taken from a second read of those rows, which the L2 still holds.  h_j <= alpha_j, so that a step with eta_j >= alpha_j
 // fails, and one with alpha_j = 1 succeeds, without its mass.
 #include "sdv_device.cuh"
 #include "sdv_tokens.cuh"
@@ -25,6 +25,7 @@ constexpr int kLogVerSegs = 3;
 constexpr int kVerSegs = kVerWarps;    // segments of a CTA's part of a row, a warp each
 constexpr int kVerRows = 2 * SDV_MAX_L + 1;
 constexpr uint32_t kStreamRace = 7;
+constexpr int64_t kOwnBytes = 72 << 10;
 
 static_assert(kVerSegs == 1 << kLogVerSegs, "");
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, cons
   constexpr int kPer = E::kPer16, kUn = 2;
   const bool vec = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(p)) & 15) == 0;
   const Row<kDtype> R(q, V);
-  const int total = vec ? R.nvec : V / kPer * kPer / kPer;          // groups of kPer
+  const int total = vec ? R.nvec : V / kPer;          // groups of kPer
   const int g0 = share(total, part, log_parts), g1 = share(total, part + 1, log_parts);
   const uint4* vq = R.vec();
   const uint4* vp = reinterpret_cast<const uint4*>(p + R.head);
@@ -161,7 +162,8 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   if (threadIdx.x == 0) A.stats[n] = RowStat{all.m, log2f(all.s)};
 }
 
-template <int kDtype>
+// kOwn: the cluster takes its chain's statistics itself (see own_stats), a warp a row's part.
+template <int kDtype, bool kOwn>
 __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVerifyArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
@@ -214,17 +216,42 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
     for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
       asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");         // the rows' statistics are there
+  if constexpr (kOwn) {
+    __shared__ Stat own[kVerRows], all[kVerRows * kVerMaxCluster];
+    const int log_seg = rows >= kVerWarps ? 0 : rows >= kVerWarps / 2 ? 1 : 2;      // few rows: parts of them
+    for (int u = warp; u < rows << log_seg; u += kVerWarps) {
+      const int r = u >> log_seg;
+      const float c = r <= n ? A.cq : A.cp;
+      const Part<kDtype, false, 32> P(Row<kDtype>(r <= n ? q0 + r * A.q_sr : p0 + (r - n - 1) * A.p_sr, V),
+                                      (rank << log_seg) + (u & ((1 << log_seg) - 1)), log_c + log_seg);
+      const Stat a = run_warp(P.read(c), c);
+      if (lane == 0) own[u] = Stat{a.m, a.s, 0.f};
+    }
+    __syncthreads();
+    if (C > 1) cl.barrier_wait();                            // every CTA of the cluster has started
+    for (int i = tid; i < rows << (log_seg + log_c); i += kVerThreads) {
+      const int u = i >> log_c, k = i & (C - 1);
+      (C > 1 ? cl.map_shared_rank(all, k) : all)[(u << log_c) + rank] = own[u];
+    }
+    if (C > 1) cl.sync();
+    else __syncthreads();
+    for (int r = warp; r < rows; r += kVerWarps) {
+      const Stat a = stat_gather(all + (r << (log_seg + log_c)), 1 << (log_seg + log_c), lane, r <= n ? A.cq : A.cp);
+      if (lane == 0) rs[r] = RowStat{a.m, log2f(a.s)};
+    }
+    __syncthreads();
+  } else {
+    asm volatile("griddepcontrol.wait;" ::: "memory");       // the rows' statistics are there
+    for (int r = tid; r < rows; r += kVerThreads) rs[r] = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
+    if (C > 1) cl.barrier_wait();
+    __syncthreads();
+  }
   for (int r = tid; r < rows; r += kVerThreads) {
-    const RowStat a = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
-    rs[r] = a;
     uint32_t st = 0;
-    if (!(a.m < INFINITY)) st |= SDV_STATUS_NONFINITE;
-    if (a.m == -INFINITY) st |= SDV_STATUS_EMPTY_ROW;
+    if (!(rs[r].m < INFINITY)) st |= SDV_STATUS_NONFINITE;
+    if (rs[r].m == -INFINITY) st |= SDV_STATUS_EMPTY_ROW;
     if (st) atomicOr(&status_s, st);
   }
-  if (C > 1) cl.barrier_wait();                              // every CTA of the cluster has started
-  __syncthreads();
   // log ratios and coins
   static_assert(SDV_MAX_L <= kVerThreads, "a thread per step");
   if (tid < n) {
@@ -420,17 +447,28 @@ static int verify_cluster(int B, int V, int dtype) {
   return c;
 }
 
+// Whether k_token_verify takes the statistics itself: where a CTA's parts of the rows are small.  Calls one
+// after another, two kernels and one (bf16): 1 chain of 4 steps, V = 32768 (37 KB a CTA), 24.6 us
+// and 20.7; 16 of 1, V = 131072 (49 KB), 24.9 and 20.9; 16 of 8, V = 32768 (70 KB), 24.5 and 23.0; 128
+// of 8, V = 4096 (70 KB), 27.2 and 20.3; 48 of 8, V = 32768 (139 KB), 25.5 and 27.2.
+static bool own_stats(int B, int L, int V, int dtype, int C) {
+  return (int64_t)(2 * L + 1) * V * (int64_t)elem_bytes(dtype) / C <= kOwnBytes;
+}
+
 template <int kDtype>
 static cudaError_t launch_token_verify(const TokenVerifyArgs& A, int B, int dtype, cudaStream_t s) {
   const int C = verify_cluster(B, A.V, dtype);
+  const bool own = own_stats(B, A.L, A.V, dtype, C);
+  const auto verify = own ? k_token_verify<kDtype, true> : k_token_verify<kDtype, false>;
   if (C > 8) {
-    const cudaError_t e = cudaFuncSetAttribute(k_token_verify<kDtype>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    const cudaError_t e = cudaFuncSetAttribute(verify, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
   }
+  if (own) return launch_cluster(verify, dim3((unsigned)B * (unsigned)C), kVerThreads, 0, (unsigned)C, false, s, A);
   const int rows = B * (2 * A.L + 1), Cs = score_cluster(rows, A.V, dtype);
   const cudaError_t e = launch_cluster(k_token_stats<kDtype>, dim3((unsigned)rows * (unsigned)Cs), kScoreThreads, 0, (unsigned)Cs, false, s, A);
   if (e != cudaSuccess) return e;
-  return launch_cluster(k_token_verify<kDtype>, dim3((unsigned)B * (unsigned)C), kVerThreads, 0, (unsigned)C, true, s, A);
+  return launch_cluster(verify, dim3((unsigned)B * (unsigned)C), kVerThreads, 0, (unsigned)C, true, s, A);
 }
 
 }  // namespace sdv

@@ -306,19 +306,20 @@ constexpr int kScoreThreads = 256;
 constexpr int kScoreVecs = 8;          // 16-byte vectors of a thread under way at once
 constexpr int kScoreMaxCluster = 8;
 
-// A thread's part of a row: vectors v0 + tid + u kScoreThreads < v1, and one of the row's single
-// elements.
-template <int kDtype, bool kEntropy>
+// A thread's part of a row: vectors v0 + tid + u kStep < v1, and one of the row's single elements;
+// kStep threads share the row's part.
+template <int kDtype, bool kEntropy, int kStep = kScoreThreads>
 struct Part {
   using E = Num<kDtype>;
+  static __device__ __forceinline__ int tid() { return (int)threadIdx.x & (kStep - 1); }
   const uint4* vec;
   int v0, v1, single;
   float x;
   __device__ __forceinline__ Part(const Row<kDtype>& R, int rank, int log_c) {
     vec = R.vec();
-    v0 = share(R.nvec, rank, log_c) + (int)threadIdx.x;
+    v0 = share(R.nvec, rank, log_c) + tid();
     v1 = share(R.nvec, rank + 1, log_c);
-    single = rank == 0 && (int)threadIdx.x < R.singles() ? R.single(threadIdx.x) : -1;
+    single = rank == 0 && tid() < R.singles() ? R.single(tid()) : -1;
     x = single >= 0 ? E::to(R.p[single]) : 0.f;
   }
   // Its statistics; what is past the part counts as masked: one copy of the code for whole and partial
@@ -326,12 +327,12 @@ struct Part {
   __device__ __forceinline__ Run read(float c) const {
     Run r = run_empty();
 #pragma unroll 1
-    for (int v = v0; v - (int)threadIdx.x < v1; v += kScoreVecs * kScoreThreads) {
+    for (int v = v0; v - tid() < v1; v += kScoreVecs * kStep) {
       uint4 raw[kScoreVecs];
 #pragma unroll
       for (int u = 0; u < kScoreVecs; ++u) {
         raw[u] = vec_masked<kDtype>();
-        if (v + u * kScoreThreads < v1) raw[u] = vec[v + u * kScoreThreads];
+        if (v + u * kStep < v1) raw[u] = vec[v + u * kStep];
       }
 #pragma unroll
       for (int u = 0; u < kScoreVecs; ++u) {

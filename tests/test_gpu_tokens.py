@@ -365,6 +365,17 @@ def test_verify(api, B, L, V, dtype, mode):
     check_verify(api, tl, dl, tok, coins, race, mode, n, T=0.9, Td=1.2)
 
 
+@pytest.mark.parametrize("B,L,V,dtype", [(16, 8, 32768, BF16), (16, 8, 40001, BF16), (3, 1, 3, F32), (2, 3, 20000, F32),
+                                         (128, 8, 4096, F16), (128, 8, 5000, F16)])
+def test_verify_with_statistics_taken_in_one_kernel_or_two(api, B, L, V, dtype):
+    """Sizes on both sides of where the chains' clusters take their rows' statistics themselves."""
+    g = gen(B + L + V)
+    tl, dl, tok, coins, race = make_verify(g, B, L, V, dtype)
+    n = torch.randint(-1, L + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    check_verify(api, tl, dl, tok, coins, race, "block", n, T=0.9)
+    check_verify(api, tl, dl, tok, coins, race, "sample")
+
+
 def test_verify_of_strided_and_unaligned_rows(api):
     g = gen(11)
     for dtype in (F32, BF16):
