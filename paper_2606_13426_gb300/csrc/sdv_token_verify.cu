@@ -45,6 +45,8 @@ struct TokenVerifyArgs {
   float* ell;
   uint32_t* status;
   struct RowStat* stats;                // workspace [B, 2 L + 1]: target rows, then draft rows
+  struct StepIn* steps;                 // workspace [B, L]
+  int* windows;                         // workspace [B]
 };
 
 struct Best {
@@ -64,6 +66,25 @@ __device__ __forceinline__ bool row_ok(const RowStat& r) { return r.m > -INFINIT
 // log2 of the probability, with `shift` (a log2) added.
 __device__ __forceinline__ float prob(const RowStat& r, float x, float c, float shift) {
   return ex2(fmaf(fmaxf(x - r.m, kFar), c, shift - r.l2));
+}
+
+// What a step needs beside its rows' statistics: its token, the token's logits and the coin.
+struct StepIn {
+  int t;
+  float xq, xp, eta;
+};
+template <int kDtype>
+__device__ __forceinline__ StepIn step_in(const TokenVerifyArgs& A, int b, int j) {
+  using E = Num<kDtype>;
+  using T = typename E::T;
+  StepIn s{A.tokens[(int64_t)b * A.L + j], 0.f, 0.f, 0.f};
+  if (s.t >= 0 && s.t < A.V) {
+    s.xq = E::to((reinterpret_cast<const T*>(A.q) + b * A.q_sb + j * A.q_sr)[s.t]);
+    s.xp = E::to((reinterpret_cast<const T*>(A.p) + b * A.p_sb + j * A.p_sr)[s.t]);
+  }
+  s.eta = A.coins ? A.coins[(int64_t)b * A.L + j]
+                  : ((float)philox_block(A.seed, (uint32_t)b, (uint32_t)j, kStreamCoin, 0).x + 0.5f) * 0x1p-32f;
+  return s;
 }
 
 // Four exponential variates: E_v of elements 4 block .. 4 block + 3 of chain b, from the seed.
@@ -136,7 +157,8 @@ __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, cons
   }
 }
 
-// The statistics of one row a cluster; rows past a chain's window are left out.
+// The statistics of one row a cluster (rows past a chain's window are left out), and beside them what
+// the CTAs of k_token_verify's clusters must all see alike: the windows, tokens, their logits and coins.
 template <int kDtype>
 __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVerifyArgs A) {
   using T = typename Num<kDtype>::T;
@@ -145,9 +167,19 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
   const int n = blockIdx.x >> log_c, per = 2 * A.L + 1, b = n / per, r = n % per;
   const int window = A.L_eff ? min(A.L_eff[b], A.L) : A.L;
-  if (r <= A.L ? r > window : r - A.L - 1 >= window) return;
   __shared__ Stat stats[kScoreMaxCluster * kWarps];
   if (C > 1) cl.barrier_arrive();
+  const bool first = rank == 0 && threadIdx.x == 0;
+  if (first && r == 0) A.windows[b] = window;
+  if (r <= A.L ? r > window : r - A.L - 1 >= window) {
+    if (C > 1) {                               // with as many barriers as the other CTAs, whatever they read
+      cl.barrier_wait();
+      cl.sync();
+    }
+    return;
+  }
+  StepIn in{};
+  if (first && r < window) in = step_in<kDtype>(A, b, r);
   const T* row = r <= A.L ? reinterpret_cast<const T*>(A.q) + b * A.q_sb + r * A.q_sr
                           : reinterpret_cast<const T*>(A.p) + b * A.p_sb + (r - A.L - 1) * A.p_sr;
   const float c = r <= A.L ? A.cq : A.cp;
@@ -159,12 +191,17 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   else __syncthreads();
   if (rank || threadIdx.x >= 32) return;
   const Stat all = stat_gather(stats, C * kWarps, threadIdx.x, c);
-  if (threadIdx.x == 0) A.stats[n] = RowStat{all.m, log2f(all.s)};
+  if (threadIdx.x == 0) {
+    A.stats[n] = RowStat{all.m, log2f(all.s)};
+    if (r < window) A.steps[(int64_t)b * A.L + r] = in;
+  }
 }
 
 // kOwn: the cluster takes its chain's statistics itself (see own_stats), a warp a row's part.
+// The CTAs of a cluster decide alike, and so meet at the same barriers: what they decide on comes from one
+// place, k_token_stats' workspace or the first CTA, even if the caller's arrays change meanwhile.
 template <int kDtype, bool kOwn>
-__global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVerifyArgs A) {
+__global__ void __launch_bounds__(kVerThreads, 3) k_token_verify(const TokenVerifyArgs A) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
@@ -172,9 +209,71 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), log_c = __ffs(C) - 1;
   const int b = blockIdx.x >> log_c, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int L = A.L, V = A.V;
-  const int n_in = A.L_eff ? A.L_eff[b] : L;
-  if (n_in < 0) {                                  // an inactive chain
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+  __shared__ RowStat rs[kVerRows];
+  __shared__ StepIn in[SDV_MAX_L];
+  __shared__ float mass_seg[SDV_MAX_L * kVerSegs];
+  __shared__ float mass_part[kVerMaxCluster * SDV_MAX_L];
+  __shared__ float la[SDV_MAX_L + 1], ell_s[SDV_MAX_L];
+  __shared__ int need[SDV_MAX_L];
+  __shared__ int n_need, acc_s, window_s;
+  __shared__ uint32_t status_s;
+  __shared__ Best best_w[kVerWarps];
+  __shared__ Best best_c[2][kVerMaxCluster];
+  static_assert(SDV_MAX_L <= kVerThreads, "a thread per step");
+  if (C > 1) cl.barrier_arrive();
+  if (tid == 0) status_s = 0;
+  const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
+  const T* p0 = reinterpret_cast<const T*>(A.p) + b * A.p_sb;
+  if (A.race) {
+    const float* race = A.race + (int64_t)b * V;
+    for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
+  }
+  int n_in;                                                  // the chain's window
+  if constexpr (kOwn) {
+    __shared__ Stat own[kVerRows], all[kVerRows * kVerMaxCluster];
+    const int window = A.L_eff ? A.L_eff[b] : L, nw = max(min(window, L), 0);
+    const bool sends = rank == 0 && tid < nw;
+    StepIn mine{};
+    if (sends) mine = step_in<kDtype>(A, b, tid);
+    auto log_segs = [](int rows) { return rows >= kVerWarps ? 0 : rows >= kVerWarps / 2 ? 1 : 2; };   // few rows: parts of them
+    int log_seg = log_segs(2 * nw + 1);
+    for (int u = warp; u < (2 * nw + 1) << log_seg; u += kVerWarps) {
+      const int r = u >> log_seg;
+      const float c = r <= nw ? A.cq : A.cp;
+      const Part<kDtype, false, 32> P(Row<kDtype>(r <= nw ? q0 + r * A.q_sr : p0 + (r - nw - 1) * A.p_sr, V),
+                                      (rank << log_seg) + (u & ((1 << log_seg) - 1)), log_c + log_seg);
+      const Stat a = run_warp(P.read(c), c);
+      if (lane == 0) own[u] = Stat{a.m, a.s, 0.f};
+    }
+    __syncthreads();
+    if (C > 1) cl.barrier_wait();                            // every CTA of the cluster has started
+    for (int i = tid; i < (2 * nw + 1) << (log_seg + log_c); i += kVerThreads) {
+      const int u = i >> log_c, k = i & (C - 1);
+      (C > 1 ? cl.map_shared_rank(all, k) : all)[(u << log_c) + rank] = own[u];
+    }
+    for (int k = 0; k < C; ++k) {
+      if (sends) (C > 1 ? cl.map_shared_rank(in, k) : in)[tid] = mine;
+      if (rank == 0 && tid == 0) *(C > 1 ? cl.map_shared_rank(&window_s, k) : &window_s) = window;
+    }
+    if (C > 1) cl.sync();
+    else __syncthreads();
+    n_in = window_s;
+    const int n = max(min(n_in, L), 0);
+    log_seg = log_segs(2 * n + 1);
+    for (int r = warp; r < 2 * n + 1; r += kVerWarps) {
+      const Stat a = stat_gather(all + (r << (log_seg + log_c)), 1 << (log_seg + log_c), lane, r <= n ? A.cq : A.cp);
+      if (lane == 0) rs[r] = RowStat{a.m, log2f(a.s)};
+    }
+  } else {
+    asm volatile("griddepcontrol.wait;" ::: "memory");       // the rows' statistics are there
+    n_in = A.windows[b];
+    const int n = max(min(n_in, L), 0);
+    for (int r = tid; r < 2 * n + 1; r += kVerThreads) rs[r] = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
+    if (tid < n) in[tid] = A.steps[(int64_t)b * L + tid];
+    if (C > 1) cl.barrier_wait();
+  }
+  if (n_in < 0) {                                            // an inactive chain
     if (rank == 0) {
       if (tid == 0) {
         A.accepted[b] = 0;
@@ -186,80 +285,21 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
     }
     return;
   }
-  const int n = min(n_in, L);
-  const int rows = 2 * n + 1;
-  __shared__ RowStat rs[kVerRows];
-  __shared__ float mass_seg[SDV_MAX_L * kVerSegs];
-  __shared__ float mass_part[kVerMaxCluster * SDV_MAX_L];
-  __shared__ float la[SDV_MAX_L + 1], ell_s[SDV_MAX_L], eta[SDV_MAX_L];
-  __shared__ int need[SDV_MAX_L];
-  __shared__ int n_need, acc_s;
-  __shared__ uint32_t status_s;
-  __shared__ Best best_w[kVerWarps];
-  __shared__ Best best_c[2][kVerMaxCluster];
-  if (C > 1) cl.barrier_arrive();
-  if (tid == 0) status_s = 0;
-  const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
-  const T* p0 = reinterpret_cast<const T*>(A.p) + b * A.p_sb;
-  // what is needed later and known now: this thread's step's token and its logits; the race's part
-  int my_token = -1;
-  float my_xq = 0.f, my_xp = 0.f;
-  if (tid < n) {
-    my_token = A.tokens[(int64_t)b * L + tid];
-    if (my_token >= 0 && my_token < V) {
-      my_xq = E::to(q0[tid * A.q_sr + my_token]);
-      my_xp = E::to(p0[tid * A.p_sr + my_token]);
-    }
-  }
-  if (A.race) {
-    const float* race = A.race + (int64_t)b * V;
-    for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
-  }
-  if constexpr (kOwn) {
-    __shared__ Stat own[kVerRows], all[kVerRows * kVerMaxCluster];
-    const int log_seg = rows >= kVerWarps ? 0 : rows >= kVerWarps / 2 ? 1 : 2;      // few rows: parts of them
-    for (int u = warp; u < rows << log_seg; u += kVerWarps) {
-      const int r = u >> log_seg;
-      const float c = r <= n ? A.cq : A.cp;
-      const Part<kDtype, false, 32> P(Row<kDtype>(r <= n ? q0 + r * A.q_sr : p0 + (r - n - 1) * A.p_sr, V),
-                                      (rank << log_seg) + (u & ((1 << log_seg) - 1)), log_c + log_seg);
-      const Stat a = run_warp(P.read(c), c);
-      if (lane == 0) own[u] = Stat{a.m, a.s, 0.f};
-    }
-    __syncthreads();
-    if (C > 1) cl.barrier_wait();                            // every CTA of the cluster has started
-    for (int i = tid; i < rows << (log_seg + log_c); i += kVerThreads) {
-      const int u = i >> log_c, k = i & (C - 1);
-      (C > 1 ? cl.map_shared_rank(all, k) : all)[(u << log_c) + rank] = own[u];
-    }
-    if (C > 1) cl.sync();
-    else __syncthreads();
-    for (int r = warp; r < rows; r += kVerWarps) {
-      const Stat a = stat_gather(all + (r << (log_seg + log_c)), 1 << (log_seg + log_c), lane, r <= n ? A.cq : A.cp);
-      if (lane == 0) rs[r] = RowStat{a.m, log2f(a.s)};
-    }
-    __syncthreads();
-  } else {
-    asm volatile("griddepcontrol.wait;" ::: "memory");       // the rows' statistics are there
-    for (int r = tid; r < rows; r += kVerThreads) rs[r] = A.stats[(int64_t)b * (2 * L + 1) + (r <= n ? r : L + r - n)];
-    if (C > 1) cl.barrier_wait();
-    __syncthreads();
-  }
+  const int n = min(n_in, L), rows = 2 * n + 1;
+  __syncthreads();
   for (int r = tid; r < rows; r += kVerThreads) {
     uint32_t st = 0;
     if (!(rs[r].m < INFINITY)) st |= SDV_STATUS_NONFINITE;
     if (rs[r].m == -INFINITY) st |= SDV_STATUS_EMPTY_ROW;
     if (st) atomicOr(&status_s, st);
   }
-  // log ratios and coins
-  static_assert(SDV_MAX_L <= kVerThreads, "a thread per step");
+  // log ratios
   if (tid < n) {
-    const int j = tid, t = my_token;
+    const int j = tid, t = in[j].t;
     float ell = NAN;
     if (t >= 0 && t < V) {
       const RowStat rq = rs[j], rp = rs[n + 1 + j];
-      const float xq = my_xq, xp = my_xp;
+      const float xq = in[j].xq, xp = in[j].xp;
       if (rq.m < INFINITY && rp.m < INFINITY) {
         const float lq = row_ok(rq) && xq > -INFINITY ? (xq - rq.m) * A.iq - rq.l2 * kLn2f : -INFINITY;
         const float lp = row_ok(rp) && xp > -INFINITY ? (xp - rp.m) * A.ip - rp.l2 * kLn2f : -INFINITY;
@@ -269,8 +309,6 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
       atomicOr(&status_s, SDV_STATUS_BAD_TOKEN);
     }
     ell_s[j] = ell;
-    eta[j] = A.coins ? A.coins[(int64_t)b * L + j]
-                     : ((float)philox_block(A.seed, (uint32_t)b, (uint32_t)j, kStreamCoin, 0).x + 0.5f) * 0x1p-32f;
   }
   __syncthreads();
   if (tid == 0) {                                             // the recursion, which is sequential
@@ -290,9 +328,9 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
       bool hit = false, may = false;
       if (j < n) {
         if (A.mode == SDV_MODE_SAMPLE) {
-          hit = ell_s[j] >= 0.f || eta[j] < expf(ell_s[j]);
+          hit = ell_s[j] >= 0.f || in[j].eta < expf(ell_s[j]);
         } else {
-          const bool below = eta[j] < expf(la[j + 1]);
+          const bool below = in[j].eta < expf(la[j + 1]);
           hit = la[j + 1] == 0.f || (j == n - 1 && below);
           may = !hit && j < n - 1 && below;
         }
@@ -350,7 +388,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_token_verify(const TokenVeri
       float s = 0.f;
       for (int k = 0; k < C; ++k) s += mass_part[k * SDV_MAX_L + i];
       const float h = s / (s + 1.f - expf(la[j]));
-      if (eta[j - 1] < h) {
+      if (in[j - 1].eta < h) {
         acc = max(acc, j);
         break;
       }
@@ -479,7 +517,7 @@ extern "C" {
 
 size_t sdv_token_verify_workspace_bytes(int B, int L) {
   if (B < 1 || B > (1 << 20) || L < 1 || L > SDV_MAX_L) return 0;
-  return ((size_t)B * (2 * L + 1) * sizeof(RowStat) + 255) / 256 * 256;
+  return ((size_t)B * ((2 * L + 1) * sizeof(RowStat) + L * sizeof(StepIn) + sizeof(int)) + 255) / 256 * 256;
 }
 
 int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target_stride_row, const void* draft,
@@ -502,7 +540,8 @@ int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target
   const TokenVerifyArgs A{target, draft, target_stride_b, target_stride_row, draft_stride_b, draft_stride_row, tokens, L, V,
                           mode, kLog2E / temperature, kLog2E / draft_temperature, 1.f / temperature,
                           1.f / draft_temperature, L_eff, seed, coins, race, accepted_len, next_token, log_ratio_out,
-                          status_out, (RowStat*)workspace};
+                          status_out, (RowStat*)workspace, (StepIn*)((RowStat*)workspace + (size_t)B * (2 * L + 1)),
+                          (int*)((StepIn*)((RowStat*)workspace + (size_t)B * (2 * L + 1)) + (size_t)B * L)};
   cudaStream_t s = (cudaStream_t)stream;
   return launched(dtype == SDV_F32    ? launch_token_verify<SDV_F32>(A, B, dtype, s)
                   : dtype == SDV_BF16 ? launch_token_verify<SDV_BF16>(A, B, dtype, s)
