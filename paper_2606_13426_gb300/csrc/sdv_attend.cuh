@@ -250,10 +250,12 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       if (!sq.steps) {
         at_u = find_sequence(A, u / per, lane);
         b = at_u.b;
+        if (b == A.B) break;
         seq_u = at_u.before * per;
-        continue;
+        sq = seq_of(A, b);
       }
     }
+    if (u < seq_u || u >= seq_u + (int64_t)sq.steps * per) break;   // (only if the lengths have changed meanwhile)
     const int item = (int)((u - seq_u) / sq.steps);
     const int h = item / A.RT, row0 = item % A.RT * S::kRows;
     const int64_t item_u = seq_u + (int64_t)item * sq.steps;
@@ -636,10 +638,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   if (A.status && threadIdx.x == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
   if (row >= A.R) return;
   const Seq sq = seq_of(A, b);
-  const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps, u1 = u0 + sq.steps;
+  const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps;
+  const int64_t u1 = min(u0 + sq.steps, units);              // (never past them, unless the lengths have changed meanwhile)
   const int runs = run_count(units, A.ctas * S::kWarps);
   int g0 = 0, g1 = -1;
-  if (sq.steps) {
+  if (u0 < u1) {
     // the runs [units g / runs, units (g + 1) / runs) that meet [u0, u1)
     g0 = (int)((u0 * runs) / units);
     while (run_start(units, g0 + 1, runs) <= u0) ++g0;
