@@ -35,7 +35,7 @@ struct AttendSpace {
 };
 static AttendSpace attend_space(int B, int W, int Hq, int H, int D) {
   const int nt = row_tiles((int64_t)W * (Hq / H)).nt;
-  const size_t part = ((size_t)sm_count() * (size_t)attend_warps(nt) * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4 + 255) / 256 * 256;
+  const size_t part = ((size_t)sm_count() * kAttendWarps * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4 + 255) / 256 * 256;
   return AttendSpace{part, part + (B > kPrefixFrom ? ((size_t)B + 1) * sizeof(int64_t) : 0)};
 }
 

@@ -176,8 +176,9 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from, bool real) 
 constexpr int kPrefixFrom = 256;
 constexpr int kPrefixThreads = 1024;
 
-// Warps of a CTA of k_attend.
-constexpr int attend_warps(int nt) { return nt == 1 ? 16 : nt == 2 ? 12 : 8; }
+// Warps of a CTA of k_attend, one CTA an SM: 2 x 1 token of 64 query heads on 8, up to 131000 keys, takes 63 us
+// with 8 warps, 73 with 6 (and longer rings) and 67 with 16, which the registers of few rows would allow.
+constexpr int kAttendWarps = 8;
 
 __device__ __forceinline__ void put_out(const AttendArgs& A, int64_t at, float x) {
   if (A.bf16) reinterpret_cast<__nv_bfloat16*>(A.out)[at] = __float2bfloat16_rn(x);
@@ -185,17 +186,17 @@ __device__ __forceinline__ void put_out(const AttendArgs& A, int64_t at, float x
 }
 __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + log2f(l)) * kLn2f : (l == 0.f ? -INFINITY : NAN); }
 
-// A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others under
-// way; its queries' fragments are beside it.  Few rows leave registers and shared memory for more
-// warps, whose latencies overlap.
+// A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others, 8 KB, under
+// way; its queries' fragments are beside it.  (Four under way at D = 128, where few rows leave room: 1
+// to 7 % slower for 4 to 32 rows.)
 template <int kD, int kNt>
 struct AttendShape {
-  static constexpr int kWarps = attend_warps(kNt);
+  static constexpr int kWarps = kAttendWarps;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRows = 8 * kNt;
   static constexpr int kSlot = kRows * (kD + 2);         // floats of a partial: rows' output, max, sum
   static constexpr int kHalf = kSub * kD;                 // bytes
-  static constexpr int kHalves = (kNt <= 2 || kNt == 5 ? 3 : 5) * (kD == 64 ? 2 : 1) - (kD == 64 ? 1 : 0);
+  static constexpr int kHalves = kD == 64 ? 5 : 3;
   static constexpr int kAhead = (kHalves - 1) / 2;        // steps
   static constexpr int kScaleSlots = kAhead + 1;
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread

@@ -352,11 +352,14 @@ struct Part {
   }
 };
 
-// CTAs per row: while there are fewer than four an SM, as many as leave every thread four vectors.
+// CTAs per row: while there are fewer than four an SM, as many as leave every thread sixteen vectors.  With
+// 16, 4 and 32 of them, without alternatives / with 20 (us, bf16): 128 rows of 32768 4.3 / 8.5, 5.8 / 11.5
+// and 4.2 / 7.0; 300 of 8192 3.8 / 6.2, 6.0 / 10.9, 3.9 / 6.3; 32 of 65536 3.8 / 8.1, 4.2 / 9.8, 4.6 / 8.6; 1 of
+// 131072 3.3 / 8.4, 3.7 / 8.8, 4.1 / 8.4.  With up to two CTAs an SM 144 of 131072 take 11.4 in place of 10.3.
 inline int score_cluster(int64_t N, int V, int dtype) {
   const int64_t nvec = (int64_t)V * (dtype == SDV_F32 ? 4 : 2) / 16;
   int c = 1;
-  while (c < kScoreMaxCluster && N * 2 * c <= 4 * sm_count() && nvec >= 4 * c * kScoreThreads) c *= 2;
+  while (c < kScoreMaxCluster && N * 2 * c <= 4 * sm_count() && nvec >= 16 * c * kScoreThreads) c *= 2;
   return c;
 }
 
