@@ -777,6 +777,20 @@ def test_attend_missing_pages_and_zero_scales(api):
     assert st.tolist() == [32, 32, 0]
 
 
+def test_attend_f16_outputs_are_rounded_once(api):
+    """What is beside an f16 output's own rounding: scores to 2^-22 of the sum of their products' magnitudes (about 7 here, so that
+    exponentials are off by 2^-17 at most, with a margin of 8), and probabilities of 22 bits."""
+    g = gen(53)
+    for W, G, D, m in ((1, 4, 128, 900), (9, 4, 128, 700), (5, 7, 64, 3000), (17, 1, 64, 65)):
+        cache = make_cache(api, g, 200, 2, 32, D)
+        pages = torch.randperm(200, generator=g, device="cuda").to(torch.int32).view(2, 100)
+        n = torch.tensor([m, m // 2], device="cuda", dtype=torch.int32)
+        q = torch.randn(2, W, 2 * G, D, generator=g, device="cuda").to(F16)
+        out, lse, mag = plain_attend(q, cache, pages, n, [W, W], D ** -0.5, 0)
+        got = api.cache_attend(q, cache, pages, n)["out"].double()
+        assert ((got - out).abs() <= 2.0 ** -14 * mag + 1.01 * 2.0 ** -11 * out.abs() + 1e-7).all()
+
+
 def test_attend_extreme_value_scales(api):
     """Keys and values of zeros as they are appended (the least scale), then some that are not zero; scales near both
     ends of fp32."""
