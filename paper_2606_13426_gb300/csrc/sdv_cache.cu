@@ -131,6 +131,9 @@ constexpr int append_ctas(int dtype, int units) {
 // (kUnits sixteens of elements of each a thread) between the largest magnitude and the codes: the
 // loads of both are under way together.  Values go through shared memory as codes, and are
 // turned in 4 x 4 bytes on the way out.
+// 4 x 8000 tokens, 8 heads of 128, bf16: 42 us, 4.7 TB/s (131 MB in, 66 out); bound by issue slots (56 % busy:
+// conversions, the transposition) and by the chain of length, page, scale in each CTA.  64 windows
+// of 9 tokens: 6.5 us, latency.
 template <int kDtype, int kUnits>
 __global__ void __launch_bounds__(kAppendThreads, append_ctas(kDtype, kUnits)) k_cache_append(const AppendArgs A) {
   using T = typename Num<kDtype>::T;

@@ -95,8 +95,9 @@ static __device__ __noinline__ float4 race4(uint64_t seed, uint32_t b, uint32_t 
 
 // Calls f(first index, n, q, p) with n <= 8 (kPer) consecutive elements of two rows at a time: this
 // thread's share (of `step` threads) of part `part` of 2^log_parts.  Rows in the same phase of 16 bytes
-// are read as vectors, others element by element, a warp's next to each other (n = 1).  The body of
-// f is there once: the passes over the rows run from a cold instruction cache.
+// are read as vectors, others element by element; what is before and behind the groups of kPer comes
+// one at a time (n = 1, the other places masked).  The passes over the rows run from a cold instruction
+// cache: two groups under way, not more (four: no gain).
 template <int kDtype, typename F>
 __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, int V, int part,
                                           int log_parts, int lane, int step, F f) {
@@ -157,6 +158,7 @@ __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, cons
   }
 }
 
+// Bound by the read: 272 rows of 131072 bf16 (71 MB) take 15 us, 4.7 TB/s.
 // The statistics of one row a cluster (rows past a chain's window are left out), and beside them what
 // the CTAs of k_token_verify's clusters must all see alike: the windows, tokens, their logits and coins.
 template <int kDtype>
@@ -198,6 +200,10 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
 }
 
 // kOwn: the cluster takes its chain's statistics itself (see own_stats), a warp a row's part.
+// A chain of dependent phases, bound by their latency: 16 chains of 8 steps, V = 131072 bf16, 18 us in block mode
+// (masses of the steps that may succeed, a warp a segment of a row, 8 of them; then the race), 12 in sample mode; one chain
+// of 4 steps, V = 32768, with its statistics 11 us.  Three CTAs an SM: with four (64 registers) spills cost 2 to 4 %,
+// with two 48 chains wait for places (26 us become 33).
 // The CTAs of a cluster decide alike, and so meet at the same barriers: what they decide on comes from one
 // place, k_token_stats' workspace or the first CTA, even if the caller's arrays change meanwhile.
 template <int kDtype, bool kOwn>
@@ -475,9 +481,9 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_token_verify(const TokenVeri
   }
 }
 
-// CTAs per chain: as many as fit beside the other chains' (four an SM, some left for clusters that do
-// not fill their part of the chip), as long as each thread has a vector of a row.  Clusters of 16
-// leave fewer places than those of 8.
+// CTAs per chain: as many as fit beside the other chains' (three an SM), as long as each thread has a vector
+// of a row.  With half as many 16 x 8 x 131072 bf16 take 35 us in place of 33 and 48 x 7 x 50001 fp32 29 in
+// place of 26; with twice as many, more than are resident together, the latter 37.
 static int verify_cluster(int B, int V, int dtype) {
   const int64_t nvec = (int64_t)V * (int64_t)elem_bytes(dtype) / 16;
   int c = 1;
