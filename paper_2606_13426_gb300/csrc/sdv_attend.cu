@@ -34,7 +34,7 @@ struct AttendSpace {
   size_t part, total;
 };
 static AttendSpace attend_space(int B, int W, int Hq, int H, int D) {
-  const int nt = row_tiles((int64_t)W * (Hq / H)).nt;
+  const int nt = row_tiles((int64_t)W * (Hq / H), kMaxNt).nt;             // (no choice of tiles has more)
   const size_t part = ((size_t)sm_count() * kAttendWarps * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4 + 255) / 256 * 256;
   return AttendSpace{part, part + (B > kPrefixFrom ? ((size_t)B + 1) * sizeof(int64_t) : 0)};
 }
@@ -69,7 +69,9 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   AttendArgs A{};
-  const RowTiles tiles = row_tiles(R);
+  A.span = span < max_pages * block ? span : 0;             // as many as there can be, or more: all
+  const int64_t tokens = min(A.span > 0 ? (int64_t)A.span + W + kSub : kMaxTokens, (int64_t)max_pages * block);
+  const RowTiles tiles = choose_tiles(R, (int64_t)B * H, (tokens + kSub - 1) / kSub, D, sm_count() * kAttendWarps);
   A.q = q;
   A.bf16 = dtype == SDV_BF16;
   A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
@@ -79,7 +81,6 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   A.B = B, A.W = W, A.G = Hq / H, A.R = (int)R, A.RT = tiles.rt;
   A.lengths = lengths, A.counts = counts;
   A.scale2 = scale * kLog2E;
-  A.span = span < max_pages * block ? span : 0;             // as many as there can be, or more: all
   A.out = out, A.lse = lse, A.status = status;
   A.part = (float*)workspace;
   A.ctas = sm_count();

@@ -31,7 +31,7 @@ namespace sdv {
 constexpr int kSub = 32;                  // keys of a step
 constexpr int kJoinWarps = 8;
 constexpr int kJoinThreads = 32 * kJoinWarps;
-constexpr int kMinSteps = 2;              // of a run, where there are fewer steps than warps could take
+constexpr int kMinSteps = 2;              // of a run, where there are fewer steps than warps could take (but see run_count)
 constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
@@ -140,8 +140,11 @@ __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, i
 }
 
 __device__ __forceinline__ int64_t run_start(int64_t units, int g, int runs) { return units * g / runs; }
-__device__ __forceinline__ int run_count(int64_t units, int warps) {
-  return (int)min((int64_t)warps, (units + kMinSteps - 1) / kMinSteps);
+// Runs for `units` steps of `items` items.  Where the items have a step each, a run has one: 144 rows over 19 keys
+// take 18 us, and 27 with two steps a run; items of two steps want them together (32 rows over 48 keys: 40 us, and
+// 53 apart).
+__device__ __forceinline__ int run_count(int64_t units, int64_t items, int warps) {
+  return (int)min((int64_t)warps, units <= items ? units : (units + kMinSteps - 1) / kMinSteps);
 }
 
 // Four e4m3 codes as two pairs of f16.
@@ -239,7 +242,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   float* scales = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes);
 
   const int64_t units = step_sums(A, 0, lane).total * per;
-  const int runs = run_count(units, A.ctas * S::kWarps);   // none of them empty
+  const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);   // none of them empty
   // neighbours in the order of the runs sit on different SMs when there are few
   const int run = runs < A.ctas * S::kWarps ? warp * A.ctas + (int)blockIdx.x : (int)blockIdx.x * S::kWarps + warp;
   if (run >= runs) return;
@@ -659,7 +662,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   const Seq sq = seq_of(A, b);
   const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps;
   const int64_t u1 = min(u0 + sq.steps, units);              // (never past them, unless the lengths have changed meanwhile)
-  const int runs = run_count(units, A.ctas * S::kWarps);
+  const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);
   int g0 = 0, g1 = -1;
   if (u0 < u1) {
     // the runs [units g / runs, units (g + 1) / runs) that meet [u0, u1)
@@ -711,13 +714,37 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   if (A.lse && lane == 0) A.lse[at] = lse_of(m, l);
 }
 
-// Row tiles of R rows (as few as kMaxNt eights allow, of about equal size), and the eights of each.
+// Row tiles of R rows, and the eights of each.
 struct RowTiles {
   int rt, nt;
 };
-inline RowTiles row_tiles(int64_t R) {
-  const int64_t rt = (R + 8 * kMaxNt - 1) / (8 * kMaxNt);
+// As few tiles as `most` eights allow, of about equal size.
+inline RowTiles row_tiles(int64_t R, int most) {
+  const int64_t rt = (R + 8 * most - 1) / (8 * most);
   return RowTiles{(int)rt, (int)((((R + rt - 1) / rt) + 7) / 8)};
+}
+// The tiles that are likely to take least, by what was measured for 1 to 5 eights (tenths of a microsecond): a
+// call's fixed part, which grows with the kernel's code and its partials, and a round of steps over all
+// warps.  Many eights read the cache less often, few start sooner: 36 rows (D = 128) over 3 x 24000 keys and 8
+// heads take 82 us in two tiles of 3 eights and 96 in one of 5, over 32 x 8000 keys 235 and 206; 45 rows over 31
+// keys 12 us in six tiles of 1 and 17 in two of 3.  `longest`: steps of the longest sequence that the page
+// table allows, since the lengths are on the device.
+inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, int warps) {
+  static const int fixed[kMaxNt] = {110, 130, 160, 200, 360};
+  static const int round[2][kMaxNt] = {{11, 13, 16, 17, 18}, {15, 19, 22, 26, 33}};
+  RowTiles best{0, 0};
+  int64_t least = INT64_MAX;
+  for (int most = kMaxNt; most >= 1; --most) {
+    const RowTiles t = row_tiles(R, most);
+    const int64_t items = heads * t.rt, steps = items * longest;
+    const bool whole = longest <= kMinSteps && steps <= (int64_t)kMinSteps * warps;      // an item a warp: no partials
+    const int64_t cost = fixed[t.nt - 1] - (whole ? 60 : 0) + steps * round[D == 128][t.nt - 1] / warps;
+    if (cost < least) {
+      least = cost;
+      best = t;
+    }
+  }
+  return best;
 }
 
 template <int kD, int kNt>

@@ -13,7 +13,10 @@
 
 namespace sdv {
 
-constexpr int kGroups = 32;            // groups of threads whose maxima give the alternatives' threshold
+// Groups of threads whose maxima give the alternatives' threshold, the k-th largest of them: 32, or twice as
+// many where k is near 32, the least of 32 maxima being a low one (32 alternatives of 26 x 128050 fp32:
+// 36 us with 32 groups).
+constexpr int kGroups = 32, kManyGroups = 64, kManyFrom = 25;
 constexpr int kCandMax = 512;          // candidates a CTA ranks; more: k passes over its part
 
 struct ScoreArgs {
@@ -118,7 +121,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   const int tid = threadIdx.x;
   __shared__ Stat stats[kScoreMaxCluster * kWarps];           // the leader's: every warp's
   __shared__ int listed[kScoreMaxCluster];
-  __shared__ __align__(16) float gmax[kGroups];
+  __shared__ __align__(16) float gmax[kManyGroups];
   __shared__ int ncand, nhot;
   __shared__ int hot[kTop ? kCandMax : 1];
   __shared__ Cand cand[kTop ? kCandMax : 1];
@@ -136,10 +139,11 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   const float tm = run.top;                   // the largest of this thread's logits
   Stat a = run_warp(run, A.c);
   if constexpr (kTop) {
-    float g = tm;                             // a group's: of kScoreThreads / kGroups threads
-#pragma unroll
-    for (int o = 1; o < kScoreThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-    if (tid % (kScoreThreads / kGroups) == 0) gmax[tid / (kScoreThreads / kGroups)] = g;
+    float g = tm;                             // a group's
+    const int of = kScoreThreads / (A.top_k < kManyFrom ? kGroups : kManyGroups);
+#pragma unroll 1
+    for (int o = 1; o < of; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if ((tid & (of - 1)) == 0) gmax[tid / of] = g;
     if (tid == 0) ncand = nhot = 0;
     __syncthreads();
   }
@@ -147,14 +151,19 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_scores(const ScoreArgs A) 
   if ((tid & 31) == 0) (C > 1 ? cl.map_shared_rank(stats, 0) : stats)[rank * kWarps + tid / 32] = a;
   if constexpr (kTop) {
     // At least k of the part's logits are at or above the k-th largest of the groups' maxima.
-    const float mine_max = gmax[tid & 31];
-    int above = 0;
-#pragma unroll
-    for (int j = 0; j < kGroups; j += 4) {
-      const float4 o = *reinterpret_cast<const float4*>(gmax + j);
-      above += (o.x > mine_max) + (o.y > mine_max) + (o.z > mine_max) + (o.w > mine_max);
+    float thr = INFINITY;
+    const int groups = A.top_k < kManyFrom ? kGroups : kManyGroups;
+#pragma unroll 1
+    for (int i = tid & 31; i < groups; i += 32) {
+      const float mine_max = gmax[i];
+      int above = 0;
+#pragma unroll 8
+      for (int j = 0; j < groups; j += 4) {
+        const float4 o = *reinterpret_cast<const float4*>(gmax + j);
+        above += (o.x > mine_max) + (o.y > mine_max) + (o.z > mine_max) + (o.w > mine_max);
+      }
+      if (above < A.top_k) thr = fminf(thr, mine_max);
     }
-    float thr = above < A.top_k ? mine_max : INFINITY;
 #pragma unroll
     for (int o = 16; o; o >>= 1) thr = fminf(thr, __shfl_xor_sync(0xffffffffu, thr, o));
     auto keep = [&](float x, int i) {

@@ -58,7 +58,7 @@ struct Racer {
   int i;
 };
 
-// A row's softmax as e^{(x - m)/T} / s: m and log2 s.  mass: 1, or 0 for a row that has none.
+// A row's softmax as e^{(x - m)/T} / s: m and log2 s.
 struct RowStat {
   float m, l2;
 };
