@@ -538,8 +538,7 @@ size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
  * a query sees makes its row NaN; what it does not see has no effect.  Tokens of a page
  * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL), and a
  * length beyond the page table counts as its end.  Probabilities (together with their
- * values' scale) are rounded to fp16, 11 bits, before they meet the values where the output is bf16,
- * and to the sum of two fp16, 22 bits, where it is fp16; bf16 queries go through fp16
+ * values' scale) are rounded to the sum of two fp16, 22 bits, before they meet the values; bf16 queries go through fp16
  * with a common power of two (exact above 2^-36 of a key head's largest); codes are exact and
  * sums fp32.  The lengths of the batch decide where a sequence's keys are split, and so
  * the order of its sums.

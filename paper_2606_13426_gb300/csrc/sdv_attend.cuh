@@ -225,10 +225,10 @@ __device__ __forceinline__ uint4 q_load8(const AttendArgs& A, int64_t at) {
 // scheduler waiting on their own instructions where there are 36 (32 windows of 9 tokens, 4 query heads a
 // head, up to 16000 keys: 210 us, 2.8 TB/s and 0.2 PFLOP/s); the matrix instructions alone, 8 cycles each
 // a scheduler, need 1280 cycles a step there, HBM's pace 1400.
-// kFine: the probabilities go into the second product as a sum of two f16, 22 bits.  For f16 outputs: with one f16
-// their errors were as large as the output's own rounding (2.9e-4 of it in all, 2.0e-4 with two; with 8 bits in
-// the output it does not show).  5 % of the time with 4 to 8 rows, 17 % with 36.
-template <int kD, int kNt, bool kFine>
+// The probabilities go into the second product as a sum of two f16, 22 bits: with one, f16 outputs were off by as much
+// as their own rounding again (2.9e-4 of their size, 2.0e-4 with two), and bf16 outputs were roundings of numbers
+// up to 2^-12 off, so that some fell on the neighbouring value.
+template <int kD, int kNt>
 __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
   constexpr int kKv = S::kKv;
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       const float pw = fmaxf(fabsf(vs) * winv, 0x1p-80f), ipw = __frcp_rn(pw), lw = __log2f(pw);
       const uint32_t sign = vs < 0.f ? 0x80008000u : 0u;
       uint32_t pb[2][kNt][2];                               // probabilities, transposed
-      uint32_t pl[2][kFine ? kNt : 1][2];                   // what f16 leaves of them
+      uint32_t pl[2][kNt][2];                               // what f16 leaves of them
 #pragma unroll
       for (int k = 0; k < kNt; ++k) {
         const float m0 = lw - mx[2 * k], m1 = lw - mx[2 * k + 1];
@@ -563,10 +563,8 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
             s1 += e1;
             const uint32_t high = pack_half(e0, e1);
             pb[s][k][e] = transpose8(high ^ sign);
-            if constexpr (kFine) {
-              const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&high));
-              pl[s][k][e] = transpose8(pack_half(e0 - held.x, e1 - held.y) ^ sign);
-            }
+            const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&high));
+            pl[s][k][e] = transpose8(pack_half(e0 - held.x, e1 - held.y) ^ sign);
           }
         sum[2 * k] = fmaf(s0, ipw, sum[2 * k]);
         sum[2 * k + 1] = fmaf(s1, ipw, sum[2 * k + 1]);
@@ -592,7 +590,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
 #pragma unroll
           for (int k = 0; k < kNt; ++k) {
             mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
-            if constexpr (kFine) mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
+            mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
           }
         }
       }
@@ -750,7 +748,7 @@ inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, i
 template <int kD, int kNt>
 static cudaError_t launch_attend(const AttendArgs& A, cudaStream_t s) {
   using S = AttendShape<kD, kNt>;
-  const auto attend = A.bf16 ? k_attend<kD, kNt, false> : k_attend<kD, kNt, true>;
+  const auto attend = k_attend<kD, kNt>;
   cudaError_t e = cudaFuncSetAttribute(attend, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
   attend<<<(unsigned)A.ctas, S::kThreads, S::kSmem, s>>>(A);
