@@ -378,6 +378,14 @@ def _outs(out, names, n, dtype, dev):
     return {k: _out(out, k, (n,), dtype, dev) for k in names}
 
 
+def _workspace(t, need, dev):
+    """A workspace of `need` bytes: the caller's (whose size the entry point checks), or a new one."""
+    if t is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    _need_cuda(t)
+    return t
+
+
 _verify_workspace = functools.lru_cache(maxsize=None)(B.sdv_token_verify_workspace_bytes)
 _attend_workspace = functools.lru_cache(maxsize=None)(B.sdv_attend_workspace_bytes)
 
@@ -486,8 +494,7 @@ def token_verify(target_logits, draft_logits, tokens, seed=0, mode="block", *, L
     _dense("race", race, f32, (Bn, V))
     r = _outs(out, ("accepted_len", "next_token", "status") if with_status else ("accepted_len", "next_token"), Bn, i32, dev)
     r["log_ratio"] = _out(out, "log_ratio", (Bn, L), f32, dev)
-    if workspace is None:
-        workspace = torch.empty(_verify_workspace(Bn, L), dtype=torch.uint8, device=dev)
+    workspace = _workspace(workspace, _verify_workspace(Bn, L), dev)
     B._call("sdv_token_verify", target_logits.data_ptr(), target_logits.stride(0), _row_stride(target_logits),
             draft_logits.data_ptr(), draft_logits.stride(0), _row_stride(draft_logits), tokens.data_ptr(), Bn, L, V, dt,
             float(temperature), float(temperature if draft_temperature is None else draft_temperature), _MODES[mode],
@@ -528,7 +535,7 @@ def cache_append(cache, k_new, v_new, page_table, lengths, *, counts=None, statu
     P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
     dt = _rows("k_new", k_new, 4)
     W = k_new.shape[1]
-    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or v_new.stride() != k_new.stride():
+    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or v_new.stride() != k_new.stride() or not v_new.is_cuda:
         raise ValueError("k_new and v_new: [B, W, heads, dim] of one type and layout expected")
     _dense("status", status, torch.int32, (Bn,))
     B._call("sdv_cache_append", k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), k_new.stride(2), dt, Bn, W, H,
@@ -548,8 +555,7 @@ def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span
     _dense("status", status, torch.int32, (Bn,))
     dev = q.device
     r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
-    if workspace is None:
-        workspace = torch.empty(max(_attend_workspace(Bn, W, Hq, H, D), 256), dtype=torch.uint8, device=dev)
+    workspace = _workspace(workspace, _attend_workspace(Bn, W, Hq, H, D), dev)
     B._call("sdv_cache_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
             cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
             page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),

@@ -1012,3 +1012,37 @@ def test_gradients_of_a_few_whole_sizes(api, dtype):
         o = plain_scores(x, tok, 1.0, 0)
         assert grad_ok(t["d_logits"], x, tok, o, gl, gh, 1.0)
         assert near(t["logprob"], o["logprob"], 1e-5) and near(t["entropy"], o["entropy"], 2e-5)
+
+
+def test_host_tensors_are_refused_wherever_a_kernel_would_read_them(api):
+    g = gen(34)
+    cache = api.make_token_cache(4, 2, 16, 64)
+    pt = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    n = torch.full((1,), 2, dtype=torch.int32, device="cuda")
+    x = torch.randn(1, 2, 2, 64, generator=g, device="cuda")
+    for kv in ((x, x.cpu()), (x.cpu(), x), (x.cpu(), x.cpu())):
+        with pytest.raises(ValueError):
+            api.cache_append(cache, *kv, pt, n)
+    host = torch.zeros(1 << 22, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        api.cache_attend(x.to(BF16), cache, pt, n, workspace=host)
+    with pytest.raises(ValueError):
+        api.cache_attend(x.to(BF16), cache, pt, n, workspace=host.cuda()[::2])
+    tl, dl, tok, coins, race = make_verify(g, 2, 3, 50, F32)
+    with pytest.raises(ValueError):
+        api.token_verify(tl, dl, tok, workspace=host)
+    for kw in (dict(coins=coins.cpu()), dict(race=race.cpu()), dict(L_eff=torch.ones(2, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            api.token_verify(tl, dl, tok, **kw)
+    with pytest.raises(ValueError):
+        api.token_verify(tl, dl.cpu(), tok)
+    with pytest.raises(ValueError):
+        api.token_verify(tl, dl, tok.cpu())
+    for name in cache:
+        with pytest.raises(ValueError):
+            api.cache_attend(x.to(BF16), dict(cache, **{name: cache[name].cpu()}), pt, n)
+    one = torch.ones(2, device="cuda")
+    with pytest.raises(ValueError):
+        api.token_scores_train(tl[:, 0], None, None, one, d_logits=tl[:, 0].cpu())
+    with pytest.raises(ValueError):
+        api.token_scores(tl[:, 0], out=dict(entropy=torch.zeros(2)))
