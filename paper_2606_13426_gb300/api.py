@@ -529,13 +529,21 @@ def _cache_args(cache, page_table, lengths, counts):
     return P, H, block, D, Bn, M
 
 
+def _same_layout(a, b):
+    """One shape, and one stride along every axis of more than one place."""
+    if a.shape != b.shape:
+        return False
+    s, t = a.stride(), b.stride()
+    return s == t or all(x == y or n == 1 for n, x, y in zip(a.shape, s, t))
+
+
 def cache_append(cache, k_new, v_new, page_table, lengths, *, counts=None, status=None):
     """Appends k_new, v_new [B, W, H, D] behind the lengths [B] tokens that the cache holds of each
     sequence (sdv_cache_append); status [B] int32 gets bits added to it."""
     P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
     dt = _rows("k_new", k_new, 4)
     W = k_new.shape[1]
-    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or v_new.stride() != k_new.stride() or not v_new.is_cuda:
+    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.dtype != k_new.dtype or not v_new.is_cuda or not _same_layout(k_new, v_new):
         raise ValueError("k_new and v_new: [B, W, heads, dim] of one type and layout expected")
     _dense("status", status, torch.int32, (Bn,))
     B._call("sdv_cache_append", k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), k_new.stride(2), dt, Bn, W, H,

@@ -1046,3 +1046,25 @@ def test_host_tensors_are_refused_wherever_a_kernel_would_read_them(api):
         api.token_scores_train(tl[:, 0], None, None, one, d_logits=tl[:, 0].cpu())
     with pytest.raises(ValueError):
         api.token_scores(tl[:, 0], out=dict(entropy=torch.zeros(2)))
+
+
+@pytest.mark.parametrize("B,W,H", [(1, 1, 1), (1, 3, 2), (2, 1, 2), (3, 4, 1), (1, 1, 2)])
+def test_append_takes_any_stride_of_an_axis_of_one_place(api, B, W, H):
+    """Keys and values whose strides differ only where there is one sequence, one token or one head."""
+    g = gen(33)
+    caches = [api.make_token_cache(2 * B, H, 16, 64) for _ in range(2)]
+    pages = torch.arange(2 * B, device="cuda", dtype=torch.int32).view(B, 2)
+    n = torch.arange(B, device="cuda", dtype=torch.int32) * 7 + 5
+    x, y = (torch.randn(B, W, H, 64, generator=g, device="cuda") for _ in range(2))
+    api.cache_append(caches[0], x, y, pages, n)
+    sizes, strides = list(y.shape), list(y.stride())
+    for i in range(3):
+        if sizes[i] == 1:
+            strides[i] = 12345
+    z = y.as_strided(sizes, strides)
+    assert torch.equal(z, y) and z.stride() != y.stride()
+    api.cache_append(caches[1], x, z, pages, n)
+    assert all(torch.equal(caches[0][k].view(torch.uint8), caches[1][k].view(torch.uint8)) for k in caches[0])
+    for other in [y[..., :32]] + ([torch.zeros(B, W, H, 72, device="cuda")[..., :64]] if B * W * H > 1 else []):
+        with pytest.raises(ValueError):
+            api.cache_append(caches[0], x, other, pages, n)
