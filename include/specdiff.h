@@ -537,8 +537,9 @@ size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
  * Queries i >= counts[b], or with nothing to see, get 0 and -inf.  A NaN code in a key or value that
  * a query sees makes its row NaN; what it does not see has no effect.  Tokens of a page
  * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL), and a
- * length beyond the page table counts as its end.  Probabilities (together with their
- * values' scale) are rounded to the sum of two fp16, 22 bits, before they meet the values; bf16 queries go through fp16
+ * length beyond the page table counts as its end.  Probabilities times their
+ * values' scale are rounded to the sum of two fp16 before they meet the values: to 22 bits, or 2^-32 of
+ * the row's largest; bf16 queries go through fp16
  * with a common power of two (exact above 2^-36 of a key head's largest); codes are exact and
  * sums fp32.  The lengths of the batch decide where a sequence's keys are split, and so
  * the order of its sums.

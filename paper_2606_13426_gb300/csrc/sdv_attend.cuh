@@ -19,9 +19,14 @@
 //   * a thread's sixteen contiguous elements of a key are its share of four steps of the first
 //     product (the queries' fragments follow the same order of elements);
 //   * an 8 x 8 tile of probabilities is transposed on its way to the second product (movmatrix).
-// The reference that a row's exponentials are taken against moves only when a score passes it by
-// 2^kSlack (probabilities are held in f16 below that), so that most tiles need no exchange
-// between lanes and no rescaling of the output.
+//
+// A row's exponentials are taken against a reference of its own, on score + log2(vs / U): what they are
+// multiplied by with the values, p' = 2^(s + log2(vs / U) - m) kPScale, has to fit f16, and a row whose weight
+// lies on pages of small values must keep its bits whatever the other pages hold.  The sum's terms 2^(s - m) are
+// p' U / vs.  The unit U is a power of two near an item's first scale; from where a scale that rows see is far
+// from it, or 0, the sums of the rest of the item are kept apart, against references on the score alone ("wide").
+// m moves only when a score passes it by 2^kSlack, so that most steps need no exchange between lanes and
+// no rescaling of the output.
 #pragma once
 
 #include "sdv_cache.cuh"
@@ -35,9 +40,13 @@ constexpr int kMinSteps = 2;              // of a run, where there are fewer ste
 constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
-// The values' scale that the others are taken relative to, 4 times it and kPScale over that, stay finite.
-constexpr float kLeastVs = 0x1p-118f, kMostVs = 0x1.fp125f;
-constexpr float kPScale = 128.f;          // f16 holds 2^kSlack * kPScale; what is below 2^-28 of the reference is lost
+constexpr float kPScale = 128.f, kLogPScale = 7.f;   // f16 holds 2^kSlack kPScale; its least step is 2^-31 of a row's largest
+constexpr int kLeastUnit = -119, kMostUnit = 126;    // kPScale over the unit, and the unit over kPScale, are normal numbers
+constexpr float kLeastPw = 0x1p-33f, kMostPw = 0x1p48f;   // kPScale vs / U where the sums are kept with p'
+
+__device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(n + 127) << 23); }     // n from -126 to 127
+// floor(log2 x) of x > 0 (-127 for what is below the normal numbers).
+__device__ __forceinline__ int log2_of(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }
 
 // Division by the chunks of a page (up to 8) of numbers below 2^28: a product's upper half.
 struct ChunkDiv {
@@ -205,7 +214,8 @@ struct AttendShape {
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
   static constexpr int kQBytes = kRows * kD * 2;
   static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
-  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes;
+  static constexpr int kRefBytes = kRows * 4;
+  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRefBytes;
   static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
   static_assert(kHalves % 2 == 1 && kSmem <= 227 * 1024, "");
 };
@@ -240,6 +250,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   uint8_t* ring = smem + warp * S::kWarpBytes;
   uint4* qf = reinterpret_cast<uint4*>(ring + S::kHalves * S::kHalf);
   float* scales = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes);
+  float* refs = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes);   // the sums', where they are kept apart
 
   const int64_t units = step_sums(A, 0, lane).total * per;
   const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);   // none of them empty
@@ -336,6 +347,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
     };
     look(0);
+    const float first_vs = np0 >= 0 ? fabsf(A.c.vs[(int64_t)np0 * H + h]) : 0.f;
 #pragma unroll
     for (int n = 0; n < S::kAhead; ++n) {
       if (n < steps) {
@@ -390,13 +402,17 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
       __syncwarp();
     }
+    // log2 of U, and kPScale / U
+    const int unit = first_vs > 0.f && first_vs < INFINITY ? min(max(log2_of(first_vs), kLeastUnit), kMostUnit) : 0;
+    const float winv = pow2(7 - unit);
     // the window's rows of this item: the last key that all of them see, the first that one does not
     const int at0 = sq.len - sq.count;                     // position of the window's first query
     const int i0 = row0 / A.G, i1 = min((min(row0 + S::kRows, A.R) - 1) / A.G, sq.count - 1);
     const int min_last = at0 + i0, max_begin = A.span > 0 ? at0 + i1 - A.span + 1 : 0;
+    const int max_last = at0 + i1, min_begin = A.span > 0 ? at0 + i0 - A.span + 1 : 0;   // and what any of them sees
     float acc[kMt][kNt][4];
-    float mx[kR], sum[kR];
-    float vref = 0.f, winv = 0.f;
+    float mx[kR], sum[kR];                                 // (mx: of p', so kLogPScale below the largest)
+    bool wide = false;
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
@@ -458,9 +474,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       float f = (chunk ? s4.z : s4.x) * rsc;                 // what a raw score is to be multiplied by
       float vs = chunk ? s4.w : s4.y;
       const int absent = __float_as_int(sc[4]);
-      float va = max_nan(fabsf(s4.y), fabsf(s4.w));
-      const bool odd_scale = !(va < INFINITY);
-      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || odd_scale;
+      float lw = __log2f(fabsf(vs) * winv), ipw = ex2(-lw);    // of kPScale vs / U; what takes a sum of p' to one of 2^(s - m)
+      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || wide ||
+                          !(max_nan(fabsf(s4.y), fabsf(s4.w)) * winv <= kMostPw && fminf(fabsf(s4.y), fabsf(s4.w)) * winv >= kLeastPw);
       if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
         const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
 #pragma unroll
@@ -475,6 +491,27 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
       if (masked) {
+        // magnitudes of the value scales, of chunks that some row sees (-1: none does; 0: a scale that is none)
+        const auto seen = [&](int key, float va, int out) {
+          return absent & out || key > max_last || key + kChunk <= min_begin ? -1.f : va < INFINITY ? va : 0.f;
+        };
+        const float va0 = seen(key0, fabsf(s4.y), 1), va1 = seen(key0 + kChunk, fabsf(s4.w), 2), va = chunk ? va1 : va0;
+        const auto far = [&](float x) { return x >= 0.f && !(x * winv <= kMostPw && x * winv >= kLeastPw); };
+        if (!wide && (far(va0) || far(va1))) {
+          wide = true;
+          if (g == 0) {
+#pragma unroll
+            for (int k = 0; k < kR; ++k) refs[8 * (k >> 1) + 2 * t + (k & 1)] = mx[k];
+          }
+          __syncwarp();
+        }
+        if (wide) {
+          ipw = 0.f;
+          lw = va > 0.f ? __log2f(va) + __log2f(winv) : -INFINITY;
+        } else if (!(va >= 0.f)) {                         // (no row sees the chunk)
+          ipw = 1.f;
+          lw = 0.f;
+        }
         const int have = sq.len - key0 - 8 * t;
         drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
         uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
@@ -490,12 +527,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         nan_keys &= ~drop;
         drop |= nan_keys;
         nan_keys = __shfl_sync(0xffffffffu, nan_keys, g >> 1);   // of this thread's keys
-        if (odd_scale) {                                   // a scale that is none: as NaN codes
-          va = fmaxf(fabsf(s4.y) < INFINITY ? fabsf(s4.y) : 0.f, fabsf(s4.w) < INFINITY ? fabsf(s4.w) : 0.f);
-          if (!(fabsf(vs) < INFINITY)) {
-            nan_keys = 0xffu;
-            vs = 0.f;
-          }
+        if (!(fabsf(vs) < INFINITY)) {                     // a scale that is none: as NaN codes
+          nan_keys = 0xffu;
+          vs = 0.f;
         }
         const bool here = !(absent >> chunk & 1);
 #pragma unroll
@@ -512,41 +546,52 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
               else if (nan_keys >> tok & 1) x = NAN;
             }
         }
+        if (wide) {
+#pragma unroll
+          for (int k = 0; k < kR; ++k) {
+            float* at = refs + 8 * (k >> 1) + 2 * t + (k & 1);
+            float x = f * max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
+                                  max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+            const float was = *at, m = max_nan(was, x), c = ex2(was - m);
+            float add = 0.f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) add += ex2(fmaf(sx[s][k >> 1][2 * e + (k & 1)], f, -m));
+            sum[k] = fmaf(sum[k], c, add);
+            __syncwarp();
+            if (g == 0) *at = m;
+          }
+          __syncwarp();
+        }
       }
-      va = fminf(fmaxf(va, kLeastVs), kMostVs);
-      float top[kR];
-      bool move = va > vref;
+      float top[kR];                                         // of log2 p' + mx
+      bool move = false;
 #pragma unroll
       for (int k = 0; k < kR; ++k) {
-        top[k] = f * max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
-                             max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
-        move |= !(top[k] <= mx[k] + kSlack);
+        top[k] = fmaf(f, max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
+                                 max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)])), lw);
+        move |= !(top[k] <= mx[k] + (kSlack + kLogPScale));
       }
       if (__any_sync(0xffffffffu, move)) {
-        float vc = 1.f;
-        if (va > vref) {
-          vc = vref / (4.f * va);
-          vref = 4.f * va;
-          winv = kPScale / vref;
-        }
 #pragma unroll
         for (int k = 0; k < kR; ++k) {
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) top[k] = max_nan(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
-          const float m = top[k] <= mx[k] + kSlack ? mx[k] : max_nan(mx[k], top[k]);   // a row's own affair
+          // a row's own affair
+          const float m = top[k] <= mx[k] + (kSlack + kLogPScale) ? mx[k] : max_nan(mx[k], top[k] - kLogPScale);
           const float c = ex2(mx[k] - m);
           mx[k] = m;
-          sum[k] *= c;
+          if (!wide) sum[k] *= c;
 #pragma unroll
           for (int q = 0; q < kMt; ++q) {
-            acc[q][k >> 1][k & 1] *= c * vc;
-            acc[q][k >> 1][2 + (k & 1)] *= c * vc;
+            acc[q][k >> 1][k & 1] *= c;
+            acc[q][k >> 1][2 + (k & 1)] *= c;
           }
         }
       }
-      // The values' scale goes into the exponent, and out of the sums: p' = p pw, sum += (sum p') / pw.  A
-      // weight below 2^-80 (a scale of 0) leaves p' = 0 in f16, and the sums right.
-      const float pw = fmaxf(fabsf(vs) * winv, 0x1p-80f), ipw = __frcp_rn(pw), lw = __log2f(pw);
       const uint32_t sign = vs < 0.f ? 0x80008000u : 0u;
       uint32_t pb[2][kNt][2];                               // probabilities, transposed
       uint32_t pl[2][kNt][2];                               // what f16 leaves of them
@@ -599,35 +644,41 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       __syncwarp();
     }
     asm volatile("cp.async.wait_group 0;");
-    // the item's results, or a partial of them (its output in value units, unnormalised)
+    // the item's results, or a partial of them: its output, and 2^m l for the sum, 1 <= l < 2
     const bool whole = steps == sq.steps;
     float* part = A.part + ((int64_t)run * 2 + (first_segment ? 0 : 1)) * S::kSlot;
-    const float unit = vref * (1.f / kPScale);
+    const float by_unit = 1.f / winv;
+    __syncwarp();
 #pragma unroll
     for (int k = 0; k < kR; ++k) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
       const int r = 8 * (k >> 1) + 2 * t + (k & 1), row = row0 + r;
       if (row >= A.R) continue;
+      // the sum's reference; what the output's differs by, in two steps, either of which fp32 holds
+      const float ref = wide ? refs[r] : mx[k], half_up = wide ? ex2(.5f * (mx[k] - ref)) : 1.f, up = half_up * by_unit;
       if (whole) {
         const int i = row / A.G;
         const float l = i < sq.count ? sum[k] : 0.f;         // a row past the sequence's window gets zeros
-        const float by = l == 0.f ? 0.f : unit / l;
+        const float by = l == 0.f ? 0.f : 1.f / l;
         const int64_t at = ((int64_t)b * A.W + i) * (H * A.G) + h * A.G + row - i * A.G;
 #pragma unroll
         for (int m = 0; m < kMt; ++m)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            put_out(A, at * kD + 16 * m + 8 * e + g, l == 0.f ? 0.f : acc[m][k >> 1][2 * e + (k & 1)] * by);
-        if (A.lse && g == 0) A.lse[at] = lse_of(mx[k], l);
+            put_out(A, at * kD + 16 * m + 8 * e + g, l == 0.f ? 0.f : acc[m][k >> 1][2 * e + (k & 1)] * by * half_up * up);
+        if (A.lse && g == 0) A.lse[at] = lse_of(ref, l);
       } else {
+        const float by = sum[k] == 0.f ? 0.f : 1.f / sum[k];
 #pragma unroll
         for (int m = 0; m < kMt; ++m)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) part[r * kD + 16 * m + 8 * e + g] = acc[m][k >> 1][2 * e + (k & 1)] * unit;
+          for (int e = 0; e < 2; ++e) part[r * kD + 16 * m + 8 * e + g] = acc[m][k >> 1][2 * e + (k & 1)] * by * half_up * up;
         if (g == 0) {
-          part[S::kRows * kD + r] = mx[k];
-          part[S::kRows * kD + S::kRows + r] = sum[k];
+          const bool some = sum[k] > 0.f && sum[k] < INFINITY;
+          const int e = some ? log2_of(sum[k]) : 0;
+          part[S::kRows * kD + r] = ref + (float)e;
+          part[S::kRows * kD + S::kRows + r] = some ? sum[k] * pow2(-e) : sum[k];
         }
       }
     }
@@ -685,8 +736,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
 #pragma unroll 4
   for (int gi = kSplit ? g0 + warp : g0; gi <= g1; gi += kSplit ? kJoinWarps : 1) {
     const float* slot = slot_of(gi);
-    const float c = ex2(slot[S::kRows * kD + r] - m);
-    l = fmaf(c, slot[S::kRows * kD + S::kRows + r], l);
+    const float c = ex2(slot[S::kRows * kD + r] - m) * slot[S::kRows * kD + S::kRows + r];
+    l += c;
 #pragma unroll
     for (int e = 0; e < kV; ++e) o[e] = fmaf(c, slot[r * kD + e * 32 + lane], o[e]);
   }

@@ -1,4 +1,6 @@
-"""The attention over the 8-bit cache, each output against the 64-bit form of its own row.
+"""The attention over the 8-bit cache where one row's result must not hang on what other rows see, hold
+or are scaled by: value scales far apart, pages behind the span, NaN codes, queries of very different
+size.  Every row is compared with the 64-bit form of itself.
 
 Tolerances: scores are within 2^-22 of the sum of their products' magnitudes and probabilities within
 2^-20 of themselves, so that an output is within 2^-14 sum p |v| (of its own row) and its rounding.
@@ -6,9 +8,26 @@ Tolerances: scores are within 2^-22 of the sum of their products' magnitudes and
 import pytest
 import torch
 
-from test_gpu_tokens import BF16, api, gen, make_cache, plain_attend  # noqa: F401
+from test_gpu_tokens import BF16, F16, api, gen, make_cache, near, plain_attend  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+HALF = {BF16: 2.0 ** -8, F16: 2.0 ** -11}
+
+
+def check_rows(api, q, cache, pages, lengths, counts=None, span=0, scale=None, **kw):
+    """As check_attend, with 2^-14 for 2^-11 and nothing absolute but the output's own least step."""
+    B, W, Hq, D = q.shape
+    r = api.cache_attend(q, cache, pages, lengths, counts=counts, span=span, scale=scale, **kw)
+    out, lse, mag = plain_attend(q, cache, pages, lengths, [W] * B if counts is None else counts, D ** -0.5 if scale is None else scale, span)
+    least = 2.0 ** -132 if q.dtype == BF16 else 2.0 ** -25
+    tol = 2.0 ** -14 * mag + 1.01 * HALF[q.dtype] * out.abs() + least
+    err = (r["out"].double() - out).abs()
+    assert (err <= tol).all(), "output off by %g of its bound" % float((err / tol).max())
+    assert near(r["lse"], lse, 2e-5)
+    return r
+
+
 
 
 # ------------------------------------------------------------------------------ roundings
@@ -27,3 +46,88 @@ def test_bf16_outputs_are_rounded_once(api, W, G, D, n):
         # (through fp32, whose rounding is 2^-24 of it)
         low, high = ((out - tol).float().to(BF16).double(), (out + tol).float().to(BF16).double())
         assert (low <= got).all() and (got <= high).all()
+
+
+# ------------------------------------------------------------------------------ value scales
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("k", [20, 27, 30, 40, 60, 100])
+def test_a_page_that_a_row_does_not_see_may_have_any_value_scale(api, k, dtype):
+    """17 tokens in pages of 16, two queries: the first sees one page, the second's page is 2^k larger."""
+    g = gen(80 + k)
+    cache = make_cache(api, g, 2, 1, 16, 64)
+    lift = 0 if dtype == BF16 else 8                    # (f16 outputs: the large page's values below 2^16)
+    cache["v_scale"][0] *= 2.0 ** -(k - lift)
+    cache["v_scale"][1] *= 2.0 ** lift
+    pages = torch.arange(2, device="cuda", dtype=torch.int32)[None]
+    n = torch.tensor([17], device="cuda", dtype=torch.int32)
+    q = torch.randn(1, 2, 2, 64, generator=g, device="cuda").to(dtype)
+    if dtype == F16 and k > 30:                         # values below f16's least step: nothing to compare
+        return
+    r = check_rows(api, q, cache, pages, n)
+    alone = api.cache_attend(q[:, :1], cache, pages, n - 1)
+    a, b = r["out"][:, :1].double(), alone["out"].double()
+    assert ((a - b).abs() <= 2 * HALF[dtype] * b.abs() + 2.0 ** -24 * (dtype == F16)).all() and near(r["lse"][:, :1], alone["lse"], 2e-5)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (BF16, 64), (F16, 64)])
+@pytest.mark.parametrize("k", [20, 30, 40, 80, 140])
+def test_rows_whose_weight_lies_on_pages_of_small_values(api, k, dtype, D):
+    """Sharp rows over pages whose value scales spread over 2^k, in runs of many steps and in sequences of a
+    few; heads whose scales only grow, only fall and are mixed."""
+    g = gen(90 + k + D)
+    B, H, G, W, block = 5, 4, 2, 3, 32
+    M = 640
+    cache = make_cache(api, g, B * M, H, block, D)
+    pages = torch.randperm(B * M, generator=g, device="cuda").to(torch.int32).view(B, M)
+    e = torch.rand(B, M, H, generator=g, device="cuda")
+    e[:, :, 0] = torch.linspace(0, 1, M, device="cuda")
+    e[:, :, 1] = torch.linspace(1, 0, M, device="cuda")
+    e[:, :, 2] = (e[:, :, 2] < 0.5).float()              # two sizes, side by side
+    e = torch.floor(k * (e - (1.0 if dtype == F16 else 0.5)))
+    cache["v_scale"][pages.long()] *= torch.exp2(e)
+    cache["v_scale"][pages[:, ::7].long(), 3] *= -1
+    cache["v_scale"][pages[:, 3::11].long(), 3] = 0
+    n = torch.tensor([M * block - 5, 20000, 13000, 400, 31], device="cuda", dtype=torch.int32)
+    for sharp in (1.0, 6.0, 20.0):
+        q = (sharp * torch.randn(B, W, H * G, D, generator=g, device="cuda")).to(dtype)
+        if dtype == F16:
+            cache_ = dict(cache, v_scale=cache["v_scale"] * 2.0 ** 8)
+            check_rows(api, q, cache_, pages, n)
+        else:
+            check_rows(api, q, cache, pages, n)
+
+
+def test_pages_of_zeros_and_of_huge_values_beside_ordinary_ones(api):
+    """Pages of zeros as they are appended (scale 2^-126) first, and a last page that only the later queries see, near
+    fp32's end: the earlier queries' results are those without it."""
+    g = gen(101)
+    H, D, block = 2, 64, 16
+    cache = api.make_token_cache(64, H, block, D)
+    pages = torch.randperm(64, generator=g, device="cuda").to(torch.int32).view(1, 64)
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x = torch.randn(1, 900, H, D, generator=g, device="cuda")
+    x[:, :100] = 0
+    x[:, 300:340] = 0
+    api.cache_append(cache, x, x, pages, none)
+    q = (2 * torch.randn(1, 6, 4, D, generator=g, device="cuda")).to(BF16)
+    n = none + 900
+    check_rows(api, q, cache, pages, n)
+    for huge in (1e20, 1e30, 3e38):
+        y = torch.full((1, 3, H, D), huge, device="cuda")
+        c = {k: v.clone() for k, v in cache.items()}
+        last = torch.randn(1, 9, H, D, generator=g, device="cuda")       # up to a page's end: 909 = 56 * 16 + 13
+        c2 = {k: v.clone() for k, v in c.items()}
+        api.cache_append(c, last, last, pages, n)
+        api.cache_append(c2, last, last, pages, n)
+        api.cache_append(c, last[:, :3], last[:, :3], pages, n + 9)      # to 912
+        api.cache_append(c2, last[:, :3], last[:, :3], pages, n + 9)
+        api.cache_append(c, last[:, :3], y, pages, n + 12)
+        api.cache_append(c2, last[:, :3], last[:, :3], pages, n + 12)
+        a = api.cache_attend(q, c, pages, n + 15)                        # queries at 909 .. 914: three see the page at 912
+        b = api.cache_attend(q, c2, pages, n + 15)
+        u, v = a["out"][:, :3].double(), b["out"][:, :3].double()
+        assert ((u - v).abs() <= 2 * HALF[BF16] * v.abs() + 2.0 ** -16).all(), huge
+        assert near(a["lse"][:, :3], b["lse"][:, :3].double(), 2e-5)
+        out, _, mag = plain_attend(q, c, pages, n + 15, [6], D ** -0.5, 0)
+        live = mag < 3e38
+        assert ((a["out"].double() - out).abs() <= 2.0 ** -14 * mag + 1.01 * 2.0 ** -8 * out.abs())[live].all()
