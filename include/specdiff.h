@@ -535,7 +535,8 @@ size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
  * q is [B, W, Hq, D] (BF16 or F16) with the strides given; query heads h G .. h G + G - 1,
  * G = Hq / H, read key head h.  out [B, W, Hq, D] (`dtype`), lse [B, W, Hq] fp32 or NULL, dense.
  * Queries i >= counts[b], or with nothing to see, get 0 and -inf.  A NaN code in a key or value that
- * a query sees makes its row NaN; what it does not see has no effect.  Tokens of a page
+ * a query sees makes its row NaN; what it does not see has no effect, and pages that no query of the
+ * sequence sees a token of (before the span) may have any table entry.  Tokens of a page
  * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL), and a
  * length beyond the page table counts as its end.  Probabilities times their
  * values' scale are rounded to the sum of two fp16 before they meet the values: to 22 bits, or 2^-32 of

@@ -78,14 +78,15 @@ struct AttendArgs {
 // A sequence's tokens, new ones and steps.
 struct Seq {
   int len, count, first, steps;            // first: the first step that a query sees
+  int begin;                               // the first key that one sees
 };
 __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   Seq s;
   const int cap = A.c.max_pages * A.c.block;
   s.len = min(max(A.lengths[b], 0), cap);
   s.count = min(max(A.counts ? A.counts[b] : A.W, 0), A.W);
-  s.first = 0;
-  if (A.span > 0) s.first = max(0, s.len - s.count - A.span + 1) / kSub;
+  s.begin = A.span > 0 ? max(0, s.len - s.count - A.span + 1) : 0;
+  s.first = s.begin / kSub;
   s.steps = s.count && s.len ? (s.len + kSub - 1) / kSub - s.first : 0;
   return s;
 }
@@ -286,9 +287,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     const int steps = (int)min((int64_t)sq.steps, u_end - item_u) - step0;
     const int32_t* table = A.c.table + (int64_t)b * A.c.max_pages;
     auto key_of = [&](int n) { return (sq.first + step0 + n) * kSub; };
-    // the page of the chunk of 16 tokens from `key` on, or -1 where there is none
+    // the page of the chunk of 16 tokens from `key` on, or -1 where there is none or no query sees a token of it
     auto page_of = [&](int key) {
-      if (key >= sq.len) return -1;
+      if (key >= sq.len || key + kChunk <= sq.begin) return -1;
       const int p = table[A.cpb.over(key / kChunk)];
       if (p >= 0 && p < (int)A.c.pages) return p;
       if (A.status && lane == 0) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);

@@ -8,7 +8,7 @@ Tolerances: scores are within 2^-22 of the sum of their products' magnitudes and
 import pytest
 import torch
 
-from test_gpu_tokens import BF16, F16, api, gen, make_cache, near, plain_attend  # noqa: F401
+from test_gpu_tokens import BF16, F16, NAN, api, gen, make_cache, near, plain_attend  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +131,35 @@ def test_pages_of_zeros_and_of_huge_values_beside_ordinary_ones(api):
         out, _, mag = plain_attend(q, c, pages, n + 15, [6], D ** -0.5, 0)
         live = mag < 3e38
         assert ((a["out"].double() - out).abs() <= 2.0 ** -14 * mag + 1.01 * 2.0 ** -8 * out.abs())[live].all()
+
+
+# ------------------------------------------------------------------------------ pages behind the span
+@pytest.mark.parametrize("block,n,span", [(16, 100, 48), (48, 1150, 1000), (80, 570, 321), (16, 3010, 2000)])
+def test_pages_behind_the_span_are_not_looked_at(api, block, n, span):
+    """A page whose last token lies before every query's span: its table entry may be anything, and so may its scales."""
+    g = gen(110 + n)
+    M = n // block + 1
+    cache = make_cache(api, g, M + 1, 2, block, 64)
+    pages = torch.arange(M, device="cuda", dtype=torch.int32)[None].contiguous()
+    lengths = torch.tensor([n], device="cuda", dtype=torch.int32)
+    for W in (1, 3):
+        q = torch.randn(1, W, 4, 64, generator=g, device="cuda").to(BF16)
+        first = n - W - span + 1                         # the first key that is seen
+        assert first > block
+        gone = first // block                            # pages wholly before it
+        ref = check_rows(api, q, cache, pages, lengths, span=span)
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        for entry in (-1, 1 << 30):
+            freed = pages.clone()
+            freed[0, :gone] = entry
+            r = api.cache_attend(q, cache, freed, lengths, span=span, status=st)
+            assert st.tolist() == [0]
+            assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"])
+        for size in (2.0 ** 100, NAN, 0.0, -1e30):       # another sequence has the page
+            c = {k: v.clone() for k, v in cache.items()}
+            c["v_scale"][M] = size
+            c["k_scale"][M] = size
+            lent = pages.clone()
+            lent[0, :gone] = M
+            r = api.cache_attend(q, c, lent, lengths, span=span)
+            assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"]), size
