@@ -652,6 +652,11 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < kR; ++k) {
+      // a NaN code of a value that all rows of a step see is in the output's element alone: the row is NaN
+      float any = 0.f;
+#pragma unroll
+      for (int m = 0; m < kMt; ++m) any = max_nan(any, max_nan(acc[m][k >> 1][k & 1], acc[m][k >> 1][2 + (k & 1)]));
+      if (any != any) sum[k] = NAN;
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
       const int r = 8 * (k >> 1) + 2 * t + (k & 1), row = row0 + r;

@@ -163,3 +163,34 @@ def test_pages_behind_the_span_are_not_looked_at(api, block, n, span):
             lent[0, :gone] = M
             r = api.cache_attend(q, c, lent, lengths, span=span)
             assert torch.equal(r["out"], ref["out"]) and torch.equal(r["lse"], ref["lse"]), size
+
+
+# ------------------------------------------------------------------------------ NaN codes
+@pytest.mark.parametrize("B,H,G,W,D,n", [(1, 1, 2, 1, 64, 5000), (2, 2, 4, 9, 128, 900), (40, 2, 1, 3, 64, 30), (3, 1, 5, 4, 64, 64),
+                                         (300, 4, 1, 2, 128, 700)])
+def test_a_nan_element_makes_the_rows_that_see_it_nan(api, B, H, G, W, D, n):
+    """One element of one key or value, in a step inside the sequence and in the last ones: all of the output and lse of
+    the rows that see it, nothing of the others."""
+    g = gen(120 + B + n)
+    block = 32
+    M = n // block + 1
+    cache = make_cache(api, g, B * M, H, block, D)
+    pages = torch.randperm(B * M, generator=g, device="cuda").to(torch.int32).view(B, M)
+    lengths = torch.full((B,), n, device="cuda", dtype=torch.int32)
+    q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(BF16)
+    ref = api.cache_attend(q, cache, pages, lengths)
+    b, h = B // 2, H - 1
+    for which in ("k", "v"):
+        for at in sorted({0, n // 3, n - W - 1, n - W, n - 1}):
+            d = (7 * at + 3) % D
+            codes = cache[which].view(torch.uint8)
+            page, row = int(pages[b, at // block]), at % block
+            where = (page, h, row, d) if which == "k" else (page, h, d, row)
+            was = int(codes[where])
+            codes[where] = 0x7f if at % 2 else 0xff
+            r = api.cache_attend(q, cache, pages, lengths)
+            codes[where] = was
+            sees = torch.zeros(B, W, H * G, dtype=torch.bool, device="cuda")
+            sees[b, max(0, at - (n - W)):, h * G:(h + 1) * G] = True
+            assert r["out"][sees].isnan().all() and r["lse"][sees].isnan().all(), (which, at)
+            assert torch.equal(r["out"][~sees], ref["out"][~sees]) and torch.equal(r["lse"][~sees], ref["lse"][~sees]), (which, at)
