@@ -25,7 +25,8 @@
 // lies on pages of small values must keep its bits whatever the other pages hold.  The sum's terms 2^(s - m) are
 // p' U / vs.  The unit U is a power of two near an item's first scale; from where a scale that rows see is far
 // from it, or 0, the sums of the rest of the item are kept apart, against references on the score alone ("wide").
-// m moves only when a score passes it by 2^kSlack, so that most steps need no exchange between lanes and
+// Scores in the millions, of which fp32 holds no fraction, are taken less a base of their row ("based"): an exact
+// difference.  m moves only when a score passes it by 2^kSlack, so that most steps need no exchange between lanes and
 // no rescaling of the output.
 #pragma once
 
@@ -41,6 +42,8 @@ constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
 constexpr float kPScale = 128.f, kLogPScale = 7.f;   // f16 holds 2^kSlack kPScale; its least step is 2^-31 of a row's largest
+constexpr float kMostScore = 0x1p22f;                 // a bound on the scores (as powers of 2) up to which there is no base
+constexpr float kBaseRoom = 64.f;                     // scores less their base stay below
 constexpr int kLeastUnit = -119, kMostUnit = 126;    // kPScale over the unit, and the unit over kPScale, are normal numbers
 constexpr float kLeastPw = 0x1p-33f, kMostPw = 0x1p48f;   // kPScale vs / U where the sums are kept with p'
 
@@ -197,7 +200,9 @@ __device__ __forceinline__ void put_out(const AttendArgs& A, int64_t at, float x
   if (A.bf16) reinterpret_cast<__nv_bfloat16*>(A.out)[at] = __float2bfloat16_rn(x);
   else reinterpret_cast<__half*>(A.out)[at] = __float2half_rn(x);
 }
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + log2f(l)) * kLn2f : (l == 0.f ? -INFINITY : NAN); }
+__device__ __forceinline__ float lse_of(float m, float l, float base) {
+  return l > 0.f ? (base + (m + log2f(l))) * kLn2f : (l == 0.f ? -INFINITY : NAN);
+}
 
 // A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others, 8 KB, under
 // way; its queries' fragments are beside it.  (Four under way at D = 128, where few rows leave room: 1
@@ -215,8 +220,8 @@ struct AttendShape {
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
   static constexpr int kQBytes = kRows * kD * 2;
   static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
-  static constexpr int kRefBytes = kRows * 4;
-  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRefBytes;
+  static constexpr int kRowBytes = kRows * 8;             // of a row: the sum's reference, the score's base
+  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRowBytes;
   static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
   static_assert(kHalves % 2 == 1 && kSmem <= 227 * 1024, "");
 };
@@ -229,6 +234,21 @@ __device__ __forceinline__ uint4 q_load8(const AttendArgs& A, int64_t at) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The largest finite magnitude of eight elements of a query.
+__device__ __forceinline__ float q_largest(uint4 v, bool bf16) {
+  v.x &= 0x7fff7fffu, v.y &= 0x7fff7fffu, v.z &= 0x7fff7fffu, v.w &= 0x7fff7fffu;
+  float m = bf16 ? vec_max_num<SDV_BF16>(v) : vec_max_num<SDV_F16>(v);
+  if (!(m < INFINITY)) {
+    float f[8];
+    if (bf16) Num<SDV_BF16>::unpack(v, f);
+    else Num<SDV_F16>::unpack(v, f);
+    m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = f[e] < INFINITY ? fmaxf(m, f[e]) : m;
+  }
+  return m;
 }
 
 // Bytes: every key and value once for each row tile, 2 D codes a token and head; operations: 4 D a row of those.  Bound
@@ -252,6 +272,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   uint4* qf = reinterpret_cast<uint4*>(ring + S::kHalves * S::kHalf);
   float* scales = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes);
   float* refs = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes);   // the sums', where they are kept apart
+  float* bases = refs + S::kRows;
 
   const int64_t units = step_sums(A, 0, lane).total * per;
   const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);   // none of them empty
@@ -361,11 +382,10 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       look(n + 1);
     }
     // the rows' queries as fragments, in f16: bf16 ones are scaled by a power of two into its range
-    float rsc = A.scale2;
+    float rsc = A.scale2, amax = 0.f;
     {
       constexpr int kN = S::kRows * kD / 8 / 32;            // eights of elements of a lane
       uint4 raw[kN];
-      float amax = 0.f;
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
         const int p = lane + 32 * j, row = row0 + p / (kD / 8), i = row / A.G;
@@ -373,16 +393,11 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         if (row < A.R && i < sq.count) raw[j] = q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
       }
       float up = 1.f;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) amax = fmaxf(amax, q_largest(raw[j], A.bf16));
+#pragma unroll
+      for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       if (A.bf16) {
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          float f[8];
-          Num<SDV_BF16>::unpack(raw[j], f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[e]) < INFINITY ? fabsf(f[e]) : 0.f);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         if (amax > 0.f) {
           const int k = min(max(139 - (int)(__float_as_uint(amax) >> 23), -100), 100);
           up = __uint_as_float((uint32_t)(127 + k) << 23);
@@ -403,6 +418,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
       __syncwarp();
     }
+    const float most_score = amax * (448.f * kD) * fabsf(A.scale2);   // times a key's scale
     // log2 of U, and kPScale / U
     const int unit = first_vs > 0.f && first_vs < INFINITY ? min(max(log2_of(first_vs), kLeastUnit), kMostUnit) : 0;
     const float winv = pow2(7 - unit);
@@ -413,7 +429,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     const int max_last = at0 + i1, min_begin = A.span > 0 ? at0 + i0 - A.span + 1 : 0;   // and what any of them sees
     float acc[kMt][kNt][4];
     float mx[kR], sum[kR];                                 // (mx: of p', so kLogPScale below the largest)
-    bool wide = false;
+    bool wide = false, based = false;
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
@@ -476,7 +492,8 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       float vs = chunk ? s4.w : s4.y;
       const int absent = __float_as_int(sc[4]);
       float lw = __log2f(fabsf(vs) * winv), ipw = ex2(-lw);    // of kPScale vs / U; what takes a sum of p' to one of 2^(s - m)
-      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || wide ||
+      const bool big = !(fmaxf(fabsf(s4.x), fabsf(s4.z)) * most_score <= kMostScore);
+      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || wide || based || big ||
                           !(max_nan(fabsf(s4.y), fabsf(s4.w)) * winv <= kMostPw && fminf(fabsf(s4.y), fabsf(s4.w)) * winv >= kLeastPw);
       if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
         const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
@@ -546,6 +563,41 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
               if (key > last || key < begin || !here) x = -INFINITY;
               else if (nan_keys >> tok & 1) x = NAN;
             }
+        }
+        if (based || big) {                                // from here on scores have bases, the sums' references to begin with
+#pragma unroll
+          for (int k = 0; k < kR; ++k) {
+            const int r = 8 * (k >> 1) + 2 * t + (k & 1);
+            const float ref = wide ? refs[r] : mx[k];       // (of the sum; without its base, if that is new)
+            const bool some = ref > kNone;
+            const float was = based ? bases[r] : 0.f, now = based || !some ? was : ref;
+            float top = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float& x = sx[s][k >> 1][2 * e + (k & 1)];
+                x = __fmul_rn(x, f);
+                top = max_nan(top, x);
+              }
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            // moved by what is far above it; by whatever is far from it, where the row has seen nothing
+            const float base = (some ? top - now : fabsf(top - now)) > kBaseRoom && fabsf(top) < INFINITY ? top : now;
+            if (mx[k] > kNone) mx[k] = fmaxf(mx[k] + (was - base), kNone);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) sx[s][k >> 1][2 * e + (k & 1)] -= base;
+            __syncwarp();
+            if (g == 0) {
+              bases[r] = base;
+              if (wide && some) refs[r] = fmaxf(ref + (was - base), kNone);
+            }
+          }
+          __syncwarp();
+          based = true;
+          f = 1.f;
         }
         if (wide) {
 #pragma unroll
@@ -663,6 +715,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       if (row >= A.R) continue;
       // the sum's reference; what the output's differs by, in two steps, either of which fp32 holds
       const float ref = wide ? refs[r] : mx[k], half_up = wide ? ex2(.5f * (mx[k] - ref)) : 1.f, up = half_up * by_unit;
+      const float base = based ? bases[r] : 0.f;
       if (whole) {
         const int i = row / A.G;
         const float l = i < sq.count ? sum[k] : 0.f;         // a row past the sequence's window gets zeros
@@ -673,7 +726,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
 #pragma unroll
           for (int e = 0; e < 2; ++e)
             put_out(A, at * kD + 16 * m + 8 * e + g, l == 0.f ? 0.f : acc[m][k >> 1][2 * e + (k & 1)] * by * half_up * up);
-        if (A.lse && g == 0) A.lse[at] = lse_of(ref, l);
+        if (A.lse && g == 0) A.lse[at] = lse_of(ref, l, base);
       } else {
         const float by = sum[k] == 0.f ? 0.f : 1.f / sum[k];
 #pragma unroll
@@ -683,8 +736,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         if (g == 0) {
           const bool some = sum[k] > 0.f && sum[k] < INFINITY;
           const int e = some ? log2_of(sum[k]) : 0;
-          part[S::kRows * kD + r] = ref + (float)e;
-          part[S::kRows * kD + S::kRows + r] = some ? sum[k] * pow2(-e) : sum[k];
+          // (with a base: that, exactly, since two partials may tie on it)
+          part[S::kRows * kD + r] = !based ? ref + (float)e : sum[k] == 0.f ? kNone : base;
+          part[S::kRows * kD + S::kRows + r] = based ? sum[k] * ex2(ref) : some ? sum[k] * pow2(-e) : sum[k];
         }
       }
     }
@@ -766,7 +820,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < kV; ++e) put_out(A, at * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
-  if (A.lse && lane == 0) A.lse[at] = lse_of(m, l);
+  if (A.lse && lane == 0) A.lse[at] = lse_of(0.f, l, m);
 }
 
 // Row tiles of R rows, and the eights of each.

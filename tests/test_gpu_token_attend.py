@@ -194,3 +194,46 @@ def test_a_nan_element_makes_the_rows_that_see_it_nan(api, B, H, G, W, D, n):
             sees[b, max(0, at - (n - W)):, h * G:(h + 1) * G] = True
             assert r["out"][sees].isnan().all() and r["lse"][sees].isnan().all(), (which, at)
             assert torch.equal(r["out"][~sees], ref["out"][~sees]) and torch.equal(r["lse"][~sees], ref["lse"][~sees]), (which, at)
+
+
+# ------------------------------------------------------------------------------ large scores
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,G,W,n", [(64, 2, 2, 300), (128, 4, 9, 1000), (64, 1, 1, 20)])
+@pytest.mark.parametrize("size", [2.0 ** 22, 2.0 ** 27, 2.0 ** 40, 2.0 ** 90])
+def test_scores_of_any_size(api, D, G, W, n, size, dtype):
+    """Scores up to 1e30, where one key stands out, where several are equal, far below 0, and beside
+    ordinary ones (the second key head's): queries along one axis, so that the products are exact."""
+    g = gen(130 + D)
+    H, block = 2, 16
+    M = n // block + 1
+    cache = make_cache(api, g, M, H, block, D)
+    codes = (20 * torch.randn(M, H, block, D, generator=g, device="cuda")).clamp(-200, 200)
+    codes[..., 0] = codes[..., 0].clamp(-20, 20)
+    codes[M // 3, :, 5, 0] = 448
+    codes[M // 2, :, 3, 0] = codes[M // 4, :, 9, 0] = -448
+    cache["k"].copy_(codes.to(torch.float8_e4m3fn))
+    cache["k_scale"].fill_(2.0 ** -4)
+    cache["k_scale"][M // 2 + 1:] = 2.0 ** -6
+    cache["v_scale"][::2] *= 2.0 ** 9
+    pages = torch.arange(M, device="cuda", dtype=torch.int32)[None]
+    lengths = torch.tensor([n], device="cuda", dtype=torch.int32)
+    q = torch.zeros(1, W, H * G, D, device="cuda")
+    q[..., 0] = 1.0
+    q[:, :, G:] = 0.25 * torch.randn(1, W, G, D, generator=g, device="cuda").to(BF16).float()
+    q[:, :, G:, 0] = 0
+    for sign in (1.0, -1.0):
+        z = q.clone()
+        z[:, :, :G] *= sign
+        z = z.to(dtype)
+        if dtype == BF16:
+            big = z.clone()
+            big[:, :, :G] *= size
+            check_rows(api, big, cache, pages, lengths)
+        c = dict(cache, k_scale=cache["k_scale"].clone())
+        c["k_scale"][:, 0] *= size
+        check_rows(api, z, c, pages, lengths)
+        if n > 100:                                       # the large ones after ordinary ones, and before
+            for part in (slice(0, M // 4), slice(M // 4, M)):
+                c = dict(cache, k_scale=cache["k_scale"].clone())
+                c["k_scale"][part, 0] *= size
+                check_rows(api, z, c, pages, lengths)
