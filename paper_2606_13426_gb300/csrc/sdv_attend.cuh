@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
       const uint8_t* from = ring + half * S::kHalf;
-      const uint8_t* values = ring + after(half, 1, S::kHalves) * S::kHalf;
+      uint8_t* values = ring + after(half, 1, S::kHalves) * S::kHalf;
       const float* sc = scales + slot * 8;
       const int key0 = key_of(n);
       // scores: sx[s][n][0, 1] of key row g and rows 2t, 2t + 1; [2, 3] of key row g + 8
@@ -505,7 +505,6 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
             for (int e = 0; e < 4; ++e) sx[s][k][e] *= by;
         f = f < 0.f ? -f : 1.f;
       }
-      uint32_t drop = 0;                                   // which of this thread's 8 value tokens count as 0
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
       if (masked) {
@@ -530,8 +529,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
           ipw = 1.f;
           lw = 0.f;
         }
+        // which of this thread's 8 value tokens count as 0
         const int have = sq.len - key0 - 8 * t;
-        drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
+        uint32_t drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
         uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
 #pragma unroll 1
         for (int m = 0; m < 2 * kMt; ++m) {
@@ -545,6 +545,19 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         nan_keys &= ~drop;
         drop |= nan_keys;
         nan_keys = __shfl_sync(0xffffffffu, nan_keys, g >> 1);   // of this thread's keys
+        if (drop) {                                        // in the ring: a thread reads what it alone has written here
+          uint2 keep = make_uint2(0u, 0u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            keep.x |= drop >> e & 1 ? 0u : 0xffu << (8 * e);
+            keep.y |= drop >> (e + 4) & 1 ? 0u : 0xffu << (8 * e);
+          }
+#pragma unroll 1
+          for (int m = 0; m < 2 * kMt; ++m) {
+            uint2* at = reinterpret_cast<uint2*>(values + (m * 32 + lane) * 8);
+            *at = make_uint2(at->x & keep.x, at->y & keep.y);
+          }
+        }
         if (!(fabsf(vs) < INFINITY)) {                     // a scale that is none: as NaN codes
           nan_keys = 0xffu;
           vs = 0.f;
@@ -669,27 +682,17 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
 #pragma unroll
       for (int m = 0; m < kMt; ++m) {
-        uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
-        uint2 w1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
-        if (drop) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (drop >> e & 1) {
-              const uint32_t keep = ~(0xffu << (8 * (e & 3)));
-              if (e < 4) w0.x &= keep, w1.x &= keep;
-              else w0.y &= keep, w1.y &= keep;
-            }
-        }
+        const uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
+        const uint2 w1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           uint32_t a[4];
           widen4(s ? w0.y : w0.x, a[0], a[2]);
           widen4(s ? w1.y : w1.x, a[1], a[3]);
 #pragma unroll
-          for (int k = 0; k < kNt; ++k) {
-            mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
-            mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
-          }
+          for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
+#pragma unroll
+          for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
         }
       }
       half = after(half, 2, S::kHalves);
