@@ -42,6 +42,8 @@ constexpr int kMaxNt = 5;                 // eights of rows of an item
 constexpr float kNone = -3e38f;           // the reference of a row that has seen nothing
 constexpr float kSlack = 8.f;
 constexpr float kPScale = 128.f, kLogPScale = 7.f;   // f16 holds 2^kSlack kPScale; its least step is 2^-31 of a row's largest
+// What few items need: a power of two per query, sums kept apart, scores less a base (see above and k_attend).
+constexpr int kUneven = 1, kWide = 2, kBased = 4;
 constexpr float kMostScore = 0x1p22f;                 // a bound on the scores (as powers of 2) up to which there is no base
 constexpr float kBaseRoom = 64.f;                     // scores less their base stay below
 constexpr int kLeastUnit = -119, kMostUnit = 126;    // kPScale over the unit, and the unit over kPScale, are normal numbers
@@ -220,7 +222,7 @@ struct AttendShape {
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
   static constexpr int kQBytes = kRows * kD * 2;
   static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
-  static constexpr int kRowBytes = kRows * 8;             // of a row: the sum's reference, the score's base
+  static constexpr int kRowBytes = kRows * 12;            // of a row: the sum's reference, the score's base, the query's power of two
   static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRowBytes;
   static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
   static_assert(kHalves % 2 == 1 && kSmem <= 227 * 1024, "");
@@ -273,6 +275,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   float* scales = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes);
   float* refs = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes);   // the sums', where they are kept apart
   float* bases = refs + S::kRows;
+  float* downs = bases + S::kRows;
 
   const int64_t units = step_sums(A, 0, lane).total * per;
   const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);   // none of them empty
@@ -381,40 +384,61 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       }
       look(n + 1);
     }
-    // the rows' queries as fragments, in f16: bf16 ones are scaled by a power of two into its range
+    // The rows' queries as fragments, in f16: bf16 ones are scaled into its range by a power of two, one for all rows
+    // where every eight elements' largest is within 2^-8 of the largest of all, else ("uneven") one a row, whose scores are
+    // brought to the common one again.  So an element is within 2^-32 of its row's largest, whatever the other rows hold.
     float rsc = A.scale2, amax = 0.f;
+    int modes = 0;                                         // what the steps of this item take care of
     {
       constexpr int kN = S::kRows * kD / 8 / 32;            // eights of elements of a lane
-      uint4 raw[kN];
-#pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const int p = lane + 32 * j, row = row0 + p / (kD / 8), i = row / A.G;
-        raw[j] = make_uint4(0, 0, 0, 0);
-        if (row < A.R && i < sq.count) raw[j] = q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
-      }
-      float up = 1.f;
-#pragma unroll
-      for (int j = 0; j < kN; ++j) amax = fmaxf(amax, q_largest(raw[j], A.bf16));
-#pragma unroll
-      for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      if (A.bf16) {
-        if (amax > 0.f) {
-          const int k = min(max(139 - (int)(__float_as_uint(amax) >> 23), -100), 100);
-          up = __uint_as_float((uint32_t)(127 + k) << 23);
-          rsc *= __uint_as_float((uint32_t)(127 - k) << 23);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const int p = lane + 32 * j, r = p / (kD / 8), e8 = p % (kD / 8);
+      const auto load = [&](int p) {
+        const int row = row0 + p / (kD / 8), i = row / A.G;
+        if (row >= A.R || i >= sq.count) return make_uint4(0, 0, 0, 0);
+        return q_load8(A, b * A.q_sb + i * A.q_st + (int64_t)(h * A.G + row - i * A.G) * A.q_sh + p % (kD / 8) * 8);
+      };
+      const auto put = [&](int p, uint4 v, int up) {
+        const int r = p / (kD / 8), e8 = p % (kD / 8);
         if (A.bf16) {
           float f[8];
-          Num<SDV_BF16>::unpack(raw[j], f);
+          Num<SDV_BF16>::unpack(v, f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= up;
-          raw[j] = Num<SDV_F16>::pack(f);
+          for (int e = 0; e < 8; ++e) f[e] *= pow2(up);
+          v = Num<SDV_F16>::pack(f);
         }
-        qf[(((r >> 3) * kKv + (e8 >> 3)) * 2 + (e8 & 1)) * 32 + (r & 7) * 4 + (e8 >> 1 & 3)] = raw[j];
+        qf[(((r >> 3) * kKv + (e8 >> 3)) * 2 + (e8 & 1)) * 32 + (r & 7) * 4 + (e8 >> 1 & 3)] = v;
+      };
+      uint4 raw[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) raw[j] = load(lane + 32 * j);
+      float least = INFINITY;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const float m = q_largest(raw[j], A.bf16);
+        amax = fmaxf(amax, m);
+        least = fminf(least, m > 0.f ? m : INFINITY);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) {
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+      }
+      const auto power = [](float m) { return min(max(15 - log2_of(m), -112), 100); };   // takes m to [2^15, 2^16)
+      const int up = A.bf16 && amax > 0.f ? power(amax) : 0;
+      rsc *= pow2(-up);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) put(lane + 32 * j, raw[j], up);
+      if (A.bf16 && least < amax * 0x1p-8f) {
+        modes = kUneven;
+#pragma unroll 1
+        for (int p = lane; p < 32 * kN; p += 32) {
+          const uint4 v = load(p);
+          float m = q_largest(v, true);
+#pragma unroll
+          for (int o = 1; o < kD / 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          const int mine = m > 0.f ? min(power(m), up + 120) : up;
+          if (p % (kD / 8) == 0) downs[p / (kD / 8)] = pow2(up - mine);
+          put(p, v, mine);
+        }
       }
       __syncwarp();
     }
@@ -429,7 +453,6 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     const int max_last = at0 + i1, min_begin = A.span > 0 ? at0 + i0 - A.span + 1 : 0;   // and what any of them sees
     float acc[kMt][kNt][4];
     float mx[kR], sum[kR];                                 // (mx: of p', so kLogPScale below the largest)
-    bool wide = false, based = false;
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
@@ -493,7 +516,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       const int absent = __float_as_int(sc[4]);
       float lw = __log2f(fabsf(vs) * winv), ipw = ex2(-lw);    // of kPScale vs / U; what takes a sum of p' to one of 2^(s - m)
       const bool big = !(fmaxf(fabsf(s4.x), fabsf(s4.z)) * most_score <= kMostScore);
-      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || wide || based || big ||
+      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || modes || big ||
                           !(max_nan(fabsf(s4.y), fabsf(s4.w)) * winv <= kMostPw && fminf(fabsf(s4.y), fabsf(s4.w)) * winv >= kLeastPw);
       if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
         const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
@@ -508,20 +531,29 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
       __syncwarp();
       if (masked) {
+        if (modes & kUneven) {
+#pragma unroll
+          for (int k = 0; k < kNt; ++k) {
+            const float2 d = *reinterpret_cast<const float2*>(downs + 8 * k + 2 * t);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) sx[s][k][0] *= d.x, sx[s][k][1] *= d.y, sx[s][k][2] *= d.x, sx[s][k][3] *= d.y;
+          }
+        }
         // magnitudes of the value scales, of chunks that some row sees (-1: none does; 0: a scale that is none)
         const auto seen = [&](int key, float va, int out) {
           return absent & out || key > max_last || key + kChunk <= min_begin ? -1.f : va < INFINITY ? va : 0.f;
         };
         const float va0 = seen(key0, fabsf(s4.y), 1), va1 = seen(key0 + kChunk, fabsf(s4.w), 2), va = chunk ? va1 : va0;
         const auto far = [&](float x) { return x >= 0.f && !(x * winv <= kMostPw && x * winv >= kLeastPw); };
-        if (!wide && (far(va0) || far(va1))) {
-          wide = true;
+        if (!(modes & kWide) && (far(va0) || far(va1))) {
+          modes |= kWide;
           if (g == 0) {
 #pragma unroll
             for (int k = 0; k < kR; ++k) refs[8 * (k >> 1) + 2 * t + (k & 1)] = mx[k];
           }
           __syncwarp();
         }
+        const bool wide = modes & kWide, based = modes & kBased;
         if (wide) {
           ipw = 0.f;
           lw = va > 0.f ? __log2f(va) + __log2f(winv) : -INFINITY;
@@ -609,7 +641,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
             }
           }
           __syncwarp();
-          based = true;
+          modes |= kBased;
           f = 1.f;
         }
         if (wide) {
@@ -650,7 +682,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
           const float m = top[k] <= mx[k] + (kSlack + kLogPScale) ? mx[k] : max_nan(mx[k], top[k] - kLogPScale);
           const float c = ex2(mx[k] - m);
           mx[k] = m;
-          if (!wide) sum[k] *= c;
+          if (!(modes & kWide)) sum[k] *= c;
 #pragma unroll
           for (int q = 0; q < kMt; ++q) {
             acc[q][k >> 1][k & 1] *= c;
@@ -704,6 +736,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     const bool whole = steps == sq.steps;
     float* part = A.part + ((int64_t)run * 2 + (first_segment ? 0 : 1)) * S::kSlot;
     const float by_unit = 1.f / winv;
+    const bool wide = modes & kWide, based = modes & kBased;
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < kR; ++k) {

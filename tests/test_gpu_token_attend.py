@@ -237,3 +237,46 @@ def test_scores_of_any_size(api, D, G, W, n, size, dtype):
                 c = dict(cache, k_scale=cache["k_scale"].clone())
                 c["k_scale"][part, 0] *= size
                 check_rows(api, z, c, pages, lengths)
+
+
+# ------------------------------------------------------------------------------ queries
+@pytest.mark.parametrize("D,G,W", [(64, 2, 2), (128, 4, 9), (64, 1, 1)])
+def test_queries_of_very_different_size_side_by_side(api, D, G, W):
+    """A large query in the same call leaves the others what they are.  (It is along one axis, where one key stands
+    out, so that its own softmax is decided.)"""
+    g = gen(130 + D)
+    H, block, n = 2, 16, 300
+    cache = make_cache(api, g, 20, H, block, D)
+    codes = (20 * torch.randn(20, H, block, D, generator=g, device="cuda")).clamp(-200, 200)
+    codes[..., 0] = codes[..., 0].clamp(-50, 50)
+    codes[3, :, 5, 0] = 448
+    cache["k"].copy_(codes.to(torch.float8_e4m3fn))
+    cache["k_scale"].fill_(2.0 ** -4)
+    pages = torch.arange(20, device="cuda", dtype=torch.int32)[None]
+    lengths = torch.tensor([n], device="cuda", dtype=torch.int32)
+    q = torch.randn(1, W, H * G, D, generator=g, device="cuda")
+    for size in (2.0 ** 10, 2.0 ** 30, 2.0 ** 60, 2.0 ** 90):
+        z = q.clone()
+        z[0, W - 1, 0] = 0
+        z[0, W - 1, 0, 0] = size
+        check_rows(api, z.to(BF16), cache, pages, lengths)
+    z = q.clone()
+    z[0, 0] *= 2.0 ** -40                                # and small ones: all but flat
+    check_rows(api, z.to(BF16), cache, pages, lengths)
+
+
+@pytest.mark.parametrize("below", [20, 26, 29, 31])
+def test_small_elements_of_a_query_count(api, below):
+    """Elements 2^-below of a row's largest, all eight of their bits, where the largest meets keys of zero."""
+    g = gen(140 + below)
+    D = 64
+    cache = make_cache(api, g, 4, 1, 32, D)
+    codes = cache["k"].float()
+    codes[..., 0] = 0
+    cache["k"].copy_(codes.to(torch.float8_e4m3fn))
+    pages = torch.arange(4, device="cuda", dtype=torch.int32)[None]
+    lengths = torch.tensor([100], device="cuda", dtype=torch.int32)
+    q = (1 + torch.rand(1, 2, 2, D, generator=g, device="cuda")) * 2.0 ** -below
+    q = q * torch.where(torch.rand(1, 2, 2, D, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    q[..., 0] = 1.0
+    check_rows(api, q.to(BF16), cache, pages, lengths, scale=2.0 ** below * 0.5)
