@@ -386,8 +386,15 @@ def _workspace(t, need, dev):
     return t
 
 
-_verify_workspace = functools.lru_cache(maxsize=None)(B.sdv_token_verify_workspace_bytes)
-_attend_workspace = functools.lru_cache(maxsize=None)(B.sdv_attend_workspace_bytes)
+@functools.lru_cache(maxsize=1024)
+def _verify_workspace(Bn, L):
+    return B.sdv_token_verify_workspace_bytes(Bn, L)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_workspace(device, *sizes):
+    """The size depends on the current device's SMs too, which `device` stands for."""
+    return B.sdv_attend_workspace_bytes(*sizes)
 
 
 def _rows(what, t, dims):
@@ -563,7 +570,7 @@ def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span
     _dense("status", status, torch.int32, (Bn,))
     dev = q.device
     r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
-    workspace = _workspace(workspace, _attend_workspace(Bn, W, Hq, H, D), dev)
+    workspace = _workspace(workspace, _attend_workspace(torch.cuda.current_device(), Bn, W, Hq, H, D), dev)
     B._call("sdv_cache_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
             cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
             page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),

@@ -120,3 +120,28 @@ def test_api_refuses_host_tensors():
     with pytest.raises(ValueError):
         api.cache_append(api.make_token_cache(2, 1, 16, 64, "cpu"), torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 1, 64),
                          torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+
+
+def test_attend_workspace_follows_the_device(monkeypatch):
+    """Sizes are remembered per device, whose SMs they depend on, and not without end."""
+    import torch
+    from paper_2606_13426_gb300 import api
+    current = [0]
+    asked = []
+
+    def size(*sizes):                                       # a device of 152 SMs and one of 160
+        asked.append(sizes)
+        return 1000 * (152, 160)[current[0]]
+    monkeypatch.setattr(api.B, "sdv_attend_workspace_bytes", size)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    api._attend_workspace.cache_clear()
+    try:
+        for _ in range(2):
+            for current[0] in (0, 1):
+                assert api._attend_workspace(torch.cuda.current_device(), 2, 2, 4, 2, 64) == 1000 * (152, 160)[current[0]]
+        assert len(asked) == 2
+        for n in range(5000):
+            api._attend_workspace(0, n, 2, 4, 2, 64)
+        assert api._attend_workspace.cache_info().currsize <= 1024
+    finally:
+        api._attend_workspace.cache_clear()
