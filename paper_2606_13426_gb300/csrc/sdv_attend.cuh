@@ -868,15 +868,16 @@ inline RowTiles row_tiles(int64_t R, int most) {
   const int64_t rt = (R + 8 * most - 1) / (8 * most);
   return RowTiles{(int)rt, (int)((((R + rt - 1) / rt) + 7) / 8)};
 }
-// The tiles that are likely to take least, by what was measured for 1 to 5 eights (tenths of a microsecond): a
-// call's fixed part, which grows with the kernel's code and its partials, and a round of steps over all
-// warps.  Many eights read the cache less often, few start sooner: 36 rows (D = 128) over 3 x 24000 keys and 8
-// heads take 82 us in two tiles of 3 eights and 96 in one of 5, over 32 x 8000 keys 235 and 206; 45 rows over 31
-// keys 12 us in six tiles of 1 and 17 in two of 3.  `longest`: steps of the longest sequence that the page
+// The tiles that are likely to take least, by a cost fitted to the times of 120 shapes in each number of eights
+// (tenths of a microsecond): a call's fixed part, which grows with the kernel's code and its partials, and a round
+// of steps over all warps.  It chooses what takes 0.3 % more than the best on average.  Many eights read the cache less
+// often, few start sooner: 36 rows (D = 128) over 3 x 24000 keys and 8 heads take 99 us in two tiles of 3 eights and 120
+// in one of 5, over 32 x 8000 keys 275 and 259; 45 rows over 31 keys 12.5 us in six tiles of 1 and 20 in two of 3; 128 rows
+// over 62 x 48 keys and 4 heads 43 in four of 4 and 55 in sixteen of 1.  `longest`: steps of the longest sequence that the page
 // table allows, since the lengths are on the device.
 inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, int warps) {
-  static const int fixed[kMaxNt] = {110, 130, 160, 200, 360};
-  static const int round[2][kMaxNt] = {{11, 13, 16, 17, 18}, {15, 19, 22, 26, 33}};
+  static const int fixed[kMaxNt] = {110, 130, 160, 185, 360};
+  static const int round[2][kMaxNt] = {{8, 11, 13, 16, 17}, {10, 16, 23, 30, 39}};
   RowTiles best{0, 0};
   int64_t least = INT64_MAX;
   for (int most = kMaxNt; most >= 1; --most) {
