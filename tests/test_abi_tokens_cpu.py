@@ -145,3 +145,26 @@ def test_attend_workspace_follows_the_device(monkeypatch):
         assert api._attend_workspace.cache_info().currsize <= 1024
     finally:
         api._attend_workspace.cache_clear()
+
+
+def test_binding_functions_hand_their_arguments_on(lib):
+    """The binding's function of each entry point: arguments in the header's order, refusals as SDVError."""
+    from paper_2606_13426_gb300 import binding as B
+    ok = dict(
+        sdv_token_scores=[0x1000, 100, 0, 100, B.SDV_F32, 0x2000, 1.0, 0, 0x3000, 0, 0, 0, 0, 0, 0, 0],
+        sdv_token_scores_grad=[0x1000, 100, 0, 100, B.SDV_F32, 0x2000, 1.0, 0x3000, 0x4000, 0, 0x5000, 0, 0x6000, 100, 0],
+        sdv_token_scores_train=[0x1000, 100, 0, 100, B.SDV_F32, 0x2000, 1.0, 0x3000, 0, 0x4000, 0x5000, 0x6000, 0x7000, 0, 0x8000, 100, 0])
+    for name, args in ok.items():                           # no rows: nothing is launched
+        assert getattr(B, name)(*args) == B.SDV_OK
+    wrong = dict(
+        {k: v[:3] + [0] + v[4:] for k, v in ok.items()},    # V = 0
+        sdv_token_verify=[0x1000, 400, 100, 0x2000, 300, 100, 0x3000, 2, 3, 100, B.SDV_BF16, 1.0, 1.0, 2, 0, 1, 0, 0, 0x4000, 0x5000, 0, 0, 0x6000,
+                          1 << 20, 0],                      # mode 2
+        sdv_cache_append=[0x1000, 0x2000, 256, 128, 64, B.SDV_F32, 2, 2, 2, 96, 16, 0x10000, 0x20000, 0x30000, 0x40000, 8, 0x50000, 4, 0x60000, 0, 0,
+                          0],                               # D = 96
+        sdv_cache_attend=[0x1000, 512, 256, 64, B.SDV_BF16, 2, 2, 3, 2, 64, 16, 0x10000, 0x20000, 0x30000, 0x40000, 8, 0x50000, 4, 0x60000, 0, 0.1, 0,
+                          0x2000, 0x3000, 0, 0x100000, 1 << 30, 0])   # 3 query heads on 2
+    for name, args in wrong.items():
+        with pytest.raises(B.SDVError) as e:
+            getattr(B, name)(*args)
+        assert e.value.code == B.SDV_EINVAL, name

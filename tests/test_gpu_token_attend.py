@@ -280,3 +280,21 @@ def test_small_elements_of_a_query_count(api, below):
     q = q * torch.where(torch.rand(1, 2, 2, D, generator=g, device="cuda") < 0.5, -1.0, 1.0)
     q[..., 0] = 1.0
     check_rows(api, q.to(BF16), cache, pages, lengths, scale=2.0 ** below * 0.5)
+
+
+# ------------------------------------------------------------------------------ prompts
+@pytest.mark.parametrize("B,W,H,G,D,span", [(2, 100, 2, 4, 128, 0), (1, 700, 2, 2, 64, 0), (3, 257, 1, 8, 64, 100), (1, 600, 1, 1, 128, 33)])
+def test_windows_of_whole_prompts(api, B, W, H, G, D, span):
+    """Windows far longer than a row tile: prompts from nothing, prompts behind cached tokens, shorter ones than
+    the window; each row against its own reference."""
+    g = gen(160 + W)
+    block = 64
+    M = (W + 300) // block + 1
+    cache = make_cache(api, g, B * M, H, block, D)
+    pages = torch.randperm(B * M, generator=g, device="cuda").to(torch.int32).view(B, M)
+    q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(BF16)
+    n = torch.full((B,), W, device="cuda", dtype=torch.int32)
+    check_rows(api, q, cache, pages, n, span=span)
+    n += torch.randint(0, 300, (B,), generator=g, device="cuda", dtype=torch.int32)
+    counts = torch.randint(1, W + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    check_rows(api, q, cache, pages, n, counts, span=span)
