@@ -35,7 +35,7 @@ struct TokenVerifyArgs {
   int64_t q_sb, q_sr, p_sb, p_sr;
   const int32_t* tokens;
   int L, V, mode;
-  float cq, cp, iq, ip;                // log2(e) / T and 1 / T of target and draft
+  float cq, cp, tq, tp;                // log2(e) / T and T of target and draft
   const int32_t* L_eff;
   uint64_t seed;
   const float* coins;
@@ -58,9 +58,9 @@ struct Racer {
   int i;
 };
 
-// A row's softmax as e^{(x - m)/T} / s: m and log2 s.
+// A row's softmax as e^{(x - m)/T} / s: m, log2 s and s.
 struct RowStat {
-  float m, l2;
+  float m, l2, s;
 };
 __device__ __forceinline__ bool row_ok(const RowStat& r) { return r.m > -INFINITY && r.m < INFINITY; }
 // log2 of the probability, with `shift` (a log2) added.
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) k_token_stats(const TokenVer
   if (rank || threadIdx.x >= 32) return;
   const Stat all = stat_gather(stats, C * kWarps, threadIdx.x, c);
   if (threadIdx.x == 0) {
-    A.stats[n] = RowStat{all.m, log2f(all.s)};
+    A.stats[n] = RowStat{all.m, log2f(all.s), all.s};
     if (r < window) A.steps[(int64_t)b * A.L + r] = in;
   }
 }
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_token_verify(const TokenVeri
     log_seg = log_segs(2 * n + 1);
     for (int r = warp; r < 2 * n + 1; r += kVerWarps) {
       const Stat a = stat_gather(all + (r << (log_seg + log_c)), 1 << (log_seg + log_c), lane, r <= n ? A.cq : A.cp);
-      if (lane == 0) rs[r] = RowStat{a.m, log2f(a.s)};
+      if (lane == 0) rs[r] = RowStat{a.m, log2f(a.s), a.s};
     }
   } else {
     asm volatile("griddepcontrol.wait;" ::: "memory");       // the rows' statistics are there
@@ -307,9 +307,9 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_token_verify(const TokenVeri
       const RowStat rq = rs[j], rp = rs[n + 1 + j];
       const float xq = in[j].xq, xp = in[j].xp;
       if (rq.m < INFINITY && rp.m < INFINITY) {
-        const float lq = row_ok(rq) && xq > -INFINITY ? (xq - rq.m) * A.iq - rq.l2 * kLn2f : -INFINITY;
-        const float lp = row_ok(rp) && xp > -INFINITY ? (xp - rp.m) * A.ip - rp.l2 * kLn2f : -INFINITY;
-        ell = lq > -INFINITY ? lq - lp : -INFINITY;
+        // The sums' logarithms are large and nearly equal: that of their ratio, near 0, costs no bits.
+        const float dq = row_ok(rq) ? (xq - rq.m) / A.tq : -INFINITY, dp = row_ok(rp) ? (xp - rp.m) / A.tp : -INFINITY;
+        ell = !(dq > -INFINITY) ? -INFINITY : dp > -INFINITY ? (dq - dp) + logf(rp.s / rq.s) : INFINITY;
       }
     } else {
       atomicOr(&status_s, SDV_STATUS_BAD_TOKEN);
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_token_verify(const TokenVeri
     }
   }
   // the next token
-  const RowStat rq = rs[acc], rp = acc < n ? rs[n + 1 + acc] : RowStat{-INFINITY, 0.f};
+  const RowStat rq = rs[acc], rp = acc < n ? rs[n + 1 + acc] : RowStat{-INFINITY, 0.f, 1.f};
   const float sh = la[acc] * kLog2E;
   const T* q = q0 + acc * A.q_sr;
   Best best{0.f, -1};
@@ -544,9 +544,9 @@ int sdv_token_verify(const void* target, int64_t target_stride_b, int64_t target
   if (!workspace || workspace_bytes < sdv_token_verify_workspace_bytes(B, L)) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   const TokenVerifyArgs A{target, draft, target_stride_b, target_stride_row, draft_stride_b, draft_stride_row, tokens, L, V,
-                          mode, kLog2E / temperature, kLog2E / draft_temperature, 1.f / temperature,
-                          1.f / draft_temperature, L_eff, seed, coins, race, accepted_len, next_token, log_ratio_out,
-                          status_out, (RowStat*)workspace, (StepIn*)((RowStat*)workspace + (size_t)B * (2 * L + 1)),
+                          mode, kLog2E / temperature, kLog2E / draft_temperature, temperature, draft_temperature, L_eff,
+                          seed, coins, race, accepted_len, next_token, log_ratio_out, status_out,
+                          (RowStat*)workspace, (StepIn*)((RowStat*)workspace + (size_t)B * (2 * L + 1)),
                           (int*)((StepIn*)((RowStat*)workspace + (size_t)B * (2 * L + 1)) + (size_t)B * L)};
   cudaStream_t s = (cudaStream_t)stream;
   return launched(dtype == SDV_F32    ? launch_token_verify<SDV_F32>(A, B, dtype, s)

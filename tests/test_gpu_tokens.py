@@ -1068,3 +1068,18 @@ def test_append_takes_any_stride_of_an_axis_of_one_place(api, B, W, H):
     for other in [y[..., :32]] + ([torch.zeros(B, W, H, 72, device="cuda")[..., :64]] if B * W * H > 1 else []):
         with pytest.raises(ValueError):
             api.cache_append(caches[0], x, other, pages, n)
+
+
+@pytest.mark.parametrize("B,L,V,dtype,T", [(4, 4, 32768, BF16, 1.0), (3, 8, 131072, F16, 1.0), (40, 6, 50001, BF16, 1.0), (200, 3, 70, BF16, 1.0),
+                                           (8, 5, 32768, BF16, 0.8), (8, 5, 40001, F32, 1.3)])
+def test_log_ratios_to_the_last_bits(api, B, L, V, dtype, T):
+    """Log ratios beside the 64-bit ones.  Differences to the maximum are exact for 16-bit logits (to half a step of 2^-20 in 8 .. 16
+    for fp32 ones, and so are quotients by a temperature: 2^-21 each); the sums' ratio is within 2^-22, its logarithm and the
+    additions within half a step of the result."""
+    tl, dl, tok, coins, race = make_verify(gen(B + V), B, L, V, dtype, T)
+    r = api.token_verify(tl, dl, tok, coins=coins, race=race, temperature=T)
+    q, p = (torch.log_softmax(x.double() / T, 2) for x in (tl[:, :L], dl))
+    want = (q - p).gather(2, tok[..., None].long())[..., 0]
+    steps = 0 if T == 1.0 and dtype != F32 else 4 * 2.0 ** -21
+    err = (r["log_ratio"].double() - want).abs()
+    assert (err <= 2.0 ** -21 + steps + 2.0 ** -22 * want.abs()).all(), float((err / (2.0 ** -21 + steps + 2.0 ** -22 * want.abs())).max())
