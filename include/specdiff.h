@@ -540,8 +540,8 @@ size_t sdv_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
  * that does not exist are not seen (SDV_STATUS_BAD_PAGE is added to status [B], or NULL), and a
  * length beyond the page table counts as its end.  Probabilities times their
  * values' scale are rounded to the sum of two fp16 before they meet the values: to 22 bits, or 2^-32 of
- * the row's largest.  bf16 queries go through fp16 under powers of two: elements are exact above 2^-24 of
- * their row's largest and within 2^-32 of it below (where that largest is 2^-85 or more).  Codes are exact and
+ * the row's largest.  bf16 queries go through fp16 under powers of two: elements are exact above 2^-18 of
+ * their row's largest and within 2^-26 of it below (where that largest is 2^-85 or more).  Codes are exact and
  * sums fp32.  The lengths of the batch decide where a sequence's keys are split, and so
  * the order of its sums.
  */

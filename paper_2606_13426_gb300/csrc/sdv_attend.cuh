@@ -25,7 +25,7 @@
 // lies on pages of small values must keep its bits whatever the other pages hold.  The sum's terms 2^(s - m) are
 // p' U / vs.  The unit U is a power of two near an item's first scale; from where a scale that rows see is far
 // from it, or 0, the sums of the rest of the item are kept apart, against references on the score alone ("wide").
-// Scores in the millions, of which fp32 holds no fraction, are taken less a base of their row ("based"): an exact
+// Scores past 2^24, of which fp32 holds no fraction, are taken less a base of their row ("based"): an exact
 // difference.  m moves only when a score passes it by 2^kSlack, so that most steps need no exchange between lanes and
 // no rescaling of the output.
 #pragma once
@@ -44,7 +44,7 @@ constexpr float kSlack = 8.f;
 constexpr float kPScale = 128.f, kLogPScale = 7.f;   // f16 holds 2^kSlack kPScale; its least step is 2^-31 of a row's largest
 // What few items need: a power of two per query, sums kept apart, scores less a base (see above and k_attend).
 constexpr int kUneven = 1, kWide = 2, kBased = 4;
-constexpr float kMostScore = 0x1p22f;                 // a bound on the scores (as powers of 2) up to which there is no base
+constexpr float kMostScore = 0x1p24f;                 // a bound on the scores (as powers of 2) up to which half a step of theirs fits f16's range too
 constexpr float kBaseRoom = 64.f;                     // scores less their base stay below
 constexpr int kLeastUnit = -119, kMostUnit = 126;    // kPScale over the unit, and the unit over kPScale, are normal numbers
 constexpr float kLeastPw = 0x1p-33f, kMostPw = 0x1p48f;   // kPScale vs / U where the sums are kept with p'
@@ -155,9 +155,9 @@ __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, i
 }
 
 __device__ __forceinline__ int64_t run_start(int64_t units, int g, int runs) { return units * g / runs; }
-// Runs for `units` steps of `items` items.  Where the items have a step each, a run has one: 144 rows over 19 keys
-// take 18 us, and 27 with two steps a run; items of two steps want them together (32 rows over 48 keys: 40 us, and
-// 53 apart).
+// Runs for `units` steps of `items` items.  Where the items have a step each, a run has one: 53 x 25 rows over 8 keys and
+// 8 heads take 21 us, and 29 with two steps a run; items of two steps want them together (62 x 32 rows over 48 keys and
+// 4 heads: 17 us, and 23 apart).
 __device__ __forceinline__ int run_count(int64_t units, int64_t items, int warps) {
   return (int)min((int64_t)warps, units <= items ? units : (units + kMinSteps - 1) / kMinSteps);
 }
@@ -189,13 +189,13 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from, bool real) 
 }
 
 // With more sequences than this their steps are added up once, by a kernel of its own; with fewer each
-// warp does it.  4 heads of 60 tokens, without that kernel and with it: 11.4 us and 13.5 for 128
-// sequences, 15.7 and 16.1 for 256, 26.2 and 20.0 for 512, 169 and 56 for 2048.
+// warp does it.  4 heads of 60 tokens, without that kernel and with it: 12.5 us and 14.6 for 128
+// sequences, 16.7 and 17.0 for 256, 36 and 30 for 512, 188 and 80 for 2048.
 constexpr int kPrefixFrom = 256;
 constexpr int kPrefixThreads = 1024;
 
-// Warps of a CTA of k_attend, one CTA an SM: 2 x 1 token of 64 query heads on 8, up to 131000 keys, takes 63 us
-// with 8 warps, 73 with 6 (and longer rings) and 67 with 16, which the registers of few rows would allow.
+// Warps of a CTA of k_attend, one CTA an SM, as many as its registers allow: 2 x 1 token of 64 query heads on 8, 131000
+// keys, takes 97 us with 8 warps and 105 with 6, 16 x 4 tokens of 32 heads on 8, 16000 keys, 110 and 130.
 constexpr int kAttendWarps = 8;
 
 __device__ __forceinline__ void put_out(const AttendArgs& A, int64_t at, float x) {
@@ -207,8 +207,8 @@ __device__ __forceinline__ float lse_of(float m, float l, float base) {
 }
 
 // A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others, 8 KB, under
-// way; its queries' fragments are beside it.  (Four under way at D = 128, where few rows leave room: 1
-// to 7 % slower for 4 to 32 rows.)
+// way; its queries' fragments are beside it.  (Four under way at D = 128, where few rows leave room: within
+// 2 % either way for 4 to 36 rows.)
 template <int kD, int kNt>
 struct AttendShape {
   static constexpr int kWarps = kAttendWarps;
@@ -254,13 +254,13 @@ __device__ __forceinline__ float q_largest(uint4 v, bool bf16) {
 }
 
 // Bytes: every key and value once for each row tile, 2 D codes a token and head; operations: 4 D a row of those.  Bound
-// by DRAM where rows are few (8 a head, 2 x 131000 keys or 16 x 16000: 5.1 to 5.7 TB/s while it runs), by the two warps a
-// scheduler waiting on their own instructions where there are 36 (32 windows of 9 tokens, 4 query heads a
-// head, up to 16000 keys: 210 us, 2.8 TB/s and 0.2 PFLOP/s); the matrix instructions alone, 8 cycles each
-// a scheduler, need 1280 cycles a step there, HBM's pace 1400.
+// by DRAM where rows are few (4 or 8 a head, 2 x 131000 keys or 16 x 16000: 97 us, 5.4 to 5.5 TB/s with the join), by the two
+// warps a scheduler waiting on their own instructions where there are 36 (32 windows of 9 tokens, 4 query heads a
+// head, up to 16000 keys: 273 to 280 us, 2.1 TB/s and 0.15 PFLOP/s); the matrix instructions alone, 8 cycles each
+// a scheduler, need 1920 cycles a step there, HBM's pace 1400.
 // The probabilities go into the second product as a sum of two f16, 22 bits: with one, f16 outputs were off by as much
 // as their own rounding again (2.9e-4 of their size, 2.0e-4 with two), and bf16 outputs were roundings of numbers
-// up to 2^-12 off, so that some fell on the neighbouring value.
+// up to 2^-12 off, so that some fell on the neighbouring value.  The second half costs those windows 48 us, few rows nothing.
 template <int kD, int kNt>
 __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
@@ -385,8 +385,8 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       look(n + 1);
     }
     // The rows' queries as fragments, in f16: bf16 ones are scaled into its range by a power of two, one for all rows
-    // where every eight elements' largest is within 2^-8 of the largest of all, else ("uneven") one a row, whose scores are
-    // brought to the common one again.  So an element is within 2^-32 of its row's largest, whatever the other rows hold.
+    // where every eight elements' largest is within 2^-14 of the largest of all, else ("uneven") one a row, whose scores are
+    // brought to the common one again.  So an element is within 2^-26 of its row's largest, whatever the other rows hold.
     float rsc = A.scale2, amax = 0.f;
     int modes = 0;                                         // what the steps of this item take care of
     {
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
       rsc *= pow2(-up);
 #pragma unroll
       for (int j = 0; j < kN; ++j) put(lane + 32 * j, raw[j], up);
-      if (A.bf16 && least < amax * 0x1p-8f) {
+      if (A.bf16 && least < amax * 0x1p-14f) {
         modes = kUneven;
 #pragma unroll 1
         for (int p = lane; p < 32 * kN; p += 32) {
@@ -785,8 +785,8 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
 
 // Joins the partials of an item that several warps' runs hold; an item without steps gets zeros.
 // kSplit: a CTA has one row, and its warps take the partials in turn (few items, many partials of
-// each); otherwise a warp has a row.  Bound by latency: 6 to 14 us.  16 items of 76 partials: 10 us split, 70
-// not; 256 items of 5: 20 split, 14 not.
+// each); otherwise a warp has a row.  Bound by latency: 6 to 14 us.  Whole calls with 16
+// items of 76 partials and 8 rows take 98 us split and 114 not, with 256 of 5 partials 104 and 99 (4 rows) or 301 and 259 (36).
 template <int kD, int kNt, bool kSplit>
 __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A) {
   using S = AttendShape<kD, kNt>;
