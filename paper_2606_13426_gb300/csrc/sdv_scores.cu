@@ -103,7 +103,7 @@ __device__ __forceinline__ void rank_candidates(const Cand* c, int n, int k, Put
 
 // Statistics of a row in one read: a thread keeps sums against a reference that moves only when a logit
 // passes it by 2^8, a warp, then the cluster's leader rebase them to the row's maximum.  Alternatives: the
-// k-th largest of 32 groups' maxima is a threshold that at least k logits reach; the few threads above it
+// k-th largest of 32 groups' maxima (64 groups' from k = 25 on) is a threshold that at least k logits reach; the few threads above it
 // read their vectors again (from the L2), and what reaches it is ranked by counting.
 // Bound by the read where rows are many (600 x 131072 bf16 without alternatives 26.8 us, 5.9 TB/s; 38 with
 // 20), by latency where they are few (8 x 65536: 3.7 us, 5.7 with 8; 144 x 131072: 10.3 us, 15 with 20).
