@@ -408,7 +408,10 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
 #define SDV_STATUS_BAD_TOKEN 16u   /* a token outside [0, V) */
 #define SDV_STATUS_BAD_PAGE  32u   /* a page outside the cache, or a token past the page table */
 
+#define SDV_STATUS_BAD_TREE  64u   /* a parent that does not come before its child, or a path that leaves the tree */
+
 #define SDV_MAX_TOP   32       /* largest number of alternatives */
+#define SDV_MAX_TREE  64       /* largest number of nodes of a drafted tree */
 #define SDV_MAX_BLOCK 128      /* largest number of tokens of a cache page (a multiple of 16) */
 
 /*
@@ -552,6 +555,104 @@ int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int6
                      int max_pages, const int32_t *lengths, const int32_t *counts, float scale,
                      int span, void *out, float *lse, uint32_t *status, void *workspace,
                      size_t workspace_bytes, sdv_stream_t stream);
+
+/* ---- trees of drafted tokens ------------------------------------------------
+ *
+ * A drafted tree has up to W nodes, in an order in which parents come before their children; node 0, the
+ * last emitted token, is its root.  parents [B, W] int32: parents[b, i] < i, -1 for a root; of any other
+ * value SDV_STATUS_BAD_TREE tells, and the node counts as a root.  counts [B] int32 or NULL: the nodes in use
+ * (W if NULL; at most W).  A round:
+ * sdv_cache_append_rotary writes the nodes' keys and values behind the lengths[b] tokens that the cache
+ * holds, node i in place lengths[b] + i but turned by its position lengths[b] + depth; sdv_tree_attend attends;
+ * sdv_tree_verify verifies; sdv_cache_keep moves the rows of the accepted path to places lengths[b], lengths[b] + 1, ...
+ */
+
+/*
+ * sdv_cache_append_rotary - sdv_cache_append with the position rotation applied to the keys (and to
+ * queries, if given) on the way.  Pair i, 0 <= i < rot / 2, of a head's elements (a, b) = (i, i + rot / 2)
+ * (halves = 1) or (2 i, 2 i + 1) (halves = 0) becomes
+ *   (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos freqs[i];
+ * elements from rot on stay.  freqs [rot / 2] float64, radians a position (the angle's error is that of freqs[i] /
+ * 2 pi in 64 bits times pos: positions need no small range).  positions [B, W] int32, or NULL: lengths[b] + i.
+ * Keys are turned in fp32 and rounded once, to their codes.  q [B, W, Hq, D] and q_out (`dtype`) have strides of
+ * their own, 0 <= Hq D <= 2^27; q_out may be q, with its strides.  Queries i >= counts[b] become 0.  q and q_out may both be NULL.
+ * 2 <= rot <= D, even.  The rest as in sdv_cache_append.
+ */
+int sdv_cache_append_rotary(const void *k_new, const void *v_new, int64_t stride_b, int64_t stride_t,
+                            int64_t stride_h, const void *q, int64_t q_stride_b, int64_t q_stride_t,
+                            int64_t q_stride_h, void *q_out, int64_t out_stride_b,
+                            int64_t out_stride_t, int64_t out_stride_h, int dtype, int B, int W,
+                            int Hq, int H, int D, int block, const double *freqs, int rot,
+                            int halves, const int32_t *positions, void *k_codes, void *v_codes,
+                            float *k_scale, float *v_scale, int64_t pages,
+                            const int32_t *page_table, int max_pages, const int32_t *lengths,
+                            const int32_t *counts, uint32_t *status, sdv_stream_t stream);
+
+/* Bytes of device workspace sdv_tree_attend needs; 0 for invalid sizes. */
+size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
+
+/*
+ * sdv_tree_attend - sdv_cache_attend for a tree: the last counts[b] of the lengths[b] tokens in the cache are the
+ * nodes, and node i sees the tokens before them, its ancestors and itself.  W at most SDV_MAX_TREE.  Nodes
+ * i >= counts[b] get 0 and -inf, as all of a sequence with lengths[b] < counts[b] do (SDV_STATUS_BAD_TREE).
+ */
+int sdv_tree_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h,
+                    int dtype, int B, int W, int Hq, int H, int D, int block, const void *k_codes,
+                    const void *v_codes, const float *k_scale, const float *v_scale, int64_t pages,
+                    const int32_t *page_table, int max_pages, const int32_t *lengths,
+                    const int32_t *parents, const int32_t *counts, float scale, void *out,
+                    float *lse, uint32_t *status, void *workspace, size_t workspace_bytes,
+                    sdv_stream_t stream);
+
+/*
+ * sdv_tree_verify - verification of a drafted tree and the next token.  At a node u, from the root on, with
+ * q = softmax(target row u / temperature), p = softmax(draft row u / draft_temperature), the children
+ * c_1 < c_2 < ... of u are tried in turn, with beta_1 = 0, M_1 = 1:
+ *   c_k with token x is taken if eta < max{0, q(x) / p(x) - beta_k} / M_k, eta = coins[b, c_k];
+ *   else beta_{k+1} = beta_k + M_k, M_{k+1} = sum_v max{0, q(v) - beta_{k+1} p(v)}.
+ * (Recursive rejection: what is left of q after k rejections of tokens drawn from p is
+ * max{0, q - beta p} / M.)  From a taken child it goes on; where none is, the next token is drawn from
+ * max{0, q - beta p}, with beta after the last rejection (q, where u has no children), as the index of the largest
+ * r_v / E_v, the lower of equal ones.  So the emitted tokens are distributed as the target's, if each child's token was
+ * drawn from p, independently of its siblings'.
+ * draft = NULL: children chosen without chance (a drafter's likeliest tokens): a child is taken if
+ * eta < q(x) / M, 0 for a token that a sibling before it had, where M is q's mass without the tokens rejected at u;
+ * the next token is drawn from q without them.
+ *   target, draft [B, W, V]: rows at b stride_b + u stride_row, `dtype`; a draft row is read where its node has children
+ *   tokens [B, W] int32 (a root's is not read), parents [B, W]; a node without a parent but node 0 is never reached
+ *   counts: 0 or less marks a sequence that is not verified (accepted_len 0, next_token -1)
+ *   coins [B, W] fp32 in [0, 1) or NULL: eta of each node; NULL draws them, Philox counter (b, i, 0, 0) word 0
+ *   race [B, V] fp32 > 0 or NULL: E, as in sdv_token_verify
+ *   accepted_len [B] int32 out: drafted nodes taken; path [B, W] int32 out: the nodes from the root on, -1 behind them
+ *   next_token [B] int32 out; log_ratio_out [B, W] fp32 out or NULL: log q(x) - log p(x) of the nodes tried (log q(x) without
+ *     a draft), 0 elsewhere; status_out [B] uint32 out or NULL
+ * A token outside [0, V) is passed over (SDV_STATUS_BAD_TOKEN), as all children of a node are whose rows hold a NaN or +inf
+ * (SDV_STATUS_NONFINITE) or whose target row has no probabilities; a draft row without any counts as 0.  Where nothing of
+ * q is left, the next token is drawn from q itself (SDV_STATUS_ZERO_DELTA); a target row without probabilities gives
+ * next_token -1.
+ */
+int sdv_tree_verify(const void *target, int64_t target_stride_b, int64_t target_stride_row,
+                    const void *draft, int64_t draft_stride_b, int64_t draft_stride_row,
+                    const int32_t *tokens, const int32_t *parents, int B, int W, int V, int dtype,
+                    float temperature, float draft_temperature, const int32_t *counts,
+                    uint64_t seed, const float *coins, const float *race, int32_t *accepted_len,
+                    int32_t *path, int32_t *next_token, float *log_ratio_out, uint32_t *status_out,
+                    sdv_stream_t stream);
+
+/*
+ * sdv_cache_keep - moves the rows of an accepted path: what stands in place lengths[b] + path[b, j] of the cache
+ * goes to place lengths[b] + j, for the entries of path [B, W] up to the first negative one.  All rows are
+ * read before any is written.  A page's scale stays, or grows to the least power of two whose 448-fold holds the
+ * rows that come into it; then all of the page's codes are restated under it (exact but for underflow where both scales
+ * are powers of two).  Rows keep the values that they stood for, rounded to nearest even under the new page's scale; NaN
+ * codes stay NaN.  An entry of W or more is left out
+ * (SDV_STATUS_BAD_TREE), as is a row from or to a page that does not exist (SDV_STATUS_BAD_PAGE).  status [B] uint32 or
+ * NULL: bits are added to it.
+ */
+int sdv_cache_keep(const int32_t *path, int B, int W, int H, int D, int block, void *k_codes,
+                   void *v_codes, float *k_scale, float *v_scale, int64_t pages,
+                   const int32_t *page_table, int max_pages, const int32_t *lengths,
+                   uint32_t *status, sdv_stream_t stream);
 
 /*
  * Profiling aid (not part of the method): when enabled, sdv_verify /

@@ -576,3 +576,135 @@ def cache_attend(q, cache, page_table, lengths, *, counts=None, scale=None, span
             page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale), int(span),
             r["out"].data_ptr(), r["lse"].data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel(), _stream())
     return r
+
+
+# ---- speculative decoding with trees of drafted tokens
+
+
+@functools.lru_cache(maxsize=1024)
+def _tree_attend_workspace(device, *sizes):
+    """The size depends on the current device's SMs too, which `device` stands for."""
+    return B.sdv_tree_attend_workspace_bytes(*sizes)
+
+
+def _here(*ts):
+    """All on the current device, whose stream the call goes to."""
+    dev = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor on cuda:%d, the current device, expected (got %s)" % (dev, t.device))
+
+
+def _cache_here(cache, *ts):
+    _here(cache["k"], cache["v"], cache["k_scale"], cache["v_scale"], *ts)
+
+
+def rotary_freqs(rot, base=10000.0, device="cuda"):
+    """Radians a position of the pairs of a head's first `rot` elements, base^(-2 i / rot), float64
+    [rot / 2], as cache_append_rotary takes them; scaled variants are the caller's own tensor."""
+    return float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+
+
+def cache_append_rotary(cache, k_new, v_new, page_table, lengths, freqs, *, pairs="halves", q=None, positions=None,
+                        counts=None, status=None, out=None):
+    """cache_append with the keys turned by their positions on the way (sdv_cache_append_rotary): positions
+    [B, W] int32, by default lengths[b] + i (a tree's nodes take lengths[b] + depth); freqs [rot / 2] float64
+    (rotary_freqs); pairs "halves" (i, i + rot / 2) or "neighbours" (2 i, 2 i + 1).  q [B, W, Hq, D] is
+    turned too and returned as a new tensor, or in `out`, which may be q itself."""
+    P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
+    dt = _rows("k_new", k_new, 4)
+    W = k_new.shape[1]
+    if tuple(k_new.shape) != (Bn, W, H, D) or v_new.dtype != k_new.dtype or not v_new.is_cuda or not _same_layout(k_new, v_new):
+        raise ValueError("k_new and v_new: [B, W, heads, dim] of one type and layout expected")
+    if pairs not in ("halves", "neighbours"):
+        raise ValueError("pairs: \"halves\" or \"neighbours\" expected")
+    _dense("freqs", freqs, torch.float64, (freqs.numel(),))
+    _dense("positions", positions, torch.int32, (Bn, W))
+    _dense("status", status, torch.int32, (Bn,))
+    Hq, qs, os_ = 0, (0, 0, 0), (0, 0, 0)
+    if q is not None:
+        if _rows("q", q, 4) != dt or tuple(q.shape) != (Bn, W, q.shape[2], D):
+            raise ValueError("q: [B, W, query heads, dim] of the keys' type expected")
+        Hq, qs = q.shape[2], q.stride()[:3]
+        if out is None:
+            out = torch.empty((Bn, W, Hq, D), dtype=q.dtype, device=q.device)
+        elif _rows("out", out, 4) != dt or out.shape != q.shape:
+            raise ValueError("out: a tensor like q expected")
+        os_ = out.stride()[:3]
+        if out.data_ptr() == q.data_ptr():
+            if not _same_layout(q, out):
+                raise ValueError("out: q itself or a tensor apart from it expected")
+            os_ = qs
+    elif out is not None:
+        raise ValueError("out without q")
+    _cache_here(cache, k_new, v_new, page_table, lengths, freqs, q, out, positions, counts, status)
+    B._call("sdv_cache_append_rotary", k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), k_new.stride(2),
+            _ptr(q), qs[0], qs[1], qs[2], _ptr(out), os_[0], os_[1], os_[2], dt, Bn, W, Hq, H, D, block, freqs.data_ptr(),
+            2 * freqs.numel(), int(pairs == "halves"), _ptr(positions), cache["k"].data_ptr(), cache["v"].data_ptr(),
+            cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P, page_table.data_ptr(), M, lengths.data_ptr(), _ptr(counts),
+            _ptr(status), _stream())
+    return out
+
+
+def tree_attend(q, cache, page_table, lengths, parents, *, counts=None, scale=None, status=None, workspace=None, out=None):
+    """Attention of a drafted tree's nodes q [B, W, Hq, D], whose tokens are the last ones of the cache, each over
+    the tokens before the tree, its ancestors and itself (sdv_tree_attend); parents [B, W] int32 (-1 for a
+    root).  lengths [B] count the nodes too.  Returns out [B, W, Hq, D] and lse [B, W, Hq].  scale defaults to D^-1/2."""
+    P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
+    dt = _rows("q", q, 4)
+    W, Hq = q.shape[1], q.shape[2]
+    if tuple(q.shape) != (Bn, W, Hq, D):
+        raise ValueError("q: [B, W, query heads, dim] expected")
+    _dense("parents", parents, torch.int32, (Bn, W))
+    _dense("status", status, torch.int32, (Bn,))
+    dev = q.device
+    r = dict(out=_out(out, "out", (Bn, W, Hq, D), q.dtype, dev), lse=_out(out, "lse", (Bn, W, Hq), torch.float32, dev))
+    _cache_here(cache, q, page_table, lengths, parents, counts, status, r["out"], r["lse"], workspace)
+    workspace = _workspace(workspace, _tree_attend_workspace(torch.cuda.current_device(), Bn, W, Hq, H, D), dev)
+    B._call("sdv_tree_attend", q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), dt, Bn, W, Hq, H, D, block,
+            cache["k"].data_ptr(), cache["v"].data_ptr(), cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P,
+            page_table.data_ptr(), M, lengths.data_ptr(), parents.data_ptr(), _ptr(counts), float(D ** -0.5 if scale is None else scale),
+            r["out"].data_ptr(), r["lse"].data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel(), _stream())
+    return r
+
+
+def tree_verify(target_logits, draft_logits, tokens, parents, seed=0, *, counts=None, temperature=1.0, draft_temperature=None,
+                coins=None, race=None, with_status=False, out=None):
+    """Verification of drafted trees: tokens, parents [B, W], target and draft logits [B, W, V] of their nodes
+    (sdv_tree_verify).  The children of a node were drawn from its draft logits; with draft_logits None they
+    were chosen without chance.  Returns accepted_len [B], path [B, W] (the nodes taken from the root on, -1
+    behind them, as cache_keep takes it), next_token [B], log_ratio [B, W], and status [B] if wanted."""
+    dt = _rows("target_logits", target_logits, 3)
+    Bn, W, V = target_logits.shape
+    if draft_logits is not None and (_rows("draft_logits", draft_logits, 3) != dt or draft_logits.shape != target_logits.shape):
+        raise ValueError("draft_logits: a tensor of the target's type and shape expected")
+    i32, f32, dev = torch.int32, torch.float32, target_logits.device
+    _dense("tokens", tokens, i32, (Bn, W))
+    _dense("parents", parents, i32, (Bn, W))
+    _dense("counts", counts, i32, (Bn,))
+    _dense("coins", coins, f32, (Bn, W))
+    _dense("race", race, f32, (Bn, V))
+    r = _outs(out, ("accepted_len", "next_token", "status") if with_status else ("accepted_len", "next_token"), Bn, i32, dev)
+    r["path"] = _out(out, "path", (Bn, W), i32, dev)
+    r["log_ratio"] = _out(out, "log_ratio", (Bn, W), f32, dev)
+    _here(target_logits, draft_logits, tokens, parents, counts, coins, race, *r.values())
+    db, dr = (0, V) if draft_logits is None else (draft_logits.stride(0), _row_stride(draft_logits))
+    B._call("sdv_tree_verify", target_logits.data_ptr(), target_logits.stride(0), _row_stride(target_logits), _ptr(draft_logits), db,
+            dr, tokens.data_ptr(), parents.data_ptr(), Bn, W, V, dt, float(temperature),
+            float(temperature if draft_temperature is None else draft_temperature), _ptr(counts), int(seed) & 0xFFFFFFFFFFFFFFFF,
+            _ptr(coins), _ptr(race), r["accepted_len"].data_ptr(), r["path"].data_ptr(), r["next_token"].data_ptr(),
+            r["log_ratio"].data_ptr(), _ptr(r.get("status")), _stream())
+    return r
+
+
+def cache_keep(cache, path, page_table, lengths, *, status=None):
+    """Moves the rows of accepted paths [B, W] (tree_verify's) to the places behind the lengths [B] tokens that
+    the cache held before the trees (sdv_cache_keep); status [B] int32 gets bits added to it."""
+    P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, None)
+    W = path.shape[-1]
+    _dense("path", path, torch.int32, (Bn, W))
+    _dense("status", status, torch.int32, (Bn,))
+    _cache_here(cache, path, page_table, lengths, status)
+    B._call("sdv_cache_keep", path.data_ptr(), Bn, W, H, D, block, cache["k"].data_ptr(), cache["v"].data_ptr(),
+            cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr(), P, page_table.data_ptr(), M, lengths.data_ptr(), _ptr(status),
+            _stream())

@@ -34,8 +34,10 @@ SDV_F16 = 2
 SDV_STATUS_EMPTY_ROW = 8
 SDV_STATUS_BAD_TOKEN = 16
 SDV_STATUS_BAD_PAGE = 32
+SDV_STATUS_BAD_TREE = 64
 SDV_MAX_TOP = 32
 SDV_MAX_BLOCK = 128
+SDV_MAX_TREE = 64
 SDV_MAX_COMPONENTS = 16
 SDV_DRAFTER_FREE = 0
 SDV_DRAFTER_FROZEN = 1
@@ -94,6 +96,15 @@ SIGNATURES = {
     "sdv_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
     "sdv_cache_attend": (_I, [_P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
                               _P, _I, _P, _P, _F, _I, _P, _P, _P, _P, _SZ, _P]),
+    "sdv_cache_append_rotary": (_I, [_P, _P, _I64, _I64, _I64, _P, _I64, _I64, _I64, _P, _I64, _I64, _I64,
+                                     _I, _I, _I, _I, _I, _I, _I, _P, _I, _I, _P, _P, _P, _P, _P, _I64, _P,
+                                     _I, _P, _P, _P, _P]),
+    "sdv_tree_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "sdv_tree_attend": (_I, [_P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
+                             _P, _I, _P, _P, _P, _F, _P, _P, _P, _P, _SZ, _P]),
+    "sdv_tree_verify": (_I, [_P, _I64, _I64, _P, _I64, _I64, _P, _P, _I, _I, _I, _I, _F, _F, _P, _U64, _P,
+                             _P, _P, _P, _P, _P, _P, _P]),
+    "sdv_cache_keep": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64, _P, _I, _P, _P, _P]),
     "sdv_timing_enable": (_I, [_I]),
     "sdv_timing_stride": (_I, [_I]),
     "sdv_timing_read": (_I, [_I, _P]),
@@ -151,7 +162,9 @@ def _bind_native(lib):
     for name, fn in (("sdv_verify_ex", mod.verify), ("sdv_verify_pipelined", mod.verify),
                      ("sdv_log_ratios", mod.ratios), ("sdv_token_scores", mod.scores),
                      ("sdv_token_scores_train", mod.train), ("sdv_token_verify", mod.token_verify),
-                     ("sdv_cache_append", mod.append), ("sdv_cache_attend", mod.attend)):
+                     ("sdv_cache_append", mod.append), ("sdv_cache_attend", mod.attend),
+                     ("sdv_cache_append_rotary", mod.append_rotary), ("sdv_tree_attend", mod.tree_attend),
+                     ("sdv_tree_verify", mod.tree_verify), ("sdv_cache_keep", mod.keep)):
         _fns[name] = functools.partial(fn, ctypes.cast(getattr(lib, name), ctypes.c_void_p).value)
 
 
@@ -371,3 +384,39 @@ def sdv_cache_attend(q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, 
     return _call("sdv_cache_attend", q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D,
                  block, k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths,
                  counts, scale, span, out, lse, status, workspace, workspace_bytes, stream)
+
+
+def sdv_cache_append_rotary(k_new, v_new, stride_b, stride_t, stride_h, q, q_stride_b, q_stride_t, q_stride_h,
+                            q_out, out_stride_b, out_stride_t, out_stride_h, dtype, B, W, Hq, H, D, block,
+                            freqs, rot, halves, positions, k_codes, v_codes, k_scale, v_scale, pages,
+                            page_table, max_pages, lengths, counts, status, stream):
+    return _call("sdv_cache_append_rotary", k_new, v_new, stride_b, stride_t, stride_h, q, q_stride_b,
+                 q_stride_t, q_stride_h, q_out, out_stride_b, out_stride_t, out_stride_h, dtype, B, W, Hq, H,
+                 D, block, freqs, rot, halves, positions, k_codes, v_codes, k_scale, v_scale, pages,
+                 page_table, max_pages, lengths, counts, status, stream)
+
+
+def sdv_tree_attend_workspace_bytes(B, W, Hq, H, D):
+    return int(load().sdv_tree_attend_workspace_bytes(B, W, Hq, H, D))
+
+
+def sdv_tree_attend(q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D, block, k_codes, v_codes,
+                    k_scale, v_scale, pages, page_table, max_pages, lengths, parents, counts, scale, out, lse,
+                    status, workspace, workspace_bytes, stream):
+    return _call("sdv_tree_attend", q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D, block,
+                 k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages, lengths, parents, counts,
+                 scale, out, lse, status, workspace, workspace_bytes, stream)
+
+
+def sdv_tree_verify(target, target_stride_b, target_stride_row, draft, draft_stride_b, draft_stride_row,
+                    tokens, parents, B, W, V, dtype, temperature, draft_temperature, counts, seed, coins, race,
+                    accepted_len, path, next_token, log_ratio_out, status_out, stream):
+    return _call("sdv_tree_verify", target, target_stride_b, target_stride_row, draft, draft_stride_b,
+                 draft_stride_row, tokens, parents, B, W, V, dtype, temperature, draft_temperature, counts,
+                 seed, coins, race, accepted_len, path, next_token, log_ratio_out, status_out, stream)
+
+
+def sdv_cache_keep(path, B, W, H, D, block, k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages,
+                   lengths, status, stream):
+    return _call("sdv_cache_keep", path, B, W, H, D, block, k_codes, v_codes, k_scale, v_scale, pages,
+                 page_table, max_pages, lengths, status, stream)

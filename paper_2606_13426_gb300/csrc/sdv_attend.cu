@@ -4,12 +4,13 @@
 namespace sdv {
 
 // prefix[b]: the steps of the sequences before b, b = 0 .. B.
+template <bool kTree>
 __global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendArgs A, int64_t* prefix) {
   __shared__ int64_t warps[kPrefixThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31;
   int64_t before = 0;
   for (int b0 = 0; b0 < A.B; b0 += kPrefixThreads) {
-    const int64_t mine = b0 + tid < A.B ? seq_of(A, b0 + tid).steps : 0;
+    const int64_t mine = b0 + tid < A.B ? seq_of<kTree>(A, b0 + tid).steps : 0;
     int64_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -29,11 +30,13 @@ __global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendAr
   if (tid == 0) prefix[A.B] = before;
 }
 
-// The workspace: the warps' partials, then the sums of the steps.
-struct AttendSpace {
-  size_t part, total;
-};
-static AttendSpace attend_space(int B, int W, int Hq, int H, int D) {
+cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s) {
+  if (A.parents) k_attend_prefix<true><<<1, kPrefixThreads, 0, s>>>(A, prefix);
+  else k_attend_prefix<false><<<1, kPrefixThreads, 0, s>>>(A, prefix);
+  return cudaGetLastError();
+}
+
+AttendSpace attend_space(int B, int W, int Hq, int H, int D) {
   const int nt = row_tiles((int64_t)W * (Hq / H), kMaxNt).nt;             // (no choice of tiles has more)
   const size_t part = ((size_t)sm_count() * kAttendWarps * 2 * 8 * (size_t)nt * (size_t)(D + 2) * 4 + 255) / 256 * 256;
   return AttendSpace{part, part + (B > kPrefixFrom ? ((size_t)B + 1) * sizeof(int64_t) : 0)};
@@ -87,8 +90,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
-    k_attend_prefix<<<1, kPrefixThreads, 0, s>>>(A, prefix);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_attend_prefix(A, prefix, s);
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
   }

@@ -31,6 +31,7 @@
 #pragma once
 
 #include "sdv_cache.cuh"
+#include "sdv_tree.cuh"
 
 namespace sdv {
 
@@ -70,6 +71,7 @@ struct AttendArgs {
   int B, W, G, R, RT;                      // rows W * G, row tiles
   const int32_t* lengths;
   const int32_t* counts;
+  const int32_t* parents;                  // [B, W]: the window is a tree (kTree), else NULL
   float scale2;                            // scale * log2(e)
   int span;
   void* out;
@@ -85,11 +87,13 @@ struct Seq {
   int len, count, first, steps;            // first: the first step that a query sees
   int begin;                               // the first key that one sees
 };
+template <bool kTree>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   Seq s;
   const int cap = A.c.max_pages * A.c.block;
   s.len = min(max(A.lengths[b], 0), cap);
   s.count = min(max(A.counts ? A.counts[b] : A.W, 0), A.W);
+  if (kTree && s.count > s.len) s.count = 0;             // more nodes than tokens
   s.begin = A.span > 0 ? max(0, s.len - s.count - A.span + 1) : 0;
   s.first = s.begin / kSub;
   s.steps = s.count && s.len ? (s.len + kSub - 1) / kSub - s.first : 0;
@@ -101,11 +105,12 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
 struct Sums {
   int64_t before, total;
 };
+template <bool kTree>
 __device__ __forceinline__ Sums step_sums(const AttendArgs& A, int b, int lane) {
   if (A.prefix) return Sums{A.prefix[b], A.prefix[A.B]};
   Sums s{0, 0};
   for (int i = lane; i < A.B; i += 32) {
-    const int t = seq_of(A, i).steps;
+    const int t = seq_of<kTree>(A, i).steps;
     s.total += t;
     if (i < b) s.before += t;
   }
@@ -122,6 +127,7 @@ struct Found {
   int b;
   int64_t before;
 };
+template <bool kTree>
 __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, int lane) {
   if (A.prefix) {                                           // the last b with prefix[b] <= u, 32 places at a time
     int lo = 0, hi = A.B;                                   // prefix[lo] <= u < prefix[hi]
@@ -137,7 +143,7 @@ __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, i
   }
   int64_t before = 0;
   for (int b0 = 0; b0 < A.B; b0 += 32) {
-    const int64_t mine = b0 + lane < A.B ? seq_of(A, b0 + lane).steps : 0;
+    const int64_t mine = b0 + lane < A.B ? seq_of<kTree>(A, b0 + lane).steps : 0;
     int64_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -209,7 +215,7 @@ __device__ __forceinline__ float lse_of(float m, float l, float base) {
 // A warp's ring holds kHalves half steps (32 keys, or their values): one in use, the others, 8 KB, under
 // way; its queries' fragments are beside it.  (Four under way at D = 128, where few rows leave room: within
 // 2 % either way for 4 to 36 rows.)
-template <int kD, int kNt>
+template <int kD, int kNt, bool kTree = false>
 struct AttendShape {
   static constexpr int kWarps = kAttendWarps;
   static constexpr int kThreads = 32 * kWarps;
@@ -223,7 +229,8 @@ struct AttendShape {
   static constexpr int kQBytes = kRows * kD * 2;
   static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
   static constexpr int kRowBytes = kRows * 12;            // of a row: the sum's reference, the score's base, the query's power of two
-  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRowBytes;
+  static constexpr int kSetBytes = kTree ? SDV_MAX_TREE * 8 : 0;   // of a node: what it sees of the tree
+  static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRowBytes + kSetBytes;
   static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
   static_assert(kHalves % 2 == 1 && kSmem <= 227 * 1024, "");
 };
@@ -261,9 +268,11 @@ __device__ __forceinline__ float q_largest(uint4 v, bool bf16) {
 // The probabilities go into the second product as a sum of two f16, 22 bits: with one, f16 outputs were off by as much
 // as their own rounding again (2.9e-4 of their size, 2.0e-4 with two), and bf16 outputs were roundings of numbers
 // up to 2^-12 off, so that some fell on the neighbouring value.  The second half costs those windows 48 us, few rows nothing.
-template <int kD, int kNt>
-__global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(const AttendArgs A) {
-  using S = AttendShape<kD, kNt>;
+// kTree: the window's queries are the nodes of a tree (sdv_tree.cuh), each of which sees the tokens before the window, the nodes
+// above it and itself; whole steps before the window are as they are for a chain.
+template <int kD, int kNt, bool kTree>
+__global__ void __launch_bounds__(AttendShape<kD, kNt, kTree>::kThreads, 1) k_attend(const AttendArgs A) {
+  using S = AttendShape<kD, kNt, kTree>;
   constexpr int kKv = S::kKv;
   constexpr int kMt = kD / 16;                             // sixteens of the output
   constexpr int kR = 2 * kNt;                              // rows of a thread: 8 n + 2 t + e
@@ -276,8 +285,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   float* refs = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes);   // the sums', where they are kept apart
   float* bases = refs + S::kRows;
   float* downs = bases + S::kRows;
+  uint64_t* sets = reinterpret_cast<uint64_t*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes + S::kRowBytes);
 
-  const int64_t units = step_sums(A, 0, lane).total * per;
+  const int64_t units = step_sums<kTree>(A, 0, lane).total * per;
   const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);   // none of them empty
   // neighbours in the order of the runs sit on different SMs when there are few
   const int run = runs < A.ctas * S::kWarps ? warp * A.ctas + (int)blockIdx.x : (int)blockIdx.x * S::kWarps + warp;
@@ -285,22 +295,22 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
   int64_t u = run_start(units, run, runs);
   const int64_t u_end = run_start(units, run + 1, runs);
   // the sequence that holds unit u, and the unit of its first step
-  Found at_u = find_sequence(A, u / per, lane);
+  Found at_u = find_sequence<kTree>(A, u / per, lane);
   int b = at_u.b;
   int64_t seq_u = at_u.before * per;
   bool first_segment = true;
   while (u < u_end && b < A.B) {
-    Seq sq = seq_of(A, b);
+    Seq sq = seq_of<kTree>(A, b);
     if (u >= seq_u + (int64_t)sq.steps * per) {              // on to the next sequence, or over empty ones
       seq_u += (int64_t)sq.steps * per;
       if (++b == A.B) break;
-      sq = seq_of(A, b);
+      sq = seq_of<kTree>(A, b);
       if (!sq.steps) {
-        at_u = find_sequence(A, u / per, lane);
+        at_u = find_sequence<kTree>(A, u / per, lane);
         b = at_u.b;
         if (b == A.B) break;
         seq_u = at_u.before * per;
-        sq = seq_of(A, b);
+        sq = seq_of<kTree>(A, b);
       }
     }
     if (u < seq_u || u >= seq_u + (int64_t)sq.steps * per) break;   // (only if the lengths have changed meanwhile)
@@ -440,6 +450,15 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
           put(p, v, mine);
         }
       }
+      if constexpr (kTree) {
+        bool bad = false;
+        const int32_t* parents = A.parents + (int64_t)b * A.W;
+        uint64_t a0, a1;
+        ancestors(lane < A.W ? parent_of(parents[lane], lane, bad) : -1, 32 + lane < A.W ? parent_of(parents[32 + lane], 32 + lane, bad) : -1,
+                  lane, a0, a1);
+        sets[lane] = a0;
+        sets[32 + lane] = a1;
+      }
       __syncwarp();
     }
     const float most_score = amax * (448.f * kD) * fabsf(A.scale2);   // times a key's scale
@@ -449,7 +468,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
     // the window's rows of this item: the last key that all of them see, the first that one does not
     const int at0 = sq.len - sq.count;                     // position of the window's first query
     const int i0 = row0 / A.G, i1 = min((min(row0 + S::kRows, A.R) - 1) / A.G, sq.count - 1);
-    const int min_last = at0 + i0, max_begin = A.span > 0 ? at0 + i1 - A.span + 1 : 0;
+    const int min_last = kTree ? at0 - 1 : at0 + i0, max_begin = A.span > 0 ? at0 + i1 - A.span + 1 : 0;
     const int max_last = at0 + i1, min_begin = A.span > 0 ? at0 + i0 - A.span + 1 : 0;   // and what any of them sees
     float acc[kMt][kNt][4];
     float mx[kR], sum[kR];                                 // (mx: of p', so kLogPScale below the largest)
@@ -599,13 +618,15 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
         for (int k = 0; k < kR; ++k) {
           const int row = row0 + 8 * (k >> 1) + 2 * t + (k & 1);
           const int last = at0 + row / A.G, begin = A.span > 0 ? last - A.span + 1 : 0;
+          const uint64_t set = kTree ? sets[min(row / A.G, SDV_MAX_TREE - 1)] : 0;
 #pragma unroll
           for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int tok = 4 * s + 2 * e + (g & 1), key = key0 + 8 * (g >> 1) + tok;
               float& x = sx[s][k >> 1][2 * e + (k & 1)];
-              if (key > last || key < begin || !here) x = -INFINITY;
+              const bool hidden = kTree ? key >= at0 && (key > last || !(set >> ((key - at0) & 63) & 1)) : key > last || key < begin;
+              if (hidden || !here) x = -INFINITY;
               else if (nan_keys >> tok & 1) x = NAN;
             }
         }
@@ -787,9 +808,9 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt>::kThreads, 1) k_attend(co
 // kSplit: a CTA has one row, and its warps take the partials in turn (few items, many partials of
 // each); otherwise a warp has a row.  Bound by latency: 6 to 14 us.  Whole calls with 16
 // items of 76 partials and 8 rows take 98 us split and 114 not, with 256 of 5 partials 104 and 99 (4 rows) or 301 and 259 (36).
-template <int kD, int kNt, bool kSplit>
+template <int kD, int kNt, bool kSplit, bool kTree>
 __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A) {
-  using S = AttendShape<kD, kNt>;
+  using S = AttendShape<kD, kNt, kTree>;
   constexpr int kV = kD / 32;                                // elements of a lane
   __shared__ float wo[kSplit ? kJoinWarps : 1][kD];
   __shared__ float wl[kJoinWarps];
@@ -799,12 +820,17 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const AttendArgs A
   const int ib = blockIdx.x / ctas;
   const int r = kSplit ? blockIdx.x % ctas : blockIdx.x % ctas * 8 + warp;
   const int b = ib / per, item = ib % per, h = item / A.RT, row = item % A.RT * S::kRows + r;
-  const Sums ts = step_sums(A, b, lane);
+  const Sums ts = step_sums<kTree>(A, b, lane);
   // the partials are there; CTAs without work wait as well, so that this kernel ends after k_attend
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (A.status && threadIdx.x == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
+  if (kTree && A.status && warp == 0 && item == 0) {          // a tree that is none
+    bool bad = lane == 0 && A.lengths[b] < min(A.counts ? A.counts[b] : A.W, A.W);
+    for (int i = lane; i < min(A.counts ? A.counts[b] : A.W, A.W); i += 32) parent_of(A.parents[(int64_t)b * A.W + i], i, bad);
+    if (bad) atomicOr(A.status + b, SDV_STATUS_BAD_TREE);
+  }
   if (row >= A.R) return;
-  const Seq sq = seq_of(A, b);
+  const Seq sq = seq_of<kTree>(A, b);
   const int64_t units = ts.total * per, u0 = ts.before * per + (int64_t)item * sq.steps;
   const int64_t u1 = min(u0 + sq.steps, units);              // (never past them, unless the lengths have changed meanwhile)
   const int runs = run_count(units, (int64_t)A.B * per, A.ctas * S::kWarps);
@@ -893,10 +919,10 @@ inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, i
   return best;
 }
 
-template <int kD, int kNt>
+template <int kD, int kNt, bool kTree>
 static cudaError_t launch_attend(const AttendArgs& A, cudaStream_t s) {
-  using S = AttendShape<kD, kNt>;
-  const auto attend = k_attend<kD, kNt>;
+  using S = AttendShape<kD, kNt, kTree>;
+  const auto attend = k_attend<kD, kNt, kTree>;
   cudaError_t e = cudaFuncSetAttribute(attend, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
   attend<<<(unsigned)A.ctas, S::kThreads, S::kSmem, s>>>(A);
@@ -914,20 +940,31 @@ static cudaError_t launch_attend(const AttendArgs& A, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return split ? cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, true>, A) : cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, false>, A);
+  return split ? cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, true, kTree>, A) : cudaLaunchKernelEx(&cfg, k_attend_join<kD, kNt, false, kTree>, A);
 }
 
-template <int kD>
+template <int kD, bool kTree = false>
 cudaError_t launch_attend_d(const AttendArgs& A, int nt, cudaStream_t s) {
   switch (nt) {
-    case 1: return launch_attend<kD, 1>(A, s);
-    case 2: return launch_attend<kD, 2>(A, s);
-    case 3: return launch_attend<kD, 3>(A, s);
-    case 4: return launch_attend<kD, 4>(A, s);
-    default: return launch_attend<kD, 5>(A, s);
+    case 1: return launch_attend<kD, 1, kTree>(A, s);
+    case 2: return launch_attend<kD, 2, kTree>(A, s);
+    case 3: return launch_attend<kD, 3, kTree>(A, s);
+    case 4: return launch_attend<kD, 4, kTree>(A, s);
+    default: return launch_attend<kD, 5, kTree>(A, s);
   }
 }
 cudaError_t launch_attend_64(const AttendArgs& A, int nt, cudaStream_t s);
 cudaError_t launch_attend_128(const AttendArgs& A, int nt, cudaStream_t s);
+cudaError_t launch_tree_attend_64(const AttendArgs& A, int nt, cudaStream_t s);
+cudaError_t launch_tree_attend_128(const AttendArgs& A, int nt, cudaStream_t s);
+
+// The steps before each sequence, by a kernel (many sequences).
+cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s);
+
+// The workspace: the warps' partials, then the sums of the steps.
+struct AttendSpace {
+  size_t part, total;
+};
+AttendSpace attend_space(int B, int W, int Hq, int H, int D);
 
 }  // namespace sdv

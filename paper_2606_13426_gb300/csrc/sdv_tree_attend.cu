@@ -1,0 +1,56 @@
+// sdv_tree_attend.cu - the entry points of the attention of a drafted tree over the 8-bit cache.
+#include "sdv_attend.cuh"
+
+using namespace sdv;
+
+extern "C" {
+
+size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D) {
+  if (B < 1 || W < 1 || W > SDV_MAX_TREE || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
+  return attend_space(B, W, Hq, H, D).total;
+}
+
+int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int dtype, int B, int W, int Hq,
+                    int H, int D, int block, const void* k_codes, const void* v_codes, const float* k_scale,
+                    const float* v_scale, int64_t pages, const int32_t* page_table, int max_pages, const int32_t* lengths,
+                    const int32_t* parents, const int32_t* counts, float scale, void* out, float* lse, uint32_t* status,
+                    void* workspace, size_t workspace_bytes, sdv_stream_t stream) {
+  if ((dtype != SDV_BF16 && dtype != SDV_F16) || B < 1 || W < 1 || W > SDV_MAX_TREE || H < 1 || Hq < H || Hq % H || !q || !lengths ||
+      !parents || !out)
+    return SDV_EINVAL;
+  int rc = check_cache(k_codes, v_codes, k_scale, v_scale, pages, page_table, max_pages, H, D, block);
+  if (rc) return rc;
+  if (q_stride_b < 0 || q_stride_t < 0 || q_stride_h < 0 || !(fabsf(scale) < INFINITY)) return SDV_EINVAL;
+  const int64_t R = (int64_t)W * (Hq / H);
+  if (R > (1 << 24) || (int64_t)B * H * ((R + 7) / 8 + kMaxNt) > 0x7fffffff) return SDV_EINVAL;
+  if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(status, 4) || !aligned_to(lengths, 4) ||
+      !aligned_to(parents, 4) || !aligned_to(counts, 4))
+    return SDV_EALIGN;
+  const AttendSpace space = attend_space(B, W, Hq, H, D);
+  if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
+  if (!aligned_to(workspace, 256)) return SDV_EALIGN;
+  AttendArgs A{};
+  const RowTiles tiles = choose_tiles(R, (int64_t)B * H, ((int64_t)max_pages * block + kSub - 1) / kSub, D, sm_count() * kAttendWarps);
+  A.q = q;
+  A.bf16 = dtype == SDV_BF16;
+  A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
+  A.q_sb = q_stride_b, A.q_st = q_stride_t, A.q_sh = q_stride_h;
+  A.c = CacheView{(uint8_t*)k_codes, (uint8_t*)v_codes, (float*)k_scale, (float*)v_scale, page_table, pages, max_pages, H, D, block};
+  A.cpb = chunk_div(block / kChunk);
+  A.B = B, A.W = W, A.G = Hq / H, A.R = (int)R, A.RT = tiles.rt;
+  A.lengths = lengths, A.counts = counts, A.parents = parents;
+  A.scale2 = scale * kLog2E;
+  A.out = out, A.lse = lse, A.status = status;
+  A.part = (float*)workspace;
+  A.ctas = sm_count();
+  cudaStream_t s = (cudaStream_t)stream;
+  if (B > kPrefixFrom) {
+    int64_t* prefix = (int64_t*)((char*)workspace + space.part);
+    const cudaError_t e = launch_attend_prefix(A, prefix, s);
+    if (e != cudaSuccess) return launched(e);
+    A.prefix = prefix;
+  }
+  return launched(D == 64 ? launch_tree_attend_64(A, tiles.nt, s) : launch_tree_attend_128(A, tiles.nt, s));
+}
+
+}  // extern "C"
