@@ -409,6 +409,7 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
 #define SDV_STATUS_BAD_PAGE  32u   /* a page outside the cache, or a token past the page table */
 
 #define SDV_STATUS_BAD_TREE  64u   /* a parent that does not come before its child, or a path that leaves the tree */
+#define SDV_STATUS_STUCK    128u   /* (never, as far as is known) a kernel gave up waiting for its own parts: its results are none */
 
 #define SDV_MAX_TOP   32       /* largest number of alternatives */
 #define SDV_MAX_TREE  64       /* largest number of nodes of a drafted tree */

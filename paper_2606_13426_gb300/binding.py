@@ -35,6 +35,7 @@ SDV_STATUS_EMPTY_ROW = 8
 SDV_STATUS_BAD_TOKEN = 16
 SDV_STATUS_BAD_PAGE = 32
 SDV_STATUS_BAD_TREE = 64
+SDV_STATUS_STUCK = 128
 SDV_MAX_TOP = 32
 SDV_MAX_BLOCK = 128
 SDV_MAX_TREE = 64

@@ -4,13 +4,13 @@
 namespace sdv {
 
 // prefix[b]: the steps of the sequences before b, b = 0 .. B.
-template <bool kTree>
+template <bool kTree, int kStep>
 __global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendArgs A, int64_t* prefix) {
   __shared__ int64_t warps[kPrefixThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31;
   int64_t before = 0;
   for (int b0 = 0; b0 < A.B; b0 += kPrefixThreads) {
-    const int64_t mine = b0 + tid < A.B ? seq_of<kTree>(A, b0 + tid).steps : 0;
+    const int64_t mine = b0 + tid < A.B ? seq_of<kTree, kStep>(A, b0 + tid).steps : 0;
     int64_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -30,9 +30,9 @@ __global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendAr
   if (tid == 0) prefix[A.B] = before;
 }
 
-cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s) {
-  if (A.parents) k_attend_prefix<true><<<1, kPrefixThreads, 0, s>>>(A, prefix);
-  else k_attend_prefix<false><<<1, kPrefixThreads, 0, s>>>(A, prefix);
+cudaError_t launch_attend_prefix(const AttendArgs& A, int step, int64_t* prefix, cudaStream_t s) {
+  const auto kern = !A.parents ? k_attend_prefix<false, kSub> : step == kSub ? k_attend_prefix<true, kSub> : k_attend_prefix<true, kTileKeys>;
+  kern<<<1, kPrefixThreads, 0, s>>>(A, prefix);
   return cudaGetLastError();
 }
 
@@ -90,7 +90,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
-    const cudaError_t e = launch_attend_prefix(A, prefix, s);
+    const cudaError_t e = launch_attend_prefix(A, kSub, prefix, s);
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
   }

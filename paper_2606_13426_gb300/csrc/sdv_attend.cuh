@@ -36,6 +36,7 @@
 namespace sdv {
 
 constexpr int kSub = 32;                  // keys of a step
+constexpr int kTileKeys = 128;            // of a step of the kernels for many rows
 constexpr int kJoinWarps = 8;
 constexpr int kJoinThreads = 32 * kJoinWarps;
 constexpr int kMinSteps = 2;              // of a run, where there are fewer steps than warps could take (but see run_count)
@@ -64,7 +65,7 @@ inline ChunkDiv chunk_div(int n) { return ChunkDiv{n == 1 ? 0u : (uint32_t)((0x1
 
 struct AttendArgs {
   const void* q;
-  bool bf16, q_vec;                        // queries in whole aligned vectors of 16 bytes
+  bool bf16, q_vec, out_vec;               // queries, outputs in whole aligned vectors of 16 bytes
   int64_t q_sb, q_st, q_sh;
   CacheView c;
   ChunkDiv cpb;
@@ -87,7 +88,7 @@ struct Seq {
   int len, count, first, steps;            // first: the first step that a query sees
   int begin;                               // the first key that one sees
 };
-template <bool kTree>
+template <bool kTree, int kStep = kSub>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   Seq s;
   const int cap = A.c.max_pages * A.c.block;
@@ -95,8 +96,8 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   s.count = min(max(A.counts ? A.counts[b] : A.W, 0), A.W);
   if (kTree && s.count > s.len) s.count = 0;             // more nodes than tokens
   s.begin = A.span > 0 ? max(0, s.len - s.count - A.span + 1) : 0;
-  s.first = s.begin / kSub;
-  s.steps = s.count && s.len ? (s.len + kSub - 1) / kSub - s.first : 0;
+  s.first = s.begin / kStep;
+  s.steps = s.count && s.len ? (s.len + kStep - 1) / kStep - s.first : 0;
   return s;
 }
 
@@ -105,12 +106,12 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
 struct Sums {
   int64_t before, total;
 };
-template <bool kTree>
+template <bool kTree, int kStep = kSub>
 __device__ __forceinline__ Sums step_sums(const AttendArgs& A, int b, int lane) {
   if (A.prefix) return Sums{A.prefix[b], A.prefix[A.B]};
   Sums s{0, 0};
   for (int i = lane; i < A.B; i += 32) {
-    const int t = seq_of<kTree>(A, i).steps;
+    const int t = seq_of<kTree, kStep>(A, i).steps;
     s.total += t;
     if (i < b) s.before += t;
   }
@@ -127,7 +128,7 @@ struct Found {
   int b;
   int64_t before;
 };
-template <bool kTree>
+template <bool kTree, int kStep = kSub>
 __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, int lane) {
   if (A.prefix) {                                           // the last b with prefix[b] <= u, 32 places at a time
     int lo = 0, hi = A.B;                                   // prefix[lo] <= u < prefix[hi]
@@ -143,7 +144,7 @@ __device__ __forceinline__ Found find_sequence(const AttendArgs& A, int64_t u, i
   }
   int64_t before = 0;
   for (int b0 = 0; b0 < A.B; b0 += 32) {
-    const int64_t mine = b0 + lane < A.B ? seq_of<kTree>(A, b0 + lane).steps : 0;
+    const int64_t mine = b0 + lane < A.B ? seq_of<kTree, kStep>(A, b0 + lane).steps : 0;
     int64_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -959,12 +960,17 @@ cudaError_t launch_tree_attend_64(const AttendArgs& A, int nt, cudaStream_t s);
 cudaError_t launch_tree_attend_128(const AttendArgs& A, int nt, cudaStream_t s);
 
 // The steps before each sequence, by a kernel (many sequences).
-cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s);
+cudaError_t launch_attend_prefix(const AttendArgs& A, int step, int64_t* prefix, cudaStream_t s);
 
 // The workspace: the warps' partials, then the sums of the steps.
 struct AttendSpace {
   size_t part, total;
 };
 AttendSpace attend_space(int B, int W, int Hq, int H, int D);
+
+// The kernels for many rows of a key head (sdv_tree_rows.cuh), in tiles of `rows` of them.
+cudaError_t launch_tree_rows_64(const AttendArgs& A, int rows, cudaStream_t s);
+cudaError_t launch_tree_rows_128(const AttendArgs& A, int rows, cudaStream_t s);
+size_t tree_rows_part(int D);                            // bytes of their partials
 
 }  // namespace sdv

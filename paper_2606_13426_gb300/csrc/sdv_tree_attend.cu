@@ -1,13 +1,31 @@
 // sdv_tree_attend.cu - the entry points of the attention of a drafted tree over the 8-bit cache.
 #include "sdv_attend.cuh"
 
+namespace sdv {
+
+// Rows of a key head from which on the matrix unit's kernels take them.
+static bool many_rows(int64_t R, int D) { return R > (D == 128 ? 16 : 32) && (R + 127) / 128 <= sm_count(); }
+
+static AttendSpace tree_space(int B, int W, int Hq, int H, int D) {
+  AttendSpace space = attend_space(B, W, Hq, H, D);
+  const size_t part = many_rows((int64_t)W * (Hq / H), D) ? tree_rows_part(D) : 0;
+  if (part > space.part) {
+    space.total += part - space.part;
+    space.part = part;
+  }
+  return space;
+}
+size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * 128 * (size_t)(D + 2) * 4 / 256 * 256 + 256; }
+
+}  // namespace sdv
+
 using namespace sdv;
 
 extern "C" {
 
 size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D) {
   if (B < 1 || W < 1 || W > SDV_MAX_TREE || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
-  return attend_space(B, W, Hq, H, D).total;
+  return tree_space(B, W, Hq, H, D).total;
 }
 
 int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int dtype, int B, int W, int Hq,
@@ -26,14 +44,17 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(status, 4) || !aligned_to(lengths, 4) ||
       !aligned_to(parents, 4) || !aligned_to(counts, 4))
     return SDV_EALIGN;
-  const AttendSpace space = attend_space(B, W, Hq, H, D);
+  const AttendSpace space = tree_space(B, W, Hq, H, D);
   if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   AttendArgs A{};
-  const RowTiles tiles = choose_tiles(R, (int64_t)B * H, ((int64_t)max_pages * block + kSub - 1) / kSub, D, sm_count() * kAttendWarps);
+  const bool many = many_rows(R, D);
+  const RowTiles tiles = many ? RowTiles{(int)((R + 127) / 128), 0}
+                              : choose_tiles(R, (int64_t)B * H, ((int64_t)max_pages * block + kSub - 1) / kSub, D, sm_count() * kAttendWarps);
   A.q = q;
   A.bf16 = dtype == SDV_BF16;
   A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
+  A.out_vec = aligned_to(out, 16);
   A.q_sb = q_stride_b, A.q_st = q_stride_t, A.q_sh = q_stride_h;
   A.c = CacheView{(uint8_t*)k_codes, (uint8_t*)v_codes, (float*)k_scale, (float*)v_scale, page_table, pages, max_pages, H, D, block};
   A.cpb = chunk_div(block / kChunk);
@@ -46,9 +67,13 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
-    const cudaError_t e = launch_attend_prefix(A, prefix, s);
+    const cudaError_t e = launch_attend_prefix(A, many ? kTileKeys : kSub, prefix, s);
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
+  }
+  if (many) {
+    const int rows = (int)((R + tiles.rt - 1) / tiles.rt);
+    return launched(D == 64 ? launch_tree_rows_64(A, rows, s) : launch_tree_rows_128(A, rows, s));
   }
   return launched(D == 64 ? launch_tree_attend_64(A, tiles.nt, s) : launch_tree_attend_128(A, tiles.nt, s));
 }
