@@ -30,8 +30,8 @@ __global__ void __launch_bounds__(kPrefixThreads) k_attend_prefix(const AttendAr
   if (tid == 0) prefix[A.B] = before;
 }
 
-cudaError_t launch_attend_prefix(const AttendArgs& A, int step, int64_t* prefix, cudaStream_t s) {
-  const auto kern = !A.parents ? k_attend_prefix<false, kSub> : step == kSub ? k_attend_prefix<true, kSub> : k_attend_prefix<true, kTileKeys>;
+cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s) {
+  const auto kern = !A.parents ? k_attend_prefix<false, kSub> : !A.step ? k_attend_prefix<true, kSub> : k_attend_prefix<true, 0>;
   kern<<<1, kPrefixThreads, 0, s>>>(A, prefix);
   return cudaGetLastError();
 }
@@ -90,7 +90,7 @@ int sdv_cache_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int6
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
-    const cudaError_t e = launch_attend_prefix(A, kSub, prefix, s);
+    const cudaError_t e = launch_attend_prefix(A, prefix, s);
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
   }

@@ -36,7 +36,7 @@
 namespace sdv {
 
 constexpr int kSub = 32;                  // keys of a step
-constexpr int kTileKeys = 128;            // of a step of the kernels for many rows
+constexpr int kTileKeys = 128;            // of a step of the kernels for many rows, at most: whole pages
 constexpr int kJoinWarps = 8;
 constexpr int kJoinThreads = 32 * kJoinWarps;
 constexpr int kMinSteps = 2;              // of a run, where there are fewer steps than warps could take (but see run_count)
@@ -78,6 +78,7 @@ struct AttendArgs {
   void* out;
   float* lse;
   uint32_t* status;
+  int step;                                // keys of a step (the kernels for many rows)
   const int64_t* prefix;                   // workspace: steps before each sequence, or NULL (few sequences)
   float* part;                             // workspace: 2 slots a warp
   int ctas;
@@ -88,6 +89,7 @@ struct Seq {
   int len, count, first, steps;            // first: the first step that a query sees
   int begin;                               // the first key that one sees
 };
+// kStep: keys of a step, or 0: A.step of them.
 template <bool kTree, int kStep = kSub>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   Seq s;
@@ -96,8 +98,9 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& A, int b) {
   s.count = min(max(A.counts ? A.counts[b] : A.W, 0), A.W);
   if (kTree && s.count > s.len) s.count = 0;             // more nodes than tokens
   s.begin = A.span > 0 ? max(0, s.len - s.count - A.span + 1) : 0;
-  s.first = s.begin / kStep;
-  s.steps = s.count && s.len ? (s.len + kStep - 1) / kStep - s.first : 0;
+  const int step = kStep ? kStep : A.step;
+  s.first = s.begin / step;
+  s.steps = s.count && s.len ? (s.len + step - 1) / step - s.first : 0;
   return s;
 }
 
@@ -960,7 +963,7 @@ cudaError_t launch_tree_attend_64(const AttendArgs& A, int nt, cudaStream_t s);
 cudaError_t launch_tree_attend_128(const AttendArgs& A, int nt, cudaStream_t s);
 
 // The steps before each sequence, by a kernel (many sequences).
-cudaError_t launch_attend_prefix(const AttendArgs& A, int step, int64_t* prefix, cudaStream_t s);
+cudaError_t launch_attend_prefix(const AttendArgs& A, int64_t* prefix, cudaStream_t s);
 
 // The workspace: the warps' partials, then the sums of the steps.
 struct AttendSpace {

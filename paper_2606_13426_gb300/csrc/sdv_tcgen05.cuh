@@ -7,14 +7,9 @@
 
 namespace sdv {
 
-// ---- mbarriers.  Every wait gives up after kWaitMost nanoseconds, upon which the kernel ends with an error.
-constexpr uint64_t kWaitMost = 2000000000ull;
-
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
+// ---- mbarriers.  Every wait gives up after kWaitMost clocks (two seconds), upon which the kernel ends with an error.
+constexpr long long kWaitMost = 4000000000ll;
+constexpr uint32_t kWaitHint = 1000000;           // nanoseconds that a waiting warp may sleep
 
 __device__ __forceinline__ void barrier_init(uint64_t* bar, int count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
@@ -25,27 +20,37 @@ __device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
 __device__ __forceinline__ bool barrier_try(uint64_t* bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
-      "{ .reg .pred p;\n  mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n  selp.b32 %0, 1, 0, p; }"
+      "{ .reg .pred p;\n  mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n  selp.b32 %0, 1, 0, p; }"
       : "=r"(done)
-      : "r"(smem_addr(bar)), "r"(parity)
+      : "r"(smem_addr(bar)), "r"(parity), "r"(kWaitHint)
       : "memory");
   return done;
 }
 // Waits for the phase of that parity; false if it gave up, or another thread did (*dead).
 __device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity, volatile int* dead) {
   if (barrier_try(bar, parity)) return true;
-  const uint64_t since = now_ns();
+  const long long since = clock64();
 #pragma unroll 1
   do {
     if (barrier_try(bar, parity)) return true;
     if (*dead) return false;
-  } while (now_ns() - since < kWaitMost);
+  } while (clock64() - since < kWaitMost);
   *dead = 1;
   return false;
 }
 // What this thread wrote to shared memory is there for the matrix unit.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// ---- copies of whole vectors of 16 bytes from global to shared memory, which the barrier counts
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {   // an arrival that waits for them
+  asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes),
+               "r"(smem_addr(bar))
+               : "memory");
+}
 
 // ---- tensor memory: 128 lanes of 512 columns of 32 bits
 __device__ __forceinline__ void tmem_alloc(uint32_t* to, int columns) {          // by one warp
@@ -57,6 +62,13 @@ __device__ __forceinline__ void tmem_free(uint32_t at, int columns) {           
 }
 __device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// The largest of three.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 
 #define SDV_R4(x, i) x(i), x(i + 1), x(i + 2), x(i + 3)
 #define SDV_R16(x, i) SDV_R4(x, i), SDV_R4(x, i + 4), SDV_R4(x, i + 8), SDV_R4(x, i + 12)
@@ -84,6 +96,12 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
       "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
       SDV_R32(SDV_IN)
       : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+      SDV_R16(SDV_IN, 0)
+      : "memory");
 #undef SDV_IN
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -99,6 +117,12 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t at) {
 __host__ __device__ constexpr uint32_t mma_desc(int type, int m, int n) {
   return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
+// One lane of a warp whose lanes are all here.
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{ .reg .pred p;\n  elect.sync _|p, 0xffffffff;\n  selp.b32 %0, 1, 0, p; }" : "=r"(yes));
+  return yes;
+}
 // d (tensor memory) = a b' (+ d): 16 of K; a in shared memory, or in tensor memory.  By one thread.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
   asm volatile("{ .reg .pred p;\n  setp.ne.b32 p, %4, 0;\n  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a),
@@ -109,6 +133,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
   asm volatile("{ .reg .pred p;\n  setp.ne.b32 p, %4, 0;\n  tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a),
                "l"(b), "r"(desc), "r"((uint32_t)add)
                : "memory");
+}
+// Registers of a thread of this warp's four, from here on (sums over the block's warps stay within its launch).
+template <int kN>
+__device__ __forceinline__ void registers_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN));
+}
+template <int kN>
+__device__ __forceinline__ void registers_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN));
 }
 // The barrier gets an arrival when all that this thread has issued before is done.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {

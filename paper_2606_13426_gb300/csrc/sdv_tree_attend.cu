@@ -15,7 +15,7 @@ static AttendSpace tree_space(int B, int W, int Hq, int H, int D) {
   }
   return space;
 }
-size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * 128 * (size_t)(D + 2) * 4 / 256 * 256 + 256; }
+size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * 128 * (size_t)(D + 3) * 4 / 256 * 256 + 256; }
 
 }  // namespace sdv
 
@@ -64,10 +64,11 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   A.out = out, A.lse = lse, A.status = status;
   A.part = (float*)workspace;
   A.ctas = sm_count();
+  A.step = many ? kTileKeys / block * block : 0;
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
-    const cudaError_t e = launch_attend_prefix(A, many ? kTileKeys : kSub, prefix, s);
+    const cudaError_t e = launch_attend_prefix(A, prefix, s);
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
   }

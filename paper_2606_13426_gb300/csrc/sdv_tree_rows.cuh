@@ -1,17 +1,20 @@
 // sdv_tree_rows.cuh - the tree attention for many rows, on the fifth-generation matrix unit.
 //
-// A CTA takes up to 128 rows (nodes times the query heads of a key head) through the keys in steps of 128:
+// A CTA takes up to 128 rows (nodes times the query heads of a key head) through the keys in steps of whole pages, up to 128
+// keys:
 //   S = Q K' (tensor memory, fp32), P = 2^(S f - m) vs, O += P V.
 // A row is a lane of tensor memory and a thread of a softmax warp, so that its maximum and sum need no exchange; a page's
 // scales are one number for 16 keys or more.  Three kinds of warps work at once:
-//   * loading warps read codes (registers, a step ahead) and widen them into the matrix unit's operands:
-//     keys to f16 (exact, NaN stays NaN), values to bf16 (exact: an e4m3 code is a bf16 number times 2^120);
-//   * one thread issues the products;
+//   * one warp plans: which part of which item comes next;
+//   * one warp copies: a step's pages of codes, in bulk, into rings of steps of keys and of values;
+//   * loading warps widen them to f16 (exactly; a value's NaN becomes 0 and is told apart), the matrix unit's operands;
+//   * one warp issues the products;
 //   * two groups of softmax warps take the steps in turn, each with scores and sums of its own, joined at the
 //     end of a segment.
 // Queries go through f16: bf16 ones under a power of two of their row.  Probabilities times their value's scale
-// stand in tensor memory in place of their scores, as the sum of two bf16 (2^-17 of each; bf16 has fp32's range, so
-// that no page's scale costs another page's bits).
+// stand in tensor memory in place of their scores, as the sum of two f16: 22 bits, or 2^-32 of the row's largest.  So that they
+// fit f16 whatever the scales of other pages, a row's reference m is taken on the score plus log2 of that scale;
+// the sum of 2^(S f - m) is had from the same exponentials, in fp32.
 //
 // The steps of all (sequence, head) items, laid end to end, are cut into equal runs, one for each team of as many CTAs as
 // an item has tiles of 128 rows: a team's CTAs read the same keys at about the same time, so that DRAM gives them once.
@@ -23,13 +26,17 @@
 namespace sdv {
 
 constexpr int kTileRows = 128;
-constexpr int kSoftWarps = 8, kLoadWarps = 8;
-constexpr int kTreeThreads = 32 * (kSoftWarps + kLoadWarps + 1);
-constexpr int kLoadThreads = 32 * kLoadWarps;
-constexpr int kStages = 2;
-constexpr int kSegRing = 8, kScaleRing = 4;
+constexpr int kSoftWarps = 8, kLoadWarps = 8, kMmaWarp = kSoftWarps + kLoadWarps, kPlanWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
+constexpr int kTreeThreads = 32 * (kMmaWarp + 4);
+constexpr int kGroupWarps = kLoadWarps / 2, kGroupThreads = 32 * kGroupWarps;   // of the loading warps: keys, values
+constexpr int kKStages = 1, kVStages = 2;          // of widened operands: keys are free again once the scores are had
+constexpr int kRawK = 2, kRawV = 3;                // steps of codes under way
+constexpr int kSegRing = 8, kScaleRing = 8;
 constexpr int kTileChunks = kTileKeys / kChunk;
-constexpr float kMostPlain = 0x1p20f;             // a reference from where on scores are rounded before it is taken off
+// Registers of a thread: softmax, loading, the others.  (96 at the launch.)
+constexpr int kSoftRegs = 144, kLoadRegs = 72, kOtherRegs = 40;
+static_assert(32 * (kSoftWarps * kSoftRegs + kLoadWarps * kLoadRegs + 4 * kOtherRegs) <= kTreeThreads * 96, "");
+constexpr float kMostPlain = 0x1p20f;             // scores up to which a reference of one number serves
 constexpr int kMinTileSteps = 2;                  // of a run, where there are fewer steps than teams could take
 
 // Steps [step0, step0 + steps) of an item; steps = 0: no more.
@@ -37,18 +44,18 @@ struct Segment {
   int b, h, step0, steps, len, count, whole, slot;
 };
 
-struct TreeSmall {
-  uint64_t k_full[kStages], v_full[kStages], k_free[kStages], v_free[kStages];
+struct alignas(16) TreeSmall {
+  uint64_t rk_full[kRawK], rk_free[kRawK], rv_full[kRawV], rv_free[kRawV];
+  uint64_t k_full[kKStages], k_free[kKStages], v_full[kVStages], v_free[kVStages];
   uint64_t s_full[2], p_full[2], o_full, drained;
-  uint64_t q_full[kSegRing];
-  uint64_t soft, load, half[2];                   // the softmax warps', loading warps', a group's meeting points
+  uint64_t seg_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
+  uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
   float downs[kSegRing][kTileRows];               // what a row's queries were divided by
-  float scales[kScaleRing][2 * kTileChunks];      // ks, then vs of a step's chunks
-  uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_tile)
-  uint32_t nans[kScaleRing][kLoadWarps];          // whether a loading warp met NaN among the values
-  uint32_t nan_keys[2][4];
-  float ml[2][2][kTileRows];
+  float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
+  uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_probs)
+  alignas(16) uint32_t nan_keys[kScaleRing][4];               // keys that have NaN among their values
+  float ml[2][3][kTileRows];                      // the groups' references, sums, bases
   uint32_t tmem;
   int dead;
 };
@@ -58,10 +65,11 @@ struct TreeShape {
   static constexpr int kTile = kTileKeys * kD * 2;                  // bytes of an operand
   static constexpr int kBlock = kTileRows * 128;                     // of [128 rows][64 elements]
   static constexpr int kVBlock = kD * 128;                           // of [D rows][64 keys]
-  static constexpr int kQ = 0, kK = kTile, kV = kK + kStages * kTile, kSmallAt = kV + kStages * kTile;
+  static constexpr int kHalf = kTileKeys * kD;                       // codes of half a step
+  static constexpr int kQ = 0, kK = kTile, kV = kK + kKStages * kTile, kRk = kV + kVStages * kTile, kRv = kRk + kRawK * kHalf, kSmallAt = kRv + kRawV * kHalf;
   static constexpr size_t kSmem = 1024 + kSmallAt + sizeof(TreeSmall);
-  static constexpr int kSlot = kTileRows * (kD + 2);
-  static constexpr int kLoads = kD / 32;                             // sixteens of a thread's keys, and of its values
+  static constexpr int kSlot = kTileRows * (kD + 3);                 // floats of a partial: output, reference (two numbers), sum
+  static constexpr int kLoads = kD / 16;                             // sixteens of a thread's keys, or of its values
   static_assert(kSmem <= 227 * 1024, "");
 };
 
@@ -93,178 +101,39 @@ struct Meeting {
   }
 };
 
-// Four codes as bf16: the exponent and mantissa bits stand for 2^-120 of the value, where bf16's are.
-__device__ __forceinline__ uint32_t bf16_of(uint32_t x) {        // codes in bytes 1 and 3
-  const uint32_t bits = (x & 0x80008000u) | (x >> 4 & 0x07f007f0u);
-  const __nv_bfloat162 up = __halves2bfloat162(__ushort_as_bfloat16(0x7b80), __ushort_as_bfloat16(0x7b80));   // 2^120
-  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&bits), up);
-  return *reinterpret_cast<const uint32_t*>(&y);
-}
-__device__ __forceinline__ void widen4_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  lo = bf16_of(__byte_perm(w, 0, 0x1404));
-  hi = bf16_of(__byte_perm(w, 0, 0x3424));
-}
 // The bytes' top bits tell which of four codes are NaN.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// log2 |vs| as a reference takes it: powers of two by it, their sums and their quotients by such sums stay in fp32's range.
+// (Values smaller than that lose bits.)
+__device__ __forceinline__ float log2_scale(float vs) { return fminf(fmaxf(log2f(fabsf(vs)), -100.f), 119.f); }
 
-// ------------------------------------------------------------------------------ loading warps
-template <int kD>
-struct Loader {
-  using S = TreeShape<kD>;
-  static constexpr int kN = S::kLoads;
-  static constexpr int kPieces = kD / 16;                 // of a key
-  static constexpr int kKeysOf = kLoadThreads / kPieces;  // keys that the threads take at once
-  const AttendArgs& A;
-  uint8_t* smem;
-  TreeSmall& sm;
-  int lt, lane, warp;
-  uint4 kr[kN], vr[kN];                                   // codes of the step to come
-  float ks, vs;
-  bool gone;                                              // this lane's chunk (lanes 0 .. 7 of the first warp)
-
-  __device__ __forceinline__ int page_of(const Segment& g, int chunk) const {
-    if (chunk * kChunk >= g.len) return -1;
-    const int p = __ldg(A.c.table + (int64_t)g.b * A.c.max_pages + A.cpb.over(chunk));
-    return p >= 0 && p < (int)A.c.pages ? p : -1;
-  }
-  __device__ __forceinline__ void load_keys(const Segment& g, int step) {
-    const int c0 = step * kTileChunks;
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const int key = lt / kPieces + j * kKeysOf, chunk = c0 + key / kChunk, p = page_of(g, chunk);
-      kr[j] = make_uint4(0, 0, 0, 0);
-      if (p >= 0)
-        kr[j] = __ldg(reinterpret_cast<const uint4*>(A.c.k + (((int64_t)p * A.c.H + g.h) * A.c.block + A.cpb.rest(chunk) * kChunk + (key & (kChunk - 1))) * kD +
-                                                     lt % kPieces * 16));
-    }
-    if (warp == 0 && lane < kTileChunks) {
-      const int chunk = c0 + lane, p = page_of(g, chunk);
-      gone = p < 0;
-      ks = gone ? 1.f : __ldg(A.c.ks + (int64_t)p * A.c.H + g.h);
-      vs = gone ? 0.f : __ldg(A.c.vs + (int64_t)p * A.c.H + g.h);
-      if (gone && chunk * kChunk < g.len && A.status) atomicOr(A.status + g.b, SDV_STATUS_BAD_PAGE);
-    }
-  }
-  __device__ __forceinline__ void load_values(const Segment& g, int step) {
-    const int chunk = step * kTileChunks + (lt & (kTileChunks - 1)), p = page_of(g, chunk);
-    const uint8_t* from = A.c.v + (((int64_t)max(p, 0) * A.c.H + g.h) * kD + lt / kTileChunks) * A.c.block + A.cpb.rest(chunk) * kChunk;
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      vr[j] = make_uint4(0, 0, 0, 0);
-      if (p >= 0) vr[j] = __ldg(reinterpret_cast<const uint4*>(from + (int64_t)j * (kLoadThreads / kTileChunks) * A.c.block));
-    }
-  }
-  // A sixteen's two pieces; lanes of the second block write theirs the other way round: no two lanes meet in a bank.
-  __device__ __forceinline__ void put(uint8_t* block, int row, int piece, bool other, const uint4& a, const uint4& b) {
-    *reinterpret_cast<uint4*>(block + swizzled(row, piece + other)) = other ? b : a;
-    *reinterpret_cast<uint4*>(block + swizzled(row, piece + !other)) = other ? a : b;
-  }
-  __device__ __forceinline__ void put_keys(int stage, int t) {
-    uint8_t* tile = smem + S::kK + stage * S::kTile;
-    const int p = lt % kPieces;
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      uint4 a, b;
-      widen4(kr[j].x, a.x, a.y);
-      widen4(kr[j].y, a.z, a.w);
-      widen4(kr[j].z, b.x, b.y);
-      widen4(kr[j].w, b.z, b.w);
-      put(tile + (p >> 2) * S::kBlock, lt / kPieces + j * kKeysOf, (p & 3) * 2, p >> 2 & 1, a, b);
-    }
-    if (warp == 0) {
-      const bool plain = gone ? false : ks >= 0.f && ks < INFINITY && fabsf(vs) < INFINITY;
-      const uint32_t absent = __ballot_sync(0xffffffffu, lane < kTileChunks && gone), fine = __ballot_sync(0xffffffffu, lane >= kTileChunks || plain);
-      if (lane < kTileChunks) {
-        sm.scales[t & (kScaleRing - 1)][lane] = ks;
-        sm.scales[t & (kScaleRing - 1)][kTileChunks + lane] = vs;
-      }
-      if (lane == 0) sm.absent[t & (kScaleRing - 1)] = absent | (fine == 0xffffffffu ? 0x80000000u : 0u);
-    }
-  }
-  __device__ __forceinline__ void put_values(int stage, int t) {
-    uint8_t* tile = smem + S::kV + stage * S::kTile;
-    const int c = lt & (kTileChunks - 1);
-    uint32_t nan = 0;
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      uint4 a, b;
-      widen4_bf16(vr[j].x, a.x, a.y);
-      widen4_bf16(vr[j].y, a.z, a.w);
-      widen4_bf16(vr[j].z, b.x, b.y);
-      widen4_bf16(vr[j].w, b.z, b.w);
-      nan |= nan_codes(vr[j].x) | nan_codes(vr[j].y) | nan_codes(vr[j].z) | nan_codes(vr[j].w);
-      put(tile + (c >> 2) * S::kVBlock, lt / kTileChunks + j * (kLoadThreads / kTileChunks), (c & 3) * 2, c >> 2 & 1, a, b);
-    }
-    const bool any = __any_sync(0xffffffffu, nan);
-    if (lane == 0) sm.nans[t & (kScaleRing - 1)][warp] = any;
-  }
-  // The rows' queries, two threads a row.
-  __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
-    const int row = lt >> 1, half = lt & 1, r = rt * rows + row, i = r / A.G;
-    const bool live = row < rows && r < A.R && i < g.count;
-    const int64_t at = live ? g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh : 0;
-    constexpr int kEights = kD / 16;                      // of a thread
-    float most = 0.f;
-    uint4 v[kEights];
-#pragma unroll
-    for (int e = 0; e < kEights; ++e) {
-      v[e] = live ? q_load8(A, at + (half * kEights + e) * 8) : make_uint4(0, 0, 0, 0);
-      if (A.bf16) most = fmaxf(most, q_largest(v[e], true));
-    }
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    const int up = A.bf16 && most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;   // takes the largest to [2^15, 2^16)
-#pragma unroll
-    for (int e = 0; e < kEights; ++e) {
-      const int e8 = half * kEights + e;
-      if (A.bf16) {
-        float f[8];
-        Num<SDV_BF16>::unpack(v[e], f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] *= pow2(up);
-        v[e] = Num<SDV_F16>::pack(f);
-      }
-      *reinterpret_cast<uint4*>(smem + S::kQ + (e8 >> 3) * S::kBlock + swizzled(row, e8 & 7)) = v[e];
-    }
-    if (half == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
-  }
-};
-
-template <int kD>
-__device__ __forceinline__ void load_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int team, int rt, int tid) {
-  using S = TreeShape<kD>;
+// ------------------------------------------------------------------------------ the warp that plans
+// The run's segments one after another, as far ahead as their ring allows.
+__device__ __forceinline__ void plan_role(const TreeRowsArgs& T, TreeSmall& sm, int team, int lane) {
   const AttendArgs& A = T.a;
-  Loader<kD> L{A, smem, sm};
-  L.lt = tid, L.lane = tid & 31, L.warp = tid >> 5;
-  const int lane = L.lane;
-  Meeting meet{&sm.load, 0};
-  int* dead = &sm.dead;
-  // the run's segments, by the first warp
   const int per = A.c.H;
+  const int64_t units = step_sums<true, 0>(A, 0, lane).total * per;
+  const int runs = tree_runs(units, T.teams);
   int64_t u = 0, u_end = 0, seq_u = 0;
   int b = 0;
-  bool first = true;
-  if (L.warp == 0) {
-    const int64_t units = step_sums<true, kTileKeys>(A, 0, lane).total * per;
-    const int runs = tree_runs(units, T.teams);
-    if (team < runs) {
-      u = run_start(units, team, runs);
-      u_end = run_start(units, team + 1, runs);
-      const Found f = find_sequence<true, kTileKeys>(A, u / per, lane);
-      b = f.b;
-      seq_u = f.before * per;
-    }
+  if (team < runs) {
+    u = run_start(units, team, runs);
+    u_end = run_start(units, team + 1, runs);
+    const Found f = find_sequence<true, 0>(A, u / per, lane);
+    b = f.b;
+    seq_u = f.before * per;
   }
-  auto next_segment = [&](int seg) {
-    if (L.warp) return;
+#pragma unroll 1
+  for (int seg = 0;; ++seg) {
     Segment g{};
     while (u < u_end && b < A.B) {
-      Seq sq = seq_of<true, kTileKeys>(A, b);
+      const Seq sq = seq_of<true, 0>(A, b);
       const int64_t mine = (int64_t)sq.steps * per;
       if (u >= seq_u + mine) {                            // on to the next sequence, or over empty ones
         seq_u += mine;
         if (++b == A.B) break;
-        if (!seq_of<true, kTileKeys>(A, b).steps) {
-          const Found f = find_sequence<true, kTileKeys>(A, u / per, lane);
+        if (!seq_of<true, 0>(A, b).steps) {
+          const Found f = find_sequence<true, 0>(A, u / per, lane);
           b = f.b;
           seq_u = f.before * per;
         }
@@ -277,107 +146,348 @@ __device__ __forceinline__ void load_role(const TreeRowsArgs& T, uint8_t* smem, 
       g.steps = (int)min((int64_t)sq.steps, u_end - item_u) - g.step0;
       g.len = sq.len, g.count = sq.count;
       g.whole = g.steps == sq.steps;
-      g.slot = first ? 0 : 1;
-      first = false;
+      g.slot = seg ? 1 : 0;
       u += g.steps;
       break;
     }
-    if (lane == 0) sm.segs[seg & (kSegRing - 1)] = g;
+    const int slot = seg & (kSegRing - 1);
+    if (seg >= kSegRing && !warp_wait(&sm.seg_done[slot], (seg / kSegRing - 1) & 1, &sm.dead)) return;
+    if (lane == 0) sm.segs[slot] = g;
+    warp_arrive(&sm.seg_full[slot], lane);
+    if (!g.steps) return;
+  }
+}
+
+// ------------------------------------------------------------------------------ the warp that copies
+// A place among the run's steps: step `n` of a segment.
+struct Cursor {
+  int seg, n;
+  Segment g;                                              // (steps = 0: past the end)
+};
+__device__ __forceinline__ bool next_step(Cursor& c, TreeSmall& sm) {
+  if (++c.n < c.g.steps) return true;
+  c.n = 0;
+  ++c.seg;
+  if (!warp_wait(&sm.seg_full[c.seg & (kSegRing - 1)], c.seg / kSegRing & 1, &sm.dead)) return false;
+  c.g = sm.segs[c.seg & (kSegRing - 1)];
+  return true;
+}
+
+// Page `lane` of each step: its number two steps ahead, its scales one, then its keys and values.
+template <int kD>
+__device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int lane) {
+  using S = TreeShape<kD>;
+  const AttendArgs& A = T.a;
+  int* dead = &sm.dead;
+  const int block = A.c.block, pages = A.step / block, chunks = block / kChunk;
+  const uint32_t bytes = (uint32_t)(block * kD);
+  const auto page_of = [&](const Cursor& c) {
+    const int at = (c.g.step0 + c.n) * pages + lane;
+    if (!c.g.steps || lane >= pages || (int64_t)at * block >= c.g.len) return -1;
+    const int p = __ldg(A.c.table + (int64_t)c.g.b * A.c.max_pages + at);
+    if (p >= 0 && p < (int)A.c.pages) return p;
+    if (A.status) atomicOr(A.status + c.g.b, SDV_STATUS_BAD_PAGE);
+    return -1;
   };
-  next_segment(0);
-  if (!meet(lane, dead)) return;
+  const auto scale_of = [&](const float* of, int page, int h, float none) { return page < 0 ? none : __ldg(of + (int64_t)page * A.c.H + h); };
+  Cursor c{0, 0, Segment{}};
+  if (!warp_wait(&sm.seg_full[0], 0, dead)) return;
+  c.g = sm.segs[0];
+  int page = page_of(c), h = c.g.h, more = c.g.steps;      // this step's; its scales
+  float ks = scale_of(A.c.ks, page, h, 1.f), vs = scale_of(A.c.vs, page, h, 0.f);
+  if (more && !next_step(c, sm)) return;
+  int page1 = page_of(c), h1 = c.g.h, more1 = c.g.steps;   // the next one's
+#pragma unroll 1
+  for (int t = 0; more; ++t) {
+    const int64_t head = (int64_t)max(page, 0) * A.c.H + h;
+    const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+    {                                                        // the scales are read behind the keys' barrier
+      const int slot = t % kRawK, turn = t / kRawK;
+      if (turn && !warp_wait(&sm.rk_free[slot], (turn - 1) & 1, dead)) return;
+      {
+        const bool plain = lane >= pages || (page >= 0 && ks >= 0.f && ks < INFINITY && fabsf(vs) < INFINITY);
+        const int at = t & (kScaleRing - 1);
+        uint32_t absent = 0;
+        const float lw = log2_scale(vs);
+        if (lane < 4) sm.nan_keys[at][lane] = 0;
+        if (lane < pages)
+          for (int k = lane * chunks; k < (lane + 1) * chunks; ++k) {
+            sm.scales[at][k] = ks;
+            sm.scales[at][kTileChunks + k] = kPScale * vs;
+            sm.scales[at][2 * kTileChunks + k] = lw;
+            absent |= (uint32_t)(page < 0) << k;
+          }
+        absent = __reduce_or_sync(0xffffffffu, absent);
+        const bool all = __all_sync(0xffffffffu, plain);
+        if (lane == 0) sm.absent[at] = absent | (all ? 0x80000000u : 0u);
+        __syncwarp();
+      }
+      if (lane == 0) barrier_expect(&sm.rk_full[slot], __popc(there) * bytes);
+      __syncwarp();
+      if (page >= 0) copy_bulk(smem_addr(smem + S::kRk + slot * S::kHalf) + lane * bytes, A.c.k + head * bytes, bytes, &sm.rk_full[slot]);
+    }
+    {
+      const int slot = t % kRawV, turn = t / kRawV;
+      if (turn && !warp_wait(&sm.rv_free[slot], (turn - 1) & 1, dead)) return;
+      if (lane == 0) barrier_expect(&sm.rv_full[slot], __popc(there) * bytes);
+      __syncwarp();
+      if (page >= 0) copy_bulk(smem_addr(smem + S::kRv + slot * S::kHalf) + lane * bytes, A.c.v + head * bytes, bytes, &sm.rv_full[slot]);
+    }
+    page = page1, h = h1, more = more1;
+    ks = scale_of(A.c.ks, page, h, 1.f);
+    vs = scale_of(A.c.vs, page, h, 0.f);
+    if (more && !next_step(c, sm)) return;
+    page1 = page_of(c), h1 = c.g.h, more1 = c.g.steps;
+  }
+}
+
+// ------------------------------------------------------------------------------ loading warps
+// A thread's values again, with 0 for NaN; their keys are noted.
+template <int kD>
+__device__ __noinline__ void put_nan(const uint8_t* codes, uint8_t* tile, uint32_t* nan_keys, int block, int lt, int live) {
+  const int chunks = block / kChunk, region = chunks * kD;
+  for (int i = lt; i < live; i += kGroupThreads) {
+    const uint4 y = reinterpret_cast<const uint4*>(codes)[i];
+    const uint32_t x[4] = {y.x, y.y, y.z, y.w};
+    const int page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
+    uint32_t keys = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t n = nan_codes(x[k]);
+      keys |= (n >> 7 & 1 | n >> 14 & 2 | n >> 21 & 4 | n >> 28 & 8) << (4 * k);
+      uint2 f;
+      widen4(x[k] & ~((n >> 7) * 0xffu), f.x, f.y);
+      *reinterpret_cast<uint2*>(tile + (c >> 2) * TreeShape<kD>::kVBlock + swizzled(d, (c & 3) * 2 + (k >> 1)) + (k & 1) * 8) = f;
+    }
+    if (keys) atomicOr(&nan_keys[c >> 1], keys << (16 * (c & 1)));
+  }
+}
+
+template <int kD>
+struct Loader {
+  using S = TreeShape<kD>;
+  static constexpr int kN = S::kLoads;
+  static constexpr int kPieces = kD / 16;                  // of a key
+  const AttendArgs& A;
+  uint8_t* smem;
+  TreeSmall& sm;
+  int lt, lane;
+  uint32_t v_to[kN];                                       // where a thread's sixteens of values go: place, and whether its pieces change places
+
+  __device__ __forceinline__ void init() {
+    const int chunks = A.c.block / kChunk, region = chunks * kD;               // sixteens of a page's values: [D][chunks]
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const int i = lt + j * kGroupThreads, page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
+      v_to[j] = (uint32_t)((c >> 2) * S::kVBlock) + swizzled(d, (c & 3) * 2) + (c >> 2 & 1);
+    }
+  }
+  // A sixteen's two pieces, in places p and p ^ 16; lanes of the second block write theirs the other way round, so that
+  // no two of eight lanes meet in a bank.
+  __device__ __forceinline__ void put(uint8_t* at, bool other, const uint4& a, const uint4& b) {
+    const uintptr_t one = reinterpret_cast<uintptr_t>(at), two = one ^ 16;
+    *reinterpret_cast<uint4*>(other ? two : one) = other ? b : a;
+    *reinterpret_cast<uint4*>(other ? one : two) = other ? a : b;
+  }
+  // Half of the thread's sixteens at a time.
+  __device__ __forceinline__ void put_keys(const uint8_t* codes, int stage, int live) {
+    uint8_t* tile = smem + S::kK + stage * S::kTile;
+    const int p = lt % kPieces, row = lt / kPieces;
+    uint8_t* to = tile + (p >> 2) * S::kBlock + swizzled(row, (p & 3) * 2);
+#pragma unroll
+    for (int j0 = 0; j0 < kN; j0 += kN / 2) {
+      uint4 x[kN / 2];
+#pragma unroll
+      for (int j = 0; j < kN / 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
+#pragma unroll
+      for (int j = 0; j < kN / 2; ++j) {
+        if (lt + (j0 + j) * kGroupThreads >= live) break;
+        uint4 a, b;
+        widen4(x[j].x, a.x, a.y);
+        widen4(x[j].y, a.z, a.w);
+        widen4(x[j].z, b.x, b.y);
+        widen4(x[j].w, b.z, b.w);
+        put(to + (j0 + j) * (kGroupThreads / kPieces) * 128, p >> 2 & 1, a, b);
+      }
+    }
+  }
+  __device__ __forceinline__ void put_values(const uint8_t* codes, int stage, int t, int live) {
+    uint8_t* tile = smem + S::kV + stage * S::kTile;
+    __half2 nan = __float2half2_rn(0.f);                   // stays 0 unless a code is NaN
+    const __half2 zero = nan;
+#pragma unroll
+    for (int j0 = 0; j0 < kN; j0 += kN / 2) {
+      uint4 x[kN / 2];
+#pragma unroll
+      for (int j = 0; j < kN / 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
+#pragma unroll
+      for (int j = 0; j < kN / 2; ++j) {
+        if (lt + (j0 + j) * kGroupThreads >= live) break;
+        uint32_t w[8];
+        widen4(x[j].x, w[0], w[1]);
+        widen4(x[j].y, w[2], w[3]);
+        widen4(x[j].z, w[4], w[5]);
+        widen4(x[j].w, w[6], w[7]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) nan = __hfma2(*reinterpret_cast<const __half2*>(&w[k]), zero, nan);
+        put(tile + (v_to[j0 + j] & ~1u), v_to[j0 + j] & 1, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+      }
+    }
+    if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
+  }
+  // The rows' queries, a thread a row.
+  __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
+    const int row = lt, r = rt * rows + row, i = r / A.G;
+    const bool live = row < rows && r < A.R && i < g.count;
+    const int64_t at = live ? g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh : 0;
+    constexpr int kEights = kD / 8;
+    float most = 0.f;
+    if (A.bf16 && live) {
+#pragma unroll 8
+      for (int e = 0; e < kEights; ++e) most = fmaxf(most, q_largest(q_load8(A, at + e * 8), true));
+    }
+    const int up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;       // takes the largest to [2^15, 2^16)
+#pragma unroll 8
+    for (int e = 0; e < kEights; ++e) {
+      uint4 v = live ? q_load8(A, at + e * 8) : make_uint4(0, 0, 0, 0);
+      if (A.bf16) {
+        float f[8];
+        Num<SDV_BF16>::unpack(v, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] *= pow2(up);
+        v = Num<SDV_F16>::pack(f);
+      }
+      *reinterpret_cast<uint4*>(smem + S::kQ + (e >> 3) * S::kBlock + swizzled(row, e & 7)) = v;
+    }
+    sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
+  }
+};
+
+// The keys' group, which brings the queries too.
+template <int kD>
+__device__ __forceinline__ void keys_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int rt, int tid) {
+  using S = TreeShape<kD>;
+  Loader<kD> L{T.a, smem, sm};
+  L.lt = tid, L.lane = tid & 31;
+  const int lane = L.lane, live = T.a.step * kD / 16;
+  int* dead = &sm.dead;
   int t = 0;
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
+    if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
     const Segment g = sm.segs[seg & (kSegRing - 1)];
-    if (g.steps && seg == 0) {
-      L.load_keys(g, g.step0);
-      L.load_values(g, g.step0);
-    }
-    if (g.steps) {
-      next_segment(seg + 1);
-      if (t && !warp_wait(&sm.k_free[(t - 1) % kStages], (t - 1) / kStages & 1, dead)) return;   // its last scores are had
-      L.put_queries(g, rt, T.rows, seg);
-      fence_async();
-    }
-    warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
     if (!g.steps) return;
+    // its queries, once the last scores before are had
+    if (t && !warp_wait(&sm.k_free[(t - 1) % kKStages], (t - 1) / kKStages & 1, dead)) return;
+    L.put_queries(g, rt, T.rows, seg);
+    fence_async();
+    warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
 #pragma unroll 1
-    for (int n = 0; n < g.steps; ++n, ++t) {
-      const int st = t % kStages;
-      const uint32_t before = (t / kStages - 1) & 1;
-      if (t >= kStages && !warp_wait(&sm.k_free[st], before, dead)) return;
-      L.put_keys(st, t);
+    for (const int end = t + g.steps; t < end; ++t) {
+      const int slot = t % kRawK, st = t % kKStages, turn = t / kKStages;
+      if (!warp_wait(&sm.rk_full[slot], t / kRawK & 1, dead)) return;
+      if (turn && !warp_wait(&sm.k_free[st], (turn - 1) & 1, dead)) return;
+      L.put_keys(smem + S::kRk + slot * S::kHalf, st, live);
+      warp_arrive(&sm.rk_free[slot], lane);
       fence_async();
       warp_arrive(&sm.k_full[st], lane);
-      Segment ng = g;
-      int step = g.step0 + n + 1;
-      if (n + 1 == g.steps) {
-        if (!meet(lane, dead)) return;
-        ng = sm.segs[(seg + 1) & (kSegRing - 1)];
-        step = ng.step0;
-      }
-      if (ng.steps) L.load_keys(ng, step);
-      if (t >= kStages && !warp_wait(&sm.v_free[st], before, dead)) return;
-      L.put_values(st, t);
+    }
+  }
+}
+template <int kD>
+__device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int tid) {
+  using S = TreeShape<kD>;
+  Loader<kD> L{T.a, smem, sm};
+  L.lt = tid, L.lane = tid & 31;
+  L.init();
+  const int lane = L.lane, live = T.a.step * kD / 16;
+  int* dead = &sm.dead;
+  int t = 0;
+#pragma unroll 1
+  for (int seg = 0;; ++seg) {
+    if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
+    const int steps = sm.segs[seg & (kSegRing - 1)].steps;
+    if (!steps) return;
+#pragma unroll 1
+    for (const int end = t + steps; t < end; ++t) {
+      const int slot = t % kRawV, st = t % kVStages, turn = t / kVStages;
+      if (!warp_wait(&sm.rv_full[slot], t / kRawV & 1, dead)) return;
+      if (turn && !warp_wait(&sm.v_free[st], (turn - 1) & 1, dead)) return;
+      L.put_values(smem + S::kRv + slot * S::kHalf, st, t, live);
+      warp_arrive(&sm.rv_free[slot], lane);
       fence_async();
       warp_arrive(&sm.v_full[st], lane);
-      if (ng.steps) L.load_values(ng, step);
     }
   }
 }
 
-// ------------------------------------------------------------------------------ the thread that issues the products
+// ------------------------------------------------------------------------------ the warp that issues the products
+// All of its lanes go along, so that addresses and descriptors are the warp's (uniform registers); one of them issues.  (With
+// a single thread in this role a product took 100 cycles to issue, 64 to run.)
 template <int kD>
-__device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm) {
+__device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step) {
   using S = TreeShape<kD>;
   int* dead = &sm.dead;
-  const uint32_t base = sm.tmem, q = smem_addr(smem + S::kQ);
-  constexpr uint32_t kScore = mma_desc(0, kTileRows, kTileKeys), kOut = mma_desc(1, kTileRows, kD);
+  const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
+  const uint64_t q = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kQ), 0)), k = q + (S::kK - S::kQ) / 16, v = q + (S::kV - S::kQ) / 16;
+  const uint32_t score = mma_desc(0, kTileRows, step);
+  constexpr uint32_t kOut = mma_desc(0, kTileRows, kD);
+  const bool one = elected();
   int t = 0;
   auto scores = [&](int t) {
-    const int st = t % kStages;
-    if (!barrier_wait(&sm.k_full[st], t / kStages & 1, dead)) return false;
+    const int st = t % kKStages;
+    if (!warp_wait(&sm.k_full[st], t / kKStages & 1, dead)) return false;
     tmem_after_sync();
-    const uint32_t k = smem_addr(smem + S::kK + st * S::kTile);
+    const uint32_t to = base + (t & 1) * kTileKeys;
+    const uint64_t kt = k + st * (S::kTile / 16);
+    if (one) {
 #pragma unroll
-    for (int i = 0; i < kD / 16; ++i) {
-      const uint32_t off = (i >> 2) * S::kBlock + (i & 3) * 32;
-      mma_ss(base + (t & 1) * kTileKeys, tile_desc(q + off), tile_desc(k + off), kScore, i > 0);
+      for (int i = 0; i < kD / 16; ++i) {
+        const int off = ((i >> 2) * S::kBlock + (i & 3) * 32) / 16;
+        mma_ss(to, q + off, kt + off, score, i > 0);
+      }
+      mma_commit(&sm.s_full[t & 1]);
+      mma_commit(&sm.k_free[st]);
     }
-    mma_commit(&sm.s_full[t & 1]);
-    mma_commit(&sm.k_free[st]);
+    __syncwarp();
     return true;
   };
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
-    if (!barrier_wait(&sm.q_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) break;
-    const int steps = sm.segs[seg & (kSegRing - 1)].steps;
-    if (!steps || !scores(t)) break;
+    const uint32_t turn = seg / kSegRing & 1;
+    if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], turn, dead)) break;
+    const int steps = __shfl_sync(0xffffffffu, sm.segs[seg & (kSegRing - 1)].steps, 0);
+    if (!steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead) || !scores(t)) break;
     bool ok = true;
 #pragma unroll 1
     for (int n = 0; n < steps && ok; ++n, ++t) {
       if (n + 1 < steps) ok = scores(t + 1);
-      const int st = t % kStages, s = t & 1;
-      ok = ok && barrier_wait(&sm.p_full[s], t >> 1 & 1, dead) && barrier_wait(&sm.v_full[st], t / kStages & 1, dead);
+      const int st = t % kVStages, s = t & 1;
+      ok = ok && warp_wait(&sm.p_full[s], t >> 1 & 1, dead) && warp_wait(&sm.v_full[st], t / kVStages & 1, dead);
       if (!ok) break;
       tmem_after_sync();
-      const uint32_t v = smem_addr(smem + S::kV + st * S::kTile), out = base + 2 * kTileKeys + s * 128;
+      const uint32_t out = base + 2 * kTileKeys + s * 128, p = base + s * kTileKeys;
+      const uint64_t vt = v + st * (S::kTile / 16);
+      const bool first = n < 2;
+      if (one) {
 #pragma unroll
-      for (int i = 0; i < kTileKeys / 16; ++i) {
-        const uint64_t vd = tile_desc(v + (i >> 2) * S::kVBlock + (i & 3) * 32);
-        const uint32_t p = base + s * kTileKeys + (i >> 1) * 32 + (i & 1) * 8;
-        mma_ts(out, p, vd, kOut, i > 0 || n >= 2);
-        mma_ts(out, p + 16, vd, kOut, true);
+        for (int i = 0; i < kTileKeys / 16; ++i) {
+          if (i * 16 >= step) break;
+          const int off = ((i >> 2) * S::kVBlock + (i & 3) * 32) / 16;
+          mma_ts(out, p + i * 16, vt + off, kOut, i > 0 || !first);
+          mma_ts(out, p + i * 16 + 8, vt + off, kOut, true);
+        }
+        mma_commit(&sm.v_free[st]);
+        if (n + 1 == steps) mma_commit(&sm.o_full);
       }
-      mma_commit(&sm.v_free[st]);
-      if (n + 1 == steps) mma_commit(&sm.o_full);
+      __syncwarp();
     }
     if (!ok) break;
   }
-  mma_commit(&sm.drained);                                // nothing is under way when the memory is given back
+  if (one) mma_commit(&sm.drained);                        // nothing is under way when the memory is given back
+  __syncwarp();
   int ignore = 0;
-  barrier_wait(&sm.drained, 0, &ignore);
+  warp_wait(&sm.drained, 0, &ignore);
 }
 
 // ------------------------------------------------------------------------------ softmax warps
@@ -395,110 +505,169 @@ __device__ __forceinline__ Bits128 placed(uint64_t set, int at) {   // bit 0 in 
 }
 __device__ __forceinline__ uint32_t word(const Bits128& x, int i) { return (uint32_t)((i & 2 ? x.hi : x.lo) >> (i & 1 ? 32 : 0)); }
 
-// A row's step: scores in columns [at, at + 128) become probabilities times their values' scale, in halves (of each 32 scores
-// sixteen columns of first ones, sixteen of second ones, in their place); l goes on.
-// kPlain: every row sees every key, no scale is negative or none, no code NaN, no reference large.  Else what a row does
-// not see gets 0, and of what it sees NaN is what has no number; and the score is rounded before the reference is
-// taken off: the fused product is off by half a step of the reference, which large scores make a large power.
+// A row's running state: its reference base + m (log2; base is 0 unless its scores are past 2^20), and the sum of
+// 2^(score - reference).
+struct SoftRow {
+  float m, l, base;
+};
+// x 2^d for d <= 0, in two steps: neither factor underflows where the product does not.
+__device__ __forceinline__ float scaled(float x, float half) { return x * half * half; }
+
+// A row's step: scores in columns [at, at + 128) become probabilities times their values' scale, in halves (a chunk's sixteen
+// columns: eight of first ones, eight of second ones); l goes on.  The first half is the number cut off after eleven bits, the
+// second the rest of it, rounded.
+// kPlain: every row sees every key, no scale of keys is negative, none without a number, no reference large.  Else what
+// a row does not see gets 0, and what it sees of a scale without a number NaN; and the score is rounded before
+// reference is taken off: the fused product is off by half a step of the reference, which large scores make a large power.
 template <bool kPlain>
-__device__ __forceinline__ void soft_probs(uint32_t at, const float* scales, float f0, const Bits128& sees, const Bits128& nans, float m, float& l) {
-  uint32_t r[32];
-  f32x2 sum = pair(0.f, 0.f);
-  const f32x2 nm = pair(-m, -m);
+__device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float* scales, float f0, const Bits128& sees, SoftRow& s) {
+  uint32_t r[2][32];
+  f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+  const f32x2 nm = pair(-s.m, -s.m), minus = pair(-1.f, -1.f);
+  tmem_load32(at, r[0]);
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    tmem_load32(at + 32 * g, r);
-    tmem_loaded(r);
-    uint32_t w = 0, bad = 0;
-    if constexpr (!kPlain) w = word(sees, g), bad = word(nans, g);
-    uint32_t o[32];
+    uint32_t* x = r[g & 1];
+    tmem_loaded(x);
+    if (g < 3) tmem_load32(at + 32 * (g + 1), r[(g + 1) & 1]);
+    uint32_t w = 0;
+    if constexpr (!kPlain) w = word(sees, g);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
+      if (2 * g + c >= chunks) break;
       const float f = f0 * scales[2 * g + c], vs = scales[kTileChunks + 2 * g + c];
+      uint32_t o[16];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int k = 16 * c + 2 * e;
-        const float x0 = __uint_as_float(r[k]), x1 = __uint_as_float(r[k + 1]);
-        float2 p;
-        f32x2 v;
+        const float x0 = __uint_as_float(x[k]), x1 = __uint_as_float(x[k + 1]);
+        f32x2 p, v;
         if constexpr (kPlain) {
-          const float2 x = unpair(fma2(pair(x0, x1), pair(f, f), nm));
-          p = make_float2(ex2(x.x), ex2(x.y));
-          v = mul2(pair(p.x, p.y), pair(vs, vs));
+          const float2 a = unpair(fma2(pair(x0, x1), pair(f, f), nm));
+          p = pair(ex2(a.x), ex2(a.y));
+          v = mul2(p, pair(vs, vs));
         } else {
           const bool none = !(fabsf(vs) < INFINITY) || !(fabsf(f) < INFINITY);
-          p = make_float2(ex2(__fmul_rn(x0, f) - m), ex2(__fmul_rn(x1, f) - m));
-          p.x = !(w >> k & 1) ? 0.f : none || (bad >> k & 1) ? NAN : p.x;
-          p.y = !(w >> (k + 1) & 1) ? 0.f : none || (bad >> (k + 1) & 1) ? NAN : p.y;
-          v = none ? pair(p.x, p.y) : mul2(pair(p.x, p.y), pair(vs, vs));
+          float2 a = make_float2(ex2((__fmul_rn(x0, f) - s.base) - s.m), ex2((__fmul_rn(x1, f) - s.base) - s.m));
+          a.x = !(w >> k & 1) ? 0.f : none ? NAN : a.x;
+          a.y = !(w >> (k + 1) & 1) ? 0.f : none ? NAN : a.y;
+          p = pair(a.x, a.y);
+          v = none ? p : mul2(p, pair(vs, vs));
         }
-        sum = add2(sum, pair(p.x, p.y));
+        sum[e & 1] = add2(sum[e & 1], p);
         const float2 y = unpair(v);
-        const __nv_bfloat162 h = __floats2bfloat162_rn(y.x, y.y);
-        const uint32_t hw = *reinterpret_cast<const uint32_t*>(&h);
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(y.x - __uint_as_float(hw << 16), y.y - __uint_as_float(hw & 0xffff0000u));
-        o[8 * c + e] = hw;
-        o[16 + 8 * c + e] = *reinterpret_cast<const uint32_t*>(&lo);
+        const uint32_t y0 = __float_as_uint(y.x), y1 = __float_as_uint(y.y);
+        const float c0 = __uint_as_float(y0 & 0xffffe000u), c1 = __uint_as_float(y1 & 0xffffe000u);
+        o[e] = pack_half(c0, c1);
+        const float2 rest = unpair(fma2(pair(c0, c1), minus, v));
+        o[8 + e] = pack_half(rest.x, rest.y);
       }
+      tmem_store16(at + 32 * g + 16 * c, o);
     }
-    tmem_store32(at + 32 * g, o);
   }
-  const float2 s2 = unpair(sum);
-  l += s2.x + s2.y;
+  const float2 s2 = unpair(add2(sum[0], sum[1]));
+  s.l += s2.x + s2.y;
   tmem_stored();
 }
 
-// The whole step: the row's largest score first, against which its reference m may move (`more`: O holds sums already).
-template <int kD, bool kPlain>
-__device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, const float* scales, float f0, const Bits128& sees, const Bits128& nans,
-                                          bool more, float& m, float& l) {
-  float top = -INFINITY;
-  uint32_t r[32];
+// By how much the reference (m, base) exceeds that of (m0, base0).
+__device__ __forceinline__ float reference_less(float m0, float base0, float m, float base) { return (base - base0) + (m - m0); }
+
+// The sums of a row that goes over to a reference higher by 2^-d.
+template <int kD>
+__device__ __forceinline__ void soft_move(uint32_t out, bool more, float d, SoftRow& s) {
+  const float half = ex2(.5f * d);
+  s.l = scaled(s.l, half);
+  if (more) {
+    uint32_t r[32];
+#pragma unroll 1
+    for (int g = 0; g < kD / 32; ++g) {
+      tmem_load32(out + 32 * g, r);
+      tmem_loaded(r);
 #pragma unroll
+      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(scaled(__uint_as_float(r[e]), half));
+      tmem_store32(out + 32 * g, r);
+    }
+    tmem_stored();
+  }
+}
+
+// The row's largest score less its base, plus log2 of the values' scale (`scale`: or without), of what it sees.
+__device__ __forceinline__ float soft_top(uint32_t at, const float* scales, float f0, const Bits128& sees, float base, bool scale) {
+  float top = -INFINITY;
+#pragma unroll 1
   for (int g = 0; g < 4; ++g) {
+    uint32_t r[32];
     tmem_load32(at + 32 * g, r);
     tmem_loaded(r);
-    if constexpr (kPlain) {
+    const uint32_t w = word(sees, g);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x = __uint_as_float(r[16 * c]);
+    for (int e = 0; e < 32; ++e) {
+      const int c = 2 * g + e / 16;                         // (scales past the step: not seen)
+      const float x = (__fmul_rn(__uint_as_float(r[e]), f0 * scales[c]) - base) + (scale ? scales[2 * kTileChunks + c] : 0.f);
+      top = w >> e & 1 ? fmaxf(top, x) : top;
+    }
+  }
+  return top;
+}
+
+// A step where some row does not see all, or of unusual scales.
+template <int kD>
+__device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees_lo,
+                                         uint64_t sees_hi, bool more, SoftRow s) {
+  const Bits128 sees{sees_lo, sees_hi};
+  // a base for scores past 2^20: of the row's own, when they pass the old one or nothing has been seen
+  const float raw = soft_top(at, scales, f0, sees, s.base, false);
+  const bool large = fabsf(raw) < INFINITY && (s.m > kNone ? raw > kMostPlain : fabsf(raw) > kMostPlain);
+  if (__any_sync(0xffffffffu, large)) {
+    const float base = large ? s.base + raw : s.base;
+    if (s.m > kNone) s.m = fmaxf(s.m + (s.base - base), kNone);
+    s.base = base;
+  }
+  const float top = soft_top(at, scales, f0, sees, s.base, true);
+  const bool move = top > s.m + kSlack;
+  if (__any_sync(0xffffffffu, move)) {
+    const float now = move ? top : s.m, d = s.m - now;
+    s.m = now;
+    soft_move<kD>(out, more, d, s);
+  }
+  soft_probs<false>(at, chunks, scales, f0, sees, s);
+  return s;
+}
+
+// An ordinary step: the row's largest score first, against which its reference may move (`more`: O holds sums already).
+template <int kD>
+__device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, bool more, SoftRow& s) {
+  float top = -INFINITY;
+  uint32_t rr[2][32];
+  tmem_load32(at, rr[0]);
 #pragma unroll
-        for (int e = 1; e < 16; ++e) x = fmaxf(x, __uint_as_float(r[16 * c + e]));
-        top = fmaxf(top, x * (f0 * scales[2 * g + c]));
-      }
-    } else {
-      const uint32_t w = word(sees, g);
+  for (int g = 0; g < 4; ++g) {
+    uint32_t* r = rr[g & 1];
+    tmem_loaded(r);
+    if (g < 3) tmem_load32(at + 32 * (g + 1), rr[(g + 1) & 1]);
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const float x = __uint_as_float(r[e]) * (f0 * scales[2 * g + e / 16]);
-        top = w >> e & 1 ? fmaxf(top, x) : top;
-      }
+    for (int c = 0; c < 2; ++c) {
+      if (2 * g + c >= chunks) break;
+      float x[5];
+#pragma unroll
+      for (int e = 0; e < 5; ++e) x[e] = max3(__uint_as_float(r[16 * c + 3 * e]), __uint_as_float(r[16 * c + 3 * e + 1]), __uint_as_float(r[16 * c + 3 * e + 2]));
+      const float most = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], __uint_as_float(r[16 * c + 15])));
+      top = fmaxf(top, fmaf(most, f0 * scales[2 * g + c], scales[2 * kTileChunks + 2 * g + c]));
     }
   }
   // the reference moves when a score passes it by 2^kSlack
-  const bool move = top > m + kSlack;
-  if (__any_sync(0xffffffffu, move)) {
-    const float now = move ? top : m, c = ex2(m - now);
-    m = now;
-    l *= c;
-    if (more) {
-#pragma unroll 1
-      for (int g = 0; g < kD / 32; ++g) {
-        tmem_load32(out + 32 * g, r);
-        tmem_loaded(r);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * c);
-        tmem_store32(out + 32 * g, r);
-      }
-      tmem_stored();
+  const bool move = top > s.m + kSlack;
+  if (__any_sync(0xffffffffu, move || s.base != 0.f)) {
+    if (__any_sync(0xffffffffu, s.base != 0.f || (move && fabsf(top) > kMostPlain))) {
+      s = soft_any<kD>(at, out, chunks, scales, f0, ~0ull, ~0ull, more, s);
+      return;
     }
+    const float now = move ? top : s.m, d = s.m - now;
+    s.m = now;
+    soft_move<kD>(out, more, d, s);
   }
-  if (kPlain && !__any_sync(0xffffffffu, fabsf(m) > kMostPlain)) {
-    soft_probs<true>(at, scales, f0, sees, nans, m, l);
-  } else {
-    const Bits128 all{~0ull, ~0ull};
-    soft_probs<false>(at, scales, f0, kPlain ? all : sees, nans, m, l);
-  }
+  soft_probs<true>(at, chunks, scales, f0, Bits128{0, 0}, s);
 }
 
 template <int kD>
@@ -509,14 +678,15 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
   int* dead = &sm.dead;
   const uint32_t lanes = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16);
   const uint32_t at = lanes + s * kTileKeys, out = lanes + 2 * kTileKeys;
-  Meeting meet{&sm.soft, 0}, meet_half{&sm.half[s], 0};
-  const int r = rt * T.rows + row, i = r / A.G;
+  Meeting meet{&sm.soft, 0};
+  const int r = rt * T.rows + row, i = r / A.G, chunks = A.step / kChunk;
   int t = 0;
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
-    if (!warp_wait(&sm.q_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
+    const uint32_t turn = seg / kSegRing & 1;
+    if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], turn, dead)) return;
     const Segment g = sm.segs[seg & (kSegRing - 1)];
-    if (!g.steps) return;
+    if (!g.steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead)) return;
     const bool have = row < T.rows && r < A.R, live = have && i < g.count;
     const bool busy = __any_sync(0xffffffffu, live);
     uint64_t set;
@@ -531,50 +701,37 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     }
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
-    float m = kNone, l = 0.f;
+    SoftRow mine{kNone, 0.f, 0.f};
     int done = 0;                                          // this group's steps of the segment
     const int t_end = t + g.steps;
     const bool any0 = g.steps > 1 || !(t & 1), any1 = g.steps > 1 || (t & 1);
 #pragma unroll 1
     for (int n = 0; t < t_end; ++t, ++n) {
       if ((t & 1) != s) continue;
-      if (!warp_wait(&sm.v_full[t % kStages], t / kStages & 1, dead) || !warp_wait(&sm.s_full[s], t >> 1 & 1, dead)) return;
+      if (!warp_wait(&sm.s_full[s], t >> 1 & 1, dead)) return;
       tmem_after_sync();
-      const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * kTileKeys;
+      const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step;
       const uint32_t absent = sm.absent[slot];
-      uint32_t nan = 0;
-#pragma unroll
-      for (int k = 0; k < kLoadWarps; ++k) nan |= sm.nans[slot][k];
-      const Bits128 none{0, 0};
-      if (absent >> 31 && !nan && key0 + kTileKeys <= at0 && A.scale2 >= 0.f) {
-        if (busy) soft_tile<kD, true>(at, out + s * 128, sm.scales[slot], f0, none, none, done > 0, m, l);
-      } else {
-        Bits128 nans = none;
-        if (nan) {                                         // which keys' values: a thread a key
-          const uint8_t* tile = smem + S::kV + (t % kStages) * S::kTile + (row >> 6) * S::kVBlock;
-          bool mine = false;
-#pragma unroll 1
-          for (int d = 0; d < kD; ++d)
-            mine |= (*reinterpret_cast<const uint16_t*>(tile + swizzled(d, (row & 63) >> 3) + (row & 7) * 2) & 0x7fff) == 0x43f0;   // 480
-          const uint32_t w = __ballot_sync(0xffffffffu, mine);
-          if (lane == 0) sm.nan_keys[s][warp & 3] = w;
-          if (!meet_half(lane, dead)) return;
-          nans = Bits128{sm.nan_keys[s][0] | (uint64_t)sm.nan_keys[s][1] << 32, sm.nan_keys[s][2] | (uint64_t)sm.nan_keys[s][3] << 32};
-          if (!meet_half(lane, dead)) return;
+      Bits128 sees = below(A.step);
+      if (absent >> 31 && key0 + A.step <= at0 && A.scale2 >= 0.f) {
+        if (busy) soft_tile<kD>(at, out + s * 128, chunks, sm.scales[slot], f0, done > 0, mine);
+      } else if (busy) {
+        const Bits128 before = below(at0 - key0);
+        Bits128 can = before;
+        if (at0 - key0 > -64 && at0 - key0 < kTileKeys) {
+          const Bits128 tree = placed(set, at0 - key0);
+          can.lo |= tree.lo, can.hi |= tree.hi;
         }
-        if (busy) {
-          Bits128 sees = below(at0 - key0);
-          if (at0 - key0 > -64 && at0 - key0 < kTileKeys) {
-            const Bits128 tree = placed(set, at0 - key0);
-            sees.lo |= tree.lo, sees.hi |= tree.hi;
-          }
 #pragma unroll
-          for (int c = 0; c < kTileChunks; ++c)
-            if (absent >> c & 1) (c < 4 ? sees.lo : sees.hi) &= ~(0xffffull << (16 * (c & 3)));
-          if (!live) sees = none;
-          soft_tile<kD, false>(at, out + s * 128, sm.scales[slot], f0, sees, nans, done > 0, m, l);
-        }
+        for (int c = 0; c < kTileChunks; ++c)
+          if (absent >> c & 1) (c < 4 ? can.lo : can.hi) &= ~(0xffffull << (16 * (c & 3)));
+        sees.lo = live ? sees.lo & can.lo : 0, sees.hi = live ? sees.hi & can.hi : 0;
+        mine = soft_any<kD>(at, out + s * 128, chunks, sm.scales[slot], f0, sees.lo, sees.hi, done > 0, mine);
       }
+      // NaN among the values that a row sees: its own affair, since they are 0 for the others
+      if (!warp_wait(&sm.v_full[t % kVStages], t / kVStages & 1, dead)) return;
+      const uint4 nan = *reinterpret_cast<const uint4*>(sm.nan_keys[slot]);
+      if ((sees.lo & (nan.x | (uint64_t)nan.y << 32)) | (sees.hi & (nan.z | (uint64_t)nan.w << 32))) mine.l = NAN;
       ++done;
       tmem_before_sync();
       warp_arrive(&sm.p_full[s], lane);
@@ -582,13 +739,17 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     // the segment's rows: both groups' sums, a half of the columns each
     if (!warp_wait(&sm.o_full, seg & 1, dead)) return;
     tmem_after_sync();
-    sm.ml[s][0][row] = m;
-    sm.ml[s][1][row] = l;
+    sm.ml[s][0][row] = mine.m;
+    sm.ml[s][1][row] = mine.l;
+    sm.ml[s][2][row] = mine.base;
     if (!meet(lane, dead)) return;
     if (busy || (__any_sync(0xffffffffu, have))) {
-      const float m0 = sm.ml[0][0][row], m1 = sm.ml[1][0][row], l0 = sm.ml[0][1][row], l1 = sm.ml[1][1][row];
-      const float top = fmaxf(m0, m1), c0 = ex2(m0 - top), c1 = ex2(m1 - top);
-      const float sum = live ? l0 * c0 + l1 * c1 : 0.f, by = !g.whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+      const float m0 = sm.ml[0][0][row], m1 = sm.ml[1][0][row], b0 = sm.ml[0][2][row], b1 = sm.ml[1][2][row];
+      const float ahead = reference_less(m1, b1, m0, b0);    // of the first group's reference
+      const float top = ahead >= 0.f ? m0 : m1, base = ahead >= 0.f ? b0 : b1;
+      const float c0 = ex2(.5f * fminf(ahead, 0.f)), c1 = ex2(-.5f * fmaxf(ahead, 0.f));
+      const float sum = live ? scaled(sm.ml[0][1][row], c0) + scaled(sm.ml[1][1][row], c1) : 0.f;
+      const float by = !g.whole ? 1.f / kPScale : sum == 0.f ? 0.f : 1.f / sum / kPScale;
       const int64_t to = ((int64_t)g.b * A.W + i) * (A.c.H * A.G) + g.h * A.G + (r - i * A.G);
       float* part = A.part + ((int64_t)(blockIdx.x * 2 + g.slot)) * S::kSlot;
 #pragma unroll 1
@@ -602,13 +763,13 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
           tmem_load32(out + col, a);
           tmem_loaded(a);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(a[e]) * c0;
+          for (int e = 0; e < 32; ++e) o[e] = scaled(__uint_as_float(a[e]), c0);
         }
         if (busy && any1) {
           tmem_load32(out + 128 + col, a);
           tmem_loaded(a);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(a[e]), c1, o[e]);
+          for (int e = 0; e < 32; ++e) o[e] += scaled(__uint_as_float(a[e]), c1);
         }
         if (!have) continue;
         if (g.whole) {
@@ -626,20 +787,22 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         } else {
           float4* y = reinterpret_cast<float4*>(part + (int64_t)row * kD + col);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          for (int e = 0; e < 8; ++e) y[e] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
         }
       }
       if (have && s == 0) {
         if (g.whole) {
-          if (A.lse) A.lse[to] = lse_of(top, sum, 0.f);
+          if (A.lse) A.lse[to] = lse_of(top, sum, base);
         } else {
           part[kTileRows * kD + row] = top;
-          part[kTileRows * kD + kTileRows + row] = sum;
+          part[kTileRows * kD + kTileRows + row] = base;
+          part[kTileRows * kD + 2 * kTileRows + row] = sum;
         }
       }
     }
     tmem_before_sync();
     if (!meet(lane, dead)) return;                         // the sums are read: the next products may come
+    warp_arrive(&sm.seg_done[seg & (kSegRing - 1)], lane);
   }
 }
 
@@ -650,38 +813,60 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   uint8_t* smem = raw + (-smem_addr(raw) & 1023);
   TreeSmall& sm = *reinterpret_cast<TreeSmall*>(smem + S::kSmallAt);
   const int tid = threadIdx.x, warp = tid >> 5, team = blockIdx.x / T.a.RT, rt = blockIdx.x - team * T.a.RT;
-  if (warp == kSoftWarps + kLoadWarps) tmem_alloc(&sm.tmem, 512);
+  if (warp == kMmaWarp) tmem_alloc(&sm.tmem, 512);
   if (tid == 0) {
-    for (int k = 0; k < kStages; ++k) {
-      barrier_init(&sm.k_full[k], kLoadWarps);
-      barrier_init(&sm.v_full[k], kLoadWarps);
-      barrier_init(&sm.k_free[k], 1);
-      barrier_init(&sm.v_free[k], 1);
-    }
     for (int k = 0; k < 2; ++k) {
       barrier_init(&sm.s_full[k], 1);
       barrier_init(&sm.p_full[k], kSoftWarps / 2);
-      barrier_init(&sm.half[k], kSoftWarps / 2);
     }
-    for (int k = 0; k < kSegRing; ++k) barrier_init(&sm.q_full[k], kLoadWarps);
+    for (int k = 0; k < kSegRing; ++k) {
+      barrier_init(&sm.seg_full[k], 1);
+      barrier_init(&sm.seg_done[k], kSoftWarps);
+      barrier_init(&sm.q_full[k], kGroupWarps);
+    }
+    for (int k = 0; k < kKStages; ++k) {
+      barrier_init(&sm.k_full[k], kGroupWarps);
+      barrier_init(&sm.k_free[k], 1);
+    }
+    for (int k = 0; k < kVStages; ++k) {
+      barrier_init(&sm.v_full[k], kGroupWarps);
+      barrier_init(&sm.v_free[k], 1);
+    }
+    for (int k = 0; k < kRawK; ++k) {
+      barrier_init(&sm.rk_full[k], 1);
+      barrier_init(&sm.rk_free[k], kGroupWarps);
+    }
+    for (int k = 0; k < kRawV; ++k) {
+      barrier_init(&sm.rv_full[k], 1);
+      barrier_init(&sm.rv_free[k], kGroupWarps);
+    }
     barrier_init(&sm.o_full, 1);
     barrier_init(&sm.drained, 1);
     barrier_init(&sm.soft, kSoftWarps);
-    barrier_init(&sm.load, kLoadWarps);
     sm.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
-  if (warp < kSoftWarps) soft_role<kD>(T, smem, sm, team, rt, tid);
-  else if (warp < kSoftWarps + kLoadWarps) load_role<kD>(T, smem, sm, team, rt, tid - 32 * kSoftWarps);
-  else if (tid == 32 * (kSoftWarps + kLoadWarps)) mma_role<kD>(smem, sm);
+  if (warp < kSoftWarps) {
+    registers_up<kSoftRegs>();
+    soft_role<kD>(T, smem, sm, team, rt, tid);
+  } else if (warp < kMmaWarp) {
+    registers_down<kLoadRegs>();
+    if (warp < kSoftWarps + kGroupWarps) keys_role<kD>(T, smem, sm, rt, tid - 32 * kSoftWarps);
+    else values_role<kD>(T, smem, sm, tid - 32 * (kSoftWarps + kGroupWarps));
+  } else {
+    registers_down<kOtherRegs>();
+    if (warp == kPlanWarp) plan_role(T, sm, team, tid & 31);
+    else if (warp == kCopyWarp) copy_role<kD>(T, smem, sm, tid & 31);
+    else if (warp == kMmaWarp) mma_role<kD>(smem, sm, T.a.step);
+  }
   __syncwarp();
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
-  if (warp == kSoftWarps + kLoadWarps) tmem_free(sm.tmem, 512);
+  if (warp == kMmaWarp) tmem_free(sm.tmem, 512);
   if (sm.dead && tid == 0 && T.a.status) atomicOr(T.a.status, SDV_STATUS_STUCK);
 }
 
@@ -695,7 +880,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int ib = blockIdx.x / kCtas, row = blockIdx.x % kCtas * kJoinWarps + warp;
   const int per = A.c.H * A.RT, b = ib / per, item = ib % per, h = item / A.RT, rt = item % A.RT, r = rt * T.rows + row;
-  const Sums ts = step_sums<true, kTileKeys>(A, b, lane);
+  const Sums ts = step_sums<true, 0>(A, b, lane);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (A.status && item == 0 && row == 0) {
     bool bad = lane == 0 && A.lengths[b] < min(A.counts ? A.counts[b] : A.W, A.W);
@@ -704,7 +889,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
     if (lane == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
   }
   if (row >= T.rows || r >= A.R) return;
-  const Seq sq = seq_of<true, kTileKeys>(A, b);
+  const Seq sq = seq_of<true, 0>(A, b);
   const int64_t units = ts.total * A.c.H, u0 = ts.before * A.c.H + (int64_t)h * sq.steps, u1 = min(u0 + sq.steps, units);
   const int runs = tree_runs(units, T.teams);
   int g0 = 0, g1 = -1;
@@ -720,20 +905,26 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   }
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
   auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
-  float m = kNone;
-  for (int gi = g0 + lane; gi <= g1; gi += 32) m = fmaxf(m, slot_of(gi)[kTileRows * kD + row]);
+  float m = kNone, base = 0.f;
+  const auto higher = [&](float om, float ob) {
+    if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
+  };
+  for (int gi = g0 + lane; gi <= g1; gi += 32) higher(slot_of(gi)[kTileRows * kD + row], slot_of(gi)[kTileRows * kD + kTileRows + row]);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int o = 16; o; o >>= 1) {
+    const float om = __shfl_xor_sync(0xffffffffu, m, o), ob = __shfl_xor_sync(0xffffffffu, base, o);
+    higher(om, ob);
+  }
   float l = 0.f, o[kV];
 #pragma unroll
   for (int e = 0; e < kV; ++e) o[e] = 0.f;
 #pragma unroll 4
   for (int gi = g0; gi <= g1; ++gi) {
     const float* slot = slot_of(gi);
-    const float c = ex2(slot[kTileRows * kD + row] - m);
-    l = fmaf(c, slot[kTileRows * kD + kTileRows + row], l);
+    const float half = ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
+    l += scaled(slot[kTileRows * kD + 2 * kTileRows + row], half);
 #pragma unroll
-    for (int e = 0; e < kV; ++e) o[e] = fmaf(c, slot[(int64_t)row * kD + e * 32 + lane], o[e]);
+    for (int e = 0; e < kV; ++e) o[e] += scaled(slot[(int64_t)row * kD + e * 32 + lane], half);
   }
   const int i = r / A.G;
   if (i >= sq.count) l = 0.f;
@@ -741,7 +932,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < kV; ++e) put_out(A, to * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
-  if (A.lse && lane == 0) A.lse[to] = lse_of(m, l, 0.f);
+  if (A.lse && lane == 0) A.lse[to] = lse_of(m, l, base);
 }
 
 template <int kD>
