@@ -81,12 +81,21 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* r) {
       "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : SDV_R32(SDV_OUT)
       : "r"(at));
+}
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : SDV_R16(SDV_OUT, 0)
+      : "r"(at));
 #undef SDV_OUT
 }
 // (The registers pass through, so that nothing that uses them comes before.)
 __device__ __forceinline__ void tmem_loaded(uint32_t* r) {
 #define SDV_INOUT(i) "+r"(r[i])
   asm volatile("tcgen05.wait::ld.sync.aligned;" : SDV_R32(SDV_INOUT)::"memory");
+}
+__device__ __forceinline__ void tmem_loaded16(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : SDV_R16(SDV_INOUT, 0)::"memory");
 #undef SDV_INOUT
 }
 __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {

@@ -9,8 +9,8 @@
 //   * one warp copies: a step's pages of codes, in bulk, into rings of steps of keys and of values;
 //   * loading warps widen them to f16 (exactly; a value's NaN becomes 0 and is told apart), the matrix unit's operands;
 //   * one warp issues the products;
-//   * two groups of softmax warps take the steps in turn, each with scores and sums of its own, joined at the
-//     end of a segment.
+//   * two groups of softmax warps take a half of each step's keys, each with references and sums of its own, joined
+//     at the end of a segment.  The scores of the next step are had meanwhile, in the other half of their memory.
 // Queries go through f16: bf16 ones under a power of two of their row.  Probabilities times their value's scale
 // stand in tensor memory in place of their scores, as the sum of two f16: 22 bits, or 2^-32 of the row's largest.  So that they
 // fit f16 whatever the scales of other pages, a row's reference m is taken on the score plus log2 of that scale;
@@ -47,10 +47,11 @@ struct Segment {
 struct alignas(16) TreeSmall {
   uint64_t rk_full[kRawK], rk_free[kRawK], rv_full[kRawV], rv_free[kRawV];
   uint64_t k_full[kKStages], k_free[kKStages], v_full[kVStages], v_free[kVStages];
-  uint64_t s_full[2], p_full[2], o_full, drained;
+  uint64_t s_full[2], p_full[2][2], o_full, drained;   // p_full: of a step's parity and a group
   uint64_t seg_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
   uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
+  uint16_t v_to[kTileChunks * 128];               // (see Loader::init)
   float downs[kSegRing][kTileRows];               // what a row's queries were divided by
   float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
   uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_probs)
@@ -106,6 +107,9 @@ __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7
 // log2 |vs| as a reference takes it: powers of two by it, their sums and their quotients by such sums stay in fp32's range.
 // (Values smaller than that lose bits.)
 __device__ __forceinline__ float log2_scale(float vs) { return fminf(fmaxf(log2f(fabsf(vs)), -100.f), 119.f); }
+
+// Chunks of a step that the first group takes.
+__device__ __forceinline__ int first_half(int chunks) { return (chunks + 1) / 2; }
 
 // ------------------------------------------------------------------------------ the warp that plans
 // The run's segments one after another, as far ahead as their ring allows.
@@ -272,14 +276,13 @@ struct Loader {
   uint8_t* smem;
   TreeSmall& sm;
   int lt, lane;
-  uint32_t v_to[kN];                                       // where a thread's sixteens of values go: place, and whether its pieces change places
 
+  // Where the sixteens of values go: the place in the operand, and whether its pieces change places.
   __device__ __forceinline__ void init() {
     const int chunks = A.c.block / kChunk, region = chunks * kD;               // sixteens of a page's values: [D][chunks]
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const int i = lt + j * kGroupThreads, page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
-      v_to[j] = (uint32_t)((c >> 2) * S::kVBlock) + swizzled(d, (c & 3) * 2) + (c >> 2 & 1);
+    for (int i = lt; i < kTileChunks * kD; i += kGroupThreads) {
+      const int page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
+      sm.v_to[i] = (uint16_t)((c >> 2) * S::kVBlock + swizzled(d, (c & 3) * 2) + (c >> 2 & 1));
     }
   }
   // A sixteen's two pieces, in places p and p ^ 16; lanes of the second block write theirs the other way round, so that
@@ -289,18 +292,18 @@ struct Loader {
     *reinterpret_cast<uint4*>(other ? two : one) = other ? b : a;
     *reinterpret_cast<uint4*>(other ? one : two) = other ? a : b;
   }
-  // Half of the thread's sixteens at a time.
+  // Two of the thread's sixteens at a time (short loops, as elsewhere here).
   __device__ __forceinline__ void put_keys(const uint8_t* codes, int stage, int live) {
     uint8_t* tile = smem + S::kK + stage * S::kTile;
     const int p = lt % kPieces, row = lt / kPieces;
     uint8_t* to = tile + (p >> 2) * S::kBlock + swizzled(row, (p & 3) * 2);
+#pragma unroll 1
+    for (int j0 = 0; j0 < kN; j0 += 2) {
+      uint4 x[2];
 #pragma unroll
-    for (int j0 = 0; j0 < kN; j0 += kN / 2) {
-      uint4 x[kN / 2];
+      for (int j = 0; j < 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
 #pragma unroll
-      for (int j = 0; j < kN / 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
-#pragma unroll
-      for (int j = 0; j < kN / 2; ++j) {
+      for (int j = 0; j < 2; ++j) {
         if (lt + (j0 + j) * kGroupThreads >= live) break;
         uint4 a, b;
         widen4(x[j].x, a.x, a.y);
@@ -315,13 +318,17 @@ struct Loader {
     uint8_t* tile = smem + S::kV + stage * S::kTile;
     __half2 nan = __float2half2_rn(0.f);                   // stays 0 unless a code is NaN
     const __half2 zero = nan;
+#pragma unroll 1
+    for (int j0 = 0; j0 < kN; j0 += 2) {
+      uint4 x[2];
+      uint32_t to[2];
 #pragma unroll
-    for (int j0 = 0; j0 < kN; j0 += kN / 2) {
-      uint4 x[kN / 2];
+      for (int j = 0; j < 2; ++j) {
+        x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
+        to[j] = sm.v_to[lt + (j0 + j) * kGroupThreads];
+      }
 #pragma unroll
-      for (int j = 0; j < kN / 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
-#pragma unroll
-      for (int j = 0; j < kN / 2; ++j) {
+      for (int j = 0; j < 2; ++j) {
         if (lt + (j0 + j) * kGroupThreads >= live) break;
         uint32_t w[8];
         widen4(x[j].x, w[0], w[1]);
@@ -330,7 +337,7 @@ struct Loader {
         widen4(x[j].w, w[6], w[7]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) nan = __hfma2(*reinterpret_cast<const __half2*>(&w[k]), zero, nan);
-        put(tile + (v_to[j0 + j] & ~1u), v_to[j0 + j] & 1, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+        put(tile + (to[j] & ~1u), to[j] & 1, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
       }
     }
     if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
@@ -431,6 +438,7 @@ __device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step)
   const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
   const uint64_t q = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kQ), 0)), k = q + (S::kK - S::kQ) / 16, v = q + (S::kV - S::kQ) / 16;
   const uint32_t score = mma_desc(0, kTileRows, step);
+  const int chunks = step / kChunk, half = first_half(chunks);
   constexpr uint32_t kOut = mma_desc(0, kTileRows, kD);
   const bool one = elected();
   int t = 0;
@@ -441,7 +449,7 @@ __device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step)
     const uint32_t to = base + (t & 1) * kTileKeys;
     const uint64_t kt = k + st * (S::kTile / 16);
     if (one) {
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < kD / 16; ++i) {
         const int off = ((i >> 2) * S::kBlock + (i & 3) * 32) / 16;
         mma_ss(to, q + off, kt + off, score, i > 0);
@@ -462,25 +470,30 @@ __device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step)
 #pragma unroll 1
     for (int n = 0; n < steps && ok; ++n, ++t) {
       if (n + 1 < steps) ok = scores(t + 1);
-      const int st = t % kVStages, s = t & 1;
-      ok = ok && warp_wait(&sm.p_full[s], t >> 1 & 1, dead) && warp_wait(&sm.v_full[st], t / kVStages & 1, dead);
-      if (!ok) break;
-      tmem_after_sync();
-      const uint32_t out = base + 2 * kTileKeys + s * 128, p = base + s * kTileKeys;
-      const uint64_t vt = v + st * (S::kTile / 16);
-      const bool first = n < 2;
-      if (one) {
-#pragma unroll
-        for (int i = 0; i < kTileKeys / 16; ++i) {
-          if (i * 16 >= step) break;
-          const int off = ((i >> 2) * S::kVBlock + (i & 3) * 32) / 16;
-          mma_ts(out, p + i * 16, vt + off, kOut, i > 0 || !first);
-          mma_ts(out, p + i * 16 + 8, vt + off, kOut, true);
+      const int st = t % kVStages;
+      ok = ok && warp_wait(&sm.v_full[st], t / kVStages & 1, dead);
+#pragma unroll 1
+      for (int h = 0; h < 2 && ok; ++h) {                  // a group's keys
+        ok = warp_wait(&sm.p_full[t & 1][h], t >> 1 & 1, dead);
+        if (!ok) break;
+        tmem_after_sync();
+        const uint32_t out = base + 2 * kTileKeys + h * 128, p = base + (t & 1) * kTileKeys;
+        const uint64_t vt = v + st * (S::kTile / 16);
+        if (one) {
+          const int i0 = h ? half : 0, i1 = h ? chunks : half;
+#pragma unroll 1
+          for (int i = i0; i < i1; ++i) {
+            const int off = ((i >> 2) * S::kVBlock + (i & 3) * 32) / 16;
+            mma_ts(out, p + i * 16, vt + off, kOut, n > 0 || i > i0);
+            mma_ts(out, p + i * 16 + 8, vt + off, kOut, true);
+          }
+          if (h) {
+            mma_commit(&sm.v_free[st]);
+            if (n + 1 == steps) mma_commit(&sm.o_full);
+          }
         }
-        mma_commit(&sm.v_free[st]);
-        if (n + 1 == steps) mma_commit(&sm.o_full);
+        __syncwarp();
       }
-      __syncwarp();
     }
     if (!ok) break;
   }
@@ -491,19 +504,11 @@ __device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step)
 }
 
 // ------------------------------------------------------------------------------ softmax warps
-// What a row sees of a step's 128 keys, as bits.
-struct Bits128 {
-  uint64_t lo, hi;
-};
-__device__ __forceinline__ Bits128 below(int n) {         // the first n
-  return Bits128{n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1, n >= 128 ? ~0ull : n <= 64 ? 0ull : (1ull << (n - 64)) - 1};
+// What a row sees of 64 keys, as bits: the first n, and the set of the tree whose node 0 stands in place `at`.
+__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t placed(uint64_t set, int at) {
+  return at <= -64 || at >= 64 ? 0ull : at <= 0 ? set >> -at : set << at;
 }
-__device__ __forceinline__ Bits128 placed(uint64_t set, int at) {   // bit 0 in place `at`, -64 < at < 128
-  if (at <= 0) return Bits128{set >> -at, 0};
-  if (at < 64) return Bits128{set << at, set >> (64 - at)};
-  return Bits128{0, set << (at - 64)};
-}
-__device__ __forceinline__ uint32_t word(const Bits128& x, int i) { return (uint32_t)((i & 2 ? x.hi : x.lo) >> (i & 1 ? 32 : 0)); }
 
 // A row's running state: its reference base + m (log2; base is 0 unless its scores are past 2^20), and the sum of
 // 2^(score - reference).
@@ -513,58 +518,67 @@ struct SoftRow {
 // x 2^d for d <= 0, in two steps: neither factor underflows where the product does not.
 __device__ __forceinline__ float scaled(float x, float half) { return x * half * half; }
 
-// A row's step: scores in columns [at, at + 128) become probabilities times their values' scale, in halves (a chunk's sixteen
+// f(c, scores) for the chunks c in turn, the next one's scores under way.  (Short loops: with the steps unrolled, warps
+// waited for instructions a quarter of their time.)
+template <typename F>
+__device__ __forceinline__ void each_chunk(uint32_t at, int chunks, F f) {
+  uint32_t x[16], y[16];
+  tmem_load16(at, x);
+#pragma unroll 1
+  for (int c = 0; c < chunks; c += 2) {
+    tmem_loaded16(x);
+    const bool second = c + 1 < chunks;
+    if (second) tmem_load16(at + 16 * c + 16, y);
+    f(c, x);
+    if (second) {
+      tmem_loaded16(y);
+      if (c + 2 < chunks) tmem_load16(at + 16 * c + 32, x);
+      f(c + 1, y);
+    }
+  }
+}
+
+// A row's part of a step, up to 64 keys: scores in columns from `at` on become probabilities times their values' scale, in halves (a chunk's sixteen
 // columns: eight of first ones, eight of second ones); l goes on.  The first half is the number cut off after eleven bits, the
 // second the rest of it, rounded.
 // kPlain: every row sees every key, no scale of keys is negative, none without a number, no reference large.  Else what
 // a row does not see gets 0, and what it sees of a scale without a number NaN; and the score is rounded before
 // reference is taken off: the fused product is off by half a step of the reference, which large scores make a large power.
 template <bool kPlain>
-__device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float* scales, float f0, const Bits128& sees, SoftRow& s) {
-  uint32_t r[2][32];
+__device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float* scales, float f0, uint64_t sees, SoftRow& s) {
   f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
   const f32x2 nm = pair(-s.m, -s.m), minus = pair(-1.f, -1.f);
-  tmem_load32(at, r[0]);
+  const auto chunk = [&](int c, const uint32_t* x) {
+    const float f = f0 * scales[c], vs = scales[kTileChunks + c];
+    const uint32_t w = kPlain ? 0u : (uint32_t)(sees >> (16 * c));
+    uint32_t o[16];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    uint32_t* x = r[g & 1];
-    tmem_loaded(x);
-    if (g < 3) tmem_load32(at + 32 * (g + 1), r[(g + 1) & 1]);
-    uint32_t w = 0;
-    if constexpr (!kPlain) w = word(sees, g);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if (2 * g + c >= chunks) break;
-      const float f = f0 * scales[2 * g + c], vs = scales[kTileChunks + 2 * g + c];
-      uint32_t o[16];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int k = 16 * c + 2 * e;
-        const float x0 = __uint_as_float(x[k]), x1 = __uint_as_float(x[k + 1]);
-        f32x2 p, v;
-        if constexpr (kPlain) {
-          const float2 a = unpair(fma2(pair(x0, x1), pair(f, f), nm));
-          p = pair(ex2(a.x), ex2(a.y));
-          v = mul2(p, pair(vs, vs));
-        } else {
-          const bool none = !(fabsf(vs) < INFINITY) || !(fabsf(f) < INFINITY);
-          float2 a = make_float2(ex2((__fmul_rn(x0, f) - s.base) - s.m), ex2((__fmul_rn(x1, f) - s.base) - s.m));
-          a.x = !(w >> k & 1) ? 0.f : none ? NAN : a.x;
-          a.y = !(w >> (k + 1) & 1) ? 0.f : none ? NAN : a.y;
-          p = pair(a.x, a.y);
-          v = none ? p : mul2(p, pair(vs, vs));
-        }
-        sum[e & 1] = add2(sum[e & 1], p);
-        const float2 y = unpair(v);
-        const uint32_t y0 = __float_as_uint(y.x), y1 = __float_as_uint(y.y);
-        const float c0 = __uint_as_float(y0 & 0xffffe000u), c1 = __uint_as_float(y1 & 0xffffe000u);
-        o[e] = pack_half(c0, c1);
-        const float2 rest = unpair(fma2(pair(c0, c1), minus, v));
-        o[8 + e] = pack_half(rest.x, rest.y);
+    for (int e = 0; e < 8; ++e) {
+      const float x0 = __uint_as_float(x[2 * e]), x1 = __uint_as_float(x[2 * e + 1]);
+      f32x2 p, v;
+      if constexpr (kPlain) {
+        const float2 a = unpair(fma2(pair(x0, x1), pair(f, f), nm));
+        p = pair(ex2(a.x), ex2(a.y));
+        v = mul2(p, pair(vs, vs));
+      } else {
+        const bool none = !(fabsf(vs) < INFINITY) || !(fabsf(f) < INFINITY);
+        float2 a = make_float2(ex2((__fmul_rn(x0, f) - s.base) - s.m), ex2((__fmul_rn(x1, f) - s.base) - s.m));
+        a.x = !(w >> (2 * e) & 1) ? 0.f : none ? NAN : a.x;
+        a.y = !(w >> (2 * e + 1) & 1) ? 0.f : none ? NAN : a.y;
+        p = pair(a.x, a.y);
+        v = none ? p : mul2(p, pair(vs, vs));
       }
-      tmem_store16(at + 32 * g + 16 * c, o);
+      sum[e & 1] = add2(sum[e & 1], p);
+      const float2 y = unpair(v);
+      const uint32_t y0 = __float_as_uint(y.x), y1 = __float_as_uint(y.y);
+      const float c0 = __uint_as_float(y0 & 0xffffe000u), c1 = __uint_as_float(y1 & 0xffffe000u);
+      o[e] = pack_half(c0, c1);
+      const float2 rest = unpair(fma2(pair(c0, c1), minus, v));
+      o[8 + e] = pack_half(rest.x, rest.y);
     }
-  }
+    tmem_store16(at + 16 * c, o);
+  };
+  each_chunk(at, chunks, chunk);
   const float2 s2 = unpair(add2(sum[0], sum[1]));
   s.l += s2.x + s2.y;
   tmem_stored();
@@ -573,12 +587,20 @@ __device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float*
 // By how much the reference (m, base) exceeds that of (m0, base0).
 __device__ __forceinline__ float reference_less(float m0, float base0, float m, float base) { return (base - base0) + (m - m0); }
 
-// The sums of a row that goes over to a reference higher by 2^-d.
+// The sums of a row that goes over to a reference higher by 2^-d.  `before`: where the products that they are of end, or
+// no barrier (a segment's first step).
+struct Before {
+  uint64_t* bar;
+  uint32_t parity;
+  int* dead;
+};
 template <int kD>
-__device__ __forceinline__ void soft_move(uint32_t out, bool more, float d, SoftRow& s) {
+__device__ __forceinline__ void soft_move(uint32_t out, const Before& before, float d, SoftRow& s) {
   const float half = ex2(.5f * d);
   s.l = scaled(s.l, half);
-  if (more) {
+  if (before.bar) {
+    warp_wait(before.bar, before.parity, before.dead);      // (given up: so does the next wait)
+    tmem_after_sync();
     uint32_t r[32];
 #pragma unroll 1
     for (int g = 0; g < kD / 32; ++g) {
@@ -593,81 +615,65 @@ __device__ __forceinline__ void soft_move(uint32_t out, bool more, float d, Soft
 }
 
 // The row's largest score less its base, plus log2 of the values' scale (`scale`: or without), of what it sees.
-__device__ __forceinline__ float soft_top(uint32_t at, const float* scales, float f0, const Bits128& sees, float base, bool scale) {
+static __device__ __noinline__ float soft_top(uint32_t at, int chunks, const float* scales, float f0, uint64_t sees, float base, bool scale) {
   float top = -INFINITY;
-#pragma unroll 1
-  for (int g = 0; g < 4; ++g) {
-    uint32_t r[32];
-    tmem_load32(at + 32 * g, r);
-    tmem_loaded(r);
-    const uint32_t w = word(sees, g);
+  each_chunk(at, chunks, [&](int c, const uint32_t* x) {
+    const uint32_t w = (uint32_t)(sees >> (16 * c));
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const int c = 2 * g + e / 16;                         // (scales past the step: not seen)
-      const float x = (__fmul_rn(__uint_as_float(r[e]), f0 * scales[c]) - base) + (scale ? scales[2 * kTileChunks + c] : 0.f);
-      top = w >> e & 1 ? fmaxf(top, x) : top;
+    for (int e = 0; e < 16; ++e) {
+      const float y = (__fmul_rn(__uint_as_float(x[e]), f0 * scales[c]) - base) + (scale ? scales[2 * kTileChunks + c] : 0.f);
+      top = w >> e & 1 ? fmaxf(top, y) : top;
     }
-  }
+  });
   return top;
 }
 
 // A step where some row does not see all, or of unusual scales.
 template <int kD>
-__device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees_lo,
-                                         uint64_t sees_hi, bool more, SoftRow s) {
-  const Bits128 sees{sees_lo, sees_hi};
+__device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees,
+                                         Before before, SoftRow s) {
   // a base for scores past 2^20: of the row's own, when they pass the old one or nothing has been seen
-  const float raw = soft_top(at, scales, f0, sees, s.base, false);
+  const float raw = soft_top(at, chunks, scales, f0, sees, s.base, false);
   const bool large = fabsf(raw) < INFINITY && (s.m > kNone ? raw > kMostPlain : fabsf(raw) > kMostPlain);
   if (__any_sync(0xffffffffu, large)) {
     const float base = large ? s.base + raw : s.base;
     if (s.m > kNone) s.m = fmaxf(s.m + (s.base - base), kNone);
     s.base = base;
   }
-  const float top = soft_top(at, scales, f0, sees, s.base, true);
+  const float top = soft_top(at, chunks, scales, f0, sees, s.base, true);
   const bool move = top > s.m + kSlack;
   if (__any_sync(0xffffffffu, move)) {
     const float now = move ? top : s.m, d = s.m - now;
     s.m = now;
-    soft_move<kD>(out, more, d, s);
+    soft_move<kD>(out, before, d, s);
   }
   soft_probs<false>(at, chunks, scales, f0, sees, s);
   return s;
 }
 
-// An ordinary step: the row's largest score first, against which its reference may move (`more`: O holds sums already).
+// An ordinary step: the row's largest score first, against which its reference may move.
 template <int kD>
-__device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, bool more, SoftRow& s) {
+__device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, const Before& before, SoftRow& s) {
   float top = -INFINITY;
-  uint32_t rr[2][32];
-  tmem_load32(at, rr[0]);
+  each_chunk(at, chunks, [&](int c, const uint32_t* r) {
+    float x[5];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    uint32_t* r = rr[g & 1];
-    tmem_loaded(r);
-    if (g < 3) tmem_load32(at + 32 * (g + 1), rr[(g + 1) & 1]);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if (2 * g + c >= chunks) break;
-      float x[5];
-#pragma unroll
-      for (int e = 0; e < 5; ++e) x[e] = max3(__uint_as_float(r[16 * c + 3 * e]), __uint_as_float(r[16 * c + 3 * e + 1]), __uint_as_float(r[16 * c + 3 * e + 2]));
-      const float most = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], __uint_as_float(r[16 * c + 15])));
-      top = fmaxf(top, fmaf(most, f0 * scales[2 * g + c], scales[2 * kTileChunks + 2 * g + c]));
-    }
-  }
+    for (int e = 0; e < 5; ++e) x[e] = max3(__uint_as_float(r[3 * e]), __uint_as_float(r[3 * e + 1]), __uint_as_float(r[3 * e + 2]));
+    const float most = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], __uint_as_float(r[15])));
+    top = fmaxf(top, fmaf(most, f0 * scales[c], scales[2 * kTileChunks + c]));
+  });
   // the reference moves when a score passes it by 2^kSlack
   const bool move = top > s.m + kSlack;
   if (__any_sync(0xffffffffu, move || s.base != 0.f)) {
     if (__any_sync(0xffffffffu, s.base != 0.f || (move && fabsf(top) > kMostPlain))) {
-      s = soft_any<kD>(at, out, chunks, scales, f0, ~0ull, ~0ull, more, s);
+      s = soft_any<kD>(at, out, chunks, scales, f0, ~0ull, before, s);
       return;
     }
     const float now = move ? top : s.m, d = s.m - now;
     s.m = now;
-    soft_move<kD>(out, more, d, s);
+    soft_move<kD>(out, before, d, s);
   }
-  soft_probs<true>(at, chunks, scales, f0, Bits128{0, 0}, s);
+  soft_probs<true>(at, chunks, scales, f0, 0, s);
 }
 
 template <int kD>
@@ -677,9 +683,10 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
   const int lane = tid & 31, warp = tid >> 5, s = warp >> 2, row = (warp & 3) * 32 + lane;
   int* dead = &sm.dead;
   const uint32_t lanes = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16);
-  const uint32_t at = lanes + s * kTileKeys, out = lanes + 2 * kTileKeys;
+  const uint32_t out = lanes + 2 * kTileKeys;
+  const int all = T.a.step / kChunk, chunk0 = s ? first_half(all) : 0, chunks = s ? all - chunk0 : first_half(all);   // this group's
   Meeting meet{&sm.soft, 0};
-  const int r = rt * T.rows + row, i = r / A.G, chunks = A.step / kChunk;
+  const int r = rt * T.rows + row, i = r / A.G;
   int t = 0;
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
@@ -702,39 +709,34 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
     SoftRow mine{kNone, 0.f, 0.f};
-    int done = 0;                                          // this group's steps of the segment
-    const int t_end = t + g.steps;
-    const bool any0 = g.steps > 1 || !(t & 1), any1 = g.steps > 1 || (t & 1);
 #pragma unroll 1
-    for (int n = 0; t < t_end; ++t, ++n) {
-      if ((t & 1) != s) continue;
-      if (!warp_wait(&sm.s_full[s], t >> 1 & 1, dead)) return;
+    for (int n = 0; n < g.steps; ++n, ++t) {
+      if (!warp_wait(&sm.s_full[t & 1], t >> 1 & 1, dead)) return;
       tmem_after_sync();
-      const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step;
-      const uint32_t absent = sm.absent[slot];
-      Bits128 sees = below(A.step);
-      if (absent >> 31 && key0 + A.step <= at0 && A.scale2 >= 0.f) {
-        if (busy) soft_tile<kD>(at, out + s * 128, chunks, sm.scales[slot], f0, done > 0, mine);
+      const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step + chunk0 * kChunk;
+      const uint32_t absent = sm.absent[slot], at = lanes + (t & 1) * kTileKeys + chunk0 * kChunk;
+      const float* scales = sm.scales[slot] + chunk0;
+      const Before before{n ? &sm.v_free[(t - 1) % kVStages] : nullptr, (uint32_t)((t - 1) / kVStages & 1), dead};
+      uint64_t sees = below(chunks * kChunk);
+      if (absent >> 31 && key0 + chunks * kChunk <= at0 && A.scale2 >= 0.f) {
+        if (busy) soft_tile<kD>(at, out + s * 128, chunks, scales, f0, before, mine);
       } else if (busy) {
-        const Bits128 before = below(at0 - key0);
-        Bits128 can = before;
-        if (at0 - key0 > -64 && at0 - key0 < kTileKeys) {
-          const Bits128 tree = placed(set, at0 - key0);
-          can.lo |= tree.lo, can.hi |= tree.hi;
-        }
+        uint64_t can = below(at0 - key0) | placed(set, at0 - key0);
 #pragma unroll
-        for (int c = 0; c < kTileChunks; ++c)
-          if (absent >> c & 1) (c < 4 ? can.lo : can.hi) &= ~(0xffffull << (16 * (c & 3)));
-        sees.lo = live ? sees.lo & can.lo : 0, sees.hi = live ? sees.hi & can.hi : 0;
-        mine = soft_any<kD>(at, out + s * 128, chunks, sm.scales[slot], f0, sees.lo, sees.hi, done > 0, mine);
+        for (int c = 0; c < 4; ++c)
+          if (absent >> (chunk0 + c) & 1) can &= ~(0xffffull << (16 * c));
+        sees = live ? sees & can : 0;
+        mine = soft_any<kD>(at, out + s * 128, chunks, scales, f0, sees, before, mine);
       }
       // NaN among the values that a row sees: its own affair, since they are 0 for the others
       if (!warp_wait(&sm.v_full[t % kVStages], t / kVStages & 1, dead)) return;
       const uint4 nan = *reinterpret_cast<const uint4*>(sm.nan_keys[slot]);
-      if ((sees.lo & (nan.x | (uint64_t)nan.y << 32)) | (sees.hi & (nan.z | (uint64_t)nan.w << 32))) mine.l = NAN;
-      ++done;
+      if (nan.x | nan.y | nan.z | nan.w) {
+        const uint64_t lo = nan.x | (uint64_t)nan.y << 32, hi = nan.z | (uint64_t)nan.w << 32;
+        if (sees & (!chunk0 ? lo : chunk0 == 4 ? hi : lo >> (16 * chunk0) | hi << (64 - 16 * chunk0))) mine.l = NAN;
+      }
       tmem_before_sync();
-      warp_arrive(&sm.p_full[s], lane);
+      warp_arrive(&sm.p_full[t & 1][s], lane);
     }
     // the segment's rows: both groups' sums, a half of the columns each
     if (!warp_wait(&sm.o_full, seg & 1, dead)) return;
@@ -759,13 +761,11 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         float o[32];
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
-        if (busy && any0) {
+        if (busy) {
           tmem_load32(out + col, a);
           tmem_loaded(a);
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = scaled(__uint_as_float(a[e]), c0);
-        }
-        if (busy && any1) {
           tmem_load32(out + 128 + col, a);
           tmem_loaded(a);
 #pragma unroll
@@ -817,7 +817,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   if (tid == 0) {
     for (int k = 0; k < 2; ++k) {
       barrier_init(&sm.s_full[k], 1);
-      barrier_init(&sm.p_full[k], kSoftWarps / 2);
+      barrier_init(&sm.p_full[k][0], kSoftWarps / 2);
+      barrier_init(&sm.p_full[k][1], kSoftWarps / 2);
     }
     for (int k = 0; k < kSegRing; ++k) {
       barrier_init(&sm.seg_full[k], 1);
