@@ -51,7 +51,7 @@ struct alignas(16) TreeSmall {
   uint64_t seg_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
   uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
-  uint16_t v_to[kTileChunks * 128];               // (see Loader::init)
+  uint16_t v_to[kTileChunks * 128];               // (Loader::init)
   float downs[kSegRing][kTileRows];               // what a row's queries were divided by
   float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
   uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_probs)
@@ -250,7 +250,8 @@ __device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, 
 template <int kD>
 __device__ __noinline__ void put_nan(const uint8_t* codes, uint8_t* tile, uint32_t* nan_keys, int block, int lt, int live) {
   const int chunks = block / kChunk, region = chunks * kD;
-  for (int i = lt; i < live; i += kGroupThreads) {
+  for (int n = lt; n < live; n += kGroupThreads) {
+    const int i = chunks == 8 ? n ^ (n & 4) << 1 : n;
     const uint4 y = reinterpret_cast<const uint4*>(codes)[i];
     const uint32_t x[4] = {y.x, y.y, y.z, y.w};
     const int page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
@@ -277,67 +278,62 @@ struct Loader {
   TreeSmall& sm;
   int lt, lane;
 
-  // Where the sixteens of values go: the place in the operand, and whether its pieces change places.
+  // Where the sixteens of values go in the operand.
   __device__ __forceinline__ void init() {
     const int chunks = A.c.block / kChunk, region = chunks * kD;               // sixteens of a page's values: [D][chunks]
     for (int i = lt; i < kTileChunks * kD; i += kGroupThreads) {
-      const int page = i / region, r = i - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
-      sm.v_to[i] = (uint16_t)((c >> 2) * S::kVBlock + swizzled(d, (c & 3) * 2) + (c >> 2 & 1));
+      const int at = turn_pairs(i, chunks == 8), page = at / region, r = at - page * region, d = r / chunks, c = page * chunks + r - d * chunks;
+      sm.v_to[i] = (uint16_t)((c >> 2) * S::kVBlock + swizzled(d, (c & 3) * 2));
     }
   }
-  // A sixteen's two pieces, in places p and p ^ 16; lanes of the second block write theirs the other way round, so that
-  // no two of eight lanes meet in a bank.
-  __device__ __forceinline__ void put(uint8_t* at, bool other, const uint4& a, const uint4& b) {
-    const uintptr_t one = reinterpret_cast<uintptr_t>(at), two = one ^ 16;
-    *reinterpret_cast<uint4*>(other ? two : one) = other ? b : a;
-    *reinterpret_cast<uint4*>(other ? one : two) = other ? a : b;
+  // Which of 1024 sixteens, eight to a row, thread i takes: rows change places in pairs for the second four of each, so
+  // that no two of eight lanes meet in a bank, neither here nor where their pieces go.
+  static __device__ __forceinline__ int turn_pairs(int i, bool eight) { return eight ? i ^ (i & 4) << 1 : i; }
+  // A sixteen's two pieces, in places p and p ^ 16.
+  __device__ __forceinline__ void put(uint8_t* at, const uint4& x) {
+    uint4 a, b;
+    widen4(x.x, a.x, a.y);
+    widen4(x.y, a.z, a.w);
+    widen4(x.z, b.x, b.y);
+    widen4(x.w, b.z, b.w);
+    *reinterpret_cast<uint4*>(at) = a;
+    *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(at) ^ 16) = b;
   }
   // Two of the thread's sixteens at a time (short loops, as elsewhere here).
   __device__ __forceinline__ void put_keys(const uint8_t* codes, int stage, int live) {
-    uint8_t* tile = smem + S::kK + stage * S::kTile;
-    const int p = lt % kPieces, row = lt / kPieces;
-    uint8_t* to = tile + (p >> 2) * S::kBlock + swizzled(row, (p & 3) * 2);
+    const int first = turn_pairs(lt, kPieces == 8), p = first % kPieces, row = first / kPieces;
+    uint8_t* to = smem + S::kK + stage * S::kTile + (p >> 2) * S::kBlock + swizzled(row, (p & 3) * 2);
+    const uint4* from = reinterpret_cast<const uint4*>(codes) + first;
 #pragma unroll 1
-    for (int j0 = 0; j0 < kN; j0 += 2) {
-      uint4 x[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (lt + (j0 + j) * kGroupThreads >= live) break;
-        uint4 a, b;
-        widen4(x[j].x, a.x, a.y);
-        widen4(x[j].y, a.z, a.w);
-        widen4(x[j].z, b.x, b.y);
-        widen4(x[j].w, b.z, b.w);
-        put(to + (j0 + j) * (kGroupThreads / kPieces) * 128, p >> 2 & 1, a, b);
-      }
+    for (int j = 0; j < kN; j += 2) {
+      if (lt + j * kGroupThreads >= live) break;             // (whole rows of threads)
+      const uint4 x = from[j * kGroupThreads], y = from[(j + 1) * kGroupThreads];
+      put(to + j * (kGroupThreads / kPieces) * 128, x);
+      if (lt + (j + 1) * kGroupThreads < live) put(to + (j + 1) * (kGroupThreads / kPieces) * 128, y);
     }
   }
   __device__ __forceinline__ void put_values(const uint8_t* codes, int stage, int t, int live) {
     uint8_t* tile = smem + S::kV + stage * S::kTile;
+    const uint4* from = reinterpret_cast<const uint4*>(codes) + turn_pairs(lt, A.c.block == 128);
     __half2 nan = __float2half2_rn(0.f);                   // stays 0 unless a code is NaN
     const __half2 zero = nan;
 #pragma unroll 1
-    for (int j0 = 0; j0 < kN; j0 += 2) {
-      uint4 x[2];
-      uint32_t to[2];
+    for (int j = 0; j < kN; j += 2) {
+      if (lt + j * kGroupThreads >= live) break;
+      const uint4 x[2] = {from[j * kGroupThreads], from[(j + 1) * kGroupThreads]};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        x[j] = reinterpret_cast<const uint4*>(codes)[lt + (j0 + j) * kGroupThreads];
-        to[j] = sm.v_to[lt + (j0 + j) * kGroupThreads];
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (lt + (j0 + j) * kGroupThreads >= live) break;
+      for (int k = 0; k < 2; ++k) {
+        if (lt + (j + k) * kGroupThreads >= live) break;
         uint32_t w[8];
-        widen4(x[j].x, w[0], w[1]);
-        widen4(x[j].y, w[2], w[3]);
-        widen4(x[j].z, w[4], w[5]);
-        widen4(x[j].w, w[6], w[7]);
+        widen4(x[k].x, w[0], w[1]);
+        widen4(x[k].y, w[2], w[3]);
+        widen4(x[k].z, w[4], w[5]);
+        widen4(x[k].w, w[6], w[7]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) nan = __hfma2(*reinterpret_cast<const __half2*>(&w[k]), zero, nan);
-        put(tile + (to[j] & ~1u), to[j] & 1, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+        for (int e = 0; e < 8; ++e) nan = __hfma2(*reinterpret_cast<const __half2*>(&w[e]), zero, nan);
+        uint8_t* at = tile + sm.v_to[lt + (j + k) * kGroupThreads];
+        *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(at) ^ 16) = make_uint4(w[4], w[5], w[6], w[7]);
       }
     }
     if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
@@ -518,26 +514,6 @@ struct SoftRow {
 // x 2^d for d <= 0, in two steps: neither factor underflows where the product does not.
 __device__ __forceinline__ float scaled(float x, float half) { return x * half * half; }
 
-// f(c, scores) for the chunks c in turn, the next one's scores under way.  (Short loops: with the steps unrolled, warps
-// waited for instructions a quarter of their time.)
-template <typename F>
-__device__ __forceinline__ void each_chunk(uint32_t at, int chunks, F f) {
-  uint32_t x[16], y[16];
-  tmem_load16(at, x);
-#pragma unroll 1
-  for (int c = 0; c < chunks; c += 2) {
-    tmem_loaded16(x);
-    const bool second = c + 1 < chunks;
-    if (second) tmem_load16(at + 16 * c + 16, y);
-    f(c, x);
-    if (second) {
-      tmem_loaded16(y);
-      if (c + 2 < chunks) tmem_load16(at + 16 * c + 32, x);
-      f(c + 1, y);
-    }
-  }
-}
-
 // A row's part of a step, up to 64 keys: scores in columns from `at` on become probabilities times their values' scale, in halves (a chunk's sixteen
 // columns: eight of first ones, eight of second ones); l goes on.  The first half is the number cut off after eleven bits, the
 // second the rest of it, rounded.
@@ -545,10 +521,13 @@ __device__ __forceinline__ void each_chunk(uint32_t at, int chunks, F f) {
 // a row does not see gets 0, and what it sees of a scale without a number NaN; and the score is rounded before
 // reference is taken off: the fused product is off by half a step of the reference, which large scores make a large power.
 template <bool kPlain>
-__device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float* scales, float f0, uint64_t sees, SoftRow& s) {
+__device__ __forceinline__ void soft_probs(uint32_t at, const uint32_t* scores, int chunks, const float* scales, float f0, uint64_t sees, SoftRow& s) {
   f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
   const f32x2 nm = pair(-s.m, -s.m), minus = pair(-1.f, -1.f);
-  const auto chunk = [&](int c, const uint32_t* x) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (c >= chunks) break;
+    const uint32_t* x = scores + 16 * c;
     const float f = f0 * scales[c], vs = scales[kTileChunks + c];
     const uint32_t w = kPlain ? 0u : (uint32_t)(sees >> (16 * c));
     uint32_t o[16];
@@ -577,8 +556,7 @@ __device__ __forceinline__ void soft_probs(uint32_t at, int chunks, const float*
       o[8 + e] = pack_half(rest.x, rest.y);
     }
     tmem_store16(at + 16 * c, o);
-  };
-  each_chunk(at, chunks, chunk);
+  }
   const float2 s2 = unpair(add2(sum[0], sum[1]));
   s.l += s2.x + s2.y;
   tmem_stored();
@@ -614,54 +592,70 @@ __device__ __forceinline__ void soft_move(uint32_t out, const Before& before, fl
   }
 }
 
+__device__ __forceinline__ void soft_load(uint32_t at, uint32_t* x) {
+  tmem_load32(at, x);
+  tmem_load32(at + 32, x + 32);
+  tmem_loaded(x);
+  tmem_loaded(x + 32);
+}
+
 // The row's largest score less its base, plus log2 of the values' scale (`scale`: or without), of what it sees.
-static __device__ __noinline__ float soft_top(uint32_t at, int chunks, const float* scales, float f0, uint64_t sees, float base, bool scale) {
+__device__ __forceinline__ float soft_top(const uint32_t* x, const float* scales, float f0, uint64_t sees, float base, bool scale) {
   float top = -INFINITY;
-  each_chunk(at, chunks, [&](int c, const uint32_t* x) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {                              // (scales past the step: not seen)
     const uint32_t w = (uint32_t)(sees >> (16 * c));
+    const float f = f0 * scales[c], lw = scale ? scales[2 * kTileChunks + c] : 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = (__fmul_rn(__uint_as_float(x[e]), f0 * scales[c]) - base) + (scale ? scales[2 * kTileChunks + c] : 0.f);
+      const float y = (__fmul_rn(__uint_as_float(x[16 * c + e]), f) - base) + lw;
       top = w >> e & 1 ? fmaxf(top, y) : top;
     }
-  });
+  }
   return top;
 }
 
 // A step where some row does not see all, or of unusual scales.
 template <int kD>
-__device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees,
-                                         Before before, SoftRow s) {
+__device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees, Before before,
+                                         SoftRow s) {
+  uint32_t x[64];
+  soft_load(at, x);
   // a base for scores past 2^20: of the row's own, when they pass the old one or nothing has been seen
-  const float raw = soft_top(at, chunks, scales, f0, sees, s.base, false);
-  const bool large = fabsf(raw) < INFINITY && (s.m > kNone ? raw > kMostPlain : fabsf(raw) > kMostPlain);
+  float top = soft_top(x, scales, f0, sees, s.base, false);
+  const bool large = fabsf(top) < INFINITY && (s.m > kNone ? top > kMostPlain : fabsf(top) > kMostPlain);
   if (__any_sync(0xffffffffu, large)) {
-    const float base = large ? s.base + raw : s.base;
+    const float base = large ? s.base + top : s.base;
     if (s.m > kNone) s.m = fmaxf(s.m + (s.base - base), kNone);
     s.base = base;
   }
-  const float top = soft_top(at, chunks, scales, f0, sees, s.base, true);
+  top = soft_top(x, scales, f0, sees, s.base, true);
   const bool move = top > s.m + kSlack;
   if (__any_sync(0xffffffffu, move)) {
     const float now = move ? top : s.m, d = s.m - now;
     s.m = now;
     soft_move<kD>(out, before, d, s);
   }
-  soft_probs<false>(at, chunks, scales, f0, sees, s);
+  soft_probs<false>(at, x, chunks, scales, f0, sees, s);
   return s;
 }
 
 // An ordinary step: the row's largest score first, against which its reference may move.
 template <int kD>
 __device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, const Before& before, SoftRow& s) {
+  uint32_t x[64];
+  soft_load(at, x);
   float top = -INFINITY;
-  each_chunk(at, chunks, [&](int c, const uint32_t* r) {
-    float x[5];
 #pragma unroll
-    for (int e = 0; e < 5; ++e) x[e] = max3(__uint_as_float(r[3 * e]), __uint_as_float(r[3 * e + 1]), __uint_as_float(r[3 * e + 2]));
-    const float most = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], __uint_as_float(r[15])));
+  for (int c = 0; c < 4; ++c) {
+    if (c >= chunks) break;
+    const uint32_t* r = x + 16 * c;
+    float y[5];
+#pragma unroll
+    for (int e = 0; e < 5; ++e) y[e] = max3(__uint_as_float(r[3 * e]), __uint_as_float(r[3 * e + 1]), __uint_as_float(r[3 * e + 2]));
+    const float most = fmaxf(max3(y[0], y[1], y[2]), max3(y[3], y[4], __uint_as_float(r[15])));
     top = fmaxf(top, fmaf(most, f0 * scales[c], scales[2 * kTileChunks + c]));
-  });
+  }
   // the reference moves when a score passes it by 2^kSlack
   const bool move = top > s.m + kSlack;
   if (__any_sync(0xffffffffu, move || s.base != 0.f)) {
@@ -673,7 +667,7 @@ __device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks,
     s.m = now;
     soft_move<kD>(out, before, d, s);
   }
-  soft_probs<true>(at, chunks, scales, f0, 0, s);
+  soft_probs<true>(at, x, chunks, scales, f0, 0, s);
 }
 
 template <int kD>
@@ -709,31 +703,38 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
     SoftRow mine{kNone, 0.f, 0.f};
+    // what the row sees of a step's keys from key0 on
+    const auto seen = [&](int key0, uint32_t absent) {
+      uint64_t can = (below(at0 - key0) | placed(set, at0 - key0)) & below(chunks * kChunk);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (absent >> (chunk0 + c) & 1) can &= ~(0xffffull << (16 * c));
+      return live ? can : 0ull;
+    };
+    // NaN among the values that a row saw two steps ago, whose products are done: its own affair, since they are 0 for the others
+    const auto look_for_nan = [&](int t, int n) {
+      const int slot = t & (kScaleRing - 1);
+      const uint4 nan = *reinterpret_cast<const uint4*>(sm.nan_keys[slot]);
+      if (nan.x | nan.y | nan.z | nan.w) {
+        const uint64_t lo = nan.x | (uint64_t)nan.y << 32, hi = nan.z | (uint64_t)nan.w << 32;
+        const uint64_t keys = !chunk0 ? lo : chunk0 == 4 ? hi : lo >> (16 * chunk0) | hi << (64 - 16 * chunk0);
+        if (seen((g.step0 + n) * A.step + chunk0 * kChunk, sm.absent[slot]) & keys) mine.l = NAN;
+      }
+    };
 #pragma unroll 1
     for (int n = 0; n < g.steps; ++n, ++t) {
       if (!warp_wait(&sm.s_full[t & 1], t >> 1 & 1, dead)) return;
       tmem_after_sync();
+      if (n >= 2) look_for_nan(t - 2, n - 2);
       const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step + chunk0 * kChunk;
       const uint32_t absent = sm.absent[slot], at = lanes + (t & 1) * kTileKeys + chunk0 * kChunk;
       const float* scales = sm.scales[slot] + chunk0;
       const Before before{n ? &sm.v_free[(t - 1) % kVStages] : nullptr, (uint32_t)((t - 1) / kVStages & 1), dead};
-      uint64_t sees = below(chunks * kChunk);
       if (absent >> 31 && key0 + chunks * kChunk <= at0 && A.scale2 >= 0.f) {
         if (busy) soft_tile<kD>(at, out + s * 128, chunks, scales, f0, before, mine);
       } else if (busy) {
-        uint64_t can = below(at0 - key0) | placed(set, at0 - key0);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (absent >> (chunk0 + c) & 1) can &= ~(0xffffull << (16 * c));
-        sees = live ? sees & can : 0;
+        const uint64_t sees = seen(key0, absent);
         mine = soft_any<kD>(at, out + s * 128, chunks, scales, f0, sees, before, mine);
-      }
-      // NaN among the values that a row sees: its own affair, since they are 0 for the others
-      if (!warp_wait(&sm.v_full[t % kVStages], t / kVStages & 1, dead)) return;
-      const uint4 nan = *reinterpret_cast<const uint4*>(sm.nan_keys[slot]);
-      if (nan.x | nan.y | nan.z | nan.w) {
-        const uint64_t lo = nan.x | (uint64_t)nan.y << 32, hi = nan.z | (uint64_t)nan.w << 32;
-        if (sees & (!chunk0 ? lo : chunk0 == 4 ? hi : lo >> (16 * chunk0) | hi << (64 - 16 * chunk0))) mine.l = NAN;
       }
       tmem_before_sync();
       warp_arrive(&sm.p_full[t & 1][s], lane);
@@ -741,6 +742,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     // the segment's rows: both groups' sums, a half of the columns each
     if (!warp_wait(&sm.o_full, seg & 1, dead)) return;
     tmem_after_sync();
+    if (g.steps > 1) look_for_nan(t - 2, g.steps - 2);
+    look_for_nan(t - 1, g.steps - 1);
     sm.ml[s][0][row] = mine.m;
     sm.ml[s][1][row] = mine.l;
     sm.ml[s][2][row] = mine.base;
