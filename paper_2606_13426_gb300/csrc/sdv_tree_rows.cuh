@@ -5,10 +5,10 @@
 //   S = Q K' (tensor memory, fp32), P = 2^(S f - m) vs, O += P V.
 // A row is a lane of tensor memory and a thread of a softmax warp, so that its maximum and sum need no exchange; a page's
 // scales are one number for 16 keys or more.  Three kinds of warps work at once:
-//   * one warp plans: which part of which item comes next;
+//   * one warp plans: which part of which item comes next, and what its nodes see of the tree;
 //   * one warp copies: a step's pages of codes, in bulk, into rings of steps of keys and of values;
 //   * loading warps widen them to f16 (exactly; a value's NaN becomes 0 and is told apart), the matrix unit's operands;
-//   * one warp issues the products;
+//   * two warps issue the products, scores and output, each as soon as it can;
 //   * two groups of softmax warps take a half of each step's keys, each with references and sums of its own, joined
 //     at the end of a segment.  The scores of the next step are had meanwhile, in the other half of their memory.
 // Queries go through f16: bf16 ones under a power of two of their row.  Probabilities times their value's scale
@@ -26,8 +26,8 @@
 namespace sdv {
 
 constexpr int kTileRows = 128;
-constexpr int kSoftWarps = 8, kLoadWarps = 8, kMmaWarp = kSoftWarps + kLoadWarps, kPlanWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
-constexpr int kTreeThreads = 32 * (kMmaWarp + 4);
+constexpr int kSoftWarps = 8, kLoadWarps = 8, kScoreWarp = kSoftWarps + kLoadWarps, kPlanWarp = kScoreWarp + 1, kCopyWarp = kScoreWarp + 2, kOutWarp = kScoreWarp + 3;
+constexpr int kTreeThreads = 32 * (kScoreWarp + 4);
 constexpr int kGroupWarps = kLoadWarps / 2, kGroupThreads = 32 * kGroupWarps;   // of the loading warps: keys, values
 constexpr int kKStages = 1, kVStages = 2;          // of widened operands: keys are free again once the scores are had
 constexpr int kRawK = 2, kRawV = 3;                // steps of codes under way
@@ -51,6 +51,8 @@ struct alignas(16) TreeSmall {
   uint64_t seg_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
   uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
+  uint64_t sets[kSegRing][SDV_MAX_TREE];          // what their nodes see of the tree
+  int64_t before[kPrefixFrom + 1];                // steps before each sequence, where they are few
   uint16_t v_to[kTileChunks * 128];               // (Loader::init)
   float downs[kSegRing][kTileRows];               // what a row's queries were divided by
   float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
@@ -77,6 +79,7 @@ struct TreeShape {
 struct TreeRowsArgs {
   AttendArgs a;                    // RT: row tiles, R: rows; part: 2 slots a CTA
   int rows, teams;                 // rows of a tile; teams of RT CTAs
+  int join_rows;                   // of a warp of k_tree_join
 };
 
 __device__ __forceinline__ int tree_runs(int64_t units, int teams) {
@@ -116,47 +119,75 @@ __device__ __forceinline__ int first_half(int chunks) { return (chunks + 1) / 2;
 __device__ __forceinline__ void plan_role(const TreeRowsArgs& T, TreeSmall& sm, int team, int lane) {
   const AttendArgs& A = T.a;
   const int per = A.c.H;
-  const int64_t units = step_sums<true, 0>(A, 0, lane).total * per;
+  int64_t total = 0;
+  if (A.prefix) {
+    total = A.prefix[A.B];
+  } else {
+    int64_t sum = 0;
+    for (int b0 = 0; b0 < A.B; b0 += 32) {
+      const int mine = b0 + lane < A.B ? seq_of<true, 0>(A, b0 + lane).steps : 0;
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += x;
+      }
+      if (b0 + lane <= A.B) sm.before[b0 + lane] = sum + inc - mine;
+      sum += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) sm.before[A.B] = sum;
+    __syncwarp();
+    total = sum;
+  }
+  const auto before = [&](int b) { return A.prefix ? A.prefix[b] : sm.before[b]; };
+  // the last sequence whose steps begin at `at` or earlier, of which there are `total` in all: 32 places at a time
+  const auto find = [&](int64_t at) {
+    int lo = 0, hi = A.B;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, here = lo + lane * step;
+      const unsigned le = __ballot_sync(0xffffffffu, here < hi && before(here) <= at);
+      const int k = 31 - __clz(le);                        // (lane 0 holds)
+      hi = min(hi, lo + (k + 1) * step);
+      lo += k * step;
+    }
+    return lo;
+  };
+  const int64_t units = total * per;
   const int runs = tree_runs(units, T.teams);
-  int64_t u = 0, u_end = 0, seq_u = 0;
-  int b = 0;
+  int64_t u = 0, u_end = 0;
   if (team < runs) {
     u = run_start(units, team, runs);
     u_end = run_start(units, team + 1, runs);
-    const Found f = find_sequence<true, 0>(A, u / per, lane);
-    b = f.b;
-    seq_u = f.before * per;
   }
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
     Segment g{};
-    while (u < u_end && b < A.B) {
+    if (u < u_end) {
+      const int b = find(u / per);
+      const int64_t seq_u = before(b) * per;
       const Seq sq = seq_of<true, 0>(A, b);
-      const int64_t mine = (int64_t)sq.steps * per;
-      if (u >= seq_u + mine) {                            // on to the next sequence, or over empty ones
-        seq_u += mine;
-        if (++b == A.B) break;
-        if (!seq_of<true, 0>(A, b).steps) {
-          const Found f = find_sequence<true, 0>(A, u / per, lane);
-          b = f.b;
-          seq_u = f.before * per;
-        }
-        continue;
+      if (u >= seq_u && u < seq_u + (int64_t)sq.steps * per) {   // (else the lengths have changed meanwhile)
+        const int item = (int)((u - seq_u) / sq.steps);
+        g.b = b, g.h = item, g.step0 = (int)(u - seq_u - (int64_t)item * sq.steps);
+        g.steps = (int)min((int64_t)sq.steps - g.step0, u_end - u);
+        g.len = sq.len, g.count = sq.count;
+        g.whole = g.steps == sq.steps;
+        g.slot = seg ? 1 : 0;
+        u += g.steps;
       }
-      if (u < seq_u) break;                               // (only if the lengths have changed meanwhile)
-      const int item = (int)((u - seq_u) / sq.steps);
-      const int64_t item_u = seq_u + (int64_t)item * sq.steps;
-      g.b = b, g.h = item, g.step0 = (int)(u - item_u);
-      g.steps = (int)min((int64_t)sq.steps, u_end - item_u) - g.step0;
-      g.len = sq.len, g.count = sq.count;
-      g.whole = g.steps == sq.steps;
-      g.slot = seg ? 1 : 0;
-      u += g.steps;
-      break;
+    }
+    uint64_t a0 = 0, a1 = 0;
+    if (g.steps) {
+      bool bad = false;
+      const int32_t* parents = A.parents + (int64_t)g.b * A.W;
+      ancestors(lane < A.W ? parent_of(parents[lane], lane, bad) : -1, 32 + lane < A.W ? parent_of(parents[32 + lane], 32 + lane, bad) : -1,
+                lane, a0, a1);
     }
     const int slot = seg & (kSegRing - 1);
     if (seg >= kSegRing && !warp_wait(&sm.seg_done[slot], (seg / kSegRing - 1) & 1, &sm.dead)) return;
     if (lane == 0) sm.segs[slot] = g;
+    sm.sets[slot][lane] = a0;
+    sm.sets[slot][32 + lane] = a1;
     warp_arrive(&sm.seg_full[slot], lane);
     if (!g.steps) return;
   }
@@ -338,31 +369,30 @@ struct Loader {
     }
     if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
   }
-  // The rows' queries, a thread a row.
+  // The rows' queries, D / 8 lanes a row.
   __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
-    const int row = lt, r = rt * rows + row, i = r / A.G;
-    const bool live = row < rows && r < A.R && i < g.count;
-    const int64_t at = live ? g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh : 0;
-    constexpr int kEights = kD / 8;
-    float most = 0.f;
-    if (A.bf16 && live) {
-#pragma unroll 8
-      for (int e = 0; e < kEights; ++e) most = fmaxf(most, q_largest(q_load8(A, at + e * 8), true));
-    }
-    const int up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;       // takes the largest to [2^15, 2^16)
-#pragma unroll 8
-    for (int e = 0; e < kEights; ++e) {
-      uint4 v = live ? q_load8(A, at + e * 8) : make_uint4(0, 0, 0, 0);
-      if (A.bf16) {
+    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes;
+    const int e8 = lt % kLanes;
+#pragma unroll 4
+    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
+      const int r = rt * rows + row, i = r / A.G;
+      const bool live = row < rows && r < A.R && i < g.count;
+      uint4 v = live ? q_load8(A, g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8) : make_uint4(0, 0, 0, 0);
+      int up = 0;
+      if (A.bf16) {                                          // takes the row's largest to [2^15, 2^16)
+        float most = q_largest(v, true);
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;
         float f[8];
         Num<SDV_BF16>::unpack(v, f);
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] *= pow2(up);
         v = Num<SDV_F16>::pack(f);
       }
-      *reinterpret_cast<uint4*>(smem + S::kQ + (e >> 3) * S::kBlock + swizzled(row, e & 7)) = v;
+      *reinterpret_cast<uint4*>(smem + S::kQ + (e8 >> 3) * S::kBlock + swizzled(row, e8 & 7)) = v;
+      if (e8 == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
     }
-    sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
   }
 };
 
@@ -424,57 +454,80 @@ __device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem
   }
 }
 
-// ------------------------------------------------------------------------------ the warp that issues the products
-// All of its lanes go along, so that addresses and descriptors are the warp's (uniform registers); one of them issues.  (With
-// a single thread in this role a product took 100 cycles to issue, 64 to run.)
+// ------------------------------------------------------------------------------ the warps that issue the products
+// All of a warp's lanes go along, so that addresses and descriptors are the warp's (uniform registers); one of them issues.
+// (With a single thread in this role a product took 100 cycles to issue, 64 to run.)
 template <int kD>
-__device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step) {
+__device__ __forceinline__ void scores_role(uint8_t* smem, TreeSmall& sm, int step) {
   using S = TreeShape<kD>;
   int* dead = &sm.dead;
   const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
-  const uint64_t q = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kQ), 0)), k = q + (S::kK - S::kQ) / 16, v = q + (S::kV - S::kQ) / 16;
+  const uint64_t q = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kQ), 0)), k = q + (S::kK - S::kQ) / 16;
   const uint32_t score = mma_desc(0, kTileRows, step);
-  const int chunks = step / kChunk, half = first_half(chunks);
-  constexpr uint32_t kOut = mma_desc(0, kTileRows, kD);
   const bool one = elected();
   int t = 0;
-  auto scores = [&](int t) {
-    const int st = t % kKStages;
-    if (!warp_wait(&sm.k_full[st], t / kKStages & 1, dead)) return false;
-    tmem_after_sync();
-    const uint32_t to = base + (t & 1) * kTileKeys;
-    const uint64_t kt = k + st * (S::kTile / 16);
-    if (one) {
-#pragma unroll 1
-      for (int i = 0; i < kD / 16; ++i) {
-        const int off = ((i >> 2) * S::kBlock + (i & 3) * 32) / 16;
-        mma_ss(to, q + off, kt + off, score, i > 0);
-      }
-      mma_commit(&sm.s_full[t & 1]);
-      mma_commit(&sm.k_free[st]);
-    }
-    __syncwarp();
-    return true;
-  };
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
     const uint32_t turn = seg / kSegRing & 1;
     if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], turn, dead)) break;
     const int steps = __shfl_sync(0xffffffffu, sm.segs[seg & (kSegRing - 1)].steps, 0);
-    if (!steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead) || !scores(t)) break;
+    if (!steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead)) break;
     bool ok = true;
 #pragma unroll 1
-    for (int n = 0; n < steps && ok; ++n, ++t) {
-      if (n + 1 < steps) ok = scores(t + 1);
+    for (const int end = t + steps; t < end; ++t) {
+      const int st = t % kKStages;
+      // the probabilities two steps ago, in whose place the scores go, are used
+      ok = (t < 2 || warp_wait(&sm.v_free[t % kVStages], ((t >> 1) - 1) & 1, dead)) && warp_wait(&sm.k_full[st], t / kKStages & 1, dead);
+      if (!ok) break;
+      tmem_after_sync();
+      const uint32_t to = base + (t & 1) * kTileKeys;
+      const uint64_t kt = k + st * (S::kTile / 16);
+      if (one) {
+#pragma unroll 1
+        for (int i = 0; i < kD / 16; ++i) {
+          const int off = ((i >> 2) * S::kBlock + (i & 3) * 32) / 16;
+          mma_ss(to, q + off, kt + off, score, i > 0);
+        }
+        mma_commit(&sm.s_full[t & 1]);
+        mma_commit(&sm.k_free[st]);
+      }
+      __syncwarp();
+    }
+    if (!ok) break;
+  }
+  if (one) mma_commit(&sm.drained);                        // nothing is under way when the memory is given back
+  __syncwarp();
+}
+static_assert(kVStages == 2, "");
+
+template <int kD>
+__device__ __forceinline__ void out_role(uint8_t* smem, TreeSmall& sm, int step) {
+  using S = TreeShape<kD>;
+  int* dead = &sm.dead;
+  const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
+  const uint64_t v = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kV), 0));
+  constexpr uint32_t kOut = mma_desc(0, kTileRows, kD);
+  const int chunks = step / kChunk, half = first_half(chunks);
+  const bool one = elected();
+  int t = 0;
+#pragma unroll 1
+  for (int seg = 0;; ++seg) {
+    if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) break;
+    const int steps = __shfl_sync(0xffffffffu, sm.segs[seg & (kSegRing - 1)].steps, 0);
+    if (!steps) break;
+    bool ok = true;
+#pragma unroll 1
+    for (int n = 0; n < steps; ++n, ++t) {
       const int st = t % kVStages;
-      ok = ok && warp_wait(&sm.v_full[st], t / kVStages & 1, dead);
+      const uint32_t p = base + (t & 1) * kTileKeys;
+      const uint64_t vt = v + st * (S::kTile / 16);
+      ok = warp_wait(&sm.v_full[st], t / kVStages & 1, dead);
 #pragma unroll 1
       for (int h = 0; h < 2 && ok; ++h) {                  // a group's keys
         ok = warp_wait(&sm.p_full[t & 1][h], t >> 1 & 1, dead);
         if (!ok) break;
         tmem_after_sync();
-        const uint32_t out = base + 2 * kTileKeys + h * 128, p = base + (t & 1) * kTileKeys;
-        const uint64_t vt = v + st * (S::kTile / 16);
+        const uint32_t out = base + 2 * kTileKeys + h * 128;
         if (one) {
           const int i0 = h ? half : 0, i1 = h ? chunks : half;
 #pragma unroll 1
@@ -490,10 +543,11 @@ __device__ __forceinline__ void mma_role(uint8_t* smem, TreeSmall& sm, int step)
         }
         __syncwarp();
       }
+      if (!ok) break;
     }
     if (!ok) break;
   }
-  if (one) mma_commit(&sm.drained);                        // nothing is under way when the memory is given back
+  if (one) mma_commit(&sm.drained);
   __syncwarp();
   int ignore = 0;
   warp_wait(&sm.drained, 0, &ignore);
@@ -690,16 +744,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     if (!g.steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead)) return;
     const bool have = row < T.rows && r < A.R, live = have && i < g.count;
     const bool busy = __any_sync(0xffffffffu, live);
-    uint64_t set;
-    {
-      bool bad = false;
-      const int32_t* parents = A.parents + (int64_t)g.b * A.W;
-      uint64_t a0, a1;
-      ancestors(lane < A.W ? parent_of(parents[lane], lane, bad) : -1, 32 + lane < A.W ? parent_of(parents[32 + lane], 32 + lane, bad) : -1,
-                lane, a0, a1);
-      const uint64_t lo = __shfl_sync(0xffffffffu, a0, i & 31), hi = __shfl_sync(0xffffffffu, a1, i & 31);
-      set = !live ? 0 : i < 32 ? lo : hi;
-    }
+    const uint64_t set = live ? sm.sets[seg & (kSegRing - 1)][i] : 0;
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
     SoftRow mine{kNone, 0.f, 0.f};
@@ -816,7 +861,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   uint8_t* smem = raw + (-smem_addr(raw) & 1023);
   TreeSmall& sm = *reinterpret_cast<TreeSmall*>(smem + S::kSmallAt);
   const int tid = threadIdx.x, warp = tid >> 5, team = blockIdx.x / T.a.RT, rt = blockIdx.x - team * T.a.RT;
-  if (warp == kMmaWarp) tmem_alloc(&sm.tmem, 512);
+  if (warp == kScoreWarp) tmem_alloc(&sm.tmem, 512);
   if (tid == 0) {
     for (int k = 0; k < 2; ++k) {
       barrier_init(&sm.s_full[k], 1);
@@ -845,7 +890,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
       barrier_init(&sm.rv_free[k], kGroupWarps);
     }
     barrier_init(&sm.o_full, 1);
-    barrier_init(&sm.drained, 1);
+    barrier_init(&sm.drained, 2);
     barrier_init(&sm.soft, kSoftWarps);
     sm.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -856,7 +901,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   if (warp < kSoftWarps) {
     registers_up<kSoftRegs>();
     soft_role<kD>(T, smem, sm, team, rt, tid);
-  } else if (warp < kMmaWarp) {
+  } else if (warp < kScoreWarp) {
     registers_down<kLoadRegs>();
     if (warp < kSoftWarps + kGroupWarps) keys_role<kD>(T, smem, sm, rt, tid - 32 * kSoftWarps);
     else values_role<kD>(T, smem, sm, tid - 32 * (kSoftWarps + kGroupWarps));
@@ -864,35 +909,37 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
     registers_down<kOtherRegs>();
     if (warp == kPlanWarp) plan_role(T, sm, team, tid & 31);
     else if (warp == kCopyWarp) copy_role<kD>(T, smem, sm, tid & 31);
-    else if (warp == kMmaWarp) mma_role<kD>(smem, sm, T.a.step);
+    else if (warp == kScoreWarp) scores_role<kD>(smem, sm, T.a.step);
+    else out_role<kD>(smem, sm, T.a.step);
   }
   __syncwarp();
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
-  if (warp == kMmaWarp) tmem_free(sm.tmem, 512);
+  if (warp == kScoreWarp) tmem_free(sm.tmem, 512);
   if (sm.dead && tid == 0 && T.a.status) atomicOr(T.a.status, SDV_STATUS_STUCK);
 }
 
-// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A warp a row.
+// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A warp has T.join_rows rows,
+// one after another.
 template <int kD>
 __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T) {
   using S = TreeShape<kD>;
   constexpr int kV = kD / 32;
   const AttendArgs& A = T.a;
-  constexpr int kCtas = kTileRows / kJoinWarps;             // of an item
+  const int ctas = kTileRows / kJoinWarps / T.join_rows;    // of an item
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int ib = blockIdx.x / kCtas, row = blockIdx.x % kCtas * kJoinWarps + warp;
-  const int per = A.c.H * A.RT, b = ib / per, item = ib % per, h = item / A.RT, rt = item % A.RT, r = rt * T.rows + row;
+  const int ib = blockIdx.x / ctas, row0 = (blockIdx.x % ctas * kJoinWarps + warp) * T.join_rows;
+  const int per = A.c.H * A.RT, b = ib / per, item = ib % per, h = item / A.RT, rt = item % A.RT;
   const Sums ts = step_sums<true, 0>(A, b, lane);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (A.status && item == 0 && row == 0) {
+  if (A.status && item == 0 && row0 == 0) {
     bool bad = lane == 0 && A.lengths[b] < min(A.counts ? A.counts[b] : A.W, A.W);
     for (int i = lane; i < min(A.counts ? A.counts[b] : A.W, A.W); i += 32) parent_of(A.parents[(int64_t)b * A.W + i], i, bad);
     if (bad) atomicOr(A.status + b, SDV_STATUS_BAD_TREE);
     if (lane == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
   }
-  if (row >= T.rows || r >= A.R) return;
+  if (row0 >= T.rows || rt * T.rows + row0 >= A.R) return;
   const Seq sq = seq_of<true, 0>(A, b);
   const int64_t units = ts.total * A.c.H, u0 = ts.before * A.c.H + (int64_t)h * sq.steps, u1 = min(u0 + sq.steps, units);
   const int runs = tree_runs(units, T.teams);
@@ -909,38 +956,42 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   }
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
   auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
-  float m = kNone, base = 0.f;
-  const auto higher = [&](float om, float ob) {
-    if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
-  };
-  for (int gi = g0 + lane; gi <= g1; gi += 32) higher(slot_of(gi)[kTileRows * kD + row], slot_of(gi)[kTileRows * kD + kTileRows + row]);
+  for (int row = row0; row < min(row0 + T.join_rows, T.rows); ++row) {
+    const int r = rt * T.rows + row;
+    if (r >= A.R) return;
+    float m = kNone, base = 0.f;
+    const auto higher = [&](float om, float ob) {
+      if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
+    };
+    for (int gi = g0 + lane; gi <= g1; gi += 32) higher(slot_of(gi)[kTileRows * kD + row], slot_of(gi)[kTileRows * kD + kTileRows + row]);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const float om = __shfl_xor_sync(0xffffffffu, m, o), ob = __shfl_xor_sync(0xffffffffu, base, o);
-    higher(om, ob);
-  }
-  float l = 0.f, o[kV];
+    for (int o = 16; o; o >>= 1) {
+      const float om = __shfl_xor_sync(0xffffffffu, m, o), ob = __shfl_xor_sync(0xffffffffu, base, o);
+      higher(om, ob);
+    }
+    float l = 0.f, o[kV];
 #pragma unroll
-  for (int e = 0; e < kV; ++e) o[e] = 0.f;
+    for (int e = 0; e < kV; ++e) o[e] = 0.f;
 #pragma unroll 4
-  for (int gi = g0; gi <= g1; ++gi) {
-    const float* slot = slot_of(gi);
-    const float half = ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
-    l += scaled(slot[kTileRows * kD + 2 * kTileRows + row], half);
+    for (int gi = g0; gi <= g1; ++gi) {
+      const float* slot = slot_of(gi);
+      const float half = ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
+      l += scaled(slot[kTileRows * kD + 2 * kTileRows + row], half);
 #pragma unroll
-    for (int e = 0; e < kV; ++e) o[e] += scaled(slot[(int64_t)row * kD + e * 32 + lane], half);
+      for (int e = 0; e < kV; ++e) o[e] += scaled(slot[(int64_t)row * kD + e * 32 + lane], half);
+    }
+    const int i = r / A.G;
+    if (i >= sq.count) l = 0.f;
+    const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
+    const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) put_out(A, to * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
+    if (A.lse && lane == 0) A.lse[to] = lse_of(m, l, base);
   }
-  const int i = r / A.G;
-  if (i >= sq.count) l = 0.f;
-  const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
-  const float by = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < kV; ++e) put_out(A, to * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
-  if (A.lse && lane == 0) A.lse[to] = lse_of(m, l, base);
 }
 
 template <int kD>
-static cudaError_t launch_tree_rows(const TreeRowsArgs& T, cudaStream_t s) {
+static cudaError_t launch_tree_rows(TreeRowsArgs T, cudaStream_t s) {
   using S = TreeShape<kD>;
   const auto kern = k_tree_rows<kD>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
@@ -949,7 +1000,11 @@ static cudaError_t launch_tree_rows(const TreeRowsArgs& T, cudaStream_t s) {
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((int64_t)T.a.B * T.a.c.H * T.a.RT * (kTileRows / kJoinWarps)));
+  // as many rows a warp as leave four CTAs an SM
+  const int64_t items = (int64_t)T.a.B * T.a.c.H * T.a.RT;
+  T.join_rows = 1;
+  while (T.join_rows < kTileRows / kJoinWarps && items * (kTileRows / kJoinWarps / T.join_rows) > 8 * (int64_t)sm_count()) T.join_rows *= 2;
+  cfg.gridDim = dim3((unsigned)(items * (kTileRows / kJoinWarps / T.join_rows)));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
