@@ -47,8 +47,8 @@ struct Segment {
 struct alignas(16) TreeSmall {
   uint64_t rk_full[kRawK], rk_free[kRawK], rv_full[kRawV], rv_free[kRawV];
   uint64_t k_full[kKStages], k_free[kKStages], v_full[kVStages], v_free[kVStages];
-  uint64_t s_full[2], p_full[2][2], o_full, drained;   // p_full: of a step's parity and a group
-  uint64_t seg_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
+  uint64_t s_full[2], p_full[2][2], p_free[2], o_full, drained;   // scores, probabilities: of a step's parity (and a group)
+  uint64_t seg_full[kSegRing], set_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
   uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
   uint64_t sets[kSegRing][SDV_MAX_TREE];          // what their nodes see of the tree
@@ -71,7 +71,8 @@ struct TreeShape {
   static constexpr int kHalf = kTileKeys * kD;                       // codes of half a step
   static constexpr int kQ = 0, kK = kTile, kV = kK + kKStages * kTile, kRk = kV + kVStages * kTile, kRv = kRk + kRawK * kHalf, kSmallAt = kRv + kRawV * kHalf;
   static constexpr size_t kSmem = 1024 + kSmallAt + sizeof(TreeSmall);
-  static constexpr int kSlot = kTileRows * (kD + 3);                 // floats of a partial: output, reference (two numbers), sum
+  // floats of a partial: output [D / 4][row][4], so that a warp's rows are written together; reference (two numbers), sum
+  static constexpr int kSlot = kTileRows * (kD + 3);
   static constexpr int kLoads = kD / 16;                             // sixteens of a thread's keys, or of its values
   static_assert(kSmem <= 227 * 1024, "");
 };
@@ -79,7 +80,6 @@ struct TreeShape {
 struct TreeRowsArgs {
   AttendArgs a;                    // RT: row tiles, R: rows; part: 2 slots a CTA
   int rows, teams;                 // rows of a tile; teams of RT CTAs
-  int join_rows;                   // of a warp of k_tree_join
 };
 
 __device__ __forceinline__ int tree_runs(int64_t units, int teams) {
@@ -176,6 +176,10 @@ __device__ __forceinline__ void plan_role(const TreeRowsArgs& T, TreeSmall& sm, 
         u += g.steps;
       }
     }
+    const int slot = seg & (kSegRing - 1);
+    if (seg >= kSegRing && !warp_wait(&sm.seg_done[slot], (seg / kSegRing - 1) & 1, &sm.dead)) return;
+    if (lane == 0) sm.segs[slot] = g;
+    warp_arrive(&sm.seg_full[slot], lane);
     uint64_t a0 = 0, a1 = 0;
     if (g.steps) {
       bool bad = false;
@@ -183,12 +187,9 @@ __device__ __forceinline__ void plan_role(const TreeRowsArgs& T, TreeSmall& sm, 
       ancestors(lane < A.W ? parent_of(parents[lane], lane, bad) : -1, 32 + lane < A.W ? parent_of(parents[32 + lane], 32 + lane, bad) : -1,
                 lane, a0, a1);
     }
-    const int slot = seg & (kSegRing - 1);
-    if (seg >= kSegRing && !warp_wait(&sm.seg_done[slot], (seg / kSegRing - 1) & 1, &sm.dead)) return;
-    if (lane == 0) sm.segs[slot] = g;
     sm.sets[slot][lane] = a0;
     sm.sets[slot][32 + lane] = a1;
-    warp_arrive(&sm.seg_full[slot], lane);
+    warp_arrive(&sm.set_full[slot], lane);
     if (!g.steps) return;
   }
 }
@@ -371,27 +372,37 @@ struct Loader {
   }
   // The rows' queries, D / 8 lanes a row.
   __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
-    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes;
+    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes, kRows = kTileRows / kAtOnce, kBatch = 8;
     const int e8 = lt % kLanes;
-#pragma unroll 4
-    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
-      const int r = rt * rows + row, i = r / A.G;
-      const bool live = row < rows && r < A.R && i < g.count;
-      uint4 v = live ? q_load8(A, g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8) : make_uint4(0, 0, 0, 0);
-      int up = 0;
-      if (A.bf16) {                                          // takes the row's largest to [2^15, 2^16)
-        float most = q_largest(v, true);
+#pragma unroll 1
+    for (int k0 = 0; k0 < kRows; k0 += kBatch) {
+      uint4 x[kBatch];
 #pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;
-        float f[8];
-        Num<SDV_BF16>::unpack(v, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] *= pow2(up);
-        v = Num<SDV_F16>::pack(f);
+      for (int k = 0; k < kBatch; ++k) {
+        const int row = lt / kLanes + (k0 + k) * kAtOnce, r = rt * rows + row, i = r / A.G;
+        x[k] = make_uint4(0, 0, 0, 0);
+        if (row < rows && r < A.R && i < g.count)
+          x[k] = q_load8(A, g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8);
       }
-      *reinterpret_cast<uint4*>(smem + S::kQ + (e8 >> 3) * S::kBlock + swizzled(row, e8 & 7)) = v;
-      if (e8 == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int row = lt / kLanes + (k0 + k) * kAtOnce;
+        uint4 v = x[k];
+        int up = 0;
+        if (A.bf16) {                                        // takes the row's largest to [2^15, 2^16)
+          float most = q_largest(v, true);
+#pragma unroll
+          for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;
+          float f[8];
+          Num<SDV_BF16>::unpack(v, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] *= pow2(up);
+          v = Num<SDV_F16>::pack(f);
+        }
+        *reinterpret_cast<uint4*>(smem + S::kQ + (e8 >> 3) * S::kBlock + swizzled(row, e8 & 7)) = v;
+        if (e8 == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
+      }
     }
   }
 };
@@ -477,7 +488,7 @@ __device__ __forceinline__ void scores_role(uint8_t* smem, TreeSmall& sm, int st
     for (const int end = t + steps; t < end; ++t) {
       const int st = t % kKStages;
       // the probabilities two steps ago, in whose place the scores go, are used
-      ok = (t < 2 || warp_wait(&sm.v_free[t % kVStages], ((t >> 1) - 1) & 1, dead)) && warp_wait(&sm.k_full[st], t / kKStages & 1, dead);
+      ok = (t < 2 || warp_wait(&sm.p_free[t & 1], ((t >> 1) - 1) & 1, dead)) && warp_wait(&sm.k_full[st], t / kKStages & 1, dead);
       if (!ok) break;
       tmem_after_sync();
       const uint32_t to = base + (t & 1) * kTileKeys;
@@ -498,7 +509,6 @@ __device__ __forceinline__ void scores_role(uint8_t* smem, TreeSmall& sm, int st
   if (one) mma_commit(&sm.drained);                        // nothing is under way when the memory is given back
   __syncwarp();
 }
-static_assert(kVStages == 2, "");
 
 template <int kD>
 __device__ __forceinline__ void out_role(uint8_t* smem, TreeSmall& sm, int step) {
@@ -537,6 +547,7 @@ __device__ __forceinline__ void out_role(uint8_t* smem, TreeSmall& sm, int step)
             mma_ts(out, p + i * 16 + 8, vt + off, kOut, true);
           }
           if (h) {
+            mma_commit(&sm.p_free[t & 1]);
             mma_commit(&sm.v_free[st]);
             if (n + 1 == steps) mma_commit(&sm.o_full);
           }
@@ -744,6 +755,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     if (!g.steps || !warp_wait(&sm.q_full[seg & (kSegRing - 1)], turn, dead)) return;
     const bool have = row < T.rows && r < A.R, live = have && i < g.count;
     const bool busy = __any_sync(0xffffffffu, live);
+    if (!warp_wait(&sm.set_full[seg & (kSegRing - 1)], turn, dead)) return;
     const uint64_t set = live ? sm.sets[seg & (kSegRing - 1)][i] : 0;
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
@@ -774,7 +786,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
       const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step + chunk0 * kChunk;
       const uint32_t absent = sm.absent[slot], at = lanes + (t & 1) * kTileKeys + chunk0 * kChunk;
       const float* scales = sm.scales[slot] + chunk0;
-      const Before before{n ? &sm.v_free[(t - 1) % kVStages] : nullptr, (uint32_t)((t - 1) / kVStages & 1), dead};
+      const Before before{n ? &sm.p_free[(t - 1) & 1] : nullptr, (uint32_t)((t - 1) >> 1 & 1), dead};
       if (absent >> 31 && key0 + chunks * kChunk <= at0 && A.scale2 >= 0.f) {
         if (busy) soft_tile<kD>(at, out + s * 128, chunks, scales, f0, before, mine);
       } else if (busy) {
@@ -833,9 +845,9 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
             for (int e = 0; e < 32; ++e) put_out(A, to * kD + col + e, o[e]);
           }
         } else {
-          float4* y = reinterpret_cast<float4*>(part + (int64_t)row * kD + col);
+          float4* y = reinterpret_cast<float4*>(part) + (col / 4) * kTileRows + row;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
+          for (int e = 0; e < 8; ++e) y[e * kTileRows] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
         }
       }
       if (have && s == 0) {
@@ -867,9 +879,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
       barrier_init(&sm.s_full[k], 1);
       barrier_init(&sm.p_full[k][0], kSoftWarps / 2);
       barrier_init(&sm.p_full[k][1], kSoftWarps / 2);
+      barrier_init(&sm.p_free[k], 1);
     }
     for (int k = 0; k < kSegRing; ++k) {
       barrier_init(&sm.seg_full[k], 1);
+      barrier_init(&sm.set_full[k], 1);
       barrier_init(&sm.seg_done[k], kSoftWarps);
       barrier_init(&sm.q_full[k], kGroupWarps);
     }
@@ -920,26 +934,24 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   if (sm.dead && tid == 0 && T.a.status) atomicOr(T.a.status, SDV_STATUS_STUCK);
 }
 
-// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A warp has T.join_rows rows,
-// one after another.
+// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A CTA has 32 rows, a lane each;
+// its warps take eight columns at a time.
 template <int kD>
 __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T) {
   using S = TreeShape<kD>;
-  constexpr int kV = kD / 32;
   const AttendArgs& A = T.a;
-  const int ctas = kTileRows / kJoinWarps / T.join_rows;    // of an item
+  constexpr int kCtas = kTileRows / 32;                      // of an item
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int ib = blockIdx.x / ctas, row0 = (blockIdx.x % ctas * kJoinWarps + warp) * T.join_rows;
-  const int per = A.c.H * A.RT, b = ib / per, item = ib % per, h = item / A.RT, rt = item % A.RT;
+  const int ib = blockIdx.x / kCtas, row = blockIdx.x % kCtas * 32 + lane;
+  const int per = A.c.H * A.RT, b = ib / per, item = ib % per, h = item / A.RT, rt = item % A.RT, r = rt * T.rows + row;
   const Sums ts = step_sums<true, 0>(A, b, lane);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (A.status && item == 0 && row0 == 0) {
+  if (A.status && item == 0 && blockIdx.x % kCtas == 0 && warp == 0) {
     bool bad = lane == 0 && A.lengths[b] < min(A.counts ? A.counts[b] : A.W, A.W);
     for (int i = lane; i < min(A.counts ? A.counts[b] : A.W, A.W); i += 32) parent_of(A.parents[(int64_t)b * A.W + i], i, bad);
     if (bad) atomicOr(A.status + b, SDV_STATUS_BAD_TREE);
     if (lane == 0 && A.lengths[b] > A.c.max_pages * A.c.block) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
   }
-  if (row0 >= T.rows || rt * T.rows + row0 >= A.R) return;
   const Seq sq = seq_of<true, 0>(A, b);
   const int64_t units = ts.total * A.c.H, u0 = ts.before * A.c.H + (int64_t)h * sq.steps, u1 = min(u0 + sq.steps, units);
   const int runs = tree_runs(units, T.teams);
@@ -954,44 +966,50 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
     while (run_start(units, g1, runs) > u1 - 1) --g1;
     if (g0 == g1) return;                                   // written by that run's CTA
   }
+  if (row >= T.rows || r >= A.R) return;
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
-  auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
-  for (int row = row0; row < min(row0 + T.join_rows, T.rows); ++row) {
-    const int r = rt * T.rows + row;
-    if (r >= A.R) return;
-    float m = kNone, base = 0.f;
-    const auto higher = [&](float om, float ob) {
-      if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
-    };
-    for (int gi = g0 + lane; gi <= g1; gi += 32) higher(slot_of(gi)[kTileRows * kD + row], slot_of(gi)[kTileRows * kD + kTileRows + row]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const float om = __shfl_xor_sync(0xffffffffu, m, o), ob = __shfl_xor_sync(0xffffffffu, base, o);
-      higher(om, ob);
-    }
-    float l = 0.f, o[kV];
-#pragma unroll
-    for (int e = 0; e < kV; ++e) o[e] = 0.f;
+  const auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
+  float m = kNone, base = 0.f, l = 0.f;
+#pragma unroll 4
+  for (int gi = g0; gi <= g1; ++gi) {
+    const float om = slot_of(gi)[kTileRows * kD + row], ob = slot_of(gi)[kTileRows * kD + kTileRows + row];
+    if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
+  }
+  const auto weight = [&](const float* slot) {
+    return ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
+  };
+#pragma unroll 4
+  for (int gi = g0; gi <= g1; ++gi) l += scaled(slot_of(gi)[kTileRows * kD + 2 * kTileRows + row], weight(slot_of(gi)));
+  const int i = r / A.G;
+  if (i >= sq.count) l = 0.f;
+  const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  for (int c8 = warp; c8 < kD / 8; c8 += kJoinWarps) {
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int gi = g0; gi <= g1; ++gi) {
       const float* slot = slot_of(gi);
-      const float half = ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
-      l += scaled(slot[kTileRows * kD + 2 * kTileRows + row], half);
+      const float half = weight(slot);
+      const float4* x = reinterpret_cast<const float4*>(slot) + 2 * c8 * kTileRows + row;
+      const float4 a = x[0], c = x[kTileRows];
+      const float f[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
 #pragma unroll
-      for (int e = 0; e < kV; ++e) o[e] += scaled(slot[(int64_t)row * kD + e * 32 + lane], half);
+      for (int e = 0; e < 8; ++e) o[e] += scaled(f[e], half);
     }
-    const int i = r / A.G;
-    if (i >= sq.count) l = 0.f;
-    const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
-    const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int e = 0; e < kV; ++e) put_out(A, to * kD + e * 32 + lane, l == 0.f ? 0.f : o[e] * by);
-    if (A.lse && lane == 0) A.lse[to] = lse_of(m, l, base);
+    for (int e = 0; e < 8; ++e) o[e] = l == 0.f ? 0.f : o[e] * by;
+    if (A.out_vec) {
+      reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(A.out) + to * kD)[c8] = A.bf16 ? Num<SDV_BF16>::pack(o) : Num<SDV_F16>::pack(o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) put_out(A, to * kD + 8 * c8 + e, o[e]);
+    }
   }
+  if (A.lse && warp == 0) A.lse[to] = lse_of(m, l, base);
 }
 
 template <int kD>
-static cudaError_t launch_tree_rows(TreeRowsArgs T, cudaStream_t s) {
+static cudaError_t launch_tree_rows(const TreeRowsArgs& T, cudaStream_t s) {
   using S = TreeShape<kD>;
   const auto kern = k_tree_rows<kD>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
@@ -1000,11 +1018,7 @@ static cudaError_t launch_tree_rows(TreeRowsArgs T, cudaStream_t s) {
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  // as many rows a warp as leave four CTAs an SM
-  const int64_t items = (int64_t)T.a.B * T.a.c.H * T.a.RT;
-  T.join_rows = 1;
-  while (T.join_rows < kTileRows / kJoinWarps && items * (kTileRows / kJoinWarps / T.join_rows) > 8 * (int64_t)sm_count()) T.join_rows *= 2;
-  cfg.gridDim = dim3((unsigned)(items * (kTileRows / kJoinWarps / T.join_rows)));
+  cfg.gridDim = dim3((unsigned)((int64_t)T.a.B * T.a.c.H * T.a.RT * (kTileRows / 32)));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
