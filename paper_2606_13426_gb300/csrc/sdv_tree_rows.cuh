@@ -370,39 +370,37 @@ struct Loader {
     }
     if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
   }
-  // The rows' queries, D / 8 lanes a row.
+  // The rows' queries, D / 8 lanes a row: first as they are, then, if bf16, made f16 in place.
   __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
-    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes, kRows = kTileRows / kAtOnce, kBatch = 8;
+    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes;
     const int e8 = lt % kLanes;
+    uint8_t* block = smem + S::kQ + (e8 >> 3) * S::kBlock;
 #pragma unroll 1
-    for (int k0 = 0; k0 < kRows; k0 += kBatch) {
-      uint4 x[kBatch];
+    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
+      const int r = rt * rows + row, i = r / A.G;
+      const bool live = row < rows && r < A.R && i < g.count;
+      const int64_t at = live ? g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8 : 0;
+      if (A.q_vec) copy16(smem_addr(block + swizzled(row, e8 & 7)), reinterpret_cast<const uint16_t*>(A.q) + at, live);
+      else *reinterpret_cast<uint4*>(block + swizzled(row, e8 & 7)) = live ? q_load8(A, at) : make_uint4(0, 0, 0, 0);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");         // (a thread's own)
+#pragma unroll 2
+    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
+      int up = 0;
+      if (A.bf16) {                                          // takes the row's largest to [2^15, 2^16)
+        uint4* at = reinterpret_cast<uint4*>(block + swizzled(row, e8 & 7));
+        uint4 v = *at;
+        float most = q_largest(v, true);
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int row = lt / kLanes + (k0 + k) * kAtOnce, r = rt * rows + row, i = r / A.G;
-        x[k] = make_uint4(0, 0, 0, 0);
-        if (row < rows && r < A.R && i < g.count)
-          x[k] = q_load8(A, g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8);
+        for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;
+        float f[8];
+        Num<SDV_BF16>::unpack(v, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= pow2(up);
+        *at = Num<SDV_F16>::pack(f);
       }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int row = lt / kLanes + (k0 + k) * kAtOnce;
-        uint4 v = x[k];
-        int up = 0;
-        if (A.bf16) {                                        // takes the row's largest to [2^15, 2^16)
-          float most = q_largest(v, true);
-#pragma unroll
-          for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-          up = most > 0.f ? min(max(15 - log2_of(most), -112), 100) : 0;
-          float f[8];
-          Num<SDV_BF16>::unpack(v, f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= pow2(up);
-          v = Num<SDV_F16>::pack(f);
-        }
-        *reinterpret_cast<uint4*>(smem + S::kQ + (e8 >> 3) * S::kBlock + swizzled(row, e8 & 7)) = v;
-        if (e8 == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
-      }
+      if (e8 == 0) sm.downs[seg & (kSegRing - 1)][row] = pow2(-up);
     }
   }
 };
@@ -579,52 +577,47 @@ struct SoftRow {
 // x 2^d for d <= 0, in two steps: neither factor underflows where the product does not.
 __device__ __forceinline__ float scaled(float x, float half) { return x * half * half; }
 
-// A row's part of a step, up to 64 keys: scores in columns from `at` on become probabilities times their values' scale, in halves (a chunk's sixteen
-// columns: eight of first ones, eight of second ones); l goes on.  The first half is the number cut off after eleven bits, the
-// second the rest of it, rounded.
-// kPlain: every row sees every key, no scale of keys is negative, none without a number, no reference large.  Else what
-// a row does not see gets 0, and what it sees of a scale without a number NaN; and the score is rounded before
-// reference is taken off: the fused product is off by half a step of the reference, which large scores make a large power.
-template <bool kPlain>
-__device__ __forceinline__ void soft_probs(uint32_t at, const uint32_t* scores, int chunks, const float* scales, float f0, uint64_t sees, SoftRow& s) {
-  f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
-  const f32x2 nm = pair(-s.m, -s.m), minus = pair(-1.f, -1.f);
+// A chunk's sixteen probabilities p, which are added to the sums, times vs, as halves into the chunk's columns: eight of first
+// ones, eight of second ones.  The first half is the number cut off after eleven bits, the second the rest of it, rounded.
+__device__ __forceinline__ void put_probs(uint32_t at, const f32x2* p, float vs, f32x2* sum) {
+  const f32x2 minus = pair(-1.f, -1.f);
+  uint32_t o[16];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (c >= chunks) break;
-    const uint32_t* x = scores + 16 * c;
-    const float f = f0 * scales[c], vs = scales[kTileChunks + c];
-    const uint32_t w = kPlain ? 0u : (uint32_t)(sees >> (16 * c));
-    uint32_t o[16];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x0 = __uint_as_float(x[2 * e]), x1 = __uint_as_float(x[2 * e + 1]);
-      f32x2 p, v;
-      if constexpr (kPlain) {
-        const float2 a = unpair(fma2(pair(x0, x1), pair(f, f), nm));
-        p = pair(ex2(a.x), ex2(a.y));
-        v = mul2(p, pair(vs, vs));
-      } else {
-        const bool none = !(fabsf(vs) < INFINITY) || !(fabsf(f) < INFINITY);
-        float2 a = make_float2(ex2((__fmul_rn(x0, f) - s.base) - s.m), ex2((__fmul_rn(x1, f) - s.base) - s.m));
-        a.x = !(w >> (2 * e) & 1) ? 0.f : none ? NAN : a.x;
-        a.y = !(w >> (2 * e + 1) & 1) ? 0.f : none ? NAN : a.y;
-        p = pair(a.x, a.y);
-        v = none ? p : mul2(p, pair(vs, vs));
-      }
-      sum[e & 1] = add2(sum[e & 1], p);
-      const float2 y = unpair(v);
-      const uint32_t y0 = __float_as_uint(y.x), y1 = __float_as_uint(y.y);
-      const float c0 = __uint_as_float(y0 & 0xffffe000u), c1 = __uint_as_float(y1 & 0xffffe000u);
-      o[e] = pack_half(c0, c1);
-      const float2 rest = unpair(fma2(pair(c0, c1), minus, v));
-      o[8 + e] = pack_half(rest.x, rest.y);
-    }
-    tmem_store16(at + 16 * c, o);
+  for (int e = 0; e < 8; ++e) {
+    const f32x2 v = mul2(p[e], pair(vs, vs));
+    sum[e & 1] = add2(sum[e & 1], p[e]);
+    const float2 y = unpair(v);
+    const float c0 = __uint_as_float(__float_as_uint(y.x) & 0xffffe000u), c1 = __uint_as_float(__float_as_uint(y.y) & 0xffffe000u);
+    o[e] = pack_half(c0, c1);
+    const float2 rest = unpair(fma2(pair(c0, c1), minus, v));
+    o[8 + e] = pack_half(rest.x, rest.y);
   }
+  tmem_store16(at, o);
+}
+__device__ __forceinline__ void add_sums(const f32x2* sum, SoftRow& s) {
   const float2 s2 = unpair(add2(sum[0], sum[1]));
   s.l += s2.x + s2.y;
   tmem_stored();
+}
+
+// A row's part of a step, up to 64 keys: scores in columns from `at` on (and in x) become probabilities times their values'
+// scale; l goes on.  Every row sees every key, no scale of keys is negative, none without a number, no reference large.
+__device__ __forceinline__ void soft_probs(uint32_t at, const uint32_t* x, int chunks, const float* scales, float f0, SoftRow& s) {
+  f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+  const f32x2 nm = pair(-s.m, -s.m);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (c >= chunks) break;
+    const float f = f0 * scales[c];
+    f32x2 p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 a = unpair(fma2(pair(__uint_as_float(x[16 * c + 2 * e]), __uint_as_float(x[16 * c + 2 * e + 1])), pair(f, f), nm));
+      p[e] = pair(ex2(a.x), ex2(a.y));
+    }
+    put_probs(at + 16 * c, p, scales[kTileChunks + c], sum);
+  }
+  add_sums(sum, s);
 }
 
 // By how much the reference (m, base) exceeds that of (m0, base0).
@@ -638,25 +631,26 @@ struct Before {
   int* dead;
 };
 template <int kD>
+__device__ __noinline__ void move_out(uint32_t out, Before before, float half) {
+  warp_wait(before.bar, before.parity, before.dead);        // (given up: so does the next wait)
+  tmem_after_sync();
+  uint32_t r[16];
+#pragma unroll 1
+  for (int g = 0; g < kD / 16; ++g) {
+    tmem_load16(out + 16 * g, r);
+    tmem_loaded16(r);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(scaled(__uint_as_float(r[e]), half));
+    tmem_store16(out + 16 * g, r);
+  }
+  tmem_stored();
+}
+template <int kD>
 __device__ __forceinline__ void soft_move(uint32_t out, const Before& before, float d, SoftRow& s) {
   const float half = ex2(.5f * d);
   s.l = scaled(s.l, half);
-  if (before.bar) {
-    warp_wait(before.bar, before.parity, before.dead);      // (given up: so does the next wait)
-    tmem_after_sync();
-    uint32_t r[32];
-#pragma unroll 1
-    for (int g = 0; g < kD / 32; ++g) {
-      tmem_load32(out + 32 * g, r);
-      tmem_loaded(r);
-#pragma unroll
-      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(scaled(__uint_as_float(r[e]), half));
-      tmem_store32(out + 32 * g, r);
-    }
-    tmem_stored();
-  }
+  if (before.bar) move_out<kD>(out, before, half);
 }
-
 __device__ __forceinline__ void soft_load(uint32_t at, uint32_t* x) {
   tmem_load32(at, x);
   tmem_load32(at + 32, x + 32);
@@ -665,43 +659,68 @@ __device__ __forceinline__ void soft_load(uint32_t at, uint32_t* x) {
 }
 
 // The row's largest score less its base, plus log2 of the values' scale (`scale`: or without), of what it sees.
-__device__ __forceinline__ float soft_top(const uint32_t* x, const float* scales, float f0, uint64_t sees, float base, bool scale) {
+static __device__ __noinline__ float soft_top(uint32_t at, int chunks, const float* scales, float f0, uint64_t sees, float base, bool scale) {
   float top = -INFINITY;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {                              // (scales past the step: not seen)
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
+    uint32_t x[16];
+    tmem_load16(at + 16 * c, x);
     const uint32_t w = (uint32_t)(sees >> (16 * c));
     const float f = f0 * scales[c], lw = scale ? scales[2 * kTileChunks + c] : 0.f;
+    tmem_loaded16(x);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = (__fmul_rn(__uint_as_float(x[16 * c + e]), f) - base) + lw;
+      const float y = (__fmul_rn(__uint_as_float(x[e]), f) - base) + lw;
       top = w >> e & 1 ? fmaxf(top, y) : top;
     }
   }
   return top;
 }
 
-// A step where some row does not see all, or of unusual scales.
+// A step where some row does not see all, or of unusual scales or scores.  What a row does not see gets 0, what it sees of a scale
+// without a number NaN; and the score is rounded before the reference is taken off: the fused product is off by half a step of
+// the reference, which large scores make a large power.
+// (This code runs once or twice a segment, and so from a cold instruction cache: short loops.  With its loops unrolled such a
+// step took 7 us.)
 template <int kD>
 __device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees, Before before,
                                          SoftRow s) {
-  uint32_t x[64];
-  soft_load(at, x);
   // a base for scores past 2^20: of the row's own, when they pass the old one or nothing has been seen
-  float top = soft_top(x, scales, f0, sees, s.base, false);
+  float top = soft_top(at, chunks, scales, f0, sees, s.base, false);
   const bool large = fabsf(top) < INFINITY && (s.m > kNone ? top > kMostPlain : fabsf(top) > kMostPlain);
   if (__any_sync(0xffffffffu, large)) {
     const float base = large ? s.base + top : s.base;
     if (s.m > kNone) s.m = fmaxf(s.m + (s.base - base), kNone);
     s.base = base;
   }
-  top = soft_top(x, scales, f0, sees, s.base, true);
+  top = soft_top(at, chunks, scales, f0, sees, s.base, true);
   const bool move = top > s.m + kSlack;
   if (__any_sync(0xffffffffu, move)) {
     const float now = move ? top : s.m, d = s.m - now;
     s.m = now;
     soft_move<kD>(out, before, d, s);
   }
-  soft_probs<false>(at, x, chunks, scales, f0, sees, s);
+  f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
+    uint32_t x[16];
+    tmem_load16(at + 16 * c, x);
+    const uint32_t w = (uint32_t)(sees >> (16 * c));
+    const float f = f0 * scales[c], vs = scales[kTileChunks + c];
+    const bool none = !(fabsf(vs) < INFINITY) || !(fabsf(f) < INFINITY);
+    tmem_loaded16(x);
+    f32x2 p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float2 a = make_float2(ex2((__fmul_rn(__uint_as_float(x[2 * e]), f) - s.base) - s.m),
+                             ex2((__fmul_rn(__uint_as_float(x[2 * e + 1]), f) - s.base) - s.m));
+      a.x = !(w >> (2 * e) & 1) ? 0.f : none ? NAN : a.x;
+      a.y = !(w >> (2 * e + 1) & 1) ? 0.f : none ? NAN : a.y;
+      p[e] = pair(a.x, a.y);
+    }
+    put_probs(at + 16 * c, p, none ? 1.f : vs, sum);
+  }
+  add_sums(sum, s);
   return s;
 }
 
@@ -732,7 +751,7 @@ __device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks,
     s.m = now;
     soft_move<kD>(out, before, d, s);
   }
-  soft_probs<true>(at, x, chunks, scales, f0, 0, s);
+  soft_probs(at, x, chunks, scales, f0, s);
 }
 
 template <int kD>
@@ -970,7 +989,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
   const auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
   float m = kNone, base = 0.f, l = 0.f;
-#pragma unroll 4
+#pragma unroll 8
   for (int gi = g0; gi <= g1; ++gi) {
     const float om = slot_of(gi)[kTileRows * kD + row], ob = slot_of(gi)[kTileRows * kD + kTileRows + row];
     if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
@@ -978,7 +997,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   const auto weight = [&](const float* slot) {
     return ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
   };
-#pragma unroll 4
+#pragma unroll 8
   for (int gi = g0; gi <= g1; ++gi) l += scaled(slot_of(gi)[kTileRows * kD + 2 * kTileRows + row], weight(slot_of(gi)));
   const int i = r / A.G;
   if (i >= sq.count) l = 0.f;
