@@ -370,13 +370,13 @@ struct Loader {
     }
     if (*reinterpret_cast<const uint32_t*>(&nan) & 0x7fff7fffu) put_nan<kD>(codes, tile, sm.nan_keys[t & (kScaleRing - 1)], A.c.block, lt, live);
   }
-  // The rows' queries, D / 8 lanes a row: first as they are, then, if bf16, made f16 in place.
-  __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg) {
-    constexpr int kLanes = kD / 8, kAtOnce = kGroupThreads / kLanes;
-    const int e8 = lt % kLanes;
+  // The rows' queries, by both groups' threads n, D / 8 lanes a row: first as they are, then, if bf16, made f16 in place.
+  __device__ __forceinline__ void put_queries(const Segment& g, int rt, int rows, int seg, int n) {
+    constexpr int kLanes = kD / 8, kAtOnce = 2 * kGroupThreads / kLanes;
+    const int e8 = n % kLanes;
     uint8_t* block = smem + S::kQ + (e8 >> 3) * S::kBlock;
 #pragma unroll 1
-    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
+    for (int row = n / kLanes; row < kTileRows; row += kAtOnce) {
       const int r = rt * rows + row, i = r / A.G;
       const bool live = row < rows && r < A.R && i < g.count;
       const int64_t at = live ? g.b * A.q_sb + i * A.q_st + (int64_t)(g.h * A.G + r - i * A.G) * A.q_sh + e8 * 8 : 0;
@@ -385,7 +385,7 @@ struct Loader {
     }
     asm volatile("cp.async.wait_all;" ::: "memory");         // (a thread's own)
 #pragma unroll 2
-    for (int row = lt / kLanes; row < kTileRows; row += kAtOnce) {
+    for (int row = n / kLanes; row < kTileRows; row += kAtOnce) {
       int up = 0;
       if (A.bf16) {                                          // takes the row's largest to [2^15, 2^16)
         uint4* at = reinterpret_cast<uint4*>(block + swizzled(row, e8 & 7));
@@ -405,7 +405,7 @@ struct Loader {
   }
 };
 
-// The keys' group, which brings the queries too.
+// The keys' group; both bring a segment's queries.
 template <int kD>
 __device__ __forceinline__ void keys_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int rt, int tid) {
   using S = TreeShape<kD>;
@@ -421,7 +421,7 @@ __device__ __forceinline__ void keys_role(const TreeRowsArgs& T, uint8_t* smem, 
     if (!g.steps) return;
     // its queries, once the last scores before are had
     if (t && !warp_wait(&sm.k_free[(t - 1) % kKStages], (t - 1) / kKStages & 1, dead)) return;
-    L.put_queries(g, rt, T.rows, seg);
+    L.put_queries(g, rt, T.rows, seg, tid);
     fence_async();
     warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
 #pragma unroll 1
@@ -437,7 +437,7 @@ __device__ __forceinline__ void keys_role(const TreeRowsArgs& T, uint8_t* smem, 
   }
 }
 template <int kD>
-__device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int tid) {
+__device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int rt, int tid) {
   using S = TreeShape<kD>;
   Loader<kD> L{T.a, smem, sm};
   L.lt = tid, L.lane = tid & 31;
@@ -448,10 +448,14 @@ __device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem
 #pragma unroll 1
   for (int seg = 0;; ++seg) {
     if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
-    const int steps = sm.segs[seg & (kSegRing - 1)].steps;
-    if (!steps) return;
+    const Segment g = sm.segs[seg & (kSegRing - 1)];
+    if (!g.steps) return;
+    if (t && !warp_wait(&sm.k_free[(t - 1) % kKStages], (t - 1) / kKStages & 1, dead)) return;
+    L.put_queries(g, rt, T.rows, seg, kGroupThreads + tid);
+    fence_async();
+    warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
 #pragma unroll 1
-    for (const int end = t + steps; t < end; ++t) {
+    for (const int end = t + g.steps; t < end; ++t) {
       const int slot = t % kRawV, st = t % kVStages, turn = t / kVStages;
       if (!warp_wait(&sm.rv_full[slot], t / kRawV & 1, dead)) return;
       if (turn && !warp_wait(&sm.v_free[st], (turn - 1) & 1, dead)) return;
@@ -904,7 +908,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
       barrier_init(&sm.seg_full[k], 1);
       barrier_init(&sm.set_full[k], 1);
       barrier_init(&sm.seg_done[k], kSoftWarps);
-      barrier_init(&sm.q_full[k], kGroupWarps);
+      barrier_init(&sm.q_full[k], kLoadWarps);
     }
     for (int k = 0; k < kKStages; ++k) {
       barrier_init(&sm.k_full[k], kGroupWarps);
@@ -937,7 +941,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   } else if (warp < kScoreWarp) {
     registers_down<kLoadRegs>();
     if (warp < kSoftWarps + kGroupWarps) keys_role<kD>(T, smem, sm, rt, tid - 32 * kSoftWarps);
-    else values_role<kD>(T, smem, sm, tid - 32 * (kSoftWarps + kGroupWarps));
+    else values_role<kD>(T, smem, sm, rt, tid - 32 * (kSoftWarps + kGroupWarps));
   } else {
     registers_down<kOtherRegs>();
     if (warp == kPlanWarp) plan_role(T, sm, team, tid & 31);
@@ -953,8 +957,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   if (sm.dead && tid == 0 && T.a.status) atomicOr(T.a.status, SDV_STATUS_STUCK);
 }
 
-// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A CTA has 32 rows, a lane each;
-// its warps take eight columns at a time.
+// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A CTA has 32 rows, a lane each.
+// Its warps share out the partials for the rows' references and weights (kept in shared memory, a batch at a time), and the
+// columns, eight at a time, for the sums.
+constexpr int kJoinBatch = 64;
 template <int kD>
 __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T) {
   using S = TreeShape<kD>;
@@ -985,43 +991,80 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
     while (run_start(units, g1, runs) > u1 - 1) --g1;
     if (g0 == g1) return;                                   // written by that run's CTA
   }
-  if (row >= T.rows || r >= A.R) return;
+  const bool live = row < T.rows && r < A.R;
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
   const auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
-  float m = kNone, base = 0.f, l = 0.f;
-#pragma unroll 8
-  for (int gi = g0; gi <= g1; ++gi) {
-    const float om = slot_of(gi)[kTileRows * kD + row], ob = slot_of(gi)[kTileRows * kD + kTileRows + row];
+  __shared__ float ref[2][kJoinWarps][32], weights[kJoinBatch][32], sums[kJoinWarps][32];
+  const auto scalar = [&](int gi, int which) { return slot_of(gi)[kTileRows * kD + which * kTileRows + row]; };
+  float m = kNone, base = 0.f;
+  if (live) {
+#pragma unroll 4
+    for (int gi = g0 + warp; gi <= g1; gi += kJoinWarps) {
+      const float om = scalar(gi, 0), ob = scalar(gi, 1);
+      if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
+    }
+  }
+  ref[0][warp][lane] = m;
+  ref[1][warp][lane] = base;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float om = ref[0][w][lane], ob = ref[1][w][lane];
     if (reference_less(m, base, om, ob) > 0.f) m = om, base = ob;
   }
-  const auto weight = [&](const float* slot) {
-    return ex2(.5f * reference_less(m, base, slot[kTileRows * kD + row], slot[kTileRows * kD + kTileRows + row]));
-  };
-#pragma unroll 8
-  for (int gi = g0; gi <= g1; ++gi) l += scaled(slot_of(gi)[kTileRows * kD + 2 * kTileRows + row], weight(slot_of(gi)));
+  constexpr int kPer = kD / 8 / kJoinWarps;                  // eights of columns of a warp
+  float l = 0.f, o[kPer][8];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[k][e] = 0.f;
+  for (int first_of = g0; first_of <= g1; first_of += kJoinBatch) {
+    const int n = min(kJoinBatch, g1 + 1 - first_of);
+    __syncthreads();                                         // the weights before are used
+    if (live) {
+#pragma unroll 4
+      for (int k = warp; k < n; k += kJoinWarps) {
+        const float half = ex2(.5f * reference_less(m, base, scalar(first_of + k, 0), scalar(first_of + k, 1)));
+        weights[k][lane] = half;
+        l += scaled(scalar(first_of + k, 2), half);
+      }
+    }
+    __syncthreads();
+    if (live) {
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float4* x = reinterpret_cast<const float4*>(slot_of(first_of + k)) + row;
+        const float half = weights[k][lane];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const float4 a = x[2 * (warp * kPer + j) * kTileRows], c = x[(2 * (warp * kPer + j) + 1) * kTileRows];
+          const float f[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[j][e] += scaled(f[e], half);
+        }
+      }
+    }
+  }
+  sums[warp][lane] = l;
+  __syncthreads();
+  if (!live) return;
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) l += sums[w][lane];
   const int i = r / A.G;
   if (i >= sq.count) l = 0.f;
   const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
   const float by = l == 0.f ? 0.f : 1.f / l;
-  for (int c8 = warp; c8 < kD / 8; c8 += kJoinWarps) {
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int gi = g0; gi <= g1; ++gi) {
-      const float* slot = slot_of(gi);
-      const float half = weight(slot);
-      const float4* x = reinterpret_cast<const float4*>(slot) + 2 * c8 * kTileRows + row;
-      const float4 a = x[0], c = x[kTileRows];
-      const float f[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += scaled(f[e], half);
-    }
+  for (int j = 0; j < kPer; ++j) {
+    const int c8 = warp * kPer + j;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = l == 0.f ? 0.f : o[e] * by;
+    for (int e = 0; e < 8; ++e) o[j][e] = l == 0.f ? 0.f : o[j][e] * by;
     if (A.out_vec) {
-      reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(A.out) + to * kD)[c8] = A.bf16 ? Num<SDV_BF16>::pack(o) : Num<SDV_F16>::pack(o);
+      reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(A.out) + to * kD)[c8] = A.bf16 ? Num<SDV_BF16>::pack(o[j]) : Num<SDV_F16>::pack(o[j]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) put_out(A, to * kD + 8 * c8 + e, o[e]);
+      for (int e = 0; e < 8; ++e) put_out(A, to * kD + 8 * c8 + e, o[j][e]);
     }
   }
   if (A.lse && warp == 0) A.lse[to] = lse_of(m, l, base);
