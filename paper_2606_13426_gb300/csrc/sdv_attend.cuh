@@ -905,7 +905,7 @@ inline RowTiles row_tiles(int64_t R, int most) {
 // in one of 5, over 32 x 8000 keys 275 and 259; 45 rows over 31 keys 12.5 us in six tiles of 1 and 20 in two of 3; 128 rows
 // over 62 x 48 keys and 4 heads 43 in four of 4 and 55 in sixteen of 1.  `longest`: steps of the longest sequence that the page
 // table allows, since the lengths are on the device.
-inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, int warps) {
+inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, int warps, int64_t* cost_of = nullptr) {
   static const int fixed[kMaxNt] = {110, 130, 160, 185, 360};
   static const int round[2][kMaxNt] = {{8, 11, 13, 16, 17}, {10, 16, 23, 30, 39}};
   RowTiles best{0, 0};
@@ -920,6 +920,7 @@ inline RowTiles choose_tiles(int64_t R, int64_t heads, int64_t longest, int D, i
       best = t;
     }
   }
+  if (cost_of) *cost_of = least;
   return best;
 }
 

@@ -3,19 +3,28 @@
 
 namespace sdv {
 
-// Rows of a key head from which on the matrix unit's kernels take them.
-static bool many_rows(int64_t R, int D) { return R > (D == 128 ? 16 : 32) && (R + 127) / 128 <= sm_count(); }
+constexpr int kTileRowsMost = 128;          // rows of a tile of the matrix unit's kernels
+
+// The time of a call of those kernels, in tenths of a microsecond, as choose_tiles has it for the others: a fixed part, the
+// steps of a team and the items that it begins or ends.  Fitted to 60 shapes of 20 to 256 rows; both kernels (us), heads of 128,
+// 8 key heads: 64 rows over 1 x 3000 keys 22 and 29 here, 8 x 1000 37 and 28, 32 x 600 77 and 53, 32 x 3000 164 and 101,
+// 128 x 200 155 and 116; 20 rows over 32 x 3000 79 and 100, 48 rows 130 and 101; heads of 64: 64 rows over 32 x 3000 105 and 88,
+// 32 rows 67 and 70.
+static int64_t rows_cost(int64_t rt, int64_t heads, int64_t longest, int step, int D) {
+  const int64_t teams = sm_count() / rt;
+  return (D == 128 ? 190 : 150) + heads * ((longest + step - 1) / step) * (D == 128 ? 15 : 11) / teams + (heads / teams + 1) * 90;
+}
 
 static AttendSpace tree_space(int B, int W, int Hq, int H, int D) {
   AttendSpace space = attend_space(B, W, Hq, H, D);
-  const size_t part = many_rows((int64_t)W * (Hq / H), D) ? tree_rows_part(D) : 0;
+  const size_t part = tree_rows_part(D);
   if (part > space.part) {
     space.total += part - space.part;
     space.part = part;
   }
   return space;
 }
-size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * 128 * (size_t)(D + 3) * 4 / 256 * 256 + 256; }
+size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * kTileRowsMost * (size_t)(D + 3) * 4 / 256 * 256 + 256; }
 
 }  // namespace sdv
 
@@ -48,9 +57,12 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   AttendArgs A{};
-  const bool many = many_rows(R, D);
-  const RowTiles tiles = many ? RowTiles{(int)((R + 127) / 128), 0}
-                              : choose_tiles(R, (int64_t)B * H, ((int64_t)max_pages * block + kSub - 1) / kSub, D, sm_count() * kAttendWarps);
+  const int64_t longest = (int64_t)max_pages * block, rt = (R + kTileRowsMost - 1) / kTileRowsMost;
+  const int step = kTileKeys / block * block;
+  int64_t cost = 0;
+  RowTiles tiles = choose_tiles(R, (int64_t)B * H, (longest + kSub - 1) / kSub, D, sm_count() * kAttendWarps, &cost);
+  const bool many = rt <= sm_count() && rows_cost(rt, (int64_t)B * H, longest, step, D) < cost;
+  if (many) tiles.rt = (int)rt;
   A.q = q;
   A.bf16 = dtype == SDV_BF16;
   A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
@@ -64,7 +76,7 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   A.out = out, A.lse = lse, A.status = status;
   A.part = (float*)workspace;
   A.ctas = sm_count();
-  A.step = many ? kTileKeys / block * block : 0;
+  A.step = many ? step : 0;
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);

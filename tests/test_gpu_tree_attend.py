@@ -75,7 +75,20 @@ def plain_tree(q, cache, pages, lengths, counts, parents, scale):
     return out, lse, mag, most
 
 
+def widened(pages, tokens=200_000):
+    """The page table in a much wider one: calls are laid out for the tokens that it could hold, so that the kernels for many
+    rows and long sequences run on these."""
+    more = torch.full((pages.shape[0], tokens // 16), -1, dtype=torch.int32, device="cuda")
+    return torch.cat([pages, more], 1)
+
+
 def check_tree(api, q, cache, pages, lengths, parents, counts=None, scale=None, **kw):
+    """Both ways: as the table is, and in a wide one."""
+    check_tree_as(api, q, cache, widened(pages), lengths, parents, counts, scale, **kw)
+    return check_tree_as(api, q, cache, pages, lengths, parents, counts, scale, **kw)
+
+
+def check_tree_as(api, q, cache, pages, lengths, parents, counts=None, scale=None, **kw):
     B, W, Hq, D = q.shape
     par = torch.as_tensor(parents, dtype=torch.int32, device="cuda").view(-1, W).expand(B, W).contiguous()
     r = api.tree_attend(q, cache, pages, lengths, par, counts=counts, scale=scale, **kw)
@@ -140,10 +153,12 @@ def test_a_chain_is_a_window(api):
         n = torch.tensor([600, 64, 333], device="cuda", dtype=torch.int32)
         q = torch.randn(3, W, 8, D, generator=g, device="cuda").to(BF16)
         par = torch.arange(-1, W - 1, device="cuda", dtype=torch.int32).expand(3, W).contiguous()
-        a, b = api.tree_attend(q, cache, pages, n, par), api.cache_attend(q, cache, pages, n)
-        x, y = a["out"].double(), b["out"].double()
-        assert ((x - y).abs() <= 2 * HALF[BF16] * y.abs() + 2.0 ** -12 * y.abs().amax()).all()
-        assert ((a["lse"] - b["lse"]).abs() <= 3e-5 * (1 + b["lse"].abs())).all()
+        b = api.cache_attend(q, cache, pages, n)
+        for table in (pages, widened(pages)):
+            a = api.tree_attend(q, cache, table, n, par)
+            x, y = a["out"].double(), b["out"].double()
+            assert ((x - y).abs() <= 2 * HALF[BF16] * y.abs() + 2.0 ** -12 * y.abs().amax()).all()
+            assert ((a["lse"] - b["lse"]).abs() <= 3e-5 * (1 + b["lse"].abs())).all()
 
 
 @pytest.mark.parametrize("W,G", [(6, 2), (48, 4)])
@@ -168,25 +183,27 @@ def test_what_is_no_tree_is_told(api, W, G):
     assert status.tolist() == [0, 0, 0, 0]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("W,G", [(5, 1), (40, 4)])
-def test_nodes_that_are_not_seen_do_not_matter(api, W, G):
+def test_nodes_that_are_not_seen_do_not_matter(api, W, G, wide):
     """NaN codes of a sibling's branch and behind the sequence, pages that do not exist."""
     from paper_2606_13426_gb300 import binding as B
     g = gen(12)
     block, D = 16, 128
     cache = make_cache(api, g, 20, 1, block, D)
     pages = torch.arange(20, device="cuda", dtype=torch.int32).view(2, 10)
+    pages = widened(pages) if wide else pages
     n = torch.tensor([100, 64], device="cuda", dtype=torch.int32)
     q = torch.randn(2, W, G, D, generator=g, device="cuda").to(BF16)
     par = tree_of("star", W)
-    before = check_tree(api, q, cache, pages, n, par)
+    before = check_tree_as(api, q, cache, pages, n, par)
     k8, v8 = cache["k"].view(torch.uint8), cache["v"].view(torch.uint8)
     for b in range(2):                                  # everything behind the sequence's end
         last = int(n[b])
         for t in range(last, 10 * block):
             k8[pages[b, t // block].long(), 0, t % block] = 0x7f
             v8[pages[b, t // block].long(), 0, :, t % block] = 0xff
-    after = check_tree(api, q, cache, pages, n, par)
+    after = check_tree_as(api, q, cache, pages, n, par)
     assert torch.equal(before["out"], after["out"]) and torch.equal(before["lse"], after["lse"])
     # a NaN code in one leaf's key and another one's value: those two rows alone
     at = [100 - W + 2, 100 - W + 3]
@@ -208,7 +225,7 @@ def test_nodes_that_are_not_seen_do_not_matter(api, W, G):
     assert (status & B.SDV_STATUS_BAD_PAGE).bool().all()
     v8[pages[0, at[1] // block].long(), 0, 7, at[1] % block] = 0
     k8[pages[0, at[0] // block].long(), 0, at[0] % block, 5] = 0
-    check_tree(api, q, cache, pages, n, par)
+    check_tree_as(api, q, cache, pages, n, par)
 
 
 def check_nan(api, q, cache, pages, n, par, rows):
@@ -224,15 +241,17 @@ def check_nan(api, q, cache, pages, n, par, rows):
     return r
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("W,G", [(4, 2), (40, 4)])
-def test_extreme_scales_queries_and_scores(api, W, G, dtype):
+def test_extreme_scales_queries_and_scores(api, W, G, dtype, wide):
     """Value scales far apart, of either sign and zero; key scales that make sharp rows and scores past 2^24; queries of very
     different size; NaN and infinite queries, which are their own rows' affair."""
     g = gen(21)
     B, H, block, D, M = 2, 2, 32, 64, 40
     cache = make_cache(api, g, B * M, H, block, D)
     pages = torch.randperm(B * M, generator=g, device="cuda").to(torch.int32).view(B, M)
+    pages = widened(pages) if wide else pages
     n = torch.tensor([M * block - 7, 300], device="cuda", dtype=torch.int32)
     par = tree_of("tree", W)
     q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(dtype)
@@ -244,14 +263,14 @@ def test_extreme_scales_queries_and_scores(api, W, G, dtype):
         c["k_scale"][1::4] *= -1
         c["k_scale"][2::9] = 0
         for sharp in (1.0, 8.0):
-            check_tree(api, (sharp * q).to(dtype), c, pages, n, par)
+            check_tree_as(api, (sharp * q).to(dtype), c, pages, n, par)
     big = {a: t.clone() for a, t in cache.items()}
     big["k_scale"] *= 2.0 ** 30
     r = api.tree_attend(q, big, pages, n, torch.tensor([par] * B, device="cuda", dtype=torch.int32))
     out, lse, _, _ = plain_tree(q, big, pages, n, [W] * B, [par] * B, D ** -0.5)
     assert r["out"].isfinite().all() and ((r["lse"].double() - lse).abs() <= 2.0 ** -16 * lse.abs()).all()
     sizes = torch.exp2(torch.randint(-20, 5, (B, W, H * G, 1), generator=g, device="cuda").float()) if dtype == BF16 else 1.0
-    check_tree(api, (q.float() * sizes).to(dtype), cache, pages, n, par)
+    check_tree_as(api, (q.float() * sizes).to(dtype), cache, pages, n, par)
     bad = q.clone()
     bad[0, 1, 0, 3] = NAN
     bad[1, 2, 1, 0] = INF
@@ -275,7 +294,7 @@ def test_bf16_outputs_are_rounded_once(api, W, H, G, D):
     for sharp in (1.0, 3.0):
         q = (sharp * torch.randn(2, W, H * G, D, generator=g, device="cuda")).to(BF16)
         out, _, mag, most = plain_tree(q, cache, pages, n, [W, W], par.tolist(), D ** -0.5)
-        got = api.tree_attend(q, cache, pages, n, par)["out"].double()
+        got = torch.cat([api.tree_attend(q, cache, t, n, par)["out"].double()[None] for t in (pages, widened(pages))])
         tol = (2.0 ** -13 + 2 * (2 * D + 8) * 2.0 ** -24 * most[..., None]) * mag
         low, high = (out - tol).float().to(BF16).double(), (out + tol).float().to(BF16).double()
         assert (low <= got).all() and (got <= high).all()
@@ -319,28 +338,29 @@ def test_graphs_streams_and_shared_workspaces(api):
     pages = torch.arange(120, device="cuda", dtype=torch.int32).view(3, 40)
     n = torch.tensor([500, 64, 333], device="cuda", dtype=torch.int32)
     calls = []
+    wide = widened(pages)
     for W, G in ((7, 2), (40, 4)):
         q = torch.randn(3, W, 2 * G, 128, generator=g, device="cuda").to(BF16)
         par = torch.tensor([tree_of("tree", W, b) for b in range(3)], device="cuda", dtype=torch.int32)
-        calls.append((q, par))
-    size = max(B.sdv_tree_attend_workspace_bytes(3, q.shape[1], q.shape[2], 2, 128) for q, _ in calls)
+        calls.append((q, par, pages if W == 7 else wide))
+    size = max(B.sdv_tree_attend_workspace_bytes(3, q.shape[1], q.shape[2], 2, 128) for q, _, _ in calls)
     ws = torch.empty(size, device="cuda", dtype=torch.uint8)
-    ref = [api.tree_attend(q, cache, pages, n, p) for q, p in calls]
+    ref = [api.tree_attend(q, cache, t, n, p) for q, p, t in calls]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        got = [api.tree_attend(q, cache, pages, n, p) for q, p in calls]
+        got = [api.tree_attend(q, cache, t, n, p) for q, p, t in calls]
     side.synchronize()
     assert all(torch.equal(a[k], b[k]) for a, b in zip(ref, got) for k in ("out", "lse"))
     graphs, outs = [], []
-    for q, p in calls:
+    for q, p, t in calls:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            outs.append(api.tree_attend(q, cache, pages, n, p, workspace=ws))
+            outs.append(api.tree_attend(q, cache, t, n, p, workspace=ws))
         graphs.append(graph)
     for lengths in ([500, 64, 333], [64, 639, 41], [0, 40, 600]):
         n.copy_(torch.tensor(lengths, dtype=torch.int32))
-        ref = [api.tree_attend(q, cache, pages, n, p) for q, p in calls]
+        ref = [api.tree_attend(q, cache, t, n, p) for q, p, t in calls]
         for _ in range(2):
             for graph in graphs:
                 graph.replay()
