@@ -14,6 +14,10 @@ namespace sdv {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotQueryElems = 16384;    // elements of a CTA that turns queries, about
+constexpr int kQueryTokens = 32;         // of it at most
+constexpr int kGroupCtas = 6;            // CTAs on an SM from which on they take more heads each
+constexpr int kQueriesApart = 6;         // CTAs of queries on an SM from which on they have a launch of their own
+constexpr int kQueryItems = 4;           // pairs of 16-byte vectors that a thread asks for at once
 enum : int { kNeighbours = 0, kHalvesOfUnits = 1, kHalves = 2 };
 
 struct RotaryArgs {
@@ -51,14 +55,24 @@ __device__ __forceinline__ uint64_t turn_of(double f) {
   return (uint64_t)((t - floor(t)) * 0x1p64);
 }
 
-// Cosines and sines of `tokens` tokens' pairs, [token][rot / 2]; pos: the token's position.
+// The pairs' turns per position: 64-bit products and a floor, which this machine has few units for, so once a CTA.
+__device__ __forceinline__ void fill_turns(uint64_t* turns, const RotaryArgs& A, int tid) {
+  if (tid < A.rot / 2) turns[tid] = turn_of(__ldg(A.freqs + tid));
+}
+// A table of cosines and sines: token t's pair i at t * table_row(pairs) + table_at(i).  Without the gaps the lanes of a warp,
+// which read pairs 8 or 16 apart and of several tokens, would meet in the same banks, up to 32 at once.
+__host__ __device__ __forceinline__ int table_at(int i) { return i + (i >> 3); }
+__host__ __device__ __forceinline__ int table_row(int pairs) { return (pairs + (pairs >> 3) + 15) / 16 * 16 + 5; }
+// `tokens` tokens' table; pos: a token's position.
 template <typename F>
-__device__ __forceinline__ void fill_table(float2* table, const RotaryArgs& A, int tokens, int tid, F pos) {
-  const int pairs = A.rot / 2;
-  // a thread keeps its pair where the pairs divide the threads; else it looks its frequency up again
+__device__ __forceinline__ void fill_table(float2* table, const uint64_t* turns, int pairs, int tokens, int tid, F pos) {
+  const bool keeps = kRotThreads % pairs == 0;
+  int t = tid / pairs, p = tid - t * pairs;
+  const int step = kRotThreads / pairs, row = table_row(pairs);
   for (int i = tid; i < tokens * pairs; i += kRotThreads) {
-    const int t = i / pairs, p = i - t * pairs;
-    table[i] = turned(turn_of(__ldg(A.freqs + p)), pos(t));
+    if (!keeps) t = i / pairs, p = i - t * pairs;
+    table[t * row + table_at(p)] = turned(turns[p], pos(t));
+    t += step;
   }
 }
 
@@ -82,7 +96,7 @@ __device__ __forceinline__ void turn_key(const typename Num<kDtype>::T* x, bool 
     if (u1 * 16 < rot) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float2 c = cs[u0 * 16 + e];
+        const float2 c = cs[table_at(u0 * 16 + e)];
         const float a = f[e], b = f[16 + e];
         f[e] = a * c.x - b * c.y;
         f[16 + e] = b * c.x + a * c.y;
@@ -93,7 +107,7 @@ __device__ __forceinline__ void turn_key(const typename Num<kDtype>::T* x, bool 
     for (int e = 0; e < 32; e += 2) {
       const int at = (e < 16 ? u0 * 16 : u1 * 16 - 16) + e;
       if (at < rot) {
-        const float2 c = cs[at / 2];
+        const float2 c = cs[table_at(at / 2)];
         const float a = f[e], b = f[e + 1];
         f[e] = a * c.x - b * c.y;
         f[e + 1] = b * c.x + a * c.y;
@@ -106,7 +120,7 @@ __device__ __forceinline__ void turn_key(const typename Num<kDtype>::T* x, bool 
       const int at = (e < 16 ? u0 * 16 : u1 * 16 - 16) + e;
       if (at < rot) {
         const bool low = at < half;
-        const float2 c = cs[low ? at : at - half];
+        const float2 c = cs[table_at(low ? at : at - half)];
         const float o = E::to(x[low ? at + half : at - half]);
         f[e] = low ? f[e] * c.x - o * c.y : f[e] * c.x + o * c.y;
       }
@@ -132,94 +146,127 @@ __device__ __forceinline__ uint4 codes16(const float* f, bool pow2, float inv, f
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A CTA's queries: tokens [t0, t0 + q_tokens) of all sequences' in their order.
+// A CTA's queries: tokens [t0, t0 + q_tokens) of all sequences' in their order.  A thread's item is two 16-byte vectors that
+// are each other's other half, or neighbours; it asks for kQueryItems of them before the first is used.
 template <int kDtype>
-__device__ __forceinline__ void turn_queries(const RotaryArgs& A, float2* table, int cta) {
+__device__ __forceinline__ void turn_queries(const RotaryArgs& A, float2* table, uint64_t* turns, int cta) {
   using E = Num<kDtype>;
   using T = typename E::T;
   constexpr int kPer = E::kPer16;
+  __shared__ int64_t from[kQueryTokens], to[kQueryTokens];
+  __shared__ int where[kQueryTokens], live[kQueryTokens];
   const int tid = threadIdx.x, D = A.c.D, rot = A.rot, pairs = rot / 2;
   const int64_t total = (int64_t)A.B * A.W, t0 = (int64_t)cta * A.q_tokens;
   const int n = (int)min((int64_t)A.q_tokens, total - t0);
-  fill_table(table, A, n, tid, [&](int t) {
-    const int64_t at = t0 + t;
-    if (A.positions) return A.positions[at];
-    const int b = (int)(at / A.W);
-    return max(A.lengths[b], 0) + (int)(at - (int64_t)b * A.W);
-  });
+  int b = 0, w = 0;
+  if (tid < n) {
+    const int64_t at = t0 + tid;
+    b = (int)(at / A.W), w = (int)(at - (int64_t)b * A.W);
+    from[tid] = b * A.q_sb + w * A.q_st;
+    to[tid] = b * A.o_sb + w * A.o_st;
+  }
   __syncthreads();
-  const int vecs = D / kPer, per = A.Hq * vecs;
-  const bool vec = aligned16(A.q) && aligned16(A.q_out) && ((A.q_sb | A.q_st | A.q_sh | A.o_sb | A.o_st | A.o_sh) * (int64_t)sizeof(T)) % 16 == 0;
+  const auto fill = [&] {
+    fill_turns(turns, A, tid);
+    if (tid < n) {
+      live[tid] = !A.counts || w < A.counts[b];
+      where[tid] = A.positions ? A.positions[t0 + tid] : (int)((int64_t)max(A.lengths[b], 0) + w);
+    }
+    __syncthreads();
+    fill_table(table, turns, pairs, n, tid, [&](int t) { return where[t]; });
+    __syncthreads();
+  };
+  const T* q = reinterpret_cast<const T*>(A.q);
+  T* out = reinterpret_cast<T*>(A.q_out);
+  const bool vec = aligned16(q) && aligned16(out) && ((A.q_sb | A.q_st | A.q_sh | A.o_sb | A.o_st | A.o_sh) * (int64_t)sizeof(T)) % 16 == 0;
+  if (vec && (!A.halves || pairs % kPer == 0)) {
+    const int lper = __ffs(D / kPer / 2) - 1, per = A.Hq << lper, items = n * per;
+    const int hv = A.halves ? pairs / kPer : 0;                   // vectors of a half
+    bool filled = false;
+    for (int i0 = tid; i0 - tid < items; i0 += kRotThreads * kQueryItems) {
+      uint4 raw[kQueryItems][2];
+      int tok[kQueryItems], head[kQueryItems], e0[kQueryItems], e1[kQueryItems];
+#pragma unroll
+      for (int k = 0; k < kQueryItems; ++k) {
+        const int i = i0 + k * kRotThreads;
+        tok[k] = -1;
+        if (i < items) {
+          const int t = i / per, r = i - t * per, p = r & ((1 << lper) - 1);
+          tok[k] = t;
+          head[k] = r >> lper;
+          e0[k] = (p < hv ? p : 2 * p) * kPer;
+          e1[k] = (p < hv ? p + hv : 2 * p + 1) * kPer;
+          const T* x = q + from[t] + head[k] * A.q_sh;
+          raw[k][0] = *reinterpret_cast<const uint4*>(x + e0[k]);
+          raw[k][1] = *reinterpret_cast<const uint4*>(x + e1[k]);
+        }
+      }
+      if (!filled) {                                              // while they are on their way
+        fill();
+        filled = true;
+      }
+#pragma unroll
+      for (int k = 0; k < kQueryItems; ++k) {
+        if (tok[k] < 0) continue;
+        const float2* cs = table + tok[k] * table_row(pairs);
+        if (!live[tok[k]]) {
+          raw[k][0] = raw[k][1] = make_uint4(0, 0, 0, 0);
+        } else if (e0[k] < rot) {                                 // (neighbours: the second may lie behind the turned ones)
+          float a[kPer], b[kPer];
+          E::unpack(raw[k][0], a);
+          E::unpack(raw[k][1], b);
+          if (A.halves) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+              const float2 c = cs[table_at(e0[k] + e)];
+              const float x = a[e], y = b[e];
+              a[e] = x * c.x - y * c.y;
+              b[e] = y * c.x + x * c.y;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < kPer; e += 2) {
+              if (e0[k] + e < rot) {
+                const float2 c = cs[table_at((e0[k] + e) / 2)];
+                const float x = a[e], y = a[e + 1];
+                a[e] = x * c.x - y * c.y;
+                a[e + 1] = y * c.x + x * c.y;
+              }
+              if (e1[k] + e < rot) {
+                const float2 c = cs[table_at((e1[k] + e) / 2)];
+                const float x = b[e], y = b[e + 1];
+                b[e] = x * c.x - y * c.y;
+                b[e + 1] = y * c.x + x * c.y;
+              }
+            }
+          }
+          raw[k][0] = E::pack(a);
+          raw[k][1] = E::pack(b);
+        }
+        T* y = out + to[tok[k]] + head[k] * A.o_sh;
+        *reinterpret_cast<uint4*>(y + e0[k]) = raw[k][0];
+        *reinterpret_cast<uint4*>(y + e1[k]) = raw[k][1];
+      }
+    }
+    return;
+  }
+  // by elements: a pair by the thread that has its first
+  fill();
+  const int per = A.Hq * D;
   for (int i = tid; i < n * per; i += kRotThreads) {
-    const int t = i / per, r = i - t * per, h = r / vecs, e0 = (r - h * vecs) * kPer;
-    const int64_t at = t0 + t;
-    const int b = (int)(at / A.W), w = (int)(at - (int64_t)b * A.W);
-    const T* x = reinterpret_cast<const T*>(A.q) + b * A.q_sb + w * A.q_st + h * A.q_sh;
-    T* y = reinterpret_cast<T*>(A.q_out) + b * A.o_sb + w * A.o_st + h * A.o_sh;
-    const float2* cs = table + t * pairs;
-    const bool live = !A.counts || w < A.counts[b];
-    float f[kPer], o[kPer];
-    const auto get = [&](int e, float* to) {
-      if (vec) {
-        E::unpack(*reinterpret_cast<const uint4*>(x + e), to);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) to[k] = E::to(x[e + k]);
-      }
-    };
-    const auto put = [&](int e, const float* from) {
-      if (vec) {
-        *reinterpret_cast<uint4*>(y + e) = E::pack(from);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) y[e + k] = E::from(from[k]);
-      }
-    };
-    if (!live) {
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) f[k] = 0.f;
-      put(e0, f);
-    } else if (!A.halves) {
-      get(e0, f);
-#pragma unroll
-      for (int k = 0; k < kPer; k += 2)
-        if (e0 + k < rot) {
-          const float2 c = cs[(e0 + k) / 2];
-          const float a = f[k], bb = f[k + 1];
-          f[k] = a * c.x - bb * c.y;
-          f[k + 1] = bb * c.x + a * c.y;
-        }
-      put(e0, f);
-    } else if (pairs % kPer == 0) {       // both halves' vectors by one thread
-      if (e0 < pairs) {
-        get(e0, f);
-        get(e0 + pairs, o);
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-          const float2 c = cs[e0 + k];
-          const float a = f[k], bb = o[k];
-          f[k] = a * c.x - bb * c.y;
-          o[k] = bb * c.x + a * c.y;
-        }
-        put(e0, f);
-        put(e0 + pairs, o);
-      } else if (e0 >= rot) {
-        get(e0, f);
-        put(e0, f);
-      }
-    } else {                              // pairs by the thread that has their first element; the rest by their own
-#pragma unroll 1
-      for (int k = 0; k < kPer; ++k) {
-        const int e = e0 + k;
-        if (e < pairs) {
-          const float2 c = cs[e];
-          const float a = E::to(x[e]), bb = E::to(x[e + pairs]);
-          y[e] = E::from(a * c.x - bb * c.y);
-          y[e + pairs] = E::from(bb * c.x + a * c.y);
-        } else if (e >= rot) {
-          y[e] = x[e];
-        }
-      }
+    const int t = i / per, r = i - t * per, h = r / D, e = r - h * D;
+    const T* x = q + from[t] + h * A.q_sh;
+    T* y = out + to[t] + h * A.o_sh;
+    const int p = A.halves ? e : e / 2, other = A.halves ? e + pairs : e + 1;
+    if (!live[t]) {
+      y[e] = E::from(0.f);
+    } else if (e >= rot) {
+      y[e] = x[e];
+    } else if (A.halves ? e < pairs : e % 2 == 0) {
+      const float2 c = table[t * table_row(pairs) + table_at(p)];
+      const float a = E::to(x[e]), b = E::to(x[other]);
+      y[e] = E::from(a * c.x - b * c.y);
+      y[other] = E::from(b * c.x + a * c.y);
     }
   }
 }
@@ -228,13 +275,14 @@ __device__ __forceinline__ void turn_queries(const RotaryArgs& A, float2* table,
 // tokens are computed once for the group's heads, in shared memory; a thread has two sixteens of a key that are each other's
 // other half.  The rest is k_cache_append's.
 template <int kDtype, int kItems, int kPairs>
-__global__ void __launch_bounds__(kRotThreads, kItems == 1 && kDtype != SDV_F32 ? 3 : kItems == 1 ? 2 : 1) k_append_rotary(const RotaryArgs A) {
+__global__ void __launch_bounds__(kRotThreads, kItems == 1 ? 2 : 1) k_append_rotary(const RotaryArgs A) {
   using T = typename Num<kDtype>::T;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float red[2][kRotThreads / 32];
+  __shared__ uint64_t turns[64];
   const int tid = threadIdx.x;
   if ((int)blockIdx.x >= A.append_ctas) {
-    turn_queries<kDtype>(A, reinterpret_cast<float2*>(smem), (int)blockIdx.x - A.append_ctas);
+    turn_queries<kDtype>(A, reinterpret_cast<float2*>(smem), turns, (int)blockIdx.x - A.append_ctas);
     return;
   }
   const int T_ = A.c.block, D = A.c.D;
@@ -254,7 +302,9 @@ __global__ void __launch_bounds__(kRotThreads, kItems == 1 && kDtype != SDV_F32 
     if (A.status && tid == 0) atomicOr(A.status + b, SDV_STATUS_BAD_PAGE);
     return;
   }
-  fill_table(table, A, m, tid, [&](int t) { return A.positions ? A.positions[(int64_t)b * A.W + first + t] : (int)((int64_t)n + first + t); });
+  fill_turns(turns, A, tid);
+  __syncthreads();
+  fill_table(table, turns, A.rot / 2, m, tid, [&](int t) { return A.positions ? A.positions[(int64_t)b * A.W + first + t] : (int)((int64_t)n + first + t); });
   __syncthreads();
   const int per = D / 32, lper = per == 4 ? 2 : 1, lrow = lper + 1, items = m * per;
   const int hu = kPairs == kHalvesOfUnits ? A.rot / 32 : 0;       // sixteens of a half
@@ -275,7 +325,7 @@ __global__ void __launch_bounds__(kRotThreads, kItems == 1 && kDtype != SDV_F32 
       if (i < items) {
         vr[k][0].load(vx + row * A.st + u0[k] * 16, vvec);
         vr[k][1].load(vx + row * A.st + u1[k] * 16, vvec);
-        turn_key<kDtype, kPairs>(kx + row * A.st, kvec, table + row * (A.rot / 2), A.rot, u0[k], u1[k], kf[k]);
+        turn_key<kDtype, kPairs>(kx + row * A.st, kvec, table + row * table_row(A.rot / 2), A.rot, u0[k], u1[k], kf[k]);
       }
     }
     float was[2];                                                 // (r0 > 0: the page holds tokens)
@@ -348,6 +398,14 @@ __global__ void __launch_bounds__(kRotThreads, kItems == 1 && kDtype != SDV_F32 
   }
 }
 
+// The queries alone, where there are many: with the keys' registers half as many of these CTAs would be in flight.
+template <int kDtype>
+__global__ void __launch_bounds__(kRotThreads, 4) k_turn_queries(const RotaryArgs A) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint64_t turns[64];
+  turn_queries<kDtype>(A, reinterpret_cast<float2*>(smem), turns, (int)blockIdx.x);
+}
+
 template <int kDtype, int kItems, int kPairs>
 static cudaError_t launch_rotary_as(const RotaryArgs& A, int64_t grid, size_t smem, cudaStream_t s) {
   const auto kern = k_append_rotary<kDtype, kItems, kPairs>;
@@ -361,7 +419,15 @@ static cudaError_t launch_rotary_as(const RotaryArgs& A, int64_t grid, size_t sm
 template <int kDtype>
 static cudaError_t launch_rotary(const RotaryArgs& A, int64_t grid, cudaStream_t s) {
   const int rows = min_int(A.W, A.c.block);
-  const size_t table = (size_t)A.rot / 2 * sizeof(float2), append = (size_t)A.c.block * A.c.D + rows * table, query = A.q ? A.q_tokens * table : 0;
+  const size_t table = (size_t)table_row(A.rot / 2) * sizeof(float2), append = (size_t)A.c.block * A.c.D + rows * table;
+  size_t query = A.q ? A.q_tokens * table : 0;
+  if (A.q && grid - A.append_ctas > kQueriesApart * (int64_t)sm_count()) {
+    k_turn_queries<kDtype><<<(unsigned)(grid - A.append_ctas), kRotThreads, query, s>>>(A);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    grid = A.append_ctas;
+    query = 0;
+  }
   const size_t smem = append > query ? append : query;
   const int pairs = !A.halves ? kNeighbours : A.rot % 32 == 0 ? kHalvesOfUnits : kHalves;
   const bool one = rows * A.c.D / 32 <= kRotThreads;
@@ -400,7 +466,7 @@ extern "C" int sdv_cache_append_rotary(const void* k_new, const void* v_new, int
   // the heads of a CTA: as few as fill the GPU's places twice
   const int64_t pages_most = (int64_t)B * A.nb;
   A.group = 1;
-  while (A.group < H && pages_most * ((H + A.group - 1) / A.group) > 6 * (int64_t)sm_count()) A.group *= 2;
+  while (A.group < H && pages_most * ((H + A.group - 1) / A.group) > kGroupCtas * (int64_t)sm_count()) A.group *= 2;
   if (A.group > H) A.group = H;
   A.groups = (H + A.group - 1) / A.group;
   int64_t grid = pages_most * A.groups;
@@ -409,7 +475,7 @@ extern "C" int sdv_cache_append_rotary(const void* k_new, const void* v_new, int
   if (q) {
     const int64_t tokens = (int64_t)B * W;
     int per = kRotQueryElems / (Hq * D);
-    per = per < 1 ? 1 : per > 32 ? 32 : per;
+    per = per < 1 ? 1 : per > kQueryTokens ? kQueryTokens : per;
     while (per > 1 && (tokens + per - 1) / per < 4 * sm_count()) per /= 2;
     A.q_tokens = per;
     grid += (tokens + per - 1) / per;

@@ -188,7 +188,7 @@ def test_rotary_extreme_values_and_missing_pages(api):
     assert got[2, 0, [8, 40]].isnan().all() and int(got.isnan().sum()) == 2
     y, size = turn(k[0, :6], torch.arange(10, 16, device="cuda"), freqs, "halves")
     top = float(y[y.isfinite()].abs().max())
-    assert float(cache["k_scale"][0, 0]) == 2.0 ** math.ceil(math.log2(top / 448))
+    assert float(cache["k_scale"][0, 0]) == max(1.0, 2.0 ** math.ceil(math.log2(top / 448)))    # (ten tokens were held at 1)
     fine = y.isfinite()
     assert ((got - y).abs()[fine] <= (2.0 ** -4 * 1.01 * y.abs() + 2.0 ** -9 * cache["k_scale"][0, 0].double())[fine]).all()
 
