@@ -102,11 +102,15 @@ __device__ __forceinline__ void each_pair(const typename Num<kDtype>::T* q, cons
   }
 }
 
-// A thread's best of the race for r / E over its share of two rows (each_pair's), r = rest(index, q's logit, p's).
-template <int kDtype, typename F>
+struct AnyToken {
+  __device__ __forceinline__ bool operator()(int) const { return true; }
+};
+// A thread's best of the race for r / E over its share of two rows (each_pair's), r = rest(index, q's logit, p's), among the
+// tokens that are `in`: asked of those that would win alone.
+template <int kDtype, typename F, typename G = AnyToken>
 __device__ __forceinline__ void race_part(const typename Num<kDtype>::T* q, const typename Num<kDtype>::T* p, int V, int part,
                                           int log_parts, int lane, int step, const float* race, uint64_t seed, uint32_t b, Racer& top,
-                                          F rest) {
+                                          F rest, G in = G()) {
   constexpr int kPer = Num<kDtype>::kPer16;
   each_pair<kDtype>(q, p, V, part, log_parts, lane, step, [&](int i, int count, const float* x, const float* y) {
     float r[kPer], e[kPer];
@@ -135,7 +139,7 @@ __device__ __forceinline__ void race_part(const typename Num<kDtype>::T* q, cons
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {                            // r / e against the best so far
       const float mine = r[k] * top.e, theirs = top.r * e[k];
-      if (mine > theirs || (mine == theirs && r[k] > 0.f && i + k < top.i)) top = Racer{r[k], e[k], i + k};
+      if ((mine > theirs || (mine == theirs && r[k] > 0.f && i + k < top.i)) && in(i + k)) top = Racer{r[k], e[k], i + k};
     }
   });
 }

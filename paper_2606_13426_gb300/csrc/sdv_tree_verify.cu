@@ -16,6 +16,8 @@
 
 namespace sdv {
 
+constexpr int64_t kAheadBytes = 8 << 20;
+
 struct TreeVerifyArgs {
   const void* q;
   const void* p;                       // NULL: children chosen without chance
@@ -24,6 +26,7 @@ struct TreeVerifyArgs {
   const int32_t* parents;
   int W, V;
   float cq, cp, iq, ip;                // log2(e) / T and 1 / T of target and draft
+  int ahead;                           // children whose rows are asked for before it is known which is taken
   const int32_t* counts;
   uint64_t seed;
   const float* coins;
@@ -47,8 +50,59 @@ __device__ __forceinline__ bool tried_before(const Tried& t, const int* list, in
   return false;
 }
 
+// Asks for part `rank` of a row of V elements before it is read.
+__device__ __forceinline__ void ask_ahead(const void* row, int V, int bytes, int rank, int log_c, int tid) {
+  const int64_t all = (int64_t)V * bytes;
+  const char* x = static_cast<const char*>(row);
+  const int64_t end = (all * (rank + 1) >> log_c);
+  for (int64_t i = (all * rank >> log_c) + tid * 128; i < end; i += kVerThreads * 128)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(x + i));
+}
+
+// Statistics of this thread's parts of two rows (the second of none, if !pairs), both on their way at once.  Few vectors a
+// turn: a thread's part is often no longer, and the code is run cold.
+template <int kDtype>
+__device__ __forceinline__ void read_two(const Row<kDtype>& Q, const Row<kDtype>& P, bool pairs, int rank, int log_c, float cq, float cp,
+                                         Run& a, Run& c) {
+  using E = Num<kDtype>;
+  constexpr int kVecs = 4;
+  const Part<kDtype, false, kVerThreads> q(Q, rank, log_c), p(P, rank, log_c);
+  const int p1 = pairs ? p.v1 : 0, tid = (int)threadIdx.x;
+  a = run_empty();
+  c = run_empty();
+  const auto add = [&](Run& r, const uint4* raw, float scale, int some) {
+    float top = vec_max<kDtype>(raw[0]);
+#pragma unroll
+    for (int u = 1; u < kVecs; ++u) top = max_nan(top, vec_max<kDtype>(raw[u]));
+    run_see(r, top, scale);
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+      if (u * kVerThreads >= some) break;                    // (for all threads of the CTA)
+      float f[E::kPer16];
+      E::unpack(raw[u], f);
+      run_add<E::kPer16, false>(r, f, scale);
+    }
+  };
+#pragma unroll 1
+  for (int v = q.v0, w = p.v0; v - tid < q.v1 || w - tid < p1; v += kVecs * kVerThreads, w += kVecs * kVerThreads) {
+    uint4 x[kVecs], y[kVecs];
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+      x[u] = y[u] = vec_masked<kDtype>();
+      if (v + u * kVerThreads < q.v1) x[u] = q.vec[v + u * kVerThreads];
+      if (w + u * kVerThreads < p1) y[u] = p.vec[w + u * kVerThreads];
+    }
+    add(a, x, cq, q.v1 - v + tid);
+    if (pairs) add(c, y, cp, p1 - w + tid);
+  }
+  if (q.single >= 0) run_one(a, q.x, cq);
+  if (pairs && p.single >= 0) run_one(c, p.x, cp);
+}
+
 // Bound by latency: a node is a read of its rows' parts, a barrier for their statistics, and with each rejection that leaves
-// children a pass and a barrier more.
+// children a pass and a barrier more.  From cold rows: about 9 us for a root without children and its draw, 4 for each node
+// (5.4 before both rows were read at once and the children's asked for ahead), 1 to 2 for a rejection.  1 x 16 x 32768 bf16: 13 us
+// with one node taken, 25 with four; 16 x 32 x 131072 42; 48 x 24 x 50001 fp32, children chosen, 26.
 template <int kDtype, bool kDrawn>
 __global__ void __launch_bounds__(kVerThreads, 3) k_tree_verify(const TreeVerifyArgs A) {
   using E = Num<kDtype>;
@@ -74,31 +128,40 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_tree_verify(const TreeVerify
     if (C > 1) cl.sync();
     else __syncthreads();
   };
-  if (C > 1) cl.barrier_arrive();
-  const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
-  const T* p0 = kDrawn ? reinterpret_cast<const T*>(A.p) + b * A.p_sb : nullptr;
-  const float* race = A.race ? A.race + (int64_t)b * V : nullptr;
-  if (race)
-    for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
+  // Cleared before the arrival: the first CTA writes into all of them as soon as all have arrived.
   for (int i = tid; i < SDV_MAX_TREE; i += kVerThreads) {
     kids_s[i] = 0;
     ell_s[i] = 0.f;
     path_s[i] = -1;
   }
   if (tid == 0) bad_s = 0;
+  if (C > 1) cl.barrier_arrive();
+  const T* q0 = reinterpret_cast<const T*>(A.q) + b * A.q_sb;
+  const T* p0 = kDrawn ? reinterpret_cast<const T*>(A.p) + b * A.p_sb : nullptr;
+  const float* race = A.race ? A.race + (int64_t)b * V : nullptr;
+  ask_ahead(q0, V, sizeof(T), rank, log_c, tid);             // the root's
+  if (kDrawn) ask_ahead(p0, V, sizeof(T), rank, log_c, tid);
+  if (race)
+    for (int i = share(V, rank, log_c) + tid * 32; i < share(V, rank + 1, log_c); i += kVerThreads * 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(race + i));
   __syncthreads();
-  if (C > 1) cl.barrier_wait();                              // every CTA of the cluster has started
+  if (C > 1) cl.barrier_wait();                              // every CTA of the cluster has started, and has its kids_s cleared
   if (rank == 0) {
+    const int64_t at = (int64_t)b * W + tid;
+    int up = 0, t = 0;
+    float coin = 0.f;
+    if (tid < W) {                                           // (beside the counts, not behind them)
+      up = A.parents[at];
+      t = A.tokens[at];
+      if (A.coins) coin = A.coins[at];
+    }
     const int n = A.counts ? min(A.counts[b], W) : W;
     if (tid < n) {
-      const int64_t at = (int64_t)b * W + tid;
       bool bad = false;
-      const int p = parent_of(A.parents[at], tid, bad);
+      const int p = parent_of(up, tid, bad);
       if (p >= 0) atomicOr(&kids_s[p], 1ull << tid);
       if (bad) atomicOr(&bad_s, SDV_STATUS_BAD_TREE);
-      const int t = A.tokens[at];
-      const float eta = A.coins ? A.coins[at] : ((float)philox_block(A.seed, (uint32_t)b, (uint32_t)tid, kStreamCoin, 0).x + 0.5f) * 0x1p-32f;
+      const float eta = A.coins ? coin : ((float)philox_block(A.seed, (uint32_t)b, (uint32_t)tid, kStreamCoin, 0).x + 0.5f) * 0x1p-32f;
       for (int k = 0; k < C; ++k) {
         at_rank(tok_s, k)[tid] = t;
         at_rank(eta_s, k)[tid] = eta;
@@ -139,22 +202,36 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_tree_verify(const TreeVerify
     const bool pairs = kDrawn && kids;
     const T* q = q0 + u * A.q_sr;
     const T* p = pairs ? p0 + u * A.p_sr : q;
-    if (rank == 0 && tid < SDV_MAX_TREE && (kids >> tid & 1)) {
+    const bool child = rank == 0 && tid < SDV_MAX_TREE && (kids >> tid & 1);
+    float xq = 0.f, xp = 0.f;
+    if (child) {
       const int t = tok_s[tid];
-      const bool in = t >= 0 && t < V;
-      const float xq = in ? E::to(q[t]) : 0.f, xp = in && kDrawn ? E::to(p[t]) : 0.f;
-      for (int k = 0; k < C; ++k) {
-        at_rank(xq_s, k)[tid] = xq;
-        at_rank(xp_s, k)[tid] = xp;
+      if (t >= 0 && t < V) {
+        xq = E::to(q[t]);
+        if (kDrawn) xp = E::to(p[t]);
       }
     }
     // the rows' statistics
     {
-      const Stat a = run_warp(Part<kDtype, false, kVerThreads>(Row<kDtype>(q, V), rank, log_c).read(A.cq), A.cq);
+      Run mine, other;
+      read_two<kDtype>(Row<kDtype>(q, V), Row<kDtype>(p, V), pairs, rank, log_c, A.cq, A.cp, mine, other);
+      const Stat a = run_warp(mine, A.cq);
       if (lane == 0) warp_stat[0][warp] = a;
       if (pairs) {
-        const Stat c = run_warp(Part<kDtype, false, kVerThreads>(Row<kDtype>(p, V), rank, log_c).read(A.cp), A.cp);
+        const Stat c = run_warp(other, A.cp);
         if (lane == 0) warp_stat[1][warp] = c;
+      }
+      if (child)
+        for (int k = 0; k < C; ++k) {
+          at_rank(xq_s, k)[tid] = xq;
+          at_rank(xp_s, k)[tid] = xp;
+        }
+      // the rows of the children likeliest to be taken, while the CTAs meet
+      unsigned long long next = kids;
+      for (int k = 0; next && k < A.ahead; ++k, next &= next - 1) {
+        const int c = __ffsll((long long)next) - 1;
+        ask_ahead(q0 + c * A.q_sr, V, sizeof(T), rank, log_c, tid);
+        if (kDrawn && kids_s[c]) ask_ahead(p0 + c * A.p_sr, V, sizeof(T), rank, log_c, tid);
       }
       __syncthreads();
       if (warp < 2 && (warp == 0 || pairs)) {
@@ -260,12 +337,14 @@ __global__ void __launch_bounds__(kVerThreads, 3) k_tree_verify(const TreeVerify
     Racer top{0.f, 1.f, 0x7fffffff};
     if (row_ok(rq))
       race_part<kDtype>(q, kDrawn && rest ? p0 + u * A.p_sr : q, V, rank, log_c, tid, kVerThreads, race, A.seed, (uint32_t)b, top,
-                        [&](int i, float x, float y) {
+                        [&](int, float x, float y) {
                           const float a = prob(rq, x, A.cq, 0.f);
-                          if (!rest) return a;
-                          if constexpr (kDrawn) return fmaf(-beta, prob(rp, y, A.cp, 0.f), a);
-                          else return tried_before(tried, tried_s, i) ? 0.f : a;
-                        });
+                          if constexpr (kDrawn) {
+                            if (rest) return fmaf(-beta, prob(rp, y, A.cp, 0.f), a);
+                          }
+                          return a;
+                        },
+                        [&](int i) { return kDrawn || !rest || !tried_before(tried, tried_s, i); });
     Best me{top.r > 0.f ? top.r / top.e : 0.f, top.i};
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -333,8 +412,11 @@ extern "C" int sdv_tree_verify(const void* target, int64_t target_stride_b, int6
   const void* four[] = {tokens, parents, counts, coins, race, accepted_len, path, next_token, log_ratio_out, status_out};
   for (const void* p : four)
     if (!aligned_to(p, 4)) return SDV_EALIGN;
+  // as many as make 8 MB of all sequences' rows: with one 48 x 24 x 50001 fp32, chosen, take 27.6 us in place of 25.8
+  const int64_t rows = (int64_t)B * V * (int64_t)elem_bytes(dtype) * (draft ? 2 : 1);
+  const int ahead = (int)(kAheadBytes / rows > SDV_MAX_TREE ? SDV_MAX_TREE : kAheadBytes / rows);
   const TreeVerifyArgs A{target, draft, target_stride_b, target_stride_row, draft_stride_b, draft_stride_row, tokens, parents, W, V,
-                         kLog2E / temperature, kLog2E / draft_temperature, 1.f / temperature, 1.f / draft_temperature,
+                         kLog2E / temperature, kLog2E / draft_temperature, 1.f / temperature, 1.f / draft_temperature, ahead,
                          counts, seed, coins, race, accepted_len, path, next_token, log_ratio_out, status_out};
   cudaStream_t s = (cudaStream_t)stream;
   return launched(dtype == SDV_F32    ? launch_tree_verify<SDV_F32>(A, B, dtype, s)

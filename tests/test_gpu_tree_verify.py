@@ -319,3 +319,20 @@ def test_refusals(api):
     big = torch.zeros(1, 65, 4, device="cuda")
     with pytest.raises(B.SDVError):
         api.tree_verify(big, big, torch.zeros(1, 65, dtype=torch.int32, device="cuda"), torch.zeros(1, 65, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("chosen", [False, True])
+def test_many_calls_at_once_agree(api, chosen):
+    """Clusters side by side on a full GPU, many times over: all of a cluster's CTAs see the same tree."""
+    g = gen(11)
+    B, W, V = 48, 24, 20001
+    target = torch.randn(B, W, V, generator=g, device="cuda")
+    draft = None if chosen else torch.randn(B, W, V, generator=g, device="cuda")
+    tokens = torch.randint(0, V, (B, W), generator=g, device="cuda", dtype=torch.int32)
+    parents = torch.stack([torch.tensor(tree_of("tree", W, b)) for b in range(B)]).to(torch.int32).cuda()
+    coins = torch.rand(B, W, generator=g, device="cuda") * (1e-4 if chosen else 1.0)
+    first = api.tree_verify(target, draft, tokens, parents, seed=3, coins=coins, with_status=True)
+    outs = [api.tree_verify(target, draft, tokens, parents, seed=3, coins=coins, with_status=True) for _ in range(300)]
+    assert int(first["accepted_len"].max()) > 0 and not first["status"].any()
+    for r in outs:
+        assert all(torch.equal(r[key], first[key]) for key in first)
