@@ -574,7 +574,7 @@ int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int6
  * (halves = 1) or (2 i, 2 i + 1) (halves = 0) becomes
  *   (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos freqs[i];
  * elements from rot on stay.  freqs [rot / 2] float64, radians a position (the angle's error is that of freqs[i] /
- * 2 pi in 64 bits times pos: positions need no small range).  positions [B, W] int32, or NULL: lengths[b] + i.
+ * 2 pi in 64 bits times pos: positions need no small range; frequencies are finite).  positions [B, W] int32, or NULL: lengths[b] + i.
  * Keys are turned in fp32 and rounded once, to their codes.  q [B, W, Hq, D] and q_out (`dtype`) have strides of
  * their own, 0 <= Hq D <= 2^27; q_out may be q, with its strides.  Queries i >= counts[b] become 0.  q and q_out may both be NULL.
  * 2 <= rot <= D, even.  The rest as in sdv_cache_append.
@@ -596,6 +596,11 @@ size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
  * sdv_tree_attend - sdv_cache_attend for a tree: the last counts[b] of the lengths[b] tokens in the cache are the
  * nodes, and node i sees the tokens before them, its ancestors and itself.  W at most SDV_MAX_TREE.  Nodes
  * i >= counts[b] get 0 and -inf, as all of a sequence with lengths[b] < counts[b] do (SDV_STATUS_BAD_TREE).
+ * As in sdv_cache_attend, a code that is NaN makes NaN of the rows that see it alone. Scores, sums and outputs are fp32;
+ * probabilities times their value's scale are rounded to the sum of two f16 (22 bits, or 2^-32 of the row's largest), and
+ * bf16 queries go through f16 under a power of two of their row. Value scales outside 2^-100 to 2^119 lose bits.
+ * Which kernel runs follows from the sizes and from the tokens that the page table could hold; both keep to this.
+ * SDV_STATUS_STUCK: a wait within the kernel ran out; the output is not to be used.
  */
 int sdv_tree_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h,
                     int dtype, int B, int W, int Hq, int H, int D, int block, const void *k_codes,

@@ -49,6 +49,7 @@ struct alignas(16) TreeSmall {
   uint64_t k_full[kKStages], k_free[kKStages], v_full[kVStages], v_free[kVStages];
   uint64_t s_full[2], p_full[2][2], p_free[2], o_full, drained;   // scores, probabilities: of a step's parity (and a group)
   uint64_t seg_full[kSegRing], set_full[kSegRing], seg_done[kSegRing], q_full[kSegRing];
+  uint64_t q_free;                                // of a segment: its last scores are had
   uint64_t soft;                                  // the softmax warps' meeting point
   Segment segs[kSegRing];
   uint64_t sets[kSegRing][SDV_MAX_TREE];          // what their nodes see of the tree
@@ -419,8 +420,9 @@ __device__ __forceinline__ void keys_role(const TreeRowsArgs& T, uint8_t* smem, 
     if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
     const Segment g = sm.segs[seg & (kSegRing - 1)];
     if (!g.steps) return;
-    // its queries, once the last scores before are had
-    if (t && !warp_wait(&sm.k_free[(t - 1) % kKStages], (t - 1) / kKStages & 1, dead)) return;
+    // its queries, once the last scores before are had.  (A barrier of its own: the values' warps may be two steps ahead of the
+    // scores, where the parity of the keys' would tell them of the step before the last.)
+    if (seg && !warp_wait(&sm.q_free, (seg - 1) & 1, dead)) return;
     L.put_queries(g, rt, T.rows, seg, tid);
     fence_async();
     warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
@@ -450,7 +452,7 @@ __device__ __forceinline__ void values_role(const TreeRowsArgs& T, uint8_t* smem
     if (!warp_wait(&sm.seg_full[seg & (kSegRing - 1)], seg / kSegRing & 1, dead)) return;
     const Segment g = sm.segs[seg & (kSegRing - 1)];
     if (!g.steps) return;
-    if (t && !warp_wait(&sm.k_free[(t - 1) % kKStages], (t - 1) / kKStages & 1, dead)) return;
+    if (seg && !warp_wait(&sm.q_free, (seg - 1) & 1, dead)) return;
     L.put_queries(g, rt, T.rows, seg, kGroupThreads + tid);
     fence_async();
     warp_arrive(&sm.q_full[seg & (kSegRing - 1)], lane);
@@ -503,6 +505,7 @@ __device__ __forceinline__ void scores_role(uint8_t* smem, TreeSmall& sm, int st
         }
         mma_commit(&sm.s_full[t & 1]);
         mma_commit(&sm.k_free[st]);
+        if (t + 1 == end) mma_commit(&sm.q_free);
       }
       __syncwarp();
     }
@@ -927,6 +930,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
       barrier_init(&sm.rv_free[k], kGroupWarps);
     }
     barrier_init(&sm.o_full, 1);
+    barrier_init(&sm.q_free, 1);
     barrier_init(&sm.drained, 2);
     barrier_init(&sm.soft, kSoftWarps);
     sm.dead = 0;

@@ -329,6 +329,24 @@ def test_offsets_past_32_bits(api):
         check_tree(api, q, cache, pages, n, tree_of("tree", W))
 
 
+@pytest.mark.parametrize("B,W,H,G,D,block,most", [(30, 59, 8, 4, 128, 64, 790), (14, 46, 4, 16, 128, 32, 717),
+                                                  (107, 52, 4, 4, 128, 64, 624), (60, 33, 8, 8, 64, 16, 400)])
+def test_many_short_sequences_time_and_again(api, B, W, H, G, D, block, most):
+    """Runs of several short items, whose queries follow one another: every call gives the same, and what 64 bits give."""
+    g = gen(B)
+    M = -(-most // block)
+    cache = make_cache(api, g, B * M, H, block, D)
+    pages = torch.randperm(B * M, generator=g, device="cuda").to(torch.int32).view(B, M)
+    n = torch.randint(W, most + 1, (B,), generator=g, device="cuda").to(torch.int32)
+    par = torch.stack([torch.tensor(tree_of("tree", W, b)) for b in range(B)]).to(torch.int32).cuda()
+    q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(BF16)
+    wide = widened(pages)
+    calls = [api.tree_attend(q, cache, wide, n, par) for _ in range(40)]
+    for r in calls[1:]:
+        assert torch.equal(r["out"], calls[0]["out"]) and torch.equal(r["lse"], calls[0]["lse"])
+    check_tree_as(api, q, cache, wide, n, [tree_of("tree", W, b) for b in range(B)])
+
+
 def test_graphs_streams_and_shared_workspaces(api):
     """Captured calls that share a workspace, replayed in turn with lengths that change; another stream; outputs of the
     caller; the same bits each time."""
