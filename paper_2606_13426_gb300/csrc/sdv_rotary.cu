@@ -65,9 +65,11 @@ __device__ __forceinline__ void fill_turns(uint64_t* turns, const RotaryArgs& A,
   if (tid < A.rot / 2) turns[tid] = turn_of(__ldg(A.freqs + tid));
 }
 // A table of cosines and sines: token t's pair i at t * table_row(pairs) + table_at(i).  Without the gaps the lanes of a warp,
-// which read pairs 8 or 16 apart and of several tokens, would meet in the same banks, up to 32 at once.
-__host__ __device__ __forceinline__ int table_at(int i) { return i + (i >> 3); }
-__host__ __device__ __forceinline__ int table_row(int pairs) { return (pairs + (pairs >> 3) + 15) / 16 * 16 + 5; }
+// which read pairs 8 or 16 apart and of several tokens, would meet in the same banks, up to 32 at once.  Two pairs from an even
+// one on are read together.
+__host__ __device__ __forceinline__ int table_at(int i) { return i + (i >> 3) * 2; }
+__host__ __device__ __forceinline__ int table_row(int pairs) { return (pairs + (pairs >> 3) * 2 + 15) / 16 * 16 + 2; }
+__device__ __forceinline__ float4 two_pairs(const float2* cs, int i) { return *reinterpret_cast<const float4*>(cs + table_at(i)); }
 // `tokens` tokens' table; pos: a token's position.
 template <typename F>
 __device__ __forceinline__ void fill_table(float2* table, const uint64_t* turns, int pairs, int tokens, int tid, F pos) {
@@ -82,6 +84,15 @@ __device__ __forceinline__ void fill_table(float2* table, const uint64_t* turns,
 }
 
 // Sixteen consecutive elements from x on, as fp32.
+// Four elements, two pairs (the second, if it is one).
+__device__ __forceinline__ void turn_neighbours(const float4& c, bool both, float* f) {
+  const float a = f[0], b = f[1], x = f[2], y = f[3];
+  f[0] = a * c.x - b * c.y;
+  f[1] = b * c.x + a * c.y;
+  f[2] = both ? x * c.z - y * c.w : x;
+  f[3] = both ? y * c.z + x * c.w : y;
+}
+
 template <int kDtype>
 __device__ __forceinline__ void load16(const typename Num<kDtype>::T* x, bool vec, float* f) {
   using E = Num<kDtype>;
@@ -100,23 +111,20 @@ __device__ __forceinline__ void turn_key(const typename Num<kDtype>::T* x, bool 
   if constexpr (kPairs == kHalvesOfUnits) {
     if (u1 * 16 < rot) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float2 c = cs[table_at(u0 * 16 + e)];
-        const float a = f[e], b = f[16 + e];
+      for (int e = 0; e < 16; e += 2) {
+        const float4 c = two_pairs(cs, u0 * 16 + e);
+        const float a = f[e], b = f[16 + e], x = f[e + 1], y = f[17 + e];
         f[e] = a * c.x - b * c.y;
         f[16 + e] = b * c.x + a * c.y;
+        f[e + 1] = x * c.z - y * c.w;
+        f[17 + e] = y * c.z + x * c.w;
       }
     }
   } else if constexpr (kPairs == kNeighbours) {
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
+    for (int e = 0; e < 32; e += 4) {
       const int at = (e < 16 ? u0 * 16 : u1 * 16 - 16) + e;
-      if (at < rot) {
-        const float2 c = cs[table_at(at / 2)];
-        const float a = f[e], b = f[e + 1];
-        f[e] = a * c.x - b * c.y;
-        f[e + 1] = b * c.x + a * c.y;
-      }
+      if (at < rot) turn_neighbours(two_pairs(cs, at / 2), at + 2 < rot, f + e);
     }
   } else {                               // halves that end inside a sixteen: the other half is read again
     const int half = rot / 2;
@@ -222,27 +230,19 @@ __device__ __forceinline__ void turn_queries(const RotaryArgs& A, float2* table,
           E::unpack(raw[k][1], b);
           if (A.halves) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-              const float2 c = cs[table_at(e0[k] + e)];
-              const float x = a[e], y = b[e];
+            for (int e = 0; e < kPer; e += 2) {
+              const float4 c = two_pairs(cs, e0[k] + e);
+              const float x = a[e], y = b[e], z = a[e + 1], w = b[e + 1];
               a[e] = x * c.x - y * c.y;
               b[e] = y * c.x + x * c.y;
+              a[e + 1] = z * c.z - w * c.w;
+              b[e + 1] = w * c.z + z * c.w;
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < kPer; e += 2) {
-              if (e0[k] + e < rot) {
-                const float2 c = cs[table_at((e0[k] + e) / 2)];
-                const float x = a[e], y = a[e + 1];
-                a[e] = x * c.x - y * c.y;
-                a[e + 1] = y * c.x + x * c.y;
-              }
-              if (e1[k] + e < rot) {
-                const float2 c = cs[table_at((e1[k] + e) / 2)];
-                const float x = b[e], y = b[e + 1];
-                b[e] = x * c.x - y * c.y;
-                b[e + 1] = y * c.x + x * c.y;
-              }
+            for (int e = 0; e < kPer; e += 4) {
+              if (e0[k] + e < rot) turn_neighbours(two_pairs(cs, (e0[k] + e) / 2), e0[k] + e + 2 < rot, a + e);
+              if (e1[k] + e < rot) turn_neighbours(two_pairs(cs, (e1[k] + e) / 2), e1[k] + e + 2 < rot, b + e);
             }
           }
           raw[k][0] = E::pack(a);
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kRotThreads, kItems == 1 ? 2 : 1) k_append_rot
 
 // The queries alone, where there are many: with the keys' registers half as many of these CTAs would be in flight.
 template <int kDtype>
-__global__ void __launch_bounds__(kRotThreads, 4) k_turn_queries(const RotaryArgs A) {
+__global__ void __launch_bounds__(kRotThreads, 3) k_turn_queries(const RotaryArgs A) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ uint64_t turns[64];
   turn_queries<kDtype>(A, reinterpret_cast<float2*>(smem), turns, (int)blockIdx.x);
