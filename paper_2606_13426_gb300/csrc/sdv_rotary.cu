@@ -16,7 +16,8 @@ constexpr int kRotThreads = 256;
 constexpr int kRotQueryElems = 16384;    // elements of a CTA that turns queries, about
 constexpr int kQueryTokens = 32;         // of it at most
 // CTAs on an SM above which they take more heads each, so that a page's cosines are computed fewer times.  With 6 and with 1, 64 x 1
-// tokens of 8 heads of 128 take 9.8 and 12.5 us in place of 8.8, 32 x 32 17.6 and 20.8 in place of 17.2.
+// tokens of 8 heads of 128 take 9.8 and 12.5 us in place of 8.8, 32 x 32 17.6 and 20.8 in
+// place of 17.2.
 constexpr int kGroupCtas = 3;
 constexpr int kQueriesApart = 6;         // CTAs of queries on an SM from which on they have a launch of their own
 constexpr int kQueryItems = 4;           // pairs of 16-byte vectors that a thread asks for at once
@@ -68,7 +69,7 @@ __device__ __forceinline__ void fill_turns(uint64_t* turns, const RotaryArgs& A,
 // which read pairs 8 or 16 apart and of several tokens, would meet in the same banks, up to 32 at once.  Two pairs from an even
 // one on are read together.
 __host__ __device__ __forceinline__ int table_at(int i) { return i + (i >> 3) * 2; }
-__host__ __device__ __forceinline__ int table_row(int pairs) { return (pairs + (pairs >> 3) * 2 + 15) / 16 * 16 + 2; }
+__host__ __device__ constexpr int table_row(int pairs) { return (pairs + (pairs >> 3) * 2 + 15) / 16 * 16 + 2; }
 __device__ __forceinline__ float4 two_pairs(const float2* cs, int i) { return *reinterpret_cast<const float4*>(cs + table_at(i)); }
 // `tokens` tokens' table; pos: a token's position.
 template <typename F>
@@ -277,9 +278,9 @@ __device__ __forceinline__ void turn_queries(const RotaryArgs& A, float2* table,
 }
 
 // Bound by what an SM has under way: a head's keys and values are read, their scales found by the CTA together, and written, with two
-// CTAs on an SM (three spill: 64-token pages of 4 x 8000 tokens then take 107 us in place of 89).  The queries go at the pace
-// of a copy.  4 x 8000 tokens of 8 key and 32 query heads of 128, bf16: 173 us, 720 MB, 4.2 TB/s; before the cosines' table
-// was laid out without bank conflicts and the queries asked for four vectors at a time 264.
+// CTAs on an SM (three spill: 64-token pages of 4 x 8000 tokens then take 107 us in place of 89; asking for the next head's rows
+// ahead 94).  The queries go at the pace of a copy.  4 x 8000 tokens of 8 key and 32 query heads of 128, bf16: 165 us, 720 MB,
+// 4.4 TB/s; before the cosines' table was laid out without bank conflicts and the queries asked for four vectors at a time 264.
 //
 // One CTA per (sequence, page, group of heads), and behind them the queries' CTAs.  Cosines and sines of the page's new
 // tokens are computed once for the group's heads, in shared memory; a thread has two sixteens of a key that are each other's
@@ -408,7 +409,8 @@ __global__ void __launch_bounds__(kRotThreads, kItems == 1 ? 2 : 1) k_append_rot
   }
 }
 
-// The queries alone, where there are many: with the keys' registers half as many of these CTAs would be in flight.
+// The queries alone, where there are many: with the keys' registers a third fewer of these CTAs would be in flight.  Bound by issue slots
+// (65 % busy) as much as by DRAM.
 template <int kDtype>
 __global__ void __launch_bounds__(kRotThreads, 3) k_turn_queries(const RotaryArgs A) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -419,8 +421,10 @@ __global__ void __launch_bounds__(kRotThreads, 3) k_turn_queries(const RotaryArg
 template <int kDtype, int kItems, int kPairs>
 static cudaError_t launch_rotary_as(const RotaryArgs& A, int64_t grid, size_t smem, cudaStream_t s) {
   const auto kern = k_append_rotary<kDtype, kItems, kPairs>;
-  if (smem > 48 << 10) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 40 << 10) {                                           // (48 KB with the kernel's own, without asking)
+    // the limit is shared by all host threads: its largest value
+    constexpr int kMost = SDV_MAX_BLOCK * (128 + table_row(128 / 2) * (int)sizeof(float2));
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
   }
   kern<<<(unsigned)grid, kRotThreads, smem, s>>>(A);

@@ -116,6 +116,26 @@ def test_append_rotary(api, B, W, H, G, D, block, pairs, rots, dtype):
         check_rotary(api, cache, k, v, pages, first, freqs, pairs, q, positions, counts)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_rotary_of_any_window(api, D):
+    """Every window against its tokens one by one: what a CTA holds grows with it."""
+    g = gen(D)
+    for block in (16, 48, 64, 80, 128):
+        k = torch.randn(1, 130, 1, D, generator=g, device="cuda").to(BF16)
+        pages = torch.arange(3 + 130 // block, device="cuda", dtype=torch.int32)[None]
+        n = torch.zeros(1, dtype=torch.int32, device="cuda")
+        freqs = api.rotary_freqs(D)
+        for W in list(range(1, 8)) + list(range(52, 131)):
+            cache = api.make_token_cache(pages.shape[1], 1, block, D)
+            q = api.cache_append_rotary(cache, k[:, :W], k[:, :W], pages, n, freqs, q=k[:, :W])
+            c = cache["k"].view(torch.uint8)[:, 0].reshape(-1, D).view(torch.float8_e4m3fn)[:W].double()
+            s = cache["k_scale"][:, 0].double().repeat_interleave(block)[:W, None]
+            y, size = turn(k[0, :W], torch.arange(W, device="cuda"), freqs, "halves")
+            tol = torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * s[:, None]) * 1.001 + 2.0 ** -21 * size
+            assert ((c * s - y[:, 0]).abs() <= tol[:, 0]).all(), (block, W)
+            assert ((q[0].double() - y).abs() <= HALF[BF16] * 1.01 * y.abs() + 2.0 ** -20 * size).all(), (block, W)
+
+
 def test_positions_far_and_negative(api):
     """Positions up to 2^30, frequencies of a caller's own (zero and negative ones among them)."""
     g = gen(2)
