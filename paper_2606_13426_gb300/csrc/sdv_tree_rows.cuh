@@ -895,7 +895,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 // A step of 128 keys and 128 rows of 128 takes about 1.45 us.  What bounds it is shared memory: codes in (32 KB), operands out
 // and in (128 KB), and read again by the products (96 KB) are 2048 cycles at 128 bytes a cycle, 1.07 us.  The products alone take
 // 1540 cycles (a third of them for the second half of the probabilities), the exponentials of both groups 1680, HBM's pace 1390.
-// 32 x 32 nodes of 8 x 4 heads over up to 16000 keys 217 us, 2.8 TB/s; 2 x 60 of 8 x 8 heads over up to 65000 360 us, 707
+// 32 x 32 nodes of 8 x 4 heads over up to 16000 keys 217 to 239 us by their lengths, 2.6 to
+// 2.8 TB/s; 2 x 60 of 8 x 8 heads over up to 65000 360 us, 707
 // TFLOP/s; k_attend on mma.sync takes 781 and 1124.  Tried without gain: one issuing warp for both products, groups that take
 // every other step, scores in two halves of 64 keys (1.84 us a step), codes read by the widening warps themselves.
 template <int kD>
