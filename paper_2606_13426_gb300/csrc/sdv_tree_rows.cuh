@@ -699,6 +699,7 @@ __device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, 
     const float base = large ? s.base + top : s.base;
     if (s.m > kNone) s.m = fmaxf(s.m + (s.base - base), kNone);
     s.base = base;
+    __syncwarp();
   }
   top = soft_top(at, chunks, scales, f0, sees, s.base, true);
   const bool move = top > s.m + kSlack;
@@ -802,6 +803,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         const uint64_t lo = nan.x | (uint64_t)nan.y << 32, hi = nan.z | (uint64_t)nan.w << 32;
         const uint64_t keys = !chunk0 ? lo : chunk0 == 4 ? hi : lo >> (16 * chunk0) | hi << (64 - 16 * chunk0);
         if (seen((g.step0 + n) * A.step + chunk0 * kChunk, sm.absent[slot]) & keys) mine.l = NAN;
+        __syncwarp();                                        // (tensor memory is read by all lanes at once)
       }
     };
 #pragma unroll 1
@@ -817,6 +819,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         if (busy) soft_tile<kD>(at, out + s * 128, chunks, scales, f0, before, mine);
       } else if (busy) {
         const uint64_t sees = seen(key0, absent);
+        __syncwarp();
         mine = soft_any<kD>(at, out + s * 128, chunks, scales, f0, sees, before, mine);
       }
       tmem_before_sync();
@@ -857,8 +860,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] += scaled(__uint_as_float(a[e]), c1);
         }
-        if (!have) continue;
-        if (g.whole) {
+        if (have && g.whole) {
           const bool zero = sum == 0.f;
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = zero ? 0.f : o[e] * by;
@@ -870,11 +872,12 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 #pragma unroll
             for (int e = 0; e < 32; ++e) put_out(A, to * kD + col + e, o[e]);
           }
-        } else {
+        } else if (have) {
           float4* y = reinterpret_cast<float4*>(part) + (col / 4) * kTileRows + row;
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e * kTileRows] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
         }
+        __syncwarp();                                        // the next columns are read by all lanes at once
       }
       if (have && s == 0) {
         if (g.whole) {
