@@ -592,6 +592,10 @@ int sdv_cache_append_rotary(const void *k_new, const void *v_new, int64_t stride
 /* Bytes of device workspace sdv_tree_attend needs; 0 for invalid sizes. */
 size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D);
 
+/* Which kernels sdv_tree_attend runs for these sizes on the current device: the tiles of up to 128 rows (W Hq / H) that those for
+ * many rows take, or 0 for the kernels of sdv_cache_attend; SDV_EINVAL for invalid sizes. */
+int sdv_tree_attend_row_tiles(int B, int W, int Hq, int H, int D, int block, int max_pages);
+
 /*
  * sdv_tree_attend - sdv_cache_attend for a tree: the last counts[b] of the lengths[b] tokens in the cache are the
  * nodes, and node i sees the tokens before them, its ancestors and itself.  W at most SDV_MAX_TREE.  Nodes

@@ -101,6 +101,7 @@ SIGNATURES = {
                                      _I, _I, _I, _I, _I, _I, _I, _P, _I, _I, _P, _P, _P, _P, _P, _I64, _P,
                                      _I, _P, _P, _P, _P]),
     "sdv_tree_attend_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "sdv_tree_attend_row_tiles": (_I, [_I, _I, _I, _I, _I, _I, _I]),
     "sdv_tree_attend": (_I, [_P, _I64, _I64, _I64, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I64,
                              _P, _I, _P, _P, _P, _F, _P, _P, _P, _P, _SZ, _P]),
     "sdv_tree_verify": (_I, [_P, _I64, _I64, _P, _I64, _I64, _P, _P, _I, _I, _I, _I, _F, _F, _P, _U64, _P,
@@ -399,6 +400,10 @@ def sdv_cache_append_rotary(k_new, v_new, stride_b, stride_t, stride_h, q, q_str
 
 def sdv_tree_attend_workspace_bytes(B, W, Hq, H, D):
     return int(load().sdv_tree_attend_workspace_bytes(B, W, Hq, H, D))
+
+
+def sdv_tree_attend_row_tiles(B, W, Hq, H, D, block, max_pages):
+    return int(load().sdv_tree_attend_row_tiles(B, W, Hq, H, D, block, max_pages))
 
 
 def sdv_tree_attend(q, q_stride_b, q_stride_t, q_stride_h, dtype, B, W, Hq, H, D, block, k_codes, v_codes,

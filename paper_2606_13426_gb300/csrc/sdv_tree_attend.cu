@@ -24,6 +24,23 @@ static AttendSpace tree_space(int B, int W, int Hq, int H, int D) {
   }
   return space;
 }
+
+// How a call is laid out: the tiles of rows, and which kernels take them.
+struct TreeChoice {
+  RowTiles tiles;
+  int step;                                 // keys of a step of the kernels for many rows
+  bool many;                                // those kernels
+};
+static TreeChoice choose_tree(int64_t R, int64_t heads, int D, int block, int max_pages) {
+  TreeChoice c;
+  const int64_t longest = (int64_t)max_pages * block, rt = (R + kTileRowsMost - 1) / kTileRowsMost;
+  int64_t cost = 0;
+  c.step = kTileKeys / block * block;
+  c.tiles = choose_tiles(R, heads, (longest + kSub - 1) / kSub, D, sm_count() * kAttendWarps, &cost);
+  c.many = rt <= sm_count() && rows_cost(rt, heads, longest, c.step, D) < cost;
+  if (c.many) c.tiles.rt = (int)rt;
+  return c;
+}
 size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * kTileRowsMost * (size_t)(D + 3) * 4 / 256 * 256 + 256; }
 
 }  // namespace sdv
@@ -35,6 +52,14 @@ extern "C" {
 size_t sdv_tree_attend_workspace_bytes(int B, int W, int Hq, int H, int D) {
   if (B < 1 || W < 1 || W > SDV_MAX_TREE || H < 1 || Hq < H || Hq % H || (D != 64 && D != 128)) return 0;
   return tree_space(B, W, Hq, H, D).total;
+}
+
+int sdv_tree_attend_row_tiles(int B, int W, int Hq, int H, int D, int block, int max_pages) {
+  if (!sdv_tree_attend_workspace_bytes(B, W, Hq, H, D) || block < 16 || block % 16 || block > SDV_MAX_BLOCK || max_pages < 1 ||
+      (int64_t)max_pages * block > kMaxTokens)
+    return SDV_EINVAL;
+  const TreeChoice c = choose_tree((int64_t)W * (Hq / H), (int64_t)B * H, D, block, max_pages);
+  return c.many ? c.tiles.rt : 0;
 }
 
 int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int dtype, int B, int W, int Hq,
@@ -57,12 +82,8 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   if (!workspace || workspace_bytes < space.total) return SDV_ENOWORKSPACE;
   if (!aligned_to(workspace, 256)) return SDV_EALIGN;
   AttendArgs A{};
-  const int64_t longest = (int64_t)max_pages * block, rt = (R + kTileRowsMost - 1) / kTileRowsMost;
-  const int step = kTileKeys / block * block;
-  int64_t cost = 0;
-  RowTiles tiles = choose_tiles(R, (int64_t)B * H, (longest + kSub - 1) / kSub, D, sm_count() * kAttendWarps, &cost);
-  const bool many = rt <= sm_count() && rows_cost(rt, (int64_t)B * H, longest, step, D) < cost;
-  if (many) tiles.rt = (int)rt;
+  const TreeChoice choice = choose_tree(R, (int64_t)B * H, D, block, max_pages);
+  const RowTiles tiles = choice.tiles;
   A.q = q;
   A.bf16 = dtype == SDV_BF16;
   A.q_vec = aligned_to(q, 16) && q_stride_b % 8 == 0 && q_stride_t % 8 == 0 && q_stride_h % 8 == 0;
@@ -76,7 +97,7 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
   A.out = out, A.lse = lse, A.status = status;
   A.part = (float*)workspace;
   A.ctas = sm_count();
-  A.step = many ? step : 0;
+  A.step = choice.many ? choice.step : 0;
   cudaStream_t s = (cudaStream_t)stream;
   if (B > kPrefixFrom) {
     int64_t* prefix = (int64_t*)((char*)workspace + space.part);
@@ -84,7 +105,7 @@ int sdv_tree_attend(const void* q, int64_t q_stride_b, int64_t q_stride_t, int64
     if (e != cudaSuccess) return launched(e);
     A.prefix = prefix;
   }
-  if (many) {
+  if (choice.many) {
     const int rows = (int)((R + tiles.rt - 1) / tiles.rt);
     return launched(D == 64 ? launch_tree_rows_64(A, rows, s) : launch_tree_rows_128(A, rows, s));
   }
