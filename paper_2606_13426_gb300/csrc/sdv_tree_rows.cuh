@@ -37,6 +37,7 @@ constexpr int kTileChunks = kTileKeys / kChunk;
 constexpr int kSoftRegs = 144, kLoadRegs = 72, kOtherRegs = 40;
 static_assert(32 * (kSoftWarps * kSoftRegs + kLoadWarps * kLoadRegs + 4 * kOtherRegs) <= kTreeThreads * 96, "");
 constexpr float kMostPlain = 0x1p20f;             // scores up to which a reference of one number serves
+constexpr int kAside = 64;                        // steps whose products are summed in tensor memory (see put_aside)
 constexpr int kMinTileSteps = 2;                  // of a run, where there are fewer steps than teams could take
 
 // Steps [step0, step0 + steps) of an item; steps = 0: no more.
@@ -59,7 +60,7 @@ struct alignas(16) TreeSmall {
   float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
   uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_probs)
   alignas(16) uint32_t nan_keys[kScaleRing][4];               // keys that have NaN among their values
-  float ml[2][3][kTileRows];                      // the groups' references, sums, bases
+  float ml[2][4][kTileRows];                      // the groups' references, sums, bases, lags
   uint32_t tmem;
   int dead;
 };
@@ -74,6 +75,7 @@ struct TreeShape {
   static constexpr size_t kSmem = 1024 + kSmallAt + sizeof(TreeSmall);
   // floats of a partial: output [D / 4][row][4], so that a warp's rows are written together; reference (two numbers), sum
   static constexpr int kSlot = kTileRows * (kD + 3);
+  static constexpr int kAsideAt = kTileRows * kD;                     // floats that a group has put aside, [D / 4][row][4]
   static constexpr int kLoads = kD / 16;                             // sixteens of a thread's keys, or of its values
   static_assert(kSmem <= 227 * 1024, "");
 };
@@ -548,7 +550,7 @@ __device__ __forceinline__ void out_role(uint8_t* smem, TreeSmall& sm, int step)
 #pragma unroll 1
           for (int i = i0; i < i1; ++i) {
             const int off = ((i >> 2) * S::kVBlock + (i & 3) * 32) / 16;
-            mma_ts(out, p + i * 16, vt + off, kOut, n > 0 || i > i0);
+            mma_ts(out, p + i * 16, vt + off, kOut, n % kAside > 0 || i > i0);
             mma_ts(out, p + i * 16 + 8, vt + off, kOut, true);
           }
           if (h) {
@@ -577,9 +579,9 @@ __device__ __forceinline__ uint64_t placed(uint64_t set, int at) {
 }
 
 // A row's running state: its reference base + m (log2; base is 0 unless its scores are past 2^20), and the sum of
-// 2^(score - reference).
+// 2^(score - reference).  lag: log2 of what takes the sums put aside to the reference (not above 0).
 struct SoftRow {
-  float m, l, base;
+  float m, l, base, lag;
 };
 // x 2^d for d <= 0, in two steps: neither factor underflows where the product does not.
 __device__ __forceinline__ float scaled(float x, float half) { return x * half * half; }
@@ -656,7 +658,41 @@ template <int kD>
 __device__ __forceinline__ void soft_move(uint32_t out, const Before& before, float d, SoftRow& s) {
   const float half = ex2(.5f * d);
   s.l = scaled(s.l, half);
+  s.lag += d;
   if (before.bar) move_out<kD>(out, before, half);
+}
+// The matrix unit cuts its sums off instead of rounding them: where the products have one sign, 128 keys more cost 5e-7 of the
+// sum, 1.6e-4 after 250 steps, a third of f16's half step and more with every key.  So what kAside steps have
+// summed in tensor memory goes over into sums that are rounded to nearest, a group's and row's own in the workspace (in L2), and
+// the next product begins from nothing: 3.1e-5 at most, whatever a sequence's length.  It comes behind a step's probabilities,
+// when the products before are done, and takes about 2 us: 2 x 60 nodes of 8 x 8 heads over 65000 keys 377 us in place of 368 (every
+// 32 steps 382), 32 x 32 of 8 x 4 heads over up to 16000 keys 255 in place of 254 (261).
+template <int kD>
+__device__ __noinline__ void put_aside(uint32_t out, float* aside, int row, Before before, float lag, bool first) {
+  const float half = ex2(.5f * lag);
+  float4* y = reinterpret_cast<float4*>(aside) + row;
+#pragma unroll 1
+  for (int g = 0; g < kD / 64; ++g, y += 16 * kTileRows) {
+    float4 b[16];                                            // (64 numbers of a row on their way at once)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b[e] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : y[e * kTileRows];
+    if (g == 0) {
+      warp_wait(before.bar, before.parity, before.dead);
+      tmem_after_sync();
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t r[16];
+      tmem_load16(out + 64 * g + 16 * c, r);
+      tmem_loaded16(r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = b[4 * c + e];
+        y[(4 * c + e) * kTileRows] = make_float4(scaled(v.x, half) + __uint_as_float(r[4 * e]), scaled(v.y, half) + __uint_as_float(r[4 * e + 1]),
+                                                 scaled(v.z, half) + __uint_as_float(r[4 * e + 2]), scaled(v.w, half) + __uint_as_float(r[4 * e + 3]));
+      }
+    }
+  }
 }
 __device__ __forceinline__ void soft_load(uint32_t at, uint32_t* x) {
   tmem_load32(at, x);
@@ -772,6 +808,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
   const uint32_t out = lanes + 2 * kTileKeys;
   const int all = T.a.step / kChunk, chunk0 = s ? first_half(all) : 0, chunks = s ? all - chunk0 : first_half(all);   // this group's
   Meeting meet{&sm.soft, 0};
+  // the groups' sums that are put aside: behind all partials
+  float* aside = A.part + (int64_t)A.ctas * 2 * S::kSlot + (int64_t)blockIdx.x * 2 * S::kAsideAt;
   const int r = rt * T.rows + row, i = r / A.G;
   int t = 0;
 #pragma unroll 1
@@ -786,7 +824,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     const uint64_t set = live ? sm.sets[seg & (kSegRing - 1)][i] : 0;
     const float f0 = A.scale2 * sm.downs[seg & (kSegRing - 1)][row];
     const int at0 = g.len - g.count;                      // the root's place
-    SoftRow mine{kNone, 0.f, 0.f};
+    SoftRow mine{kNone, 0.f, 0.f, 0.f};
     // what the row sees of a step's keys from key0 on
     const auto seen = [&](int key0, uint32_t absent) {
       uint64_t can = (below(at0 - key0) | placed(set, at0 - key0)) & below(chunks * kChunk);
@@ -822,6 +860,10 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         __syncwarp();
         mine = soft_any<kD>(at, out + s * 128, chunks, scales, f0, sees, before, mine);
       }
+      if (busy && n && n % kAside == 0) {                    // (behind the probabilities: the products before are done by now)
+        put_aside<kD>(out + s * 128, aside + s * S::kAsideAt, row, before, mine.lag, n == kAside);
+        mine.lag = 0.f;
+      }
       tmem_before_sync();
       warp_arrive(&sm.p_full[t & 1][s], lane);
     }
@@ -833,6 +875,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     sm.ml[s][0][row] = mine.m;
     sm.ml[s][1][row] = mine.l;
     sm.ml[s][2][row] = mine.base;
+    sm.ml[s][3][row] = mine.lag;
     if (!meet(lane, dead)) return;
     if (busy || (__any_sync(0xffffffffu, have))) {
       const float m0 = sm.ml[0][0][row], m1 = sm.ml[1][0][row], b0 = sm.ml[0][2][row], b1 = sm.ml[1][2][row];
@@ -842,6 +885,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
       const float sum = live ? scaled(sm.ml[0][1][row], c0) + scaled(sm.ml[1][1][row], c1) : 0.f;
       const float by = !g.whole ? 1.f / kPScale : sum == 0.f ? 0.f : 1.f / sum / kPScale;
       const int64_t to = ((int64_t)g.b * A.W + i) * (A.c.H * A.G) + g.h * A.G + (r - i * A.G);
+      const bool more = g.steps > kAside;                    // some sums were put aside
+      const float h0 = ex2(.5f * sm.ml[0][3][row]), h1 = ex2(.5f * sm.ml[1][3][row]);
       float* part = A.part + ((int64_t)(blockIdx.x * 2 + g.slot)) * S::kSlot;
 #pragma unroll 1
       for (int k = 0; k < kD / 64; ++k) {
@@ -851,10 +896,24 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
         if (busy) {
+          if (more) {                                        // what both groups have put aside, on its way at once
+            const float4* x = reinterpret_cast<const float4*>(aside) + (col / 4) * kTileRows + row;
+            float4 v[2][8];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = x[(e >> 3) * (S::kAsideAt / 4) + (e & 7) * kTileRows];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              o[4 * e] = scaled(scaled(v[0][e].x, h0), c0) + scaled(scaled(v[1][e].x, h1), c1);
+              o[4 * e + 1] = scaled(scaled(v[0][e].y, h0), c0) + scaled(scaled(v[1][e].y, h1), c1);
+              o[4 * e + 2] = scaled(scaled(v[0][e].z, h0), c0) + scaled(scaled(v[1][e].z, h1), c1);
+              o[4 * e + 3] = scaled(scaled(v[0][e].w, h0), c0) + scaled(scaled(v[1][e].w, h1), c1);
+            }
+            __syncwarp();
+          }
           tmem_load32(out + col, a);
           tmem_loaded(a);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = scaled(__uint_as_float(a[e]), c0);
+          for (int e = 0; e < 32; ++e) o[e] += scaled(__uint_as_float(a[e]), c0);
           tmem_load32(out + 128 + col, a);
           tmem_loaded(a);
 #pragma unroll

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from test_gpu_tokens import BF16, F16, api, gen, make_cache  # noqa: F401
-from test_gpu_tree_attend import check_tree_as, tree_of, widened
+from test_gpu_tree_attend import HALF, LEAST, check_tree_as, plain_tree, tree_of, widened
 
 pytestmark = pytest.mark.gpu
 
@@ -37,6 +37,20 @@ def laid_out(api, g, lengths, H, block, D, spare=3):
     cache = make_cache(api, g, B * M + spare, H, block, D)
     pages = torch.randperm(B * M + spare, generator=g, device="cuda")[:B * M].to(torch.int32).view(B, M)
     return cache, widened(pages), torch.tensor(lengths, device="cuda", dtype=torch.int32)
+
+
+def check_result(r, q, cache, pages, lengths, par):
+    """A result against 64 bits, as check_tree_as holds its own to them, but for the sums: 2^-15 for those of 64 steps, and 2^-24
+    of a step's 128 terms and each step after it."""
+    D, n = q.shape[3], float(lengths.max())
+    out, lse, mag, most = plain_tree(q, cache, pages, lengths, [q.shape[1]] * q.shape[0], par, D ** -0.5)
+    sums = (128 + n / 128) * 2.0 ** -24
+    E = (2 * D + 8) * 2.0 ** -24 * most
+    tol = 2 * (E[..., None] + 2.0 ** -15 + sums) * mag + 1.01 * HALF[q.dtype] * out.abs() + LEAST[q.dtype]
+    err = (r["out"].double() - out).abs()
+    assert (err <= tol).all(), "output off by %g of its bound" % float((err / tol).max())
+    err = (r["lse"].double() - lse).abs()
+    assert (err <= E + 2.0 ** -19 + sums + 2.0 ** -22 * lse.abs()).all(), "lse off by %g" % float(err.max())
 
 
 PAGES = [(block, D) for block in range(16, 129, 16) for D in (64, 128)]
@@ -127,3 +141,56 @@ def test_which_kernels_run(api):
     from paper_2606_13426_gb300 import binding as B
     assert B.sdv_tree_attend_row_tiles(2, 4, 8, 8, 128, 64, 1000) == 0
     assert [B.sdv_tree_attend_row_tiles(32, W, 32, 8, 128, 64, 250) for W in (32, 33, 64)] == [1, 2, 2]
+
+
+@pytest.mark.parametrize("W,H,G,D,B", [(64, 1, 8, 128, 40), (64, 1, 8, 64, 40), (32, 1, 4, 128, 152)])
+def test_sums_do_not_lose_with_their_length(api, W, H, G, D, B):
+    """Values that are all alike, so that an output is the ratio of two sums of the same probabilities, 2^-14 to either side of the
+    middle between two f16 numbers: it rounds to the one on its side if it is within 2^-14, 6.1e-5, of the value.
+
+    The matrix unit's sums are cut off: 5e-7 for a step of 128 keys, 3.2e-5 for the 64 that are summed there (without a limit
+    these runs of 250 steps lose 1.6e-4).  Probabilities' halves lose 2^-22, the sums of probabilities, rounded to nearest, (128 +
+    250) 2^-24 at most: 5.5e-5 altogether."""
+    g = gen(91 + W + D)
+    block, n = 64, 32000
+    cache = make_cache(api, g, n // block, H, block, D)
+    cache["v"].view(torch.uint8).fill_(0x38)             # 1
+    pages = torch.arange(n // block, device="cuda", dtype=torch.int32).expand(B, -1).contiguous()
+    lengths = torch.full((B,), n, device="cuda", dtype=torch.int32)
+    q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(F16)
+    parents = torch.tensor(tree_of("tree", W), dtype=torch.int32, device="cuda").expand(B, W).contiguous()
+    assert row_tiles(q, cache, pages) == W * G // 128
+    for side, want in ((1, 1 + 2.0 ** -10), (-1, 1.0)):
+        cache["v_scale"].fill_((1 + 2.0 ** -11) * (1 + side * 2.0 ** -14))
+        r = api.tree_attend(q, cache, pages, lengths, parents)
+        assert (r["out"] == want).all(), "%d of %d" % (int((r["out"] != want).sum()), r["out"].numel())
+
+
+@pytest.mark.parametrize("growing", ["keys", "huge", "values"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_references_that_move_over_many_steps(api, D, growing):
+    """Runs of 157 steps, of which every 64 are put aside: scores that grow along the sequence, so that the rows' references pass
+    what was put aside again and again; scores past 2^20, which get bases; value scales far apart."""
+    g = gen(95 + D)
+    W, G, B, block, n = 64, 8, 38, 32, 20000
+    cache = make_cache(api, g, n // block, 1, block, D)
+    at = torch.arange(n // block, device="cuda", dtype=torch.float32)[:, None] / (n // block)
+    if growing == "keys":
+        cache["k_scale"].copy_(0.05 + 4 * at)
+    elif growing == "huge":
+        cache["k_scale"].copy_(torch.exp2(torch.floor(24 * at)))
+    else:
+        cache["v_scale"].copy_(torch.exp2(torch.floor(40 * torch.rand(at.shape, generator=g, device="cuda") - 20)))
+    one = torch.arange(n // block, device="cuda", dtype=torch.int32)[None]
+    pages = one.expand(B, -1).contiguous()
+    lengths = torch.full((B,), n, device="cuda", dtype=torch.int32)
+    for dtype in (BF16, F16):
+        if growing == "values" and dtype == F16:
+            cache["v_scale"].clamp_(2.0 ** -6, 2.0 ** 5)
+        q = torch.randn(1, W, G, D, generator=g, device="cuda").to(dtype)
+        many = q.expand(B, -1, -1, -1).contiguous()
+        assert row_tiles(many, cache, pages) == 4
+        par = tree_of("tree", W)
+        r = api.tree_attend(many, cache, pages, lengths, torch.tensor([par] * B, device="cuda", dtype=torch.int32))
+        assert all(torch.equal(r[k], r[k][:1].expand_as(r[k])) for k in ("out", "lse"))     # each of them one run
+        check_result({k: t[:1] for k, t in r.items()}, q, cache, one, lengths[:1], [par])
