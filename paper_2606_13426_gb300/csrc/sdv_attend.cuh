@@ -36,6 +36,7 @@
 namespace sdv {
 
 constexpr int kSub = 32;                  // keys of a step
+constexpr int kTreeAside = 128;           // steps of a tree's run whose products the matrix unit sums (see k_attend)
 constexpr int kTileKeys = 128;            // of a step of the kernels for many rows, at most: whole pages
 constexpr int kJoinWarps = 8;
 constexpr int kJoinThreads = 32 * kJoinWarps;
@@ -232,7 +233,8 @@ struct AttendShape {
   static constexpr int kKv = kD / 64;                     // 16-byte pieces of a key for a thread
   static constexpr int kQBytes = kRows * kD * 2;
   static constexpr int kScaleBytes = kScaleSlots * 32;    // of a step: ks, vs of both chunks; absent chunks
-  static constexpr int kRowBytes = kRows * 12;            // of a row: the sum's reference, the score's base, the query's power of two
+  // of a row: the sum's reference, the score's base, the query's power of two, what takes the sums put aside to the reference
+  static constexpr int kRowBytes = kRows * (kTree ? 16 : 12);
   static constexpr int kSetBytes = kTree ? SDV_MAX_TREE * 8 : 0;   // of a node: what it sees of the tree
   static constexpr int kWarpBytes = kHalves * kHalf + kQBytes + kScaleBytes + kRowBytes + kSetBytes;
   static constexpr size_t kSmem = (size_t)kWarps * kWarpBytes;
@@ -273,7 +275,11 @@ __device__ __forceinline__ float q_largest(uint4 v, bool bf16) {
 // as their own rounding again (2.9e-4 of their size, 2.0e-4 with two), and bf16 outputs were roundings of numbers
 // up to 2^-12 off, so that some fell on the neighbouring value.  The second half costs those windows 48 us, few rows nothing.
 // kTree: the window's queries are the nodes of a tree (sdv_tree.cuh), each of which sees the tokens before the window, the nodes
-// above it and itself; whole steps before the window are as they are for a chain.
+// above it and itself; whole steps before the window are as they are for a chain.  The matrix unit cuts its sums off: 1.6e-7 a step
+// where the products have one sign, 1.6e-4 after 1000.  For trees what kTreeAside steps have summed is added, rounded to
+// nearest, to what was put aside in the item's partial, so that 2e-5 is all, at any length.  16 x 8 nodes of 8 x 4 heads over
+// 8000 keys take 112 us with and 113 without it; with an addition after each step in its place 122, with the
+// steps in one loop 115.
 template <int kD, int kNt, bool kTree>
 __global__ void __launch_bounds__(AttendShape<kD, kNt, kTree>::kThreads, 1) k_attend(const AttendArgs A) {
   using S = AttendShape<kD, kNt, kTree>;
@@ -289,6 +295,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt, kTree>::kThreads, 1) k_at
   float* refs = reinterpret_cast<float*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes);   // the sums', where they are kept apart
   float* bases = refs + S::kRows;
   float* downs = bases + S::kRows;
+  float* lags = downs + S::kRows;                          // (kTree)
   uint64_t* sets = reinterpret_cast<uint64_t*>(ring + S::kHalves * S::kHalf + S::kQBytes + S::kScaleBytes + S::kRowBytes);
 
   const int64_t units = step_sums<kTree>(A, 0, lane).total * per;
@@ -462,6 +469,7 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt, kTree>::kThreads, 1) k_at
                   lane, a0, a1);
         sets[lane] = a0;
         sets[32 + lane] = a1;
+        for (int r = lane; r < S::kRows; r += 32) lags[r] = 1.f;
       }
       __syncwarp();
     }
@@ -487,274 +495,302 @@ __global__ void __launch_bounds__(AttendShape<kD, kNt, kTree>::kThreads, 1) k_at
       mx[k] = kNone;
       sum[k] = 0.f;
     }
+    // what has been put aside of this thread's sums (kTree), in the item's partial: [m][n][lane][4]
+    float4* aside = reinterpret_cast<float4*>(A.part + ((int64_t)run * 2 + (first_segment ? 0 : 1)) * S::kSlot) + lane;
     int half = 0, slot = 0;                                 // of this step's keys
     auto after = [](int x, int by, int of) { return x + by >= of ? x + by - of : x + by; };
-    for (int n = 0; n < steps; ++n) {
-      const int free_half = after(half, S::kHalves - 1, S::kHalves), free_slot = after(slot, S::kAhead, S::kScaleSlots);
-      if (n + S::kAhead < steps) issue_keys(n + S::kAhead, free_half, free_slot, np0, np1);
-      else nothing();
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
-      __syncwarp();
-      const uint8_t* from = ring + half * S::kHalf;
-      uint8_t* values = ring + after(half, 1, S::kHalves) * S::kHalf;
-      const float* sc = scales + slot * 8;
-      const int key0 = key_of(n);
-      // scores: sx[s][n][0, 1] of key row g and rows 2t, 2t + 1; [2, 3] of key row g + 8
-      float sx[2][kNt][4];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int k = 0; k < kNt; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sx[s][k][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < kKv; ++i) {
-        uint4 raw[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) raw[q] = *reinterpret_cast<const uint4*>(from + ((q * kKv + i) * 32 + lane) * 16);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t a[2][4];
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            widen4(reinterpret_cast<const uint32_t*>(&raw[2 * s])[w], a[s][0], a[s][2]);
-            widen4(reinterpret_cast<const uint32_t*>(&raw[2 * s + 1])[w], a[s][1], a[s][3]);
-          }
-#pragma unroll
-          for (int k = 0; k < kNt; ++k) {
-            const uint2 qb = *(reinterpret_cast<const uint2*>(qf + ((k * kKv + i) * 2 + (w >> 1)) * 32 + lane) + (w & 1));
-            mma16816(sx[0][k], a[0], qb.x, qb.y);
-            mma16816(sx[1][k], a[1], qb.x, qb.y);
-          }
-        }
-      }
-      __syncwarp();                                          // the keys are read: their half is the next values'
-      if (n + S::kAhead < steps) issue_values(n + S::kAhead, half, np0, np1);
-      else nothing();
-      look(n + S::kAhead + 1);
-      const int chunk = g >> 2;
-      const float4 s4 = *reinterpret_cast<const float4*>(sc);   // ks, vs of the first chunk, of the second
-      float f = (chunk ? s4.z : s4.x) * rsc;                 // what a raw score is to be multiplied by
-      float vs = chunk ? s4.w : s4.y;
-      const int absent = __float_as_int(sc[4]);
-      float lw = __log2f(fabsf(vs) * winv), ipw = ex2(-lw);    // of kPScale vs / U; what takes a sum of p' to one of 2^(s - m)
-      const bool big = !(fmaxf(fabsf(s4.x), fabsf(s4.z)) * most_score <= kMostScore);
-      const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || modes || big ||
-                          !(max_nan(fabsf(s4.y), fabsf(s4.w)) * winv <= kMostPw && fminf(fabsf(s4.y), fabsf(s4.w)) * winv >= kLeastPw);
-      if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
-        const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
+    for (int n0 = 0, n1 = 0; n0 < steps; n0 = n1) {
+      n1 = kTree ? min(n0 + kTreeAside, steps) : steps;
+      for (int n = n0; n < n1; ++n) {
+        const int free_half = after(half, S::kHalves - 1, S::kHalves), free_slot = after(slot, S::kAhead, S::kScaleSlots);
+        if (n + S::kAhead < steps) issue_keys(n + S::kAhead, free_half, free_slot, np0, np1);
+        else nothing();
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
+        __syncwarp();
+        const uint8_t* from = ring + half * S::kHalf;
+        uint8_t* values = ring + after(half, 1, S::kHalves) * S::kHalf;
+        const float* sc = scales + slot * 8;
+        const int key0 = key_of(n);
+        // scores: sx[s][n][0, 1] of key row g and rows 2t, 2t + 1; [2, 3] of key row g + 8
+        float sx[2][kNt][4];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int k = 0; k < kNt; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sx[s][k][e] *= by;
-        f = f < 0.f ? -f : 1.f;
-      }
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
-      __syncwarp();
-      if (masked) {
-        if (modes & kUneven) {
+            for (int e = 0; e < 4; ++e) sx[s][k][e] = 0.f;
 #pragma unroll
-          for (int k = 0; k < kNt; ++k) {
-            const float2 d = *reinterpret_cast<const float2*>(downs + 8 * k + 2 * t);
+        for (int i = 0; i < kKv; ++i) {
+          uint4 raw[4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) sx[s][k][0] *= d.x, sx[s][k][1] *= d.y, sx[s][k][2] *= d.x, sx[s][k][3] *= d.y;
+          for (int q = 0; q < 4; ++q) raw[q] = *reinterpret_cast<const uint4*>(from + ((q * kKv + i) * 32 + lane) * 16);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              widen4(reinterpret_cast<const uint32_t*>(&raw[2 * s])[w], a[s][0], a[s][2]);
+              widen4(reinterpret_cast<const uint32_t*>(&raw[2 * s + 1])[w], a[s][1], a[s][3]);
+            }
+#pragma unroll
+            for (int k = 0; k < kNt; ++k) {
+              const uint2 qb = *(reinterpret_cast<const uint2*>(qf + ((k * kKv + i) * 2 + (w >> 1)) * 32 + lane) + (w & 1));
+              mma16816(sx[0][k], a[0], qb.x, qb.y);
+              mma16816(sx[1][k], a[1], qb.x, qb.y);
+            }
           }
         }
-        // magnitudes of the value scales, of chunks that some row sees (-1: none does; 0: a scale that is none)
-        const auto seen = [&](int key, float va, int out) {
-          return absent & out || key > max_last || key + kChunk <= min_begin ? -1.f : va < INFINITY ? va : 0.f;
-        };
-        const float va0 = seen(key0, fabsf(s4.y), 1), va1 = seen(key0 + kChunk, fabsf(s4.w), 2), va = chunk ? va1 : va0;
-        const auto far = [&](float x) { return x >= 0.f && !(x * winv <= kMostPw && x * winv >= kLeastPw); };
-        if (!(modes & kWide) && (far(va0) || far(va1))) {
-          modes |= kWide;
-          if (g == 0) {
-#pragma unroll
-            for (int k = 0; k < kR; ++k) refs[8 * (k >> 1) + 2 * t + (k & 1)] = mx[k];
-          }
-          __syncwarp();
-        }
-        const bool wide = modes & kWide, based = modes & kBased;
-        if (wide) {
-          ipw = 0.f;
-          lw = va > 0.f ? __log2f(va) + __log2f(winv) : -INFINITY;
-        } else if (!(va >= 0.f)) {                         // (no row sees the chunk)
-          ipw = 1.f;
-          lw = 0.f;
-        }
-        // which of this thread's 8 value tokens count as 0
-        const int have = sq.len - key0 - 8 * t;
-        uint32_t drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
-        uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
-#pragma unroll 1
-        for (int m = 0; m < 2 * kMt; ++m) {
-          const uint2 v = *reinterpret_cast<const uint2*>(values + (m * 32 + lane) * 8);
-          // a byte's low seven bits are all ones: its top bit after adding one to them
-          const uint32_t x = ((v.x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u, y = ((v.y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-          nan_keys |= (x >> 7 & 1) | (x >> 14 & 2) | (x >> 21 & 4) | (x >> 28 & 8) | (y >> 3 & 16) | (y >> 10 & 32) | (y >> 17 & 64) | (y >> 24 & 128);
-        }
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) nan_keys |= __shfl_xor_sync(0xffffffffu, nan_keys, o);
-        nan_keys &= ~drop;
-        drop |= nan_keys;
-        nan_keys = __shfl_sync(0xffffffffu, nan_keys, g >> 1);   // of this thread's keys
-        if (drop) {                                        // in the ring: a thread reads what it alone has written here
-          uint2 keep = make_uint2(0u, 0u);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            keep.x |= drop >> e & 1 ? 0u : 0xffu << (8 * e);
-            keep.y |= drop >> (e + 4) & 1 ? 0u : 0xffu << (8 * e);
-          }
-#pragma unroll 1
-          for (int m = 0; m < 2 * kMt; ++m) {
-            uint2* at = reinterpret_cast<uint2*>(values + (m * 32 + lane) * 8);
-            *at = make_uint2(at->x & keep.x, at->y & keep.y);
-          }
-        }
-        if (!(fabsf(vs) < INFINITY)) {                     // a scale that is none: as NaN codes
-          nan_keys = 0xffu;
-          vs = 0.f;
-        }
-        const bool here = !(absent >> chunk & 1);
-#pragma unroll
-        for (int k = 0; k < kR; ++k) {
-          const int row = row0 + 8 * (k >> 1) + 2 * t + (k & 1);
-          const int last = at0 + row / A.G, begin = A.span > 0 ? last - A.span + 1 : 0;
-          const uint64_t set = kTree ? sets[min(row / A.G, SDV_MAX_TREE - 1)] : 0;
+        __syncwarp();                                          // the keys are read: their half is the next values'
+        if (n + S::kAhead < steps) issue_values(n + S::kAhead, half, np0, np1);
+        else nothing();
+        look(n + S::kAhead + 1);
+        const int chunk = g >> 2;
+        const float4 s4 = *reinterpret_cast<const float4*>(sc);   // ks, vs of the first chunk, of the second
+        float f = (chunk ? s4.z : s4.x) * rsc;                 // what a raw score is to be multiplied by
+        float vs = chunk ? s4.w : s4.y;
+        const int absent = __float_as_int(sc[4]);
+        float lw = __log2f(fabsf(vs) * winv), ipw = ex2(-lw);    // of kPScale vs / U; what takes a sum of p' to one of 2^(s - m)
+        const bool big = !(fmaxf(fabsf(s4.x), fabsf(s4.z)) * most_score <= kMostScore);
+        const bool masked = key0 + kSub - 1 > min_last || key0 < max_begin || absent || modes || big ||
+                            !(max_nan(fabsf(s4.y), fabsf(s4.w)) * winv <= kMostPw && fminf(fabsf(s4.y), fabsf(s4.w)) * winv >= kLeastPw);
+        if (!(f > 0.f)) {                                      // a scale of 0, below 0 or none
+          const float by = f == 0.f ? 0.f : f < 0.f ? -1.f : f;
 #pragma unroll
           for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int tok = 4 * s + 2 * e + (g & 1), key = key0 + 8 * (g >> 1) + tok;
-              float& x = sx[s][k >> 1][2 * e + (k & 1)];
-              const bool hidden = kTree ? key >= at0 && (key > last || !(set >> ((key - at0) & 63) & 1)) : key > last || key < begin;
-              if (hidden || !here) x = -INFINITY;
-              else if (nan_keys >> tok & 1) x = NAN;
-            }
+            for (int k = 0; k < kNt; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sx[s][k][e] *= by;
+          f = f < 0.f ? -f : 1.f;
         }
-        if (based || big) {                                // from here on scores have bases, the sums' references to begin with
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kHalves - 1));
+        __syncwarp();
+        if (masked) {
+          if (modes & kUneven) {
+#pragma unroll
+            for (int k = 0; k < kNt; ++k) {
+              const float2 d = *reinterpret_cast<const float2*>(downs + 8 * k + 2 * t);
+#pragma unroll
+              for (int s = 0; s < 2; ++s) sx[s][k][0] *= d.x, sx[s][k][1] *= d.y, sx[s][k][2] *= d.x, sx[s][k][3] *= d.y;
+            }
+          }
+          // magnitudes of the value scales, of chunks that some row sees (-1: none does; 0: a scale that is none)
+          const auto seen = [&](int key, float va, int out) {
+            return absent & out || key > max_last || key + kChunk <= min_begin ? -1.f : va < INFINITY ? va : 0.f;
+          };
+          const float va0 = seen(key0, fabsf(s4.y), 1), va1 = seen(key0 + kChunk, fabsf(s4.w), 2), va = chunk ? va1 : va0;
+          const auto far = [&](float x) { return x >= 0.f && !(x * winv <= kMostPw && x * winv >= kLeastPw); };
+          if (!(modes & kWide) && (far(va0) || far(va1))) {
+            modes |= kWide;
+            if (g == 0) {
+#pragma unroll
+              for (int k = 0; k < kR; ++k) refs[8 * (k >> 1) + 2 * t + (k & 1)] = mx[k];
+            }
+            __syncwarp();
+          }
+          const bool wide = modes & kWide, based = modes & kBased;
+          if (wide) {
+            ipw = 0.f;
+            lw = va > 0.f ? __log2f(va) + __log2f(winv) : -INFINITY;
+          } else if (!(va >= 0.f)) {                         // (no row sees the chunk)
+            ipw = 1.f;
+            lw = 0.f;
+          }
+          // which of this thread's 8 value tokens count as 0
+          const int have = sq.len - key0 - 8 * t;
+          uint32_t drop = have >= 8 ? 0u : (0xffu << max(have, 0)) & 0xffu;
+          uint32_t nan_keys = 0;                             // value codes that are NaN (0x7f, 0xff)
+#pragma unroll 1
+          for (int m = 0; m < 2 * kMt; ++m) {
+            const uint2 v = *reinterpret_cast<const uint2*>(values + (m * 32 + lane) * 8);
+            // a byte's low seven bits are all ones: its top bit after adding one to them
+            const uint32_t x = ((v.x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u, y = ((v.y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            nan_keys |= (x >> 7 & 1) | (x >> 14 & 2) | (x >> 21 & 4) | (x >> 28 & 8) | (y >> 3 & 16) | (y >> 10 & 32) | (y >> 17 & 64) | (y >> 24 & 128);
+          }
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) nan_keys |= __shfl_xor_sync(0xffffffffu, nan_keys, o);
+          nan_keys &= ~drop;
+          drop |= nan_keys;
+          nan_keys = __shfl_sync(0xffffffffu, nan_keys, g >> 1);   // of this thread's keys
+          if (drop) {                                        // in the ring: a thread reads what it alone has written here
+            uint2 keep = make_uint2(0u, 0u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              keep.x |= drop >> e & 1 ? 0u : 0xffu << (8 * e);
+              keep.y |= drop >> (e + 4) & 1 ? 0u : 0xffu << (8 * e);
+            }
+#pragma unroll 1
+            for (int m = 0; m < 2 * kMt; ++m) {
+              uint2* at = reinterpret_cast<uint2*>(values + (m * 32 + lane) * 8);
+              *at = make_uint2(at->x & keep.x, at->y & keep.y);
+            }
+          }
+          if (!(fabsf(vs) < INFINITY)) {                     // a scale that is none: as NaN codes
+            nan_keys = 0xffu;
+            vs = 0.f;
+          }
+          const bool here = !(absent >> chunk & 1);
 #pragma unroll
           for (int k = 0; k < kR; ++k) {
-            const int r = 8 * (k >> 1) + 2 * t + (k & 1);
-            const float ref = wide ? refs[r] : mx[k];       // (of the sum; without its base, if that is new)
-            const bool some = ref > kNone;
-            const float was = based ? bases[r] : 0.f, now = based || !some ? was : ref;
-            float top = -INFINITY;
+            const int row = row0 + 8 * (k >> 1) + 2 * t + (k & 1);
+            const int last = at0 + row / A.G, begin = A.span > 0 ? last - A.span + 1 : 0;
+            const uint64_t set = kTree ? sets[min(row / A.G, SDV_MAX_TREE - 1)] : 0;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
+                const int tok = 4 * s + 2 * e + (g & 1), key = key0 + 8 * (g >> 1) + tok;
                 float& x = sx[s][k >> 1][2 * e + (k & 1)];
-                x = __fmul_rn(x, f);
-                top = max_nan(top, x);
+                const bool hidden = kTree ? key >= at0 && (key > last || !(set >> ((key - at0) & 63) & 1)) : key > last || key < begin;
+                if (hidden || !here) x = -INFINITY;
+                else if (nan_keys >> tok & 1) x = NAN;
               }
+          }
+          if (based || big) {                                // from here on scores have bases, the sums' references to begin with
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-            // moved by what is far above it; by whatever is far from it, where the row has seen nothing
-            const float base = (some ? top - now : fabsf(top - now)) > kBaseRoom && fabsf(top) < INFINITY ? top : now;
-            if (mx[k] > kNone) mx[k] = fmaxf(mx[k] + (was - base), kNone);
+            for (int k = 0; k < kR; ++k) {
+              const int r = 8 * (k >> 1) + 2 * t + (k & 1);
+              const float ref = wide ? refs[r] : mx[k];       // (of the sum; without its base, if that is new)
+              const bool some = ref > kNone;
+              const float was = based ? bases[r] : 0.f, now = based || !some ? was : ref;
+              float top = -INFINITY;
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+              for (int s = 0; s < 2; ++s)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) sx[s][k >> 1][2 * e + (k & 1)] -= base;
-            __syncwarp();
-            if (g == 0) {
-              bases[r] = base;
-              if (wide && some) refs[r] = fmaxf(ref + (was - base), kNone);
+                for (int e = 0; e < 2; ++e) {
+                  float& x = sx[s][k >> 1][2 * e + (k & 1)];
+                  x = __fmul_rn(x, f);
+                  top = max_nan(top, x);
+                }
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+              // moved by what is far above it; by whatever is far from it, where the row has seen nothing
+              const float base = (some ? top - now : fabsf(top - now)) > kBaseRoom && fabsf(top) < INFINITY ? top : now;
+              if (mx[k] > kNone) mx[k] = fmaxf(mx[k] + (was - base), kNone);
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) sx[s][k >> 1][2 * e + (k & 1)] -= base;
+              __syncwarp();
+              if (g == 0) {
+                bases[r] = base;
+                if (wide && some) refs[r] = fmaxf(ref + (was - base), kNone);
+              }
             }
-          }
-          __syncwarp();
-          modes |= kBased;
-          f = 1.f;
-        }
-        if (wide) {
-#pragma unroll
-          for (int k = 0; k < kR; ++k) {
-            float* at = refs + 8 * (k >> 1) + 2 * t + (k & 1);
-            float x = f * max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
-                                  max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
-            const float was = *at, m = max_nan(was, x), c = ex2(was - m);
-            float add = 0.f;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) add += ex2(fmaf(sx[s][k >> 1][2 * e + (k & 1)], f, -m));
-            sum[k] = fmaf(sum[k], c, add);
             __syncwarp();
-            if (g == 0) *at = m;
+            modes |= kBased;
+            f = 1.f;
           }
-          __syncwarp();
-        }
-      }
-      float top[kR];                                         // of log2 p' + mx
-      bool move = false;
+          if (wide) {
 #pragma unroll
-      for (int k = 0; k < kR; ++k) {
-        top[k] = fmaf(f, max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
-                                 max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)])), lw);
-        move |= !(top[k] <= mx[k] + (kSlack + kLogPScale));
-      }
-      if (__any_sync(0xffffffffu, move)) {
+            for (int k = 0; k < kR; ++k) {
+              float* at = refs + 8 * (k >> 1) + 2 * t + (k & 1);
+              float x = f * max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
+                                    max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)]));
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+              const float was = *at, m = max_nan(was, x), c = ex2(was - m);
+              float add = 0.f;
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) add += ex2(fmaf(sx[s][k >> 1][2 * e + (k & 1)], f, -m));
+              sum[k] = fmaf(sum[k], c, add);
+              __syncwarp();
+              if (g == 0) *at = m;
+            }
+            __syncwarp();
+          }
+        }
+        float top[kR];                                         // of log2 p' + mx
+        bool move = false;
 #pragma unroll
         for (int k = 0; k < kR; ++k) {
+          top[k] = fmaf(f, max_nan(max_nan(sx[0][k >> 1][k & 1], sx[0][k >> 1][2 + (k & 1)]),
+                                   max_nan(sx[1][k >> 1][k & 1], sx[1][k >> 1][2 + (k & 1)])), lw);
+          move |= !(top[k] <= mx[k] + (kSlack + kLogPScale));
+        }
+        if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) top[k] = max_nan(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
-          // a row's own affair
-          const float m = top[k] <= mx[k] + (kSlack + kLogPScale) ? mx[k] : max_nan(mx[k], top[k] - kLogPScale);
-          const float c = ex2(mx[k] - m);
-          mx[k] = m;
-          if (!(modes & kWide)) sum[k] *= c;
+          for (int k = 0; k < kR; ++k) {
 #pragma unroll
-          for (int q = 0; q < kMt; ++q) {
-            acc[q][k >> 1][k & 1] *= c;
-            acc[q][k >> 1][2 + (k & 1)] *= c;
+            for (int o = 4; o < 32; o <<= 1) top[k] = max_nan(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+            // a row's own affair
+            const float m = top[k] <= mx[k] + (kSlack + kLogPScale) ? mx[k] : max_nan(mx[k], top[k] - kLogPScale);
+            const float c = ex2(mx[k] - m);
+            mx[k] = m;
+            if (!(modes & kWide)) sum[k] *= c;
+#pragma unroll
+            for (int q = 0; q < kMt; ++q) {
+              acc[q][k >> 1][k & 1] *= c;
+              acc[q][k >> 1][2 + (k & 1)] *= c;
+            }
+            if (kTree && g == 0) lags[8 * (k >> 1) + 2 * t + (k & 1)] *= c;
           }
         }
-      }
-      const uint32_t sign = vs < 0.f ? 0x80008000u : 0u;
-      uint32_t pb[2][kNt][2];                               // probabilities, transposed
-      uint32_t pl[2][kNt][2];                               // what f16 leaves of them
+        const uint32_t sign = vs < 0.f ? 0x80008000u : 0u;
+        uint32_t pb[2][kNt][2];                               // probabilities, transposed
+        uint32_t pl[2][kNt][2];                               // what f16 leaves of them
 #pragma unroll
-      for (int k = 0; k < kNt; ++k) {
-        const float m0 = lw - mx[2 * k], m1 = lw - mx[2 * k + 1];
-        float s0 = 0.f, s1 = 0.f;
+        for (int k = 0; k < kNt; ++k) {
+          const float m0 = lw - mx[2 * k], m1 = lw - mx[2 * k + 1];
+          float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float e0 = ex2(fmaf(sx[s][k][2 * e], f, m0)), e1 = ex2(fmaf(sx[s][k][2 * e + 1], f, m1));
-            s0 += e0;
-            s1 += e1;
-            const uint32_t high = pack_half(e0, e1);
-            pb[s][k][e] = transpose8(high ^ sign);
-            const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&high));
-            pl[s][k][e] = transpose8(pack_half(e0 - held.x, e1 - held.y) ^ sign);
-          }
-        sum[2 * k] = fmaf(s0, ipw, sum[2 * k]);
-        sum[2 * k + 1] = fmaf(s1, ipw, sum[2 * k + 1]);
-      }
-#pragma unroll
-      for (int m = 0; m < kMt; ++m) {
-        const uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
-        const uint2 w1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          uint32_t a[4];
-          widen4(s ? w0.y : w0.x, a[0], a[2]);
-          widen4(s ? w1.y : w1.x, a[1], a[3]);
-#pragma unroll
-          for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
-#pragma unroll
-          for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
+            for (int e = 0; e < 2; ++e) {
+              const float e0 = ex2(fmaf(sx[s][k][2 * e], f, m0)), e1 = ex2(fmaf(sx[s][k][2 * e + 1], f, m1));
+              s0 += e0;
+              s1 += e1;
+              const uint32_t high = pack_half(e0, e1);
+              pb[s][k][e] = transpose8(high ^ sign);
+              const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&high));
+              pl[s][k][e] = transpose8(pack_half(e0 - held.x, e1 - held.y) ^ sign);
+            }
+          sum[2 * k] = fmaf(s0, ipw, sum[2 * k]);
+          sum[2 * k + 1] = fmaf(s1, ipw, sum[2 * k + 1]);
         }
+#pragma unroll
+        for (int m = 0; m < kMt; ++m) {
+          const uint2 w0 = *reinterpret_cast<const uint2*>(values + ((2 * m) * 32 + lane) * 8);
+          const uint2 w1 = *reinterpret_cast<const uint2*>(values + ((2 * m + 1) * 32 + lane) * 8);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            uint32_t a[4];
+            widen4(s ? w0.y : w0.x, a[0], a[2]);
+            widen4(s ? w1.y : w1.x, a[1], a[3]);
+#pragma unroll
+            for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pb[s][k][0], pb[s][k][1]);
+#pragma unroll
+            for (int k = 0; k < kNt; ++k) mma16816(acc[m][k], a, pl[s][k][0], pl[s][k][1]);
+          }
+        }
+        half = after(half, 2, S::kHalves);
+        slot = after(slot, 1, S::kScaleSlots);
+        __syncwarp();
       }
-      half = after(half, 2, S::kHalves);
-      slot = after(slot, 1, S::kScaleSlots);
-      __syncwarp();
+      if (kTree && steps > kTreeAside) {                     // over to what was put aside, or, at the end, back from it
+#pragma unroll
+        for (int k = 0; k < kNt; ++k) {
+          const float2 lag = *reinterpret_cast<const float2*>(lags + 8 * k + 2 * t);
+#pragma unroll
+          for (int m = 0; m < kMt; ++m) {
+            float4* at = aside + (m * kNt + k) * 32;
+            const float4 x = n0 == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *at;
+            acc[m][k][0] = fmaf(x.x, lag.x, acc[m][k][0]);
+            acc[m][k][1] = fmaf(x.y, lag.y, acc[m][k][1]);
+            acc[m][k][2] = fmaf(x.z, lag.x, acc[m][k][2]);
+            acc[m][k][3] = fmaf(x.w, lag.y, acc[m][k][3]);
+            if (n1 < steps) {
+              *at = make_float4(acc[m][k][0], acc[m][k][1], acc[m][k][2], acc[m][k][3]);
+              acc[m][k][0] = acc[m][k][1] = acc[m][k][2] = acc[m][k][3] = 0.f;
+            }
+          }
+        }
+        __syncwarp();                                          // (read by all before the lags, or the partial, are written)
+        for (int r = lane; r < S::kRows; r += 32) lags[r] = 1.f;
+        __syncwarp();
+      }
     }
     asm volatile("cp.async.wait_group 0;");
     // the item's results, or a partial of them: its output, and 2^m l for the sum, 1 <= l < 2

@@ -41,10 +41,10 @@ def laid_out(api, g, lengths, H, block, D, spare=3):
 
 def check_result(r, q, cache, pages, lengths, par):
     """A result against 64 bits, as check_tree_as holds its own to them, but for the sums: 2^-15 for those of 64 steps, and 2^-24
-    of a step's 128 terms and each step after it."""
+    of a step's 128 terms and each of up to n / 32 steps after it."""
     D, n = q.shape[3], float(lengths.max())
     out, lse, mag, most = plain_tree(q, cache, pages, lengths, [q.shape[1]] * q.shape[0], par, D ** -0.5)
-    sums = (128 + n / 128) * 2.0 ** -24
+    sums = (128 + n / 32) * 2.0 ** -24
     E = (2 * D + 8) * 2.0 ** -24 * most
     tol = 2 * (E[..., None] + 2.0 ** -15 + sums) * mag + 1.01 * HALF[q.dtype] * out.abs() + LEAST[q.dtype]
     err = (r["out"].double() - out).abs()
@@ -193,4 +193,51 @@ def test_references_that_move_over_many_steps(api, D, growing):
         par = tree_of("tree", W)
         r = api.tree_attend(many, cache, pages, lengths, torch.tensor([par] * B, device="cuda", dtype=torch.int32))
         assert all(torch.equal(r[k], r[k][:1].expand_as(r[k])) for k in ("out", "lse"))     # each of them one run
+        check_result({k: t[:1] for k, t in r.items()}, q, cache, one, lengths[:1], [par])
+
+
+@pytest.mark.parametrize("W,D", [(2, 64), (2, 128), (8, 128)])
+def test_sums_of_few_rows_do_not_lose_with_their_length(api, W, D):
+    """As above for the kernels for few rows, a run of 1000 steps of 32 keys a warp: a step's products are summed by the matrix unit
+    (1.3e-7), the steps rounded to nearest, within 1000 2^-24 = 6e-5 were they all one way, in fact within a hundredth of it."""
+    g = gen(97 + W + D)
+    B, H, G, block, n = torch.cuda.get_device_properties(0).multi_processor_count, 8, 4, 64, 32000
+    cache = make_cache(api, g, n // block, H, block, D)
+    cache["v"].view(torch.uint8).fill_(0x38)             # 1
+    pages = torch.arange(n // block, device="cuda", dtype=torch.int32).expand(B, -1).contiguous()
+    lengths = torch.full((B,), n, device="cuda", dtype=torch.int32)
+    q = torch.randn(B, W, H * G, D, generator=g, device="cuda").to(F16)
+    parents = torch.tensor(tree_of("tree", W), dtype=torch.int32, device="cuda").expand(B, W).contiguous()
+    assert row_tiles(q, cache, pages) == 0
+    for side, want in ((1, 1 + 2.0 ** -10), (-1, 1.0)):
+        cache["v_scale"].fill_((1 + 2.0 ** -11) * (1 + side * 2.0 ** -14))
+        r = api.tree_attend(q, cache, pages, lengths, parents)
+        assert (r["out"] == want).all(), "%d of %d" % (int((r["out"] != want).sum()), r["out"].numel())
+
+
+@pytest.mark.parametrize("growing", ["keys", "huge", "values"])
+@pytest.mark.parametrize("W,D", [(3, 64), (2, 128), (8, 128)])
+def test_references_of_few_rows_that_move_over_many_steps(api, W, D, growing):
+    """The same on the kernels for few rows, in runs of 625 steps of 32 keys."""
+    g = gen(99 + W + D)
+    B, H, G, block, n = torch.cuda.get_device_properties(0).multi_processor_count, 8, 4, 32, 20000
+    cache = make_cache(api, g, n // block, H, block, D)
+    at = torch.arange(n // block, device="cuda", dtype=torch.float32)[:, None] / (n // block)
+    if growing == "keys":
+        cache["k_scale"].copy_((0.05 + 4 * at).expand(-1, H))
+    elif growing == "huge":
+        cache["k_scale"].copy_(torch.exp2(torch.floor(24 * at)).expand(-1, H))
+    one = torch.arange(n // block, device="cuda", dtype=torch.int32)[None]
+    pages = one.expand(B, -1).contiguous()
+    lengths = torch.full((B,), n, device="cuda", dtype=torch.int32)
+    for dtype in (BF16, F16):
+        if growing == "values":
+            span = 40 if dtype == BF16 else 10
+            cache["v_scale"].copy_(torch.exp2(torch.floor(span * torch.rand(at.shape[0], H, generator=g, device="cuda") - span / 2)))
+        q = torch.randn(1, W, H * G, D, generator=g, device="cuda").to(dtype)
+        many = q.expand(B, -1, -1, -1).contiguous()
+        assert row_tiles(many, cache, pages) == 0
+        par = tree_of("tree", W)
+        r = api.tree_attend(many, cache, pages, lengths, torch.tensor([par] * B, device="cuda", dtype=torch.int32))
+        assert all(torch.equal(r[k], r[k][:1].expand_as(r[k])) for k in ("out", "lse"))     # each item one warp's
         check_result({k: t[:1] for k, t in r.items()}, q, cache, one, lengths[:1], [par])
