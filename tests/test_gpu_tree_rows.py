@@ -241,3 +241,43 @@ def test_references_of_few_rows_that_move_over_many_steps(api, W, D, growing):
         r = api.tree_attend(many, cache, pages, lengths, torch.tensor([par] * B, device="cuda", dtype=torch.int32))
         assert all(torch.equal(r[k], r[k][:1].expand_as(r[k])) for k in ("out", "lse"))     # each item one warp's
         check_result({k: t[:1] for k, t in r.items()}, q, cache, one, lengths[:1], [par])
+
+
+@pytest.mark.parametrize("wide", [True, False])
+@pytest.mark.parametrize("W,H,G,D", [(64, 2, 2, 128), (64, 2, 2, 64), (4, 2, 4, 128), (6, 2, 2, 64)])
+def test_probabilities_have_22_bits(api, W, H, G, D, wide):
+    """Scores without rounding errors (whole queries, keys and scales): f16 outputs are roundings of numbers within 2^-18 sum p |v|.
+
+    A score is a whole number times scale / ln 2 in fp32, below 32: half a step of it, with the argument's own rounding, makes
+    2^-19.5 of a probability; ex2 2^-22; its halves 2^-22; the sum of probabilities 2^-22 (pairs of 64 terms, few steps); what the matrix unit cuts off of
+    the sum of products 5e-7, 2^-21, a step of 128 keys, runs have two steps here.  Together below 2^-18.4.  With eleven bits
+    (one half alone), outputs are off by up to 2^-10 of them: the bound has to turn them down."""
+    g = gen(101 + W + D)
+    block, n = 32, 1500
+    M = 200_000 // block if wide else n // block + 1
+    cache = make_cache(api, g, 2 * (n // block + 1), H, block, D)
+    cache["k"].copy_((torch.randint(-2, 3, cache["k"].shape, generator=g, device="cuda")).float().to(torch.float8_e4m3fn))
+    cache["k_scale"].fill_(0.25)
+    cache["v"].copy_((1 + torch.rand(cache["v"].shape, generator=g, device="cuda")).to(torch.float8_e4m3fn))
+    cache["v_scale"].copy_(torch.exp2(torch.randint(-1, 2, cache["v_scale"].shape, generator=g, device="cuda").float()))
+    pages = torch.full((2, M), -1, dtype=torch.int32, device="cuda")
+    pages[:, :n // block + 1] = torch.arange(2 * (n // block + 1), device="cuda", dtype=torch.int32).view(2, -1)
+    lengths = torch.tensor([n, 321], device="cuda", dtype=torch.int32)
+    q = torch.randint(-2, 3, (2, W, H * G, D), generator=g, device="cuda").to(F16)
+    assert (row_tiles(q, cache, pages) > 0) == (wide and W == 64)
+    par = [tree_of("tree", W)] * 2
+    scale = D ** -0.5
+    out, _, mag, most = plain_tree(q, cache, pages[:, :n // block + 1], lengths, [W, W], par, scale)
+    got = api.tree_attend(q, cache, pages, lengths, torch.tensor(par, device="cuda", dtype=torch.int32))["out"].double()
+    low, high = [x.to(F16).double() for x in (out - 2.0 ** -18 * mag, out + 2.0 ** -18 * mag)]
+    assert (low <= got).all() and (got <= high).all()
+    # a row of the oracle's with probabilities of eleven bits, cut off below the row's largest
+    at = torch.arange(n - W + 1, device="cuda")
+    k = (cache["k"][pages[0, at // block].long(), 0, at % block].double() * 0.25)
+    v = cache["v"][pages[0, at // block].long(), 0, :, at % block].double() * cache["v_scale"][pages[0, at // block].long(), 0].double()[:, None]
+    p = torch.softmax(scale * (q[0, 0, :G].double() @ k.T), 1)
+    assert ((p @ v - out[0, 0, :G]).abs() <= 1e-12).all()
+    _, e = torch.frexp(p)
+    cut = torch.floor(p * torch.exp2(11.0 - e)) * torch.exp2(e - 11.0)
+    bad = (cut @ v).to(F16).double()
+    assert not ((low[0, 0, :G] <= bad) & (bad <= high[0, 0, :G])).all()
