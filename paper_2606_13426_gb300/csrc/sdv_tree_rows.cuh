@@ -212,9 +212,10 @@ __device__ __forceinline__ bool next_step(Cursor& c, TreeSmall& sm) {
   return true;
 }
 
-// Page `lane` of each step: its number two steps ahead, its scales one, then its keys and values.
+// Page `lane` of each step: its number two steps ahead, its scales one, then its keys and values.  `keys`, `values`: the steps
+// whose copies were issued.
 template <int kD>
-__device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int lane) {
+__device__ __forceinline__ void copy_steps(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int lane, int& keys, int& values) {
   using S = TreeShape<kD>;
   const AttendArgs& A = T.a;
   int* dead = &sm.dead;
@@ -264,6 +265,7 @@ __device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, 
       if (lane == 0) barrier_expect(&sm.rk_full[slot], __popc(there) * bytes);
       __syncwarp();
       if (page >= 0) copy_bulk(smem_addr(smem + S::kRk + slot * S::kHalf) + lane * bytes, A.c.k + head * bytes, bytes, &sm.rk_full[slot]);
+      keys = t + 1;
     }
     {
       const int slot = t % kRawV, turn = t / kRawV;
@@ -271,6 +273,7 @@ __device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, 
       if (lane == 0) barrier_expect(&sm.rv_full[slot], __popc(there) * bytes);
       __syncwarp();
       if (page >= 0) copy_bulk(smem_addr(smem + S::kRv + slot * S::kHalf) + lane * bytes, A.c.v + head * bytes, bytes, &sm.rv_full[slot]);
+      values = t + 1;
     }
     page = page1, h = h1, more = more1;
     ks = scale_of(A.c.ks, page, h, 1.f);
@@ -278,6 +281,14 @@ __device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, 
     if (more && !next_step(c, sm)) return;
     page1 = page_of(c), h1 = c.g.h, more1 = c.g.steps;
   }
+}
+// Whether all is done or a wait gave up: no copy is under way when the block ends.
+template <int kD>
+__device__ __forceinline__ void copy_role(const TreeRowsArgs& T, uint8_t* smem, TreeSmall& sm, int lane) {
+  int keys = 0, values = 0, ignore = 0;
+  copy_steps<kD>(T, smem, sm, lane, keys, values);
+  for (int t = max(0, keys - kRawK); t < keys; ++t) warp_wait(&sm.rk_full[t % kRawK], t / kRawK & 1, &ignore);
+  for (int t = max(0, values - kRawV); t < values; ++t) warp_wait(&sm.rv_full[t % kRawV], t / kRawV & 1, &ignore);
 }
 
 // ------------------------------------------------------------------------------ loading warps
