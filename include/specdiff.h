@@ -409,7 +409,7 @@ int sdv_em_sample(int B, int64_t d, const float *means, const float *log_weights
 #define SDV_STATUS_BAD_PAGE  32u   /* a page outside the cache, or a token past the page table */
 
 #define SDV_STATUS_BAD_TREE  64u   /* a parent that does not come before its child, or a path that leaves the tree */
-#define SDV_STATUS_STUCK    128u   /* (never, as far as is known) a kernel gave up waiting for its own parts: its results are none */
+#define SDV_STATUS_STUCK    128u   /* (never, as far as is known) a kernel gave up waiting for its own parts: the results are NaN */
 
 #define SDV_MAX_TOP   32       /* largest number of alternatives */
 #define SDV_MAX_TREE  64       /* largest number of nodes of a drafted tree */
@@ -604,7 +604,8 @@ int sdv_tree_attend_row_tiles(int B, int W, int Hq, int H, int D, int block, int
  * probabilities times their value's scale are rounded to the sum of two f16 (22 bits, or 2^-32 of the row's largest), and
  * bf16 queries go through f16 under a power of two of their row. Value scales outside 2^-100 to 2^119 lose bits.
  * Which kernel runs follows from the sizes and from the tokens that the page table could hold; both keep to this.
- * SDV_STATUS_STUCK: a wait within the kernel ran out; the output is not to be used.
+ * SDV_STATUS_STUCK: a wait within the kernel ran out; out and lse of what it was to write of that sequence are NaN, with or
+ * without a status.
  */
 int sdv_tree_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h,
                     int dtype, int B, int W, int Hq, int H, int D, int block, const void *k_codes,

@@ -649,7 +649,8 @@ def cache_append_rotary(cache, k_new, v_new, page_table, lengths, freqs, *, pair
 def tree_attend(q, cache, page_table, lengths, parents, *, counts=None, scale=None, status=None, workspace=None, out=None):
     """Attention of a drafted tree's nodes q [B, W, Hq, D], whose tokens are the last ones of the cache, each over
     the tokens before the tree, its ancestors and itself (sdv_tree_attend); parents [B, W] int32 (-1 for a
-    root).  lengths [B] count the nodes too.  Returns out [B, W, Hq, D] and lse [B, W, Hq].  scale defaults to D^-1/2."""
+    root).  lengths [B] count the nodes too.  Returns out [B, W, Hq, D] and lse [B, W, Hq].  scale defaults to D^-1/2.  Outputs
+    that a kernel gave up on (SDV_STATUS_STUCK) are NaN."""
     P, H, block, D, Bn, M = _cache_args(cache, page_table, lengths, counts)
     dt = _rows("q", q, 4)
     W, Hq = q.shape[1], q.shape[2]

@@ -41,8 +41,8 @@ static TreeChoice choose_tree(int64_t R, int64_t heads, int D, int block, int ma
   if (c.many) c.tiles.rt = (int)rt;
   return c;
 }
-// Two partials a CTA, with a row's references and sum, and what its two groups put aside.
-size_t tree_rows_part(int D) { return (size_t)sm_count() * 2 * kTileRowsMost * (size_t)(D + 3 + D) * 4 / 256 * 256 + 256; }
+// Two partials a CTA, with a row's references and sum, what its two groups put aside, and whether it gave up.
+size_t tree_rows_part(int D) { return (size_t)sm_count() * (2 * kTileRowsMost * (size_t)(D + 3 + D) + 1) * 4 / 256 * 256 + 256; }
 
 }  // namespace sdv
 

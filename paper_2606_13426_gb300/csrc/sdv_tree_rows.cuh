@@ -85,6 +85,12 @@ struct TreeRowsArgs {
   int rows, teams;                 // rows of a tile; teams of RT CTAs
 };
 
+// Behind the partials and what was put aside, of each CTA: whether a wait of it gave up, so that what it was to write is not there.
+template <int kD>
+__device__ __forceinline__ int* gave_up(const TreeRowsArgs& T) {
+  return reinterpret_cast<int*>(T.a.part + (int64_t)T.a.ctas * 2 * (TreeShape<kD>::kSlot + TreeShape<kD>::kAsideAt));
+}
+
 __device__ __forceinline__ int tree_runs(int64_t units, int teams) {
   return (int)min((int64_t)teams, (units + kMinTileSteps - 1) / kMinTileSteps);
 }
@@ -1038,10 +1044,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
   __syncthreads();
   tmem_after_sync();
   if (warp == kScoreWarp) tmem_free(sm.tmem, 512);
-  if (sm.dead && tid == 0 && T.a.status) atomicOr(T.a.status, SDV_STATUS_STUCK);
+  if (tid == 0) gave_up<kD>(T)[blockIdx.x] = sm.dead;      // k_tree_join tells
 }
 
-// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros.  A CTA has 32 rows, a lane each.
+// Joins the partials of an item that several teams' runs hold; an item without steps gets zeros, one of which a part is missing
+// NaN.  A CTA has 32 rows, a lane each.
 // Its warps share out the partials for the rows' references and weights (kept in shared memory, a batch at a time), and the
 // columns, eight at a time, for the sums.  Bound by latency: 14.7 us after a cold cache for 96 items of 128 rows, a few of them behind
 // the kernel before.
@@ -1074,8 +1081,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
     g1 = (int)(((u1 - 1) * runs) / units);
     while (run_start(units, g1 + 1, runs) <= u1 - 1) ++g1;
     while (run_start(units, g1, runs) > u1 - 1) --g1;
-    if (g0 == g1) return;                                   // written by that run's CTA
   }
+  bool stuck = false;                                        // a run's CTA gave up: what it had of the item is not there
+  for (int gi = g0 + lane; gi <= g1; gi += 32) stuck |= gave_up<kD>(T)[gi * A.RT + rt] != 0;
+  stuck = __any_sync(0xffffffffu, stuck);
+  if (stuck && A.status && threadIdx.x == 0) atomicOr(A.status + b, SDV_STATUS_STUCK);
+  if (g0 == g1 && !stuck) return;                           // written by that run's CTA
   const bool live = row < T.rows && r < A.R;
   const int64_t first = g0 <= g1 && run_start(units, g0, runs) < u0 ? 1 : 0;
   const auto slot_of = [&](int gi) { return A.part + (((int64_t)gi * A.RT + rt) * 2 + (gi == g0 ? first : 0)) * S::kSlot; };
@@ -1138,6 +1149,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_tree_join(const TreeRowsArgs T
   for (int w = 0; w < kJoinWarps; ++w) l += sums[w][lane];
   const int i = r / A.G;
   if (i >= sq.count) l = 0.f;
+  if (stuck) l = NAN;
   const int64_t to = ((int64_t)b * A.W + i) * (A.c.H * A.G) + h * A.G + (r - i * A.G);
   const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
