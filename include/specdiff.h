@@ -573,8 +573,8 @@ int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int6
  * queries, if given) on the way.  Pair i, 0 <= i < rot / 2, of a head's elements (a, b) = (i, i + rot / 2)
  * (halves = 1) or (2 i, 2 i + 1) (halves = 0) becomes
  *   (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos freqs[i];
- * elements from rot on stay.  freqs [rot / 2] float64, radians a position (the angle's error is that of freqs[i] /
- * 2 pi in 64 bits times pos: positions need no small range; frequencies are finite).  positions [B, W] int32, or NULL: lengths[b] + i.
+ * elements from rot on stay.  freqs [rot / 2] float64, finite, of either sign, radians a position (the angle is within pos (2^-52
+ * |freqs[i]| + 2^-61) of the exact one: positions need no small range).  positions [B, W] int32, or NULL: lengths[b] + i.
  * Keys are turned in fp32 and rounded once, to their codes.  q [B, W, Hq, D] and q_out (`dtype`) have strides of
  * their own, 0 <= Hq D <= 2^27; q_out may be q, with its strides.  Queries i >= counts[b] become 0.  q and q_out may both be NULL.
  * 2 <= rot <= D, even.  The rest as in sdv_cache_append.

@@ -4,8 +4,9 @@
 // Pair i of a head's first `rot` elements is a plane, turned by pos f_i radians:
 //   (x_a, x_b) -> (x_a cos - x_b sin, x_b cos + x_a sin).
 // The angle is had modulo a turn without a large argument: t_i = f_i / 2 pi mod 1 as a 64-bit fraction, and pos t_i
-// modulo 2^64 is the fraction of a turn, within pos 2^-53 f_i / 2 pi (f_i's own bits).  Its nearest quarter turn is taken
-// off as an integer, so that sine and cosine see an eighth of a turn at most.
+// modulo 2^64 is the fraction of a turn, within pos (2^-52 |f_i| / 2 pi + 2^-64) turns (1 / 2 pi and the product, both rounded to
+// 53 bits; the fraction cut off).  Its nearest quarter turn is taken off as an integer, so that sine and cosine see an eighth of a
+// turn at most, in steps of 2^-32.
 //
 // Codes and scales are those of sdv_cache_append for the turned keys, rounded once, from fp32.
 #include "sdv_codes.cuh"
@@ -57,8 +58,9 @@ __device__ __forceinline__ float2 turned(uint64_t turn, int pos) {
   return make_float2(quarter == 1 || quarter == 2 ? -a : a, quarter & 2 ? -b : b);
 }
 __device__ __forceinline__ uint64_t turn_of(double f) {
-  const double t = f * 0.15915494309189533577;      // 1 / 2 pi
-  return (uint64_t)((t - floor(t)) * 0x1p64);
+  const double t = fabs(f) * 0.15915494309189533577;             // 1 / 2 pi
+  const uint64_t turn = (uint64_t)((t - floor(t)) * 0x1p64);     // (exact: of a number above 0, no bits are lost)
+  return f < 0. ? 0 - turn : turn;
 }
 
 // The pairs' turns per position: 64-bit products and a floor, which this machine has few units for, so once a CTA.
