@@ -602,6 +602,8 @@ def _cache_here(cache, *ts):
 def rotary_freqs(rot, base=10000.0, device="cuda"):
     """Radians a position of the pairs of a head's first `rot` elements, base^(-2 i / rot), float64
     [rot / 2], as cache_append_rotary takes them; scaled variants are the caller's own tensor."""
+    if rot < 2 or rot % 2:
+        raise ValueError("rot: an even number of elements expected")
     return float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
 
 

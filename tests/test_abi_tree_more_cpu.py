@@ -12,3 +12,11 @@ def test_row_tiles_refuses_what_the_call_refuses(lib):  # noqa: F811
         args = list(good)
         args[at] = x
         assert B.sdv_tree_attend_row_tiles(*args) == B.SDV_EINVAL, args
+
+
+@pytest.mark.parametrize("rot", [0, 1, 7, -2])
+def test_rotary_freqs_of_no_pairs_are_refused(rot):
+    """An odd rot would give one pair more, of frequencies that no rotation of rot elements has."""
+    from paper_2606_13426_gb300 import api
+    with pytest.raises(ValueError):
+        api.rotary_freqs(rot, device="cpu")
