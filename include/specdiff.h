@@ -576,7 +576,8 @@ int sdv_cache_attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int6
  * elements from rot on stay.  freqs [rot / 2] float64, finite, of either sign, radians a position (the angle is within pos (2^-52
  * |freqs[i]| + 2^-61) of the exact one: positions need no small range).  positions [B, W] int32, or NULL: lengths[b] + i.
  * Keys are turned in fp32 and rounded once, to their codes.  q [B, W, Hq, D] and q_out (`dtype`) have strides of
- * their own, 0 <= Hq D <= 2^27; q_out may be q, with its strides.  Queries i >= counts[b] become 0.  q and q_out may both be NULL.
+ * their own, 0 <= Hq D <= 2^27; q_out may be q, with its strides, and else does not overlap it.  Rows of q_out lie apart (no
+ * stride of 0 along an axis of more than one).  Queries i >= counts[b] become 0.  q and q_out may both be NULL.
  * 2 <= rot <= D, even.  The rest as in sdv_cache_append.
  */
 int sdv_cache_append_rotary(const void *k_new, const void *v_new, int64_t stride_b, int64_t stride_t,

@@ -472,6 +472,8 @@ extern "C" int sdv_cache_append_rotary(const void* k_new, const void* v_new, int
   if (!q != !q_out) return SDV_EINVAL;
   if (q && (Hq < 1 || Hq > (1 << 20) || q_stride_b < 0 || q_stride_t < 0 || q_stride_h < 0 || out_stride_b < 0 || out_stride_t < 0 || out_stride_h < 0))
     return SDV_EINVAL;
+  // (rows that share memory would be written by several threads)
+  if (q && ((B > 1 && !out_stride_b) || (W > 1 && !out_stride_t) || (Hq > 1 && !out_stride_h))) return SDV_EINVAL;
   if (q == q_out && q && (q_stride_b != out_stride_b || q_stride_t != out_stride_t || q_stride_h != out_stride_h)) return SDV_EINVAL;
   const size_t es = elem_bytes(dtype);
   if (!aligned_to(k_new, es) || !aligned_to(v_new, es) || !aligned_to(q, es) || !aligned_to(q_out, es) || !aligned_to(freqs, 8) ||
