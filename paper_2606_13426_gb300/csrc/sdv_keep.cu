@@ -22,7 +22,7 @@ struct KeepArgs {
   int W;
 };
 
-// Sixteen codes that stand for c s, under the scale `to`.
+// Four codes that stand for c s, under the scale `to`.
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float s, float to) {
   float f[4];
 #pragma unroll

@@ -86,7 +86,6 @@ __device__ __forceinline__ void fill_table(float2* table, const uint64_t* turns,
   }
 }
 
-// Sixteen consecutive elements from x on, as fp32.
 // Four elements, two pairs (the second, if it is one).
 __device__ __forceinline__ void turn_neighbours(const float4& c, bool both, float* f) {
   const float a = f[0], b = f[1], x = f[2], y = f[3];
@@ -96,6 +95,7 @@ __device__ __forceinline__ void turn_neighbours(const float4& c, bool both, floa
   f[3] = both ? y * c.z + x * c.w : y;
 }
 
+// Sixteen consecutive elements from x on, as fp32.
 template <int kDtype>
 __device__ __forceinline__ void load16(const typename Num<kDtype>::T* x, bool vec, float* f) {
   using E = Num<kDtype>;
@@ -152,13 +152,12 @@ __device__ __forceinline__ float largest16(const float* f, bool finite) {
   }
   return m;
 }
-static __device__ __noinline__ uint32_t codes4_by(float a, float b, float c, float d, float s) { return codes4(a / s, b / s, c / s, d / s); }
 __device__ __forceinline__ uint4 codes16(const float* f, bool pow2, float inv, float s) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     w[i] = pow2 ? codes4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv)
-                : codes4_by(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], s);
+                : codes4_over(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], s);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -481,7 +480,7 @@ extern "C" int sdv_cache_append_rotary(const void* k_new, const void* v_new, int
     return SDV_EALIGN;
   RotaryArgs A{};
   A.nb = (W + block - 2) / block + 1;
-  // the heads of a CTA: as few as fill the GPU's places twice
+  // the heads of a CTA: as few as keep to kGroupCtas CTAs an SM
   const int64_t pages_most = (int64_t)B * A.nb;
   A.group = 1;
   while (A.group < H && pages_most * ((H + A.group - 1) / A.group) > kGroupCtas * (int64_t)sm_count()) A.group *= 2;

@@ -40,7 +40,6 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity, vol
 }
 // What this thread wrote to shared memory is there for the matrix unit.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // ---- copies of whole vectors of 16 bytes from global to shared memory, which the barrier counts
 __device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {   // an arrival that waits for them
@@ -98,15 +97,8 @@ __device__ __forceinline__ void tmem_loaded16(uint32_t* r) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : SDV_R16(SDV_INOUT, 0)::"memory");
 #undef SDV_INOUT
 }
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
-#define SDV_IN(i) "r"(r[i])
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
-      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
-      SDV_R32(SDV_IN)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
+#define SDV_IN(i) "r"(r[i])
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
       SDV_R16(SDV_IN, 0)
@@ -122,10 +114,8 @@ __device__ __forceinline__ uint32_t swizzled(int row, int piece) { return (uint3
 __device__ __forceinline__ uint64_t tile_desc(uint32_t at) {
   return (uint64_t)(at >> 4 & 0x3fff) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// The instruction's descriptor: fp32 sums of f16 (type 0) or bf16 (1) products, both operands K-major.
-__host__ __device__ constexpr uint32_t mma_desc(int type, int m, int n) {
-  return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
-}
+// The instruction's descriptor: fp32 sums of f16 products, both operands K-major.
+__host__ __device__ constexpr uint32_t mma_desc(int m, int n) { return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24; }
 // One lane of a warp whose lanes are all here.
 __device__ __forceinline__ bool elected() {
   uint32_t yes;

@@ -497,7 +497,7 @@ __device__ __forceinline__ void scores_role(uint8_t* smem, TreeSmall& sm, int st
   int* dead = &sm.dead;
   const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
   const uint64_t q = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kQ), 0)), k = q + (S::kK - S::kQ) / 16;
-  const uint32_t score = mma_desc(0, kTileRows, step);
+  const uint32_t score = mma_desc(kTileRows, step);
   const bool one = elected();
   int t = 0;
 #pragma unroll 1
@@ -540,7 +540,7 @@ __device__ __forceinline__ void out_role(uint8_t* smem, TreeSmall& sm, int step)
   int* dead = &sm.dead;
   const uint32_t base = __shfl_sync(0xffffffffu, sm.tmem, 0);
   const uint64_t v = tile_desc(__shfl_sync(0xffffffffu, smem_addr(smem + S::kV), 0));
-  constexpr uint32_t kOut = mma_desc(0, kTileRows, kD);
+  constexpr uint32_t kOut = mma_desc(kTileRows, kD);
   const int chunks = step / kChunk, half = first_half(chunks);
   const bool one = elected();
   int t = 0;
