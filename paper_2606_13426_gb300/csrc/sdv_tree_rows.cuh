@@ -60,7 +60,8 @@ struct alignas(16) TreeSmall {
   float scales[kScaleRing][3 * kTileChunks];      // of a step's chunks: ks, then kPScale vs, then log2 |vs|
   uint32_t absent[kScaleRing];                    // chunks that are not there; bit 31: an ordinary step (see soft_probs)
   alignas(16) uint32_t nan_keys[kScaleRing][4];               // keys that have NaN among their values
-  float ml[2][4][kTileRows];                      // the groups' references, sums, bases, lags
+  float ml[2][3][kTileRows];                      // the groups' references, sums, bases
+  float* aside;                                   // what the groups have put aside: [group], as put_aside has it
   uint32_t tmem;
   int dead;
 };
@@ -596,7 +597,7 @@ __device__ __forceinline__ uint64_t placed(uint64_t set, int at) {
 }
 
 // A row's running state: its reference base + m (log2; base is 0 unless its scores are past 2^20), and the sum of
-// 2^(score - reference).  lag: log2 of what takes the sums put aside to the reference (not above 0).
+// 2^(score - reference).  lag: log2 of what takes the sums put aside to the reference, not above 0 (put_aside).
 struct SoftRow {
   float m, l, base, lag;
 };
@@ -649,17 +650,86 @@ __device__ __forceinline__ void soft_probs(uint32_t at, const uint32_t* x, int c
 // By how much the reference (m, base) exceeds that of (m0, base0).
 __device__ __forceinline__ float reference_less(float m0, float base0, float m, float base) { return (base - base0) + (m - m0); }
 
-// The sums of a row that goes over to a reference higher by 2^-d.  `before`: where the products that they are of end, or
-// no barrier (a segment's first step).
+// A step, of the CTA and of its segment: where the products of the steps before it end.
 struct Before {
-  uint64_t* bar;
-  uint32_t parity;
-  int* dead;
+  TreeSmall* sm;
+  int t, n;
+  __device__ __forceinline__ bool any() const { return n > 0; }
+  __device__ __forceinline__ bool aside() const { return n > 0 && n % kAside == 0; }       // their sums are put aside
+  __device__ __forceinline__ void wait() const {             // (given up: so does the next wait)
+    warp_wait(&sm->p_free[(t - 1) & 1], (t - 1) >> 1 & 1, &sm->dead);
+    tmem_after_sync();
+  }
 };
+// The matrix unit cuts its sums off instead of rounding them: where the products have one sign, 128 keys more cost 5e-7 of the
+// sum, 1.6e-4 after 250 steps, a third of f16's half step and more with every key.  So what kAside steps have
+// summed in tensor memory goes over into sums that are rounded to nearest, a group's and row's own in the workspace (in L2), and
+// the next product begins from nothing: 3.1e-5 at most, whatever a sequence's length.  2 x 60 nodes of 8 x 8
+// heads over 65000 keys take 374 us with and 362 without it, 32 x 32 of 8 x 4 heads over up to 16000 keys 241 and 236: about 2 us
+// each time, and the code.  Both functions stay out of line, and away from where scores are live: a call from between
+// scores and probabilities spilled them (277 us); the sums read in the epilogue's own loops took 249.
+template <int kD>
+__device__ __forceinline__ float4* aside_of(const TreeSmall& sm) {     // this thread's row and group
+  return reinterpret_cast<float4*>(sm.aside + (threadIdx.x / kTileRows) * TreeShape<kD>::kAsideAt) + threadIdx.x % kTileRows;
+}
+// lag: log2 of what takes the sums put aside to the reference.
+template <int kD>
+__device__ __noinline__ void put_aside(uint32_t out, Before before, float lag) {
+  float4* y = aside_of<kD>(*before.sm);
+  const float by = ex2(.5f * lag);
+  const bool first = before.n == kAside;
+#pragma unroll 1
+  for (int g = 0; g < kD / 64; ++g, y += 16 * kTileRows) {
+    float4 b[16];                                            // (64 numbers of a row on their way at once)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b[e] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : y[e * kTileRows];
+    if (g == 0) before.wait();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t r[16];
+      tmem_load16(out + 64 * g + 16 * c, r);
+      tmem_loaded16(r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = b[4 * c + e];
+        y[(4 * c + e) * kTileRows] = make_float4(scaled(v.x, by) + __uint_as_float(r[4 * e]), scaled(v.y, by) + __uint_as_float(r[4 * e + 1]),
+                                                 scaled(v.z, by) + __uint_as_float(r[4 * e + 2]), scaled(v.w, by) + __uint_as_float(r[4 * e + 3]));
+      }
+    }
+  }
+}
+// At a segment's end: they are added to the last steps' sums in tensor memory.
+template <int kD>
+__device__ __noinline__ void put_back(uint32_t out, const TreeSmall& sm, float lag) {
+  const float4* aside = aside_of<kD>(sm);
+  const float by = ex2(.5f * lag);
+#pragma unroll 1
+  for (int g = 0; g < kD / 32; ++g, aside += 8 * kTileRows) {
+    float4 b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = aside[e * kTileRows];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t r[16];
+      tmem_load16(out + 32 * g + 16 * c, r);
+      tmem_loaded16(r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = b[4 * c + e];
+        r[4 * e] = __float_as_uint(__uint_as_float(r[4 * e]) + scaled(v.x, by));
+        r[4 * e + 1] = __float_as_uint(__uint_as_float(r[4 * e + 1]) + scaled(v.y, by));
+        r[4 * e + 2] = __float_as_uint(__uint_as_float(r[4 * e + 2]) + scaled(v.z, by));
+        r[4 * e + 3] = __float_as_uint(__uint_as_float(r[4 * e + 3]) + scaled(v.w, by));
+      }
+      tmem_store16(out + 32 * g + 16 * c, r);
+    }
+  }
+  tmem_stored();
+}
+// The sums of a row that goes over to a reference higher by 2^-d, half = 2^(d / 2).
 template <int kD>
 __device__ __noinline__ void move_out(uint32_t out, Before before, float half) {
-  warp_wait(before.bar, before.parity, before.dead);        // (given up: so does the next wait)
-  tmem_after_sync();
+  before.wait();
   uint32_t r[16];
 #pragma unroll 1
   for (int g = 0; g < kD / 16; ++g) {
@@ -676,40 +746,7 @@ __device__ __forceinline__ void soft_move(uint32_t out, const Before& before, fl
   const float half = ex2(.5f * d);
   s.l = scaled(s.l, half);
   s.lag += d;
-  if (before.bar) move_out<kD>(out, before, half);
-}
-// The matrix unit cuts its sums off instead of rounding them: where the products have one sign, 128 keys more cost 5e-7 of the
-// sum, 1.6e-4 after 250 steps, a third of f16's half step and more with every key.  So what kAside steps have
-// summed in tensor memory goes over into sums that are rounded to nearest, a group's and row's own in the workspace (in L2), and
-// the next product begins from nothing: 3.1e-5 at most, whatever a sequence's length.  It comes behind a step's probabilities,
-// when the products before are done, and takes about 2 us: 2 x 60 nodes of 8 x 8 heads over 65000 keys 377 us in place of 368 (every
-// 32 steps 382), 32 x 32 of 8 x 4 heads over up to 16000 keys 255 in place of 254 (261).
-template <int kD>
-__device__ __noinline__ void put_aside(uint32_t out, float* aside, int row, Before before, float lag, bool first) {
-  const float half = ex2(.5f * lag);
-  float4* y = reinterpret_cast<float4*>(aside) + row;
-#pragma unroll 1
-  for (int g = 0; g < kD / 64; ++g, y += 16 * kTileRows) {
-    float4 b[16];                                            // (64 numbers of a row on their way at once)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) b[e] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : y[e * kTileRows];
-    if (g == 0) {
-      warp_wait(before.bar, before.parity, before.dead);
-      tmem_after_sync();
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      uint32_t r[16];
-      tmem_load16(out + 64 * g + 16 * c, r);
-      tmem_loaded16(r);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 v = b[4 * c + e];
-        y[(4 * c + e) * kTileRows] = make_float4(scaled(v.x, half) + __uint_as_float(r[4 * e]), scaled(v.y, half) + __uint_as_float(r[4 * e + 1]),
-                                                 scaled(v.z, half) + __uint_as_float(r[4 * e + 2]), scaled(v.w, half) + __uint_as_float(r[4 * e + 3]));
-      }
-    }
-  }
+  if (before.any()) move_out<kD>(out, before, half);
 }
 __device__ __forceinline__ void soft_load(uint32_t at, uint32_t* x) {
   tmem_load32(at, x);
@@ -756,7 +793,7 @@ __device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, 
   }
   top = soft_top(at, chunks, scales, f0, sees, s.base, true);
   const bool move = top > s.m + kSlack;
-  if (__any_sync(0xffffffffu, move)) {
+  if (__any_sync(0xffffffffu, move) ) {
     const float now = move ? top : s.m, d = s.m - now;
     s.m = now;
     soft_move<kD>(out, before, d, s);
@@ -803,7 +840,7 @@ __device__ __forceinline__ void soft_tile(uint32_t at, uint32_t out, int chunks,
   }
   // the reference moves when a score passes it by 2^kSlack
   const bool move = top > s.m + kSlack;
-  if (__any_sync(0xffffffffu, move || s.base != 0.f)) {
+  if (__any_sync(0xffffffffu, move || s.base != 0.f) ) {
     if (__any_sync(0xffffffffu, s.base != 0.f || (move && fabsf(top) > kMostPlain))) {
       s = soft_any<kD>(at, out, chunks, scales, f0, ~0ull, before, s);
       return;
@@ -825,8 +862,6 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
   const uint32_t out = lanes + 2 * kTileKeys;
   const int all = T.a.step / kChunk, chunk0 = s ? first_half(all) : 0, chunks = s ? all - chunk0 : first_half(all);   // this group's
   Meeting meet{&sm.soft, 0};
-  // the groups' sums that are put aside: behind all partials
-  float* aside = A.part + (int64_t)A.ctas * 2 * S::kSlot + (int64_t)blockIdx.x * 2 * S::kAsideAt;
   const int r = rt * T.rows + row, i = r / A.G;
   int t = 0;
 #pragma unroll 1
@@ -869,7 +904,7 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
       const int slot = t & (kScaleRing - 1), key0 = (g.step0 + n) * A.step + chunk0 * kChunk;
       const uint32_t absent = sm.absent[slot], at = lanes + (t & 1) * kTileKeys + chunk0 * kChunk;
       const float* scales = sm.scales[slot] + chunk0;
-      const Before before{n ? &sm.p_free[(t - 1) & 1] : nullptr, (uint32_t)((t - 1) >> 1 & 1), dead};
+      const Before before{&sm, t, n};
       if (absent >> 31 && key0 + chunks * kChunk <= at0 && A.scale2 >= 0.f) {
         if (busy) soft_tile<kD>(at, out + s * 128, chunks, scales, f0, before, mine);
       } else if (busy) {
@@ -877,8 +912,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
         __syncwarp();
         mine = soft_any<kD>(at, out + s * 128, chunks, scales, f0, sees, before, mine);
       }
-      if (busy && n && n % kAside == 0) {                    // (behind the probabilities: the products before are done by now)
-        put_aside<kD>(out + s * 128, aside + s * S::kAsideAt, row, before, mine.lag, n == kAside);
+      if (busy && before.aside()) {                          // (behind the probabilities: the products before are done by now)
+        put_aside<kD>(out + s * 128, before, mine.lag);
         mine.lag = 0.f;
       }
       tmem_before_sync();
@@ -889,11 +924,15 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
     tmem_after_sync();
     if (g.steps > 1) look_for_nan(t - 2, g.steps - 2);
     look_for_nan(t - 1, g.steps - 1);
+    if (busy && g.steps > kAside) {
+      put_back<kD>(out + s * 128, sm, mine.lag);
+      tmem_before_sync();
+    }
     sm.ml[s][0][row] = mine.m;
     sm.ml[s][1][row] = mine.l;
     sm.ml[s][2][row] = mine.base;
-    sm.ml[s][3][row] = mine.lag;
     if (!meet(lane, dead)) return;
+    tmem_after_sync();
     if (busy || (__any_sync(0xffffffffu, have))) {
       const float m0 = sm.ml[0][0][row], m1 = sm.ml[1][0][row], b0 = sm.ml[0][2][row], b1 = sm.ml[1][2][row];
       const float ahead = reference_less(m1, b1, m0, b0);    // of the first group's reference
@@ -902,8 +941,6 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
       const float sum = live ? scaled(sm.ml[0][1][row], c0) + scaled(sm.ml[1][1][row], c1) : 0.f;
       const float by = !g.whole ? 1.f / kPScale : sum == 0.f ? 0.f : 1.f / sum / kPScale;
       const int64_t to = ((int64_t)g.b * A.W + i) * (A.c.H * A.G) + g.h * A.G + (r - i * A.G);
-      const bool more = g.steps > kAside;                    // some sums were put aside
-      const float h0 = ex2(.5f * sm.ml[0][3][row]), h1 = ex2(.5f * sm.ml[1][3][row]);
       float* part = A.part + ((int64_t)(blockIdx.x * 2 + g.slot)) * S::kSlot;
 #pragma unroll 1
       for (int k = 0; k < kD / 64; ++k) {
@@ -913,24 +950,10 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
         if (busy) {
-          if (more) {                                        // what both groups have put aside, on its way at once
-            const float4* x = reinterpret_cast<const float4*>(aside) + (col / 4) * kTileRows + row;
-            float4 v[2][8];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = x[(e >> 3) * (S::kAsideAt / 4) + (e & 7) * kTileRows];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              o[4 * e] = scaled(scaled(v[0][e].x, h0), c0) + scaled(scaled(v[1][e].x, h1), c1);
-              o[4 * e + 1] = scaled(scaled(v[0][e].y, h0), c0) + scaled(scaled(v[1][e].y, h1), c1);
-              o[4 * e + 2] = scaled(scaled(v[0][e].z, h0), c0) + scaled(scaled(v[1][e].z, h1), c1);
-              o[4 * e + 3] = scaled(scaled(v[0][e].w, h0), c0) + scaled(scaled(v[1][e].w, h1), c1);
-            }
-            __syncwarp();
-          }
           tmem_load32(out + col, a);
           tmem_loaded(a);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] += scaled(__uint_as_float(a[e]), c0);
+          for (int e = 0; e < 32; ++e) o[e] = scaled(__uint_as_float(a[e]), c0);
           tmem_load32(out + 128 + col, a);
           tmem_loaded(a);
 #pragma unroll
@@ -1020,6 +1043,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) k_tree_rows(const TreeRowsArg
     barrier_init(&sm.drained, 2);
     barrier_init(&sm.soft, kSoftWarps);
     sm.dead = 0;
+    sm.aside = T.a.part + (int64_t)T.a.ctas * 2 * S::kSlot + (int64_t)blockIdx.x * 2 * S::kAsideAt;      // (behind all partials)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tmem_before_sync();
