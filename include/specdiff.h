@@ -601,7 +601,8 @@ int sdv_tree_attend_row_tiles(int B, int W, int Hq, int H, int D, int block, int
  * sdv_tree_attend - sdv_cache_attend for a tree: the last counts[b] of the lengths[b] tokens in the cache are the
  * nodes, and node i sees the tokens before them, its ancestors and itself.  W at most SDV_MAX_TREE.  Nodes
  * i >= counts[b] get 0 and -inf, as all of a sequence with lengths[b] < counts[b] do (SDV_STATUS_BAD_TREE).
- * As in sdv_cache_attend, a code that is NaN makes NaN of the rows that see it alone. Scores, sums and outputs are fp32;
+ * As in sdv_cache_attend, a code that is NaN makes NaN of the rows that see it alone. Scores, sums and outputs are fp32 (the matrix
+ * unit, which cuts its sums off, sums 8192 keys at most: 2^-15 of them where products have one sign; all else is rounded to nearest);
  * probabilities times their value's scale are rounded to the sum of two f16 (22 bits, or 2^-32 of the row's largest), and
  * bf16 queries go through f16 under a power of two of their row. Value scales outside 2^-100 to 2^119 lose bits.
  * Which kernel runs follows from the sizes and from the tokens that the page table could hold; both keep to this.

@@ -38,7 +38,7 @@ __device__ __forceinline__ float code_max4(uint32_t w) {        // of the magnit
 
 // Bound by latency: length, then page and scales, then the rows, then the writes, one after another.  A row's values stand a byte
 // to a place of `dim`, 32 bytes of DRAM each, so that a moved row of 128 costs 4 KB read and written.  8 sequences x 8 heads,
-// up to 6 rows of 128: 4.4 to 5.5 us, a launch's time; 256 x 8, up to 12, pages of 16: 14 to 16.
+// up to 6 rows of 128: 4.4 to 5.5 us, a launch's time; 256 x 8, up to 12, pages of 16: 14 to 16.5.
 __global__ void __launch_bounds__(kKeepThreads) k_cache_keep(const KeepArgs A) {
   const int b = blockIdx.x / A.c.H, h = blockIdx.x - b * A.c.H, tid = threadIdx.x;
   const int D = A.c.D, T_ = A.c.block, words = D / 4;

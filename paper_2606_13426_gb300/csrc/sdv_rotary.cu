@@ -129,7 +129,8 @@ __device__ __forceinline__ void turn_key(const typename Num<kDtype>::T* x, bool 
       const int at = (e < 16 ? u0 * 16 : u1 * 16 - 16) + e;
       if (at < rot) turn_neighbours(two_pairs(cs, at / 2), at + 2 < rot, f + e);
     }
-  } else {                               // halves that end inside a sixteen: the other half is read again
+  } else {                               // halves that end inside a sixteen: the other half is read again, element by element
+    // (4 x 8000 tokens of 8 key heads of 128, keys alone: 113 to 134 us for 16 and 48 turned elements, 68 for 64)
     const int half = rot / 2;
 #pragma unroll
     for (int e = 0; e < 32; ++e) {

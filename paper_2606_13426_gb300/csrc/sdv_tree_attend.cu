@@ -6,7 +6,8 @@ namespace sdv {
 constexpr int kTileRowsMost = 128;          // rows of a tile of the matrix unit's kernels
 
 // The time of a call of those kernels, in tenths of a microsecond, as choose_tiles has it for the others: a fixed part, the
-// steps of a team and the items that it begins or ends.  Fitted to 60 shapes of 20 to 256 rows; both kernels (us), heads of 128,
+// steps of a team and the items that it begins or ends.  Fitted to 60 shapes of 20 to 256 rows whose page tables are as wide as their
+// sequences (the lengths are on the device: a wider table counts as long sequences); both kernels (us), heads of 128,
 // 8 key heads: 64 rows over 1 x 3000 keys 22 and 29 here, 8 x 1000 37 and 28, 32 x 600 77 and 53, 32 x 3000 164 and 101,
 // 128 x 200 155 and 116; 20 rows over 32 x 3000 79 and 100, 48 rows 130 and 101; heads of 64: 64 rows over 32 x 3000 105 and 88,
 // 32 rows 67 and 70.

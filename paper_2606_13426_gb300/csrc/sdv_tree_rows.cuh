@@ -778,7 +778,8 @@ static __device__ __noinline__ float soft_top(uint32_t at, int chunks, const flo
 // without a number NaN; and the score is rounded before the reference is taken off: the fused product is off by half a step of
 // the reference, which large scores make a large power.
 // (This code runs once or twice a segment, and so from a cold instruction cache: short loops.  With its loops unrolled such a
-// step took 7 us.)
+// step took 7 us.  Where every step takes it, with key scales below 0 or a scale below 0, 32 x 32 nodes of 8 x 4 heads over 8000 keys
+// take 363 us in place of 204, 2 x 64 of 8 x 8 over 65000 688 in place of 356.)
 template <int kD>
 __device__ __noinline__ SoftRow soft_any(uint32_t at, uint32_t out, int chunks, const float* scales, float f0, uint64_t sees, Before before,
                                          SoftRow s) {
@@ -997,8 +998,8 @@ __device__ __forceinline__ void soft_role(const TreeRowsArgs& T, uint8_t* smem, 
 // A step of 128 keys and 128 rows of 128 takes about 1.45 us.  What bounds it is shared memory: codes in (32 KB), operands out
 // and in (128 KB), and read again by the products (96 KB) are 2048 cycles at 128 bytes a cycle, 1.07 us.  The products alone take
 // 1540 cycles (a third of them for the second half of the probabilities), the exponentials of both groups 1680, HBM's pace 1390.
-// 32 x 32 nodes of 8 x 4 heads over up to 16000 keys 217 to 239 us by their lengths, 2.6 to
-// 2.8 TB/s; 2 x 60 of 8 x 8 heads over up to 65000 360 us, 707
+// 32 x 32 nodes of 8 x 4 heads over up to 16000 keys 234 to 244 us by their lengths, 2.5
+// TB/s; 2 x 60 of 8 x 8 heads over up to 65000 371 us, 690
 // TFLOP/s; k_attend on mma.sync takes 781 and 1124.  Tried without gain: one issuing warp for both products, groups that take
 // every other step, scores in two halves of 64 keys (1.84 us a step), codes read by the widening warps themselves.
 template <int kD>

@@ -102,7 +102,7 @@ __device__ __forceinline__ void read_two(const Row<kDtype>& Q, const Row<kDtype>
 // Bound by latency: a node is a read of its rows' parts, a barrier for their statistics, and with each rejection that leaves
 // children a pass and a barrier more.  From cold rows: about 9 us for a root without children and its draw, 4 for each node
 // (5.4 before both rows were read at once and the children's asked for ahead), 1 to 2 for a rejection.  1 x 16 x 32768 bf16: 13 us
-// with one node taken, 25 with four; 16 x 32 x 131072 42; 48 x 24 x 50001 fp32, children chosen, 26.
+// with one node taken, 25 with four; 16 x 32 x 131072 42 to 53 by their paths; 48 x 24 x 50001 fp32, children chosen, 26.
 template <int kDtype, bool kDrawn>
 __global__ void __launch_bounds__(kVerThreads, 3) k_tree_verify(const TreeVerifyArgs A) {
   using E = Num<kDtype>;
